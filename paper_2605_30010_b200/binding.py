@@ -29,7 +29,12 @@ EXPORTS = ["et_encoder_create", "et_encode_video", "et_encode_batch", "et_encode
            "et_attention_scores", "et_layernorm",
            # include/earlytom_llm.h
            "et_llm_create", "et_llm_prefill", "et_llm_destroy", "et_llm_last_error", "et_llm_profile_enable",
-           "et_llm_profile_read", "et_rmsnorm", "et_rope", "et_swiglu", "et_attention_causal"]
+           "et_llm_profile_read", "et_rmsnorm", "et_rope", "et_swiglu", "et_attention_causal",
+           # include/earlytom_decode.h
+           "et_kv_append", "et_kv_read", "et_attention_paged", "et_linear_rows"]
+ET_KV_BF16, ET_KV_E4M3 = 0, 1
+ET_PAGED_CAPACITY, ET_PAGED_BAD_PAGE = 3, 5        # values of a paged call's status word
+ET_PAGED_WORKSPACE = 4 << 20
 
 
 class EarlyTomError(RuntimeError):
@@ -124,6 +129,11 @@ class et_llm_profile(C.Structure):
     _fields_ = [("ms", C.c_double * ET_LLM_CATS), ("launches", C.c_ulonglong * ET_LLM_CATS), ("calls", C.c_int)]
 
 
+class et_kv_cache(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scale", C.c_void_p), ("n_pages", C.c_int), ("kv_heads", C.c_int), ("page_size", C.c_int),
+                ("head_dim", C.c_int), ("format", C.c_int)]
+
+
 def load_library(path: str = _LIB_PATH) -> C.CDLL:
     if not os.path.exists(path):
         raise ImportError(f"{path} is missing: build it with `python -m paper_2605_30010_b200.build` "
@@ -176,6 +186,11 @@ def load_library(path: str = _LIB_PATH) -> C.CDLL:
     lib.et_rope.argtypes = [vp, i, i, i, i, i, f, vp]
     lib.et_swiglu.argtypes = [vp, vp, i, i, vp]
     lib.et_attention_causal.argtypes = [vp, vp, i, i, i, i, i, vp, vp]
+    ll, kv = C.c_longlong, C.POINTER(et_kv_cache)
+    lib.et_kv_append.argtypes = [kv, vp, ll, i, i, vp, i, i, vp, vp, f, vp, vp, vp, vp]
+    lib.et_kv_read.argtypes = [kv, vp, ll, i, vp, i, i, vp, vp, vp, vp]
+    lib.et_attention_paged.argtypes = [kv, vp, ll, vp, vp, i, i, vp, i, vp, vp, C.c_size_t, vp, vp]
+    lib.et_linear_rows.argtypes = [vp, vp, vp, vp, i, i, i, i, i, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name.startswith("et_") and name not in ("et_destroy", "et_status_string", "et_last_error",
@@ -757,3 +772,141 @@ def et_attention_causal(qkv, n_seq, L, heads, kv_heads, head_dim, stream=None):
     _check(lib().et_attention_causal(_ptr(qkv), _ptr(out), n_seq, L, heads, kv_heads, head_dim, _ptr(status),
                                      _stream_ptr(stream)))
     return out, status
+
+
+# --------------------------------------------------------------------------------------------
+# The decode step (include/earlytom_decode.h)
+# --------------------------------------------------------------------------------------------
+
+def _need(ok, what: str):
+    if not ok:
+        raise EarlyTomError(1, what)
+
+
+def _on_device(*tensors):
+    """The library launches on the current device: every tensor has to live there."""
+    import torch
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        _need(t is None or (t.is_cuda and t.get_device() == dev), "tensors must be on the current CUDA device")
+
+
+def _int32(t, n, what):
+    import torch
+    _need(t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n), f"{what}: contiguous int32 [{n}]")
+
+
+def _rows(t, rows, width, what):
+    """bf16 [rows, >= width] with contiguous columns; its row stride in elements."""
+    import torch
+    _need(t.dtype == torch.bfloat16 and t.dim() == 2 and t.shape[0] == rows and t.shape[1] >= width
+          and (t.shape[1] == 1 or t.stride(1) == 1), f"{what}: bf16 [{rows}, >= {width}] with contiguous columns")
+    return t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
+
+
+def _kv_cache(cache, scale):
+    """cache [n_pages, 2, kv_heads, page_size, head_dim] bf16 or e4m3 (scale uint8 [n_pages, 2, kv_heads, page_size])."""
+    import torch
+    _need(cache.dim() == 5 and cache.shape[1] == 2 and cache.is_contiguous(), "cache: contiguous [n_pages, 2, kv_heads, page_size, head_dim]")
+    e4m3 = cache.dtype == torch.float8_e4m3fn
+    _need(e4m3 or cache.dtype == torch.bfloat16, "cache: bfloat16 or float8_e4m3fn")
+    _need(e4m3 == (scale is not None), "scale goes with an e4m3 cache, and only with one")
+    if e4m3:
+        _need(scale.dtype == torch.uint8 and scale.is_contiguous() and scale.shape == cache.shape[:4],
+              "scale: contiguous uint8 [n_pages, 2, kv_heads, page_size]")
+    n_pages, _, kv_heads, page_size, head_dim = cache.shape
+    return et_kv_cache(cache.data_ptr(), scale.data_ptr() if e4m3 else None, n_pages, kv_heads, page_size, head_dim,
+                       ET_KV_E4M3 if e4m3 else ET_KV_BF16)
+
+
+def _table(block_table, n_seq=None):
+    import torch
+    _need(block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.is_contiguous()
+          and (n_seq is None or block_table.shape[0] == n_seq), "block_table: contiguous int32 [n_seq, max_pages]")
+    return block_table.shape
+
+
+def et_kv_append(cache, scale, qkv, heads, block_table, start, row_offsets=None, theta=0.0, q_out=None, new_len=None,
+                 status=None, stream=None):
+    """Stores the keys and values of qkv's rows (bf16 [rows, (heads + 2*kv_heads)*head_dim]); returns the turned queries
+    (q_out, created if theta > 0 and heads > 0 and none is given), None without rotation."""
+    import torch
+    c = _kv_cache(cache, scale)
+    n_seq, max_pages = _table(block_table)
+    rows = qkv.shape[0]
+    _on_device(cache, scale, qkv, block_table, start, row_offsets, q_out, new_len, status)
+    stride = _rows(qkv, rows, (heads + 2 * c.kv_heads) * c.head_dim, "qkv")
+    _int32(start, n_seq, "start")
+    _int32(row_offsets, n_seq + 1, "row_offsets")
+    _int32(new_len, n_seq, "new_len")
+    _int32(status, 1, "status")
+    if q_out is None and theta != 0 and heads > 0:
+        q_out = torch.empty((rows, heads * c.head_dim), dtype=torch.bfloat16, device=qkv.device)
+    _need(q_out is None or (q_out.dtype == torch.bfloat16 and q_out.is_contiguous() and q_out.numel() == rows * heads * c.head_dim),
+          "q_out: contiguous bf16 [rows, heads * head_dim]")
+    _check(lib().et_kv_append(C.byref(c), _ptr(qkv), stride, rows, heads, _ptr(block_table), n_seq, max_pages, _ptr(row_offsets),
+                              _ptr(start), float(theta), _ptr(q_out), _ptr(new_len), _ptr(status), _stream_ptr(stream)))
+    return q_out
+
+
+def et_kv_read(cache, scale, block_table, start, rows, row_offsets=None, out=None, status=None, stream=None):
+    """Rows of the cache as bf16 [rows, 2*kv_heads*head_dim] = [keys | values]; rows that no sequence has are left as out has
+    them (zeros where out is created here)."""
+    import torch
+    c = _kv_cache(cache, scale)
+    n_seq, max_pages = _table(block_table)
+    width = 2 * c.kv_heads * c.head_dim
+    if out is None:
+        out = torch.zeros((rows, width), dtype=torch.bfloat16, device=cache.device)
+    _on_device(cache, scale, block_table, start, row_offsets, out, status)
+    stride = _rows(out, rows, width, "out")
+    _int32(start, n_seq, "start")
+    _int32(row_offsets, n_seq + 1, "row_offsets")
+    _int32(status, 1, "status")
+    _check(lib().et_kv_read(C.byref(c), _ptr(out), stride, rows, _ptr(block_table), n_seq, max_pages, _ptr(row_offsets), _ptr(start),
+                            _ptr(status), _stream_ptr(stream)))
+    return out
+
+
+def et_attention_paged(q, heads, cache, scale, block_table, lens, out=None, lse=None, workspace=None, status=None, stream=None):
+    """q bf16 [n_seq, >= heads*head_dim]; returns out bf16 [n_seq, heads*head_dim].  lse (fp32 [n_seq, heads]) is filled if
+    given; workspace: uint8 [ET_PAGED_WORKSPACE], created if none is given."""
+    import torch
+    c = _kv_cache(cache, scale)
+    n_seq, max_pages = _table(block_table, q.shape[0])
+    width = heads * c.head_dim
+    stride = _rows(q, n_seq, width, "q")
+    if out is None:
+        out = torch.empty((n_seq, width), dtype=torch.bfloat16, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(ET_PAGED_WORKSPACE, dtype=torch.uint8, device=q.device)
+    _on_device(q, cache, scale, block_table, lens, out, lse, workspace, status)
+    _need(out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == n_seq * width, "out: contiguous bf16 [n_seq, heads * head_dim]")
+    _need(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == n_seq * heads),
+          "lse: contiguous float32 [n_seq, heads]")
+    _need(workspace.is_contiguous(), "workspace: contiguous")
+    _int32(lens, n_seq, "lens")
+    _int32(status, 1, "status")
+    _check(lib().et_attention_paged(C.byref(c), _ptr(q), stride, _ptr(out), _ptr(lse), n_seq, heads, _ptr(block_table), max_pages,
+                                    _ptr(lens), _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(status),
+                                    _stream_ptr(stream)))
+    return out
+
+
+def et_linear_rows(a, w, bias=None, epilogue=0, gelu_tanh=1, c=None, stream=None):
+    """a [M <= 32, K] bf16, w [N, K] bf16, bias [N] f32 or None.  Returns c (bf16; fp32, added to in place, with epilogue 2)."""
+    import torch
+    M, K = a.shape
+    N = w.shape[0]
+    outs = N // 2 if epilogue == 4 else N
+    dtype = torch.float32 if epilogue == 2 else torch.bfloat16
+    if c is None:
+        _need(epilogue != 2, "epilogue 2 adds to c")
+        c = torch.empty((M, outs), dtype=dtype, device=a.device)
+    _on_device(a, w, bias, c)
+    _need(a.dtype == torch.bfloat16 and a.is_contiguous(), "a: contiguous bf16 [M, K]")
+    _need(w.dtype == torch.bfloat16 and w.is_contiguous() and w.dim() == 2 and w.shape[1] == K, "w: contiguous bf16 [N, K]")
+    _need(bias is None or (bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == N), "bias: contiguous float32 [N]")
+    _need(c.dtype == dtype and c.is_contiguous() and c.numel() == M * outs, f"c: contiguous {dtype} [M, {outs}]")
+    _check(lib().et_linear_rows(_ptr(a), _ptr(w), _ptr(bias), _ptr(c), M, N, K, int(epilogue), int(gelu_tanh), _stream_ptr(stream)))
+    return c

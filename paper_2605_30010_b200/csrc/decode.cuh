@@ -1,0 +1,65 @@
+// Internal declarations of the decode step's operators (kv_cache.cu, attention_paged.cu, linear_rows.cu, decode.cu).
+#pragma once
+
+#include "common.cuh"
+#include "earlytom_decode.h"
+
+namespace et {
+
+// A checked et_kv_cache: sizes as shifts where they are powers of two.
+struct PagedCache {
+  uint8_t* data;
+  uint8_t* scale;        // NULL: bf16
+  int n_pages, kv_heads, page_shift, head_dim;
+};
+
+// The rows of a call and the pages that they go to.
+struct PagedRows {
+  const int* table;      // [n_seq][max_pages]
+  const int* offsets;    // [n_seq + 1] or NULL: row r is sequence r
+  const int* start;      // [n_seq]
+  int rows, n_seq, max_pages;
+  int* status;           // may be NULL
+};
+
+struct RopeTurns { unsigned long long f[64]; };   // theta^(-2i/dh) / (2 pi) as a fraction of 2^64
+
+void launch_kv_append(const PagedCache& c, const PagedRows& r, const bf16* qkv, long long row_stride, int heads, bool rotate,
+                      const RopeTurns& turns, bf16* q_out, int* new_len, cudaStream_t s);
+void launch_kv_read(const PagedCache& c, const PagedRows& r, bf16* out, long long row_stride, cudaStream_t s);
+
+struct PagedAttention {
+  const bf16* q;
+  long long q_stride;
+  bf16* out;
+  float* lse;            // may be NULL
+  int n_seq, heads, max_pages;
+  const int* table;
+  const int* len;
+  float* workspace;
+  int* status;           // may be NULL
+};
+cudaError_t launch_attention_paged(const PagedCache& c, const PagedAttention& a, cudaStream_t s);
+
+// c = epi(a[M][K] * w[N][K]^T + bias), M <= LINEAR_ROWS_MAX
+constexpr int LINEAR_ROWS_MAX = 32;
+cudaError_t launch_linear_rows(const bf16* a, const bf16* w, const float* bias, void* c, int M, int N, int K, int epilogue,
+                               int gelu_tanh, cudaStream_t s);
+
+// Place of a position of sequence s; false (with the status) if it has none.
+__device__ __forceinline__ bool paged_place(const PagedCache& c, const int* table, int max_pages, int s, long long pos, int* status,
+                                            int& page, int& place) {
+  if ((pos >> c.page_shift) >= max_pages) {
+    if (status) atomicMax(status, (int)ET_PAGED_CAPACITY);
+    return false;
+  }
+  page = __ldg(table + (size_t)s * max_pages + (pos >> c.page_shift));
+  place = (int)(pos & ((1 << c.page_shift) - 1));
+  if ((unsigned)page >= (unsigned)c.n_pages) {
+    if (status) atomicMax(status, (int)ET_PAGED_BAD_PAGE);
+    return false;
+  }
+  return true;
+}
+
+}  // namespace et

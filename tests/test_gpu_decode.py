@@ -1,0 +1,670 @@
+"""The decode step's operators (include/earlytom_decode.h) against plain implementations in 64 bits: the paged cache (append,
+read), attention over it and the dense layer for few rows; then all of them together as one decode step of a model.
+
+Tolerances count roundings: a value rounded to bf16 is off by at most 2^-8 of it, to e4m3 by 2^-4 (or half the smallest step);
+fp32 sums of n terms by n * 2^-23 of the sum of magnitudes (the tensor cores may truncate where fp32 addition rounds)."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+BF16, E4M3_HALF = 2.0 ** -8, 2.0 ** -4
+
+
+@pytest.fixture(scope="module")
+def B():
+    import torch
+    assert torch.cuda.is_available()
+    from paper_2605_30010_b200 import binding
+    return binding
+
+
+# ---- plain implementations (numpy, 64 bits) ---------------------------------------------------------------------------
+
+def code_values():
+    got = np.empty(256)
+    for c in range(256):
+        e, m = (c >> 3) & 15, c & 7
+        got[c] = (-1.0 if c & 128 else 1.0) * (math.nan if c & 127 == 127 else m / 8 * 2.0 ** -6 if e == 0 else (1 + m / 8) * 2.0 ** (e - 7))
+    return got
+
+
+CODES = code_values()
+
+
+def e4m3_rows(x):
+    """x [..., d] in 64 bits -> (codes as values, exponents): the smallest e with max|x| <= 448 * 2^e, then nearest, ties to even."""
+    fin = np.where(np.isfinite(x), np.abs(x), 0.0)
+    top = fin.max(-1)
+    m, ex = np.frexp(top)
+    e = np.where(top > 0, ex - 9 + (m > 0.875), -127)
+    e = np.clip(e, -127, 127)
+    y = np.where(np.isfinite(x), x, np.nan) * np.ldexp(1.0, -e)[..., None]
+    step = np.ldexp(1.0, np.maximum(np.frexp(np.abs(np.where(np.isnan(y), 1.0, y)))[1] - 1, -6) - 3)
+    return np.round(y / step) * step, e
+
+
+def rotate(x, pos, theta):
+    """x [rows][heads][d], pos [rows]: rotate-half."""
+    half = x.shape[-1] // 2
+    ang = pos[:, None].astype(np.float64) * float(theta) ** (-np.arange(half) / half)
+    c, s = np.cos(ang)[:, None], np.sin(ang)[:, None]
+    a, b = x[..., :half], x[..., half:]
+    return np.concatenate([a * c - b * s, b * c + a * s], -1)
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def bf16(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).cuda().to(torch.bfloat16)
+
+
+def i32(a):
+    import torch
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")
+
+
+class Cache:
+    """A paged cache with every byte of it set to something, and a table of distinct pages for n_seq sequences."""
+
+    def __init__(self, rng, n_seq, max_pages, kv_heads, page, d, e4m3, spare=3):
+        import torch
+        self.page, self.kv_heads, self.d, self.e4m3 = page, kv_heads, d, e4m3
+        self.n_pages = n_seq * max_pages + spare
+        shape = (self.n_pages, 2, kv_heads, page, d)
+        x = rng.standard_normal(shape) * np.exp2(rng.integers(-3, 4, shape[:-1]))[..., None]
+        if e4m3:
+            v, e = e4m3_rows(x)
+            self.data = torch.from_numpy(v.astype(np.float32)).cuda().to(torch.float8_e4m3fn)
+            self.scale = torch.from_numpy((e + 127).astype(np.uint8)).cuda()
+        else:
+            self.data, self.scale = bf16(x), None
+        self.table = i32(rng.permutation(self.n_pages)[:n_seq * max_pages].reshape(n_seq, max_pages))
+
+    def bytes(self):
+        import torch
+        return self.data.view(torch.uint8 if self.e4m3 else torch.int16).clone(), None if self.scale is None else self.scale.clone()
+
+    def values(self):
+        import torch
+        if not self.e4m3:
+            return f64(self.data)
+        return CODES[self.data.view(torch.uint8).cpu().numpy()] * np.ldexp(1.0, self.scale.cpu().numpy().astype(int) - 127)[..., None]
+
+    def rows(self, s, first, n, values=None):
+        """[2][kv_heads][n][d] of sequence s."""
+        values = self.values() if values is None else values
+        pos = np.arange(first, first + n)
+        pages = self.table.cpu().numpy()[s][pos // self.page]
+        return values[pages, :, :, pos % self.page].transpose(1, 2, 0, 3)
+
+
+# ---- append and read --------------------------------------------------------------------------------------------------
+
+APPENDS = [
+    # rows of each sequence, start of each, heads, kv_heads, page, d, theta
+    ([1], [0], 4, 2, 16, 64, 1e4),
+    ([1], [7675], 28, 4, 64, 128, 1e6),
+    ([1, 1, 1, 1, 1], [0, 15, 16, 31, 100], 7, 1, 16, 128, 1e6),
+    ([37, 1, 0, 64, 129], [0, 63, 5, 1, 127], 6, 2, 32, 128, 5e5),
+    ([200], [3], 0, 4, 128, 128, 0.0),
+    ([5, 300, 17], [1000, 0, 2], 0, 3, 16, 64, 0.0),
+    ([2, 3], [10, 20], 5, 5, 64, 64, 0.0),
+]
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("case", range(len(APPENDS)))
+def test_append_then_read(B, case, e4m3):
+    import torch
+    counts, starts, heads, kvh, page, d, theta = APPENDS[case]
+    rng = np.random.default_rng(case)
+    n_seq, rows = len(counts), sum(counts)
+    max_pages = max((s + n + page - 1) // page for s, n in zip(starts, counts)) + 1
+    c = Cache(rng, n_seq, max_pages, kvh, page, d, e4m3)
+    data0, scale0 = c.bytes()
+    pad, extra = 3, 16                                # rows behind the last sequence; columns that belong to something else
+    x = rng.standard_normal((rows + pad, (heads + 2 * kvh) * d)) * np.exp2(rng.integers(-6, 7, (rows + pad, 1)))
+    wide = torch.full((rows + pad, x.shape[1] + extra), math.nan, dtype=torch.bfloat16, device="cuda")
+    wide[:, :x.shape[1]] = bf16(x)
+    qkv = wide[:, :x.shape[1]]
+    x = f64(qkv).reshape(rows + pad, heads + 2 * kvh, d)
+    one_each = counts == [1] * n_seq
+    offsets = None if one_each else i32(np.concatenate([[0], np.cumsum(counts)]))
+    if one_each:
+        qkv, pad = qkv[:rows], 0
+    status, new_len = i32([0]), i32([-9] * n_seq)
+    q_out = torch.full((rows + pad, heads * d), 7.0, dtype=torch.bfloat16, device="cuda") if theta and heads else None
+    before = qkv.clone()
+    B.et_kv_append(c.data, c.scale, qkv, heads, c.table, i32(starts), offsets, theta, q_out, new_len, status)
+    torch.cuda.synchronize()
+    assert status.item() == 0
+    assert new_len.tolist() == [s + n for s, n in zip(starts, counts)]
+    assert torch.equal(before, qkv)
+    pos = np.concatenate([np.arange(s, s + n) for s, n in zip(starts, counts)])
+    seq = np.repeat(np.arange(n_seq), counts)
+    k, v, q = x[:rows, heads:heads + kvh], x[:rows, heads + kvh:], x[:rows, :heads]
+    # a turned value is off by the fp32 roundings of two products, their factors and the angle, and by its own rounding
+    def slack(z):
+        return 2.0 ** -20 * (np.abs(z) + np.abs(np.roll(z, d // 2, -1)))
+    ks = np.zeros_like(k)
+    if theta:
+        ks, qs = slack(k), slack(q)
+        k, q = rotate(k, pos, theta), rotate(q, pos, theta)
+        if heads:
+            got = f64(q_out[:rows]).reshape(q.shape)
+            assert (np.abs(got - q) <= BF16 * np.abs(q) + qs).all()
+            assert (q_out[rows:] == 7.0).all()
+    want = np.stack([k, v], 1)                                                  # [rows][2][kvh][d]
+    places = c.table.cpu().numpy()[seq, pos // page], pos % page
+    got = c.values()[places[0], :, :, places[1]]
+    if not e4m3:
+        tol = BF16 * np.abs(want)
+        tol[:, 0] += ks
+        if not theta:
+            assert np.array_equal(got, want)
+        assert (np.abs(got - want) <= tol).all()
+    else:
+        exp = c.scale.cpu().numpy().astype(int)[places[0], :, :, places[1]] - 127
+        vals, e = e4m3_rows(want)
+        sure = slice(1, 2) if theta else slice(0, 2)                            # planes that no fp32 rounding touched
+        assert np.array_equal(exp[:, sure], e[:, sure])
+        assert np.array_equal(got[:, sure], (vals * np.ldexp(1.0, e)[..., None])[:, sure])
+        top = np.abs(want).max(-1)
+        assert (top <= 448 * np.ldexp(1.0, exp) * (1 + 2.0 ** -18)).all() and (top > 224 * np.ldexp(1.0, exp) * (1 - 2.0 ** -18)).all()
+        assert (np.abs(got - want)[:, 0] <= E4M3_HALF * np.abs(want[:, 0]) + np.ldexp(2.0 ** -10, exp)[:, 0, :, None] + 2 * ks).all()
+    # nothing else was written
+    data1, scale1 = c.bytes()
+    touched = torch.zeros((c.n_pages, page), dtype=torch.bool, device="cuda")
+    touched[torch.from_numpy(places[0]).cuda().long(), torch.from_numpy(places[1]).cuda().long()] = True
+    keep = ~touched[:, None, None, :].expand(c.n_pages, 2, kvh, page)
+    assert torch.equal(data0[keep], data1[keep])
+    if e4m3:
+        assert torch.equal(scale0[keep], scale1[keep])
+    # and the rows come back as they are stored
+    out = torch.full((rows + pad, 2 * kvh * d + 8), 5.0, dtype=torch.bfloat16, device="cuda")
+    B.et_kv_read(c.data, c.scale, c.table, i32(starts), rows + pad, offsets, out[:, :2 * kvh * d], status)
+    torch.cuda.synchronize()
+    assert np.array_equal(f64(out[:rows, :2 * kvh * d]), got.reshape(rows, -1))
+    assert (out[rows:] == 5.0).all() and (out[:, 2 * kvh * d:] == 5.0).all() and status.item() == 0
+
+
+def test_e4m3_conversion_edges(B):
+    """Ties, the border between two exponents, the smallest and largest rows, zeros, NaN and infinities."""
+    import torch
+    d, kvh, page = 64, 1, 16
+    rng = np.random.default_rng(5)
+    rows = [np.zeros(d), np.full(d, 448.0), np.full(d, 450.0), np.full(d, 447.0), np.full(d, -448.0 * 2.0 ** 30), np.full(d, 2.0 ** -133),
+            np.full(d, 2.0 ** 127 * 1.75), np.linspace(-1, 1, d), np.r_[448.0, np.arange(d - 1) / 8 + 1 / 16],
+            np.r_[448.0, (np.arange(d - 1) - 20) * 2.0 ** -10], np.r_[math.nan, np.ones(d - 1)], np.r_[math.inf, -math.inf, np.ones(d - 2) * 3],
+            np.full(d, math.nan), np.r_[math.inf, np.zeros(d - 1)], np.r_[-0.0, np.ones(d - 1)], np.r_[1e-38, np.zeros(d - 1)]]
+    x = np.stack([np.concatenate([r, rng.standard_normal(d)]) for r in rows])
+    c = Cache(rng, 1, 1, kvh, page, d, True)
+    qkv = bf16(x)
+    x = f64(qkv).reshape(len(rows), 2, d)
+    status = i32([0])
+    B.et_kv_append(c.data, c.scale, qkv, 0, c.table, i32([0]), i32([0, len(rows)]), status=status)
+    got = c.rows(0, 0, len(rows))[:, 0].transpose(1, 0, 2)
+    vals, e = e4m3_rows(x)
+    want = vals * np.ldexp(1.0, e)[..., None]
+    assert np.array_equal(got, want, equal_nan=True)
+    assert np.isnan(got[10, 0, 0]) and np.isnan(got[11, 0, :2]).all() and (got[11, 0, 2:] == 3).all()
+    out = B.et_kv_read(c.data, c.scale, c.table, i32([0]), len(rows), i32([0, len(rows)]))
+    back = f64(out).reshape(x.shape)
+    assert np.array_equal(back, f64(bf16(want)), equal_nan=True) and status.item() == 0
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_rows_that_cannot_be_placed_are_skipped(B, e4m3):
+    """Slots not in use, positions behind the table, pages that are not in the cache: skipped and reported, the others land."""
+    import torch
+    rng = np.random.default_rng(9)
+    kvh, page, d, heads = 2, 16, 64, 2
+    c = Cache(rng, 4, 2, kvh, page, d, e4m3)
+    good = c.table.clone()
+    for bad, code in ((c.n_pages, B.ET_PAGED_BAD_PAGE), (-1, B.ET_PAGED_BAD_PAGE), (None, B.ET_PAGED_CAPACITY), ("off", 0)):
+        table, start = good.clone(), [3, 17, 30, 9]
+        if bad is None:
+            start[1] = 32
+        elif bad == "off":
+            start[1] = -1
+        else:
+            table[1, 1] = bad
+        data0, scale0 = c.bytes()
+        qkv, status, new_len = bf16(rng.standard_normal((4, (heads + 2 * kvh) * d))), i32([0]), i32([0] * 4)
+        q = torch.full((4, heads * d), 7.0, dtype=torch.bfloat16, device="cuda")
+        B.et_kv_append(c.data, c.scale, qkv, heads, table, i32(start), theta=1e4, q_out=q, new_len=new_len, status=status)
+        assert status.item() == code
+        assert new_len.tolist() == [4, {None: 32, "off": -1}.get(bad, 18), 31, 10]
+        assert (q[1] == 7.0).all() and not (q[[0, 2, 3]] == 7.0).all(1).any()
+        data1, _ = c.bytes()
+        changed = {tuple(i) for i in (data0 != data1).any(-1).any(2).any(1).nonzero().tolist()}
+        assert changed == {(good[s, start[s] // page].item(), start[s] % page) for s in (0, 2, 3)}
+        out = torch.full((4, 2 * kvh * d), 5.0, dtype=torch.bfloat16, device="cuda")
+        status.zero_()
+        B.et_kv_read(c.data, c.scale, table, i32(start), 4, None, out, status)
+        assert status.item() == code and (out[1] == 5.0).all()
+        for s in (0, 2, 3):
+            assert np.array_equal(f64(out[s]), c.rows(s, start[s], 1).reshape(-1))
+
+
+# ---- attention --------------------------------------------------------------------------------------------------------
+
+def attention_reference(q, k, v):
+    """q [heads][d], k, v [kv_heads][n][d] in 64 bits: (out, lse, sum p|v|, max sum |q||k|)."""
+    heads, d = q.shape
+    group = heads // k.shape[0]
+    k, v = np.repeat(k, group, 0), np.repeat(v, group, 0)
+    s = np.einsum("hd,hnd->hn", q, k) / math.sqrt(d)
+    size = (np.einsum("hd,hnd->hn", np.abs(q), np.abs(k)) / math.sqrt(d)).max(-1)
+    top = s.max(-1, keepdims=True)
+    p = np.exp(s - top)
+    lse = np.log(p.sum(-1)) + top[:, 0]
+    p /= p.sum(-1, keepdims=True)
+    return np.einsum("hn,hnd->hd", p, v), lse, np.einsum("hn,hnd->hd", p, np.abs(v)), size
+
+
+def check_attention(out, lse, q, lens, cache, heads, alive=None, values=None):
+    """Scores of d fp32 products are off by d * 2^-23 of the sum of magnitudes, and the exponentials by as much relatively (plus
+    2^-20 for themselves and their sum); a probability rounded to 11 bits by 2^-11."""
+    d = cache.d
+    values = cache.values() if values is None else values
+    for s, n in enumerate(lens):
+        if n <= 0:
+            assert (out[s] == 0).all() and (lse[s] == -math.inf).all()
+            continue
+        k, v = cache.rows(s, 0, n, values)
+        if alive is not None:
+            k, v = k[:, alive[s][:n]], v[:, alive[s][:n]]
+        want, wl, mass, size = attention_reference(q[s], k, v)
+        drift = d * 2.0 ** -23 * size + 2.0 ** -20
+        got = f64(out[s]).reshape(heads, d)
+        tol = BF16 * np.abs(want) + (2.0 ** -11 + 2 * drift)[:, None] * mass + 1e-30
+        assert (np.abs(got - want) <= tol).all(), f"sequence {s} of {n}: off by {(np.abs(got - want) / tol).max():.3g} of the tolerance"
+        assert (np.abs(f64(lse[s]) - wl) <= drift + 2.0 ** -22 * np.abs(wl)).all()
+
+
+def run_attention(B, q, heads, c, lens, table=None, **kw):
+    import torch
+    n_seq = q.shape[0]
+    out = torch.full((n_seq, heads * c.d), 9.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((n_seq, heads), 9.0, dtype=torch.float32, device="cuda")
+    status = i32([0])
+    B.et_attention_paged(q, heads, c.data, c.scale, c.table if table is None else table, i32(lens), out=out, lse=lse, status=status, **kw)
+    torch.cuda.synchronize()
+    return out, lse, status.item()
+
+
+ATTENTIONS = [
+    # lengths, heads, kv_heads, page
+    ([1], 4, 4, 16),
+    ([61], 28, 4, 16),
+    ([64, 65, 63, 0, 1, 2, 15, 16, 17, 31, 33, 127, 128, 129, -4], 7, 1, 16),
+    ([300, 0, 1023], 10, 2, 32),
+    ([513, 40], 16, 2, 64),
+    ([700, 1], 9, 1, 128),
+    ([257, 256], 23, 1, 64),
+    ([150, 31], 80, 2, 32),
+    ([5000], 28, 4, 64),
+    ([4097, 3, 2000], 8, 8, 128),
+    (list(range(0, 200, 3)), 4, 2, 16),
+]
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("case", range(len(ATTENTIONS)))
+def test_attention(B, case, d, e4m3):
+    lens, heads, kvh, page = ATTENTIONS[case]
+    rng = np.random.default_rng(100 * case + d + e4m3)
+    c = Cache(rng, len(lens), max(1, (max(lens) + page - 1) // page), kvh, page, d, e4m3)
+    q = bf16(rng.standard_normal((len(lens), heads * d)) * 2)
+    out, lse, status = run_attention(B, q, heads, c, lens)
+    assert status == 0
+    check_attention(out, lse, f64(q).reshape(len(lens), heads, d), lens, c, heads)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_attention_peaked_and_far_apart_scores(B, e4m3):
+    """Scores from one key that takes all to thousands apart, growing and falling along the cache; queries of very different
+    sizes; values of very different sizes, the large ones where nothing looks."""
+    rng = np.random.default_rng(77)
+    n, heads, kvh, page, d = 900, 6, 2, 32, 128
+    c = Cache(rng, 2, (n + page - 1) // page, kvh, page, d, e4m3)
+    q = rng.standard_normal((2, heads, d))
+    q *= np.array([1e-6, 0.1, 1.0, 8.0, 40.0, 1000.0])[None, :, None]
+    x = np.empty((2 * n, 2, kvh, d))
+    for s, sign in ((0, 1.0), (1, -1.0)):
+        ramp = sign * np.linspace(-3, 3, n)[:, None, None]
+        x[s * n:(s + 1) * n, 0] = rng.standard_normal((n, kvh, d)) * 0.5 + ramp * rng.standard_normal((1, kvh, d))
+        x[s * n:(s + 1) * n, 1] = rng.standard_normal((n, kvh, d)) * np.exp2(rng.integers(-12, 13, (n, kvh, 1)))
+    B.et_kv_append(c.data, c.scale, bf16(x.reshape(2 * n, -1)), 0, c.table, i32([0, 0]), i32([0, n, 2 * n]))
+    qt = bf16(q.reshape(2, -1))
+    out, lse, status = run_attention(B, qt, heads, c, [n, n - 7])
+    assert status == 0
+    check_attention(out, lse, f64(qt).reshape(2, heads, d), [n, n - 7], c, heads)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_attention_ignores_what_stands_behind_the_length(B, e4m3):
+    """NaN, infinities and the largest numbers behind a sequence's end (in its last page and on the pages after it), and NaN on
+    the pages that no table names, change nothing, bit by bit."""
+    import torch
+    rng = np.random.default_rng(3)
+    lens, heads, kvh, page, d = [1, 17, 64, 130, 0, 79], 14, 2, 32, 128
+    c = Cache(rng, len(lens), 6, kvh, page, d, e4m3)
+    q = bf16(rng.standard_normal((len(lens), heads * d)))
+    a = run_attention(B, q, heads, c, lens)
+    used = torch.zeros((c.n_pages, page), dtype=torch.bool, device="cuda")
+    for s, n in enumerate(lens):
+        for p in range(n):
+            used[c.table[s, p // page].item(), p % page] = True
+    stale = ~used[:, None, None, :].expand(c.n_pages, 2, kvh, page)
+    for fill in (0x7f, 0xff) if e4m3 else (math.nan, math.inf, -3.0e38):
+        if e4m3:
+            c.data.view(torch.uint8)[stale] = fill
+            c.scale[stale] = 254
+        else:
+            c.data[stale] = fill
+        b = run_attention(B, q, heads, c, lens)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and b[2] == 0
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_attention_nan_in_a_live_place_is_seen(B, e4m3):
+    import torch
+    rng = np.random.default_rng(4)
+    lens, heads, kvh, page, d = [100, 100], 4, 2, 16, 64
+    c = Cache(rng, 2, 7, kvh, page, d, e4m3)
+    c.data[c.table[1, 2].item(), 0, 1, 5, 3] = math.nan                        # a key of the second head of sequence 1
+    out, lse, _ = run_attention(B, bf16(rng.standard_normal((2, heads * d))), heads, c, lens)
+    out = out.view(2, kvh, 2, d)
+    assert torch.isfinite(out[0].float()).all() and torch.isfinite(out[1, 0].float()).all()
+    assert torch.isnan(out[1, 1].float()).all() and torch.isnan(lse[1, 2:]).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_attention_over_bad_pages_and_long_lengths(B, e4m3):
+    """Pages that are not in the cache count as absent, lengths behind the table as the table's end; both are reported."""
+    rng = np.random.default_rng(6)
+    heads, kvh, page, d, max_pages = 7, 1, 16, 128, 9
+    c = Cache(rng, 3, max_pages, kvh, page, d, e4m3)
+    q = bf16(rng.standard_normal((3, heads * d)))
+    table, lens = c.table.clone(), [140, 100, 60]
+    table[0, 3], table[0, 8], table[2, 0] = c.n_pages, -7, 2 ** 31 - 1
+    alive = [np.ones(144, dtype=bool) for _ in lens]
+    alive[0][48:64] = alive[0][128:] = alive[2][:16] = False
+    out, lse, status = run_attention(B, q, heads, c, lens, table)
+    assert status == B.ET_PAGED_BAD_PAGE
+    good = f64(q).reshape(3, heads, d)
+    check_attention(out, lse, good, lens, c, heads, alive)
+    out, lse, status = run_attention(B, q, heads, c, [2 ** 31 - 1, 145, 60])
+    assert status == B.ET_PAGED_CAPACITY
+    check_attention(out, lse, good, [144, 144, 60], c, heads)
+    table[1] = -1                                                               # every page of a sequence is bad: an empty row
+    out, lse, status = run_attention(B, q, heads, c, lens, table)
+    assert (out[1] == 0).all() and (lse[1] == -math.inf).all() and status == B.ET_PAGED_BAD_PAGE
+
+
+def test_attention_reads_queries_from_packed_rows(B):
+    import torch
+    rng = np.random.default_rng(8)
+    lens, heads, kvh, page, d = [90, 33, 7], 6, 2, 16, 64
+    c = Cache(rng, 3, 6, kvh, page, d, False)
+    packed = bf16(rng.standard_normal((3, (heads + 2 * kvh) * d)))
+    a = run_attention(B, packed[:, :heads * d], heads, c, lens)
+    b = run_attention(B, packed[:, :heads * d].contiguous(), heads, c, lens)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    out = B.et_attention_paged(packed, heads, c.data, c.scale, c.table, i32(lens))          # no lse, no status, own workspace
+    assert torch.equal(out, a[0])
+
+
+def test_attention_is_reproducible_and_independent_of_its_workspace(B):
+    import torch
+    rng = np.random.default_rng(12)
+    lens, heads, kvh, page, d = [3001, 17, 900, 0, 2500], 28, 4, 64, 128
+    c = Cache(rng, 5, 47, kvh, page, d, True)
+    q = bf16(rng.standard_normal((5, heads * d)))
+    a = run_attention(B, q, heads, c, lens)
+    for fill in (0, 255, 127):
+        ws = torch.full((B.ET_PAGED_WORKSPACE,), fill, dtype=torch.uint8, device="cuda")
+        b = run_attention(B, q, heads, c, lens, workspace=ws)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_attention_in_a_graph_follows_its_inputs(B):
+    """Captured once, replayed with other lengths, tables and queries; beside it, eager calls on another stream with a workspace
+    of their own."""
+    import torch
+    rng = np.random.default_rng(13)
+    n, heads, kvh, page, d = 4, 14, 2, 32, 128
+    c = Cache(rng, n, 60, kvh, page, d, False)
+    q, lens = bf16(rng.standard_normal((n, heads * d))), i32([5, 5, 5, 5])
+    out, lse = torch.empty((n, heads * d), dtype=torch.bfloat16, device="cuda"), torch.empty((n, heads), dtype=torch.float32, device="cuda")
+    ws = torch.empty(B.ET_PAGED_WORKSPACE, dtype=torch.uint8, device="cuda")
+    B.et_attention_paged(q, heads, c.data, None, c.table, lens, out=out, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.et_attention_paged(q, heads, c.data, None, c.table, lens, out=out, lse=lse, workspace=ws)
+    other, results = torch.cuda.Stream(), []
+    values = c.values()
+    for now in ([1900, 0, 64, 3], [1, 1920, 700, 1700]):
+        lens.copy_(i32(now))
+        q.copy_(bf16(rng.standard_normal((n, heads * d))))
+        torch.cuda.synchronize()
+        for _ in range(3):
+            graph.replay()
+            with torch.cuda.stream(other):
+                results.append(B.et_attention_paged(q, heads, c.data, None, c.table, lens, stream=other))
+        torch.cuda.synchronize()
+        check_attention(out, lse, f64(q).reshape(n, heads, d), now, c, heads, values=values)
+        assert all(torch.equal(r, out) for r in results)
+        results.clear()
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_cache_beyond_32_bit_offsets(B, e4m3):
+    """A cache of more than 2^32 bytes: pages at its end are written, read and attended to."""
+    import torch
+    kvh, page, d, heads, n = 8, 128, 128, 16, 300
+    row = 2 * kvh * page * d * (1 if e4m3 else 2)
+    n_pages = (1 << 32) // row + 40
+    data = torch.zeros((n_pages, 2, kvh, page, d), dtype=torch.uint8 if e4m3 else torch.bfloat16, device="cuda")
+    data = data.view(torch.float8_e4m3fn) if e4m3 else data
+    scale = torch.zeros((n_pages, 2, kvh, page), dtype=torch.uint8, device="cuda") if e4m3 else None
+    rng = np.random.default_rng(21)
+    table = i32([[n_pages - 1, n_pages - 20, 1], [2, n_pages - 3, n_pages - 2]])
+    x = bf16(rng.standard_normal((2 * n, 2 * kvh * d)))
+    B.et_kv_append(data, scale, x, 0, table, i32([0, 0]), i32([0, n, 2 * n]))
+    back = B.et_kv_read(data, scale, table, i32([0, 0]), 2 * n, i32([0, n, 2 * n]))
+    if e4m3:
+        vals, e = e4m3_rows(f64(x).reshape(2 * n, 2, kvh, d))
+        want = (vals * np.ldexp(1.0, e)[..., None]).reshape(2 * n, -1)
+    else:
+        want = f64(x)
+    assert np.array_equal(f64(back), want)
+    small = Cache(rng, 2, 3, kvh, page, d, e4m3)                                # the same rows in a small cache give the same bits
+    B.et_kv_append(small.data, small.scale, x, 0, small.table, i32([0, 0]), i32([0, n, 2 * n]))
+    q = bf16(rng.standard_normal((2, heads * d)))
+    a = B.et_attention_paged(q, heads, data, scale, table, i32([n, n - 9]))
+    b = B.et_attention_paged(q, heads, small.data, small.scale, small.table, i32([n, n - 9]))
+    assert torch.equal(a, b)
+
+
+# ---- dense layer for few rows -----------------------------------------------------------------------------------------
+
+def linear_reference(a, w, bias, epilogue, gelu_tanh, c0):
+    """(result, what it may be off) in 64 bits."""
+    y = a @ w.T + bias
+    # K products summed in fp32, at least 16 at a time inside an instruction
+    err = (a.shape[1] / 16 + 32) * 2.0 ** -22 * (np.abs(a) @ np.abs(w).T + np.abs(bias))
+    if epilogue == 2:
+        return c0 + y, err + 2.0 ** -23 * (np.abs(c0) + np.abs(y))
+    if epilogue == 1:
+        if gelu_tanh:
+            z = 0.5 * y * (1 + np.tanh(math.sqrt(2 / math.pi) * (y + 0.044715 * y ** 3)))
+        else:
+            z = 0.5 * y * (1 + np.vectorize(math.erf)(y / math.sqrt(2)))
+        # the slope is at most 1.13; 1 + tanh and 1 + erf are off by 2^-23 where they nearly vanish
+        return z, 1.13 * err + 2.0 ** -21 * np.abs(y) + BF16 * np.abs(z)
+    if epilogue == 4:
+        t, e = y.reshape(y.shape[0], -1, 2, 32), err.reshape(y.shape[0], -1, 2, 32)
+        g, u = t[:, :, 0].reshape(y.shape[0], -1), t[:, :, 1].reshape(y.shape[0], -1)
+        eg, eu = e[:, :, 0].reshape(g.shape), e[:, :, 1].reshape(g.shape)
+        s = g / (1 + np.exp(-g))
+        return s * u, 1.1 * eg * (np.abs(u) + eu) + np.abs(s) * eu + (BF16 + 2.0 ** -20) * np.abs(s * u)
+    return y, err + BF16 * np.abs(y)
+
+
+LINEARS = [(1, 64, 64), (1, 3584, 4608), (3, 8, 5), (7, 520, 1), (8, 1000, 333), (9, 18944, 256), (16, 72, 3584), (17, 1152, 512),
+           (25, 2048, 1000), (32, 3584, 768), (31, 40, 2049), (5, 18944, 3584)]
+
+
+@pytest.mark.parametrize("epilogue,gelu_tanh,with_bias", [(0, 1, True), (0, 1, False), (1, 1, True), (1, 0, True), (2, 1, True), (2, 1, False), (4, 1, True), (4, 1, False)])
+@pytest.mark.parametrize("M,K,N", LINEARS)
+def test_linear_rows(B, M, K, N, epilogue, gelu_tanh, with_bias):
+    import torch
+    if epilogue == 4:
+        N = max(256, N // 256 * 256)
+    rng = np.random.default_rng(M * 1000 + K + N + epilogue)
+    a, w = bf16(rng.standard_normal((M, K))), bf16(rng.standard_normal((N, K)) / math.sqrt(K))
+    bias = rng.standard_normal(N).astype(np.float32) if with_bias else None
+    outs = N // 2 if epilogue == 4 else N
+    c0 = rng.standard_normal((M, outs)).astype(np.float32)
+    guard = torch.full((M * outs + 64,), 3.0, dtype=torch.float32 if epilogue == 2 else torch.bfloat16, device="cuda")
+    c = guard[:M * outs].view(M, outs)
+    if epilogue == 2:
+        c.copy_(torch.from_numpy(c0))
+    B.et_linear_rows(a, w, None if bias is None else torch.from_numpy(bias).cuda(), epilogue, gelu_tanh, c=c)
+    want, tol = linear_reference(f64(a), f64(w), np.zeros(N) if bias is None else bias.astype(np.float64), epilogue, gelu_tanh, c0.astype(np.float64))
+    err = np.abs(f64(c) - want)
+    assert (err <= tol + 1e-30).all(), f"{(err / tol).max():.3g} of the tolerance"
+    assert (guard[M * outs:] == 3.0).all()
+
+
+def test_linear_rows_rows_do_not_touch_each_other(B):
+    """A NaN row stays alone, and a row gives the same bits whatever the other rows of the call hold."""
+    import torch
+    rng = np.random.default_rng(2)
+    a, w = bf16(rng.standard_normal((13, 777 * 8))), bf16(rng.standard_normal((300, 777 * 8)))
+    x = B.et_linear_rows(a, w)
+    b = a.clone()
+    b[5] = math.nan
+    b[7:] *= 3
+    y = B.et_linear_rows(b, w)
+    assert torch.isnan(y[5].float()).all() and torch.equal(x[[0, 1, 2, 3, 4, 6]], y[[0, 1, 2, 3, 4, 6]])
+
+
+def test_linear_rows_agrees_with_linear_bf16(B):
+    """The same arguments and weight order as the wide dense layer: results within the roundings of both."""
+    import torch
+    rng = np.random.default_rng(3)
+    for epilogue, N in ((0, 640), (1, 640), (2, 640), (4, 1024)):
+        a, w = bf16(rng.standard_normal((24, 512))), bf16(rng.standard_normal((N, 512)) / math.sqrt(512))
+        bias = torch.from_numpy(rng.standard_normal(N).astype(np.float32)).cuda()
+        c = torch.zeros((24, 640), dtype=torch.float32, device="cuda") if epilogue == 2 else None
+        x, _ = B.et_linear_bf16(a, w, bias, epilogue, c=None if c is None else c.clone())
+        y = B.et_linear_rows(a, w, bias, epilogue, c=c)
+        d = (x.float() - y.float()).abs()
+        # the wide layer's GELU uses the hardware tanh (2^-11 of the argument)
+        assert (d <= 2 * BF16 * x.float().abs() + (2.0 ** -10 if epilogue == 1 else 2.0 ** -16) * (1 + x.float().abs())).all()
+
+
+# ---- together ---------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_decode_step_follows_the_prefill(B, e4m3):
+    """A prompt is prefilled, its cache moved into pages, and the next token decoded layer by layer with the operators: logits
+    agree with the prefill of the longer sequence.  Both paths keep activations in bf16 but round at different places; the bound
+    is the framework's for whole bf16 models, 2e-2 of the largest logit; an e4m3 cache adds the spread of its own rounding,
+    2^-4 / sqrt(3) of each key and value, averaged over many positions and layers: 0.1 of the largest logit."""
+    import torch
+    from synthetic.llm import LLM_SMALL, llm_views, make_llm_weights, make_prompt, make_visual_tokens
+    sh = LLM_SMALL
+    blob = make_llm_weights(sh, 4)
+    n = 150
+    ids, _ = make_prompt(sh, n + 1, 0, 4)
+    vis = torch.from_numpy(make_visual_tokens(sh, 40, 4)).cuda()
+    llm = B.LanguageModel(sh, blob, max_tokens=256, keep_kv_cache=True)
+    want = llm.prefill(ids[:100], vis, ids[100:]).logits
+    pre = llm.prefill(ids[:100], vis, ids[100:n], want_kv=True)
+    total = pre.n_tokens
+    W = {k: torch.from_numpy(np.ascontiguousarray(v)).cuda() for k, v in llm_views(sh, blob).items()}
+    def t16(x):
+        return x.to(torch.bfloat16).T.contiguous()
+    page, kvh, d = 32, sh.kv_heads, sh.head_dim
+    rng = np.random.default_rng(1)
+    x = W["embed"].to(torch.bfloat16)[int(ids[n])].float().view(1, -1).clone()
+    table = i32(rng.permutation(16)[:8].reshape(1, 8))
+    lens, new, status = i32([total]), i32([0]), i32([0])
+    for i in range(sh.num_layers):
+        w = {k[len(f"l{i}."):]: v for k, v in W.items() if k.startswith(f"l{i}.")}
+        cache = torch.zeros((16, 2, kvh, page, d), dtype=torch.float8_e4m3fn if e4m3 else torch.bfloat16, device="cuda")
+        scale = torch.zeros((16, 2, kvh, page), dtype=torch.uint8, device="cuda") if e4m3 else None
+        B.et_kv_append(cache, scale, pre.kv_cache[i], 0, table, i32([0]), i32([0, total]), status=status)
+        if not e4m3:
+            assert torch.equal(B.et_kv_read(cache, scale, table, i32([0]), total, i32([0, total])), pre.kv_cache[i])
+        qkv = B.et_linear_rows(B.et_rmsnorm(x, w["rms1_g"], sh.rms_eps), t16(w["wqkv"]), w["bqkv"])
+        q = B.et_kv_append(cache, scale, qkv, sh.heads, table, lens, theta=sh.rope_theta, new_len=new, status=status)
+        att = B.et_attention_paged(q, sh.heads, cache, scale, table, new, status=status)
+        B.et_linear_rows(att, t16(w["wo"]), None, 2, c=x)
+        h = B.et_rmsnorm(x, w["rms2_g"], sh.rms_eps)
+        m = sh.mlp_dim
+        gate, up = t16(w["wgu"])[:m], t16(w["wgu"])[m:]
+        pad = -m % 128                                  # whole tiles of 256 weight rows; the padding's outputs are dropped
+        gate, up = (torch.cat([z, torch.zeros((pad, z.shape[1]), dtype=z.dtype, device="cuda")]) for z in (gate, up))
+        tiled = torch.stack([gate.view(-1, 32, gate.shape[1]), up.view(-1, 32, up.shape[1])], 1).reshape(-1, gate.shape[1])
+        act = B.et_linear_rows(h, tiled.contiguous(), None, 4)[:, :m].contiguous()
+        B.et_linear_rows(act, t16(w["wd"]), None, 2, c=x)
+    logits = torch.zeros((1, sh.vocab), dtype=torch.float32, device="cuda")
+    B.et_linear_rows(B.et_rmsnorm(x, W["final_g"], sh.rms_eps), t16(W["lm_head"]), None, 2, c=logits)
+    assert status.item() == 0 and new.item() == total + 1
+    off = (logits[0] - want).abs().max().item() / want.abs().max().item()
+    assert off <= (0.1 if e4m3 else 2e-2), off
+
+
+def test_decode_operators_in_one_graph(B):
+    """Three tokens decoded by one captured step (append, attention) whose lengths advance on the device, on a side stream,
+    against the same steps run one by one."""
+    import torch
+    rng = np.random.default_rng(31)
+    n, heads, kvh, page, d = 3, 6, 2, 16, 64
+    lens0 = [14, 0, 33]
+
+    def fresh():
+        return Cache(np.random.default_rng(32), n, 4, kvh, page, d, True)
+
+    qkvs = [bf16(rng.standard_normal((n, (heads + 2 * kvh) * d))) for _ in range(3)]
+    a, want, lens = fresh(), [], i32(lens0)
+    for qkv in qkvs:
+        new = torch.empty_like(lens)
+        q = B.et_kv_append(a.data, a.scale, qkv, heads, a.table, lens, theta=1e4, new_len=new)
+        want.append(B.et_attention_paged(q, heads, a.data, a.scale, a.table, new))
+        lens = new
+    b, stream = fresh(), torch.cuda.Stream()
+    lens, new, qkv = i32(lens0), i32([0] * n), qkvs[0].clone()
+    q = torch.empty((n, heads * d), dtype=torch.bfloat16, device="cuda")
+    out = torch.empty_like(q)
+    ws = torch.empty(B.ET_PAGED_WORKSPACE, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+
+    def step():
+        B.et_kv_append(b.data, b.scale, qkv, heads, b.table, lens, theta=1e4, q_out=q, new_len=new)
+        B.et_attention_paged(q, heads, b.data, b.scale, b.table, new, out=out, workspace=ws)
+        lens.copy_(new)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    for x, y in zip(qkvs, want):
+        qkv.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, y)
+    assert torch.equal(b.bytes()[0], a.bytes()[0]) and torch.equal(b.scale, a.scale)
