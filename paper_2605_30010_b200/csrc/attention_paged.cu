@@ -1,92 +1,691 @@
 // Attention of one new token of each sequence over its paged key / value cache.
+//
+// Every cached byte is read once and used for `group` query heads (7 in a Qwen2-7B layer), about 7 multiply-adds a byte:
+// the cache's bytes over the memory bandwidth bound it, and the work is arranged to keep copies in flight.
+//
+//   * A tile is 64 positions of one key / value head.  All tiles of the call, in the order (sequence, key / value head,
+//     tile), are cut into one equal run per CTA (one CTA per SM), so a single long sequence and a ragged batch load every
+//     SM alike.  Lengths are on the device, so each CTA works the cut out for itself.
+//   * One warp copies: TMA boxes of a page's rows (hardware swizzle, so that ldmatrix meets no bank conflicts) into a ring
+//     of stages.  Eight warps compute, four to a tile, 16 positions each, every warp with a running maximum, sum and
+//     output of its own; they meet only at the end of a piece (the part of a sequence that falls into the CTA's run).
+//   * The product is transposed, S^T = K Q^T and O^T = V^T P^T, so that the query heads are the narrow side (8) of
+//     mma.sync's m16n8k16: up to 8 heads cost no padded rows.  (tcgen05 wants 64 or more rows a tile, and the tensor work
+//     here is a few per cent of the time.)
+//   * A piece that is a whole item is written out at once; the others leave (output, maximum, sum) in the workspace, and a
+//     second, small kernel joins them in a fixed order.
+#include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
 #include "decode.cuh"
-#include "rowops.cuh"
+#include "tcgen05.cuh"
 
 namespace et {
 
 namespace {
 
-constexpr int WARPS = 4;
+using namespace tc;
 
-// The simplest form: one block per (sequence, query head), keys dealt to the warps in turn, each warp with a running
-// maximum and sum of its own, joined through shared memory at the end.
-template <int DH, bool E4M3>
-__global__ void __launch_bounds__(WARPS * 32)
-attention_paged_kernel(PagedCache c, PagedAttention g) {
-  constexpr int V = DH / 32;                     // values of a row per lane
-  const int s = blockIdx.x / g.heads, h = blockIdx.x % g.heads, kvh = h / (g.heads / c.kv_heads);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const float scale = rsqrtf((float)DH);
-  float q[V], o[V], m = -INFINITY, l = 0.f;
+constexpr int TILE = 64;                       // positions
+constexpr int GROUP_WARPS = 4;                 // warps of one tile, 16 positions each
+constexpr int COMPUTE_WARPS = 8;
+constexpr int THREADS = 32 * (COMPUTE_WARPS + 1);
+constexpr int MAX_CTAS = 148;
+constexpr int PAD = 4;                         // floats between heads of the joining buffer: no bank conflicts
+constexpr int SMEM_LIMIT = 232448 - 512;       // 227 KB, less the static part
+constexpr int CONTROL_BYTES = 1024;            // barriers and the ring's flags
+
+template <int DH, bool E4M3, int NT>
+struct Cfg {
+  static constexpr int ROW = DH * (E4M3 ? 1 : 2);                 // bytes of a row
+  static constexpr int BOX_ROW = ROW > 128 ? 128 : ROW;           // bytes of a box row: the swizzle's width
+  static constexpr int BOXES = ROW / BOX_ROW;
+  static constexpr int PLANE = TILE * ROW;
+  static constexpr int STAGE = 2 * PLANE;                         // keys, values
+  static constexpr int SCALES = E4M3 ? 2 * TILE : 0;
+  static constexpr int HEADS = 8 * NT;
+  static constexpr int JOIN = COMPUTE_WARPS * HEADS * (DH + PAD) * 4 + COMPUTE_WARPS * HEADS * 3 * 4;
+  static constexpr int FIT = (SMEM_LIMIT - 1024 - CONTROL_BYTES - JOIN) / (STAGE + SCALES);
+  // even, so that a stage is always the same four warps': they wait for its copies in turn, where warps that come to a
+  // stage for the first time in its second round could take the barrier's state of the first for their own
+  static constexpr int STAGES = (FIT > 12 ? 12 : FIT) & ~1;
+  static constexpr int SMEM = 1024 + STAGES * (STAGE + SCALES) + JOIN + CONTROL_BYTES;
+  static_assert(STAGES >= 4 && STAGES % (COMPUTE_WARPS / GROUP_WARPS) == 0, "ring");
+  static_assert(2 * 8 * STAGES + 4 * STAGES + 16 <= CONTROL_BYTES, "control area");
+};
+
+// Workspace: one descriptor per CTA, then two slots of partial results per CTA.
+struct alignas(16) Join { int seq, part, pieces, slot; };         // pieces == 0: nothing of this CTA is to be joined
+constexpr int SLOT0 = 1024;                                       // floats
+static_assert(MAX_CTAS * sizeof(Join) <= SLOT0 * 4, "descriptors");
+template <int DH, int NT> struct Slot { static constexpr int FLOATS = 8 * NT * (DH + 2); };
+static_assert((SLOT0 + 2 * MAX_CTAS * Slot<128, 2>::FLOATS) * 4 <= (int)ET_PAGED_WORKSPACE, "workspace");
+
+struct Args {
+  PagedCache c;
+  PagedAttention a;
+  int group, parts, whole;          // heads per key / value head; head tiles per key / value head; 1: items are not cut
+};
+
+__device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+template <bool F16>
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if (F16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// two e4m3 values (the low 16 bits) as two halves, exactly
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t x) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)x, __NV_E4M3);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// 2^e for e in [-127, 127]
+__device__ __forceinline__ float pow2(int e) { return __int_as_float(e > -127 ? (e + 127) << 23 : 1 << 22); }
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void compute_warps_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * COMPUTE_WARPS) : "memory"); }
+
+// The run of units (tiles; whole items where args.whole) that falls to a CTA, walked piece by piece.
+struct Walk {
+  long long left;                  // units still to do
+  int s, part, unit;               // next unit: sequence, key / value head x head tile, unit of the item
+  int n_seq, parts_all;
+};
+
+__device__ __forceinline__ int clamped_len(const Args& g, int s) {
+  const long long cap = (long long)g.a.max_pages << g.c.page_shift;
+  return (int)min((long long)max(__ldg(g.a.len + s), 0), cap);
+}
+__device__ __forceinline__ int units_of(const Args& g, int len) { return g.whole ? (len > 0) : (len + TILE - 1) / TILE; }
+
+struct Piece { int s, part, len, t0, t1; bool first, last; };     // tiles t0 .. t1 - 1; first / last: contains the item's first / last tile
+
+__device__ __forceinline__ bool next_piece(const Args& g, Walk& w, Piece& p) {
+  if (w.left <= 0) return false;
+  int len = clamped_len(g, w.s);
+  while (units_of(g, len) == 0) {                                 // only between items: the walk's units are accounted for
+    if (++w.s >= w.n_seq) return false;
+    len = clamped_len(g, w.s);
+  }
+  const int units = units_of(g, len), tiles = (len + TILE - 1) / TILE;
+  const int n = (int)min(w.left, (long long)(units - w.unit));
+  p.s = w.s; p.part = w.part; p.len = len;
+  p.first = w.unit == 0; p.last = w.unit + n == units;
+  p.t0 = g.whole ? 0 : w.unit; p.t1 = g.whole ? tiles : w.unit + n;
+  w.left -= n; w.unit += n;
+  if (w.unit == units) {
+    w.unit = 0;
+    if (++w.part == w.parts_all) { w.part = 0; ++w.s; if (w.s >= w.n_seq) w.left = 0; }
+  }
+  return true;
+}
+
+template <int DH, bool E4M3, int NT>
+__global__ void __launch_bounds__(THREADS, 1)
+attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ Args g) {
+  using C = Cfg<DH, E4M3, NT>;
+  constexpr int STAGES = C::STAGES, KS = DH / 16;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* const gen = smem_raw + (base - raw);
+  const uint32_t scales = base + STAGES * C::STAGE;
+  float* const join = reinterpret_cast<float*>(gen + STAGES * (C::STAGE + C::SCALES));
+  float* const join_m = join + COMPUTE_WARPS * C::HEADS * (DH + PAD);       // [3][COMPUTE_WARPS][HEADS]: maximum, output's maximum, sum
+  uint8_t* const ctl = gen + STAGES * (C::STAGE + C::SCALES) + C::JOIN;
+  const uint32_t bars = smem_u32(ctl);
+  auto full = [&](int s) { return bars + 8u * (uint32_t)s; };
+  auto empty = [&](int s) { return bars + 8u * (uint32_t)(STAGES + s); };
+  volatile int* const absent = reinterpret_cast<volatile int*>(ctl + 16 * STAGES);   // [STAGES]: bit i = slice i has no page
+  volatile int* const abort_flag = absent + STAGES;
+  __shared__ long long warp_sum_s[THREADS / 32];
+  __shared__ long long total_s;
+  __shared__ int walk_s[3];
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int b = blockIdx.x;
+  const int kv_heads = g.c.kv_heads, parts_all = kv_heads * g.parts;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");    // the joining kernel may be set up; it waits for this grid's end
+
+  if (tid == 0) {
+    for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), GROUP_WARPS); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+
+  // ---- this CTA's run: an exclusive prefix sum of the sequences' units over the threads
+  Walk walk;
+  long long begin, chunk;
+  {
+    const int per = (g.a.n_seq + THREADS - 1) / THREADS, s0 = min(tid * per, g.a.n_seq), s1 = min(s0 + per, g.a.n_seq);
+    long long sum = 0;
+    for (int s = s0; s < s1; ++s) sum += units_of(g, clamped_len(g, s));
+    sum *= parts_all;
+    long long inc = sum;
 #pragma unroll
-  for (int k = 0; k < V; ++k) { q[k] = __bfloat162float(g.q[(size_t)s * g.q_stride + h * DH + lane * V + k]) * scale; o[k] = 0.f; }
-  auto load = [&](size_t row, float (&x)[V]) {
-    const float f = E4M3 ? __int_as_float(c.scale[row] ? c.scale[row] << 23 : 1 << 22) : 1.f;
+    for (int o = 1; o < 32; o <<= 1) { const long long v = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += v; }
+    if (lane == 31) warp_sum_s[warp] = inc;
+    __syncthreads();
+    long long before = inc - sum, total = 0;
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const size_t at = row * DH + lane * V + k;
-      if (E4M3) {
-        const __half_raw y = __nv_cvt_fp8_to_halfraw(c.data[at], __NV_E4M3);
-        x[k] = __half2float(*reinterpret_cast<const __half*>(&y)) * f;
-      } else {
-        x[k] = __bfloat162float(reinterpret_cast<const bf16*>(c.data)[at]);
+    for (int w = 0; w < THREADS / 32; ++w) { const long long v = warp_sum_s[w]; if (w < warp) before += v; total += v; }
+    chunk = (total + gridDim.x - 1) / gridDim.x;
+    begin = chunk * b;
+    if (begin >= before && begin < before + sum) {
+      long long r = begin - before;
+      for (int s = s0; s < s1; ++s) {
+        const int u = units_of(g, clamped_len(g, s));
+        const long long all = (long long)u * parts_all;
+        if (r < all) { walk_s[0] = s; walk_s[1] = (int)(r / u); walk_s[2] = (int)(r % u); break; }
+        r -= all;
       }
     }
-  };
-  long long len = g.len[s];
-  const long long cap = (long long)g.max_pages << c.page_shift;
-  if (len > cap) {
-    if (g.status && threadIdx.x == 0) atomicMax(g.status, (int)ET_PAGED_CAPACITY);
-    len = cap;
+    if (tid == 0) total_s = total;
+    __syncthreads();
+    walk.left = max(0ll, min(chunk, total_s - begin));
+    walk.n_seq = g.a.n_seq; walk.parts_all = parts_all;
+    walk.s = walk_s[0]; walk.part = walk_s[1]; walk.unit = walk_s[2];
   }
-  for (long long t = warp; t < len; t += WARPS) {
-    int page, place;
-    if (!paged_place(c, g.table, g.max_pages, s, t, g.status, page, place)) continue;
-    const size_t row = ((((size_t)page * 2) * c.kv_heads + kvh) << c.page_shift) + place;
-    float k[V], v[V], d = 0.f;
-    load(row, k);
-    load(row + ((size_t)c.kv_heads << c.page_shift), v);
-#pragma unroll
-    for (int j = 0; j < V; ++j) d += q[j] * k[j];
-    d = warp_sum(d);
-    const float mn = fmaxf(m, d), a = expf(m - mn), p = expf(d - mn);
-    l = l * a + p;
-#pragma unroll
-    for (int j = 0; j < V; ++j) o[j] = o[j] * a + p * v[j];
-    m = mn;
+
+  // ---- sequences without positions, and lengths that the table cannot hold
+  for (int s = b; s < g.a.n_seq; s += gridDim.x) {
+    const int len = __ldg(g.a.len + s);
+    if (len <= 0) {
+      for (int i = tid; i < g.a.heads * DH / 8; i += THREADS)
+        reinterpret_cast<uint4*>(g.a.out + (size_t)s * g.a.heads * DH)[i] = make_uint4(0, 0, 0, 0);
+      if (g.a.lse) for (int i = tid; i < g.a.heads; i += THREADS) g.a.lse[(size_t)s * g.a.heads + i] = -INFINITY;
+    } else if (tid == 0 && g.a.status && len > (long long)g.a.max_pages << g.c.page_shift) {
+      atomicMax(g.a.status, (int)ET_PAGED_CAPACITY);
+    }
   }
-  __shared__ float so[WARPS][DH], sm[WARPS], sl[WARPS];
+
+  bool ok = true;
+  if (warp == COMPUTE_WARPS) {
+    // ------------------------------------------------------------------ copies
+    const int box_shift = min(g.c.page_shift, 6), box_rows = 1 << box_shift, boxes_tile = TILE >> box_shift;
+    constexpr int OPS = 2 * C::BOXES + (E4M3 ? 2 : 0);               // copies of one page's rows: keys, values, their scales
+    const int my_box = lane / OPS, my_op = lane % OPS;
+    const uint32_t box_bytes = (uint32_t)box_rows * (2 * C::ROW + (E4M3 ? 2 : 0));
+    if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
+    int stage = 0;
+    uint32_t phase = 0;
+    long long issued = 0;
+    Piece p;
+    while (ok && next_piece(g, walk, p)) {
+      const int* table = g.a.table + (size_t)p.s * g.a.max_pages;
+      const int kvh = p.part / g.parts;
+      const int first_page = (int)(((long long)p.t0 * TILE) >> g.c.page_shift);
+      auto page_ids = [&](int batch) {                               // 32 entries of the table, one per lane
+        const long long i = (long long)first_page + batch * 32 + lane;
+        return i < g.a.max_pages ? __ldg(table + i) : -1;
+      };
+      int batch = 0, ids = page_ids(0), ids_next = page_ids(1);
+      for (int t = p.t0; t < p.t1; ++t) {
+        const long long pos = (long long)t * TILE;
+        const int page0 = (int)(pos >> g.c.page_shift) - first_page;  // a multiple of the tile's pages: one batch has them all
+        while ((page0 >> 5) > batch) { ++batch; ids = ids_next; ids_next = page_ids(batch + 1); }
+        const bool box_live = my_box < boxes_tile && pos + ((long long)my_box << box_shift) < p.len;
+        const int page = __shfl_sync(0xffffffffu, ids, (page0 + (my_box < boxes_tile ? my_box : 0)) & 31);
+        const bool good = (unsigned)page < (unsigned)g.c.n_pages;
+        const bool copy = box_live && good;
+        if (box_live && !good && g.a.status) atomicMax(g.a.status, (int)ET_PAGED_BAD_PAGE);
+        const unsigned bad = __ballot_sync(0xffffffffu, box_live && !good && my_op == 0);
+        const unsigned copies = __ballot_sync(0xffffffffu, copy && my_op == 0);
+        ok = mbar_wait_warp(empty(stage), phase ^ 1u, abort_flag);
+        if (!ok) break;
+        if (lane == 0) {
+          int mask = 0;
+          for (int i = 0; i < boxes_tile; ++i)
+            if (bad >> (i * OPS) & 1u) mask |= ((1 << (box_rows / 16)) - 1) << (i * (box_rows / 16));
+          absent[stage] = mask;
+          mbar_arrive_expect_tx(full(stage), (uint32_t)__popc(copies) * box_bytes);
+        }
+        __syncwarp();
+        if (copy) {
+          const int row0 = my_box << box_shift;                       // of the tile
+          const int place = (int)((pos + row0) & ((1 << g.c.page_shift) - 1));
+          const int plane = my_op < 2 * C::BOXES ? my_op / C::BOXES : my_op - 2 * C::BOXES;
+          const int y = (((page * 2 + plane) * kv_heads + kvh) << g.c.page_shift) + place;
+          if (my_op < 2 * C::BOXES) {
+            const int half = my_op % C::BOXES;
+            tma_load_2d(base + stage * C::STAGE + plane * C::PLANE + half * (TILE * C::BOX_ROW) + row0 * C::BOX_ROW, &map, full(stage),
+                        half * (C::BOX_ROW / (E4M3 ? 1 : 2)), y);
+          } else {
+            bulk_load(scales + stage * C::SCALES + plane * TILE + row0, g.c.scale + (size_t)(unsigned)y, (uint32_t)box_rows, full(stage));
+          }
+        }
+        ++issued;
+        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+      }
+    }
+    if (!ok && lane == 0) {
+      // copies in flight have to land before this CTA's shared memory is given up
+      for (int i = 0; i < STAGES && i < issued; ++i) {
+        if (--stage < 0) { stage = STAGES - 1; phase ^= 1u; }
+        int given_up = 0;
+        mbar_wait(full(stage), phase, &given_up);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ the product
+    const int my_group = warp / GROUP_WARPS, slice = warp % GROUP_WARPS, r0 = slice * 16;
+    const int gq = lane >> 2, tq = lane & 3;                         // mma's row group and column pair
+    // this lane's row of the 16 and its 16-byte chunk (K: both halves of a k-step; V, transposed: see below)
+    const int krow = r0 + (lane & 7) + ((lane >> 3) & 1) * 8, kchunk = lane >> 4;
+    const int vrow = E4M3 ? krow : r0 + (lane & 7) + (lane >> 4) * 8, vchunk = E4M3 ? kchunk : (lane >> 3) & 1;
+    auto swizzled = [&](int row, int chunk) -> uint32_t {            // 16-byte chunk of a row, as the copies place it
+      if constexpr (C::BOX_ROW == 128)
+        return (uint32_t)((chunk >> 3) * (TILE * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4));
+      else
+        return (uint32_t)(row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4));
+    };
+    const float softmax_scale = 1.4426950408889634f * (DH == 128 ? 0.08838834764831845f : 0.125f);   // log2(e) / sqrt(DH)
+
+    int stage = 0, pieces_done = 0;
+    uint32_t phase = 0;
+    long long count = 0;                                             // tiles of this CTA so far
+    Piece p;
+    Join mine{0, 0, 0, 0};
+    while (next_piece(g, walk, p)) {
+      const int kvh = p.part / g.parts, h0 = (p.part % g.parts) * C::HEADS;       // first head of the tile inside its group
+      const int heads_live = min(C::HEADS, g.group - h0);
+      // ---- Q^T as the B operand: column gq = head, two rows (pairs of dimensions) a register
+      uint32_t q[NT][KS][2];
+      float qscale[NT][2];                                           // of heads 2 tq and 2 tq + 1
 #pragma unroll
-  for (int j = 0; j < V; ++j) so[warp][lane * V + j] = o[j];
-  if (lane == 0) { sm[warp] = m; sl[warp] = l; }
+      for (int n = 0; n < NT; ++n) {
+        const bool live = n * 8 + gq < heads_live;
+        const bf16* src = g.a.q + (size_t)p.s * g.a.q_stride + (size_t)(kvh * g.group + h0 + (live ? n * 8 + gq : 0)) * DH;
+        if constexpr (!E4M3) {
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            q[n][k][0] = live ? __ldg(reinterpret_cast<const uint32_t*>(src + k * 16 + 2 * tq)) : 0u;
+            q[n][k][1] = live ? __ldg(reinterpret_cast<const uint32_t*>(src + k * 16 + 8 + 2 * tq)) : 0u;
+          }
+          qscale[n][0] = qscale[n][1] = softmax_scale;
+        } else {
+          // e4m3 keys are multiplied as halves, which hold them exactly.  A query row is scaled by a power of two that
+          // brings its largest value to 2^14 .. 2^15: a value below 2^-29 of that loses bits, no other.  The dimensions of
+          // a k-step are taken in the order that the keys' bytes come in: 4 tq, 4 tq + 1 | 4 tq + 2, 4 tq + 3.
+          uint2 raw_q[KS];
+          float top = 0.f;
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            raw_q[k] = live ? __ldg(reinterpret_cast<const uint2*>(src + k * 16 + 4 * tq)) : make_uint2(0, 0);
+            const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].x));
+            const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].y));
+            top = fmaxf(top, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(y.x), fabsf(y.y))));
+          }
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          const int e = top > 0.f ? max((__float_as_int(top) >> 23) - 127 - 14, -127) : 0;
+          const float f = pow2(-e);
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].x));
+            const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].y));
+            q[n][k][0] = pack_f16(x.x * f, x.y * f);
+            q[n][k][1] = pack_f16(y.x * f, y.y * f);
+          }
+          const float back = pow2(e) * softmax_scale;
+          qscale[n][0] = __shfl_sync(0xffffffffu, back, 8 * tq);
+          qscale[n][1] = __shfl_sync(0xffffffffu, back, 8 * tq + 4);
+        }
+      }
+      // per head 2 tq + i: running maximum m of the scores (base 2), sum l of this lane's positions; mo: maximum of score +
+      // log2(scale of the value), against which the output is kept (e4m3: a value's scale is part of its weight)
+      float o[NT][KS][4], m[NT][2], mo[NT][2], l[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        m[n][0] = m[n][1] = mo[n][0] = mo[n][1] = -INFINITY;
+        l[n][0] = l[n][1] = 0.f;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) o[n][k][0] = o[n][k][1] = o[n][k][2] = o[n][k][3] = 0.f;
+      }
+
+      for (int t = p.t0; t < p.t1; ++t, ++count) {
+        const int st = stage;
+        const uint32_t ph = phase;
+        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        if ((int)(count & 1) != my_group) continue;
+        if (ok) ok = mbar_wait_warp(full(st), ph, abort_flag);
+        if (!ok) continue;
+        // positions of the slice that count: up to the length, none on an absent page (a page has whole slices)
+        const long long room = (long long)p.len - (long long)t * TILE - r0;
+        const int valid = (absent[st] >> slice & 1) ? 0 : (int)max(0ll, min(16ll, room));
+        if (valid > 0) {
+          const uint32_t kb = base + st * C::STAGE, vb = kb + C::PLANE;
+          // ---- S^T = K Q^T: rows = positions gq, gq + 8, columns = heads 2 tq, 2 tq + 1
+          float s[NT][4], s2[NT][4];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) { s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f; s2[n][0] = s2[n][1] = s2[n][2] = s2[n][3] = 0.f; }
+          if constexpr (!E4M3) {
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+              uint32_t a[4];
+              ldmatrix4(kb + swizzled(krow, 2 * k + kchunk), a);
+#pragma unroll
+              for (int n = 0; n < NT; ++n) mma16816<false>((k & 1) ? s2[n] : s[n], a[0], a[1], a[2], a[3], q[n][k][0], q[n][k][1]);
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < KS; k += 2) {
+              uint32_t a[4];                                          // positions gq / gq + 8 of k-step k, then of k + 1
+              ldmatrix4(kb + swizzled(krow, k + kchunk), a);
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const uint32_t a0 = e4m3x2_to_f16x2(a[2 * i] & 0xffffu), a2 = e4m3x2_to_f16x2(a[2 * i] >> 16);
+                const uint32_t a1 = e4m3x2_to_f16x2(a[2 * i + 1] & 0xffffu), a3 = e4m3x2_to_f16x2(a[2 * i + 1] >> 16);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma16816<true>(i ? s2[n] : s[n], a0, a1, a2, a3, q[n][k + i][0], q[n][k + i][1]);
+              }
+            }
+          }
+          float ks0 = 1.f, ks1 = 1.f, ve0 = 0.f, ve1 = 0.f;
+          if constexpr (E4M3) {
+            const uint8_t* sc = gen + STAGES * C::STAGE + st * C::SCALES + r0 + gq;
+            ks0 = pow2((int)sc[0] - 127); ks1 = pow2((int)sc[8] - 127);
+            ve0 = (float)((int)sc[TILE] - 127); ve1 = (float)((int)sc[TILE + 8] - 127);
+          }
+          const bool live0 = gq < valid, live1 = gq + 8 < valid;
+          bool moved = false;
+          float pr[NT][4], alpha[NT][2];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float x[4];
+            x[0] = live0 ? (s[n][0] + s2[n][0]) * qscale[n][0] * ks0 : -INFINITY;
+            x[1] = live0 ? (s[n][1] + s2[n][1]) * qscale[n][1] * ks0 : -INFINITY;
+            x[2] = live1 ? (s[n][2] + s2[n][2]) * qscale[n][0] * ks1 : -INFINITY;
+            x[3] = live1 ? (s[n][3] + s2[n][3]) * qscale[n][1] * ks1 : -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              float top = fmaxf(x[i], x[i + 2]), topo = E4M3 ? fmaxf(x[i] + ve0, x[i + 2] + ve1) : 0.f;
+#pragma unroll
+              for (int d = 4; d < 32; d <<= 1) {
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                if (E4M3) topo = fmaxf(topo, __shfl_xor_sync(0xffffffffu, topo, d));
+              }
+              const float mn = fmaxf(m[n][i], top), mu = mn == -INFINITY ? 0.f : mn;
+              const float e0 = exp2_fast(x[i] - mu), e1 = exp2_fast(x[i + 2] - mu);
+              if (!E4M3) {
+                const float al = exp2_fast(m[n][i] - mu);
+                moved |= mn != m[n][i];
+                l[n][i] = l[n][i] * al + (e0 + e1);
+                alpha[n][i] = al;
+                pr[n][i] = e0; pr[n][i + 2] = e1;
+              } else {
+                l[n][i] = l[n][i] * exp2_fast(m[n][i] - mu) + (e0 + e1);
+                const float on = fmaxf(mo[n][i], topo), ou = on == -INFINITY ? 0.f : on;
+                moved |= on != mo[n][i];
+                alpha[n][i] = exp2_fast(mo[n][i] - ou);
+                pr[n][i] = exp2_fast(x[i] + ve0 - ou); pr[n][i + 2] = exp2_fast(x[i + 2] + ve1 - ou);
+                mo[n][i] = on;
+              }
+              m[n][i] = mn;
+            }
+          }
+          if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int k = 0; k < KS; ++k) {
+                o[n][k][0] *= alpha[n][0]; o[n][k][1] *= alpha[n][1]; o[n][k][2] *= alpha[n][0]; o[n][k][3] *= alpha[n][1];
+              }
+          }
+          // ---- O^T += V^T P^T.  P as the B operand: 8 x 8 transposes of the accumulator's pairs.  bf16: a probability is
+          // split into two bf16 (16 bits of it count); halves (e4m3) hold 11 bits of it.
+          uint32_t ph0[NT], ph1[NT], pl0[NT], pl1[NT];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            if constexpr (E4M3) {
+              ph0[n] = transpose8x8(pack_f16(pr[n][0], pr[n][1]));
+              ph1[n] = transpose8x8(pack_f16(pr[n][2], pr[n][3]));
+            } else {
+              const uint32_t a = pack_bf16(pr[n][0], pr[n][1]), c = pack_bf16(pr[n][2], pr[n][3]);
+              const float2 fa = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&a));
+              const float2 fc = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&c));
+              ph0[n] = transpose8x8(a);
+              ph1[n] = transpose8x8(c);
+              pl0[n] = transpose8x8(pack_bf16(pr[n][0] - fa.x, pr[n][1] - fa.y));
+              pl1[n] = transpose8x8(pack_bf16(pr[n][2] - fc.x, pr[n][3] - fc.y));
+            }
+          }
+          // whatever stands behind the length must not meet a zero probability: 0 * NaN is NaN
+          const uint32_t keep0 = (2 * tq < valid ? 0xffffu : 0u) | (2 * tq + 1 < valid ? 0xffff0000u : 0u);
+          const uint32_t keep1 = (2 * tq + 8 < valid ? 0xffffu : 0u) | (2 * tq + 9 < valid ? 0xffff0000u : 0u);
+          if constexpr (!E4M3) {
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+              uint32_t a[4];                                          // rows d = 16 k + gq, + 8; columns = positions
+              ldmatrix4_trans(vb + swizzled(vrow, 2 * k + vchunk), a);
+              a[0] &= keep0; a[1] &= keep0; a[2] &= keep1; a[3] &= keep1;
+#pragma unroll
+              for (int n = 0; n < NT; ++n) {
+                mma16816<false>(o[n][k], a[0], a[1], a[2], a[3], ph0[n], ph1[n]);
+                mma16816<false>(o[n][k], a[0], a[1], a[2], a[3], pl0[n], pl1[n]);
+              }
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < KS; k += 2) {
+              // a transposed 8 x 8 of byte pairs: this lane has dimensions 2 gq, 2 gq + 1 of positions 2 tq, 2 tq + 1 (and + 8)
+              uint32_t a[4];
+              ldmatrix4_trans(vb + swizzled(vrow, k + vchunk), a);
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const uint32_t x = a[2 * i] & keep0, y = a[2 * i + 1] & keep1;
+                const uint32_t a0 = e4m3x2_to_f16x2(__byte_perm(x, 0, 0x4420)), a1 = e4m3x2_to_f16x2(__byte_perm(x, 0, 0x4431));
+                const uint32_t a2 = e4m3x2_to_f16x2(__byte_perm(y, 0, 0x4420)), a3 = e4m3x2_to_f16x2(__byte_perm(y, 0, 0x4431));
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma16816<true>(o[n][k + i], a0, a1, a2, a3, ph0[n], ph1[n]);
+              }
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(st));
+      }
+
+      // ---- the eight warps' results of the piece
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float x = l[n][i];
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+          const int h = n * 8 + 2 * tq + i;
+          if (gq == 0) {
+            join_m[warp * C::HEADS + h] = m[n][i];
+            join_m[(COMPUTE_WARPS + warp) * C::HEADS + h] = E4M3 ? mo[n][i] : m[n][i];
+            join_m[(2 * COMPUTE_WARPS + warp) * C::HEADS + h] = x;
+          }
+          float* dst = join + (warp * C::HEADS + h) * (DH + PAD);
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            if (E4M3) *reinterpret_cast<float2*>(dst + 16 * k + 2 * gq) = make_float2(o[n][k][i], o[n][k][i + 2]);
+            else { dst[16 * k + gq] = o[n][k][i]; dst[16 * k + 8 + gq] = o[n][k][i + 2]; }
+          }
+        }
+      }
+      compute_warps_sync();
+      const bool whole = p.first && p.last;
+      const int slot = 2 * b + (pieces_done == 0 ? 0 : 1);
+      float* const part = g.a.workspace + SLOT0 + (size_t)slot * Slot<DH, NT>::FLOATS;
+      for (int i = tid; i < heads_live * (DH / 4); i += 32 * COMPUTE_WARPS) {
+        const int h = i / (DH / 4), d = (i % (DH / 4)) * 4;
+        float top = -INFINITY, sum = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < COMPUTE_WARPS; ++w) top = fmaxf(top, join_m[w * C::HEADS + h]);
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int w = 0; w < COMPUTE_WARPS; ++w) {
+          const float fl = exp2_fast(join_m[w * C::HEADS + h] - ref), fo = exp2_fast(join_m[(COMPUTE_WARPS + w) * C::HEADS + h] - ref);
+          const float4 x = *reinterpret_cast<const float4*>(join + (w * C::HEADS + h) * (DH + PAD) + d);
+          sum += join_m[(2 * COMPUTE_WARPS + w) * C::HEADS + h] * fl;
+          acc.x += x.x * fo; acc.y += x.y * fo; acc.z += x.z * fo; acc.w += x.w * fo;
+        }
+        if (whole) {
+          const int head = kvh * g.group + h0 + h;
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;            // every page absent: zeros
+          const size_t at = (size_t)p.s * g.a.heads + head;
+          *reinterpret_cast<uint2*>(g.a.out + at * DH + d) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+          if (d == 0 && g.a.lse) g.a.lse[at] = sum == 0.f ? -INFINITY : (log2f(sum) + top) * 0.6931471805599453f;
+        } else {
+          *reinterpret_cast<float4*>(part + h * DH + d) = acc;
+          if (d == 0) { part[C::HEADS * DH + 2 * h] = top; part[C::HEADS * DH + 2 * h + 1] = sum; }
+        }
+      }
+      if (p.first && !p.last) {
+        // the item goes on in the CTAs behind this one, each of which finds it at the start of its run
+        const long long units = units_of(g, p.len);
+        const long long item0 = begin + chunk - (p.t1 - p.t0);       // this piece ends this CTA's run (whole items are not cut)
+        mine = Join{p.s, p.part, (int)((item0 + units - 1) / chunk - b + 1), slot};
+      }
+      ++pieces_done;
+      compute_warps_sync();                                          // the joining buffer is free again
+    }
+    if (tid == 0) *reinterpret_cast<Join*>(g.a.workspace + b * 4) = mine;
+  }
   __syncthreads();
-  float top = -INFINITY, total = 0.f;
-  for (int w = 0; w < WARPS; ++w) top = fmaxf(top, sm[w]);
-  for (int w = 0; w < WARPS; ++w) if (sm[w] > -INFINITY || sl[w] != 0.f) total += sl[w] * expf(sm[w] - top);
-  const bool empty = total == 0.f;               // NaN is not empty
-  for (int j = threadIdx.x; j < DH; j += WARPS * 32) {
-    float x = 0.f;
-    for (int w = 0; w < WARPS; ++w) if (sm[w] > -INFINITY || sl[w] != 0.f) x += so[w][j] * expf(sm[w] - top);
-    g.out[((size_t)s * g.heads + h) * DH + j] = __float2bfloat16_rn(empty ? 0.f : x / total);
+  if (tid == 0 && *abort_flag && g.a.status) atomicMax(g.a.status, (int)DS_WAIT_EXPIRED);
+}
+
+// Joins the pieces of an item that was cut, one block per (first CTA of the item, head), in the order of the pieces.
+constexpr int JOIN_THREADS = 128;
+template <int DH, int NT>
+__global__ void __launch_bounds__(JOIN_THREADS)
+attention_join_kernel(const __grid_constant__ Args g) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  constexpr int HEADS = 8 * NT, LANES = DH / 4, RUNS = JOIN_THREADS / LANES;
+  const Join j = *reinterpret_cast<const Join*>(g.a.workspace + blockIdx.x * 4);
+  const int h = blockIdx.y, kvh = j.part / g.parts, h0 = (j.part % g.parts) * HEADS;
+  if (j.pieces == 0 || h0 + h >= g.group) return;
+  const int next = 2 * blockIdx.x + 2;                               // slot of the second piece; the others follow two by two
+  auto part = [&](int i) { return g.a.workspace + SLOT0 + (size_t)(i == 0 ? j.slot : next + 2 * (i - 1)) * Slot<DH, NT>::FLOATS; };
+  __shared__ float weight[MAX_CTAS];
+  __shared__ float red[JOIN_THREADS / 32];
+  __shared__ float4 accs[RUNS][LANES];
+  const int tid = threadIdx.x;
+  float top = -INFINITY;
+  for (int i = tid; i < j.pieces; i += JOIN_THREADS) top = fmaxf(top, part(i)[HEADS * DH + 2 * h]);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  if ((tid & 31) == 0) red[tid >> 5] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  const float ref = top == -INFINITY ? 0.f : top;
+  for (int i = tid; i < j.pieces; i += JOIN_THREADS) weight[i] = exp2_fast(part(i)[HEADS * DH + 2 * h] - ref);
+  __syncthreads();
+  const int run = tid / LANES, d = (tid % LANES) * 4;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int i = run; i < j.pieces; i += RUNS) {
+    const float4 x = *reinterpret_cast<const float4*>(part(i) + h * DH + d);
+    const float w = weight[i];
+    acc.x += x.x * w; acc.y += x.y * w; acc.z += x.z * w; acc.w += x.w * w;
   }
-  if (g.lse && threadIdx.x == 0) g.lse[(size_t)s * g.heads + h] = empty ? -INFINITY : logf(total) + top;
+  accs[run][tid % LANES] = acc;
+  float sum = 0.f;
+  for (int i = 0; i < j.pieces; ++i) sum += part(i)[HEADS * DH + 2 * h + 1] * weight[i];
+  __syncthreads();
+  if (run == 0) {
+    for (int r = 1; r < RUNS; ++r) {
+      const float4 x = accs[r][tid];
+      acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const size_t at = (size_t)j.seq * g.a.heads + kvh * g.group + h0 + h;
+    *reinterpret_cast<uint2*>(g.a.out + at * DH + d) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    if (tid == 0 && g.a.lse) g.a.lse[at] = sum == 0.f ? -INFINITY : (log2f(sum) + top) * 0.6931471805599453f;
+  }
+}
+
+bool make_cache_map(CUtensorMap* out, const PagedCache& c) {
+  EncodeTiledFn fn = tensor_map_encoder();
+  if (!fn) return false;
+  const bool e4m3 = c.scale != nullptr;
+  const int row = c.head_dim * (e4m3 ? 1 : 2), box_row = row > 128 ? 128 : row;
+  const cuuint64_t dims[2] = {(cuuint64_t)c.head_dim, ((cuuint64_t)c.n_pages * 2 * c.kv_heads) << c.page_shift};
+  const cuuint64_t strides[1] = {(cuuint64_t)row};
+  const cuuint32_t box[2] = {(cuuint32_t)(box_row / (e4m3 ? 1 : 2)), (cuuint32_t)(1 << (c.page_shift < 6 ? c.page_shift : 6))};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(out, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.data, dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, box_row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DH, bool E4M3, int NT>
+cudaError_t launch(const CUtensorMap& map, const Args& g, int ctas, cudaStream_t s) {
+  using C = Cfg<DH, E4M3, NT>;
+  static bool ready[64] = {};                                        // per device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64 || !ready[dev]) {
+    e = cudaFuncSetAttribute(attention_paged_kernel<DH, E4M3, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) ready[dev] = true;
+  }
+  ET_COUNT_LAUNCH();
+  attention_paged_kernel<DH, E4M3, NT><<<ctas, THREADS, C::SMEM, s>>>(map, g);
+  e = cudaGetLastError();
+  if (e != cudaSuccess || g.whole) return e;
+  ET_COUNT_LAUNCH();
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas, g.group < C::HEADS ? g.group : C::HEADS);
+  cfg.blockDim = dim3(JOIN_THREADS);
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, attention_join_kernel<DH, NT>, g);
 }
 
 }  // namespace
 
 cudaError_t launch_attention_paged(const PagedCache& c, const PagedAttention& a, cudaStream_t s) {
-  ET_COUNT_LAUNCH();
-  const int blocks = a.n_seq * a.heads;
-  if (c.head_dim == 64) {
-    if (c.scale) attention_paged_kernel<64, true><<<blocks, WARPS * 32, 0, s>>>(c, a);
-    else attention_paged_kernel<64, false><<<blocks, WARPS * 32, 0, s>>>(c, a);
-  } else {
-    if (c.scale) attention_paged_kernel<128, true><<<blocks, WARPS * 32, 0, s>>>(c, a);
-    else attention_paged_kernel<128, false><<<blocks, WARPS * 32, 0, s>>>(c, a);
-  }
-  return cudaGetLastError();
+  CUtensorMap map;
+  if (!make_cache_map(&map, c)) return cudaErrorUnknown;
+  Args g;
+  g.c = c; g.a = a;
+  g.group = a.heads / c.kv_heads;
+  const int nt = g.group <= 8 ? 1 : 2;
+  g.parts = (g.group + 8 * nt - 1) / (8 * nt);
+  const long long tiles = (((long long)a.max_pages << c.page_shift) + TILE - 1) / TILE;      // of the longest sequence there can be
+  g.whole = tiles <= 4;
+  const long long most = (long long)a.n_seq * c.kv_heads * g.parts * (g.whole ? 1 : tiles);
+  const int ctas = (int)(most < MAX_CTAS ? most : MAX_CTAS);
+#define ET_PAGED(D, E) (nt == 1 ? launch<D, E, 1>(map, g, ctas, s) : launch<D, E, 2>(map, g, ctas, s))
+  if (c.head_dim == 64) return c.scale ? ET_PAGED(64, true) : ET_PAGED(64, false);
+  return c.scale ? ET_PAGED(128, true) : ET_PAGED(128, false);
+#undef ET_PAGED
 }
 
 }  // namespace et

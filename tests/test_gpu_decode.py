@@ -330,6 +330,44 @@ def test_attention(B, case, d, e4m3):
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("heads,kvh,page,d", [(56, 8, 64, 128), (80, 8, 16, 128), (8, 8, 32, 64), (128, 8, 128, 64)])
+def test_attention_long_runs(B, heads, kvh, page, d, e4m3):
+    """Enough positions that every CTA goes round its ring of stages many times, pages out of order, a second sequence behind the
+    long one; reference in 64 bits on the GPU."""
+    import torch
+    rng = np.random.default_rng(heads + e4m3)
+    lens, gen = [40000, 777], torch.Generator(device="cuda").manual_seed(heads)
+    max_pages = (max(lens) + page - 1) // page
+    n_pages = 2 * max_pages
+    table = i32(rng.permutation(n_pages).reshape(2, max_pages))
+    rows = torch.randn((sum(lens), 2 * kvh * d), device="cuda", generator=gen, dtype=torch.bfloat16)
+    data = torch.zeros((n_pages, 2, kvh, page, d), device="cuda", dtype=torch.float8_e4m3fn if e4m3 else torch.bfloat16)
+    scale = torch.zeros((n_pages, 2, kvh, page), device="cuda", dtype=torch.uint8) if e4m3 else None
+    start, offsets = i32([0, 0]), i32([0, lens[0], sum(lens)])
+    B.et_kv_append(data, scale, rows, 0, table, start, offsets)
+    stored = B.et_kv_read(data, scale, table, start, sum(lens), offsets).double().view(-1, 2, kvh, d)
+    q = torch.randn((2, heads * d), device="cuda", generator=gen, dtype=torch.bfloat16)
+    lse = torch.empty((2, heads), device="cuda")
+    for _ in range(3):
+        status = i32([0])
+        out = B.et_attention_paged(q, heads, data, scale, table, i32(lens), lse=lse, status=status)
+        assert status.item() == 0
+        for s in range(2):
+            k, v = (stored[offsets[s]:offsets[s + 1], i].permute(1, 0, 2) for i in (0, 1))
+            qs = q[s].double().view(kvh, heads // kvh, d)
+            z = qs @ k.transpose(1, 2) / math.sqrt(d)
+            size = (qs.abs() @ k.abs().transpose(1, 2)).amax(-1) / math.sqrt(d)
+            p = torch.softmax(z, -1)
+            want, mass = p @ v, p @ v.abs()
+            drift = d * 2.0 ** -23 * size + 2.0 ** -20
+            off = (out[s].double().view_as(want) - want).abs()
+            # a sum of n positive weights in fp32, pieces of at most 64 of them joined: n / 64 more roundings
+            tol = BF16 * want.abs() + ((2.0 ** -11 + 2 * drift).unsqueeze(-1) + lens[s] / 64 * 2.0 ** -23) * mass
+            assert (off <= tol).all()
+            assert ((lse[s].double().view(kvh, -1) - torch.logsumexp(z, -1)).abs() <= drift + lens[s] / 64 * 2.0 ** -23 + 2.0 ** -19).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
 def test_attention_peaked_and_far_apart_scores(B, e4m3):
     """Scores from one key that takes all to thousands apart, growing and falling along the cache; queries of very different
     sizes; values of very different sizes, the large ones where nothing looks."""
