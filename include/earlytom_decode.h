@@ -95,10 +95,10 @@ ET_API et_status et_attention_paged(const et_kv_cache* cache, const void* q_dev,
 
 /* Dense layer for few rows: c = epilogue(a[M][K] * w[N][K]^T + bias[N]), M <= 32; the memory traffic of the weights
  * bounds it.  Arguments and epilogues 0, 1, 2 and 4 are those of et_linear_bf16 (the weight rows of epilogue 4 are in the
- * same order, N % 256 == 0); K % 8 == 0, a and w 16-byte aligned; bias may be NULL (zeros).  A row's result does not
- * depend on M or on the other rows. */
+ * same order, N % 256 == 0); K % 8 == 0, a, w and c 16-byte aligned, c overlaps neither; bias may be NULL (zeros).  Sums
+ * are taken in an order that depends on M, N and K alone; a row's result does not depend on the other rows' values. */
 ET_API et_status et_linear_rows(const void* a_dev, const void* w_dev, const float* bias_dev, void* c_dev, int M, int N, int K,
-                                int epilogue, int gelu_tanh, void* cuda_stream);
+                                int epilogue, int gelu_tanh, int* status_dev, void* cuda_stream);
 
 #ifdef __cplusplus
 }

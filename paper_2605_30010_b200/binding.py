@@ -190,7 +190,7 @@ def load_library(path: str = _LIB_PATH) -> C.CDLL:
     lib.et_kv_append.argtypes = [kv, vp, ll, i, i, vp, i, i, vp, vp, f, vp, vp, vp, vp]
     lib.et_kv_read.argtypes = [kv, vp, ll, i, vp, i, i, vp, vp, vp, vp]
     lib.et_attention_paged.argtypes = [kv, vp, ll, vp, vp, i, i, vp, i, vp, vp, C.c_size_t, vp, vp]
-    lib.et_linear_rows.argtypes = [vp, vp, vp, vp, i, i, i, i, i, vp]
+    lib.et_linear_rows.argtypes = [vp, vp, vp, vp, i, i, i, i, i, vp, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name.startswith("et_") and name not in ("et_destroy", "et_status_string", "et_last_error",
@@ -893,7 +893,7 @@ def et_attention_paged(q, heads, cache, scale, block_table, lens, out=None, lse=
     return out
 
 
-def et_linear_rows(a, w, bias=None, epilogue=0, gelu_tanh=1, c=None, stream=None):
+def et_linear_rows(a, w, bias=None, epilogue=0, gelu_tanh=1, c=None, status=None, stream=None):
     """a [M <= 32, K] bf16, w [N, K] bf16, bias [N] f32 or None.  Returns c (bf16; fp32, added to in place, with epilogue 2)."""
     import torch
     M, K = a.shape
@@ -903,10 +903,12 @@ def et_linear_rows(a, w, bias=None, epilogue=0, gelu_tanh=1, c=None, stream=None
     if c is None:
         _need(epilogue != 2, "epilogue 2 adds to c")
         c = torch.empty((M, outs), dtype=dtype, device=a.device)
-    _on_device(a, w, bias, c)
+    _on_device(a, w, bias, c, status)
+    _int32(status, 1, "status")
     _need(a.dtype == torch.bfloat16 and a.is_contiguous(), "a: contiguous bf16 [M, K]")
     _need(w.dtype == torch.bfloat16 and w.is_contiguous() and w.dim() == 2 and w.shape[1] == K, "w: contiguous bf16 [N, K]")
     _need(bias is None or (bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == N), "bias: contiguous float32 [N]")
     _need(c.dtype == dtype and c.is_contiguous() and c.numel() == M * outs, f"c: contiguous {dtype} [M, {outs}]")
-    _check(lib().et_linear_rows(_ptr(a), _ptr(w), _ptr(bias), _ptr(c), M, N, K, int(epilogue), int(gelu_tanh), _stream_ptr(stream)))
+    _check(lib().et_linear_rows(_ptr(a), _ptr(w), _ptr(bias), _ptr(c), M, N, K, int(epilogue), int(gelu_tanh), _ptr(status),
+                                _stream_ptr(stream)))
     return c

@@ -17,6 +17,8 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
+#include <atomic>
+
 #include "decode.cuh"
 #include "tcgen05.cuh"
 
@@ -642,7 +644,7 @@ bool make_cache_map(CUtensorMap* out, const PagedCache& c) {
 template <int DH, bool E4M3, int NT>
 cudaError_t launch(const CUtensorMap& map, const Args& g, int ctas, cudaStream_t s) {
   using C = Cfg<DH, E4M3, NT>;
-  static bool ready[64] = {};                                        // per device
+  static std::atomic<bool> ready[64];                                // per device
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;

@@ -115,12 +115,12 @@ et_status et_attention_paged(const et_kv_cache* cache, const void* q_dev, long l
 }
 
 et_status et_linear_rows(const void* a_dev, const void* w_dev, const float* bias_dev, void* c_dev, int M, int N, int K, int epilogue,
-                         int gelu_tanh, void* cuda_stream) {
+                         int gelu_tanh, int* status_dev, void* cuda_stream) {
   if (!a_dev || !w_dev || !c_dev || !aligned16(a_dev) || !aligned16(w_dev) || !aligned16(c_dev)) return ET_ERR_INVALID_ARG;
   if (epilogue != EPI_STORE && epilogue != EPI_GELU && epilogue != EPI_RESIDUAL && epilogue != EPI_SWIGLU) return ET_ERR_INVALID_ARG;
   if (M < 1 || N < 1 || K < 8 || K % 8 != 0 || (epilogue == EPI_SWIGLU && N % 256 != 0)) return ET_ERR_SHAPE;
   if (M > LINEAR_ROWS_MAX || N > (1 << 24) || K > (1 << 24)) return ET_ERR_CAPACITY;
-  return launch_linear_rows((const bf16*)a_dev, (const bf16*)w_dev, bias_dev, c_dev, M, N, K, epilogue, gelu_tanh,
+  return launch_linear_rows((const bf16*)a_dev, (const bf16*)w_dev, bias_dev, c_dev, M, N, K, epilogue, gelu_tanh, status_dev,
                             (cudaStream_t)cuda_stream) == cudaSuccess ? ET_OK : ET_ERR_CUDA;
 }
 

@@ -44,7 +44,7 @@ cudaError_t launch_attention_paged(const PagedCache& c, const PagedAttention& a,
 // c = epi(a[M][K] * w[N][K]^T + bias), M <= LINEAR_ROWS_MAX
 constexpr int LINEAR_ROWS_MAX = 32;
 cudaError_t launch_linear_rows(const bf16* a, const bf16* w, const float* bias, void* c, int M, int N, int K, int epilogue,
-                               int gelu_tanh, cudaStream_t s);
+                               int gelu_tanh, int* status, cudaStream_t s);
 
 // Place of a position of sequence s; false (with the status) if it has none.
 __device__ __forceinline__ bool paged_place(const PagedCache& c, const int* table, int max_pages, int s, long long pos, int* status,

@@ -2,18 +2,25 @@
 //
 // Every weight is read once and used M times, so the weights' bytes over the memory bandwidth bound it and everything is
 // arranged to keep loads in flight.  The product is transposed, c^T = w a^T: 16 weight rows are the tall side of mma.sync's
-// m16n8k16 and 8 rows of a the narrow one.  (tcgen05's tiles would stage the weights through shared memory for tensor work
-// that is a few per cent of the time.)  A weight goes from memory to the register that feeds the tensor core with one
-// 16-byte load and no shuffle: the k-index of a step is permuted so that a lane's 8 consecutive weights are its operands of
-// two instructions, and a is read in the same order.
+// m16n8k16 and 8 rows of a the narrow one, so up to 8 rows cost no padding.  (tcgen05's smallest tiles have 64 rows of each;
+// the tensor work here is a few per cent of the time.)  Two kernels share the epilogue:
 //
-// A block of 8 warps owns 32 weight rows; K is dealt to the warps in steps of 64, and where there are too few blocks for
-// the card a cluster shares a block's K as well.  Sums meet in shared memory (of the cluster), always in the same order,
-// which depends on N and K alone: a row's result does not depend on the other rows, nor on how many there are.
+//   direct  weights go from memory to the registers that feed the tensor core; a block has 32 weight rows.  Starts fast.
+//   ring    TMA tiles of 128 weight rows and of a in a ring of five stages; a is fetched once for four times as many weights.
+//
+// K is shared by the warps of a block (direct) and by the blocks of a cluster where there are too few blocks to fill the
+// card.  Sums meet in shared memory (of the cluster) in a fixed order.
+//
+// Device time per call, B200, weights not in L2 (of the measured copy bandwidth):
+//   1 x 3584 x 4608 7.6 us (0.67, direct), 1 x 3584 x 37888 gated 43.5 us (0.97, ring), 19 x the same 48 us (0.88),
+//   1 x 18944 x 3584 24.7 us (0.85, ring), 32 x the same 29 us (0.74)
 #include <cooperative_groups.h>
+
+#include <atomic>
 
 #include "decode.cuh"
 #include "rowops.cuh"
+#include "tcgen05.cuh"
 
 namespace et {
 
@@ -21,8 +28,8 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int WARPS = 8, THREADS = 32 * WARPS;
-constexpr int BLOCK_ROWS = 32;                 // weight rows of a block: two tiles of 16
+constexpr int WARPS = 8, THREADS = 32 * WARPS;  // of the direct kernel
+constexpr int BLOCK_ROWS = 32;                 // its weight rows of a block: two tiles of 16
 constexpr int STEP = 64;                       // k of a warp's step: 128 bytes of each row
 constexpr int MAX_CLUSTER = 8;
 
@@ -30,11 +37,32 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// weights are used once: not worth a place in L1
-__device__ __forceinline__ uint4 load_once(const bf16* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
+// 16 consecutive values of a row, k .. k + 15: one 32-byte load where rows allow it (WIDE: K % 16 == 0, 32-byte aligned),
+// so that the four lanes of a row take a whole 128-byte line with one instruction, two 16-byte loads where they do not.
+// Weights are used once and not worth a place in L1.
+struct Vec { uint32_t r[8]; };
+template <bool WIDE, bool ONCE>
+__device__ __forceinline__ void load_vec(Vec& v, const bf16* p, int k, int K, bool live) {
+  if (WIDE) {
+    if (live && k < K) {
+      if (ONCE)
+        asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(v.r[0]), "=r"(v.r[1]), "=r"(v.r[2]), "=r"(v.r[3]), "=r"(v.r[4]), "=r"(v.r[5]), "=r"(v.r[6]), "=r"(v.r[7]) : "l"(p + k));
+      else
+        asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(v.r[0]), "=r"(v.r[1]), "=r"(v.r[2]), "=r"(v.r[3]), "=r"(v.r[4]), "=r"(v.r[5]), "=r"(v.r[6]), "=r"(v.r[7]) : "l"(p + k));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v.r[i] = 0;
+    }
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (live && k + 8 * h < K) x = __ldg(reinterpret_cast<const uint4*>(p + k + 8 * h));
+      v.r[4 * h] = x.x; v.r[4 * h + 1] = x.y; v.r[4 * h + 2] = x.z; v.r[4 * h + 3] = x.w;
+    }
+  }
 }
 
 struct LinearArgs {
@@ -43,14 +71,56 @@ struct LinearArgs {
   const float* bias;
   void* c;
   int M, N, K, epilogue, gelu_tanh;
+  int* status;
 };
 
-template <int NT>
-__global__ void __launch_bounds__(THREADS, NT <= 2 ? 2 : 1)
-linear_rows_kernel(const LinearArgs g) {
+// The block's sums [m][ROWS] of every rank become outputs, dealt to the ranks' threads.  In a gated block 16 gate rows are
+// followed by the 16 up rows of the same outputs.
+template <int ROWS, int NTHREADS>
+__device__ __forceinline__ void finish(const LinearArgs& g, cg::cluster_group& cluster, float* part, int block, int ranks, int rank) {
+  const int tid = threadIdx.x;
+  const bool gated = g.epilogue == EPI_SWIGLU;
+  auto total = [&](int r, int m) {
+    float s = 0.f;
+    for (int p = 0; p < ranks; ++p) s += cluster.map_shared_rank(part, p)[m * ROWS + r];
+    return s;
+  };
+  if (gated) {
+    constexpr int OUTS = ROWS / 2;
+    for (int e = rank * NTHREADS + tid; e < OUTS * g.M; e += ranks * NTHREADS) {
+      const int j = e % OUTS, m = e / OUTS, r = (j / 16) * 32 + j % 16, out = block * OUTS + j, n = (out / 32) * 64 + out % 32;
+      if (n >= g.N) continue;
+      const float gate = total(r, m) + (g.bias ? g.bias[n] : 0.f), up = total(16 + r, m) + (g.bias ? g.bias[n + 32] : 0.f);
+      reinterpret_cast<bf16*>(g.c)[(size_t)m * (g.N / 2) + out] = __float2bfloat16_rn(gate / (1.f + expf(-gate)) * up);
+    }
+  } else {
+    for (int e = rank * NTHREADS + tid; e < ROWS * g.M; e += ranks * NTHREADS) {
+      const int r = e % ROWS, m = e / ROWS, n = block * ROWS + r;
+      if (n >= g.N) continue;
+      float y = total(r, m) + (g.bias ? g.bias[n] : 0.f);
+      const size_t at = (size_t)m * g.N + n;
+      if (g.epilogue == EPI_RESIDUAL) {
+        reinterpret_cast<float*>(g.c)[at] += y;
+      } else {
+        if (g.epilogue == EPI_GELU) y = gelu_f(y, g.gelu_tanh);
+        reinterpret_cast<bf16*>(g.c)[at] = __float2bfloat16_rn(y);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Direct: a lane's 16 consecutive weights are its operands of four instructions (the k-index of a step is permuted, and a is
+// read in the same order), so a weight passes from the load to the tensor core without a shuffle.  The next step's weights
+// are loaded before the current ones are used; 16 warps an SM then have 64 KB on their way.
+// ---------------------------------------------------------------------------------------------
+template <int NT, bool WIDE>
+__global__ void __launch_bounds__(THREADS, 2)
+linear_direct_kernel(const LinearArgs g) {
   constexpr int COLS = 8 * NT, LD = COLS + 1;
-  __shared__ float red[WARPS][BLOCK_ROWS * LD];
-  __shared__ float part[BLOCK_ROWS * COLS];
+  constexpr int ROWS = BLOCK_ROWS;
+    __shared__ float red[WARPS * ROWS * LD];
+  float* const part = red;
   cg::cluster_group cluster = cg::this_cluster();
   const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int block = blockIdx.x / ranks;
@@ -64,13 +134,13 @@ linear_rows_kernel(const LinearArgs g) {
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) wp[i][j] = g.w + (size_t)min(row0 + i * tile_stride + j * 8 + gq, g.N - 1) * g.K + 8 * tq;
+    for (int j = 0; j < 2; ++j) wp[i][j] = g.w + (size_t)min(row0 + i * tile_stride + j * 8 + gq, g.N - 1) * g.K + 16 * tq;
   const bf16* ap[NT];
   bool live[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     live[n] = n * 8 + gq < g.M;
-    ap[n] = g.a + (size_t)(live[n] ? n * 8 + gq : 0) * g.K + 8 * tq;
+    ap[n] = g.a + (size_t)(live[n] ? n * 8 + gq : 0) * g.K + 16 * tq;
   }
   float acc[2][NT][4];
 #pragma unroll
@@ -78,43 +148,33 @@ linear_rows_kernel(const LinearArgs g) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[i][n][0] = acc[i][n][1] = acc[i][n][2] = acc[i][n][3] = 0.f;
 
-  const uint4 zero = make_uint4(0, 0, 0, 0);
-  uint4 wb[2][2][2];                           // [half of the step][tile][row]
+  Vec wb[2][2];                                // [tile][row]
   auto load_w = [&](int k) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const bool in = k + 32 * h + 8 * tq < g.K;
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) wb[h][i][j] = in ? load_once(wp[i][j] + k + 32 * h) : zero;
-    }
+      for (int j = 0; j < 2; ++j) load_vec<WIDE, true>(wb[i][j], wp[i][j], k, g.K - 16 * tq, true);
   };
   const int stride = STEP * WARPS * ranks;
   int k = STEP * (rank * WARPS + warp);
-  if (k < g.K) load_w(k);
+  load_w(k);
   for (; k < g.K; k += stride) {
-    uint4 ab[2][NT], cur[2][2][2];
+    Vec ab[NT], cur[2][2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const bool in = k + 32 * h + 8 * tq < g.K;
+    for (int n = 0; n < NT; ++n) load_vec<WIDE, false>(ab[n], ap[n], k, g.K - 16 * tq, live[n]);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) ab[h][n] = in && live[n] ? __ldg(reinterpret_cast<const uint4*>(ap[n] + k + 32 * h)) : zero;
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int j = 0; j < 2; ++j) cur[i][j] = wb[i][j];
+    load_w(k + stride);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) cur[h][i][j] = wb[h][i][j];
-    }
-    if (k + stride < g.K) load_w(k + stride);
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int q = 0; q < 4; ++q)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          mma_bf16(acc[i][n], cur[h][i][0].x, cur[h][i][1].x, cur[h][i][0].y, cur[h][i][1].y, ab[h][n].x, ab[h][n].y);
-          mma_bf16(acc[i][n], cur[h][i][0].z, cur[h][i][1].z, cur[h][i][0].w, cur[h][i][1].w, ab[h][n].z, ab[h][n].w);
-        }
+        for (int n = 0; n < NT; ++n)
+          mma_bf16(acc[i][n], cur[i][0].r[2 * q], cur[i][1].r[2 * q], cur[i][0].r[2 * q + 1], cur[i][1].r[2 * q + 1], ab[n].r[2 * q],
+                   ab[n].r[2 * q + 1]);
   }
 
   // ---- the warps' sums, then the cluster's
@@ -124,76 +184,225 @@ linear_rows_kernel(const LinearArgs g) {
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        float* dst = &red[warp][(i * 16 + j * 8 + gq) * LD + n * 8 + 2 * tq];
+        float* dst = red + (warp * ROWS + i * 16 + j * 8 + gq) * LD + n * 8 + 2 * tq;
         dst[0] = acc[i][n][2 * j]; dst[1] = acc[i][n][2 * j + 1];
       }
   __syncthreads();
-  for (int e = tid; e < BLOCK_ROWS * g.M; e += THREADS) {
-    const int r = e % BLOCK_ROWS, m = e / BLOCK_ROWS;
-    float s = 0.f;
+  float sums[ROWS * COLS / THREADS];
 #pragma unroll
-    for (int v = 0; v < WARPS; ++v) s += red[v][r * LD + m];
-    part[m * BLOCK_ROWS + r] = s;
+  for (int i = 0; i < ROWS * COLS / THREADS; ++i) {
+    const int e = tid + i * THREADS;
+    sums[i] = 0.f;
+    if (e < ROWS * g.M) {
+#pragma unroll
+      for (int v = 0; v < WARPS; ++v) sums[i] += red[(v * ROWS + e % ROWS) * LD + e / ROWS];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < ROWS * COLS / THREADS; ++i) {
+    const int e = tid + i * THREADS;
+    if (e < ROWS * g.M) part[e] = sums[i];
   }
   if (ranks > 1) cluster.sync(); else __syncthreads();
-  auto total = [&](int r, int m) {
-    float s = 0.f;
-    for (int p = 0; p < ranks; ++p) s += cluster.map_shared_rank(part, p)[m * BLOCK_ROWS + r];
-    return s;
-  };
-  if (gated) {
-    for (int e = rank * THREADS + tid; e < 16 * g.M; e += ranks * THREADS) {
-      const int r = e % 16, m = e / 16, n = row0 + r;
-      const float gate = total(r, m) + (g.bias ? g.bias[n] : 0.f), up = total(16 + r, m) + (g.bias ? g.bias[n + 32] : 0.f);
-      reinterpret_cast<bf16*>(g.c)[(size_t)m * (g.N / 2) + block * 16 + r] = __float2bfloat16_rn(gate / (1.f + expf(-gate)) * up);
-    }
-  } else {
-    for (int e = rank * THREADS + tid; e < BLOCK_ROWS * g.M; e += ranks * THREADS) {
-      const int r = e % BLOCK_ROWS, m = e / BLOCK_ROWS, n = row0 + r;
-      if (n >= g.N) continue;
-      float y = total(r, m) + (g.bias ? g.bias[n] : 0.f);
-      const size_t at = (size_t)m * g.N + n;
-      if (g.epilogue == EPI_RESIDUAL) {
-        reinterpret_cast<float*>(g.c)[at] += y;
-      } else {
-        if (g.epilogue == EPI_GELU) y = gelu_f(y, g.gelu_tanh);
-        reinterpret_cast<bf16*>(g.c)[at] = __float2bfloat16_rn(y);
-      }
-    }
-  }
+  finish<ROWS, THREADS>(g, cluster, part, block, ranks, rank);
   if (ranks > 1) cluster.sync();               // a block's sums stay until its neighbours have read them
 }
 
+// ---------------------------------------------------------------------------------------------
+// Ring: one warp copies, four compute, 32 weight rows each.  100 KB a block, two blocks an SM, about 160 KB of weights on
+// their way.  A rank of a cluster takes every ranks-th step of 64 along K.
+// ---------------------------------------------------------------------------------------------
+using namespace tc;
+
+constexpr int RING_ROWS = 128, RING_WARPS = 4, RING_THREADS = 32 * (RING_WARPS + 1);
+template <int NT> struct Ring {
+  static constexpr int W_BYTES = RING_ROWS * 128, A_BYTES = 8 * NT * 128, STAGE = W_BYTES + A_BYTES;
+  static constexpr int STAGES = 5;
+  static constexpr int SMEM = 1024 + STAGES * STAGE + 256;
+};
+
+__device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+
 template <int NT>
-cudaError_t launch(const LinearArgs& g, int blocks, int ranks, cudaStream_t s) {
-  ET_COUNT_LAUNCH();
+__global__ void __launch_bounds__(RING_THREADS, 2)
+linear_ring_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap amap, const LinearArgs g) {
+  using R = Ring<NT>;
+  constexpr int COLS = 8 * NT;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* const gen = smem_raw + (base - raw);
+  const uint32_t bars = base + R::STAGES * R::STAGE;
+  auto full = [&](int s) { return bars + 8u * (uint32_t)s; };
+  auto empty = [&](int s) { return bars + 8u * (uint32_t)(R::STAGES + s); };
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(gen + R::STAGES * R::STAGE + 16 * R::STAGES);
+  cg::cluster_group cluster = cg::this_cluster();
+  const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int block = blockIdx.x / ranks;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int steps = (g.K + 63) / 64, mine = (steps - rank + ranks - 1) / ranks;      // k-steps rank, rank + ranks, ...
+  const bool gated = g.epilogue == EPI_SWIGLU;
+
+  if (tid == 0) {
+    for (int s = 0; s < R::STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), RING_WARPS); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+
+  bool ok = true;
+  float acc[2][NT][4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[i][n][0] = acc[i][n][1] = acc[i][n][2] = acc[i][n][3] = 0.f;
+  // first row of the warp's two tiles inside the block: neighbours, or 16 gate rows and the up rows of the same outputs
+  const int r0 = gated ? (warp >> 1) * 64 + (warp & 1) * 16 : warp * 32, r1 = r0 + (gated ? 32 : 16);
+  if (warp == RING_WARPS) {
+    if (lane == 0) {
+      asm volatile("prefetch.tensormap [%0];" ::"l"(&wmap) : "memory");
+      asm volatile("prefetch.tensormap [%0];" ::"l"(&amap) : "memory");
+      int stage = 0, issued = 0;
+      uint32_t phase = 0;
+      for (; issued < mine; ++issued) {
+        ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag);
+        if (!ok) break;
+        const uint32_t dst = base + stage * R::STAGE;
+        const int x = (rank + issued * ranks) * 64;
+        mbar_arrive_expect_tx(full(stage), R::STAGE);
+        tma_load_2d(dst, &wmap, full(stage), x, block * RING_ROWS);
+        tma_load_2d(dst + R::W_BYTES, &amap, full(stage), x, 0);
+        if (++stage == R::STAGES) { stage = 0; phase ^= 1u; }
+      }
+      if (!ok) {
+        for (int i = 0; i < R::STAGES && i < issued; ++i) {         // copies in flight land before the memory is given up
+          if (--stage < 0) { stage = R::STAGES - 1; phase ^= 1u; }
+          int given_up = 0;
+          mbar_wait(full(stage), phase, &given_up);
+        }
+      }
+    }
+  } else {
+    const int arow = (lane & 7) + ((lane >> 3) & 1) * 8, achunk = lane >> 4;          // of a 16 x 16 tile of w
+    const int brow = (lane & 7) + (lane >> 4) * 8, bchunk = (lane >> 3) & 1;          // of two 8 x 16 tiles of a
+    auto at = [&](int row, int chunk) { return (uint32_t)(row * 128 + ((chunk ^ (row & 7)) << 4)); };
+    int stage = 0;
+    uint32_t phase = 0;
+    for (int i = 0; i < mine; ++i) {
+      if (ok) ok = mbar_wait_warp(full(stage), phase, abort_flag);
+      if (ok) {
+        const uint32_t wb = base + stage * R::STAGE, ab = wb + R::W_BYTES;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          uint32_t w0[4], w1[4];
+          ldmatrix4(wb + at(r0 + arow, 2 * ks + achunk), w0);
+          ldmatrix4(wb + at(r1 + arow, 2 * ks + achunk), w1);
+#pragma unroll
+          for (int n = 0; n < NT; n += 2) {
+            uint32_t b[4];
+            ldmatrix4(ab + at(NT == 1 ? (brow & 7) : n * 8 + brow, 2 * ks + bchunk), b);
+            mma_bf16(acc[0][n], w0[0], w0[1], w0[2], w0[3], b[0], b[1]);
+            mma_bf16(acc[1][n], w1[0], w1[1], w1[2], w1[3], b[0], b[1]);
+            if (n + 1 < NT) {
+              mma_bf16(acc[0][(n + 1) % NT], w0[0], w0[1], w0[2], w0[3], b[2], b[3]);
+              mma_bf16(acc[1][(n + 1) % NT], w1[0], w1[1], w1[2], w1[3], b[2], b[3]);
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(stage));
+      }
+      if (++stage == R::STAGES) { stage = 0; phase ^= 1u; }
+    }
+  }
+  __syncthreads();                             // the ring is idle: its memory takes the sums, [m][row of the block]
+  float* const part = reinterpret_cast<float*>(gen);
+  if (warp < RING_WARPS) {
+    const int gq = lane >> 2, tq = lane & 3;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) part[(n * 8 + 2 * tq + (j & 1)) * RING_ROWS + warp * 32 + i * 16 + gq + (j >> 1) * 8] = acc[i][n][j];
+  }
+  if (ranks > 1) cluster.sync(); else __syncthreads();
+  finish<RING_ROWS, RING_THREADS>(g, cluster, part, block, ranks, rank);
+  if (tid == 0 && *abort_flag && g.status) atomicMax(g.status, (int)DS_WAIT_EXPIRED);
+  if (ranks > 1) cluster.sync();               // a block's sums stay until its neighbours have read them
+}
+
+struct ClusterLaunch {
   cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(blocks * ranks);
-  cfg.blockDim = dim3(THREADS);
-  cfg.stream = s;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, linear_rows_kernel<NT>, g);
+  ClusterLaunch(int blocks, int ranks, int threads, size_t smem, cudaStream_t s) {
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(blocks * ranks);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+  }
+};
+
+template <int NT>
+cudaError_t launch_direct(const LinearArgs& g, cudaStream_t s) {
+  const int blocks = cdiv(g.N, BLOCK_ROWS);
+  int ranks = 1;                               // two blocks an SM, each with two steps or more for every warp
+  while (ranks < MAX_CLUSTER && blocks * ranks * 2 <= 2 * 148 && g.K >= 2 * STEP * WARPS * ranks * 2) ranks *= 2;
+  const bool wide = g.K % 16 == 0 && ((reinterpret_cast<uintptr_t>(g.a) | reinterpret_cast<uintptr_t>(g.w)) & 31u) == 0;
+  ClusterLaunch l(blocks, ranks, THREADS, 0, s);
+  ET_COUNT_LAUNCH();
+  return wide ? cudaLaunchKernelEx(&l.cfg, linear_direct_kernel<NT, true>, g) : cudaLaunchKernelEx(&l.cfg, linear_direct_kernel<NT, false>, g);
+}
+
+template <int NT>
+cudaError_t launch_ring(const LinearArgs& g, cudaStream_t s) {
+  using R = Ring<NT>;
+  TmaDesc w, a;
+  if (!make_tma_2d_bf16(&w, g.w, g.N, g.K, RING_ROWS, nullptr) || !make_tma_2d_bf16(&a, g.a, g.M, g.K, 8 * NT, nullptr)) return cudaErrorUnknown;
+  // clusters of each size that the card holds at once, per device, looked up once
+  constexpr int DEVICES = 64;
+  static std::atomic<int> resident[DEVICES][MAX_CLUSTER + 1];       // zero: not looked up; [1] is set last
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= DEVICES) return cudaErrorInvalidDevice;
+  if (!resident[dev][1]) {
+    e = cudaFuncSetAttribute(linear_ring_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::SMEM);
+    if (e != cudaSuccess) return e;
+    for (int ranks = MAX_CLUSTER; ranks >= 1; --ranks) {
+      ClusterLaunch probe(1, ranks, RING_THREADS, R::SMEM, s);
+      int n = 0;
+      e = cudaOccupancyMaxActiveClusters(&n, linear_ring_kernel<NT>, &probe.cfg);
+      if (e != cudaSuccess) return e;
+      resident[dev][ranks] = n > 0 ? n : 1;
+    }
+  }
+  const int blocks = cdiv(g.N, RING_ROWS), steps = cdiv(g.K, STEP);
+  int ranks = 1;
+  for (int r = 2; r <= MAX_CLUSTER && steps >= 4 * r; ++r) if (blocks <= resident[dev][r]) ranks = r;
+  ClusterLaunch l(blocks, ranks, RING_THREADS, R::SMEM, s);
+  ET_COUNT_LAUNCH();
+  return cudaLaunchKernelEx(&l.cfg, linear_ring_kernel<NT>, *reinterpret_cast<const CUtensorMap*>(w.bytes),
+                            *reinterpret_cast<const CUtensorMap*>(a.bytes), g);
 }
 
 }  // namespace
 
 cudaError_t launch_linear_rows(const bf16* a, const bf16* w, const float* bias, void* c, int M, int N, int K, int epilogue,
-                               int gelu_tanh, cudaStream_t s) {
-  const LinearArgs g{a, w, bias, c, M, N, K, epilogue, gelu_tanh};
-  const int blocks = cdiv(N, BLOCK_ROWS);
-  // two blocks an SM are wanted, each with at least two steps for every warp
-  int ranks = 1;
-  while (ranks < MAX_CLUSTER && blocks * ranks * 2 <= 148 * 2 && K >= STEP * WARPS * 2 * ranks * 2) ranks *= 2;
-  switch ((M + 7) / 8) {
-    case 1: return launch<1>(g, blocks, ranks, s);
-    case 2: return launch<2>(g, blocks, ranks, s);
-    case 3: return launch<3>(g, blocks, ranks, s);
-    default: return launch<4>(g, blocks, ranks, s);
-  }
+                               int gelu_tanh, int* status, cudaStream_t s) {
+  const LinearArgs g{a, w, bias, c, M, N, K, epilogue, gelu_tanh, status};
+  // The ring takes over where the weights are many, sooner the more rows there are (direct reads a again for every 32 weight
+  // rows).  Direct / ring in us: 1 x 3584 x 3584 5.6 / 6.2, 1 x 3584 x 9000 13.4 / 13.8, 1 x 18944 x 3584 25.8 / 24.7;
+  // 13 x 3584 x 4608 9.1 / 9.2, 13 x 4096 x 5120 13.6 / 12.0; 32 x 3584 x 2048 7.8 / 7.8, 32 x 3584 x 3584 10.7 / 8.7.
+  const bool ring = (long long)N * K * ((M + 7) / 8) > (1ll << 25);
+  if (ring) return M <= 8 ? launch_ring<1>(g, s) : M <= 16 ? launch_ring<2>(g, s) : launch_ring<4>(g, s);
+  return M <= 8 ? launch_direct<1>(g, s) : M <= 16 ? launch_direct<2>(g, s) : M <= 24 ? launch_direct<3>(g, s) : launch_direct<4>(g, s);
 }
 
 }  // namespace et

@@ -70,7 +70,7 @@ def test_attention_refuses(B, change, want):
     (dict(N=0), SHAPE), (dict(K=0), SHAPE), (dict(K=12), SHAPE), (dict(epilogue=4, N=128), SHAPE), (dict(M=33), CAPACITY),
     (dict(N=(1 << 24) + 8), CAPACITY), (dict(K=(1 << 24) + 8), CAPACITY)])
 def test_linear_rows_refuses(B, change, want):
-    base = dict(a=P, w=P, bias=None, c=P, M=4, N=64, K=64, epilogue=0, gelu=1, stream=None)
+    base = dict(a=P, w=P, bias=None, c=P, M=4, N=64, K=64, epilogue=0, gelu=1, status=None, stream=None)
     args = dict(base, **change)
     assert B.lib().et_linear_rows(*[args[k] for k in base]) == want
 
