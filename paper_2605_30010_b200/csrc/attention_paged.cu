@@ -6,7 +6,7 @@
 //   * A tile is 64 positions of one key / value head.  All tiles of the call, in the order (sequence, key / value head,
 //     tile), are cut into one equal run per CTA (one CTA per SM), so a single long sequence and a ragged batch load every
 //     SM alike.  Lengths are on the device, so each CTA works the cut out for itself.
-//   * One warp copies: TMA boxes of a page's rows (hardware swizzle, so that ldmatrix meets no bank conflicts) into a ring
+//   * Two warps copy: TMA boxes of a page's rows (hardware swizzle, so that ldmatrix meets no bank conflicts) into a ring
 //     of stages.  Eight warps compute, four to a tile, 16 positions each, every warp with a running maximum, sum and
 //     output of its own; they meet only at the end of a piece (the part of a sequence that falls into the CTA's run).
 //   * The product is transposed, S^T = K Q^T and O^T = V^T P^T, so that the query heads are the narrow side (8) of
@@ -31,8 +31,13 @@ using namespace tc;
 constexpr int TILE = 64;                       // positions
 constexpr int GROUP_WARPS = 4;                 // warps of one tile, 16 positions each
 constexpr int COMPUTE_WARPS = 8;
-constexpr int THREADS = 32 * (COMPUTE_WARPS + 1);
+constexpr int GROUPS = COMPUTE_WARPS / GROUP_WARPS;   // tiles are dealt to the groups in turn
+constexpr int THREADS = 32 * (COMPUTE_WARPS + GROUPS);
 constexpr int MAX_CTAS = 148;
+#ifndef ITEM_COST_V
+#define ITEM_COST_V 2
+#endif
+constexpr int ITEM_COST = ITEM_COST_V;                   // units (tiles' worth of time) that an item costs beside its tiles
 constexpr int PAD = 4;                         // floats between heads of the joining buffer: no bank conflicts
 constexpr int SMEM_LIMIT = 232448 - 512;       // 227 KB, less the static part
 constexpr int CONTROL_BYTES = 1024;            // barriers and the ring's flags
@@ -52,7 +57,7 @@ struct Cfg {
   // stage for the first time in its second round could take the barrier's state of the first for their own
   static constexpr int STAGES = (FIT > 12 ? 12 : FIT) & ~1;
   static constexpr int SMEM = 1024 + STAGES * (STAGE + SCALES) + JOIN + CONTROL_BYTES;
-  static_assert(STAGES >= 4 && STAGES % (COMPUTE_WARPS / GROUP_WARPS) == 0, "ring");
+  static_assert(STAGES >= 4 && STAGES % GROUPS == 0, "ring");
   static_assert(2 * 8 * STAGES + 4 * STAGES + 16 <= CONTROL_BYTES, "control area");
 };
 
@@ -105,8 +110,19 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 // 2^e for e in [-127, 127]
 __device__ __forceinline__ float pow2(int e) { return __int_as_float(e > -127 ? (e + 127) << 23 : 1 << 22); }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+// Copies by a converged warp: all lanes execute the call, one elected lane issues.
+__device__ __forceinline__ void arrive_expect_elect(uint32_t bar, uint32_t bytes) {
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+               "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void tma_load_elect(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+               "@q cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n\t}"
+               ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void bulk_load_elect(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+               "@q cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}"
                ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void compute_warps_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * COMPUTE_WARPS) : "memory"); }
@@ -122,28 +138,37 @@ __device__ __forceinline__ int clamped_len(const Args& g, int s) {
   const long long cap = (long long)g.a.max_pages << g.c.page_shift;
   return (int)min((long long)max(__ldg(g.a.len + s), 0), cap);
 }
-__device__ __forceinline__ int units_of(const Args& g, int len) { return g.whole ? (len > 0) : (len + TILE - 1) / TILE; }
+// An item's units: its tiles and, in front of them, ITEM_COST for what every item costs however short it is.
+__device__ __forceinline__ int units_of(const Args& g, int len) {
+  return len <= 0 ? 0 : g.whole ? 1 : (int)((len + (TILE - 1ll)) / TILE) + ITEM_COST;
+}
 
-struct Piece { int s, part, len, t0, t1; bool first, last; };     // tiles t0 .. t1 - 1; first / last: contains the item's first / last tile
+struct Piece {
+  int s, part, len, t0, t1;        // tiles t0 .. t1 - 1
+  int units_end;                   // the item's units up to this piece's end
+  bool first, last;                // contains the item's first, last tile
+};
 
 __device__ __forceinline__ bool next_piece(const Args& g, Walk& w, Piece& p) {
-  if (w.left <= 0) return false;
-  int len = clamped_len(g, w.s);
-  while (units_of(g, len) == 0) {                                 // only between items: the walk's units are accounted for
-    if (++w.s >= w.n_seq) return false;
-    len = clamped_len(g, w.s);
+  while (w.left > 0) {
+    const int len = clamped_len(g, w.s), units = units_of(g, len);
+    if (units == 0) {                                             // only between items
+      if (++w.s >= w.n_seq) return false;
+      continue;
+    }
+    const int n = (int)min(w.left, (long long)(units - w.unit)), end = w.unit + n;
+    p.s = w.s; p.part = w.part; p.len = len; p.units_end = end;
+    p.t0 = g.whole ? 0 : max(w.unit - ITEM_COST, 0);
+    p.t1 = g.whole ? (len + TILE - 1) / TILE : max(end - ITEM_COST, 0);
+    p.first = p.t0 == 0; p.last = end == units;
+    w.left -= n; w.unit = end;
+    if (end == units) {
+      w.unit = 0;
+      if (++w.part == w.parts_all) { w.part = 0; if (++w.s >= w.n_seq) w.left = 0; }
+    }
+    if (p.t1 > p.t0) return true;                                 // else the run ended in front of the item's first tile
   }
-  const int units = units_of(g, len), tiles = (len + TILE - 1) / TILE;
-  const int n = (int)min(w.left, (long long)(units - w.unit));
-  p.s = w.s; p.part = w.part; p.len = len;
-  p.first = w.unit == 0; p.last = w.unit + n == units;
-  p.t0 = g.whole ? 0 : w.unit; p.t1 = g.whole ? tiles : w.unit + n;
-  w.left -= n; w.unit += n;
-  if (w.unit == units) {
-    w.unit = 0;
-    if (++w.part == w.parts_all) { w.part = 0; ++w.s; if (w.s >= w.n_seq) w.left = 0; }
-  }
-  return true;
+  return false;
 }
 
 template <int DH, bool E4M3, int NT>
@@ -225,16 +250,16 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
   }
 
   bool ok = true;
-  if (warp == COMPUTE_WARPS) {
-    // ------------------------------------------------------------------ copies
+  if (warp >= COMPUTE_WARPS) {
+    // ------------------------------------------------------------------ copies: one warp for each group's tiles
+    const int my_group = warp - COMPUTE_WARPS;
     const int box_shift = min(g.c.page_shift, 6), box_rows = 1 << box_shift, boxes_tile = TILE >> box_shift;
-    constexpr int OPS = 2 * C::BOXES + (E4M3 ? 2 : 0);               // copies of one page's rows: keys, values, their scales
-    const int my_box = lane / OPS, my_op = lane % OPS;
     const uint32_t box_bytes = (uint32_t)box_rows * (2 * C::ROW + (E4M3 ? 2 : 0));
+    const int plane_rows = kv_heads << g.c.page_shift;
     if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
-    int stage = 0;
+    int stage = my_group;
     uint32_t phase = 0;
-    long long issued = 0;
+    long long count = 0, issued = 0;
     Piece p;
     while (ok && next_piece(g, walk, p)) {
       const int* table = g.a.table + (size_t)p.s * g.a.max_pages;
@@ -245,48 +270,59 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         return i < g.a.max_pages ? __ldg(table + i) : -1;
       };
       int batch = 0, ids = page_ids(0), ids_next = page_ids(1);
-      for (int t = p.t0; t < p.t1; ++t) {
-        const long long pos = (long long)t * TILE;
-        const int page0 = (int)(pos >> g.c.page_shift) - first_page;  // a multiple of the tile's pages: one batch has them all
+      int t = p.t0 + (((int)(count & 1) ^ my_group) & 1);
+      count += p.t1 - p.t0;
+      for (; t < p.t1; t += GROUPS) {
+        const int pos = t * TILE;                                     // lengths are below 2^31
+        const int page0 = (pos >> g.c.page_shift) - first_page;       // a multiple of the tile's pages: one batch has them all
         while ((page0 >> 5) > batch) { ++batch; ids = ids_next; ids_next = page_ids(batch + 1); }
-        const bool box_live = my_box < boxes_tile && pos + ((long long)my_box << box_shift) < p.len;
-        const int page = __shfl_sync(0xffffffffu, ids, (page0 + (my_box < boxes_tile ? my_box : 0)) & 31);
-        const bool good = (unsigned)page < (unsigned)g.c.n_pages;
-        const bool copy = box_live && good;
-        if (box_live && !good && g.a.status) atomicMax(g.a.status, (int)ET_PAGED_BAD_PAGE);
-        const unsigned bad = __ballot_sync(0xffffffffu, box_live && !good && my_op == 0);
-        const unsigned copies = __ballot_sync(0xffffffffu, copy && my_op == 0);
+        const int row_in_page = pos & ((1 << g.c.page_shift) - 1);
+        int row[4];                                                   // first row of each box's keys in the cache; -1: no copy
+        uint32_t bytes = 0;
+        int absent_slices = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          row[i] = -1;
+          if (i < boxes_tile && (unsigned)(pos + (i << box_shift)) < (unsigned)p.len) {
+            const int page = __shfl_sync(0xffffffffu, ids, (page0 + i) & 31);
+            if ((unsigned)page < (unsigned)g.c.n_pages) {
+              row[i] = ((page * 2 * kv_heads + kvh) << g.c.page_shift) + row_in_page;
+              bytes += box_bytes;
+            } else {
+              if (g.a.status && lane == 0) atomicMax(g.a.status, (int)ET_PAGED_BAD_PAGE);
+              absent_slices |= ((1 << (box_rows / 16)) - 1) << (i * (box_rows / 16));
+            }
+          }
+        }
         ok = mbar_wait_warp(empty(stage), phase ^ 1u, abort_flag);
         if (!ok) break;
-        if (lane == 0) {
-          int mask = 0;
-          for (int i = 0; i < boxes_tile; ++i)
-            if (bad >> (i * OPS) & 1u) mask |= ((1 << (box_rows / 16)) - 1) << (i * (box_rows / 16));
-          absent[stage] = mask;
-          mbar_arrive_expect_tx(full(stage), (uint32_t)__popc(copies) * box_bytes);
-        }
+        if (lane == 0) absent[stage] = absent_slices;
         __syncwarp();
-        if (copy) {
-          const int row0 = my_box << box_shift;                       // of the tile
-          const int place = (int)((pos + row0) & ((1 << g.c.page_shift) - 1));
-          const int plane = my_op < 2 * C::BOXES ? my_op / C::BOXES : my_op - 2 * C::BOXES;
-          const int y = (((page * 2 + plane) * kv_heads + kvh) << g.c.page_shift) + place;
-          if (my_op < 2 * C::BOXES) {
-            const int half = my_op % C::BOXES;
-            tma_load_2d(base + stage * C::STAGE + plane * C::PLANE + half * (TILE * C::BOX_ROW) + row0 * C::BOX_ROW, &map, full(stage),
-                        half * (C::BOX_ROW / (E4M3 ? 1 : 2)), y);
-          } else {
-            bulk_load(scales + stage * C::SCALES + plane * TILE + row0, g.c.scale + (size_t)(unsigned)y, (uint32_t)box_rows, full(stage));
+        const uint32_t bar = full(stage), dst = base + stage * C::STAGE, sdst = scales + stage * C::SCALES;
+        arrive_expect_elect(bar, bytes);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (row[i] >= 0) {
+            const int r0 = i << box_shift;
+#pragma unroll
+            for (int plane = 0; plane < 2; ++plane) {
+              const int y = row[i] + plane * plane_rows;
+#pragma unroll
+              for (int half = 0; half < C::BOXES; ++half)
+                tma_load_elect(dst + plane * C::PLANE + half * (TILE * C::BOX_ROW) + r0 * C::BOX_ROW, &map, bar,
+                               half * (C::BOX_ROW / (E4M3 ? 1 : 2)), y);
+              if (E4M3) bulk_load_elect(sdst + plane * TILE + r0, g.c.scale + (unsigned)y, (uint32_t)box_rows, bar);
+            }
           }
         }
         ++issued;
-        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        if ((stage += GROUPS) >= STAGES) { stage = my_group; phase ^= 1u; }
       }
     }
     if (!ok && lane == 0) {
       // copies in flight have to land before this CTA's shared memory is given up
-      for (int i = 0; i < STAGES && i < issued; ++i) {
-        if (--stage < 0) { stage = STAGES - 1; phase ^= 1u; }
+      for (int i = 0; i < STAGES / GROUPS && i < issued; ++i) {
+        if ((stage -= GROUPS) < 0) { stage = STAGES - GROUPS + my_group; phase ^= 1u; }
         int given_up = 0;
         mbar_wait(full(stage), phase, &given_up);
       }
@@ -565,7 +601,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
       if (p.first && !p.last) {
         // the item goes on in the CTAs behind this one, each of which finds it at the start of its run
         const long long units = units_of(g, p.len);
-        const long long item0 = begin + chunk - (p.t1 - p.t0);       // this piece ends this CTA's run (whole items are not cut)
+        const long long item0 = begin + chunk - p.units_end;          // this piece ends this CTA's run (whole items are not cut)
         mine = Join{p.s, p.part, (int)((item0 + units - 1) / chunk - b + 1), slot};
       }
       ++pieces_done;
