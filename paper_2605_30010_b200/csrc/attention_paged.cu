@@ -7,7 +7,7 @@
 //     tile), are cut into one equal run per CTA (one CTA per SM), so a single long sequence and a ragged batch load every
 //     SM alike.  Lengths are on the device, so each CTA works the cut out for itself.
 //   * Two warps copy: TMA boxes of a page's rows (hardware swizzle, so that ldmatrix meets no bank conflicts) into a ring
-//     of stages.  Eight warps compute, four to a tile, 16 positions each, every warp with a running maximum, sum and
+//     of stages.  Eight warps compute, two to a tile, 32 positions each, every warp with a running maximum, sum and
 //     output of its own; they meet only at the end of a piece (the part of a sequence that falls into the CTA's run).
 //   * The product is transposed, S^T = K Q^T and O^T = V^T P^T, so that the query heads are the narrow side (8) of
 //     mma.sync's m16n8k16: up to 8 heads cost no padded rows.  (tcgen05 wants 64 or more rows a tile, and the tensor work
@@ -29,10 +29,12 @@ namespace {
 using namespace tc;
 
 constexpr int TILE = 64;                       // positions
-constexpr int GROUP_WARPS = 4;                 // warps of one tile, 16 positions each
+constexpr int GROUP_WARPS = 2;                 // warps of one tile, BLOCKS blocks of 16 positions each
+constexpr int BLOCKS = TILE / 16 / GROUP_WARPS;
 constexpr int COMPUTE_WARPS = 8;
 constexpr int GROUPS = COMPUTE_WARPS / GROUP_WARPS;   // tiles are dealt to the groups in turn
-constexpr int THREADS = 32 * (COMPUTE_WARPS + GROUPS);
+constexpr int COPY_WARPS = 2;                  // each copies every other tile
+constexpr int THREADS = 32 * (COMPUTE_WARPS + COPY_WARPS);
 constexpr int MAX_CTAS = 148;
 #ifndef ITEM_COST_V
 #define ITEM_COST_V 2
@@ -53,11 +55,11 @@ struct Cfg {
   static constexpr int HEADS = 8 * NT;
   static constexpr int JOIN = COMPUTE_WARPS * HEADS * (DH + PAD) * 4 + COMPUTE_WARPS * HEADS * 3 * 4;
   static constexpr int FIT = (SMEM_LIMIT - 1024 - CONTROL_BYTES - JOIN) / (STAGE + SCALES);
-  // even, so that a stage is always the same four warps': they wait for its copies in turn, where warps that come to a
+  // a multiple of the groups, so that a stage is always the same warps': they wait for its copies in turn, where warps that come to a
   // stage for the first time in its second round could take the barrier's state of the first for their own
-  static constexpr int STAGES = (FIT > 12 ? 12 : FIT) & ~1;
+  static constexpr int STAGES = (FIT > 12 ? 12 : FIT) / GROUPS * GROUPS;
   static constexpr int SMEM = 1024 + STAGES * (STAGE + SCALES) + JOIN + CONTROL_BYTES;
-  static_assert(STAGES >= 4 && STAGES % GROUPS == 0, "ring");
+  static_assert(STAGES >= GROUPS && STAGES % COPY_WARPS == 0 && COPY_WARPS == 2, "ring");
   static_assert(2 * 8 * STAGES + 4 * STAGES + 16 <= CONTROL_BYTES, "control area");
 };
 
@@ -251,13 +253,13 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 
   bool ok = true;
   if (warp >= COMPUTE_WARPS) {
-    // ------------------------------------------------------------------ copies: one warp for each group's tiles
-    const int my_group = warp - COMPUTE_WARPS;
+    // ------------------------------------------------------------------ copies
+    const int me = warp - COMPUTE_WARPS;
     const int box_shift = min(g.c.page_shift, 6), box_rows = 1 << box_shift, boxes_tile = TILE >> box_shift;
     const uint32_t box_bytes = (uint32_t)box_rows * (2 * C::ROW + (E4M3 ? 2 : 0));
     const int plane_rows = kv_heads << g.c.page_shift;
     if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
-    int stage = my_group;
+    int stage = me;
     uint32_t phase = 0;
     long long count = 0, issued = 0;
     Piece p;
@@ -270,9 +272,9 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         return i < g.a.max_pages ? __ldg(table + i) : -1;
       };
       int batch = 0, ids = page_ids(0), ids_next = page_ids(1);
-      int t = p.t0 + (((int)(count & 1) ^ my_group) & 1);
+      int t = p.t0 + (((int)(count & 1) ^ me) & 1);
       count += p.t1 - p.t0;
-      for (; t < p.t1; t += GROUPS) {
+      for (; t < p.t1; t += COPY_WARPS) {
         const int pos = t * TILE;                                     // lengths are below 2^31
         const int page0 = (pos >> g.c.page_shift) - first_page;       // a multiple of the tile's pages: one batch has them all
         while ((page0 >> 5) > batch) { ++batch; ids = ids_next; ids_next = page_ids(batch + 1); }
@@ -316,20 +318,20 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
           }
         }
         ++issued;
-        if ((stage += GROUPS) >= STAGES) { stage = my_group; phase ^= 1u; }
+        if ((stage += COPY_WARPS) >= STAGES) { stage = me; phase ^= 1u; }
       }
     }
     if (!ok && lane == 0) {
       // copies in flight have to land before this CTA's shared memory is given up
-      for (int i = 0; i < STAGES / GROUPS && i < issued; ++i) {
-        if ((stage -= GROUPS) < 0) { stage = STAGES - GROUPS + my_group; phase ^= 1u; }
+      for (int i = 0; i < STAGES / COPY_WARPS && i < issued; ++i) {
+        if ((stage -= COPY_WARPS) < 0) { stage = STAGES - COPY_WARPS + me; phase ^= 1u; }
         int given_up = 0;
         mbar_wait(full(stage), phase, &given_up);
       }
     }
   } else {
     // ------------------------------------------------------------------ the product
-    const int my_group = warp / GROUP_WARPS, slice = warp % GROUP_WARPS, r0 = slice * 16;
+    const int my_group = warp / GROUP_WARPS, slice = (warp % GROUP_WARPS) * BLOCKS, r0 = slice * 16;    // first slice (of 16) and row
     const int gq = lane >> 2, tq = lane & 3;                         // mma's row group and column pair
     // this lane's row of the 16 and its 16-byte chunk (K: both halves of a k-step; V, transposed: see below)
     const int krow = r0 + (lane & 7) + ((lane >> 3) & 1) * 8, kchunk = lane >> 4;
@@ -408,83 +410,110 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         const int st = stage;
         const uint32_t ph = phase;
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-        if ((int)(count & 1) != my_group) continue;
+        if ((int)(count & (GROUPS - 1)) != my_group) continue;
         if (ok) ok = mbar_wait_warp(full(st), ph, abort_flag);
         if (!ok) continue;
-        // positions of the slice that count: up to the length, none on an absent page (a page has whole slices)
-        const long long room = (long long)p.len - (long long)t * TILE - r0;
-        const int valid = (absent[st] >> slice & 1) ? 0 : (int)max(0ll, min(16ll, room));
-        if (valid > 0) {
-          const uint32_t kb = base + st * C::STAGE, vb = kb + C::PLANE;
-          // ---- S^T = K Q^T: rows = positions gq, gq + 8, columns = heads 2 tq, 2 tq + 1
-          float s[NT][4], s2[NT][4];
+        // positions of each block that count: up to the length, none on an absent page (a page has whole slices)
+        const int gone = absent[st] >> slice;
+        int valid[BLOCKS], any = 0;
 #pragma unroll
-          for (int n = 0; n < NT; ++n) { s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f; s2[n][0] = s2[n][1] = s2[n][2] = s2[n][3] = 0.f; }
+        for (int j = 0; j < BLOCKS; ++j) {
+          const int room = p.len - t * TILE - r0 - 16 * j;
+          valid[j] = (gone >> j & 1) ? 0 : max(0, min(16, room));
+          any |= valid[j];
+        }
+        if (any) {
+          const uint32_t kb = base + st * C::STAGE, vb = kb + C::PLANE;
+          // ---- S^T = K Q^T: rows = positions gq, gq + 8 of a block, columns = heads 2 tq, 2 tq + 1
+          float s[BLOCKS][NT][4];
+#pragma unroll
+          for (int j = 0; j < BLOCKS; ++j)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) s[j][n][0] = s[j][n][1] = s[j][n][2] = s[j][n][3] = 0.f;
           if constexpr (!E4M3) {
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-              uint32_t a[4];
-              ldmatrix4(kb + swizzled(krow, 2 * k + kchunk), a);
+            for (int k = 0; k < KS; ++k)
 #pragma unroll
-              for (int n = 0; n < NT; ++n) mma16816<false>((k & 1) ? s2[n] : s[n], a[0], a[1], a[2], a[3], q[n][k][0], q[n][k][1]);
-            }
+              for (int j = 0; j < BLOCKS; ++j) {
+                uint32_t a[4];
+                ldmatrix4(kb + swizzled(krow + 16 * j, 2 * k + kchunk), a);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma16816<false>(s[j][n], a[0], a[1], a[2], a[3], q[n][k][0], q[n][k][1]);
+              }
           } else {
 #pragma unroll
-            for (int k = 0; k < KS; k += 2) {
-              uint32_t a[4];                                          // positions gq / gq + 8 of k-step k, then of k + 1
-              ldmatrix4(kb + swizzled(krow, k + kchunk), a);
+            for (int k = 0; k < KS; k += 2)
 #pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const uint32_t a0 = e4m3x2_to_f16x2(a[2 * i] & 0xffffu), a2 = e4m3x2_to_f16x2(a[2 * i] >> 16);
-                const uint32_t a1 = e4m3x2_to_f16x2(a[2 * i + 1] & 0xffffu), a3 = e4m3x2_to_f16x2(a[2 * i + 1] >> 16);
+              for (int j = 0; j < BLOCKS; ++j) {
+                uint32_t a[4];                                        // positions gq / gq + 8 of k-step k, then of k + 1
+                ldmatrix4(kb + swizzled(krow + 16 * j, k + kchunk), a);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) mma16816<true>(i ? s2[n] : s[n], a0, a1, a2, a3, q[n][k + i][0], q[n][k + i][1]);
+                for (int i = 0; i < 2; ++i) {
+                  const uint32_t a0 = e4m3x2_to_f16x2(a[2 * i] & 0xffffu), a2 = e4m3x2_to_f16x2(a[2 * i] >> 16);
+                  const uint32_t a1 = e4m3x2_to_f16x2(a[2 * i + 1] & 0xffffu), a3 = e4m3x2_to_f16x2(a[2 * i + 1] >> 16);
+#pragma unroll
+                  for (int n = 0; n < NT; ++n) mma16816<true>(s[j][n], a0, a1, a2, a3, q[n][k + i][0], q[n][k + i][1]);
+                }
               }
+          }
+          // scales of the block's two positions of this lane: keys' as factors, values' as exponents
+          float ks[BLOCKS][2], ve[BLOCKS][2];
+#pragma unroll
+          for (int j = 0; j < BLOCKS; ++j) {
+            if constexpr (E4M3) {
+              const uint8_t* sc = gen + STAGES * C::STAGE + st * C::SCALES + r0 + 16 * j + gq;
+              ks[j][0] = pow2((int)sc[0] - 127); ks[j][1] = pow2((int)sc[8] - 127);
+              ve[j][0] = (float)((int)sc[TILE] - 127); ve[j][1] = (float)((int)sc[TILE + 8] - 127);
+            } else {
+              ks[j][0] = ks[j][1] = 1.f; ve[j][0] = ve[j][1] = 0.f;
             }
           }
-          float ks0 = 1.f, ks1 = 1.f, ve0 = 0.f, ve1 = 0.f;
-          if constexpr (E4M3) {
-            const uint8_t* sc = gen + STAGES * C::STAGE + st * C::SCALES + r0 + gq;
-            ks0 = pow2((int)sc[0] - 127); ks1 = pow2((int)sc[8] - 127);
-            ve0 = (float)((int)sc[TILE] - 127); ve1 = (float)((int)sc[TILE + 8] - 127);
-          }
-          const bool live0 = gq < valid, live1 = gq + 8 < valid;
           bool moved = false;
-          float pr[NT][4], alpha[NT][2];
+          float alpha[NT][2];
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            float x[4];
-            x[0] = live0 ? (s[n][0] + s2[n][0]) * qscale[n][0] * ks0 : -INFINITY;
-            x[1] = live0 ? (s[n][1] + s2[n][1]) * qscale[n][1] * ks0 : -INFINITY;
-            x[2] = live1 ? (s[n][2] + s2[n][2]) * qscale[n][0] * ks1 : -INFINITY;
-            x[3] = live1 ? (s[n][3] + s2[n][3]) * qscale[n][1] * ks1 : -INFINITY;
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              float top = fmaxf(x[i], x[i + 2]), topo = E4M3 ? fmaxf(x[i] + ve0, x[i + 2] + ve1) : 0.f;
+              float top = -INFINITY, topo = -INFINITY;
+#pragma unroll
+              for (int j = 0; j < BLOCKS; ++j) {
+                float& x = s[j][n][i];
+                float& y = s[j][n][i + 2];
+                x = gq < valid[j] ? x * qscale[n][i] * ks[j][0] : -INFINITY;
+                y = gq + 8 < valid[j] ? y * qscale[n][i] * ks[j][1] : -INFINITY;
+                top = fmaxf(top, fmaxf(x, y));
+                if (E4M3) topo = fmaxf(topo, fmaxf(x + ve[j][0], y + ve[j][1]));
+              }
 #pragma unroll
               for (int d = 4; d < 32; d <<= 1) {
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
                 if (E4M3) topo = fmaxf(topo, __shfl_xor_sync(0xffffffffu, topo, d));
               }
               const float mn = fmaxf(m[n][i], top), mu = mn == -INFINITY ? 0.f : mn;
-              const float e0 = exp2_fast(x[i] - mu), e1 = exp2_fast(x[i + 2] - mu);
+              const float al = exp2_fast(m[n][i] - mu);
+              float ou = 0.f, sum = 0.f;
               if (!E4M3) {
-                const float al = exp2_fast(m[n][i] - mu);
                 moved |= mn != m[n][i];
-                l[n][i] = l[n][i] * al + (e0 + e1);
                 alpha[n][i] = al;
-                pr[n][i] = e0; pr[n][i + 2] = e1;
               } else {
-                l[n][i] = l[n][i] * exp2_fast(m[n][i] - mu) + (e0 + e1);
-                const float on = fmaxf(mo[n][i], topo), ou = on == -INFINITY ? 0.f : on;
+                const float on = fmaxf(mo[n][i], topo);
+                ou = on == -INFINITY ? 0.f : on;
                 moved |= on != mo[n][i];
                 alpha[n][i] = exp2_fast(mo[n][i] - ou);
-                pr[n][i] = exp2_fast(x[i] + ve0 - ou); pr[n][i + 2] = exp2_fast(x[i + 2] + ve1 - ou);
                 mo[n][i] = on;
               }
+              // the scores become weights
+#pragma unroll
+              for (int j = 0; j < BLOCKS; ++j) {
+                const float x = s[j][n][i], y = s[j][n][i + 2];
+                const float e0 = exp2_fast(x - mu), e1 = exp2_fast(y - mu);
+                sum += e0 + e1;
+                s[j][n][i] = E4M3 ? exp2_fast(x + ve[j][0] - ou) : e0;
+                s[j][n][i + 2] = E4M3 ? exp2_fast(y + ve[j][1] - ou) : e1;
+              }
+              l[n][i] = l[n][i] * al + sum;
               m[n][i] = mn;
             }
-          }
           if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -494,51 +523,55 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
               }
           }
           // ---- O^T += V^T P^T.  P as the B operand: 8 x 8 transposes of the accumulator's pairs.  bf16: a probability is
-          // split into two bf16 (16 bits of it count); halves (e4m3) hold 11 bits of it.
-          uint32_t ph0[NT], ph1[NT], pl0[NT], pl1[NT];
+          // split into two bf16 (16 bits of it count); halves (e4m3) hold 11 bits of it.  Whatever stands behind the length
+          // must not meet a zero probability (0 * NaN is NaN): the values there are cleared.
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            if constexpr (E4M3) {
-              ph0[n] = transpose8x8(pack_f16(pr[n][0], pr[n][1]));
-              ph1[n] = transpose8x8(pack_f16(pr[n][2], pr[n][3]));
-            } else {
-              const uint32_t a = pack_bf16(pr[n][0], pr[n][1]), c = pack_bf16(pr[n][2], pr[n][3]);
-              const float2 fa = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&a));
-              const float2 fc = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&c));
-              ph0[n] = transpose8x8(a);
-              ph1[n] = transpose8x8(c);
-              pl0[n] = transpose8x8(pack_bf16(pr[n][0] - fa.x, pr[n][1] - fa.y));
-              pl1[n] = transpose8x8(pack_bf16(pr[n][2] - fc.x, pr[n][3] - fc.y));
-            }
-          }
-          // whatever stands behind the length must not meet a zero probability: 0 * NaN is NaN
-          const uint32_t keep0 = (2 * tq < valid ? 0xffffu : 0u) | (2 * tq + 1 < valid ? 0xffff0000u : 0u);
-          const uint32_t keep1 = (2 * tq + 8 < valid ? 0xffffu : 0u) | (2 * tq + 9 < valid ? 0xffff0000u : 0u);
-          if constexpr (!E4M3) {
+          for (int j = 0; j < BLOCKS; ++j) {
+            uint32_t ph0[NT], ph1[NT], pl0[NT], pl1[NT];
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-              uint32_t a[4];                                          // rows d = 16 k + gq, + 8; columns = positions
-              ldmatrix4_trans(vb + swizzled(vrow, 2 * k + vchunk), a);
-              a[0] &= keep0; a[1] &= keep0; a[2] &= keep1; a[3] &= keep1;
-#pragma unroll
-              for (int n = 0; n < NT; ++n) {
-                mma16816<false>(o[n][k], a[0], a[1], a[2], a[3], ph0[n], ph1[n]);
-                mma16816<false>(o[n][k], a[0], a[1], a[2], a[3], pl0[n], pl1[n]);
+            for (int n = 0; n < NT; ++n) {
+              const float* x = s[j][n];
+              if constexpr (E4M3) {
+                ph0[n] = transpose8x8(pack_f16(x[0], x[1]));
+                ph1[n] = transpose8x8(pack_f16(x[2], x[3]));
+              } else {
+                const uint32_t a = pack_bf16(x[0], x[1]), c = pack_bf16(x[2], x[3]);
+                const float2 fa = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&a));
+                const float2 fc = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&c));
+                ph0[n] = transpose8x8(a);
+                ph1[n] = transpose8x8(c);
+                pl0[n] = transpose8x8(pack_bf16(x[0] - fa.x, x[1] - fa.y));
+                pl1[n] = transpose8x8(pack_bf16(x[2] - fc.x, x[3] - fc.y));
               }
             }
-          } else {
+            const uint32_t keep0 = (2 * tq < valid[j] ? 0xffffu : 0u) | (2 * tq + 1 < valid[j] ? 0xffff0000u : 0u);
+            const uint32_t keep1 = (2 * tq + 8 < valid[j] ? 0xffffu : 0u) | (2 * tq + 9 < valid[j] ? 0xffff0000u : 0u);
+            if constexpr (!E4M3) {
 #pragma unroll
-            for (int k = 0; k < KS; k += 2) {
-              // a transposed 8 x 8 of byte pairs: this lane has dimensions 2 gq, 2 gq + 1 of positions 2 tq, 2 tq + 1 (and + 8)
-              uint32_t a[4];
-              ldmatrix4_trans(vb + swizzled(vrow, k + vchunk), a);
+              for (int k = 0; k < KS; ++k) {
+                uint32_t a[4];                                        // rows d = 16 k + gq, + 8; columns = positions
+                ldmatrix4_trans(vb + swizzled(vrow + 16 * j, 2 * k + vchunk), a);
+                a[0] &= keep0; a[1] &= keep0; a[2] &= keep1; a[3] &= keep1;
 #pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const uint32_t x = a[2 * i] & keep0, y = a[2 * i + 1] & keep1;
-                const uint32_t a0 = e4m3x2_to_f16x2(__byte_perm(x, 0, 0x4420)), a1 = e4m3x2_to_f16x2(__byte_perm(x, 0, 0x4431));
-                const uint32_t a2 = e4m3x2_to_f16x2(__byte_perm(y, 0, 0x4420)), a3 = e4m3x2_to_f16x2(__byte_perm(y, 0, 0x4431));
+                for (int n = 0; n < NT; ++n) {
+                  mma16816<false>(o[n][k], a[0], a[1], a[2], a[3], ph0[n], ph1[n]);
+                  mma16816<false>(o[n][k], a[0], a[1], a[2], a[3], pl0[n], pl1[n]);
+                }
+              }
+            } else {
 #pragma unroll
-                for (int n = 0; n < NT; ++n) mma16816<true>(o[n][k + i], a0, a1, a2, a3, ph0[n], ph1[n]);
+              for (int k = 0; k < KS; k += 2) {
+                // a transposed 8 x 8 of byte pairs: this lane has dimensions 2 gq, 2 gq + 1 of positions 2 tq, 2 tq + 1 (and + 8)
+                uint32_t a[4];
+                ldmatrix4_trans(vb + swizzled(vrow + 16 * j, k + vchunk), a);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                  const uint32_t x = a[2 * i] & keep0, y = a[2 * i + 1] & keep1;
+                  const uint32_t a0 = e4m3x2_to_f16x2(__byte_perm(x, 0, 0x4420)), a1 = e4m3x2_to_f16x2(__byte_perm(x, 0, 0x4431));
+                  const uint32_t a2 = e4m3x2_to_f16x2(__byte_perm(y, 0, 0x4420)), a3 = e4m3x2_to_f16x2(__byte_perm(y, 0, 0x4431));
+#pragma unroll
+                  for (int n = 0; n < NT; ++n) mma16816<true>(o[n][k + i], a0, a1, a2, a3, ph0[n], ph1[n]);
+                }
               }
             }
           }
