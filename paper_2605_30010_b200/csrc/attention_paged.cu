@@ -6,7 +6,7 @@
 //   * A tile is 64 positions of one key / value head.  All tiles of the call, in the order (sequence, key / value head,
 //     tile), are cut into one equal run per CTA (one CTA per SM), so a single long sequence and a ragged batch load every
 //     SM alike.  Lengths are on the device, so each CTA works the cut out for itself.
-//   * Two warps copy: TMA boxes of a page's rows (hardware swizzle, so that ldmatrix meets no bank conflicts) into a ring
+//   * Four warps copy: TMA boxes of a page's rows (hardware swizzle, so that ldmatrix meets no bank conflicts) into a ring
 //     of stages.  Eight warps compute, two to a tile, 32 positions each, every warp with a running maximum, sum and
 //     output of its own; they meet only at the end of a piece (the part of a sequence that falls into the CTA's run).
 //   * The product is transposed, S^T = K Q^T and O^T = V^T P^T, so that the query heads are the narrow side (8) of
@@ -33,8 +33,13 @@ constexpr int GROUP_WARPS = 2;                 // warps of one tile, BLOCKS bloc
 constexpr int BLOCKS = TILE / 16 / GROUP_WARPS;
 constexpr int COMPUTE_WARPS = 8;
 constexpr int GROUPS = COMPUTE_WARPS / GROUP_WARPS;   // tiles are dealt to the groups in turn
-constexpr int COPY_WARPS = 2;                  // each copies every other tile
+constexpr int COPY_WARPS = GROUPS;             // one for each group's tiles
 constexpr int THREADS = 32 * (COMPUTE_WARPS + COPY_WARPS);
+// With 16 heads (NT = 2) the computing warps take registers from the copying ones: of what a block is launched with, never more.
+constexpr int LAUNCH_REGS = 168, COMPUTE_REGS = 208, COPY_REGS = 88;
+static_assert(COMPUTE_WARPS % 4 == 0 && COPY_WARPS % 4 == 0, "whole warpgroups");
+static_assert(COMPUTE_WARPS * COMPUTE_REGS + COPY_WARPS * COPY_REGS <= (COMPUTE_WARPS + COPY_WARPS) * LAUNCH_REGS, "register budget");
+constexpr int QUERIES = 4;                     // pieces whose queries are on their way or waiting
 constexpr int MAX_CTAS = 148;
 #ifndef ITEM_COST_V
 #define ITEM_COST_V 2
@@ -53,14 +58,17 @@ struct Cfg {
   static constexpr int STAGE = 2 * PLANE;                         // keys, values
   static constexpr int SCALES = E4M3 ? 2 * TILE : 0;
   static constexpr int HEADS = 8 * NT;
-  static constexpr int JOIN = COMPUTE_WARPS * HEADS * (DH + PAD) * 4 + COMPUTE_WARPS * HEADS * 3 * 4;
-  static constexpr int FIT = (SMEM_LIMIT - 1024 - CONTROL_BYTES - JOIN) / (STAGE + SCALES);
+  static constexpr int JOIN = COMPUTE_WARPS * HEADS * (DH + PAD) * 4 + COMPUTE_WARPS * HEADS * 3 * 4;   // the warps' results of a piece
+  static constexpr int JOINS = NT == 1 ? 2 : 1;                   // pieces whose results can wait to be joined
+  static constexpr int Q_ROW = DH * 2 + 16;                       // a head's query; 16 bytes more: no bank conflicts
+  static constexpr int EDGE = JOINS * JOIN + QUERIES * HEADS * Q_ROW;
+  static constexpr int FIT = (SMEM_LIMIT - 1024 - CONTROL_BYTES - EDGE) / (STAGE + SCALES);
   // a multiple of the groups, so that a stage is always the same warps': they wait for its copies in turn, where warps that come to a
   // stage for the first time in its second round could take the barrier's state of the first for their own
-  static constexpr int STAGES = (FIT > 12 ? 12 : FIT) / GROUPS * GROUPS;
-  static constexpr int SMEM = 1024 + STAGES * (STAGE + SCALES) + JOIN + CONTROL_BYTES;
-  static_assert(STAGES >= GROUPS && STAGES % COPY_WARPS == 0 && COPY_WARPS == 2, "ring");
-  static_assert(2 * 8 * STAGES + 4 * STAGES + 16 <= CONTROL_BYTES, "control area");
+  static constexpr int STAGES = (FIT > 16 ? 16 : FIT) / GROUPS * GROUPS;
+  static constexpr int SMEM = 1024 + STAGES * (STAGE + SCALES) + EDGE + CONTROL_BYTES;
+  static_assert(STAGES >= GROUPS, "ring");
+  static_assert(8 * (2 * STAGES + 2 * QUERIES + 4) + 4 * STAGES + 16 <= CONTROL_BYTES, "control area");
 };
 
 // Workspace: one descriptor per CTA, then two slots of partial results per CTA.
@@ -127,14 +135,13 @@ __device__ __forceinline__ void bulk_load_elect(uint32_t dst, const void* src, u
                "@q cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}"
                ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void compute_warps_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * COMPUTE_WARPS) : "memory"); }
-
-// The run of units (tiles; whole items where args.whole) that falls to a CTA, walked piece by piece.
-struct Walk {
-  long long left;                  // units still to do
-  int s, part, unit;               // next unit: sequence, key / value head x head tile, unit of the item
-  int n_seq, parts_all;
-};
+// 16 bytes by a lane's own asynchronous copy (zeros if not live); copies_arrive: an arrival once the lane's copies so far are there
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
 
 __device__ __forceinline__ int clamped_len(const Args& g, int s) {
   const long long cap = (long long)g.a.max_pages << g.c.page_shift;
@@ -142,8 +149,15 @@ __device__ __forceinline__ int clamped_len(const Args& g, int s) {
 }
 // An item's units: its tiles and, in front of them, ITEM_COST for what every item costs however short it is.
 __device__ __forceinline__ int units_of(const Args& g, int len) {
-  return len <= 0 ? 0 : g.whole ? 1 : (int)((len + (TILE - 1ll)) / TILE) + ITEM_COST;
+  return len <= 0 ? 0 : g.whole ? 1 : (int)((unsigned)(len + (TILE - 1)) / TILE) + ITEM_COST;
 }
+
+// The run of units that falls to a CTA, walked piece by piece.
+struct Walk {
+  long long left;                  // units still to do
+  int s, part, unit;               // next unit: sequence, key / value head x head tile, unit of the item
+  int len;                         // of the sequence
+};
 
 struct Piece {
   int s, part, len, t0, t1;        // tiles t0 .. t1 - 1
@@ -151,24 +165,23 @@ struct Piece {
   bool first, last;                // contains the item's first, last tile
 };
 
-__device__ __forceinline__ bool next_piece(const Args& g, Walk& w, Piece& p) {
+__device__ __forceinline__ bool next_piece(const Args& g, int parts_all, Walk& w, Piece& p) {
   while (w.left > 0) {
-    const int len = clamped_len(g, w.s), units = units_of(g, len);
-    if (units == 0) {                                             // only between items
-      if (++w.s >= w.n_seq) return false;
-      continue;
+    const int units = units_of(g, w.len);
+    if (units > 0) {
+      const int n = w.left < units - w.unit ? (int)w.left : units - w.unit, end = w.unit + n;
+      p.s = w.s; p.part = w.part; p.len = w.len; p.units_end = end;
+      p.t0 = g.whole ? 0 : max(w.unit - ITEM_COST, 0);
+      p.t1 = g.whole ? (int)((unsigned)(w.len + (TILE - 1)) / TILE) : max(end - ITEM_COST, 0);
+      p.first = p.t0 == 0; p.last = end == units;
+      w.left -= n; w.unit = end;
+      if (end == units) { w.unit = 0; ++w.part; }
     }
-    const int n = (int)min(w.left, (long long)(units - w.unit)), end = w.unit + n;
-    p.s = w.s; p.part = w.part; p.len = len; p.units_end = end;
-    p.t0 = g.whole ? 0 : max(w.unit - ITEM_COST, 0);
-    p.t1 = g.whole ? (len + TILE - 1) / TILE : max(end - ITEM_COST, 0);
-    p.first = p.t0 == 0; p.last = end == units;
-    w.left -= n; w.unit = end;
-    if (end == units) {
-      w.unit = 0;
-      if (++w.part == w.parts_all) { w.part = 0; if (++w.s >= w.n_seq) w.left = 0; }
+    if (units == 0 || w.part == parts_all) {                      // on to the next sequence
+      w.part = 0;
+      if (++w.s >= g.a.n_seq) w.left = 0; else if (w.left > 0) w.len = clamped_len(g, w.s);
     }
-    if (p.t1 > p.t0) return true;                                 // else the run ended in front of the item's first tile
+    if (units > 0 && p.t1 > p.t0) return true;                    // else the run ended in front of the item's first tile
   }
   return false;
 }
@@ -182,28 +195,36 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const gen = smem_raw + (base - raw);
   const uint32_t scales = base + STAGES * C::STAGE;
-  float* const join = reinterpret_cast<float*>(gen + STAGES * (C::STAGE + C::SCALES));
-  float* const join_m = join + COMPUTE_WARPS * C::HEADS * (DH + PAD);       // [3][COMPUTE_WARPS][HEADS]: maximum, output's maximum, sum
-  uint8_t* const ctl = gen + STAGES * (C::STAGE + C::SCALES) + C::JOIN;
+  uint8_t* const edge = gen + STAGES * (C::STAGE + C::SCALES);
+  // results of a piece, each warp's: [COMPUTE_WARPS][HEADS][DH + PAD] outputs, then [3][COMPUTE_WARPS][HEADS]: maximum, output's
+  // maximum, sum
+  constexpr int JOIN_M = COMPUTE_WARPS * C::HEADS * (DH + PAD);
+  auto join_of = [&](int i) { return reinterpret_cast<float*>(edge + i * C::JOIN); };
+  auto query_of = [&](int i) { return edge + C::JOINS * C::JOIN + i * (C::HEADS * C::Q_ROW); };
+  uint8_t* const ctl = edge + C::EDGE;
   const uint32_t bars = smem_u32(ctl);
   auto full = [&](int s) { return bars + 8u * (uint32_t)s; };
   auto empty = [&](int s) { return bars + 8u * (uint32_t)(STAGES + s); };
-  volatile int* const absent = reinterpret_cast<volatile int*>(ctl + 16 * STAGES);   // [STAGES]: bit i = slice i has no page
+  auto q_full = [&](int i) { return bars + 8u * (uint32_t)(2 * STAGES + i); };
+  auto q_empty = [&](int i) { return bars + 8u * (uint32_t)(2 * STAGES + QUERIES + i); };
+  auto o_full = [&](int i) { return bars + 8u * (uint32_t)(2 * STAGES + 2 * QUERIES + i); };
+  auto o_empty = [&](int i) { return bars + 8u * (uint32_t)(2 * STAGES + 2 * QUERIES + 2 + i); };
+  volatile int* const absent = reinterpret_cast<volatile int*>(ctl + 8 * (2 * STAGES + 2 * QUERIES + 4));   // [STAGES]: bit i = slice i has no page
   volatile int* const abort_flag = absent + STAGES;
   __shared__ long long warp_sum_s[THREADS / 32];
-  __shared__ long long total_s;
-  __shared__ int walk_s[3];
+  __shared__ int walk_s[4];
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int b = blockIdx.x;
   const int kv_heads = g.c.kv_heads, parts_all = kv_heads * g.parts;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");    // the joining kernel may be set up; it waits for this grid's end
+  if (tid == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
 
-  if (tid == 0) {
-    for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), GROUP_WARPS); }
-    *abort_flag = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
+  if (tid < STAGES) { mbar_init(full(tid), 1); mbar_init(empty(tid), GROUP_WARPS); }
+  if (tid < QUERIES) { mbar_init(q_full(tid), 32); mbar_init(q_empty(tid), COMPUTE_WARPS); }
+  if (tid < C::JOINS) { mbar_init(o_full(tid), COMPUTE_WARPS); mbar_init(o_empty(tid), COMPUTE_WARPS); }
+  if (tid == 0) *abort_flag = 0;
+  if (tid < 32) asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 
   // ---- this CTA's run: an exclusive prefix sum of the sequences' units over the threads
   Walk walk;
@@ -221,94 +242,108 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     long long before = inc - sum, total = 0;
 #pragma unroll
     for (int w = 0; w < THREADS / 32; ++w) { const long long v = warp_sum_s[w]; if (w < warp) before += v; total += v; }
-    chunk = (total + gridDim.x - 1) / gridDim.x;
+    // (32-bit divisions wherever the numbers allow it: a 64-bit one takes hundreds of cycles)
+    const bool small = total + gridDim.x < (1ll << 31);
+    chunk = small ? ((unsigned)total + gridDim.x - 1) / gridDim.x : (total + gridDim.x - 1) / gridDim.x;
     begin = chunk * b;
     if (begin >= before && begin < before + sum) {
       long long r = begin - before;
       for (int s = s0; s < s1; ++s) {
-        const int u = units_of(g, clamped_len(g, s));
+        const int len = clamped_len(g, s), u = units_of(g, len);
         const long long all = (long long)u * parts_all;
-        if (r < all) { walk_s[0] = s; walk_s[1] = (int)(r / u); walk_s[2] = (int)(r % u); break; }
+        if (r < all) {
+          walk_s[0] = s; walk_s[3] = len;
+          if (small) { walk_s[1] = (int)((unsigned)r / (unsigned)u); walk_s[2] = (int)((unsigned)r % (unsigned)u); }
+          else { walk_s[1] = (int)(r / u); walk_s[2] = (int)(r % u); }
+          break;
+        }
         r -= all;
       }
     }
-    if (tid == 0) total_s = total;
     __syncthreads();
-    walk.left = max(0ll, min(chunk, total_s - begin));
-    walk.n_seq = g.a.n_seq; walk.parts_all = parts_all;
-    walk.s = walk_s[0]; walk.part = walk_s[1]; walk.unit = walk_s[2];
-  }
-
-  // ---- sequences without positions, and lengths that the table cannot hold
-  for (int s = b; s < g.a.n_seq; s += gridDim.x) {
-    const int len = __ldg(g.a.len + s);
-    if (len <= 0) {
-      for (int i = tid; i < g.a.heads * DH / 8; i += THREADS)
-        reinterpret_cast<uint4*>(g.a.out + (size_t)s * g.a.heads * DH)[i] = make_uint4(0, 0, 0, 0);
-      if (g.a.lse) for (int i = tid; i < g.a.heads; i += THREADS) g.a.lse[(size_t)s * g.a.heads + i] = -INFINITY;
-    } else if (tid == 0 && g.a.status && len > (long long)g.a.max_pages << g.c.page_shift) {
-      atomicMax(g.a.status, (int)ET_PAGED_CAPACITY);
-    }
+    walk.left = max(0ll, min(chunk, total - begin));
+    walk.s = walk_s[0]; walk.part = walk_s[1]; walk.unit = walk_s[2]; walk.len = walk_s[3];
   }
 
   bool ok = true;
+  if constexpr (NT == 2) {
+    if (warp >= COMPUTE_WARPS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(COPY_REGS));
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(COMPUTE_REGS));
+  }
   if (warp >= COMPUTE_WARPS) {
     // ------------------------------------------------------------------ copies
     const int me = warp - COMPUTE_WARPS;
     const int box_shift = min(g.c.page_shift, 6), box_rows = 1 << box_shift, boxes_tile = TILE >> box_shift;
     const uint32_t box_bytes = (uint32_t)box_rows * (2 * C::ROW + (E4M3 ? 2 : 0));
     const int plane_rows = kv_heads << g.c.page_shift;
-    if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
     int stage = me;
     uint32_t phase = 0;
     long long count = 0, issued = 0;
+    int pieces = 0;
     Piece p;
-    while (ok && next_piece(g, walk, p)) {
+    while (ok && next_piece(g, parts_all, walk, p)) {
+      if (me == 1) {                                                 // not the warp that has the first tile to fetch
+        // the piece's queries: rows of the heads, zeros for heads that the group does not have
+        const int buf = pieces % QUERIES;
+        ok = mbar_wait_warp(q_empty(buf), ((uint32_t)(pieces / QUERIES) & 1u) ^ 1u, abort_flag);
+        if (!ok) break;
+        const int h0 = (p.part % g.parts) * C::HEADS;
+        const bf16* src = g.a.q + (size_t)p.s * g.a.q_stride + (size_t)((p.part / g.parts) * g.group + h0) * DH;
+        const uint32_t dst = smem_u32(query_of(buf));
+#pragma unroll
+        for (int i = 0; i < C::HEADS * (DH / 8) / 32; ++i) {
+          const int e = i * 32 + lane, h = e / (DH / 8), d = e % (DH / 8);
+          copy16(dst + h * C::Q_ROW + d * 16, src + (h0 + h < g.group ? h * DH + d * 8 : 0), h0 + h < g.group);
+        }
+        copies_arrive(q_full(buf));
+        ++pieces;
+      }
       const int* table = g.a.table + (size_t)p.s * g.a.max_pages;
       const int kvh = p.part / g.parts;
       const int first_page = (int)(((long long)p.t0 * TILE) >> g.c.page_shift);
-      auto page_ids = [&](int batch) {                               // 32 entries of the table, one per lane
+      const int last_page = (p.len - 1) >> g.c.page_shift;            // of the sequence
+      // 32 entries of the table, one per lane, as the first rows of their keys in the cache (-1: not a page of the cache)
+      auto load_ids = [&](int batch) {
         const long long i = (long long)first_page + batch * 32 + lane;
-        return i < g.a.max_pages ? __ldg(table + i) : -1;
+        return i <= last_page ? __ldg(table + i) : 0;
       };
-      int batch = 0, ids = page_ids(0), ids_next = page_ids(1);
-      int t = p.t0 + (((int)(count & 1) ^ me) & 1);
+      auto rows_of = [&](int page) {
+        const bool good = (unsigned)page < (unsigned)g.c.n_pages;
+        if (!good && g.a.status) atomicMax(g.a.status, (int)ET_PAGED_BAD_PAGE);
+        return good ? (page * 2 * kv_heads + kvh) << g.c.page_shift : -1;
+      };
+      int batch = 0, rows = rows_of(load_ids(0)), ids_next = load_ids(1);
+      int t = p.t0 + ((me - (int)count) & (GROUPS - 1));
       count += p.t1 - p.t0;
-      for (; t < p.t1; t += COPY_WARPS) {
+      for (; t < p.t1; t += GROUPS) {
         const int pos = t * TILE;                                     // lengths are below 2^31
         const int page0 = (pos >> g.c.page_shift) - first_page;       // a multiple of the tile's pages: one batch has them all
-        while ((page0 >> 5) > batch) { ++batch; ids = ids_next; ids_next = page_ids(batch + 1); }
-        const int row_in_page = pos & ((1 << g.c.page_shift) - 1);
-        int row[4];                                                   // first row of each box's keys in the cache; -1: no copy
-        uint32_t bytes = 0;
-        int absent_slices = 0;
+        while ((page0 >> 5) > batch) { ++batch; rows = rows_of(ids_next); ids_next = load_ids(batch + 1); }
+        const int in_page = pos & ((1 << g.c.page_shift) - 1);
+        const int boxes = min(boxes_tile, (p.len - pos + box_rows - 1) >> box_shift);      // with positions
+        int row[4], missing = 0;                                      // first row of each box's keys; negative: none
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          row[i] = -1;
-          if (i < boxes_tile && (unsigned)(pos + (i << box_shift)) < (unsigned)p.len) {
-            const int page = __shfl_sync(0xffffffffu, ids, (page0 + i) & 31);
-            if ((unsigned)page < (unsigned)g.c.n_pages) {
-              row[i] = ((page * 2 * kv_heads + kvh) << g.c.page_shift) + row_in_page;
-              bytes += box_bytes;
-            } else {
-              if (g.a.status && lane == 0) atomicMax(g.a.status, (int)ET_PAGED_BAD_PAGE);
-              absent_slices |= ((1 << (box_rows / 16)) - 1) << (i * (box_rows / 16));
-            }
-          }
+          row[i] = __shfl_sync(0xffffffffu, rows, (page0 + i) & 31);
+          if (i >= boxes) row[i] = -1;
+          else if (row[i] < 0) missing |= 1 << i;
         }
         ok = mbar_wait_warp(empty(stage), phase ^ 1u, abort_flag);
         if (!ok) break;
-        if (lane == 0) absent[stage] = absent_slices;
+        int gone = 0;
+        if (missing)
+          for (int i = 0; i < boxes; ++i) if (missing >> i & 1) gone |= ((1 << (box_rows / 16)) - 1) << (i * (box_rows / 16));
+        if (lane == 0) absent[stage] = gone;
         __syncwarp();
         const uint32_t bar = full(stage), dst = base + stage * C::STAGE, sdst = scales + stage * C::SCALES;
-        arrive_expect_elect(bar, bytes);
+        arrive_expect_elect(bar, (boxes - __popc(missing)) * box_bytes);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if (row[i] >= 0) {
             const int r0 = i << box_shift;
 #pragma unroll
             for (int plane = 0; plane < 2; ++plane) {
-              const int y = row[i] + plane * plane_rows;
+              const int y = row[i] + in_page + plane * plane_rows;
 #pragma unroll
               for (int half = 0; half < C::BOXES; ++half)
                 tma_load_elect(dst + plane * C::PLANE + half * (TILE * C::BOX_ROW) + r0 * C::BOX_ROW, &map, bar,
@@ -318,13 +353,14 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
           }
         }
         ++issued;
-        if ((stage += COPY_WARPS) >= STAGES) { stage = me; phase ^= 1u; }
+        if ((stage += GROUPS) >= STAGES) { stage = me; phase ^= 1u; }
       }
     }
+    if (!ok) asm volatile("cp.async.wait_all;" ::: "memory");
     if (!ok && lane == 0) {
       // copies in flight have to land before this CTA's shared memory is given up
-      for (int i = 0; i < STAGES / COPY_WARPS && i < issued; ++i) {
-        if ((stage -= COPY_WARPS) < 0) { stage = STAGES - COPY_WARPS + me; phase ^= 1u; }
+      for (int i = 0; i < STAGES / GROUPS && i < issued; ++i) {
+        if ((stage -= GROUPS) < 0) { stage = STAGES - GROUPS + me; phase ^= 1u; }
         int given_up = 0;
         mbar_wait(full(stage), phase, &given_up);
       }
@@ -344,57 +380,112 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     };
     const float softmax_scale = 1.4426950408889634f * (DH == 128 ? 0.08838834764831845f : 0.125f);   // log2(e) / sqrt(DH)
 
-    int stage = 0, pieces_done = 0;
+    // Joins the warps' results of piece i: every warp has left its own in a buffer and takes a part of the heads' outputs.
+    Join mine{0, 0, 0, 0};
+    auto join_piece = [&](const Piece& p, int i) {
+      const int buf = i % C::JOINS;
+      if (ok) ok = mbar_wait_warp(o_full(buf), (uint32_t)(i / C::JOINS) & 1u, abort_flag);
+      const float* const join = join_of(buf);
+      const float* const join_m = join + JOIN_M;
+      const int kvh = p.part / g.parts, h0 = (p.part % g.parts) * C::HEADS, heads_live = min(C::HEADS, g.group - h0);
+      const bool whole = p.first && p.last;
+      const int slot = 2 * b + (i == 0 ? 0 : 1);
+      float* const part = g.a.workspace + SLOT0 + (size_t)slot * Slot<DH, NT>::FLOATS;
+      for (int e = tid; ok && e < heads_live * (DH / 4); e += 32 * COMPUTE_WARPS) {
+        const int h = e / (DH / 4), d = (e % (DH / 4)) * 4;
+        float top = -INFINITY, sum = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < COMPUTE_WARPS; ++w) top = fmaxf(top, join_m[w * C::HEADS + h]);
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int w = 0; w < COMPUTE_WARPS; ++w) {
+          const float lw = join_m[(2 * COMPUTE_WARPS + w) * C::HEADS + h];
+          if (lw != 0.f) {                                           // a warp without positions left no output (NaN is not zero)
+            const float fl = exp2_fast(join_m[w * C::HEADS + h] - ref), fo = exp2_fast(join_m[(COMPUTE_WARPS + w) * C::HEADS + h] - ref);
+            const float4 x = *reinterpret_cast<const float4*>(join + (w * C::HEADS + h) * (DH + PAD) + d);
+            sum += lw * fl;
+            acc.x += x.x * fo; acc.y += x.y * fo; acc.z += x.z * fo; acc.w += x.w * fo;
+          }
+        }
+        if (whole) {
+          const int head = kvh * g.group + h0 + h;
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;            // every page absent: zeros
+          const size_t at = (size_t)p.s * g.a.heads + head;
+          *reinterpret_cast<uint2*>(g.a.out + at * DH + d) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+          if (d == 0 && g.a.lse) g.a.lse[at] = sum == 0.f ? -INFINITY : (log2f(sum) + top) * 0.6931471805599453f;
+        } else {
+          *reinterpret_cast<float4*>(part + h * DH + d) = acc;
+          if (d == 0) { part[C::HEADS * DH + 2 * h] = top; part[C::HEADS * DH + 2 * h + 1] = sum; }
+        }
+      }
+      if (p.first && !p.last) {
+        // the item goes on in the CTAs behind this one, each of which finds it at the start of its run
+        const long long item0 = begin + chunk - p.units_end;          // this piece ends this CTA's run (whole items are not cut)
+        mine = Join{p.s, p.part, (int)((item0 + units_of(g, p.len) - 1) / chunk - b + 1), slot};
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(o_empty(buf));
+    };
+
+    int stage = 0, pieces = 0;
     uint32_t phase = 0;
     long long count = 0;                                             // tiles of this CTA so far
-    Piece p;
-    Join mine{0, 0, 0, 0};
-    while (next_piece(g, walk, p)) {
-      const int kvh = p.part / g.parts, h0 = (p.part % g.parts) * C::HEADS;       // first head of the tile inside its group
-      const int heads_live = min(C::HEADS, g.group - h0);
+    Piece p, before;
+    bool busy;
+    for (; next_piece(g, parts_all, walk, p); ++pieces) {
+      // A warp whose group has no tile of a short piece neither waits for its queries nor leaves an output.  (It cannot get
+      // so far ahead that it takes one use of a barrier for another: a result buffer is free again only when every warp has
+      // joined the piece that it held, and QUERIES pieces need more than JOINS results.)
+      busy = ((my_group - (int)count) & (GROUPS - 1)) < p.t1 - p.t0;
+      if (busy && ok) ok = mbar_wait_warp(q_full(pieces % QUERIES), (uint32_t)(pieces / QUERIES) & 1u, abort_flag);
+      const uint8_t* const query = query_of(pieces % QUERIES);
       // ---- Q^T as the B operand: column gq = head, two rows (pairs of dimensions) a register
       uint32_t q[NT][KS][2];
       float qscale[NT][2];                                           // of heads 2 tq and 2 tq + 1
+      if (busy) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const bool live = n * 8 + gq < heads_live;
-        const bf16* src = g.a.q + (size_t)p.s * g.a.q_stride + (size_t)(kvh * g.group + h0 + (live ? n * 8 + gq : 0)) * DH;
-        if constexpr (!E4M3) {
+        for (int n = 0; n < NT; ++n) {
+          const uint8_t* src = query + (n * 8 + gq) * C::Q_ROW;
+          if constexpr (!E4M3) {
 #pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            q[n][k][0] = live ? __ldg(reinterpret_cast<const uint32_t*>(src + k * 16 + 2 * tq)) : 0u;
-            q[n][k][1] = live ? __ldg(reinterpret_cast<const uint32_t*>(src + k * 16 + 8 + 2 * tq)) : 0u;
+            for (int k = 0; k < KS; ++k) {
+              q[n][k][0] = *reinterpret_cast<const uint32_t*>(src + k * 32 + 4 * tq);
+              q[n][k][1] = *reinterpret_cast<const uint32_t*>(src + k * 32 + 16 + 4 * tq);
+            }
+            qscale[n][0] = qscale[n][1] = softmax_scale;
+          } else {
+            // e4m3 keys are multiplied as halves, which hold them exactly.  A query row is scaled by a power of two that
+            // brings its largest value to 2^14 .. 2^15: a value below 2^-29 of that loses bits, no other.  The dimensions of
+            // a k-step are taken in the order that the keys' bytes come in: 4 tq, 4 tq + 1 | 4 tq + 2, 4 tq + 3.
+            uint2 raw_q[KS];
+            float top = 0.f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+              raw_q[k] = *reinterpret_cast<const uint2*>(src + k * 32 + 8 * tq);
+              const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].x));
+              const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].y));
+              top = fmaxf(top, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(y.x), fabsf(y.y))));
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int e = top > 0.f ? max((__float_as_int(top) >> 23) - 127 - 14, -127) : 0;
+            const float f = pow2(-e);
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+              const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].x));
+              const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].y));
+              q[n][k][0] = pack_f16(x.x * f, x.y * f);
+              q[n][k][1] = pack_f16(y.x * f, y.y * f);
+            }
+            const float back = pow2(e) * softmax_scale;
+            qscale[n][0] = __shfl_sync(0xffffffffu, back, 8 * tq);
+            qscale[n][1] = __shfl_sync(0xffffffffu, back, 8 * tq + 4);
           }
-          qscale[n][0] = qscale[n][1] = softmax_scale;
-        } else {
-          // e4m3 keys are multiplied as halves, which hold them exactly.  A query row is scaled by a power of two that
-          // brings its largest value to 2^14 .. 2^15: a value below 2^-29 of that loses bits, no other.  The dimensions of
-          // a k-step are taken in the order that the keys' bytes come in: 4 tq, 4 tq + 1 | 4 tq + 2, 4 tq + 3.
-          uint2 raw_q[KS];
-          float top = 0.f;
-#pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            raw_q[k] = live ? __ldg(reinterpret_cast<const uint2*>(src + k * 16 + 4 * tq)) : make_uint2(0, 0);
-            const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].x));
-            const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].y));
-            top = fmaxf(top, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(y.x), fabsf(y.y))));
-          }
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          const int e = top > 0.f ? max((__float_as_int(top) >> 23) - 127 - 14, -127) : 0;
-          const float f = pow2(-e);
-#pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].x));
-            const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].y));
-            q[n][k][0] = pack_f16(x.x * f, x.y * f);
-            q[n][k][1] = pack_f16(y.x * f, y.y * f);
-          }
-          const float back = pow2(e) * softmax_scale;
-          qscale[n][0] = __shfl_sync(0xffffffffu, back, 8 * tq);
-          qscale[n][1] = __shfl_sync(0xffffffffu, back, 8 * tq + 4);
         }
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_empty(pieces % QUERIES));
       // per head 2 tq + i: running maximum m of the scores (base 2), sum l of this lane's positions; mo: maximum of score +
       // log2(scale of the value), against which the output is kept (e4m3: a value's scale is part of its weight)
       float o[NT][KS][4], m[NT][2], mo[NT][2], l[NT][2];
@@ -580,65 +671,53 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         if (lane == 0) mbar_arrive(empty(st));
       }
 
-      // ---- the eight warps' results of the piece
+      const int heads_live = min(C::HEADS, g.group - (p.part % g.parts) * C::HEADS);
+      // ---- the piece before is joined now, when its slowest warp is done; then this warp leaves its result of this one
+      if (pieces > 0) join_piece(before, pieces - 1);
+      const int buf = pieces % C::JOINS;
+      if (ok) ok = mbar_wait_warp(o_empty(buf), ((uint32_t)(pieces / C::JOINS) & 1u) ^ 1u, abort_flag);
+      if (ok) {
+        float* const join = join_of(buf);
+        float* const join_m = join + JOIN_M;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float x = l[n][i];
+          for (int i = 0; i < 2; ++i) {
+            float x = l[n][i];
 #pragma unroll
-          for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-          const int h = n * 8 + 2 * tq + i;
-          if (gq == 0) {
-            join_m[warp * C::HEADS + h] = m[n][i];
-            join_m[(COMPUTE_WARPS + warp) * C::HEADS + h] = E4M3 ? mo[n][i] : m[n][i];
-            join_m[(2 * COMPUTE_WARPS + warp) * C::HEADS + h] = x;
+            for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+            const int h = n * 8 + 2 * tq + i;
+            if (gq == 0) {
+              join_m[warp * C::HEADS + h] = m[n][i];
+              join_m[(COMPUTE_WARPS + warp) * C::HEADS + h] = E4M3 ? mo[n][i] : m[n][i];
+              join_m[(2 * COMPUTE_WARPS + warp) * C::HEADS + h] = x;
+            }
+            if (busy && h < heads_live) {
+              float* dst = join + (warp * C::HEADS + h) * (DH + PAD);
+#pragma unroll
+              for (int k = 0; k < KS; ++k) {
+                if (E4M3) *reinterpret_cast<float2*>(dst + 16 * k + 2 * gq) = make_float2(o[n][k][i], o[n][k][i + 2]);
+                else { dst[16 * k + gq] = o[n][k][i]; dst[16 * k + 8 + gq] = o[n][k][i + 2]; }
+              }
+            }
           }
-          float* dst = join + (warp * C::HEADS + h) * (DH + PAD);
-#pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            if (E4M3) *reinterpret_cast<float2*>(dst + 16 * k + 2 * gq) = make_float2(o[n][k][i], o[n][k][i + 2]);
-            else { dst[16 * k + gq] = o[n][k][i]; dst[16 * k + 8 + gq] = o[n][k][i + 2]; }
-          }
-        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(o_full(buf));
       }
-      compute_warps_sync();
-      const bool whole = p.first && p.last;
-      const int slot = 2 * b + (pieces_done == 0 ? 0 : 1);
-      float* const part = g.a.workspace + SLOT0 + (size_t)slot * Slot<DH, NT>::FLOATS;
-      for (int i = tid; i < heads_live * (DH / 4); i += 32 * COMPUTE_WARPS) {
-        const int h = i / (DH / 4), d = (i % (DH / 4)) * 4;
-        float top = -INFINITY, sum = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < COMPUTE_WARPS; ++w) top = fmaxf(top, join_m[w * C::HEADS + h]);
-        const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll
-        for (int w = 0; w < COMPUTE_WARPS; ++w) {
-          const float fl = exp2_fast(join_m[w * C::HEADS + h] - ref), fo = exp2_fast(join_m[(COMPUTE_WARPS + w) * C::HEADS + h] - ref);
-          const float4 x = *reinterpret_cast<const float4*>(join + (w * C::HEADS + h) * (DH + PAD) + d);
-          sum += join_m[(2 * COMPUTE_WARPS + w) * C::HEADS + h] * fl;
-          acc.x += x.x * fo; acc.y += x.y * fo; acc.z += x.z * fo; acc.w += x.w * fo;
-        }
-        if (whole) {
-          const int head = kvh * g.group + h0 + h;
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;            // every page absent: zeros
-          const size_t at = (size_t)p.s * g.a.heads + head;
-          *reinterpret_cast<uint2*>(g.a.out + at * DH + d) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-          if (d == 0 && g.a.lse) g.a.lse[at] = sum == 0.f ? -INFINITY : (log2f(sum) + top) * 0.6931471805599453f;
-        } else {
-          *reinterpret_cast<float4*>(part + h * DH + d) = acc;
-          if (d == 0) { part[C::HEADS * DH + 2 * h] = top; part[C::HEADS * DH + 2 * h + 1] = sum; }
-        }
+      before = p;
+    }
+    if (pieces > 0) join_piece(before, pieces - 1);
+
+    // ---- sequences without positions, and lengths that the table cannot hold
+    for (int s = b; s < g.a.n_seq; s += gridDim.x) {
+      const int len = __ldg(g.a.len + s);
+      if (len <= 0) {
+        for (int i = tid; i < g.a.heads * DH / 8; i += 32 * COMPUTE_WARPS)
+          reinterpret_cast<uint4*>(g.a.out + (size_t)s * g.a.heads * DH)[i] = make_uint4(0, 0, 0, 0);
+        if (g.a.lse) for (int i = tid; i < g.a.heads; i += 32 * COMPUTE_WARPS) g.a.lse[(size_t)s * g.a.heads + i] = -INFINITY;
+      } else if (tid == 0 && g.a.status && len > (long long)g.a.max_pages << g.c.page_shift) {
+        atomicMax(g.a.status, (int)ET_PAGED_CAPACITY);
       }
-      if (p.first && !p.last) {
-        // the item goes on in the CTAs behind this one, each of which finds it at the start of its run
-        const long long units = units_of(g, p.len);
-        const long long item0 = begin + chunk - p.units_end;          // this piece ends this CTA's run (whole items are not cut)
-        mine = Join{p.s, p.part, (int)((item0 + units - 1) / chunk - b + 1), slot};
-      }
-      ++pieces_done;
-      compute_warps_sync();                                          // the joining buffer is free again
     }
     if (tid == 0) *reinterpret_cast<Join*>(g.a.workspace + b * 4) = mine;
   }
@@ -718,6 +797,13 @@ cudaError_t launch(const CUtensorMap& map, const Args& g, int ctas, cudaStream_t
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64 || !ready[dev]) {
+    if (NT == 2) {
+      // setmaxnreg.inc waits for registers that only exist if the block was launched with LAUNCH_REGS of them a thread
+      cudaFuncAttributes fa;
+      e = cudaFuncGetAttributes(&fa, attention_paged_kernel<DH, E4M3, NT>);
+      if (e != cudaSuccess) return e;
+      if (fa.numRegs < LAUNCH_REGS) return cudaErrorLaunchOutOfResources;
+    }
     e = cudaFuncSetAttribute(attention_paged_kernel<DH, E4M3, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) ready[dev] = true;
