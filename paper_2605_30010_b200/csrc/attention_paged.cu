@@ -41,10 +41,6 @@ static_assert(COMPUTE_WARPS % 4 == 0 && COPY_WARPS % 4 == 0, "whole warpgroups")
 static_assert(COMPUTE_WARPS * COMPUTE_REGS + COPY_WARPS * COPY_REGS <= (COMPUTE_WARPS + COPY_WARPS) * LAUNCH_REGS, "register budget");
 constexpr int QUERIES = 4;                     // pieces whose queries are on their way or waiting
 constexpr int MAX_CTAS = 148;
-#ifndef ITEM_COST_V
-#define ITEM_COST_V 2
-#endif
-constexpr int ITEM_COST = ITEM_COST_V;                   // units (tiles' worth of time) that an item costs beside its tiles
 constexpr int PAD = 4;                         // floats between heads of the joining buffer: no bank conflicts
 constexpr int SMEM_LIMIT = 232448 - 512;       // 227 KB, less the static part
 constexpr int CONTROL_BYTES = 1024;            // barriers and the ring's flags
@@ -56,6 +52,10 @@ struct Cfg {
   static constexpr int BOXES = ROW / BOX_ROW;
   static constexpr int PLANE = TILE * ROW;
   static constexpr int STAGE = 2 * PLANE;                         // keys, values
+#ifndef ICM
+#define ICM 1
+#endif
+  static constexpr int ITEM_COST = ICM*65536 / STAGE;                 // units (tiles' worth of time) that an item costs beside its tiles
   static constexpr int SCALES = E4M3 ? 2 * TILE : 0;
   static constexpr int HEADS = 8 * NT;
   static constexpr int JOIN = COMPUTE_WARPS * HEADS * (DH + PAD) * 4 + COMPUTE_WARPS * HEADS * 3 * 4;   // the warps' results of a piece
@@ -68,6 +68,7 @@ struct Cfg {
   static constexpr int STAGES = (FIT > 16 ? 16 : FIT) / GROUPS * GROUPS;
   static constexpr int SMEM = 1024 + STAGES * (STAGE + SCALES) + EDGE + CONTROL_BYTES;
   static_assert(STAGES >= GROUPS, "ring");
+  static_assert(ITEM_COST <= PAGED_ITEM_COST_MAX, "units");
   static_assert(8 * (2 * STAGES + 2 * QUERIES + 4) + 4 * STAGES + 16 <= CONTROL_BYTES, "control area");
 };
 
@@ -147,14 +148,14 @@ __device__ __forceinline__ int clamped_len(const Args& g, int s) {
   const long long cap = (long long)g.a.max_pages << g.c.page_shift;
   return (int)min((long long)max(__ldg(g.a.len + s), 0), cap);
 }
-// An item's units: its tiles and, in front of them, ITEM_COST for what every item costs however short it is.
-__device__ __forceinline__ int units_of(const Args& g, int len) {
-  return len <= 0 ? 0 : g.whole ? 1 : (int)((unsigned)(len + (TILE - 1)) / TILE) + ITEM_COST;
+// An item's units: its tiles and, in front of them, `cost` for what every item costs however short it is.
+__device__ __forceinline__ int units_of(const Args& g, int len, int cost) {
+  return len <= 0 ? 0 : g.whole ? 1 : (int)((unsigned)(len + (TILE - 1)) / TILE) + cost;
 }
 
 // The run of units that falls to a CTA, walked piece by piece.
 struct Walk {
-  long long left;                  // units still to do
+  int left;                        // units still to do
   int s, part, unit;               // next unit: sequence, key / value head x head tile, unit of the item
   int len;                         // of the sequence
 };
@@ -165,14 +166,14 @@ struct Piece {
   bool first, last;                // contains the item's first, last tile
 };
 
-__device__ __forceinline__ bool next_piece(const Args& g, int parts_all, Walk& w, Piece& p) {
+__device__ __forceinline__ bool next_piece(const Args& g, int parts_all, int cost, Walk& w, Piece& p) {
   while (w.left > 0) {
-    const int units = units_of(g, w.len);
+    const int units = units_of(g, w.len, cost);
     if (units > 0) {
-      const int n = w.left < units - w.unit ? (int)w.left : units - w.unit, end = w.unit + n;
+      const int n = min(w.left, units - w.unit), end = w.unit + n;
       p.s = w.s; p.part = w.part; p.len = w.len; p.units_end = end;
-      p.t0 = g.whole ? 0 : max(w.unit - ITEM_COST, 0);
-      p.t1 = g.whole ? (int)((unsigned)(w.len + (TILE - 1)) / TILE) : max(end - ITEM_COST, 0);
+      p.t0 = g.whole ? 0 : max(w.unit - cost, 0);
+      p.t1 = g.whole ? (int)((unsigned)(w.len + (TILE - 1)) / TILE) : max(end - cost, 0);
       p.first = p.t0 == 0; p.last = end == units;
       w.left -= n; w.unit = end;
       if (end == units) { w.unit = 0; ++w.part; }
@@ -190,7 +191,7 @@ template <int DH, bool E4M3, int NT>
 __global__ void __launch_bounds__(THREADS, 1)
 attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ Args g) {
   using C = Cfg<DH, E4M3, NT>;
-  constexpr int STAGES = C::STAGES, KS = DH / 16;
+  constexpr int STAGES = C::STAGES, KS = DH / 16, ITEM_COST = C::ITEM_COST;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const gen = smem_raw + (base - raw);
@@ -211,7 +212,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
   auto o_empty = [&](int i) { return bars + 8u * (uint32_t)(2 * STAGES + 2 * QUERIES + 2 + i); };
   volatile int* const absent = reinterpret_cast<volatile int*>(ctl + 8 * (2 * STAGES + 2 * QUERIES + 4));   // [STAGES]: bit i = slice i has no page
   volatile int* const abort_flag = absent + STAGES;
-  __shared__ long long warp_sum_s[THREADS / 32];
+  __shared__ int warp_sum_s[THREADS / 32];
   __shared__ int walk_s[4];
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -228,40 +229,32 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 
   // ---- this CTA's run: an exclusive prefix sum of the sequences' units over the threads
   Walk walk;
-  long long begin, chunk;
+  int begin, chunk;                            // all units together are below 2^31 (checked on the host)
   {
     const int per = (g.a.n_seq + THREADS - 1) / THREADS, s0 = min(tid * per, g.a.n_seq), s1 = min(s0 + per, g.a.n_seq);
-    long long sum = 0;
-    for (int s = s0; s < s1; ++s) sum += units_of(g, clamped_len(g, s));
+    int sum = 0;
+    for (int s = s0; s < s1; ++s) sum += units_of(g, clamped_len(g, s), ITEM_COST);
     sum *= parts_all;
-    long long inc = sum;
+    int inc = sum;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const long long v = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += v; }
+    for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += v; }
     if (lane == 31) warp_sum_s[warp] = inc;
     __syncthreads();
-    long long before = inc - sum, total = 0;
+    int before = inc - sum, total = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) { const long long v = warp_sum_s[w]; if (w < warp) before += v; total += v; }
-    // (32-bit divisions wherever the numbers allow it: a 64-bit one takes hundreds of cycles)
-    const bool small = total + gridDim.x < (1ll << 31);
-    chunk = small ? ((unsigned)total + gridDim.x - 1) / gridDim.x : (total + gridDim.x - 1) / gridDim.x;
-    begin = chunk * b;
+    for (int w = 0; w < THREADS / 32; ++w) { const int v = warp_sum_s[w]; if (w < warp) before += v; total += v; }
+    chunk = (int)(((unsigned)total + gridDim.x - 1) / gridDim.x);
+    begin = min(chunk * b, total);
     if (begin >= before && begin < before + sum) {
-      long long r = begin - before;
+      int r = begin - before;
       for (int s = s0; s < s1; ++s) {
-        const int len = clamped_len(g, s), u = units_of(g, len);
-        const long long all = (long long)u * parts_all;
-        if (r < all) {
-          walk_s[0] = s; walk_s[3] = len;
-          if (small) { walk_s[1] = (int)((unsigned)r / (unsigned)u); walk_s[2] = (int)((unsigned)r % (unsigned)u); }
-          else { walk_s[1] = (int)(r / u); walk_s[2] = (int)(r % u); }
-          break;
-        }
-        r -= all;
+        const int len = clamped_len(g, s), u = units_of(g, len, ITEM_COST);
+        if (r < u * parts_all) { walk_s[0] = s; walk_s[1] = r / u; walk_s[2] = r % u; walk_s[3] = len; break; }
+        r -= u * parts_all;
       }
     }
     __syncthreads();
-    walk.left = max(0ll, min(chunk, total - begin));
+    walk.left = min(chunk, total - begin);
     walk.s = walk_s[0]; walk.part = walk_s[1]; walk.unit = walk_s[2]; walk.len = walk_s[3];
   }
 
@@ -281,7 +274,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     long long count = 0, issued = 0;
     int pieces = 0;
     Piece p;
-    while (ok && next_piece(g, parts_all, walk, p)) {
+    while (ok && next_piece(g, parts_all, ITEM_COST, walk, p)) {
       if (me == 1) {                                                 // not the warp that has the first tile to fetch
         // the piece's queries: rows of the heads, zeros for heads that the group does not have
         const int buf = pieces % QUERIES;
@@ -421,8 +414,8 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
       }
       if (p.first && !p.last) {
         // the item goes on in the CTAs behind this one, each of which finds it at the start of its run
-        const long long item0 = begin + chunk - p.units_end;          // this piece ends this CTA's run (whole items are not cut)
-        mine = Join{p.s, p.part, (int)((item0 + units_of(g, p.len) - 1) / chunk - b + 1), slot};
+        const int item0 = begin + chunk - p.units_end;          // this piece ends this CTA's run (whole items are not cut)
+        mine = Join{p.s, p.part, (item0 + units_of(g, p.len, ITEM_COST) - 1) / chunk - b + 1, slot};
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(o_empty(buf));
@@ -433,7 +426,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     long long count = 0;                                             // tiles of this CTA so far
     Piece p, before;
     bool busy;
-    for (; next_piece(g, parts_all, walk, p); ++pieces) {
+    for (; next_piece(g, parts_all, ITEM_COST, walk, p); ++pieces) {
       // A warp whose group has no tile of a short piece neither waits for its queries nor leaves an output.  (It cannot get
       // so far ahead that it takes one use of a barrier for another: a result buffer is free again only when every warp has
       // joined the piece that it held, and QUERIES pieces need more than JOINS results.)
@@ -837,7 +830,8 @@ cudaError_t launch_attention_paged(const PagedCache& c, const PagedAttention& a,
   g.parts = (g.group + 8 * nt - 1) / (8 * nt);
   const long long tiles = (((long long)a.max_pages << c.page_shift) + TILE - 1) / TILE;      // of the longest sequence there can be
   g.whole = tiles <= 4;
-  const long long most = (long long)a.n_seq * c.kv_heads * g.parts * (g.whole ? 1 : tiles);
+  const long long most = (long long)a.n_seq * c.kv_heads * g.parts * (g.whole ? 1 : tiles + PAGED_ITEM_COST_MAX);
+  if (most >= (1ll << 31) - MAX_CTAS) return cudaErrorInvalidValue;   // refused by the entry point already
   const int ctas = (int)(most < MAX_CTAS ? most : MAX_CTAS);
 #define ET_PAGED(D, E) (nt == 1 ? launch<D, E, 1>(map, g, ctas, s) : launch<D, E, 2>(map, g, ctas, s))
   if (c.head_dim == 64) return c.scale ? ET_PAGED(64, true) : ET_PAGED(64, false);

@@ -108,6 +108,8 @@ et_status et_attention_paged(const et_kv_cache* cache, const void* q_dev, long l
   if (heads < 1 || heads % c.kv_heads != 0) return ET_ERR_SHAPE;
   if (q_stride % 8 != 0 || q_stride < (long long)heads * c.head_dim) return ET_ERR_SHAPE;
   if ((long long)n_seq * heads > (1ll << 24)) return ET_ERR_CAPACITY;
+  // the work is numbered in 32 bits: tiles of 64 positions of every sequence and head
+  if ((long long)n_seq * heads * ((((long long)max_pages << c.page_shift) + 63) / 64 + PAGED_ITEM_COST_MAX) >= (1ll << 31) - 256) return ET_ERR_CAPACITY;
   if (workspace_bytes < ET_PAGED_WORKSPACE) return ET_ERR_CAPACITY;
   const PagedAttention a{(const bf16*)q_dev, q_stride, (bf16*)out_dev, lse_dev, n_seq, heads, max_pages, block_table_dev, len_dev,
                          (float*)workspace_dev, status_dev};

@@ -39,6 +39,7 @@ struct PagedAttention {
   float* workspace;
   int* status;           // may be NULL
 };
+constexpr int PAGED_ITEM_COST_MAX = 16;   // units beside its tiles of 64 positions that an item (sequence, key / value head, head tile) counts for
 cudaError_t launch_attention_paged(const PagedCache& c, const PagedAttention& a, cudaStream_t s);
 
 // c = epi(a[M][K] * w[N][K]^T + bias), M <= LINEAR_ROWS_MAX
