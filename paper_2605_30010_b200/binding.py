@@ -775,54 +775,65 @@ def et_attention_causal(qkv, n_seq, L, heads, kv_heads, head_dim, stream=None):
 
 
 # --------------------------------------------------------------------------------------------
-# The decode step (include/earlytom_decode.h)
+# The decode step (include/earlytom_decode.h).  A decode step makes hundreds of these calls, each a few microseconds of device
+# time, so they marshal plain integers and build no messages unless a check fails.
 # --------------------------------------------------------------------------------------------
 
-def _need(ok, what: str):
-    if not ok:
-        raise EarlyTomError(1, what)
+def _refuse(what: str):
+    raise EarlyTomError(1, what)
 
 
-def _on_device(*tensors):
-    """The library launches on the current device: every tensor has to live there."""
+def _launch_on(stream, *tensors) -> int:
+    """The stream's handle.  The library launches on the current device: every tensor has to live there."""
     import torch
-    dev = torch.cuda.current_device()
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else -2
     for t in tensors:
-        _need(t is None or (t.is_cuda and t.get_device() == dev), "tensors must be on the current CUDA device")
+        if t is not None and t.get_device() != dev:
+            _refuse("tensors must be on the current CUDA device")
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
-def _int32(t, n, what):
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _ints(t, n, what):
     import torch
-    _need(t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n), f"{what}: contiguous int32 [{n}]")
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous():
+        _refuse(f"{what}: contiguous int32 [{n}]")
 
 
-def _rows(t, rows, width, what):
-    """bf16 [rows, >= width] with contiguous columns; its row stride in elements."""
+def _row_stride(t, width, what):
+    """Row stride in elements of a bf16 matrix whose rows have at least `width` contiguous values."""
     import torch
-    _need(t.dtype == torch.bfloat16 and t.dim() == 2 and t.shape[0] == rows and t.shape[1] >= width
-          and (t.shape[1] == 1 or t.stride(1) == 1), f"{what}: bf16 [{rows}, >= {width}] with contiguous columns")
-    return t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
+    if t.dtype is not torch.bfloat16 or t.dim() != 2 or t.shape[1] < width or t.stride(1) != 1:
+        _refuse(f"{what}: bf16 [rows, >= {width}] with contiguous columns")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
 
 
 def _kv_cache(cache, scale):
     """cache [n_pages, 2, kv_heads, page_size, head_dim] bf16 or e4m3 (scale uint8 [n_pages, 2, kv_heads, page_size])."""
     import torch
-    _need(cache.dim() == 5 and cache.shape[1] == 2 and cache.is_contiguous(), "cache: contiguous [n_pages, 2, kv_heads, page_size, head_dim]")
-    e4m3 = cache.dtype == torch.float8_e4m3fn
-    _need(e4m3 or cache.dtype == torch.bfloat16, "cache: bfloat16 or float8_e4m3fn")
-    _need(e4m3 == (scale is not None), "scale goes with an e4m3 cache, and only with one")
-    if e4m3:
-        _need(scale.dtype == torch.uint8 and scale.is_contiguous() and scale.shape == cache.shape[:4],
-              "scale: contiguous uint8 [n_pages, 2, kv_heads, page_size]")
-    n_pages, _, kv_heads, page_size, head_dim = cache.shape
-    return et_kv_cache(cache.data_ptr(), scale.data_ptr() if e4m3 else None, n_pages, kv_heads, page_size, head_dim,
-                       ET_KV_E4M3 if e4m3 else ET_KV_BF16)
+    shape = cache.shape
+    if len(shape) != 5 or shape[1] != 2 or not cache.is_contiguous():
+        _refuse("cache: contiguous [n_pages, 2, kv_heads, page_size, head_dim]")
+    if cache.dtype is torch.bfloat16:
+        if scale is not None:
+            _refuse("scale goes with an e4m3 cache only")
+        return et_kv_cache(cache.data_ptr(), None, shape[0], shape[2], shape[3], shape[4], ET_KV_BF16)
+    if cache.dtype is not torch.float8_e4m3fn:
+        _refuse("cache: bfloat16 or float8_e4m3fn")
+    if scale is None or scale.dtype is not torch.uint8 or scale.shape != shape[:4] or not scale.is_contiguous():
+        _refuse("an e4m3 cache needs scale: contiguous uint8 [n_pages, 2, kv_heads, page_size]")
+    return et_kv_cache(cache.data_ptr(), scale.data_ptr(), shape[0], shape[2], shape[3], shape[4], ET_KV_E4M3)
 
 
-def _table(block_table, n_seq=None):
+def _table(block_table):
     import torch
-    _need(block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.is_contiguous()
-          and (n_seq is None or block_table.shape[0] == n_seq), "block_table: contiguous int32 [n_seq, max_pages]")
+    if block_table.dtype is not torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous():
+        _refuse("block_table: contiguous int32 [n_seq, max_pages]")
     return block_table.shape
 
 
@@ -834,18 +845,24 @@ def et_kv_append(cache, scale, qkv, heads, block_table, start, row_offsets=None,
     c = _kv_cache(cache, scale)
     n_seq, max_pages = _table(block_table)
     rows = qkv.shape[0]
-    _on_device(cache, scale, qkv, block_table, start, row_offsets, q_out, new_len, status)
-    stride = _rows(qkv, rows, (heads + 2 * c.kv_heads) * c.head_dim, "qkv")
-    _int32(start, n_seq, "start")
-    _int32(row_offsets, n_seq + 1, "row_offsets")
-    _int32(new_len, n_seq, "new_len")
-    _int32(status, 1, "status")
-    if q_out is None and theta != 0 and heads > 0:
-        q_out = torch.empty((rows, heads * c.head_dim), dtype=torch.bfloat16, device=qkv.device)
-    _need(q_out is None or (q_out.dtype == torch.bfloat16 and q_out.is_contiguous() and q_out.numel() == rows * heads * c.head_dim),
-          "q_out: contiguous bf16 [rows, heads * head_dim]")
-    _check(lib().et_kv_append(C.byref(c), _ptr(qkv), stride, rows, heads, _ptr(block_table), n_seq, max_pages, _ptr(row_offsets),
-                              _ptr(start), float(theta), _ptr(q_out), _ptr(new_len), _ptr(status), _stream_ptr(stream)))
+    s = _launch_on(stream, cache, scale, qkv, block_table, start, row_offsets, q_out, new_len, status)
+    stride = _row_stride(qkv, (heads + 2 * c.kv_heads) * c.head_dim, "qkv")
+    _ints(start, n_seq, "start")
+    if row_offsets is not None:
+        _ints(row_offsets, n_seq + 1, "row_offsets")
+    if new_len is not None:
+        _ints(new_len, n_seq, "new_len")
+    if status is not None:
+        _ints(status, 1, "status")
+    if q_out is None:
+        if theta != 0 and heads > 0:
+            q_out = torch.empty((rows, heads * c.head_dim), dtype=torch.bfloat16, device=qkv.device)
+    elif q_out.dtype is not torch.bfloat16 or q_out.numel() != rows * heads * c.head_dim or not q_out.is_contiguous():
+        _refuse("q_out: contiguous bf16 [rows, heads * head_dim]")
+    st = lib().et_kv_append(C.byref(c), qkv.data_ptr(), stride, rows, heads, block_table.data_ptr(), n_seq, max_pages,
+                            _at(row_offsets), start.data_ptr(), theta, _at(q_out), _at(new_len), _at(status), s)
+    if st:
+        _check(st)
     return q_out
 
 
@@ -858,13 +875,19 @@ def et_kv_read(cache, scale, block_table, start, rows, row_offsets=None, out=Non
     width = 2 * c.kv_heads * c.head_dim
     if out is None:
         out = torch.zeros((rows, width), dtype=torch.bfloat16, device=cache.device)
-    _on_device(cache, scale, block_table, start, row_offsets, out, status)
-    stride = _rows(out, rows, width, "out")
-    _int32(start, n_seq, "start")
-    _int32(row_offsets, n_seq + 1, "row_offsets")
-    _int32(status, 1, "status")
-    _check(lib().et_kv_read(C.byref(c), _ptr(out), stride, rows, _ptr(block_table), n_seq, max_pages, _ptr(row_offsets), _ptr(start),
-                            _ptr(status), _stream_ptr(stream)))
+    elif out.shape[0] != rows:
+        _refuse("out: as many rows as are read")
+    s = _launch_on(stream, cache, scale, block_table, start, row_offsets, out, status)
+    stride = _row_stride(out, width, "out")
+    _ints(start, n_seq, "start")
+    if row_offsets is not None:
+        _ints(row_offsets, n_seq + 1, "row_offsets")
+    if status is not None:
+        _ints(status, 1, "status")
+    st = lib().et_kv_read(C.byref(c), out.data_ptr(), stride, rows, block_table.data_ptr(), n_seq, max_pages, _at(row_offsets),
+                          start.data_ptr(), _at(status), s)
+    if st:
+        _check(st)
     return out
 
 
@@ -873,23 +896,30 @@ def et_attention_paged(q, heads, cache, scale, block_table, lens, out=None, lse=
     given; workspace: uint8 [ET_PAGED_WORKSPACE], created if none is given."""
     import torch
     c = _kv_cache(cache, scale)
-    n_seq, max_pages = _table(block_table, q.shape[0])
+    n_seq, max_pages = _table(block_table)
     width = heads * c.head_dim
-    stride = _rows(q, n_seq, width, "q")
+    if q.shape[0] != n_seq:
+        _refuse("block_table: a row for each row of q")
+    stride = _row_stride(q, width, "q")
     if out is None:
         out = torch.empty((n_seq, width), dtype=torch.bfloat16, device=q.device)
+    elif out.dtype is not torch.bfloat16 or out.numel() != n_seq * width or not out.is_contiguous():
+        _refuse("out: contiguous bf16 [n_seq, heads * head_dim]")
     if workspace is None:
         workspace = torch.empty(ET_PAGED_WORKSPACE, dtype=torch.uint8, device=q.device)
-    _on_device(q, cache, scale, block_table, lens, out, lse, workspace, status)
-    _need(out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == n_seq * width, "out: contiguous bf16 [n_seq, heads * head_dim]")
-    _need(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == n_seq * heads),
-          "lse: contiguous float32 [n_seq, heads]")
-    _need(workspace.is_contiguous(), "workspace: contiguous")
-    _int32(lens, n_seq, "lens")
-    _int32(status, 1, "status")
-    _check(lib().et_attention_paged(C.byref(c), _ptr(q), stride, _ptr(out), _ptr(lse), n_seq, heads, _ptr(block_table), max_pages,
-                                    _ptr(lens), _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(status),
-                                    _stream_ptr(stream)))
+    elif not workspace.is_contiguous():
+        _refuse("workspace: contiguous")
+    s = _launch_on(stream, q, cache, scale, block_table, lens, out, lse, workspace, status)
+    if lse is not None and (lse.dtype is not torch.float32 or lse.numel() != n_seq * heads or not lse.is_contiguous()):
+        _refuse("lse: contiguous float32 [n_seq, heads]")
+    _ints(lens, n_seq, "lens")
+    if status is not None:
+        _ints(status, 1, "status")
+    st = lib().et_attention_paged(C.byref(c), q.data_ptr(), stride, out.data_ptr(), _at(lse), n_seq, heads, block_table.data_ptr(),
+                                  max_pages, lens.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                  _at(status), s)
+    if st:
+        _check(st)
     return out
 
 
@@ -897,18 +927,25 @@ def et_linear_rows(a, w, bias=None, epilogue=0, gelu_tanh=1, c=None, status=None
     """a [M <= 32, K] bf16, w [N, K] bf16, bias [N] f32 or None.  Returns c (bf16; fp32, added to in place, with epilogue 2)."""
     import torch
     M, K = a.shape
-    N = w.shape[0]
+    N, Kw = w.shape
     outs = N // 2 if epilogue == 4 else N
     dtype = torch.float32 if epilogue == 2 else torch.bfloat16
     if c is None:
-        _need(epilogue != 2, "epilogue 2 adds to c")
+        if epilogue == 2:
+            _refuse("epilogue 2 adds to c")
         c = torch.empty((M, outs), dtype=dtype, device=a.device)
-    _on_device(a, w, bias, c, status)
-    _int32(status, 1, "status")
-    _need(a.dtype == torch.bfloat16 and a.is_contiguous(), "a: contiguous bf16 [M, K]")
-    _need(w.dtype == torch.bfloat16 and w.is_contiguous() and w.dim() == 2 and w.shape[1] == K, "w: contiguous bf16 [N, K]")
-    _need(bias is None or (bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == N), "bias: contiguous float32 [N]")
-    _need(c.dtype == dtype and c.is_contiguous() and c.numel() == M * outs, f"c: contiguous {dtype} [M, {outs}]")
-    _check(lib().et_linear_rows(_ptr(a), _ptr(w), _ptr(bias), _ptr(c), M, N, K, int(epilogue), int(gelu_tanh), _ptr(status),
-                                _stream_ptr(stream)))
+    elif c.dtype is not dtype or c.numel() != M * outs or not c.is_contiguous():
+        _refuse(f"c: contiguous {dtype} [{M}, {outs}]")
+    s = _launch_on(stream, a, w, bias, c, status)
+    if a.dtype is not torch.bfloat16 or not a.is_contiguous():
+        _refuse("a: contiguous bf16 [M, K]")
+    if w.dtype is not torch.bfloat16 or Kw != K or not w.is_contiguous():
+        _refuse("w: contiguous bf16 [N, K]")
+    if bias is not None and (bias.dtype is not torch.float32 or bias.numel() != N or not bias.is_contiguous()):
+        _refuse("bias: contiguous float32 [N]")
+    if status is not None:
+        _ints(status, 1, "status")
+    st = lib().et_linear_rows(a.data_ptr(), w.data_ptr(), _at(bias), c.data_ptr(), M, N, K, epilogue, gelu_tanh, _at(status), s)
+    if st:
+        _check(st)
     return c
