@@ -126,10 +126,10 @@ __device__ __forceinline__ void arrive_expect_elect(uint32_t bar, uint32_t bytes
   asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
                "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void tma_load_elect(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+__device__ __forceinline__ void tma_load_elect(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, uint64_t policy) {
   asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
-               "@q cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n\t}"
-               ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+               "@q cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4}], [%2], %5;\n\t}"
+               ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void bulk_load_elect(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
@@ -218,7 +218,6 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int b = blockIdx.x;
   const int kv_heads = g.c.kv_heads, parts_all = kv_heads * g.parts;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");    // the joining kernel may be set up; it waits for this grid's end
   if (tid == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
 
   if (tid < STAGES) { mbar_init(full(tid), 1); mbar_init(empty(tid), GROUP_WARPS); }
@@ -227,6 +226,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
   if (tid == 0) *abort_flag = 0;
   if (tid < 32) asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 
+  begin_after_previous();
   // ---- this CTA's run: an exclusive prefix sum of the sequences' units over the threads
   Walk walk;
   int begin, chunk;                            // all units together are below 2^31 (checked on the host)
@@ -269,6 +269,10 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     const int box_shift = min(g.c.page_shift, 6), box_rows = 1 << box_shift, boxes_tile = TILE >> box_shift;
     const uint32_t box_bytes = (uint32_t)box_rows * (2 * C::ROW + (E4M3 ? 2 : 0));
     const int plane_rows = kv_heads << g.c.page_shift;
+    // the cache is read once (several head tiles read it soon after one another): it need not push other things out of L2
+    uint64_t policy;
+    if (g.parts > 1) asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
+    else asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
     int stage = me;
     uint32_t phase = 0;
     long long count = 0, issued = 0;
@@ -340,7 +344,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 #pragma unroll
               for (int half = 0; half < C::BOXES; ++half)
                 tma_load_elect(dst + plane * C::PLANE + half * (TILE * C::BOX_ROW) + r0 * C::BOX_ROW, &map, bar,
-                               half * (C::BOX_ROW / (E4M3 ? 1 : 2)), y);
+                               half * (C::BOX_ROW / (E4M3 ? 1 : 2)), y, policy);
               if (E4M3) bulk_load_elect(sdst + plane * TILE + r0, g.c.scale + (unsigned)y, (uint32_t)box_rows, bar);
             }
           }
@@ -723,7 +727,7 @@ constexpr int JOIN_THREADS = 128;
 template <int DH, int NT>
 __global__ void __launch_bounds__(JOIN_THREADS)
 attention_join_kernel(const __grid_constant__ Args g) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  begin_after_previous();
   constexpr int HEADS = 8 * NT, LANES = DH / 4, RUNS = JOIN_THREADS / LANES;
   const Join j = *reinterpret_cast<const Join*>(g.a.workspace + blockIdx.x * 4);
   const int h = blockIdx.y, kvh = j.part / g.parts, h0 = (j.part % g.parts) * HEADS;
@@ -802,20 +806,12 @@ cudaError_t launch(const CUtensorMap& map, const Args& g, int ctas, cudaStream_t
     if (dev >= 0 && dev < 64) ready[dev] = true;
   }
   ET_COUNT_LAUNCH();
-  attention_paged_kernel<DH, E4M3, NT><<<ctas, THREADS, C::SMEM, s>>>(map, g);
-  e = cudaGetLastError();
+  Launch l(ctas, THREADS, C::SMEM, s);
+  e = cudaLaunchKernelEx(&l.cfg, attention_paged_kernel<DH, E4M3, NT>, map, g);
   if (e != cudaSuccess || g.whole) return e;
   ET_COUNT_LAUNCH();
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ctas, g.group < C::HEADS ? g.group : C::HEADS);
-  cfg.blockDim = dim3(JOIN_THREADS);
-  cfg.stream = s;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attention_join_kernel<DH, NT>, g);
+  Launch join(dim3(ctas, g.group < C::HEADS ? g.group : C::HEADS), JOIN_THREADS, 0, s);
+  return cudaLaunchKernelEx(&join.cfg, attention_join_kernel<DH, NT>, g);
 }
 
 }  // namespace

@@ -47,6 +47,31 @@ constexpr int LINEAR_ROWS_MAX = 32;
 cudaError_t launch_linear_rows(const bf16* a, const bf16* w, const float* bias, void* c, int M, int N, int K, int epilogue,
                                int gelu_tanh, int* status, cudaStream_t s);
 
+// Every kernel of the decode step is launched so that it may be set up while the kernel before it in the stream still runs
+// (programmatic dependent launch), and begins, before it touches memory, by waiting for that one's end and results.
+__device__ __forceinline__ void begin_after_previous() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");    // the next kernel may be set up; it waits in turn
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+struct Launch {
+  cudaLaunchAttribute attr[2];
+  cudaLaunchConfig_t cfg = {};
+  Launch(dim3 blocks, int threads, size_t smem, cudaStream_t s, int cluster = 1) {
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.gridDim = blocks;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+  }
+  Launch(const Launch&) = delete;
+};
+
 // Place of a position of sequence s; false (with the status) if it has none.
 __device__ __forceinline__ bool paged_place(const PagedCache& c, const int* table, int max_pages, int s, long long pos, int* status,
                                             int& page, int& place) {

@@ -148,6 +148,7 @@ linear_direct_kernel(const LinearArgs g) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[i][n][0] = acc[i][n][1] = acc[i][n][2] = acc[i][n][3] = 0.f;
 
+  begin_after_previous();
   Vec wb[2][2];                                // [tile][row]
   auto load_w = [&](int k) {
 #pragma unroll
@@ -249,8 +250,11 @@ linear_ring_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
     for (int s = 0; s < R::STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), RING_WARPS); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&wmap) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&amap) : "memory");
   }
   __syncthreads();
+  begin_after_previous();
 
   bool ok = true;
   float acc[2][NT][4];
@@ -262,8 +266,6 @@ linear_ring_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
   const int r0 = gated ? (warp >> 1) * 64 + (warp & 1) * 16 : warp * 32, r1 = r0 + (gated ? 32 : 16);
   if (warp == RING_WARPS) {
     if (lane == 0) {
-      asm volatile("prefetch.tensormap [%0];" ::"l"(&wmap) : "memory");
-      asm volatile("prefetch.tensormap [%0];" ::"l"(&amap) : "memory");
       int stage = 0, issued = 0;
       uint32_t phase = 0;
       for (; issued < mine; ++issued) {
@@ -334,28 +336,13 @@ linear_ring_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
   if (ranks > 1) cluster.sync();               // a block's sums stay until its neighbours have read them
 }
 
-struct ClusterLaunch {
-  cudaLaunchAttribute attr[1];
-  cudaLaunchConfig_t cfg = {};
-  ClusterLaunch(int blocks, int ranks, int threads, size_t smem, cudaStream_t s) {
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.gridDim = dim3(blocks * ranks);
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-  }
-};
-
 template <int NT>
 cudaError_t launch_direct(const LinearArgs& g, cudaStream_t s) {
   const int blocks = cdiv(g.N, BLOCK_ROWS);
   int ranks = 1;                               // two blocks an SM, each with two steps or more for every warp
   while (ranks < MAX_CLUSTER && blocks * ranks * 2 <= 2 * 148 && g.K >= 2 * STEP * WARPS * ranks * 2) ranks *= 2;
   const bool wide = g.K % 16 == 0 && ((reinterpret_cast<uintptr_t>(g.a) | reinterpret_cast<uintptr_t>(g.w)) & 31u) == 0;
-  ClusterLaunch l(blocks, ranks, THREADS, 0, s);
+  Launch l(blocks * ranks, THREADS, 0, s, ranks);
   ET_COUNT_LAUNCH();
   return wide ? cudaLaunchKernelEx(&l.cfg, linear_direct_kernel<NT, true>, g) : cudaLaunchKernelEx(&l.cfg, linear_direct_kernel<NT, false>, g);
 }
@@ -376,7 +363,7 @@ cudaError_t launch_ring(const LinearArgs& g, cudaStream_t s) {
     e = cudaFuncSetAttribute(linear_ring_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::SMEM);
     if (e != cudaSuccess) return e;
     for (int ranks = MAX_CLUSTER; ranks >= 1; --ranks) {
-      ClusterLaunch probe(1, ranks, RING_THREADS, R::SMEM, s);
+      Launch probe(ranks, RING_THREADS, R::SMEM, s, ranks);
       int n = 0;
       e = cudaOccupancyMaxActiveClusters(&n, linear_ring_kernel<NT>, &probe.cfg);
       if (e != cudaSuccess) return e;
@@ -386,7 +373,7 @@ cudaError_t launch_ring(const LinearArgs& g, cudaStream_t s) {
   const int blocks = cdiv(g.N, RING_ROWS), steps = cdiv(g.K, STEP);
   int ranks = 1;
   for (int r = 2; r <= MAX_CLUSTER && steps >= 4 * r; ++r) if (blocks <= resident[dev][r]) ranks = r;
-  ClusterLaunch l(blocks, ranks, RING_THREADS, R::SMEM, s);
+  Launch l(blocks * ranks, RING_THREADS, R::SMEM, s, ranks);
   ET_COUNT_LAUNCH();
   return cudaLaunchKernelEx(&l.cfg, linear_ring_kernel<NT>, *reinterpret_cast<const CUtensorMap*>(w.bytes),
                             *reinterpret_cast<const CUtensorMap*>(a.bytes), g);
