@@ -39,7 +39,9 @@ constexpr int THREADS = 32 * (COMPUTE_WARPS + COPY_WARPS);
 constexpr int LAUNCH_REGS = 168, COMPUTE_REGS = 208, COPY_REGS = 88;
 static_assert(COMPUTE_WARPS % 4 == 0 && COPY_WARPS % 4 == 0, "whole warpgroups");
 static_assert(COMPUTE_WARPS * COMPUTE_REGS + COPY_WARPS * COPY_REGS <= (COMPUTE_WARPS + COPY_WARPS) * LAUNCH_REGS, "register budget");
-constexpr int QUERIES = 4;                     // pieces whose queries are on their way or waiting
+// A group takes an item of up to so many tiles alone, where a CTA has several: 72 sequences of 250, 16 heads of 128, e4m3:
+// 29.8 -> 18.3 us, 56 of 320 29.9 -> 21.5 us; with 32 a batch of long and short ones gets slower (55.8 -> 60.2 us).
+constexpr int ALONE_TILES = 8;
 constexpr int MAX_CTAS = 148;
 constexpr int PAD = 4;                         // floats between heads of the joining buffer: no bank conflicts
 constexpr int SMEM_LIMIT = 232448 - 512;       // 227 KB, less the static part
@@ -61,7 +63,9 @@ struct Cfg {
   static constexpr int JOIN = COMPUTE_WARPS * HEADS * (DH + PAD) * 4 + COMPUTE_WARPS * HEADS * 3 * 4;   // the warps' results of a piece
   static constexpr int JOINS = NT == 1 ? 2 : 1;                   // pieces whose results can wait to be joined
   static constexpr int Q_ROW = DH * 2 + 16;                       // a head's query; 16 bytes more: no bank conflicts
-  static constexpr int EDGE = JOINS * JOIN + QUERIES * HEADS * Q_ROW;
+  static constexpr bool ALONE = NT == 1;                          // (with 16 heads there is no room for what it takes)
+  static constexpr int PAIR = ALONE ? HEADS * (DH + PAD) * 4 + 3 * HEADS * 4 : 0;   // a group's own results
+  static constexpr int EDGE = JOINS * JOIN + GROUPS * (HEADS * Q_ROW + PAIR);
   static constexpr int FIT = (SMEM_LIMIT - 1024 - CONTROL_BYTES - EDGE) / (STAGE + SCALES);
   // a multiple of the groups, so that a stage is always the same warps': they wait for its copies in turn, where warps that come to a
   // stage for the first time in its second round could take the barrier's state of the first for their own
@@ -69,7 +73,7 @@ struct Cfg {
   static constexpr int SMEM = 1024 + STAGES * (STAGE + SCALES) + EDGE + CONTROL_BYTES;
   static_assert(STAGES >= GROUPS, "ring");
   static_assert(ITEM_COST <= PAGED_ITEM_COST_MAX, "units");
-  static_assert(8 * (2 * STAGES + 2 * QUERIES + 4) + 4 * STAGES + 16 <= CONTROL_BYTES, "control area");
+  static_assert(8 * (2 * STAGES + 2 * GROUPS + 4) + 4 * STAGES + 16 <= CONTROL_BYTES, "control area");
 };
 
 // Workspace: one descriptor per CTA, then two slots of partial results per CTA.
@@ -136,6 +140,7 @@ __device__ __forceinline__ void bulk_load_elect(uint32_t dst, const void* src, u
                "@q cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}"
                ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void group_sync(int group) { asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(32 * GROUP_WARPS) : "memory"); }
 // 16 bytes by a lane's own asynchronous copy (zeros if not live); copies_arrive: an arrival once the lane's copies so far are there
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
@@ -158,20 +163,37 @@ struct Walk {
   int left;                        // units still to do
   int s, part, unit;               // next unit: sequence, key / value head x head tile, unit of the item
   int len;                         // of the sequence
+  bool opened;                     // a piece has been given out
 };
 
 struct Piece {
   int s, part, len, t0, t1;        // tiles t0 .. t1 - 1
-  int units_end;                   // the item's units up to this piece's end
+  int units, units_end;            // the item's units, and those up to this piece's end
   bool first, last;                // contains the item's first, last tile
+  bool opens;                      // is the first piece of its run
 };
+
+// Which of a piece's tiles a group takes: every GROUPS-th one, or all or none of an item that is short next to the run (a
+// piece that the groups share costs them all its queries, its result and a wait for one another, as much as several tiles).
+// `turn` goes round the groups; copying and computing warps deal alike.
+struct Deal { int t, step; bool alone; };
+__device__ __forceinline__ Deal deal(const Piece& p, bool may, int chunk, int group, int& turn) {
+  Deal d;
+  const int n = p.t1 - p.t0;
+  d.alone = may && n <= ALONE_TILES && p.units * GROUPS <= chunk;
+  const int behind = (group - turn) & (GROUPS - 1);
+  d.t = d.alone ? (behind == 0 ? p.t0 : p.t1) : p.t0 + behind;
+  d.step = d.alone ? 1 : GROUPS;
+  turn = (turn + (d.alone ? 1 : n)) & (GROUPS - 1);
+  return d;
+}
 
 __device__ __forceinline__ bool next_piece(const Args& g, int parts_all, int cost, Walk& w, Piece& p) {
   while (w.left > 0) {
     const int units = units_of(g, w.len, cost);
     if (units > 0) {
       const int n = min(w.left, units - w.unit), end = w.unit + n;
-      p.s = w.s; p.part = w.part; p.len = w.len; p.units_end = end;
+      p.s = w.s; p.part = w.part; p.len = w.len; p.units = units; p.units_end = end;
       p.t0 = g.whole ? 0 : max(w.unit - cost, 0);
       p.t1 = g.whole ? (int)((unsigned)(w.len + (TILE - 1)) / TILE) : max(end - cost, 0);
       p.first = p.t0 == 0; p.last = end == units;
@@ -182,7 +204,7 @@ __device__ __forceinline__ bool next_piece(const Args& g, int parts_all, int cos
       w.part = 0;
       if (++w.s >= g.a.n_seq) w.left = 0; else if (w.left > 0) w.len = clamped_len(g, w.s);
     }
-    if (units > 0 && p.t1 > p.t0) return true;                    // else the run ended in front of the item's first tile
+    if (units > 0 && p.t1 > p.t0) { p.opens = !w.opened; w.opened = true; return true; }   // else the run ended in front of the item's first tile
   }
   return false;
 }
@@ -201,27 +223,28 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
   // maximum, sum
   constexpr int JOIN_M = COMPUTE_WARPS * C::HEADS * (DH + PAD);
   auto join_of = [&](int i) { return reinterpret_cast<float*>(edge + i * C::JOIN); };
-  auto query_of = [&](int i) { return edge + C::JOINS * C::JOIN + i * (C::HEADS * C::Q_ROW); };
+  auto query_of = [&](int i) { return edge + C::JOINS * C::JOIN + i * (C::HEADS * C::Q_ROW); };             // of a group
+  auto pair_of = [&](int i) { return reinterpret_cast<float*>(edge + C::JOINS * C::JOIN + GROUPS * (C::HEADS * C::Q_ROW) + i * C::PAIR); };
   uint8_t* const ctl = edge + C::EDGE;
   const uint32_t bars = smem_u32(ctl);
   auto full = [&](int s) { return bars + 8u * (uint32_t)s; };
   auto empty = [&](int s) { return bars + 8u * (uint32_t)(STAGES + s); };
   auto q_full = [&](int i) { return bars + 8u * (uint32_t)(2 * STAGES + i); };
-  auto q_empty = [&](int i) { return bars + 8u * (uint32_t)(2 * STAGES + QUERIES + i); };
-  auto o_full = [&](int i) { return bars + 8u * (uint32_t)(2 * STAGES + 2 * QUERIES + i); };
-  auto o_empty = [&](int i) { return bars + 8u * (uint32_t)(2 * STAGES + 2 * QUERIES + 2 + i); };
-  volatile int* const absent = reinterpret_cast<volatile int*>(ctl + 8 * (2 * STAGES + 2 * QUERIES + 4));   // [STAGES]: bit i = slice i has no page
+  auto q_empty = [&](int i) { return bars + 8u * (uint32_t)(2 * STAGES + GROUPS + i); };
+  auto o_full = [&](int i) { return bars + 8u * (uint32_t)(2 * STAGES + 2 * GROUPS + i); };
+  auto o_empty = [&](int i) { return bars + 8u * (uint32_t)(2 * STAGES + 2 * GROUPS + 2 + i); };
+  volatile int* const absent = reinterpret_cast<volatile int*>(ctl + 8 * (2 * STAGES + 2 * GROUPS + 4));   // [STAGES]: bit i = slice i has no page
   volatile int* const abort_flag = absent + STAGES;
+
   __shared__ int warp_sum_s[THREADS / 32];
   __shared__ int walk_s[4];
-
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int b = blockIdx.x;
   const int kv_heads = g.c.kv_heads, parts_all = kv_heads * g.parts;
   if (tid == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
 
   if (tid < STAGES) { mbar_init(full(tid), 1); mbar_init(empty(tid), GROUP_WARPS); }
-  if (tid < QUERIES) { mbar_init(q_full(tid), 32); mbar_init(q_empty(tid), COMPUTE_WARPS); }
+  if (tid < GROUPS) { mbar_init(q_full(tid), 32); mbar_init(q_empty(tid), GROUP_WARPS); }
   if (tid < C::JOINS) { mbar_init(o_full(tid), COMPUTE_WARPS); mbar_init(o_empty(tid), COMPUTE_WARPS); }
   if (tid == 0) *abort_flag = 0;
   if (tid < 32) asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -255,7 +278,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     }
     __syncthreads();
     walk.left = min(chunk, total - begin);
-    walk.s = walk_s[0]; walk.part = walk_s[1]; walk.unit = walk_s[2]; walk.len = walk_s[3];
+    walk.s = walk_s[0]; walk.part = walk_s[1]; walk.unit = walk_s[2]; walk.len = walk_s[3]; walk.opened = false;
   }
 
   bool ok = true;
@@ -275,25 +298,27 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     else asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
     int stage = me;
     uint32_t phase = 0;
-    long long count = 0, issued = 0;
-    int pieces = 0;
+    long long issued = 0;
+    int turn = 0;
+    uint32_t q_phase = 0;
     Piece p;
     while (ok && next_piece(g, parts_all, ITEM_COST, walk, p)) {
-      if (me == 1) {                                                 // not the warp that has the first tile to fetch
-        // the piece's queries: rows of the heads, zeros for heads that the group does not have
-        const int buf = pieces % QUERIES;
-        ok = mbar_wait_warp(q_empty(buf), ((uint32_t)(pieces / QUERIES) & 1u) ^ 1u, abort_flag);
-        if (!ok) break;
+      const Deal dl = deal(p, C::ALONE, chunk, me, turn);
+      if (dl.t >= p.t1) continue;
+      // the piece's queries: rows of the heads, zeros for heads that the group does not have
+      ok = mbar_wait_warp(q_empty(me), q_phase ^ 1u, abort_flag);
+      if (!ok) break;
+      q_phase ^= 1u;
+      {
         const int h0 = (p.part % g.parts) * C::HEADS;
         const bf16* src = g.a.q + (size_t)p.s * g.a.q_stride + (size_t)((p.part / g.parts) * g.group + h0) * DH;
-        const uint32_t dst = smem_u32(query_of(buf));
+        const uint32_t dst = smem_u32(query_of(me));
 #pragma unroll
         for (int i = 0; i < C::HEADS * (DH / 8) / 32; ++i) {
           const int e = i * 32 + lane, h = e / (DH / 8), d = e % (DH / 8);
           copy16(dst + h * C::Q_ROW + d * 16, src + (h0 + h < g.group ? h * DH + d * 8 : 0), h0 + h < g.group);
         }
-        copies_arrive(q_full(buf));
-        ++pieces;
+        copies_arrive(q_full(me));
       }
       const int* table = g.a.table + (size_t)p.s * g.a.max_pages;
       const int kvh = p.part / g.parts;
@@ -310,9 +335,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         return good ? (page * 2 * kv_heads + kvh) << g.c.page_shift : -1;
       };
       int batch = 0, rows = rows_of(load_ids(0)), ids_next = load_ids(1);
-      int t = p.t0 + ((me - (int)count) & (GROUPS - 1));
-      count += p.t1 - p.t0;
-      for (; t < p.t1; t += GROUPS) {
+      for (int t = dl.t; t < p.t1; t += dl.step) {
         const int pos = t * TILE;                                     // lengths are below 2^31
         const int page0 = (pos >> g.c.page_shift) - first_page;       // a multiple of the tile's pages: one batch has them all
         while ((page0 >> 5) > batch) { ++batch; rows = rows_of(ids_next); ids_next = load_ids(batch + 1); }
@@ -377,18 +400,29 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     };
     const float softmax_scale = 1.4426950408889634f * (DH == 128 ? 0.08838834764831845f : 0.125f);   // log2(e) / sqrt(DH)
 
-    // Joins the warps' results of piece i: every warp has left its own in a buffer and takes a part of the heads' outputs.
-    Join mine{0, 0, 0, 0};
+    // Four values of a head's output (not yet divided), its maximum and sum: to the output, or to the workspace if others follow.
+    auto put = [&](const Piece& p, int h, int d, float4 acc, float top, float sum) {
+      if (p.first && p.last) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;              // every page absent: zeros
+        const size_t at = (size_t)p.s * g.a.heads + (p.part / g.parts) * g.group + (p.part % g.parts) * C::HEADS + h;
+        *reinterpret_cast<uint2*>(g.a.out + at * DH + d) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+        if (d == 0 && g.a.lse) g.a.lse[at] = sum == 0.f ? -INFINITY : (log2f(sum) + top) * 0.6931471805599453f;
+      } else {
+        float* const part = g.a.workspace + SLOT0 + (size_t)(2 * b + (p.opens ? 0 : 1)) * Slot<DH, NT>::FLOATS;
+        *reinterpret_cast<float4*>(part + h * DH + d) = acc;
+        if (d == 0) { part[C::HEADS * DH + 2 * h] = top; part[C::HEADS * DH + 2 * h + 1] = sum; }
+      }
+    };
+    auto heads_of = [&](const Piece& p) { return min(C::HEADS, g.group - (p.part % g.parts) * C::HEADS); };
+    // Joins the warps' results of the i-th piece that all groups share: every warp has left its own in a buffer and takes a
+    // part of the heads' outputs.
     auto join_piece = [&](const Piece& p, int i) {
       const int buf = i % C::JOINS;
       if (ok) ok = mbar_wait_warp(o_full(buf), (uint32_t)(i / C::JOINS) & 1u, abort_flag);
       const float* const join = join_of(buf);
       const float* const join_m = join + JOIN_M;
-      const int kvh = p.part / g.parts, h0 = (p.part % g.parts) * C::HEADS, heads_live = min(C::HEADS, g.group - h0);
-      const bool whole = p.first && p.last;
-      const int slot = 2 * b + (i == 0 ? 0 : 1);
-      float* const part = g.a.workspace + SLOT0 + (size_t)slot * Slot<DH, NT>::FLOATS;
-      for (int e = tid; ok && e < heads_live * (DH / 4); e += 32 * COMPUTE_WARPS) {
+      const int live = heads_of(p);
+      for (int e = tid; ok && e < live * (DH / 4); e += 32 * COMPUTE_WARPS) {
         const int h = e / (DH / 4), d = (e % (DH / 4)) * 4;
         float top = -INFINITY, sum = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -405,38 +439,27 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
             acc.x += x.x * fo; acc.y += x.y * fo; acc.z += x.z * fo; acc.w += x.w * fo;
           }
         }
-        if (whole) {
-          const int head = kvh * g.group + h0 + h;
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;            // every page absent: zeros
-          const size_t at = (size_t)p.s * g.a.heads + head;
-          *reinterpret_cast<uint2*>(g.a.out + at * DH + d) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-          if (d == 0 && g.a.lse) g.a.lse[at] = sum == 0.f ? -INFINITY : (log2f(sum) + top) * 0.6931471805599453f;
-        } else {
-          *reinterpret_cast<float4*>(part + h * DH + d) = acc;
-          if (d == 0) { part[C::HEADS * DH + 2 * h] = top; part[C::HEADS * DH + 2 * h + 1] = sum; }
-        }
-      }
-      if (p.first && !p.last) {
-        // the item goes on in the CTAs behind this one, each of which finds it at the start of its run
-        const int item0 = begin + chunk - p.units_end;          // this piece ends this CTA's run (whole items are not cut)
-        mine = Join{p.s, p.part, (item0 + units_of(g, p.len, ITEM_COST) - 1) / chunk - b + 1, slot};
+        put(p, h, d, acc, top, sum);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(o_empty(buf));
     };
 
-    int stage = 0, pieces = 0;
-    uint32_t phase = 0;
-    long long count = 0;                                             // tiles of this CTA so far
+    Join mine{0, 0, 0, 0};
+    int stage = my_group, shared = 0, turn = 0;                      // shared: pieces so far that all groups shared
+    uint32_t phase = 0, q_phase = 0;
     Piece p, before;
-    bool busy;
-    for (; next_piece(g, parts_all, ITEM_COST, walk, p); ++pieces) {
-      // A warp whose group has no tile of a short piece neither waits for its queries nor leaves an output.  (It cannot get
-      // so far ahead that it takes one use of a barrier for another: a result buffer is free again only when every warp has
-      // joined the piece that it held, and QUERIES pieces need more than JOINS results.)
-      busy = ((my_group - (int)count) & (GROUPS - 1)) < p.t1 - p.t0;
-      if (busy && ok) ok = mbar_wait_warp(q_full(pieces % QUERIES), (uint32_t)(pieces / QUERIES) & 1u, abort_flag);
-      const uint8_t* const query = query_of(pieces % QUERIES);
+    while (next_piece(g, parts_all, ITEM_COST, walk, p)) {
+      if (p.first && !p.last) {
+        // the item goes on in the CTAs behind this one, each of which finds it at the start of its run
+        const int item0 = begin + chunk - p.units_end;               // this piece ends this CTA's run (whole items are not cut)
+        mine = Join{p.s, p.part, (item0 + p.units - 1) / chunk - b + 1, 2 * b + (p.opens ? 0 : 1)};
+      }
+      const Deal dl = deal(p, C::ALONE, chunk, my_group, turn);
+      const bool busy = dl.t < p.t1;                                 // this group has tiles of the piece
+      if (dl.alone && !busy) continue;
+      if (busy && ok) ok = mbar_wait_warp(q_full(my_group), q_phase, abort_flag);
+      const uint8_t* const query = query_of(my_group);
       // ---- Q^T as the B operand: column gq = head, two rows (pairs of dimensions) a register
       uint32_t q[NT][KS][2];
       float qscale[NT][2];                                           // of heads 2 tq and 2 tq + 1
@@ -481,8 +504,11 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
           }
         }
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(q_empty(pieces % QUERIES));
+      if (busy) {
+        q_phase ^= 1u;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_empty(my_group));
+      }
       // per head 2 tq + i: running maximum m of the scores (base 2), sum l of this lane's positions; mo: maximum of score +
       // log2(scale of the value), against which the output is kept (e4m3: a value's scale is part of its weight)
       float o[NT][KS][4], m[NT][2], mo[NT][2], l[NT][2];
@@ -494,11 +520,10 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         for (int k = 0; k < KS; ++k) o[n][k][0] = o[n][k][1] = o[n][k][2] = o[n][k][3] = 0.f;
       }
 
-      for (int t = p.t0; t < p.t1; ++t, ++count) {
+      for (int t = dl.t; t < p.t1; t += dl.step) {
         const int st = stage;
         const uint32_t ph = phase;
-        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-        if ((int)(count & (GROUPS - 1)) != my_group) continue;
+        if ((stage += GROUPS) >= STAGES) { stage = my_group; phase ^= 1u; }
         if (ok) ok = mbar_wait_warp(full(st), ph, abort_flag);
         if (!ok) continue;
         // positions of each block that count: up to the length, none on an absent page (a page has whole slices)
@@ -668,42 +693,96 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         if (lane == 0) mbar_arrive(empty(st));
       }
 
-      const int heads_live = min(C::HEADS, g.group - (p.part % g.parts) * C::HEADS);
-      // ---- the piece before is joined now, when its slowest warp is done; then this warp leaves its result of this one
-      if (pieces > 0) join_piece(before, pieces - 1);
-      const int buf = pieces % C::JOINS;
-      if (ok) ok = mbar_wait_warp(o_empty(buf), ((uint32_t)(pieces / C::JOINS) & 1u) ^ 1u, abort_flag);
-      if (ok) {
-        float* const join = join_of(buf);
-        float* const join_m = join + JOIN_M;
+      // ---- this warp's result
+      const int live = heads_of(p);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], d);
+      // dst: rows of heads' outputs
+      auto leave_output = [&](float* dst) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            float x = l[n][i];
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
             const int h = n * 8 + 2 * tq + i;
-            if (gq == 0) {
-              join_m[warp * C::HEADS + h] = m[n][i];
-              join_m[(COMPUTE_WARPS + warp) * C::HEADS + h] = E4M3 ? mo[n][i] : m[n][i];
-              join_m[(2 * COMPUTE_WARPS + warp) * C::HEADS + h] = x;
-            }
-            if (busy && h < heads_live) {
-              float* dst = join + (warp * C::HEADS + h) * (DH + PAD);
+            if (h >= live) continue;
 #pragma unroll
-              for (int k = 0; k < KS; ++k) {
-                if (E4M3) *reinterpret_cast<float2*>(dst + 16 * k + 2 * gq) = make_float2(o[n][k][i], o[n][k][i + 2]);
-                else { dst[16 * k + gq] = o[n][k][i]; dst[16 * k + 8 + gq] = o[n][k][i + 2]; }
-              }
+            for (int k = 0; k < KS; ++k) {
+              if (E4M3) *reinterpret_cast<float2*>(dst + h * (DH + PAD) + 16 * k + 2 * gq) = make_float2(o[n][k][i], o[n][k][i + 2]);
+              else { dst[h * (DH + PAD) + 16 * k + gq] = o[n][k][i]; dst[h * (DH + PAD) + 16 * k + 8 + gq] = o[n][k][i + 2]; }
             }
           }
+      };
+      if (C::ALONE && dl.alone) {
+        // the group's two warps: the first leaves its result, the second adds its own, both put the sum out
+        float* const pair = pair_of(my_group);
+        float* const pair_m = pair + C::HEADS * (DH + PAD);           // [3][HEADS]: maximum, output's maximum, sum
+        group_sync(my_group);                                         // the memory is free
+        if (warp % GROUP_WARPS == 0) {
+          leave_output(pair);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int h = 2 * tq + i;
+            if (gq == 0) { pair_m[h] = m[0][i]; pair_m[C::HEADS + h] = E4M3 ? mo[0][i] : m[0][i]; pair_m[2 * C::HEADS + h] = l[0][i]; }
+          }
+        }
+        group_sync(my_group);
+        if (warp % GROUP_WARPS == 1) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int h = 2 * tq + i;
+            const float ma = pair_m[h], oa = pair_m[C::HEADS + h], la = pair_m[2 * C::HEADS + h];
+            const float top = fmaxf(ma, m[0][i]), ref = top == -INFINITY ? 0.f : top;
+            const float fa = exp2_fast(oa - ref), fb = exp2_fast((E4M3 ? mo[0][i] : m[0][i]) - ref);
+            float* const dst = pair + h * (DH + PAD);
+            if (h < live)
+#pragma unroll
+              for (int k = 0; k < KS; ++k) {
+                float* const x = dst + 16 * k + (E4M3 ? 2 * gq : gq);
+                float* const y = x + (E4M3 ? 1 : 8);
+                *x = *x * fa + o[0][k][i] * fb;
+                *y = *y * fa + o[0][k][i + 2] * fb;
+              }
+            __syncwarp();
+            if (gq == 0) { pair_m[h] = top; pair_m[2 * C::HEADS + h] = la * exp2_fast(ma - ref) + l[0][i] * exp2_fast(m[0][i] - ref); }
+          }
+        }
+        group_sync(my_group);
+        for (int e = tid % (32 * GROUP_WARPS); ok && e < live * (DH / 4); e += 32 * GROUP_WARPS) {
+          const int h = e / (DH / 4), d = (e % (DH / 4)) * 4;
+          put(p, h, d, *reinterpret_cast<const float4*>(pair + h * (DH + PAD) + d), pair_m[h], pair_m[2 * C::HEADS + h]);
+        }
+        continue;
+      }
+      // ---- the shared piece before is joined now, when its slowest warp is done; then this warp leaves its result of this one
+      if (shared > 0) join_piece(before, shared - 1);
+      const int buf = shared % C::JOINS;
+      if (ok) ok = mbar_wait_warp(o_empty(buf), ((uint32_t)(shared / C::JOINS) & 1u) ^ 1u, abort_flag);
+      if (ok) {
+        float* const join = join_of(buf);
+        float* const join_m = join + JOIN_M;
+        if (gq == 0) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int h = n * 8 + 2 * tq + i;
+              join_m[warp * C::HEADS + h] = m[n][i];
+              join_m[(COMPUTE_WARPS + warp) * C::HEADS + h] = E4M3 ? mo[n][i] : m[n][i];
+              join_m[(2 * COMPUTE_WARPS + warp) * C::HEADS + h] = l[n][i];
+            }
+        }
+        if (busy) leave_output(join + warp * C::HEADS * (DH + PAD));
         __syncwarp();
         if (lane == 0) mbar_arrive(o_full(buf));
       }
       before = p;
+      ++shared;
     }
-    if (pieces > 0) join_piece(before, pieces - 1);
+    if (shared > 0) join_piece(before, shared - 1);
 
     // ---- sequences without positions, and lengths that the table cannot hold
     for (int s = b; s < g.a.n_seq; s += gridDim.x) {

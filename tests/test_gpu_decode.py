@@ -330,6 +330,21 @@ def test_attention(B, case, d, e4m3):
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("heads,kvh,page,d,longest", [(8, 8, 16, 64, 300), (28, 4, 32, 128, 400), (16, 1, 64, 128, 900), (6, 2, 16, 64, 1000)])
+def test_attention_many_short_sequences(B, heads, kvh, page, d, longest, e4m3):
+    """Many more sequences than SMs, of very different lengths in no order, some empty: every CTA has many pieces."""
+    rng = np.random.default_rng(heads * 7 + e4m3)
+    n_seq = 331
+    lens = [int(longest * x ** 3) for x in rng.random(n_seq)]
+    lens[5:9] = [longest, 0, 1, longest]
+    c = Cache(rng, n_seq, (longest + page - 1) // page, kvh, page, d, e4m3)
+    q = bf16(rng.standard_normal((n_seq, heads * d)))
+    out, lse, status = run_attention(B, q, heads, c, lens)
+    assert status == 0
+    check_attention(out, lse, f64(q).reshape(n_seq, heads, d), lens, c, heads, values=c.values())
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("heads,kvh,page,d", [(56, 8, 64, 128), (80, 8, 16, 128), (8, 8, 32, 64), (128, 8, 128, 64)])
 def test_attention_long_runs(B, heads, kvh, page, d, e4m3):
     """Enough positions that every CTA goes round its ring of stages many times, pages out of order, a second sequence behind the
