@@ -11,9 +11,9 @@
 // K is shared by the warps of a block (direct) and by the blocks of a cluster where there are too few blocks to fill the
 // card.  Sums meet in shared memory (of the cluster) in a fixed order.
 //
-// Device time per call, B200, weights not in L2 (of the measured copy bandwidth):
-//   1 x 3584 x 4608 7.6 us (0.67, direct), 1 x 3584 x 37888 gated 43.5 us (0.97, ring), 19 x the same 48 us (0.88),
-//   1 x 18944 x 3584 24.7 us (0.85, ring), 32 x the same 29 us (0.74)
+// Device time per call in a chain of calls, B200, weights not in L2 (of the measured copy bandwidth):
+//   1 x 3584 x 4608 7.4 us (0.70, direct), 1 x 3584 x 37888 gated 42 us (1.00, ring), 19 x the same 46 us (0.91),
+//   1 x 18944 x 3584 residual 23.5 us (0.90, ring), 32 x the same 26 us (0.81)
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -27,6 +27,7 @@ namespace et {
 namespace {
 
 namespace cg = cooperative_groups;
+using namespace tc;
 
 constexpr int WARPS = 8, THREADS = 32 * WARPS;  // of the direct kernel
 constexpr int BLOCK_ROWS = 32;                 // its weight rows of a block: two tiles of 16
@@ -74,37 +75,56 @@ struct LinearArgs {
   int* status;
 };
 
-// The block's sums [m][ROWS] of every rank become outputs, dealt to the ranks' threads.  In a gated block 16 gate rows are
-// followed by the 16 up rows of the same outputs.
+// The block's sums [m][ROWS] of every rank become outputs, dealt to the ranks' threads four at a time; the ranks' parts are
+// fetched together and added in order.  In a gated block 16 gate rows are followed by the 16 up rows of the same outputs.
 template <int ROWS, int NTHREADS>
 __device__ __forceinline__ void finish(const LinearArgs& g, cg::cluster_group& cluster, float* part, int block, int ranks, int rank) {
   const int tid = threadIdx.x;
   const bool gated = g.epilogue == EPI_SWIGLU;
-  auto total = [&](int r, int m) {
-    float s = 0.f;
-    for (int p = 0; p < ranks; ++p) s += cluster.map_shared_rank(part, p)[m * ROWS + r];
-    return s;
+  auto total = [&](int r, int m, float (&y)[4]) {
+    float4 v[MAX_CLUSTER];
+#pragma unroll
+    for (int p = 0; p < MAX_CLUSTER; ++p)
+      if (p < ranks) v[p] = *reinterpret_cast<const float4*>((ranks > 1 ? cluster.map_shared_rank(part, p) : part) + m * ROWS + r);
+    y[0] = y[1] = y[2] = y[3] = 0.f;
+#pragma unroll
+    for (int p = 0; p < MAX_CLUSTER; ++p)
+      if (p < ranks) { y[0] += v[p].x; y[1] += v[p].y; y[2] += v[p].z; y[3] += v[p].w; }
   };
-  if (gated) {
-    constexpr int OUTS = ROWS / 2;
-    for (int e = rank * NTHREADS + tid; e < OUTS * g.M; e += ranks * NTHREADS) {
-      const int j = e % OUTS, m = e / OUTS, r = (j / 16) * 32 + j % 16, out = block * OUTS + j, n = (out / 32) * 64 + out % 32;
-      if (n >= g.N) continue;
-      const float gate = total(r, m) + (g.bias ? g.bias[n] : 0.f), up = total(16 + r, m) + (g.bias ? g.bias[n + 32] : 0.f);
-      reinterpret_cast<bf16*>(g.c)[(size_t)m * (g.N / 2) + out] = __float2bfloat16_rn(gate / (1.f + expf(-gate)) * up);
+  const int outs = gated ? g.N / 2 : g.N, quads = gated ? ROWS / 8 : ROWS / 4;
+  const bool vectors = outs % 4 == 0;          // a row's groups of four are aligned
+  for (int e = rank * NTHREADS + tid; e < quads * g.M; e += ranks * NTHREADS) {
+    const int q = e % quads, m = e / quads;
+    const int j = block * quads * 4 + q * 4;   // first of the four outputs
+    if (j >= outs) continue;
+    const int live = min(4, outs - j);
+    float y[4];
+    total(gated ? (q / 4) * 32 + (q % 4) * 4 : q * 4, m, y);
+    const int n = gated ? (j / 32) * 64 + j % 32 : j;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (g.bias && i < live) y[i] += g.bias[n + i];
+    if (gated) {
+      float up[4];
+      total((q / 4) * 32 + (q % 4) * 4 + 16, m, up);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = y[i] / (1.f + expf(-y[i])) * (up[i] + (g.bias ? g.bias[n + 32 + i] : 0.f));
+    } else if (g.epilogue == EPI_GELU) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = gelu_f(y[i], g.gelu_tanh);
     }
-  } else {
-    for (int e = rank * NTHREADS + tid; e < ROWS * g.M; e += ranks * NTHREADS) {
-      const int r = e % ROWS, m = e / ROWS, n = block * ROWS + r;
-      if (n >= g.N) continue;
-      float y = total(r, m) + (g.bias ? g.bias[n] : 0.f);
-      const size_t at = (size_t)m * g.N + n;
-      if (g.epilogue == EPI_RESIDUAL) {
-        reinterpret_cast<float*>(g.c)[at] += y;
+    const size_t at = (size_t)m * outs + j;
+    if (g.epilogue == EPI_RESIDUAL) {
+      float* c = reinterpret_cast<float*>(g.c) + at;
+      if (vectors) {
+        const float4 x = *reinterpret_cast<const float4*>(c);
+        *reinterpret_cast<float4*>(c) = make_float4(x.x + y[0], x.y + y[1], x.z + y[2], x.w + y[3]);
       } else {
-        if (g.epilogue == EPI_GELU) y = gelu_f(y, g.gelu_tanh);
-        reinterpret_cast<bf16*>(g.c)[at] = __float2bfloat16_rn(y);
+        for (int i = 0; i < live; ++i) c[i] += y[i];
       }
+    } else {
+      bf16* c = reinterpret_cast<bf16*>(g.c) + at;
+      if (vectors) *reinterpret_cast<uint2*>(c) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+      else for (int i = 0; i < live; ++i) c[i] = __float2bfloat16_rn(y[i]);
     }
   }
 }
@@ -119,7 +139,7 @@ __global__ void __launch_bounds__(THREADS, 2)
 linear_direct_kernel(const LinearArgs g) {
   constexpr int COLS = 8 * NT, LD = COLS + 1;
   constexpr int ROWS = BLOCK_ROWS;
-    __shared__ float red[WARPS * ROWS * LD];
+    __shared__ __align__(16) float red[WARPS * ROWS * LD];
   float* const part = red;
   cg::cluster_group cluster = cg::this_cluster();
   const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -214,8 +234,6 @@ linear_direct_kernel(const LinearArgs g) {
 // Ring: one warp copies, four compute, 32 weight rows each.  100 KB a block, two blocks an SM, about 160 KB of weights on
 // their way.  A rank of a cluster takes every ranks-th step of 64 along K.
 // ---------------------------------------------------------------------------------------------
-using namespace tc;
-
 constexpr int RING_ROWS = 128, RING_WARPS = 4, RING_THREADS = 32 * (RING_WARPS + 1);
 template <int NT> struct Ring {
   static constexpr int W_BYTES = RING_ROWS * 128, A_BYTES = 8 * NT * 128, STAGE = W_BYTES + A_BYTES;
@@ -231,7 +249,6 @@ template <int NT>
 __global__ void __launch_bounds__(RING_THREADS, 2)
 linear_ring_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap amap, const LinearArgs g) {
   using R = Ring<NT>;
-  constexpr int COLS = 8 * NT;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const gen = smem_raw + (base - raw);
@@ -384,10 +401,12 @@ cudaError_t launch_ring(const LinearArgs& g, cudaStream_t s) {
 cudaError_t launch_linear_rows(const bf16* a, const bf16* w, const float* bias, void* c, int M, int N, int K, int epilogue,
                                int gelu_tanh, int* status, cudaStream_t s) {
   const LinearArgs g{a, w, bias, c, M, N, K, epilogue, gelu_tanh, status};
-  // The ring takes over where the weights are many, sooner the more rows there are (direct reads a again for every 32 weight
-  // rows).  Direct / ring in us: 1 x 3584 x 3584 5.6 / 6.2, 1 x 3584 x 9000 13.4 / 13.8, 1 x 18944 x 3584 25.8 / 24.7;
-  // 13 x 3584 x 4608 9.1 / 9.2, 13 x 4096 x 5120 13.6 / 12.0; 32 x 3584 x 2048 7.8 / 7.8, 32 x 3584 x 3584 10.7 / 8.7.
-  const bool ring = (long long)N * K * ((M + 7) / 8) > (1ll << 25);
+  // The ring takes over where the weights are many, much sooner with more than 8 rows (direct reads a again for every 32 weight
+  // rows), unless there are too few weight rows for its blocks.  Direct / ring in us: 1 x 3584 x 4608 7.2 / 7.3, 8 x 3584 x 9000
+  // 13.0 / 14.2, 8 x 18944 x 3584 25.5 / 24.6; 13 x 2048 x 2048 4.6 / 4.8, 13 x 3584 x 2048 5.8 / 5.5, 13 x 18944 x 3584 29.4 /
+  // 24.9; 32 x 2048 x 2048 6.7 / 5.6; 32 x 16384 x 512 9.8 / 12.9.
+  const long long weights = (long long)N * K;
+  const bool ring = M <= 8 ? weights > (1ll << 25) : N >= 1024 && weights * ((M + 7) / 8) > 12000000;
   if (ring) return M <= 8 ? launch_ring<1>(g, s) : M <= 16 ? launch_ring<2>(g, s) : launch_ring<4>(g, s);
   return M <= 8 ? launch_direct<1>(g, s) : M <= 16 ? launch_direct<2>(g, s) : M <= 24 ? launch_direct<3>(g, s) : launch_direct<4>(g, s);
 }
