@@ -779,20 +779,36 @@ def et_attention_causal(qkv, n_seq, L, heads, kv_heads, head_dim, stream=None):
 # time, so they marshal plain integers and build no messages unless a check fails.
 # --------------------------------------------------------------------------------------------
 
+_torch = None       # torch, once one of these calls has imported it (an import statement in every helper would cost more than they do)
+
+
+def _import_torch():
+    global _torch
+    import torch
+    _torch = torch
+
+
 def _refuse(what: str):
     raise EarlyTomError(1, what)
 
 
-def _launch_on(stream, *tensors) -> int:
+def _launch_on(stream, first, *others) -> int:
     """The stream's handle.  The library launches on the current device: every tensor has to live there."""
-    import torch
-    dev = torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else -2
-    for t in tensors:
+    dev = first.get_device()
+    for t in others:
         if t is not None and t.get_device() != dev:
-            _refuse("tensors must be on the current CUDA device")
-    if stream is not None:
-        return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(dev)
+            dev = -1
+    if dev < 0 or dev != _torch.cuda.current_device():
+        _refuse("tensors must be on the current CUDA device")
+    return _torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _new(make, shape, dtype, like, stream):
+    """A tensor of torch's allocator that belongs to the stream that the call runs on."""
+    if stream is None:
+        return make(shape, dtype=dtype, device=like.device)
+    with _torch.cuda.stream(stream):
+        return make(shape, dtype=dtype, device=like.device)
 
 
 def _at(t):
@@ -800,39 +816,35 @@ def _at(t):
 
 
 def _ints(t, n, what):
-    import torch
-    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous():
+    if t.dtype is not _torch.int32 or t.numel() != n or not t.is_contiguous():
         _refuse(f"{what}: contiguous int32 [{n}]")
 
 
 def _row_stride(t, width, what):
     """Row stride in elements of a bf16 matrix whose rows have at least `width` contiguous values."""
-    import torch
-    if t.dtype is not torch.bfloat16 or t.dim() != 2 or t.shape[1] < width or t.stride(1) != 1:
+    if t.dtype is not _torch.bfloat16 or t.dim() != 2 or t.shape[1] < width or t.stride(1) != 1:
         _refuse(f"{what}: bf16 [rows, >= {width}] with contiguous columns")
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
 
 
 def _kv_cache(cache, scale):
     """cache [n_pages, 2, kv_heads, page_size, head_dim] bf16 or e4m3 (scale uint8 [n_pages, 2, kv_heads, page_size])."""
-    import torch
     shape = cache.shape
     if len(shape) != 5 or shape[1] != 2 or not cache.is_contiguous():
         _refuse("cache: contiguous [n_pages, 2, kv_heads, page_size, head_dim]")
-    if cache.dtype is torch.bfloat16:
+    if cache.dtype is _torch.bfloat16:
         if scale is not None:
             _refuse("scale goes with an e4m3 cache only")
         return et_kv_cache(cache.data_ptr(), None, shape[0], shape[2], shape[3], shape[4], ET_KV_BF16)
-    if cache.dtype is not torch.float8_e4m3fn:
+    if cache.dtype is not _torch.float8_e4m3fn:
         _refuse("cache: bfloat16 or float8_e4m3fn")
-    if scale is None or scale.dtype is not torch.uint8 or scale.shape != shape[:4] or not scale.is_contiguous():
+    if scale is None or scale.dtype is not _torch.uint8 or scale.shape != shape[:4] or not scale.is_contiguous():
         _refuse("an e4m3 cache needs scale: contiguous uint8 [n_pages, 2, kv_heads, page_size]")
     return et_kv_cache(cache.data_ptr(), scale.data_ptr(), shape[0], shape[2], shape[3], shape[4], ET_KV_E4M3)
 
 
 def _table(block_table):
-    import torch
-    if block_table.dtype is not torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous():
+    if block_table.dtype is not _torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous():
         _refuse("block_table: contiguous int32 [n_seq, max_pages]")
     return block_table.shape
 
@@ -841,7 +853,8 @@ def et_kv_append(cache, scale, qkv, heads, block_table, start, row_offsets=None,
                  status=None, stream=None):
     """Stores the keys and values of qkv's rows (bf16 [rows, (heads + 2*kv_heads)*head_dim]); returns the turned queries
     (q_out, created if theta > 0 and heads > 0 and none is given), None without rotation."""
-    import torch
+    if _torch is None:
+        _import_torch()
     c = _kv_cache(cache, scale)
     n_seq, max_pages = _table(block_table)
     rows = qkv.shape[0]
@@ -856,8 +869,8 @@ def et_kv_append(cache, scale, qkv, heads, block_table, start, row_offsets=None,
         _ints(status, 1, "status")
     if q_out is None:
         if theta != 0 and heads > 0:
-            q_out = torch.empty((rows, heads * c.head_dim), dtype=torch.bfloat16, device=qkv.device)
-    elif q_out.dtype is not torch.bfloat16 or q_out.numel() != rows * heads * c.head_dim or not q_out.is_contiguous():
+            q_out = _new(_torch.empty, (rows, heads * c.head_dim), _torch.bfloat16, qkv, stream)
+    elif q_out.dtype is not _torch.bfloat16 or q_out.numel() != rows * heads * c.head_dim or not q_out.is_contiguous():
         _refuse("q_out: contiguous bf16 [rows, heads * head_dim]")
     st = lib().et_kv_append(C.byref(c), qkv.data_ptr(), stride, rows, heads, block_table.data_ptr(), n_seq, max_pages,
                             _at(row_offsets), start.data_ptr(), theta, _at(q_out), _at(new_len), _at(status), s)
@@ -869,12 +882,13 @@ def et_kv_append(cache, scale, qkv, heads, block_table, start, row_offsets=None,
 def et_kv_read(cache, scale, block_table, start, rows, row_offsets=None, out=None, status=None, stream=None):
     """Rows of the cache as bf16 [rows, 2*kv_heads*head_dim] = [keys | values]; rows that no sequence has are left as out has
     them (zeros where out is created here)."""
-    import torch
+    if _torch is None:
+        _import_torch()
     c = _kv_cache(cache, scale)
     n_seq, max_pages = _table(block_table)
     width = 2 * c.kv_heads * c.head_dim
     if out is None:
-        out = torch.zeros((rows, width), dtype=torch.bfloat16, device=cache.device)
+        out = _new(_torch.zeros, (rows, width), _torch.bfloat16, cache, stream)
     elif out.shape[0] != rows:
         _refuse("out: as many rows as are read")
     s = _launch_on(stream, cache, scale, block_table, start, row_offsets, out, status)
@@ -894,7 +908,8 @@ def et_kv_read(cache, scale, block_table, start, rows, row_offsets=None, out=Non
 def et_attention_paged(q, heads, cache, scale, block_table, lens, out=None, lse=None, workspace=None, status=None, stream=None):
     """q bf16 [n_seq, >= heads*head_dim]; returns out bf16 [n_seq, heads*head_dim].  lse (fp32 [n_seq, heads]) is filled if
     given; workspace: uint8 [ET_PAGED_WORKSPACE], created if none is given."""
-    import torch
+    if _torch is None:
+        _import_torch()
     c = _kv_cache(cache, scale)
     n_seq, max_pages = _table(block_table)
     width = heads * c.head_dim
@@ -902,15 +917,15 @@ def et_attention_paged(q, heads, cache, scale, block_table, lens, out=None, lse=
         _refuse("block_table: a row for each row of q")
     stride = _row_stride(q, width, "q")
     if out is None:
-        out = torch.empty((n_seq, width), dtype=torch.bfloat16, device=q.device)
-    elif out.dtype is not torch.bfloat16 or out.numel() != n_seq * width or not out.is_contiguous():
+        out = _new(_torch.empty, (n_seq, width), _torch.bfloat16, q, stream)
+    elif out.dtype is not _torch.bfloat16 or out.numel() != n_seq * width or not out.is_contiguous():
         _refuse("out: contiguous bf16 [n_seq, heads * head_dim]")
     if workspace is None:
-        workspace = torch.empty(ET_PAGED_WORKSPACE, dtype=torch.uint8, device=q.device)
+        workspace = _new(_torch.empty, ET_PAGED_WORKSPACE, _torch.uint8, q, stream)
     elif not workspace.is_contiguous():
         _refuse("workspace: contiguous")
     s = _launch_on(stream, q, cache, scale, block_table, lens, out, lse, workspace, status)
-    if lse is not None and (lse.dtype is not torch.float32 or lse.numel() != n_seq * heads or not lse.is_contiguous()):
+    if lse is not None and (lse.dtype is not _torch.float32 or lse.numel() != n_seq * heads or not lse.is_contiguous()):
         _refuse("lse: contiguous float32 [n_seq, heads]")
     _ints(lens, n_seq, "lens")
     if status is not None:
@@ -925,23 +940,24 @@ def et_attention_paged(q, heads, cache, scale, block_table, lens, out=None, lse=
 
 def et_linear_rows(a, w, bias=None, epilogue=0, gelu_tanh=1, c=None, status=None, stream=None):
     """a [M <= 32, K] bf16, w [N, K] bf16, bias [N] f32 or None.  Returns c (bf16; fp32, added to in place, with epilogue 2)."""
-    import torch
+    if _torch is None:
+        _import_torch()
     M, K = a.shape
     N, Kw = w.shape
     outs = N // 2 if epilogue == 4 else N
-    dtype = torch.float32 if epilogue == 2 else torch.bfloat16
+    dtype = _torch.float32 if epilogue == 2 else _torch.bfloat16
     if c is None:
         if epilogue == 2:
             _refuse("epilogue 2 adds to c")
-        c = torch.empty((M, outs), dtype=dtype, device=a.device)
+        c = _new(_torch.empty, (M, outs), dtype, a, stream)
     elif c.dtype is not dtype or c.numel() != M * outs or not c.is_contiguous():
         _refuse(f"c: contiguous {dtype} [{M}, {outs}]")
     s = _launch_on(stream, a, w, bias, c, status)
-    if a.dtype is not torch.bfloat16 or not a.is_contiguous():
+    if a.dtype is not _torch.bfloat16 or not a.is_contiguous():
         _refuse("a: contiguous bf16 [M, K]")
-    if w.dtype is not torch.bfloat16 or Kw != K or not w.is_contiguous():
+    if w.dtype is not _torch.bfloat16 or Kw != K or not w.is_contiguous():
         _refuse("w: contiguous bf16 [N, K]")
-    if bias is not None and (bias.dtype is not torch.float32 or bias.numel() != N or not bias.is_contiguous()):
+    if bias is not None and (bias.dtype is not _torch.float32 or bias.numel() != N or not bias.is_contiguous()):
         _refuse("bias: contiguous float32 [N]")
     if status is not None:
         _ints(status, 1, "status")

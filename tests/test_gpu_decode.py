@@ -550,6 +550,46 @@ def test_cache_beyond_32_bit_offsets(B, e4m3):
     assert torch.equal(a, b)
 
 
+def test_attention_of_sequences_that_share_pages(B):
+    """Two sequences may name the same pages (a common beginning): both read them."""
+    import torch
+    rng = np.random.default_rng(22)
+    lens, heads, kvh, page, d = [150, 150, 96], 12, 4, 32, 128
+    c = Cache(rng, 3, 5, kvh, page, d, True)
+    c.table[1] = c.table[0]
+    c.table[2, :3] = c.table[0, :3]
+    q = bf16(rng.standard_normal((3, heads * d)))
+    q[1] = q[0]
+    out, lse, status = run_attention(B, q, heads, c, lens)
+    assert status == 0 and torch.equal(out[0], out[1]) and torch.equal(lse[0], lse[1])
+    check_attention(out, lse, f64(q).reshape(3, heads, d), lens, c, heads)
+
+
+def test_calls_on_a_stream_of_their_own(B):
+    """The stream argument: what the calls create belongs to that stream, and calls on two streams at once do not disturb one
+    another (each with the workspace and the outputs that the calls create)."""
+    import torch
+    rng = np.random.default_rng(41)
+    lens, heads, kvh, page, d = [700, 3, 1500], 14, 2, 32, 128
+    c = Cache(rng, 3, 50, kvh, page, d, False)
+    q = bf16(rng.standard_normal((3, heads * d)))
+    want = B.et_attention_paged(q, heads, c.data, None, c.table, i32(lens))
+    rows = B.et_kv_read(c.data, None, c.table, i32([0, 0, 0]), 100, i32([0, 50, 53, 60]))
+    a, w = bf16(rng.standard_normal((20, 4096))), bf16(rng.standard_normal((5120, 4096)))
+    y = B.et_linear_rows(a, w)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for i in range(20):
+        s = streams[i % 2]
+        got.append((B.et_attention_paged(q, heads, c.data, None, c.table, i32(lens), stream=s),
+                    B.et_kv_read(c.data, None, c.table, i32([0, 0, 0]), 100, i32([0, 50, 53, 60]), stream=s), B.et_linear_rows(a, w, stream=s)))
+        torch.cuda.synchronize() if i == 9 else None
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want) and torch.equal(r, rows) and torch.equal(z, y) for x, r, z in got)
+    assert (rows[60:] == 0).all()
+
+
 # ---- dense layer for few rows -----------------------------------------------------------------------------------------
 
 def linear_reference(a, w, bias, epilogue, gelu_tanh, c0):
@@ -599,6 +639,20 @@ def test_linear_rows(B, M, K, N, epilogue, gelu_tanh, with_bias):
     err = np.abs(f64(c) - want)
     assert (err <= tol + 1e-30).all(), f"{(err / tol).max():.3g} of the tolerance"
     assert (guard[M * outs:] == 3.0).all()
+
+
+@pytest.mark.parametrize("M,K,N", [(2, 1024, 384), (12, 3584, 640), (30, 2048, 384)])
+def test_linear_rows_from_16_byte_aligned_operands(B, M, K, N):
+    """Operands that start 16 bytes behind a 32-byte border give what aligned ones give."""
+    import torch
+    rng = np.random.default_rng(M)
+    a, w = bf16(rng.standard_normal((M, K))), bf16(rng.standard_normal((N, K)))
+    x = B.et_linear_rows(a, w)
+    moved = [torch.empty(z.numel() + 8, dtype=torch.bfloat16, device="cuda")[8:].view_as(z).copy_(z) for z in (a, w)]
+    assert moved[0].data_ptr() % 32 == 16 and moved[1].data_ptr() % 32 == 16
+    for p, q in ((moved[0], w), (a, moved[1]), moved):
+        # two 16-byte loads in place of one of 32: the same operands in the same places of the same instructions
+        assert torch.equal(B.et_linear_rows(p, q), x)
 
 
 def test_linear_rows_rows_do_not_touch_each_other(B):
