@@ -813,37 +813,56 @@ attention_join_kernel(const __grid_constant__ Args g) {
   if (j.pieces == 0 || h0 + h >= g.group) return;
   const int next = 2 * blockIdx.x + 2;                               // slot of the second piece; the others follow two by two
   auto part = [&](int i) { return g.a.workspace + SLOT0 + (size_t)(i == 0 ? j.slot : next + 2 * (i - 1)) * Slot<DH, NT>::FLOATS; };
+  constexpr int WARPS = JOIN_THREADS / 32, AHEAD = 8;
   __shared__ float weight[MAX_CTAS];
-  __shared__ float red[JOIN_THREADS / 32];
+  __shared__ float tops[WARPS], sums[WARPS];
   __shared__ float4 accs[RUNS][LANES];
-  const int tid = threadIdx.x;
-  float top = -INFINITY;
-  for (int i = tid; i < j.pieces; i += JOIN_THREADS) top = fmaxf(top, part(i)[HEADS * DH + 2 * h]);
+  const int tid = threadIdx.x, run = tid / LANES, d = (tid % LANES) * 4;
+  // everything is on its way at once: the maxima and sums (a piece a thread), the outputs of the first pieces of each run
+  float4 x[AHEAD];
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-  if ((tid & 31) == 0) red[tid >> 5] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  const float ref = top == -INFINITY ? 0.f : top;
-  for (int i = tid; i < j.pieces; i += JOIN_THREADS) weight[i] = exp2_fast(part(i)[HEADS * DH + 2 * h] - ref);
-  __syncthreads();
-  const int run = tid / LANES, d = (tid % LANES) * 4;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int i = run; i < j.pieces; i += RUNS) {
-    const float4 x = *reinterpret_cast<const float4*>(part(i) + h * DH + d);
-    const float w = weight[i];
-    acc.x += x.x * w; acc.y += x.y * w; acc.z += x.z * w; acc.w += x.w * w;
+  for (int k = 0; k < AHEAD; ++k)
+    if (run + k * RUNS < j.pieces) x[k] = *reinterpret_cast<const float4*>(part(run + k * RUNS) + h * DH + d);
+  static_assert(MAX_CTAS <= 2 * JOIN_THREADS, "two pieces a thread");
+  float2 ml[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int i = tid + k * JOIN_THREADS;
+    ml[k] = i < j.pieces ? *reinterpret_cast<const float2*>(part(i) + HEADS * DH + 2 * h) : make_float2(-INFINITY, 0.f);
   }
-  accs[run][tid % LANES] = acc;
+  float top = fmaxf(ml[0].x, ml[1].x);
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+  if ((tid & 31) == 0) tops[tid >> 5] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) top = fmaxf(top, tops[w]);
+  const float ref = top == -INFINITY ? 0.f : top;
   float sum = 0.f;
-  for (int i = 0; i < j.pieces; ++i) sum += part(i)[HEADS * DH + 2 * h + 1] * weight[i];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int i = tid + k * JOIN_THREADS;
+    const float w = exp2_fast(ml[k].x - ref);
+    if (i < j.pieces) weight[i] = w;
+    sum += ml[k].y * w;
+  }
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+  if ((tid & 31) == 0) sums[tid >> 5] = sum;
+  __syncthreads();
+  sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) sum += sums[w];
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](const float4& v, float w) { acc.x += v.x * w; acc.y += v.y * w; acc.z += v.z * w; acc.w += v.w * w; };
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) if (run + k * RUNS < j.pieces) add(x[k], weight[run + k * RUNS]);
+#pragma unroll 4
+  for (int i = run + AHEAD * RUNS; i < j.pieces; i += RUNS) add(*reinterpret_cast<const float4*>(part(i) + h * DH + d), weight[i]);
+  accs[run][tid % LANES] = acc;
   __syncthreads();
   if (run == 0) {
-    for (int r = 1; r < RUNS; ++r) {
-      const float4 x = accs[r][tid];
-      acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
-    }
+    for (int r = 1; r < RUNS; ++r) add(accs[r][tid], 1.f);
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const size_t at = (size_t)j.seq * g.a.heads + kvh * g.group + h0 + h;
     *reinterpret_cast<uint2*>(g.a.out + at * DH + d) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
