@@ -15,7 +15,10 @@
  *
  * status_dev (int, may be NULL, set to 0 by the caller) receives ET_PAGED_CAPACITY where a position lies behind a
  * sequence's max_pages * page_size, ET_PAGED_BAD_PAGE where a table entry in use is not a page of the cache, 1 where a
- * bounded wait expired. */
+ * bounded wait expired (a larger one stays).
+ *
+ * Limits (ET_ERR_CAPACITY): max_pages * page_size <= 2^30; rows of a cache below 2^31 (see et_kv_cache); for attention also
+ * n_seq * heads <= 2^24 and n_seq * heads * (max_pages * page_size / 64 + 16) < 2^31. */
 #ifndef EARLYTOM_DECODE_H
 #define EARLYTOM_DECODE_H
 

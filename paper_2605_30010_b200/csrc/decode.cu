@@ -27,7 +27,7 @@ et_status check_cache(const et_kv_cache* c, PagedCache* out) {
 et_status check_table(const int* table, int n_seq, int max_pages, int page_shift) {
   if (!table) return ET_ERR_INVALID_ARG;
   if (n_seq < 1 || max_pages < 1) return ET_ERR_SHAPE;
-  if ((long long)max_pages > ((1ll << 31) - 1) >> page_shift) return ET_ERR_CAPACITY;
+  if ((long long)max_pages << page_shift > 1ll << 30) return ET_ERR_CAPACITY;      // positions are 32-bit, with room for tiles' ends
   return ET_OK;
 }
 

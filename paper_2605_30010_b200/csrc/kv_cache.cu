@@ -1,4 +1,8 @@
 // The paged key / value cache: rows of a projection go in (turned and quantised on the way), rows come back.
+//
+// Device time in a chain of calls, B200 (of the measured copy bandwidth, bytes read + written): append of 21 124 rows of 28 + 4 + 4
+// heads of 128, turned, bf16 66 us (0.91); of 7 675 rows of 4 + 4 heads, e4m3 6.8 us (0.54: launch and three loads that wait for
+// one another); of one token 2.7 us.  Read of 63 435 rows of 16 + 16 heads of 64, bf16 89 us (0.91); of 7 675 rows, e4m3 6.7 us.
 #include <cuda_fp8.h>
 
 #include "decode.cuh"

@@ -295,12 +295,11 @@ linear_ring_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
         tma_load_2d(dst + R::W_BYTES, &amap, full(stage), x, 0);
         if (++stage == R::STAGES) { stage = 0; phase ^= 1u; }
       }
-      if (!ok) {
-        for (int i = 0; i < R::STAGES && i < issued; ++i) {         // copies in flight land before the memory is given up
-          if (--stage < 0) { stage = R::STAGES - 1; phase ^= 1u; }
-          int given_up = 0;
-          mbar_wait(full(stage), phase, &given_up);
-        }
+      // copies have to land before the ring's memory is used for the sums, also if nobody waits for them any more
+      for (int i = 0; i < R::STAGES && i < issued; ++i) {
+        if (--stage < 0) { stage = R::STAGES - 1; phase ^= 1u; }
+        int given_up = 0;
+        mbar_wait(full(stage), phase, &given_up);
       }
     }
   } else {
