@@ -689,9 +689,9 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                 ldmatrix4_trans(vb + swizzled(vrow + 16 * j, k + vchunk), a);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                  const uint32_t x = a[2 * i] & keep0, y = a[2 * i + 1] & keep1;
-                  const uint32_t a0 = e4m3x2_to_f16x2(__byte_perm(x, 0, 0x4420)), a1 = e4m3x2_to_f16x2(__byte_perm(x, 0, 0x4431));
-                  const uint32_t a2 = e4m3x2_to_f16x2(__byte_perm(y, 0, 0x4420)), a3 = e4m3x2_to_f16x2(__byte_perm(y, 0, 0x4431));
+                  const uint32_t x = __byte_perm(a[2 * i] & keep0, 0, 0x3120), y = __byte_perm(a[2 * i + 1] & keep1, 0, 0x3120);
+                  const uint32_t a0 = e4m3x2_to_f16x2(x & 0xffffu), a1 = e4m3x2_to_f16x2(x >> 16);
+                  const uint32_t a2 = e4m3x2_to_f16x2(y & 0xffffu), a3 = e4m3x2_to_f16x2(y >> 16);
 #pragma unroll
                   for (int n = 0; n < NT; ++n) mma16816<true>(o[n][k + i], a0, a1, a2, a3, ph0[n], ph1[n]);
                 }
