@@ -312,6 +312,13 @@ linear_ring_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
       if (ok) ok = mbar_wait_warp(full(stage), phase, abort_flag);
       if (ok) {
         const uint32_t wb = base + stage * R::STAGE, ab = wb + R::W_BYTES;
+        // The tensor core truncates where fp32 addition rounds, which adds up over a long chain (1.8e-6 of the result over K =
+        // 18 944): a stage's products get accumulators of their own, and the stages are added in fp32.
+        float part_acc[2][NT][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) part_acc[i][n][0] = part_acc[i][n][1] = part_acc[i][n][2] = part_acc[i][n][3] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
           uint32_t w0[4], w1[4];
@@ -321,14 +328,20 @@ linear_ring_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
           for (int n = 0; n < NT; n += 2) {
             uint32_t b[4];
             ldmatrix4(ab + at(NT == 1 ? (brow & 7) : n * 8 + brow, 2 * ks + bchunk), b);
-            mma_bf16(acc[0][n], w0[0], w0[1], w0[2], w0[3], b[0], b[1]);
-            mma_bf16(acc[1][n], w1[0], w1[1], w1[2], w1[3], b[0], b[1]);
+            mma_bf16(part_acc[0][n], w0[0], w0[1], w0[2], w0[3], b[0], b[1]);
+            mma_bf16(part_acc[1][n], w1[0], w1[1], w1[2], w1[3], b[0], b[1]);
             if (n + 1 < NT) {
-              mma_bf16(acc[0][(n + 1) % NT], w0[0], w0[1], w0[2], w0[3], b[2], b[3]);
-              mma_bf16(acc[1][(n + 1) % NT], w1[0], w1[1], w1[2], w1[3], b[2], b[3]);
+              mma_bf16(part_acc[0][(n + 1) % NT], w0[0], w0[1], w0[2], w0[3], b[2], b[3]);
+              mma_bf16(part_acc[1][(n + 1) % NT], w1[0], w1[1], w1[2], w1[3], b[2], b[3]);
             }
           }
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][n][j] += part_acc[i][n][j];
         __syncwarp();
         if (lane == 0) mbar_arrive(empty(stage));
       }
