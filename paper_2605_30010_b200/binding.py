@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass, field
 from typing import List, Optional, Sequence
 
@@ -186,10 +187,10 @@ def load_library(path: str = _LIB_PATH) -> C.CDLL:
     lib.et_rope.argtypes = [vp, i, i, i, i, i, f, vp]
     lib.et_swiglu.argtypes = [vp, vp, i, i, vp]
     lib.et_attention_causal.argtypes = [vp, vp, i, i, i, i, i, vp, vp]
-    ll, kv = C.c_longlong, C.POINTER(et_kv_cache)
-    lib.et_kv_append.argtypes = [kv, vp, ll, i, i, vp, i, i, vp, vp, f, vp, vp, vp, vp]
-    lib.et_kv_read.argtypes = [kv, vp, ll, i, vp, i, i, vp, vp, vp, vp]
-    lib.et_attention_paged.argtypes = [kv, vp, ll, vp, vp, i, i, vp, i, vp, vp, C.c_size_t, vp, vp]
+    ll = C.c_longlong
+    lib.et_kv_append.argtypes = [vp, vp, ll, i, i, vp, i, i, vp, vp, f, vp, vp, vp, vp]
+    lib.et_kv_read.argtypes = [vp, vp, ll, i, vp, i, i, vp, vp, vp, vp]
+    lib.et_attention_paged.argtypes = [vp, vp, ll, vp, vp, i, i, vp, i, vp, vp, C.c_size_t, vp, vp]
     lib.et_linear_rows.argtypes = [vp, vp, vp, vp, i, i, i, i, i, vp, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
@@ -827,20 +828,26 @@ def _row_stride(t, width, what):
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
 
 
+_KV_CACHE = struct.Struct("@PPiiiii0P")       # et_kv_cache as bytes, a third of the time of a ctypes structure
+
+
 def _kv_cache(cache, scale):
-    """cache [n_pages, 2, kv_heads, page_size, head_dim] bf16 or e4m3 (scale uint8 [n_pages, 2, kv_heads, page_size])."""
+    """cache [n_pages, 2, kv_heads, page_size, head_dim] bf16 or e4m3 (scale uint8 [n_pages, 2, kv_heads, page_size]) as
+    (et_kv_cache, kv_heads, head_dim)."""
     shape = cache.shape
     if len(shape) != 5 or shape[1] != 2 or not cache.is_contiguous():
         _refuse("cache: contiguous [n_pages, 2, kv_heads, page_size, head_dim]")
+    n_pages, _, kv_heads, page_size, head_dim = shape
     if cache.dtype is _torch.bfloat16:
         if scale is not None:
             _refuse("scale goes with an e4m3 cache only")
-        return et_kv_cache(cache.data_ptr(), None, shape[0], shape[2], shape[3], shape[4], ET_KV_BF16)
+        return _KV_CACHE.pack(cache.data_ptr(), 0, n_pages, kv_heads, page_size, head_dim, ET_KV_BF16), kv_heads, head_dim
     if cache.dtype is not _torch.float8_e4m3fn:
         _refuse("cache: bfloat16 or float8_e4m3fn")
     if scale is None or scale.dtype is not _torch.uint8 or scale.shape != shape[:4] or not scale.is_contiguous():
         _refuse("an e4m3 cache needs scale: contiguous uint8 [n_pages, 2, kv_heads, page_size]")
-    return et_kv_cache(cache.data_ptr(), scale.data_ptr(), shape[0], shape[2], shape[3], shape[4], ET_KV_E4M3)
+    return (_KV_CACHE.pack(cache.data_ptr(), scale.data_ptr(), n_pages, kv_heads, page_size, head_dim, ET_KV_E4M3), kv_heads,
+            head_dim)
 
 
 def _table(block_table):
@@ -855,11 +862,11 @@ def et_kv_append(cache, scale, qkv, heads, block_table, start, row_offsets=None,
     (q_out, created if theta > 0 and heads > 0 and none is given), None without rotation."""
     if _torch is None:
         _import_torch()
-    c = _kv_cache(cache, scale)
+    c, kv_heads, head_dim = _kv_cache(cache, scale)
     n_seq, max_pages = _table(block_table)
     rows = qkv.shape[0]
     s = _launch_on(stream, cache, scale, qkv, block_table, start, row_offsets, q_out, new_len, status)
-    stride = _row_stride(qkv, (heads + 2 * c.kv_heads) * c.head_dim, "qkv")
+    stride = _row_stride(qkv, (heads + 2 * kv_heads) * head_dim, "qkv")
     _ints(start, n_seq, "start")
     if row_offsets is not None:
         _ints(row_offsets, n_seq + 1, "row_offsets")
@@ -869,10 +876,10 @@ def et_kv_append(cache, scale, qkv, heads, block_table, start, row_offsets=None,
         _ints(status, 1, "status")
     if q_out is None:
         if theta != 0 and heads > 0:
-            q_out = _new(_torch.empty, (rows, heads * c.head_dim), _torch.bfloat16, qkv, stream)
-    elif q_out.dtype is not _torch.bfloat16 or q_out.numel() != rows * heads * c.head_dim or not q_out.is_contiguous():
+            q_out = _new(_torch.empty, (rows, heads * head_dim), _torch.bfloat16, qkv, stream)
+    elif q_out.dtype is not _torch.bfloat16 or q_out.numel() != rows * heads * head_dim or not q_out.is_contiguous():
         _refuse("q_out: contiguous bf16 [rows, heads * head_dim]")
-    st = lib().et_kv_append(C.byref(c), qkv.data_ptr(), stride, rows, heads, block_table.data_ptr(), n_seq, max_pages,
+    st = lib().et_kv_append(c, qkv.data_ptr(), stride, rows, heads, block_table.data_ptr(), n_seq, max_pages,
                             _at(row_offsets), start.data_ptr(), theta, _at(q_out), _at(new_len), _at(status), s)
     if st:
         _check(st)
@@ -884,9 +891,9 @@ def et_kv_read(cache, scale, block_table, start, rows, row_offsets=None, out=Non
     them (zeros where out is created here)."""
     if _torch is None:
         _import_torch()
-    c = _kv_cache(cache, scale)
+    c, kv_heads, head_dim = _kv_cache(cache, scale)
     n_seq, max_pages = _table(block_table)
-    width = 2 * c.kv_heads * c.head_dim
+    width = 2 * kv_heads * head_dim
     if out is None:
         out = _new(_torch.zeros, (rows, width), _torch.bfloat16, cache, stream)
     elif out.shape[0] != rows:
@@ -898,7 +905,7 @@ def et_kv_read(cache, scale, block_table, start, rows, row_offsets=None, out=Non
         _ints(row_offsets, n_seq + 1, "row_offsets")
     if status is not None:
         _ints(status, 1, "status")
-    st = lib().et_kv_read(C.byref(c), out.data_ptr(), stride, rows, block_table.data_ptr(), n_seq, max_pages, _at(row_offsets),
+    st = lib().et_kv_read(c, out.data_ptr(), stride, rows, block_table.data_ptr(), n_seq, max_pages, _at(row_offsets),
                           start.data_ptr(), _at(status), s)
     if st:
         _check(st)
@@ -910,9 +917,9 @@ def et_attention_paged(q, heads, cache, scale, block_table, lens, out=None, lse=
     given; workspace: uint8 [ET_PAGED_WORKSPACE], created if none is given."""
     if _torch is None:
         _import_torch()
-    c = _kv_cache(cache, scale)
+    c, kv_heads, head_dim = _kv_cache(cache, scale)
     n_seq, max_pages = _table(block_table)
-    width = heads * c.head_dim
+    width = heads * head_dim
     if q.shape[0] != n_seq:
         _refuse("block_table: a row for each row of q")
     stride = _row_stride(q, width, "q")
@@ -930,7 +937,7 @@ def et_attention_paged(q, heads, cache, scale, block_table, lens, out=None, lse=
     _ints(lens, n_seq, "lens")
     if status is not None:
         _ints(status, 1, "status")
-    st = lib().et_attention_paged(C.byref(c), q.data_ptr(), stride, out.data_ptr(), _at(lse), n_seq, heads, block_table.data_ptr(),
+    st = lib().et_attention_paged(c, q.data_ptr(), stride, out.data_ptr(), _at(lse), n_seq, heads, block_table.data_ptr(),
                                   max_pages, lens.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                   _at(status), s)
     if st:

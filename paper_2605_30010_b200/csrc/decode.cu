@@ -42,14 +42,20 @@ et_status check_rows(const PagedCache& c, int rows, const int* table, int n_seq,
 }
 
 // theta^(-2i/dh) / (2 pi) as a fraction of 2^64: a geometric sequence in extended precision, off by less than 2^-56 of its
-// value after 64 steps, i.e. by less than 2^-24 of a turn at the largest position
-RopeTurns rope_turns(float theta, int head_dim) {
-  RopeTurns t;
-  const long double ratio = powl((long double)theta, -2.0L / head_dim);
-  long double f = 0.15915494309189533576888376337251436L * 18446744073709551616.0L;     // 2^64 / (2 pi)
-  for (int i = 0; i < 64; ++i) {
-    t.f[i] = i < head_dim / 2 ? (unsigned long long)(f + 0.5L) : 0ull;
-    f *= ratio;
+// value after 64 steps, i.e. by less than 2^-24 of a turn at the largest position.  A model has one theta and head size: each
+// host thread keeps the frequencies of the last ones (a microsecond of a call's five).
+const RopeTurns& rope_turns(float theta, int head_dim) {
+  static thread_local RopeTurns t;
+  static thread_local float of_theta = 0.f;
+  static thread_local int of_dim = 0;
+  if (theta != of_theta || head_dim != of_dim) {
+    const long double ratio = powl((long double)theta, -2.0L / head_dim);
+    long double f = 0.15915494309189533576888376337251436L * 18446744073709551616.0L;     // 2^64 / (2 pi) < 2^63
+    for (int i = 0; i < head_dim / 2; ++i) {
+      t.f[i] = (unsigned long long)(long long)(f + 0.5L);
+      f *= ratio;
+    }
+    of_theta = theta; of_dim = head_dim;
   }
   return t;
 }
@@ -75,10 +81,9 @@ et_status et_kv_append(const et_kv_cache* cache, const void* qkv_dev, long long 
   if ((q_out_dev != nullptr) != (rotate && heads > 0)) return ET_ERR_INVALID_ARG;
   if (new_len_dev && new_len_dev == start_dev) return ET_ERR_INVALID_ARG;
   if (row_stride % 8 != 0 || row_stride < ((long long)heads + 2ll * c.kv_heads) * c.head_dim) return ET_ERR_SHAPE;
-  RopeTurns turns = {};
-  if (rotate) turns = rope_turns(theta, c.head_dim);
-  launch_kv_append(c, r, (const bf16*)qkv_dev, row_stride, heads, rotate, turns, (bf16*)q_out_dev, new_len_dev,
-                   (cudaStream_t)cuda_stream);
+  static const RopeTurns none = {};
+  launch_kv_append(c, r, (const bf16*)qkv_dev, row_stride, heads, rotate, rotate ? rope_turns(theta, c.head_dim) : none, (bf16*)q_out_dev,
+                   new_len_dev, (cudaStream_t)cuda_stream);
   return launched();
 }
 

@@ -91,6 +91,9 @@ def test_struct_matches_the_header(B, tmp_path):
                    'ET_PAGED_WORKSPACE,ET_PAGED_CAPACITY,ET_PAGED_BAD_PAGE);return 0;}\n')
     subprocess.check_call(["gcc", "-I", os.path.join(root, "include"), str(src), "-o", str(tmp_path / "sz")])
     got = [int(x) for x in subprocess.check_output([str(tmp_path / "sz")]).split()]
+    assert B._KV_CACHE.size == ctypes.sizeof(B.et_kv_cache)
+    fields = (1 << 40, 2 << 40, 3, 4, 5, 6, 1)
+    assert B._KV_CACHE.pack(*fields)[:36] == bytes(B.et_kv_cache(*fields))[:36]
     assert got == [ctypes.sizeof(B.et_kv_cache), B.ET_PAGED_WORKSPACE, B.ET_PAGED_CAPACITY, B.ET_PAGED_BAD_PAGE]
 
 

@@ -194,6 +194,24 @@ def test_append_then_read(B, case, e4m3):
     assert (out[rows:] == 5.0).all() and (out[:, 2 * kvh * d:] == 5.0).all() and status.item() == 0
 
 
+def test_append_with_one_theta_after_another(B):
+    """Calls with different bases and head sizes in turn, far positions: each turns by its own angles."""
+    import torch
+    rng = np.random.default_rng(17)
+    for d, theta, start in ((128, 1e6, 1_000_000), (64, 1e4, 5), (128, 1e4, 70_000), (64, 5e5, 2_000_000), (128, 1e6, 999_983)):
+        page, kvh, heads = 128, 1, 2
+        max_pages = start // page + 1
+        c = Cache(rng, 1, 1, kvh, page, d, False)
+        table = i32(np.zeros((1, max_pages)))
+        x = bf16(rng.standard_normal((1, (heads + 2 * kvh) * d)))
+        q = B.et_kv_append(c.data, None, x, heads, table, i32([start]), theta=theta)
+        v = f64(x).reshape(1, heads + 2 * kvh, d)
+        want = rotate(v, np.array([start]), theta)
+        tol = BF16 * np.abs(want) + 2.0 ** -20 * (np.abs(v) + np.abs(np.roll(v, d // 2, -1)))
+        assert (np.abs(f64(q).reshape(1, heads, d) - want[:, :heads]) <= tol[:, :heads]).all()
+        assert (np.abs(f64(c.data[0, 0, 0, start % page]) - want[0, heads]) <= tol[0, heads]).all()
+
+
 def test_e4m3_conversion_edges(B):
     """Ties, the border between two exponents, the smallest and largest rows, zeros, NaN and infinities."""
     import torch
