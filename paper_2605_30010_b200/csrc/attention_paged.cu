@@ -64,9 +64,9 @@ struct Cfg {
   static constexpr int BOXES = ROW / BOX_ROW;
   static constexpr int PLANE = TILE * ROW;
   static constexpr int STAGE = 2 * PLANE;                         // keys, values
-  // what an item costs beside its tiles, in tiles' worth of time: some 3 000 cycles, where an SM's share of the memory bandwidth
-  // brings 32 KB in 1 300.  (Twice as much measured the same, 2 whatever the tile 64 us where this gives 58: 64 ragged, e4m3.)
-  static constexpr int ITEM_COST = 65536 / STAGE;
+  // What an item costs beside its tiles, in tiles' worth of time (measured: 2.3 us beside 0.6 us a tile for bf16 rows of 128, 2.0
+  // and 0.3 for e4m3 ones, 1.4 and 0.25 for bf16 rows of 64); an item that a group takes alone costs a good third of it.
+  static constexpr int COST = 2 + 65536 / STAGE, COST_SHORT = NT == 1 ? 1 + 32768 / STAGE : COST;
   static constexpr int SCALES = E4M3 ? 2 * TILE : 0;
   static constexpr int HEADS = 8 * NT;
   static constexpr int JOIN = COMPUTE_WARPS * HEADS * (DH + PAD) * 4 + COMPUTE_WARPS * HEADS * 3 * 4;   // the warps' results of a piece
@@ -81,7 +81,7 @@ struct Cfg {
   static constexpr int STAGES = (FIT > 16 ? 16 : FIT) / GROUPS * GROUPS;
   static constexpr int SMEM = 1024 + STAGES * (STAGE + SCALES) + EDGE + CONTROL_BYTES;
   static_assert(STAGES >= GROUPS, "ring");
-  static_assert(ITEM_COST <= PAGED_ITEM_COST_MAX, "units");
+  static_assert(COST <= PAGED_ITEM_COST_MAX, "units");
   static_assert(8 * (2 * STAGES + 2 * GROUPS + 4) + 4 * STAGES + 16 <= CONTROL_BYTES, "control area");
 };
 
@@ -163,9 +163,12 @@ __device__ __forceinline__ int clamped_len(const Args& g, int s) {
   const long long cap = (long long)g.a.max_pages << g.c.page_shift;
   return (int)min((long long)max(__ldg(g.a.len + s), 0), cap);
 }
-// An item's units: its tiles and, in front of them, `cost` for what every item costs however short it is.
-__device__ __forceinline__ int units_of(const Args& g, int len, int cost) {
-  return len <= 0 ? 0 : g.whole ? 1 : (int)((unsigned)(len + (TILE - 1)) / TILE) + cost;
+// An item's units: its tiles and, in front of them, units for what it costs beside them.  C: the kernel's Cfg
+__device__ __forceinline__ int tiles_of(int len) { return (int)((unsigned)(len + (TILE - 1)) / TILE); }
+template <class C> __device__ __forceinline__ int cost_of(int tiles) { return tiles <= ALONE_TILES ? C::COST_SHORT : C::COST; }
+template <class C> __device__ __forceinline__ int units_of(const Args& g, int len) {
+  const int tiles = tiles_of(len);
+  return len <= 0 ? 0 : g.whole ? 1 : tiles + cost_of<C>(tiles);
 }
 
 // The run of units that falls to a CTA, walked piece by piece.
@@ -198,14 +201,16 @@ __device__ __forceinline__ Deal deal(const Piece& p, bool may, int chunk, int gr
   return d;
 }
 
-__device__ __forceinline__ bool next_piece(const Args& g, int parts_all, int cost, Walk& w, Piece& p) {
+template <class C>
+__device__ __forceinline__ bool next_piece(const Args& g, int parts_all, Walk& w, Piece& p) {
   while (w.left > 0) {
-    const int units = units_of(g, w.len, cost);
+    const int units = units_of<C>(g, w.len);
     if (units > 0) {
       const int n = min(w.left, units - w.unit), end = w.unit + n;
       p.s = w.s; p.part = w.part; p.len = w.len; p.units = units; p.units_end = end;
+      const int tiles = tiles_of(w.len), cost = cost_of<C>(tiles);
       p.t0 = g.whole ? 0 : max(w.unit - cost, 0);
-      p.t1 = g.whole ? (int)((unsigned)(w.len + (TILE - 1)) / TILE) : max(end - cost, 0);
+      p.t1 = g.whole ? tiles : max(end - cost, 0);
       p.first = p.t0 == 0; p.last = end == units;
       w.left -= n; w.unit = end;
       if (end == units) { w.unit = 0; ++w.part; }
@@ -223,7 +228,7 @@ template <int DH, bool E4M3, int NT>
 __global__ void __launch_bounds__(THREADS, 1)
 attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ Args g) {
   using C = Cfg<DH, E4M3, NT>;
-  constexpr int STAGES = C::STAGES, KS = DH / 16, ITEM_COST = C::ITEM_COST;
+  constexpr int STAGES = C::STAGES, KS = DH / 16;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const gen = smem_raw + (base - raw);
@@ -266,7 +271,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
   {
     const int per = (g.a.n_seq + THREADS - 1) / THREADS, s0 = min(tid * per, g.a.n_seq), s1 = min(s0 + per, g.a.n_seq);
     int sum = 0;
-    for (int s = s0; s < s1; ++s) sum += units_of(g, clamped_len(g, s), ITEM_COST);
+    for (int s = s0; s < s1; ++s) sum += units_of<C>(g, clamped_len(g, s));
     sum *= parts_all;
     int inc = sum;
 #pragma unroll
@@ -281,7 +286,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     if (begin >= before && begin < before + sum) {
       int r = begin - before;
       for (int s = s0; s < s1; ++s) {
-        const int len = clamped_len(g, s), u = units_of(g, len, ITEM_COST);
+        const int len = clamped_len(g, s), u = units_of<C>(g, len);
         if (r < u * parts_all) { walk_s[0] = s; walk_s[1] = r / u; walk_s[2] = r % u; walk_s[3] = len; break; }
         r -= u * parts_all;
       }
@@ -312,7 +317,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     int turn = 0;
     uint32_t q_phase = 0;
     Piece p;
-    while (ok && next_piece(g, parts_all, ITEM_COST, walk, p)) {
+    while (ok && next_piece<C>(g, parts_all, walk, p)) {
       const Deal dl = deal(p, C::ALONE, chunk, me, turn);
       if (dl.t >= p.t1) continue;
       // the piece's queries: rows of the heads, zeros for heads that the group does not have
@@ -459,7 +464,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     int stage = my_group, shared = 0, turn = 0;                      // shared: pieces so far that all groups shared
     uint32_t phase = 0, q_phase = 0;
     Piece p, before;
-    while (next_piece(g, parts_all, ITEM_COST, walk, p)) {
+    while (next_piece<C>(g, parts_all, walk, p)) {
       if (p.first && !p.last) {
         // the item goes on in the CTAs behind this one, each of which finds it at the start of its run
         const int item0 = begin + chunk - p.units_end;               // this piece ends this CTA's run (whole items are not cut)
