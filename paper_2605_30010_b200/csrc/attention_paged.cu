@@ -21,9 +21,9 @@
 // for e4m3 ones (a half), which the output's rounding to 8 covers.
 //
 // Device time in a chain of calls, B200, cache not in L2 (of the measured copy bandwidth; a pure read can pass 1): 28 heads on 4
-// of 128, bf16, one sequence of 100 003 38 us (0.84); e4m3, 64 ragged sequences up to 16 001 56 us (0.84); 16 heads of 128 on 16,
+// of 128, bf16, one sequence of 100 003 38 us (0.83); e4m3, 64 ragged sequences up to 16 001 54 us (0.86); 16 heads of 128 on 16,
 // one of 180 000, bf16 217 us (1.05), e4m3 115 us (1.00); 24 ragged up to 2 049, 16 heads of 64, bf16 20 us (0.56: short items);
-// 16 heads to a key / value head, 64 ragged, bf16 110 us (0.84), e4m3 89 us (0.53: bound by conversions and exponentials).
+// 16 heads to a key / value head, 64 ragged, bf16 104 us (0.89), e4m3 67 us (0.70: bound by conversions and exponentials).
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
@@ -65,8 +65,9 @@ struct Cfg {
   static constexpr int PLANE = TILE * ROW;
   static constexpr int STAGE = 2 * PLANE;                         // keys, values
   // What an item costs beside its tiles, in tiles' worth of time (measured: 2.3 us beside 0.6 us a tile for bf16 rows of 128, 2.0
-  // and 0.3 for e4m3 ones, 1.4 and 0.25 for bf16 rows of 64); an item that a group takes alone costs a good third of it.
-  static constexpr int COST = 2 + 65536 / STAGE, COST_SHORT = NT == 1 ? 1 + 32768 / STAGE : COST;
+  // and 0.3 for e4m3 ones, 1.4 and 0.25 for bf16 rows of 64; with 16 heads 2.8 and 0.65, 3.7 and 0.4); an item that a group takes
+  // alone costs a good third of it.
+  static constexpr int COST = (2 + 65536 / STAGE) * (NT + 1) / 2, COST_SHORT = NT == 1 ? 1 + 32768 / STAGE : COST;
   static constexpr int SCALES = E4M3 ? 2 * TILE : 0;
   static constexpr int HEADS = 8 * NT;
   static constexpr int JOIN = COMPUTE_WARPS * HEADS * (DH + PAD) * 4 + COMPUTE_WARPS * HEADS * 3 * 4;   // the warps' results of a piece
