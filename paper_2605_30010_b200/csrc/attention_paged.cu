@@ -162,7 +162,7 @@ __device__ __forceinline__ void copies_arrive(uint32_t bar) {
 
 __device__ __forceinline__ int clamped_len(const Args& g, int s) {
   const long long cap = (long long)g.a.max_pages << g.c.page_shift;
-  return (int)min((long long)max(__ldg(g.a.len + s), 0), cap);
+  return (int)min((long long)max(g.a.len[s], 0), cap);
 }
 // An item's units: its tiles and, in front of them, units for what it costs beside them.  C: the kernel's Cfg
 __device__ __forceinline__ int tiles_of(int len) { return (int)((unsigned)(len + (TILE - 1)) / TILE); }
@@ -343,7 +343,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
       // 32 entries of the table, one per lane, as the first rows of their keys in the cache (-1: not a page of the cache)
       auto load_ids = [&](int batch) {
         const long long i = (long long)first_page + batch * 32 + lane;
-        return i <= last_page ? __ldg(table + i) : 0;
+        return i <= last_page ? table[i] : 0;
       };
       auto rows_of = [&](int page) {
         const bool good = (unsigned)page < (unsigned)g.c.n_pages;
@@ -802,7 +802,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 
     // ---- sequences without positions, and lengths that the table cannot hold
     for (int s = b; s < g.a.n_seq; s += gridDim.x) {
-      const int len = __ldg(g.a.len + s);
+      const int len = g.a.len[s];
       if (len <= 0) {
         for (int i = tid; i < g.a.heads * DH / 8; i += 32 * COMPUTE_WARPS)
           reinterpret_cast<uint4*>(g.a.out + (size_t)s * g.a.heads * DH)[i] = make_uint4(0, 0, 0, 0);

@@ -48,7 +48,9 @@ cudaError_t launch_linear_rows(const bf16* a, const bf16* w, const float* bias, 
                                int gelu_tanh, int* status, cudaStream_t s);
 
 // Every kernel of the decode step is launched so that it may be set up while the kernel before it in the stream still runs
-// (programmatic dependent launch), and begins, before it touches memory, by waiting for that one's end and results.
+// (programmatic dependent launch), and begins, before it touches memory, by waiting for that one's end and results.  What these
+// kernels read may be what the kernel before wrote while they were resident already: none of it is read with non-coherent loads
+// (__ldg, .nc, const __restrict__ parameters), which may come before the wait or from a stale line.
 __device__ __forceinline__ void begin_after_previous() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");    // the next kernel may be set up; it waits in turn
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -79,7 +81,7 @@ __device__ __forceinline__ bool paged_place(const PagedCache& c, const int* tabl
     if (status) atomicMax(status, (int)ET_PAGED_CAPACITY);
     return false;
   }
-  page = __ldg(table + (size_t)s * max_pages + (pos >> c.page_shift));
+  page = table[(size_t)s * max_pages + (pos >> c.page_shift)];
   place = (int)(pos & ((1 << c.page_shift) - 1));
   if ((unsigned)page >= (unsigned)c.n_pages) {
     if (status) atomicMax(status, (int)ET_PAGED_BAD_PAGE);

@@ -29,14 +29,14 @@ struct Places {
         int lo = 0, hi = r.n_seq;
         while (hi - lo > 1) {
           const int mid = (lo + hi) >> 1;
-          if (__ldg(r.offsets + mid) <= row) lo = mid; else hi = mid;
+          if (r.offsets[mid] <= row) lo = mid; else hi = mid;
         }
         s = lo;
-        first = __ldg(r.offsets + s);
-        behind = __ldg(r.offsets + s + 1);
+        first = r.offsets[s];
+        behind = r.offsets[s + 1];
       }
       seq = s;
-      start = __ldg(r.start + s);
+      start = r.start[s];
       page_of = -1;
     }
     if (row < first || row >= behind || start < 0) return false;
@@ -102,8 +102,8 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
 // ---------------------------------------------------------------------------------------------
 template <int DH, bool E4M3, bool ROTATE>
 __global__ void __launch_bounds__(THREADS)
-kv_append_kernel(const bf16* __restrict__ qkv, long long row_stride, int heads, PagedCache c, PagedRows r,
-                 const __grid_constant__ RopeTurns turns, bf16* __restrict__ q_out, int* __restrict__ new_len, int rows_each, int parts) {
+kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c, PagedRows r,
+                 const __grid_constant__ RopeTurns turns, bf16* q_out, int* new_len, int rows_each, int parts) {
   constexpr int HALF = DH / 2, CHUNKS = DH / 16, UNROLL = 2;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int part = warp % parts, chunk = lane % CHUNKS, head_lane = lane / CHUNKS;
@@ -135,8 +135,8 @@ kv_append_kernel(const bf16* __restrict__ qkv, long long row_stride, int heads, 
         va[j] = vb[j] = make_uint4(0, 0, 0, 0);
         if (head < all_heads) {
           const bf16* src = src_row + (size_t)head * DH;
-          va[j] = __ldg(reinterpret_cast<const uint4*>(src));
-          vb[j] = __ldg(reinterpret_cast<const uint4*>(src + HALF));
+          va[j] = *reinterpret_cast<const uint4*>(src);
+          vb[j] = *reinterpret_cast<const uint4*>(src + HALF);
         }
       }
     };
@@ -224,7 +224,7 @@ kv_append_kernel(const bf16* __restrict__ qkv, long long row_stride, int heads, 
 // ---------------------------------------------------------------------------------------------
 template <int DH, bool E4M3>
 __global__ void __launch_bounds__(THREADS)
-kv_read_kernel(bf16* __restrict__ out, long long row_stride, PagedCache c, PagedRows r, int rows_each, int parts) {
+kv_read_kernel(bf16* out, long long row_stride, PagedCache c, PagedRows r, int rows_each, int parts) {
   constexpr int VEC = E4M3 ? 16 : 8, CHUNKS = DH / VEC, UNROLL = 4;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % parts;
   const int units = 2 * c.kv_heads * CHUNKS;
@@ -248,8 +248,8 @@ kv_read_kernel(bf16* __restrict__ out, long long row_stride, PagedCache c, Paged
         if (u < units) {
           const int plane = head >= c.kv_heads ? 1 : 0;
           const size_t at = cache_row(c, page, plane, head - plane * c.kv_heads, place);
-          v[j] = __ldg(reinterpret_cast<const uint4*>(c.data + at * (DH * (E4M3 ? 1 : 2)) + chunk * 16));
-          if (E4M3) b[j] = __ldg(c.scale + at);
+          v[j] = *reinterpret_cast<const uint4*>(c.data + at * (DH * (E4M3 ? 1 : 2)) + chunk * 16);
+          if (E4M3) b[j] = c.scale[at];
         }
       }
 #pragma unroll

@@ -47,10 +47,10 @@ __device__ __forceinline__ void load_vec(Vec& v, const bf16* p, int k, int K, bo
   if (WIDE) {
     if (live && k < K) {
       if (ONCE)
-        asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+        asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                      : "=r"(v.r[0]), "=r"(v.r[1]), "=r"(v.r[2]), "=r"(v.r[3]), "=r"(v.r[4]), "=r"(v.r[5]), "=r"(v.r[6]), "=r"(v.r[7]) : "l"(p + k));
       else
-        asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                      : "=r"(v.r[0]), "=r"(v.r[1]), "=r"(v.r[2]), "=r"(v.r[3]), "=r"(v.r[4]), "=r"(v.r[5]), "=r"(v.r[6]), "=r"(v.r[7]) : "l"(p + k));
     } else {
 #pragma unroll
@@ -60,7 +60,7 @@ __device__ __forceinline__ void load_vec(Vec& v, const bf16* p, int k, int K, bo
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       uint4 x = make_uint4(0, 0, 0, 0);
-      if (live && k + 8 * h < K) x = __ldg(reinterpret_cast<const uint4*>(p + k + 8 * h));
+      if (live && k + 8 * h < K) x = *reinterpret_cast<const uint4*>(p + k + 8 * h);
       v.r[4 * h] = x.x; v.r[4 * h + 1] = x.y; v.r[4 * h + 2] = x.z; v.r[4 * h + 3] = x.w;
     }
   }

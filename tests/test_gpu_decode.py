@@ -115,6 +115,7 @@ APPENDS = [
     ([200], [3], 0, 4, 128, 128, 0.0),
     ([5, 300, 17], [1000, 0, 2], 0, 3, 16, 64, 0.0),
     ([2, 3], [10, 20], 5, 5, 64, 64, 0.0),
+    ([(7 * i) % 5 for i in range(150)], [(37 * i) % 91 for i in range(150)], 2, 2, 16, 64, 1e4),
 ]
 
 
@@ -348,11 +349,11 @@ def test_attention(B, case, d, e4m3):
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
-@pytest.mark.parametrize("heads,kvh,page,d,longest", [(8, 8, 16, 64, 300), (28, 4, 32, 128, 400), (16, 1, 64, 128, 900), (6, 2, 16, 64, 1000)])
+@pytest.mark.parametrize("heads,kvh,page,d,longest", [(8, 8, 16, 64, 300), (28, 4, 32, 128, 400), (16, 1, 64, 128, 900), (6, 2, 16, 64, 1000), (2, 1, 32, 64, 90)])
 def test_attention_many_short_sequences(B, heads, kvh, page, d, longest, e4m3):
     """Many more sequences than SMs, of very different lengths in no order, some empty: every CTA has many pieces."""
     rng = np.random.default_rng(heads * 7 + e4m3)
-    n_seq = 331
+    n_seq = 331 if longest > 100 else 1500
     lens = [int(longest * x ** 3) for x in rng.random(n_seq)]
     lens[5:9] = [longest, 0, 1, longest]
     c = Cache(rng, n_seq, (longest + page - 1) // page, kvh, page, d, e4m3)
@@ -793,3 +794,44 @@ def test_decode_operators_in_one_graph(B):
         torch.cuda.synchronize()
         assert torch.equal(out, y)
     assert torch.equal(b.bytes()[0], a.bytes()[0]) and torch.equal(b.scale, a.scale)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_steps_one_behind_the_other_without_waiting(B, e4m3):
+    """Sixty decode steps (dense layer, append, attention, dense layer), each reading what the step before has just written --
+    lengths, cache rows, activations -- enqueued without a wait, against the same steps with a wait behind every call: the
+    same bits.  (The kernels are set up while the ones before them still run.)"""
+    import torch
+    n, heads, kvh, page, d, hidden = 5, 6, 2, 16, 64, 512
+    rng = np.random.default_rng(51)
+    wqkv = bf16(rng.standard_normal(((heads + 2 * kvh) * d, hidden)) / math.sqrt(hidden))
+    wo = bf16(rng.standard_normal((hidden, heads * d)) / math.sqrt(heads * d))
+    x0 = bf16(rng.standard_normal((n, hidden)))
+
+    def run(wait):
+        c = Cache(np.random.default_rng(52), n, 6, kvh, page, d, e4m3)
+        both = i32([13, 0, 30, 5, 31] + [0] * n)                               # lengths, in turn in two halves of one line
+        lens = [both[:n], both[n:]]
+        qkv = torch.empty((n, (heads + 2 * kvh) * d), dtype=torch.bfloat16, device="cuda")
+        q = torch.empty((n, heads * d), dtype=torch.bfloat16, device="cuda")
+        att, x, ws = torch.empty_like(q), x0.clone(), torch.empty(B.ET_PAGED_WORKSPACE, dtype=torch.uint8, device="cuda")
+        out = torch.empty((60, n, hidden), dtype=torch.bfloat16, device="cuda")
+        torch.cuda.synchronize()
+        done = torch.cuda.synchronize if wait else (lambda: None)
+        for i in range(60):
+            B.et_linear_rows(x, wqkv, c=qkv)
+            done()
+            B.et_kv_append(c.data, c.scale, qkv, heads, c.table, lens[i % 2], theta=1e4, q_out=q, new_len=lens[1 - i % 2])
+            done()
+            B.et_attention_paged(q, heads, c.data, c.scale, c.table, lens[1 - i % 2], out=att, workspace=ws)
+            done()
+            x = B.et_linear_rows(att, wo, epilogue=1, c=out[i])
+            done()
+        torch.cuda.synchronize()
+        return out, both.tolist()
+
+    a, la = run(True)
+    for _ in range(3):
+        b, lb = run(False)
+        assert torch.equal(a, b) and la == lb
+    assert la[:n] == [73, 60, 90, 65, 91]
