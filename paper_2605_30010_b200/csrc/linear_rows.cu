@@ -6,7 +6,8 @@
 // the tensor work here is a few per cent of the time.)  Two kernels share the epilogue:
 //
 //   direct  weights go from memory to the registers that feed the tensor core; a block has 32 weight rows.  Starts fast.
-//   ring    TMA tiles of 128 weight rows and of a in a ring of five stages; a is fetched once for four times as many weights.
+//   ring    TMA tiles of up to 128 weight rows and of a in a ring of five stages; a is fetched once for up to four times as
+//           many weights.
 //
 // K is shared by the warps of a block (direct) and by the blocks of a cluster where there are too few blocks to fill the
 // card.  Sums meet in shared memory (of the cluster) in a fixed order.
@@ -78,7 +79,7 @@ struct LinearArgs {
 // The block's sums [m][ROWS] of every rank become outputs, dealt to the ranks' threads four at a time; the ranks' parts are
 // fetched together and added in order.  In a gated block 16 gate rows are followed by the 16 up rows of the same outputs.
 template <int ROWS, int NTHREADS>
-__device__ __forceinline__ void finish(const LinearArgs& g, cg::cluster_group& cluster, float* part, int block, int ranks, int rank) {
+__device__ __forceinline__ void finish(const LinearArgs& g, cg::cluster_group& cluster, float* part, int rows, int block, int ranks, int rank) {
   const int tid = threadIdx.x;
   const bool gated = g.epilogue == EPI_SWIGLU;
   auto total = [&](int r, int m, float (&y)[4]) {
@@ -91,7 +92,7 @@ __device__ __forceinline__ void finish(const LinearArgs& g, cg::cluster_group& c
     for (int p = 0; p < MAX_CLUSTER; ++p)
       if (p < ranks) { y[0] += v[p].x; y[1] += v[p].y; y[2] += v[p].z; y[3] += v[p].w; }
   };
-  const int outs = gated ? g.N / 2 : g.N, quads = gated ? ROWS / 8 : ROWS / 4;
+  const int outs = gated ? g.N / 2 : g.N, quads = gated ? rows / 8 : rows / 4;
   const bool vectors = outs % 4 == 0;          // a row's groups of four are aligned
   for (int e = rank * NTHREADS + tid; e < quads * g.M; e += ranks * NTHREADS) {
     const int q = e % quads, m = e / quads;
@@ -139,7 +140,7 @@ __global__ void __launch_bounds__(THREADS, 2)
 linear_direct_kernel(const LinearArgs g) {
   constexpr int COLS = 8 * NT, LD = COLS + 1;
   constexpr int ROWS = BLOCK_ROWS;
-    __shared__ __align__(16) float red[WARPS * ROWS * LD];
+  __shared__ __align__(16) float red[WARPS * ROWS * LD];
   float* const part = red;
   cg::cluster_group cluster = cg::this_cluster();
   const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -226,15 +227,15 @@ linear_direct_kernel(const LinearArgs g) {
     if (e < ROWS * g.M) part[e] = sums[i];
   }
   if (ranks > 1) cluster.sync(); else __syncthreads();
-  finish<ROWS, THREADS>(g, cluster, part, block, ranks, rank);
+  finish<ROWS, THREADS>(g, cluster, part, ROWS, block, ranks, rank);
   if (ranks > 1) cluster.sync();               // a block's sums stay until its neighbours have read them
 }
 
 // ---------------------------------------------------------------------------------------------
-// Ring: one warp copies, four compute, 32 weight rows each.  100 KB a block, two blocks an SM, about 160 KB of weights on
+// Ring: one warp copies, four compute, up to 32 weight rows each.  100 KB a block, two blocks an SM, about 160 KB of weights on
 // their way.  A rank of a cluster takes every ranks-th step of 64 along K.
 // ---------------------------------------------------------------------------------------------
-constexpr int RING_ROWS = 128, RING_WARPS = 4, RING_THREADS = 32 * (RING_WARPS + 1);
+constexpr int RING_ROWS = 128 /* at most */, RING_WARPS = 4, RING_THREADS = 32 * (RING_WARPS + 1);
 template <int NT> struct Ring {
   static constexpr int W_BYTES = RING_ROWS * 128, A_BYTES = 8 * NT * 128, STAGE = W_BYTES + A_BYTES;
   static constexpr int STAGES = 5;
@@ -247,7 +248,7 @@ __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
 
 template <int NT>
 __global__ void __launch_bounds__(RING_THREADS, 2)
-linear_ring_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap amap, const LinearArgs g) {
+linear_ring_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap amap, const LinearArgs g, const int rows) {
   using R = Ring<NT>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -290,8 +291,8 @@ linear_ring_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
         if (!ok) break;
         const uint32_t dst = base + stage * R::STAGE;
         const int x = (rank + issued * ranks) * 64;
-        mbar_arrive_expect_tx(full(stage), R::STAGE);
-        tma_load_2d(dst, &wmap, full(stage), x, block * RING_ROWS);
+        mbar_arrive_expect_tx(full(stage), (uint32_t)rows * 128u + R::A_BYTES);
+        tma_load_2d(dst, &wmap, full(stage), x, block * rows);
         tma_load_2d(dst + R::W_BYTES, &amap, full(stage), x, 0);
         if (++stage == R::STAGES) { stage = 0; phase ^= 1u; }
       }
@@ -360,7 +361,7 @@ linear_ring_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
         for (int j = 0; j < 4; ++j) part[(n * 8 + 2 * tq + (j & 1)) * RING_ROWS + warp * 32 + i * 16 + gq + (j >> 1) * 8] = acc[i][n][j];
   }
   if (ranks > 1) cluster.sync(); else __syncthreads();
-  finish<RING_ROWS, RING_THREADS>(g, cluster, part, block, ranks, rank);
+  finish<RING_ROWS, RING_THREADS>(g, cluster, part, rows, block, ranks, rank);
   if (tid == 0 && *abort_flag && g.status) atomicMax(g.status, (int)DS_WAIT_EXPIRED);
   if (ranks > 1) cluster.sync();               // a block's sums stay until its neighbours have read them
 }
@@ -379,9 +380,7 @@ cudaError_t launch_direct(const LinearArgs& g, cudaStream_t s) {
 template <int NT>
 cudaError_t launch_ring(const LinearArgs& g, cudaStream_t s) {
   using R = Ring<NT>;
-  TmaDesc w, a;
-  if (!make_tma_2d_bf16(&w, g.w, g.N, g.K, RING_ROWS, nullptr) || !make_tma_2d_bf16(&a, g.a, g.M, g.K, 8 * NT, nullptr)) return cudaErrorUnknown;
-  // clusters of each size that the card holds at once, per device, looked up once
+  // clusters of each size (of one: blocks) that the card holds at once, per device, looked up once
   constexpr int DEVICES = 64;
   static std::atomic<int> resident[DEVICES][MAX_CLUSTER + 1];       // zero: not looked up; [1] is set last
   int dev = 0;
@@ -391,21 +390,39 @@ cudaError_t launch_ring(const LinearArgs& g, cudaStream_t s) {
   if (!resident[dev][1]) {
     e = cudaFuncSetAttribute(linear_ring_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::SMEM);
     if (e != cudaSuccess) return e;
-    for (int ranks = MAX_CLUSTER; ranks >= 1; --ranks) {
+    for (int ranks = MAX_CLUSTER; ranks >= 2; --ranks) {
       Launch probe(ranks, RING_THREADS, R::SMEM, s, ranks);
       int n = 0;
       e = cudaOccupancyMaxActiveClusters(&n, linear_ring_kernel<NT>, &probe.cfg);
       if (e != cudaSuccess) return e;
       resident[dev][ranks] = n > 0 ? n : 1;
     }
+    int sms = 0, per_sm = 0;
+    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, linear_ring_kernel<NT>, RING_THREADS, R::SMEM);
+    if (e != cudaSuccess) return e;
+    resident[dev][1] = sms * per_sm > 0 ? sms * per_sm : 1;
   }
-  const int blocks = cdiv(g.N, RING_ROWS), steps = cdiv(g.K, STEP);
+  const int steps = cdiv(g.K, STEP);
   int ranks = 1;
-  for (int r = 2; r <= MAX_CLUSTER && steps >= 4 * r; ++r) if (blocks <= resident[dev][r]) ranks = r;
+  for (int r = 2; r <= MAX_CLUSTER && steps >= 4 * r; ++r) if (cdiv(g.N, RING_ROWS) <= resident[dev][r]) ranks = r;
+  // Where the places limit the ranks, a block has as few rows (a swizzle pattern's 8 at a time) as the number of waves that blocks
+  // of 128 need allows, so that the last wave is full too.  128 / these in us: 1 x 3584 x 40000 54.7 / 48.0 (72 rows), 1 x 8192 x
+  // 40000 118.8 / 103.8 (72), 32 x 3584 x 50000 74.3 / 66.2 (88), 1 x 3584 x 152064 161.8 / 159.5 (104), 32 x 2048 x 22000 22.2 /
+  // 20.4 (80), 19 x 10152 x 9728 39.3 / 38.2 (112), 32 x 2048 x 152064 115.4 / 116.7 (104).  Gated rows stay in groups of 64, of
+  // which 64 are too few for a block (3584 x 38912 54.8 / 60.1).  At eight ranks fewer rows gain nothing (13 x 3584 x 2048 5.9 / 6.1).
+  int rows = RING_ROWS;
+  if (g.epilogue != EPI_SWIGLU && ranks < MAX_CLUSTER) {
+    const int places = cdiv(cdiv(g.N, RING_ROWS), resident[dev][ranks]) * resident[dev][ranks];
+    rows = cdiv(cdiv(g.N, places), 8) * 8;
+  }
+  const int blocks = cdiv(g.N, rows);
+  TmaDesc w, a;
+  if (!make_tma_2d_bf16(&w, g.w, g.N, g.K, rows, nullptr) || !make_tma_2d_bf16(&a, g.a, g.M, g.K, 8 * NT, nullptr)) return cudaErrorUnknown;
   Launch l(blocks * ranks, RING_THREADS, R::SMEM, s, ranks);
   ET_COUNT_LAUNCH();
   return cudaLaunchKernelEx(&l.cfg, linear_ring_kernel<NT>, *reinterpret_cast<const CUtensorMap*>(w.bytes),
-                            *reinterpret_cast<const CUtensorMap*>(a.bytes), g);
+                            *reinterpret_cast<const CUtensorMap*>(a.bytes), g, rows);
 }
 
 }  // namespace

@@ -660,6 +660,13 @@ def test_linear_rows(B, M, K, N, epilogue, gelu_tanh, with_bias):
     assert (guard[M * outs:] == 3.0).all()
 
 
+@pytest.mark.parametrize("epilogue", [0, 2])
+@pytest.mark.parametrize("M,K,N", [(3, 1000, 40007), (12, 136, 46001), (32, 72, 50002), (17, 1016, 12003), (32, 264, 22010)])
+def test_linear_rows_in_blocks_of_fewer_rows(B, M, K, N, epilogue):
+    """Blocks' rows follow from how many blocks the card holds; none of these fills whole blocks of 128."""
+    test_linear_rows(B, M, K, N, epilogue, 1, True)
+
+
 @pytest.mark.parametrize("M,K,N", [(2, 1024, 384), (12, 3584, 640), (30, 2048, 384)])
 def test_linear_rows_from_16_byte_aligned_operands(B, M, K, N):
     """Operands that start 16 bytes behind a 32-byte border give what aligned ones give."""
