@@ -13,7 +13,7 @@
 // card.  Sums meet in shared memory (of the cluster) in a fixed order.
 //
 // Device time per call in a chain of calls, B200, weights not in L2 (of the measured copy bandwidth):
-//   1 x 3584 x 4608 7.4 us (0.70, direct), 1 x 3584 x 37888 gated 42 us (1.00, ring), 19 x the same 46 us (0.91),
+//   1 x 3584 x 4608 7.4 us (0.70, direct), 1 x 3584 x 37888 gated 42 us (1.00, ring), 19 x the same 46 us (0.92),
 //   1 x 18944 x 3584 residual 23.5 us (0.90, ring), 32 x the same 26 us (0.81)
 #include <cooperative_groups.h>
 
