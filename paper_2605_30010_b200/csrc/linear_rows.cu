@@ -406,11 +406,12 @@ cudaError_t launch_ring(const LinearArgs& g, cudaStream_t s) {
   const int steps = cdiv(g.K, STEP);
   int ranks = 1;
   for (int r = 2; r <= MAX_CLUSTER && steps >= 4 * r; ++r) if (cdiv(g.N, RING_ROWS) <= resident[dev][r]) ranks = r;
-  // Where the places limit the ranks, a block has as few rows (a swizzle pattern's 8 at a time) as the number of waves that blocks
-  // of 128 need allows, so that the last wave is full too.  128 / these in us: 1 x 3584 x 40000 54.7 / 48.0 (72 rows), 1 x 8192 x
-  // 40000 118.8 / 103.8 (72), 32 x 3584 x 50000 74.3 / 66.2 (88), 1 x 3584 x 152064 161.8 / 159.5 (104), 32 x 2048 x 22000 22.2 /
-  // 20.4 (80), 19 x 10152 x 9728 39.3 / 38.2 (112), 32 x 2048 x 152064 115.4 / 116.7 (104).  Gated rows stay in groups of 64, of
-  // which 64 are too few for a block (3584 x 38912 54.8 / 60.1).  At eight ranks fewer rows gain nothing (13 x 3584 x 2048 5.9 / 6.1).
+  // Below eight ranks a block has as few rows (a swizzle pattern's 8 at a time) as the number of waves that blocks of 128 need
+  // allows, so that the last wave is full too.  128 / these in us: 1 x 3584 x 40000 54.7 / 47.0 (72 rows), 1 x 8192 x 40000 118.8 /
+  // 103.8 (72), 32 x 3584 x 50000 74.3 / 66.2 (88), 1 x 3584 x 152064 161.8 / 156.4 (104), 32 x 2048 x 22000 22.2 / 20.8 (80), 32 x
+  // 520 x 8000 7.8 / 6.8 (56), 19 x 10152 x 9728 39.3 / 38.2 (112), 12 x 1504 x 5000 5.8 / 6.0, 32 x 2048 x 152064 115.4 / 116.7
+  // (104).  Gated rows stay in groups of 64, of which one is too few for a block (3584 x 38912 54.8 / 60.1).  At eight ranks
+  // fewer rows gain nothing (13 x 3584 x 2048 5.9 / 6.1).
   int rows = RING_ROWS;
   if (g.epilogue != EPI_SWIGLU && ranks < MAX_CLUSTER) {
     const int places = cdiv(cdiv(g.N, RING_ROWS), resident[dev][ranks]) * resident[dev][ranks];
