@@ -18,7 +18,10 @@
 //     second, small kernel joins them in a fixed order.
 //
 // Scores, maxima, sums and outputs are fp32; a weight is rounded to 16 bits of mantissa for bf16 values (two bf16 added), to 11
-// for e4m3 ones (a half), which the output's rounding to 8 covers.
+// for e4m3 ones (a half), which the output's rounding to 8 covers.  A half has few exponents, and an e4m3 value's scale is part of
+// its weight: the largest weight is kept at 2^15, so that 11 bits are there down to 2^-29 of it, and a tile with scales more than
+// 2^8 below those of the values that the scores favour takes two bf16 a weight instead.  So a probability has its 11 bits down
+// to 2^-21 of the largest one, whatever the scales, and is off by at most 2^-32 of that one below.
 //
 // Device time in a chain of calls, B200, cache not in L2 (of the measured copy bandwidth; a pure read can pass 1): 28 heads on 4
 // of 128, bf16, one sequence of 100 003 38 us (0.83); e4m3, 64 ragged sequences up to 16 001 54 us (0.86); 16 heads of 128 on 16,
@@ -28,6 +31,7 @@
 #include <cuda_fp8.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "decode.cuh"
 #include "tcgen05.cuh"
@@ -136,6 +140,13 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 // 2^e for e in [-127, 127]
 __device__ __forceinline__ float pow2(int e) { return __int_as_float(e > -127 ? (e + 127) << 23 : 1 << 22); }
+// two halves as two bf16, exactly for e4m3 values (4 bits, 2^-9 .. 448)
+__device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t x) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x));
+  return pack_bf16(f.x, f.y);
+}
+constexpr float WEIGHT_SHIFT = 15.f;           // e4m3: the largest weight is 2^15, halves end at 65504
+constexpr float SCALE_SPAN = 8.f;              // e4m3: binades that a tile's scales may lie low for halves to hold its weights
 // Copies by a converged warp: all lanes execute the call, one elected lane issues.
 __device__ __forceinline__ void arrive_expect_elect(uint32_t bar, uint32_t bytes) {
   asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
@@ -597,7 +608,17 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
               ks[j][0] = ks[j][1] = 1.f; ve[j][0] = ve[j][1] = 0.f;
             }
           }
-          bool moved = false;
+          // e4m3: the smallest exponent of a live value, below which by how much the scores' favourites lie (mo - m)
+          float lowest = INFINITY;
+          if constexpr (E4M3) {
+#pragma unroll
+            for (int j = 0; j < BLOCKS; ++j) {
+              if (gq < valid[j]) lowest = fminf(lowest, ve[j][0]);
+              if (gq + 8 < valid[j]) lowest = fminf(lowest, ve[j][1]);
+            }
+            lowest += SCALE_SPAN;
+          }
+          bool moved = false, spread = false;
           float alpha[NT][2];
 #pragma unroll
           for (int n = 0; n < NT; ++n)
@@ -630,6 +651,8 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                 moved |= on != mo[n][i];
                 alpha[n][i] = exp2_fast(mo[n][i] - ou);
                 mo[n][i] = on;
+                spread |= on - mn > lowest;
+                ou -= WEIGHT_SHIFT;
               }
               // the scores become weights
 #pragma unroll
@@ -643,73 +666,98 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
               l[n][i] = l[n][i] * al + sum;
               m[n][i] = mn;
             }
-          if (__any_sync(0xffffffffu, moved)) {
+          // ---- O^T += V^T P^T.  P as the B operand: 8 x 8 transposes of the accumulator's pairs.  PAIR: a probability is split
+          // into two bf16 (16 bits of it count); halves hold 11 bits of it.  Whatever stands behind the length must not meet a
+          // zero probability (0 * NaN is NaN): the values there are cleared.
+          auto add_values = [&](auto pair) {
+            constexpr bool PAIR = decltype(pair)::value;
+#pragma unroll
+            for (int j = 0; j < BLOCKS; ++j) {
+              uint32_t ph0[NT], ph1[NT], pl0[NT], pl1[NT];
+#pragma unroll
+              for (int n = 0; n < NT; ++n) {
+                const float* x = s[j][n];
+                if constexpr (!PAIR) {
+                  ph0[n] = transpose8x8(pack_f16(x[0], x[1]));
+                  ph1[n] = transpose8x8(pack_f16(x[2], x[3]));
+                } else {
+                  const uint32_t a = pack_bf16(x[0], x[1]), c = pack_bf16(x[2], x[3]);
+                  const float2 fa = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&a));
+                  const float2 fc = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&c));
+                  ph0[n] = transpose8x8(a);
+                  ph1[n] = transpose8x8(c);
+                  pl0[n] = transpose8x8(pack_bf16(x[0] - fa.x, x[1] - fa.y));
+                  pl1[n] = transpose8x8(pack_bf16(x[2] - fc.x, x[3] - fc.y));
+                }
+              }
+              const uint32_t keep0 = (2 * tq < valid[j] ? 0xffffu : 0u) | (2 * tq + 1 < valid[j] ? 0xffff0000u : 0u);
+              const uint32_t keep1 = (2 * tq + 8 < valid[j] ? 0xffffu : 0u) | (2 * tq + 9 < valid[j] ? 0xffff0000u : 0u);
+              if constexpr (!E4M3) {
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                  uint32_t a[4];                                      // rows d = 16 k + gq, + 8; columns = positions
+                  ldmatrix4_trans(vb + swizzled(vrow + 16 * j, 2 * k + vchunk), a);
+                  a[0] &= keep0; a[1] &= keep0; a[2] &= keep1; a[3] &= keep1;
+#pragma unroll
+                  for (int n = 0; n < NT; ++n) {
+                    mma16816<false>(o[n][k], a[0], a[1], a[2], a[3], ph0[n], ph1[n]);
+                    mma16816<false>(o[n][k], a[0], a[1], a[2], a[3], pl0[n], pl1[n]);
+                  }
+                }
+              } else {
+#pragma unroll
+                for (int k = 0; k < KS; k += 2) {
+                  // a transposed 8 x 8 of byte pairs: this lane has dimensions 2 gq, 2 gq + 1 of positions 2 tq, 2 tq + 1 (and + 8)
+                  uint32_t a[4];
+                  ldmatrix4_trans(vb + swizzled(vrow + 16 * j, k + vchunk), a);
+#pragma unroll
+                  for (int i = 0; i < 2; ++i) {
+                    const uint32_t x = __byte_perm(a[2 * i] & keep0, 0, 0x3120), y = __byte_perm(a[2 * i + 1] & keep1, 0, 0x3120);
+                    uint32_t a0 = e4m3x2_to_f16x2(x & 0xffffu), a1 = e4m3x2_to_f16x2(x >> 16);
+                    uint32_t a2 = e4m3x2_to_f16x2(y & 0xffffu), a3 = e4m3x2_to_f16x2(y >> 16);
+                    if constexpr (PAIR) {
+                      a0 = f16x2_to_bf16x2(a0); a1 = f16x2_to_bf16x2(a1); a2 = f16x2_to_bf16x2(a2); a3 = f16x2_to_bf16x2(a3);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                      mma16816<!PAIR>(o[n][k + i], a0, a1, a2, a3, ph0[n], ph1[n]);
+                      if constexpr (PAIR) mma16816<false>(o[n][k + i], a0, a1, a2, a3, pl0[n], pl1[n]);
+                    }
+                  }
+                }
+              }
+            }
+          };
+          // one vote for both rare things: outputs to be scaled down, scales too far apart
+          bool added = false;
+          if (__any_sync(0xffffffffu, moved || spread)) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
               for (int k = 0; k < KS; ++k) {
                 o[n][k][0] *= alpha[n][0]; o[n][k][1] *= alpha[n][1]; o[n][k][2] *= alpha[n][0]; o[n][k][3] *= alpha[n][1];
               }
+            if constexpr (E4M3)
+              if (__any_sync(0xffffffffu, spread)) {
+                add_values(std::true_type());
+                added = true;
+              }
           }
-          // ---- O^T += V^T P^T.  P as the B operand: 8 x 8 transposes of the accumulator's pairs.  bf16: a probability is
-          // split into two bf16 (16 bits of it count); halves (e4m3) hold 11 bits of it.  Whatever stands behind the length
-          // must not meet a zero probability (0 * NaN is NaN): the values there are cleared.
-#pragma unroll
-          for (int j = 0; j < BLOCKS; ++j) {
-            uint32_t ph0[NT], ph1[NT], pl0[NT], pl1[NT];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              const float* x = s[j][n];
-              if constexpr (E4M3) {
-                ph0[n] = transpose8x8(pack_f16(x[0], x[1]));
-                ph1[n] = transpose8x8(pack_f16(x[2], x[3]));
-              } else {
-                const uint32_t a = pack_bf16(x[0], x[1]), c = pack_bf16(x[2], x[3]);
-                const float2 fa = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&a));
-                const float2 fc = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&c));
-                ph0[n] = transpose8x8(a);
-                ph1[n] = transpose8x8(c);
-                pl0[n] = transpose8x8(pack_bf16(x[0] - fa.x, x[1] - fa.y));
-                pl1[n] = transpose8x8(pack_bf16(x[2] - fc.x, x[3] - fc.y));
-              }
-            }
-            const uint32_t keep0 = (2 * tq < valid[j] ? 0xffffu : 0u) | (2 * tq + 1 < valid[j] ? 0xffff0000u : 0u);
-            const uint32_t keep1 = (2 * tq + 8 < valid[j] ? 0xffffu : 0u) | (2 * tq + 9 < valid[j] ? 0xffff0000u : 0u);
-            if constexpr (!E4M3) {
-#pragma unroll
-              for (int k = 0; k < KS; ++k) {
-                uint32_t a[4];                                        // rows d = 16 k + gq, + 8; columns = positions
-                ldmatrix4_trans(vb + swizzled(vrow + 16 * j, 2 * k + vchunk), a);
-                a[0] &= keep0; a[1] &= keep0; a[2] &= keep1; a[3] &= keep1;
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                  mma16816<false>(o[n][k], a[0], a[1], a[2], a[3], ph0[n], ph1[n]);
-                  mma16816<false>(o[n][k], a[0], a[1], a[2], a[3], pl0[n], pl1[n]);
-                }
-              }
-            } else {
-#pragma unroll
-              for (int k = 0; k < KS; k += 2) {
-                // a transposed 8 x 8 of byte pairs: this lane has dimensions 2 gq, 2 gq + 1 of positions 2 tq, 2 tq + 1 (and + 8)
-                uint32_t a[4];
-                ldmatrix4_trans(vb + swizzled(vrow + 16 * j, k + vchunk), a);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                  const uint32_t x = __byte_perm(a[2 * i] & keep0, 0, 0x3120), y = __byte_perm(a[2 * i + 1] & keep1, 0, 0x3120);
-                  const uint32_t a0 = e4m3x2_to_f16x2(x & 0xffffu), a1 = e4m3x2_to_f16x2(x >> 16);
-                  const uint32_t a2 = e4m3x2_to_f16x2(y & 0xffffu), a3 = e4m3x2_to_f16x2(y >> 16);
-#pragma unroll
-                  for (int n = 0; n < NT; ++n) mma16816<true>(o[n][k + i], a0, a1, a2, a3, ph0[n], ph1[n]);
-                }
-              }
-            }
-          }
+          if (!added) add_values(std::bool_constant<!E4M3>());
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(empty(st));
       }
 
       // ---- this warp's result
+      if constexpr (E4M3) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[n][k][i] *= 1.f / 32768.f;       // 2^-WEIGHT_SHIFT
+      }
       const int live = heads_of(p);
 #pragma unroll
       for (int n = 0; n < NT; ++n)

@@ -423,6 +423,50 @@ def test_attention_peaked_and_far_apart_scores(B, e4m3):
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("heads,n", [(6, 150), (24, 150), (6, 9000), (24, 9000)])
+def test_attention_large_values_in_one_dimension(B, heads, n, e4m3):
+    """Live rows of values with one large dimension (and zeros beside it) among ordinary rows, at equal, higher and lower scores:
+    the other dimensions, to which the large rows give nothing, have to be right on their own.  A weight has 11 bits or more down
+    to 2^-21 of the largest probability, whatever the rows' scales are, and is off by 2^-32 of it at most below."""
+    import torch
+    kvh, page, d = 2, 32, 128
+    sizes = [2.0 ** p for p in (3, 9, 15, 21, 40, 90)]
+    gaps = [0.0, 8.0, -8.0]                                  # natural logarithm of a large row's weight over an ordinary one's
+    cases = [(a, g) for a in sizes for g in gaps]
+    rng = np.random.default_rng(heads + n)
+    n_seq = len(cases)
+    c = Cache(rng, n_seq, (n + page - 1) // page, kvh, page, d, e4m3)
+    q = np.zeros((n_seq, heads, d))
+    q[:, :, 0] = 16.0
+    q[:, :, 1:] = rng.standard_normal((n_seq, heads, d - 1)) * 0.25
+    x = np.empty((n_seq, n, 2, kvh, d))
+    x[:, :, 0] = rng.standard_normal((n_seq, n, kvh, d)) * 0.25
+    x[:, :, 1] = rng.standard_normal((n_seq, n, kvh, d))
+    x[:, :, 0, :, 0] = 0.0
+    for s, (size, gap) in enumerate(cases):
+        at = np.arange(5, n, 47)                             # in every warp's part of a tile, now and then
+        x[s, at, 0, :, 0] = gap * math.sqrt(d) / 16
+        x[s, at, 1] = 0.0
+        x[s, at, 1, :, 3] = 448.0 * size
+    for s in range(n_seq):
+        B.et_kv_append(c.data, c.scale, bf16(x[s].reshape(n, -1)), 0, c.table[s:s + 1], i32([0]), i32([0, n]))
+    qt = bf16(q.reshape(n_seq, -1))
+    out, lse, status = run_attention(B, qt, heads, c, [n] * n_seq)
+    assert status == 0
+    values, qs = c.values(), f64(qt).reshape(n_seq, heads, d)
+    for s, case in enumerate(cases):
+        k, v = c.rows(s, 0, n, values)
+        want, wl, mass, size = attention_reference(qs[s], k, v)
+        drift = d * 2.0 ** -23 * size + 2.0 ** -20
+        top = np.exp((np.einsum("hd,hnd->hn", qs[s], np.repeat(k, heads // kvh, 0)) / math.sqrt(d)).max(-1) - wl)   # largest probability
+        below = 2.0 ** -32 * top[:, None] * np.repeat(np.abs(v).sum(1), heads // kvh, 0)
+        tol = BF16 * np.abs(want) + (2.0 ** -11 + 2 * drift + n / 64 * 2.0 ** -23)[:, None] * mass + below + 1e-30
+        off = np.abs(f64(out[s]).reshape(heads, d) - want) / tol
+        assert (off <= 1).all(), f"size and gap {case}: off by {off.max():.3g} of the tolerance in dimension {off.max(0).argmax()}"
+        assert (np.abs(f64(lse[s]) - wl) <= drift + n / 64 * 2.0 ** -23 + 2.0 ** -22 * np.abs(wl)).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
 def test_attention_ignores_what_stands_behind_the_length(B, e4m3):
     """NaN, infinities and the largest numbers behind a sequence's end (in its last page and on the pages after it), and NaN on
     the pages that no table names, change nothing, bit by bit."""
