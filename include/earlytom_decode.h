@@ -87,7 +87,8 @@ ET_API et_status et_kv_read(const et_kv_cache* cache, void* out_dev, long long r
  * out bf16 [n_seq][heads * head_dim]; lse_dev fp32 [n_seq][heads] (may be NULL): natural logarithm of the sum of
  * exponentials.  len_dev [n_seq]; a length of 0 or less gives zeros and -infinity.  Positions behind max_pages * page_size
  * and on pages that are not in the cache are left out (see status_dev).  Whatever stands behind a sequence's length, NaN
- * included, has no influence.
+ * included, has no influence.  An infinite value is its column's result, the other columns keep theirs; below 2^-100 of the
+ * largest weight it may make a NaN of its column instead (0 * infinity).
  * workspace_dev: ET_PAGED_WORKSPACE bytes, 16-byte aligned, contents neither needed nor kept; one call at a time may use
  * it (calls, captured or not, that can run at the same time need one each). */
 #define ET_PAGED_WORKSPACE (4u << 20)

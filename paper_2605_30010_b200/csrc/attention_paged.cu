@@ -147,6 +147,13 @@ __device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t x) {
 }
 constexpr float WEIGHT_SHIFT = 15.f;           // e4m3: the largest weight is 2^15, halves end at 65504
 constexpr float SCALE_SPAN = 8.f;              // e4m3: binades that a tile's scales may lie low for halves to hold its weights
+// A weight as the sum of two bf16: its upper half, which is cut off and not rounded, and the rest.  The rest is above zero
+// wherever the weight is (by 2^-24 of the weight too large), since an infinite value is multiplied by both, and with a zero or a
+// negative number it would become a NaN or the other infinity.
+__device__ __forceinline__ uint32_t upper_halves(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632); }
+__device__ __forceinline__ float lower_part(float x) {
+  return fmaf(__uint_as_float(__float_as_uint(x) & 0xffff0000u), -(1.f - 0x1p-24f), x);
+}
 // Copies by a converged warp: all lanes execute the call, one elected lane issues.
 __device__ __forceinline__ void arrive_expect_elect(uint32_t bar, uint32_t bytes) {
   asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
@@ -681,13 +688,10 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                   ph0[n] = transpose8x8(pack_f16(x[0], x[1]));
                   ph1[n] = transpose8x8(pack_f16(x[2], x[3]));
                 } else {
-                  const uint32_t a = pack_bf16(x[0], x[1]), c = pack_bf16(x[2], x[3]);
-                  const float2 fa = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&a));
-                  const float2 fc = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&c));
-                  ph0[n] = transpose8x8(a);
-                  ph1[n] = transpose8x8(c);
-                  pl0[n] = transpose8x8(pack_bf16(x[0] - fa.x, x[1] - fa.y));
-                  pl1[n] = transpose8x8(pack_bf16(x[2] - fc.x, x[3] - fc.y));
+                  ph0[n] = transpose8x8(upper_halves(x[0], x[1]));
+                  ph1[n] = transpose8x8(upper_halves(x[2], x[3]));
+                  pl0[n] = transpose8x8(pack_bf16(lower_part(x[0]), lower_part(x[1])));
+                  pl1[n] = transpose8x8(pack_bf16(lower_part(x[2]), lower_part(x[3])));
                 }
               }
               const uint32_t keep0 = (2 * tq < valid[j] ? 0xffffu : 0u) | (2 * tq + 1 < valid[j] ? 0xffff0000u : 0u);

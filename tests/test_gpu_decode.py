@@ -504,6 +504,41 @@ def test_attention_nan_in_a_live_place_is_seen(B, e4m3):
     assert torch.isnan(out[1, 1].float()).all() and torch.isnan(lse[1, 2:]).all()
 
 
+@pytest.mark.parametrize("heads,lens", [(6, [90, 150, 33]), (24, [90, 150, 33]), (6, [9000, 150, 4001]), (24, [9000, 150, 4001])])
+def test_attention_infinite_values(B, heads, lens):
+    """An infinity among a column's live values is that column's result, both signs or a NaN make it NaN, wherever they stand: at the
+    largest weight, at ordinary ones, at one of 2^-80; the other columns keep their bits."""
+    import torch
+    kvh, page, d = 2, 32, 128
+    rng = np.random.default_rng(heads + lens[0])
+    c = Cache(rng, len(lens), (max(lens) + page - 1) // page, kvh, page, d, False)
+    table = c.table.cpu().numpy()
+    q = rng.standard_normal((len(lens), heads, d))
+    q[:, :, 0] = 8.0
+    c.data[:, 0, :, :, 0] = 0.0
+    c.data[table[0, 40 // page], 0, :, 40 % page, 0] = 64.0                     # sequence 0: position 40 has nearly all of the weight
+    for p in (50, 51):
+        c.data[table[0, p // page], 0, :, p % page, 0] = -14.0                  # and these about 2^-80 of it
+    qt = bf16(q.reshape(len(lens), -1))
+    a = run_attention(B, qt, heads, c, lens)
+    inf, nan = math.inf, math.nan
+    marks = [(0, 3, 40, inf), (0, 4, 7, inf), (0, 5, 50, -inf), (0, 6, 51, inf), (0, 7, 40, -inf), (0, 8, 12, inf), (0, 8, 13, -inf), (0, 9, 40, nan),
+             (0, 10, lens[0] - 1, -inf), (1, 3, 0, inf), (1, 4, 149, -inf), (1, 5, 64, inf), (1, 5, 65, inf), (1, 6, 100, nan), (2, 127, 32, -inf)]
+    want = {}
+    for s, dim, pos, x in marks:
+        assert pos < lens[s]
+        c.data[table[s, pos // page], 1, :, pos % page, dim] = x
+        want[s, dim] = want.get((s, dim), 0.0) + x
+    b = run_attention(B, qt, heads, c, lens)
+    got, plain = b[0].view(len(lens), heads, d), a[0].view(len(lens), heads, d)
+    for (s, dim), x in want.items():
+        assert torch.isnan(got[s, :, dim].float()).all() if x != x else (got[s, :, dim] == x).all(), (s, dim, x, got[s, :, dim].tolist())
+    keep = torch.ones_like(got, dtype=torch.bool)
+    for s, dim in want:
+        keep[s, :, dim] = False
+    assert torch.equal(got[keep], plain[keep]) and torch.equal(a[1], b[1]) and torch.isfinite(plain.float()).all()
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
 def test_attention_over_bad_pages_and_long_lengths(B, e4m3):
     """Pages that are not in the cache count as absent, lengths behind the table as the table's end; both are reported."""
