@@ -117,7 +117,7 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
       const int start = r.start[s];
       const long long n = r.offsets ? max(0, r.offsets[s + 1] - r.offsets[s]) : 1;
       const long long cap = (long long)r.max_pages << c.page_shift;
-      new_len[s] = start < 0 ? start : (int)min((long long)start + n, max(cap, (long long)start));
+      new_len[s] = start < 0 ? start : (int)min(start + n, cap);
     }
   }
 

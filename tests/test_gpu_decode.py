@@ -272,6 +272,23 @@ def test_rows_that_cannot_be_placed_are_skipped(B, e4m3):
             assert np.array_equal(f64(out[s]), c.rows(s, start[s], 1).reshape(-1))
 
 
+def test_new_lengths_stay_within_the_table(B):
+    """new_len is never more than the table's pages hold, also where a sequence started behind them; a negative start stays."""
+    rng = np.random.default_rng(10)
+    kvh, page, d = 1, 16, 64
+    starts = [33, 32, 31, 2 ** 31 - 1, 40, -5, 2 ** 31 - 3, 0]
+    counts = [1, 2, 4, 3, 0, 1, 3, 2]
+    c = Cache(rng, len(starts), 2, kvh, page, d, False)
+    rows = bf16(rng.standard_normal((sum(counts), 2 * kvh * d)))
+    new, status = i32([-9] * len(starts)), i32([0])
+    B.et_kv_append(c.data, None, rows, 0, c.table, i32(starts), i32(np.concatenate([[0], np.cumsum(counts)])), new_len=new, status=status)
+    assert new.tolist() == [32, 32, 32, 32, 32, -5, 32, 2] and status.item() == B.ET_PAGED_CAPACITY
+    n = len(starts)
+    new.fill_(-9)
+    B.et_kv_append(c.data, None, rows[:n], 0, c.table, i32(starts), new_len=new)          # one row for each
+    assert new.tolist() == [32, 32, 32, 32, 32, -5, 32, 1]
+
+
 # ---- attention --------------------------------------------------------------------------------------------------------
 
 def attention_reference(q, k, v):
