@@ -56,7 +56,8 @@ typedef struct {
  * has in the cache; a negative one marks a slot that is not in use.  block_table_dev [n_seq][max_pages]: page of positions
  * j * page_size .. (j + 1) * page_size - 1.  Padding, slots not in use and rows that cannot be placed (see status_dev)
  * are skipped: nothing is written for them.  A page that rows of one call go to must belong to one sequence only and stand
- * in its table once; where it does not, those rows' contents are unspecified.
+ * in its table once; where it does not, those rows' contents are unspecified.  Offsets that are not as said put no row outside
+ * the cache, but may put it at a wrong position of it; one behind `rows` counts as `rows`.
  *
  * theta > 1: Q and K are turned as et_rope does it, by the row's position; the turned Q goes to q_out_dev (bf16
  * [rows][heads * head_dim], dense, not overlapping qkv; may be NULL with heads = 0 only).  theta = 0: nothing is turned

@@ -28,7 +28,7 @@ struct Places {
         // the last sequence whose offset is not behind the row; outside its run the row is padding
         int lo = 0, hi = r.n_seq;
         while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
+          const int mid = lo + ((hi - lo) >> 1);
           if (r.offsets[mid] <= row) lo = mid; else hi = mid;
         }
         s = lo;
@@ -40,7 +40,7 @@ struct Places {
       page_of = -1;
     }
     if (row < first || row >= behind || start < 0) return false;
-    pos = (long long)start + (row - first);
+    pos = (long long)start + row - first;                // 64 bits and not negative, whatever the offsets hold
     const int column = (int)(pos >> c.page_shift);
     if (column != page_of) {
       int unused;
@@ -113,11 +113,13 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
 
   begin_after_previous();
   if (new_len && blockIdx.x == 0) {
-    for (int s = threadIdx.x; s < r.n_seq; s += THREADS) {
+    for (unsigned s = threadIdx.x; s < (unsigned)r.n_seq; s += THREADS) {
       const int start = r.start[s];
-      const long long n = r.offsets ? max(0, r.offsets[s + 1] - r.offsets[s]) : 1;
+      // rows that the call has: an offset that is none of theirs counts as the first or as the end
+      auto row_at = [&](unsigned i) { return min(max(r.offsets[i], 0), r.rows); };
+      const int n = r.offsets ? max(0, row_at(s + 1) - row_at(s)) : 1;
       const long long cap = (long long)r.max_pages << c.page_shift;
-      new_len[s] = start < 0 ? start : (int)min(start + n, cap);
+      new_len[s] = start < 0 ? start : (int)min((long long)start + n, cap);
     }
   }
 

@@ -289,6 +289,36 @@ def test_new_lengths_stay_within_the_table(B):
     assert new.tolist() == [32, 32, 32, 32, 32, -5, 32, 1]
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_offsets_that_do_not_fit_write_nothing_outside(B, e4m3):
+    """Offsets far below zero (a row's distance from them passes 32 bits), falling ones and ones behind the rows: nothing is placed
+    where no row belongs, and new lengths count only rows that the call has."""
+    import torch
+    rng = np.random.default_rng(11)
+    kvh, page, d, rows = 1, 16, 64, 6
+    c = Cache(rng, 2, 2, kvh, page, d, e4m3)
+    x = bf16(rng.standard_normal((rows, 2 * kvh * d)))
+    low = -2 ** 31
+    for offsets, start, placed, lengths, code in (
+            ([low, low + 1, 6], [0, 3], [], [0, 9], B.ET_PAGED_CAPACITY),       # rows stand 2^31 and more behind the second offset
+            ([low, 6, 6], [20, 0], [], [26, 0], B.ET_PAGED_CAPACITY),
+            ([0, 6, 2], [4, 30], [(0, 4 + i) for i in range(6)], [10, 30], 0),
+            ([0, 4, 2 ** 31 - 1], [1, 2], [(0, 1 + i) for i in range(4)] + [(1, 2), (1, 3)], [5, 4], 0),
+            ([9, 12, 15], [1, 2], [], [1, 2], 0)):
+        before, _ = c.bytes()
+        new, status = i32([-9, -9]), i32([0])
+        B.et_kv_append(c.data, c.scale, x, 0, c.table, i32(start), i32(offsets), new_len=new, status=status)
+        after, _ = c.bytes()
+        changed = {tuple(i) for i in (before != after).any(-1).any(2).any(1).nonzero().tolist()}
+        assert changed == {(c.table[s, p // page].item(), p % page) for s, p in placed}
+        assert new.tolist() == lengths and status.item() == code
+        out = torch.full((rows, 2 * kvh * d), 5.0, dtype=torch.bfloat16, device="cuda")
+        status.zero_()
+        B.et_kv_read(c.data, c.scale, c.table, i32(start), rows, i32(offsets), out, status)
+        assert ((out == 5.0).all(1).sum().item() == rows - len(placed)) and status.item() == code
+        c.data.view(torch.uint8 if e4m3 else torch.int16).copy_(before)
+
+
 # ---- attention --------------------------------------------------------------------------------------------------------
 
 def attention_reference(q, k, v):
