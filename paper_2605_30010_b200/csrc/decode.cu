@@ -60,7 +60,12 @@ const RopeTurns& rope_turns(float theta, int head_dim) {
   return t;
 }
 
-et_status launched() { return cudaGetLastError() == cudaSuccess ? ET_OK : ET_ERR_CUDA; }
+// A launch's own result: an error that an earlier call left behind is not this call's, and none is left for a later one.
+et_status launched(cudaError_t e) {
+  if (e == cudaSuccess) return ET_OK;
+  cudaGetLastError();
+  return ET_ERR_CUDA;
+}
 
 }  // namespace
 
@@ -82,9 +87,8 @@ et_status et_kv_append(const et_kv_cache* cache, const void* qkv_dev, long long 
   if (new_len_dev && new_len_dev == start_dev) return ET_ERR_INVALID_ARG;
   if (row_stride % 8 != 0 || row_stride < ((long long)heads + 2ll * c.kv_heads) * c.head_dim) return ET_ERR_SHAPE;
   static const RopeTurns none = {};
-  launch_kv_append(c, r, (const bf16*)qkv_dev, row_stride, heads, rotate, rotate ? rope_turns(theta, c.head_dim) : none, (bf16*)q_out_dev,
-                   new_len_dev, (cudaStream_t)cuda_stream);
-  return launched();
+  return launched(launch_kv_append(c, r, (const bf16*)qkv_dev, row_stride, heads, rotate, rotate ? rope_turns(theta, c.head_dim) : none,
+                                   (bf16*)q_out_dev, new_len_dev, (cudaStream_t)cuda_stream));
 }
 
 et_status et_kv_read(const et_kv_cache* cache, void* out_dev, long long row_stride, int rows, const int* block_table_dev, int n_seq,
@@ -97,8 +101,7 @@ et_status et_kv_read(const et_kv_cache* cache, void* out_dev, long long row_stri
   if (!out_dev || !aligned16(out_dev)) return ET_ERR_INVALID_ARG;
   if (c.kv_heads > (1 << 19)) return ET_ERR_SHAPE;
   if (row_stride % 8 != 0 || row_stride < 2ll * c.kv_heads * c.head_dim) return ET_ERR_SHAPE;
-  launch_kv_read(c, r, (bf16*)out_dev, row_stride, (cudaStream_t)cuda_stream);
-  return launched();
+  return launched(launch_kv_read(c, r, (bf16*)out_dev, row_stride, (cudaStream_t)cuda_stream));
 }
 
 et_status et_attention_paged(const et_kv_cache* cache, const void* q_dev, long long q_stride, void* out_dev, float* lse_dev, int n_seq,
@@ -118,7 +121,7 @@ et_status et_attention_paged(const et_kv_cache* cache, const void* q_dev, long l
   if (workspace_bytes < ET_PAGED_WORKSPACE) return ET_ERR_CAPACITY;
   const PagedAttention a{(const bf16*)q_dev, q_stride, (bf16*)out_dev, lse_dev, n_seq, heads, max_pages, block_table_dev, len_dev,
                          (float*)workspace_dev, status_dev};
-  return launch_attention_paged(c, a, (cudaStream_t)cuda_stream) == cudaSuccess ? ET_OK : ET_ERR_CUDA;
+  return launched(launch_attention_paged(c, a, (cudaStream_t)cuda_stream));
 }
 
 et_status et_linear_rows(const void* a_dev, const void* w_dev, const float* bias_dev, void* c_dev, int M, int N, int K, int epilogue,
@@ -127,8 +130,8 @@ et_status et_linear_rows(const void* a_dev, const void* w_dev, const float* bias
   if (epilogue != EPI_STORE && epilogue != EPI_GELU && epilogue != EPI_RESIDUAL && epilogue != EPI_SWIGLU) return ET_ERR_INVALID_ARG;
   if (M < 1 || N < 1 || K < 8 || K % 8 != 0 || (epilogue == EPI_SWIGLU && N % 256 != 0)) return ET_ERR_SHAPE;
   if (M > LINEAR_ROWS_MAX || N > (1 << 24) || K > (1 << 24)) return ET_ERR_CAPACITY;
-  return launch_linear_rows((const bf16*)a_dev, (const bf16*)w_dev, bias_dev, c_dev, M, N, K, epilogue, gelu_tanh, status_dev,
-                            (cudaStream_t)cuda_stream) == cudaSuccess ? ET_OK : ET_ERR_CUDA;
+  return launched(launch_linear_rows((const bf16*)a_dev, (const bf16*)w_dev, bias_dev, c_dev, M, N, K, epilogue, gelu_tanh, status_dev,
+                                     (cudaStream_t)cuda_stream));
 }
 
 }  // extern "C"

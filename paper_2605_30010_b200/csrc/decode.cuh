@@ -24,9 +24,9 @@ struct PagedRows {
 
 struct RopeTurns { unsigned long long f[64]; };   // theta^(-2i/dh) / (2 pi) as a fraction of 2^64
 
-void launch_kv_append(const PagedCache& c, const PagedRows& r, const bf16* qkv, long long row_stride, int heads, bool rotate,
-                      const RopeTurns& turns, bf16* q_out, int* new_len, cudaStream_t s);
-void launch_kv_read(const PagedCache& c, const PagedRows& r, bf16* out, long long row_stride, cudaStream_t s);
+cudaError_t launch_kv_append(const PagedCache& c, const PagedRows& r, const bf16* qkv, long long row_stride, int heads, bool rotate,
+                             const RopeTurns& turns, bf16* q_out, int* new_len, cudaStream_t s);
+cudaError_t launch_kv_read(const PagedCache& c, const PagedRows& r, bf16* out, long long row_stride, cudaStream_t s);
 
 struct PagedAttention {
   const bf16* q;

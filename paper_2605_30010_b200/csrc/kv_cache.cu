@@ -296,12 +296,12 @@ Deal deal_rows(int rows, int steps_row) {
 
 }  // namespace
 
-void launch_kv_append(const PagedCache& c, const PagedRows& r, const bf16* qkv, long long row_stride, int heads, bool rotate,
-                      const RopeTurns& turns, bf16* q_out, int* new_len, cudaStream_t s) {
+cudaError_t launch_kv_append(const PagedCache& c, const PagedRows& r, const bf16* qkv, long long row_stride, int heads, bool rotate,
+                             const RopeTurns& turns, bf16* q_out, int* new_len, cudaStream_t s) {
   ET_COUNT_LAUNCH();
   const Deal d = deal_rows(r.rows, cdiv(((rotate ? heads : 0) + 2 * c.kv_heads) * (c.head_dim / 16), 64));
   Launch l(d.blocks, THREADS, 0, s);
-#define ET_APPEND(D, E, R) cudaLaunchKernelEx(&l.cfg, kv_append_kernel<D, E, R>, qkv, row_stride, heads, c, r, turns, q_out, new_len, d.each, d.parts)
+#define ET_APPEND(D, E, R) return cudaLaunchKernelEx(&l.cfg, kv_append_kernel<D, E, R>, qkv, row_stride, heads, c, r, turns, q_out, new_len, d.each, d.parts)
 #define ET_APPEND_D(D)                                                       \
   do {                                                                       \
     if (c.scale) { if (rotate) ET_APPEND(D, true, true); else ET_APPEND(D, true, false); }   \
@@ -312,11 +312,11 @@ void launch_kv_append(const PagedCache& c, const PagedRows& r, const bf16* qkv, 
 #undef ET_APPEND
 }
 
-void launch_kv_read(const PagedCache& c, const PagedRows& r, bf16* out, long long row_stride, cudaStream_t s) {
+cudaError_t launch_kv_read(const PagedCache& c, const PagedRows& r, bf16* out, long long row_stride, cudaStream_t s) {
   ET_COUNT_LAUNCH();
   const Deal d = deal_rows(r.rows, cdiv(2 * c.kv_heads * c.head_dim / (c.scale ? 16 : 8), 128));
   Launch l(d.blocks, THREADS, 0, s);
-#define ET_READ(D, E) cudaLaunchKernelEx(&l.cfg, kv_read_kernel<D, E>, out, row_stride, c, r, d.each, d.parts)
+#define ET_READ(D, E) return cudaLaunchKernelEx(&l.cfg, kv_read_kernel<D, E>, out, row_stride, c, r, d.each, d.parts)
   if (c.head_dim == 64) { if (c.scale) ET_READ(64, true); else ET_READ(64, false); }
   else { if (c.scale) ET_READ(128, true); else ET_READ(128, false); }
 #undef ET_READ

@@ -735,6 +735,35 @@ def test_calls_on_a_stream_of_their_own(B):
     assert (rows[60:] == 0).all()
 
 
+def test_calls_report_their_own_errors_only(B):
+    """A model that does not fit on the card is refused (an allocation fails); the decode calls after it run and say so."""
+    import torch
+    rng = np.random.default_rng(42)
+    heads, kvh, page, d = 4, 2, 16, 64
+    c = Cache(rng, 2, 2, kvh, page, d, False)
+    qkv, lens, new = bf16(rng.standard_normal((2, (heads + 2 * kvh) * d))), i32([3, 17]), i32([0, 0])
+    a, w = bf16(rng.standard_normal((2, 64))), bf16(rng.standard_normal((64, 64)))
+
+    def step():
+        q = B.et_kv_append(c.data, None, qkv, heads, c.table, lens, theta=1e4, new_len=new)
+        return q, B.et_kv_read(c.data, None, c.table, lens, 2), B.et_attention_paged(q, heads, c.data, None, c.table, new), B.et_linear_rows(a, w)
+
+    want = step()
+    H, V = 4096, 1 << 27                                     # staging one matrix would take 2^41 bytes
+    cfg = B.et_llm_config(1152, H, 1, 32, 8, 128, 4096, V, 1e-6, 1e4, 1, 256, 0)
+    qkv_dim, m = (32 + 16) * 128, 4096
+    count = V * H + 1152 * H + H + H * H + H + (H + H * qkv_dim + qkv_dim + 4096 * H + H + H * 2 * m + m * H) + H + H * V
+    data = (B.C.c_float * 4)()                               # nothing of it is read
+    for again in range(2):
+        handle = B.C.c_void_p()
+        weights = B.et_llm_weights(B.C.cast(data, B.C.c_void_p), count, 0)
+        assert B.lib().et_llm_create(B.C.byref(cfg), B.C.byref(weights), B.C.byref(handle)) == 4       # ET_ERR_OOM
+        got = step()
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+    x, y = torch.ones((1, 64), device="cuda"), torch.empty((1, 64), dtype=torch.bfloat16, device="cuda")
+    B.lib().et_rmsnorm(x.data_ptr(), x.data_ptr(), 1e-6, y.data_ptr(), 1, 64, torch.cuda.current_stream().cuda_stream)    # takes the error with it
+
+
 # ---- dense layer for few rows -----------------------------------------------------------------------------------------
 
 def linear_reference(a, w, bias, epilogue, gelu_tanh, c0):
