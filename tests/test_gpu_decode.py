@@ -815,6 +815,24 @@ def test_linear_rows(B, M, K, N, epilogue, gelu_tanh, with_bias):
     assert (guard[M * outs:] == 3.0).all()
 
 
+@pytest.mark.parametrize("M,K,N,chain", [(5, 18944, 3584, 4), (32, 18944, 3584, 4), (13, 18944, 1100, 4), (1, 3584, 37888, 4), (1, 3584, 4608, 16),
+                                         (8, 18944, 256, 20), (1, 65536, 8, 64)])
+def test_linear_rows_long_sums(B, M, K, N, chain):
+    """Sums of positive products, where what the tensor core cuts off adds up: at most 2^-23 of a partial sum for each instruction of a
+    chain.  With many weights a chain is one stage of four instructions; with few it is a warp's share of K, `chain` instructions long.
+    Partial sums are added in fp32, whose rounding errors have no sign: in the mean over the outputs they stay below 2^-24."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(K + N + M)
+    a, w = (torch.randn((n, K), device="cuda", generator=gen).abs().to(torch.bfloat16) for n in (M, N))
+    c = torch.zeros((M, N), device="cuda")
+    B.et_linear_rows(a, w, None, 2, c=c)
+    want = a.double() @ w.double().T
+    off = (c.double() - want) / want
+    # worst case of the additions: one rounding for each of the K / 64 steps of a rank, and those of the ranks' and warps' sums
+    assert off.abs().max().item() <= chain * 2.0 ** -23 + (K / 64 + 16) * 2.0 ** -24
+    assert abs(off.mean().item()) <= chain * 2.0 ** -23 + 2.0 ** -24, off.mean().item()
+
+
 @pytest.mark.parametrize("epilogue", [0, 2])
 @pytest.mark.parametrize("M,K,N", [(3, 1000, 40007), (12, 136, 46001), (32, 72, 50002), (17, 1016, 12003), (32, 264, 22010)])
 def test_linear_rows_in_blocks_of_fewer_rows(B, M, K, N, epilogue):
