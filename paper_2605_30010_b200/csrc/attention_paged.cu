@@ -56,6 +56,10 @@ static_assert(COMPUTE_WARPS * COMPUTE_REGS + COPY_WARPS * COPY_REGS <= (COMPUTE_
 // A group takes an item of up to so many tiles alone, where a CTA has several: 72 sequences of 250, 16 heads of 128, e4m3:
 // 29.8 -> 18.3 us, 56 of 320 29.9 -> 21.5 us; with 32 a batch of long and short ones gets slower (55.8 -> 60.2 us).
 constexpr int ALONE_TILES = 8;
+// The tensor core cuts off what does not fit an accumulator, which adds up over long sums (0.0016 of positive outputs after a
+// million positions in a CTA).  So a piece has at most this many tiles, a quarter for each group; what is longer becomes several
+// pieces, whose outputs are added in fp32.
+constexpr int PIECE_TILES = 256 * GROUPS;
 constexpr int MAX_CTAS = 148;
 constexpr int PAD = 4;                         // floats between heads of the joining buffer: no bank conflicts
 constexpr int SMEM_LIMIT = 232448 - 512;       // 227 KB, less the static part
@@ -196,13 +200,15 @@ struct Walk {
   int s, part, unit;               // next unit: sequence, key / value head x head tile, unit of the item
   int len;                         // of the sequence
   bool opened;                     // a piece has been given out
+  bool cut, cut_first, cut_opens;  // the last one was ended for its length; it was `first`, `opens`
 };
 
 struct Piece {
   int s, part, len, t0, t1;        // tiles t0 .. t1 - 1
   int units, units_end;            // the item's units, and those up to this piece's end
-  bool first, last;                // contains the item's first, last tile
-  bool opens;                      // is the first piece of its run
+  bool first, last;                // contains the item's first, last tile (first: or goes on from a piece that does)
+  bool opens;                      // is the first piece of its run (or goes on from it)
+  bool goes_on, more;              // goes on from the piece before; the next piece goes on from it
 };
 
 // Which of a piece's tiles a group takes: every GROUPS-th one, or all or none of an item that is short next to the run (a
@@ -212,7 +218,7 @@ struct Deal { int t, step; bool alone; };
 __device__ __forceinline__ Deal deal(const Piece& p, bool may, int chunk, int group, int& turn) {
   Deal d;
   const int n = p.t1 - p.t0;
-  d.alone = may && n <= ALONE_TILES && p.units * GROUPS <= chunk;
+  d.alone = may && n <= ALONE_TILES && p.units * GROUPS <= chunk && !p.goes_on;
   const int behind = (group - turn) & (GROUPS - 1);
   d.t = d.alone ? (behind == 0 ? p.t0 : p.t1) : p.t0 + behind;
   d.step = d.alone ? 1 : GROUPS;
@@ -225,20 +231,28 @@ __device__ __forceinline__ bool next_piece(const Args& g, int parts_all, Walk& w
   while (w.left > 0) {
     const int units = units_of<C>(g, w.len);
     if (units > 0) {
-      const int n = min(w.left, units - w.unit), end = w.unit + n;
-      p.s = w.s; p.part = w.part; p.len = w.len; p.units = units; p.units_end = end;
+      int end = w.unit + min(w.left, units - w.unit);
+      p.s = w.s; p.part = w.part; p.len = w.len; p.units = units;
       const int tiles = tiles_of(w.len), cost = cost_of<C>(tiles);
       p.t0 = g.whole ? 0 : max(w.unit - cost, 0);
       p.t1 = g.whole ? tiles : max(end - cost, 0);
-      p.first = p.t0 == 0; p.last = end == units;
-      w.left -= n; w.unit = end;
+      p.more = p.t1 - p.t0 > PIECE_TILES;
+      if (p.more) { p.t1 = p.t0 + PIECE_TILES; end = p.t1 + cost; }        // (an item that is not cut has no such length)
+      p.goes_on = w.cut;
+      p.first = w.cut ? w.cut_first : p.t0 == 0;
+      p.last = end == units; p.units_end = end;
+      w.left -= end - w.unit; w.unit = end;
       if (end == units) { w.unit = 0; ++w.part; }
     }
     if (units == 0 || w.part == parts_all) {                      // on to the next sequence
       w.part = 0;
       if (++w.s >= g.a.n_seq) w.left = 0; else if (w.left > 0) w.len = clamped_len(g, w.s);
     }
-    if (units > 0 && p.t1 > p.t0) { p.opens = !w.opened; w.opened = true; return true; }   // else the run ended in front of the item's first tile
+    if (units > 0 && p.t1 > p.t0) {                               // else the run ended in front of the item's first tile
+      p.opens = w.cut ? w.cut_opens : !w.opened;
+      w.opened = true; w.cut = p.more; w.cut_first = p.first; w.cut_opens = p.opens;
+      return true;
+    }
   }
   return false;
 }
@@ -312,7 +326,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     }
     __syncthreads();
     walk.left = min(chunk, total - begin);
-    walk.s = walk_s[0]; walk.part = walk_s[1]; walk.unit = walk_s[2]; walk.len = walk_s[3]; walk.opened = false;
+    walk.s = walk_s[0]; walk.part = walk_s[1]; walk.unit = walk_s[2]; walk.len = walk_s[3]; walk.opened = walk.cut = false;
   }
 
   bool ok = true;
@@ -435,7 +449,18 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     const float softmax_scale = 1.4426950408889634f * (DH == 128 ? 0.08838834764831845f : 0.125f);   // log2(e) / sqrt(DH)
 
     // Four values of a head's output (not yet divided), its maximum and sum: to the output, or to the workspace if others follow.
-    auto put = [&](const Piece& p, int h, int d, float4 acc, float top, float sum) {
+    // A piece that goes on adds what the one before has left there; a head's lanes are the same ones of one warp then (`lanes`).
+    auto put = [&](const Piece& p, int h, int d, float4 acc, float top, float sum, unsigned lanes) {
+      if (p.goes_on) {
+        const float* const part = g.a.workspace + SLOT0 + (size_t)(2 * b + (p.opens ? 0 : 1)) * Slot<DH, NT>::FLOATS;
+        const float4 x = *reinterpret_cast<const float4*>(part + h * DH + d);
+        const float top0 = part[C::HEADS * DH + 2 * h], sum0 = part[C::HEADS * DH + 2 * h + 1];
+        __syncwarp(lanes);                                           // read by all before one of them writes
+        const float now = fmaxf(top0, top), ref = now == -INFINITY ? 0.f : now, f0 = exp2_fast(top0 - ref), f = exp2_fast(top - ref);
+        acc = make_float4(x.x * f0 + acc.x * f, x.y * f0 + acc.y * f, x.z * f0 + acc.z * f, x.w * f0 + acc.w * f);
+        sum = sum0 * f0 + sum * f;
+        top = now;
+      }
       if (p.first && p.last) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;              // every page absent: zeros
         const size_t at = (size_t)p.s * g.a.heads + (p.part / g.parts) * g.group + (p.part % g.parts) * C::HEADS + h;
@@ -473,7 +498,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
             acc.x += x.x * fo; acc.y += x.y * fo; acc.z += x.z * fo; acc.w += x.w * fo;
           }
         }
-        put(p, h, d, acc, top, sum);
+        put(p, h, d, acc, top, sum, live * (DH / 4) - (e - lane) >= 32 ? 0xffffffffu : 0xffffu);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(o_empty(buf));
@@ -484,7 +509,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     uint32_t phase = 0, q_phase = 0;
     Piece p, before;
     while (next_piece<C>(g, parts_all, walk, p)) {
-      if (p.first && !p.last) {
+      if (p.first && !p.last && !p.more) {
         // the item goes on in the CTAs behind this one, each of which finds it at the start of its run
         const int item0 = begin + chunk - p.units_end;               // this piece ends this CTA's run (whole items are not cut)
         mine = Join{p.s, p.part, (item0 + p.units - 1) / chunk - b + 1, 2 * b + (p.opens ? 0 : 1)};
@@ -821,7 +846,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         group_sync(my_group);
         for (int e = tid % (32 * GROUP_WARPS); ok && e < live * (DH / 4); e += 32 * GROUP_WARPS) {
           const int h = e / (DH / 4), d = (e % (DH / 4)) * 4;
-          put(p, h, d, *reinterpret_cast<const float4*>(pair + h * (DH + PAD) + d), pair_m[h], pair_m[2 * C::HEADS + h]);
+          put(p, h, d, *reinterpret_cast<const float4*>(pair + h * (DH + PAD) + d), pair_m[h], pair_m[2 * C::HEADS + h], 0u);
         }
         continue;
       }

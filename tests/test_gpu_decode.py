@@ -449,6 +449,47 @@ def test_attention_long_runs(B, heads, kvh, page, d, e4m3):
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("heads,n,rising", [(2, 1_000_000, False), (12, 1_000_000, False), (2, 300_000, True), (12, 300_000, True)])
+def test_attention_long_sums(B, heads, n, rising, e4m3):
+    """As many sequences as CTAs, over the same pages, of up to a million positions each and with positive values: the tensor core cuts
+    off what does not fit an accumulator, 2^-23 of it for each of the 1024 instructions (or fewer) after which it starts again from
+    zero.  The values follow the keys, so that the outputs differ by more than their rounding, which vanishes in the mean over
+    3 000 of them (to 1e-4, five times its spread).  rising: scores grow along the cache, by 60 nats in all."""
+    import torch
+    kvh, page, d, n_seq = 1, 128, 128, 148
+    gen = torch.Generator(device="cuda").manual_seed(n + heads)
+    pages = (n + page - 1) // page
+    k = torch.randn((n, d), device="cuda", generator=gen)
+    v = (3 + k + 0.5 * torch.randn((n, d), device="cuda", generator=gen)).clamp(min=0.01) * torch.exp2(torch.arange(d, device="cuda") / d)
+    if rising:
+        k[:, 0] = torch.linspace(-30, 30, n, device="cuda") * math.sqrt(d) / 16
+    rows = torch.cat([k, v], 1).to(torch.bfloat16)
+    data = torch.zeros((pages, 2, kvh, page, d), device="cuda", dtype=torch.float8_e4m3fn if e4m3 else torch.bfloat16)
+    scale = torch.zeros((pages, 2, kvh, page), device="cuda", dtype=torch.uint8) if e4m3 else None
+    table = torch.randperm(pages, device="cuda", generator=gen).to(torch.int32).view(1, -1)
+    B.et_kv_append(data, scale, rows, 0, table, i32([0]), i32([0, n]))
+    k, v = B.et_kv_read(data, scale, table, i32([0]), n, i32([0, n])).double().split(d, 1)
+    q = torch.randn((n_seq, heads, d), device="cuda", generator=gen)
+    if rising:
+        q[:, :, 0] = 16.0
+    q = q.to(torch.bfloat16)
+    lse = torch.empty((n_seq, heads), device="cuda")
+    out = B.et_attention_paged(q.view(n_seq, -1), heads, data, scale, table.expand(n_seq, -1).contiguous(), i32([n] * n_seq), lse=lse)
+    mean = []
+    for s in range(0, n_seq, 13):
+        z = q[s].double() @ k.T / math.sqrt(d)
+        size = (q[s].double().abs() @ k.abs().T).amax(-1) / math.sqrt(d)
+        want = torch.softmax(z, -1) @ v
+        drift = d * 2.0 ** -23 * size + 2.0 ** -20
+        off = (out[s].view(heads, d).double() - want) / want
+        assert (off.abs() <= BF16 + 2.0 ** -11 + 2 * drift.unsqueeze(-1)).all(), f"{off.abs().max().item():.3g}"
+        assert ((lse[s].double() - torch.logsumexp(z, -1)).abs() <= drift + n / 512 * 2.0 ** -24 + 2.0 ** -19).all()
+        mean.append(off)
+    mean = torch.stack(mean).mean().item()
+    assert abs(mean) <= 1024 * 2.0 ** -23 + 1e-4, mean
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
 def test_attention_peaked_and_far_apart_scores(B, e4m3):
     """Scores from one key that takes all to thousands apart, growing and falling along the cache; queries of very different
     sizes; values of very different sizes, the large ones where nothing looks."""
