@@ -33,6 +33,7 @@ using namespace tc;
 constexpr int WARPS = 8, THREADS = 32 * WARPS;  // of the direct kernel
 constexpr int BLOCK_ROWS = 32;                 // its weight rows of a block: two tiles of 16
 constexpr int STEP = 64;                       // k of a warp's step: 128 bytes of each row
+constexpr int SUM_STEPS = 32;                  // steps of a warp that the tensor core sums at most
 constexpr int MAX_CLUSTER = 8;
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -135,7 +136,7 @@ __device__ __forceinline__ void finish(const LinearArgs& g, cg::cluster_group& c
 // read in the same order), so a weight passes from the load to the tensor core without a shuffle.  The next step's weights
 // are loaded before the current ones are used; 16 warps an SM then have 64 KB on their way.
 // ---------------------------------------------------------------------------------------------
-template <int NT, bool WIDE>
+template <int NT, bool WIDE, bool LONG>
 __global__ void __launch_bounds__(THREADS, 2)
 linear_direct_kernel(const LinearArgs g) {
   constexpr int COLS = 8 * NT, LD = COLS + 1;
@@ -180,7 +181,30 @@ linear_direct_kernel(const LinearArgs g) {
   const int stride = STEP * WARPS * ranks;
   int k = STEP * (rank * WARPS + warp);
   load_w(k);
+  // The tensor core truncates where fp32 addition rounds, which adds up over a long chain (1.7e-3 of the result over K = 2^24): LONG
+  // ones go to shared memory every SUM_STEPS steps, and are added there in fp32.  (In every layer that costs a tenth: 1 x 3584 x 4608
+  // 8.4 -> 9.2 us.)
+  auto sum_at = [&](int i, int n, int j) { return red + (warp * ROWS + i * 16 + j * 8 + gq) * LD + n * 8 + 2 * tq; };
+  int steps = 0;
+  auto leave_sums = [&]() {
+    const bool more = LONG && steps > SUM_STEPS;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float* const dst = sum_at(i, n, j);
+          dst[0] = acc[i][n][2 * j] + (more ? dst[0] : 0.f);
+          dst[1] = acc[i][n][2 * j + 1] + (more ? dst[1] : 0.f);
+          if (LONG) acc[i][n][2 * j] = acc[i][n][2 * j + 1] = 0.f;
+        }
+  };
   for (; k < g.K; k += stride) {
+    if (LONG) {
+      if (steps > 0 && steps % SUM_STEPS == 0) leave_sums();
+      ++steps;
+    }
     Vec ab[NT], cur[2][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) load_vec<WIDE, false>(ab[n], ap[n], k, g.K - 16 * tq, live[n]);
@@ -200,15 +224,7 @@ linear_direct_kernel(const LinearArgs g) {
   }
 
   // ---- the warps' sums, then the cluster's
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float* dst = red + (warp * ROWS + i * 16 + j * 8 + gq) * LD + n * 8 + 2 * tq;
-        dst[0] = acc[i][n][2 * j]; dst[1] = acc[i][n][2 * j + 1];
-      }
+  leave_sums();
   __syncthreads();
   float sums[ROWS * COLS / THREADS];
 #pragma unroll
@@ -374,7 +390,11 @@ cudaError_t launch_direct(const LinearArgs& g, cudaStream_t s) {
   const bool wide = g.K % 16 == 0 && ((reinterpret_cast<uintptr_t>(g.a) | reinterpret_cast<uintptr_t>(g.w)) & 31u) == 0;
   Launch l(blocks * ranks, THREADS, 0, s, ranks);
   ET_COUNT_LAUNCH();
-  return wide ? cudaLaunchKernelEx(&l.cfg, linear_direct_kernel<NT, true>, g) : cudaLaunchKernelEx(&l.cfg, linear_direct_kernel<NT, false>, g);
+  if (g.K > STEP * WARPS * ranks * SUM_STEPS)
+    return wide ? cudaLaunchKernelEx(&l.cfg, linear_direct_kernel<NT, true, true>, g)
+                : cudaLaunchKernelEx(&l.cfg, linear_direct_kernel<NT, false, true>, g);
+  return wide ? cudaLaunchKernelEx(&l.cfg, linear_direct_kernel<NT, true, false>, g)
+              : cudaLaunchKernelEx(&l.cfg, linear_direct_kernel<NT, false, false>, g);
 }
 
 template <int NT>

@@ -874,6 +874,12 @@ def test_linear_rows_long_sums(B, M, K, N, chain):
     assert abs(off.mean().item()) <= chain * 2.0 ** -23 + 2.0 ** -24, off.mean().item()
 
 
+@pytest.mark.parametrize("M,K,N", [(1, 1 << 20, 32), (12, 1 << 20, 64), (20, 1 << 18, 70), (31, 1 << 20, 8), (1, 1 << 24, 1), (2, 300_008, 3)])
+def test_linear_rows_longest_sums(B, M, K, N):
+    """Few weight rows as long as can be: chains of at most 128 instructions."""
+    test_linear_rows_long_sums(B, M, K, N, 128)
+
+
 @pytest.mark.parametrize("epilogue", [0, 2])
 @pytest.mark.parametrize("M,K,N", [(3, 1000, 40007), (12, 136, 46001), (32, 72, 50002), (17, 1016, 12003), (32, 264, 22010)])
 def test_linear_rows_in_blocks_of_fewer_rows(B, M, K, N, epilogue):
