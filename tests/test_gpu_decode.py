@@ -195,6 +195,39 @@ def test_append_then_read(B, case, e4m3):
     assert (out[rows:] == 5.0).all() and (out[:, 2 * kvh * d:] == 5.0).all() and status.item() == 0
 
 
+@pytest.mark.parametrize("d,theta,start", [(128, 1e6, 0), (128, 1e4, 900_000), (64, 5e5, 0), (64, 1e4, 77_777)])
+def test_turned_keys_are_exact(B, d, theta, start):
+    """A turned key on its way to e4m3 is off by two fp32 roundings (and 2^-39 of the pair that it comes from): what is stored lies
+    between the conversions of the two ends of that interval, in all of two million values."""
+    n, kvh, heads, page = 4000, 4 if d == 128 else 8, 1, 128
+    rng = np.random.default_rng(d + start)
+    first = start // page
+    max_pages = (start + n + page - 1) // page
+    c = Cache(rng, 1, max_pages - first, kvh, page, d, True)
+    table = i32(np.concatenate([np.zeros(first), c.table.cpu().numpy()[0]])[None])
+    qkv = bf16(rng.standard_normal((n, (heads + 2 * kvh) * d)))
+    status = i32([0])
+    B.et_kv_append(c.data, c.scale, qkv, heads, table, i32([start]), i32([0, n]), theta=theta, status=status)
+    assert status.item() == 0
+    x = f64(qkv).reshape(n, heads + 2 * kvh, d)[:, heads:heads + kvh]
+    pos = np.arange(start, start + n)
+    want = rotate(x, pos, theta)
+    pages, place = table.cpu().numpy()[0][pos // page], pos % page
+    got = c.values()[pages, 0, :, place]
+    e = c.scale.cpu().numpy().astype(int)[pages, 0, :, place] - 127
+    # the reference's angles, up to 2^20, are off by 2^-53 of them for the frequency and as much for the product: 2^-32
+    slack = 2.0 ** -23 * np.abs(want) + 2.0 ** -31 * (np.abs(x) + np.abs(np.roll(x, d // 2, -1)))
+
+    def nearest(y):
+        y = y * np.ldexp(1.0, -e)[..., None]
+        step = np.ldexp(1.0, np.maximum(np.frexp(np.abs(y))[1] - 1, -6) - 3)
+        return np.round(y / step) * step * np.ldexp(1.0, e)[..., None]
+
+    top = np.abs(want).max(-1)
+    assert (top <= 448 * np.ldexp(1.0, e) * (1 + 2.0 ** -22)).all() and (top >= 224 * np.ldexp(1.0, e) * (1 - 2.0 ** -22)).all()
+    assert ((nearest(want - slack) <= got) & (got <= nearest(want + slack))).all()
+
+
 def test_append_with_one_theta_after_another(B):
     """Calls with different bases and head sizes in turn, far positions: each turns by its own angles."""
     import torch
