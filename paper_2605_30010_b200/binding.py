@@ -864,6 +864,8 @@ def et_kv_append(cache, scale, qkv, heads, block_table, start, row_offsets=None,
         _import_torch()
     c, kv_heads, head_dim = _kv_cache(cache, scale)
     n_seq, max_pages = _table(block_table)
+    if qkv.dim() != 2 or heads < 0:
+        _refuse("qkv: bf16 [rows, (heads + 2 * kv_heads) * head_dim], heads >= 0")
     rows = qkv.shape[0]
     s = _launch_on(stream, cache, scale, qkv, block_table, start, row_offsets, q_out, new_len, status)
     stride = _row_stride(qkv, (heads + 2 * kv_heads) * head_dim, "qkv")
@@ -894,10 +896,12 @@ def et_kv_read(cache, scale, block_table, start, rows, row_offsets=None, out=Non
     c, kv_heads, head_dim = _kv_cache(cache, scale)
     n_seq, max_pages = _table(block_table)
     width = 2 * kv_heads * head_dim
+    if rows < 0:
+        _refuse("rows: how many are read")
     if out is None:
         out = _new(_torch.zeros, (rows, width), _torch.bfloat16, cache, stream)
-    elif out.shape[0] != rows:
-        _refuse("out: as many rows as are read")
+    elif out.dim() != 2 or out.shape[0] != rows:
+        _refuse("out: [rows, >= 2 * kv_heads * head_dim], as many rows as are read")
     s = _launch_on(stream, cache, scale, block_table, start, row_offsets, out, status)
     stride = _row_stride(out, width, "out")
     _ints(start, n_seq, "start")
@@ -920,8 +924,8 @@ def et_attention_paged(q, heads, cache, scale, block_table, lens, out=None, lse=
     c, kv_heads, head_dim = _kv_cache(cache, scale)
     n_seq, max_pages = _table(block_table)
     width = heads * head_dim
-    if q.shape[0] != n_seq:
-        _refuse("block_table: a row for each row of q")
+    if q.dim() != 2 or q.shape[0] != n_seq or heads < 1:
+        _refuse("q: bf16 [n_seq, >= heads * head_dim], a row for each row of block_table, heads >= 1")
     stride = _row_stride(q, width, "q")
     if out is None:
         out = _new(_torch.empty, (n_seq, width), _torch.bfloat16, q, stream)
@@ -949,6 +953,8 @@ def et_linear_rows(a, w, bias=None, epilogue=0, gelu_tanh=1, c=None, status=None
     """a [M <= 32, K] bf16, w [N, K] bf16, bias [N] f32 or None.  Returns c (bf16; fp32, added to in place, with epilogue 2)."""
     if _torch is None:
         _import_torch()
+    if a.dim() != 2 or w.dim() != 2:
+        _refuse("a: [M, K], w: [N, K]")
     M, K = a.shape
     N, Kw = w.shape
     outs = N // 2 if epilogue == 4 else N

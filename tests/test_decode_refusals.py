@@ -115,3 +115,21 @@ def test_python_calls_refuse_what_they_cannot_pass_on(B):
         with pytest.raises(B.EarlyTomError) as e:
             f()
         assert e.value.status == INVALID
+
+
+def test_python_calls_refuse_shapes_with_the_binding_s_error(B):
+    """Tensors of another number of dimensions and negative counts are refused like everything else, not by an error of torch's."""
+    bf = torch.bfloat16
+    cache = torch.zeros((4, 2, 2, 16, 64), dtype=bf)
+    table, lens = torch.zeros((3, 2), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    q, a, w = torch.zeros((3, 256), dtype=bf), torch.zeros((2, 64), dtype=bf), torch.zeros((64, 64), dtype=bf)
+    bad = [lambda: B.et_linear_rows(a[0], w), lambda: B.et_linear_rows(a, w[0]), lambda: B.et_linear_rows(a[None], w),
+           lambda: B.et_linear_rows(a.sum(), w), lambda: B.et_attention_paged(q.sum(), 4, cache, None, table, lens),
+           lambda: B.et_attention_paged(q, -1, cache, None, table, lens), lambda: B.et_attention_paged(q[None], 4, cache, None, table, lens),
+           lambda: B.et_kv_append(cache, None, q.sum(), 0, table, lens), lambda: B.et_kv_append(cache, None, q, -1, table, lens, theta=1e4),
+           lambda: B.et_kv_read(cache, None, table, lens, -1), lambda: B.et_kv_read(cache, None, table, lens, 3, out=q.sum()),
+           lambda: B.et_kv_read(cache, None, table, lens, 3, out=q[:, 0])]
+    for i, f in enumerate(bad):
+        with pytest.raises(B.EarlyTomError) as e:
+            f()
+        assert e.value.status == INVALID, i
