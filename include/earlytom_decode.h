@@ -65,19 +65,19 @@ typedef struct {
  *
  * ET_KV_E4M3: a row x of head_dim values is stored as x * 2^-e rounded to e4m3 (nearest, ties to even), with the smallest
  * e in [-127, 127] for which max|x| <= 448 * 2^e; scaling by a power of two is exact, so the conversion is the only
- * rounding.  Turned keys are converted from fp32.  A value that is not finite is stored as NaN and not counted in the
- * maximum.
+ * rounding.  Turned keys are converted from fp32, off by two roundings of that.  A value that is not finite is stored as NaN
+ * and not counted in the maximum.
  *
- * new_len_dev (int [n_seq], may be NULL, not start_dev): positions in the cache after the call, start + rows (at most
- * max_pages * page_size), or the negative start. */
+ * new_len_dev (int [n_seq], may be NULL, not start_dev): positions in the cache after the call, start + rows but at most
+ * max_pages * page_size (also where the start is behind that already), or the negative start. */
 ET_API et_status et_kv_append(const et_kv_cache* cache, const void* qkv_dev, long long row_stride, int rows, int heads,
                               const int* block_table_dev, int n_seq, int max_pages, const int* row_offsets_dev,
                               const int* start_dev, float theta, void* q_out_dev, int* new_len_dev, int* status_dev,
                               void* cuda_stream);
 
 /* Reads rows back: out bf16, row r at out + r * row_stride elements = [K (kv_heads) | V (kv_heads)] x head_dim as stored
- * (exact: an e4m3 value times a power of two has 4 significant bits).  Rows are named as in et_kv_append; rows that are
- * skipped there are left as they were here. */
+ * (an e4m3 value times a power of two has 4 significant bits: exact from 2^-130 on, rounded to bf16's smallest steps of 2^-133
+ * below, infinite from 2^128 on).  Rows are named as in et_kv_append; rows that are skipped there are left as they were here. */
 ET_API et_status et_kv_read(const et_kv_cache* cache, void* out_dev, long long row_stride, int rows,
                             const int* block_table_dev, int n_seq, int max_pages, const int* row_offsets_dev,
                             const int* start_dev, int* status_dev, void* cuda_stream);
@@ -88,7 +88,9 @@ ET_API et_status et_kv_read(const et_kv_cache* cache, void* out_dev, long long r
  * out bf16 [n_seq][heads * head_dim]; lse_dev fp32 [n_seq][heads] (may be NULL): natural logarithm of the sum of
  * exponentials.  len_dev [n_seq]; a length of 0 or less gives zeros and -infinity.  Positions behind max_pages * page_size
  * and on pages that are not in the cache are left out (see status_dev).  Whatever stands behind a sequence's length, NaN
- * included, has no influence.  An infinite value is its column's result, the other columns keep theirs; below 2^-100 of the
+ * included, has no influence.  Scores, their maximum and sum and the outputs are fp32.  A probability counts with 16 bits for a
+ * bf16 cache; for e4m3 with 11 or more down to 2^-21 of the largest one, below that it is off by at most 2^-32 of the largest.
+ * An infinite value is its column's result, the other columns keep theirs; below 2^-100 of the
  * largest weight it may make a NaN of its column instead (0 * infinity).
  * workspace_dev: ET_PAGED_WORKSPACE bytes, 16-byte aligned, contents neither needed nor kept; one call at a time may use
  * it (calls, captured or not, that can run at the same time need one each). */
@@ -101,7 +103,8 @@ ET_API et_status et_attention_paged(const et_kv_cache* cache, const void* q_dev,
 /* Dense layer for few rows: c = epilogue(a[M][K] * w[N][K]^T + bias[N]), M <= 32; the memory traffic of the weights
  * bounds it.  Arguments and epilogues 0, 1, 2 and 4 are those of et_linear_bf16 (the weight rows of epilogue 4 are in the
  * same order, N % 256 == 0); K % 8 == 0, a, w and c 16-byte aligned, c overlaps neither; bias may be NULL (zeros).  Sums
- * are taken in an order that depends on M, N and K alone; a row's result does not depend on the other rows' values. */
+ * are taken in an order that depends on M, N, K and the device (on how many clusters of blocks it holds at once); a row's result
+ * does not depend on the other rows' values. */
 ET_API et_status et_linear_rows(const void* a_dev, const void* w_dev, const float* bias_dev, void* c_dev, int M, int N, int K,
                                 int epilogue, int gelu_tanh, int* status_dev, void* cuda_stream);
 

@@ -23,10 +23,12 @@
 // 2^8 below those of the values that the scores favour takes two bf16 a weight instead.  So a probability has its 11 bits down
 // to 2^-21 of the largest one, whatever the scales, and is off by at most 2^-32 of that one below.
 //
-// Device time in a chain of calls, B200, cache not in L2 (of the measured copy bandwidth; a pure read can pass 1): 28 heads on 4
-// of 128, bf16, one sequence of 100 003 38 us (0.83); e4m3, 64 ragged sequences up to 16 001 54 us (0.86); 16 heads of 128 on 16,
-// one of 180 000, bf16 217 us (1.05), e4m3 115 us (1.00); 24 ragged up to 2 049, 16 heads of 64, bf16 20 us (0.56: short items);
-// 16 heads to a key / value head, 64 ragged, bf16 104 us (0.89), e4m3 67 us (0.70: bound by conversions and exponentials).
+// Device time in a chain of calls, B200, cache not in L2 (of the measured copy bandwidth; a pure read can pass 1); a second figure is
+// for calls repeated for a second, at the clock that the power limit leaves.  28 heads on 4 of 128, bf16, one sequence of 100 003 38.5 us
+// (0.82), of 7 675 10.5 (0.23: start and joining kernel); e4m3, 64 ragged sequences up to 16 001 55 / 59 us (0.85 / 0.79); 16 heads
+// of 128 on 16, one of 180 000, bf16 219 / 221 us (1.04), e4m3 116 / 121 us (0.99 / 0.95); 24 ragged up to 2 049, 16 heads of 64, bf16
+// 22 / 21 us (0.51 / 0.54), e4m3 the same (0.27): short items; 16 heads to a key / value head, 64 ragged, bf16 105 / 110 us (0.88 /
+// 0.85), e4m3 71 / 74 us (0.66 / 0.64: bound by conversions and exponentials).
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
@@ -73,8 +75,8 @@ struct Cfg {
   static constexpr int PLANE = TILE * ROW;
   static constexpr int STAGE = 2 * PLANE;                         // keys, values
   // What an item costs beside its tiles, in tiles' worth of time (measured: 2.3 us beside 0.6 us a tile for bf16 rows of 128, 2.0
-  // and 0.3 for e4m3 ones, 1.4 and 0.25 for bf16 rows of 64; with 16 heads 2.8 and 0.65, 3.7 and 0.4); an item that a group takes
-  // alone costs a good third of it.
+  // and 0.3 for e4m3 ones, 1.4 and 0.25 for bf16 rows of 64; with 16 heads 2.8 and 0.65, 3.7 and 0.4; e4m3 rows of 64 follow the
+  // same formula unmeasured); an item that a group takes alone costs a good third of it.
   static constexpr int COST = (2 + 65536 / STAGE) * (NT + 1) / 2, COST_SHORT = NT == 1 ? 1 + 32768 / STAGE : COST;
   static constexpr int SCALES = E4M3 ? 2 * TILE : 0;
   static constexpr int HEADS = 8 * NT;
@@ -1016,6 +1018,8 @@ cudaError_t launch_attention_paged(const PagedCache& c, const PagedAttention& a,
   const int nt = g.group <= 8 ? 1 : 2;
   g.parts = (g.group + 8 * nt - 1) / (8 * nt);
   const long long tiles = (((long long)a.max_pages << c.page_shift) + TILE - 1) / TILE;      // of the longest sequence there can be
+  // Where no sequence can have more than four tiles, items are not cut and nothing has to be joined.  The host knows the table's width
+  // only: in one for 32 768 positions the same lengths take the other way, 1 x 61 6.7 us in place of 5.5, 16 x 200 8.7 of 6.5.
   g.whole = tiles <= 4;
   const long long most = (long long)a.n_seq * c.kv_heads * g.parts * (g.whole ? 1 : tiles + PAGED_ITEM_COST_MAX);
   if (most >= (1ll << 31) - MAX_CTAS) return cudaErrorInvalidValue;   // refused by the entry point already

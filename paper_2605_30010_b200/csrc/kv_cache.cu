@@ -1,8 +1,9 @@
 // The paged key / value cache: rows of a projection go in (turned and quantised on the way), rows come back.
 //
-// Device time in a chain of calls, B200 (of the measured copy bandwidth, bytes read + written): append of 21 124 rows of 28 + 4 + 4
-// heads of 128, turned, bf16 66 us (0.91); of 7 675 rows of 4 + 4 heads, e4m3 6.8 us (0.54: launch and three loads that wait for
-// one another); of one token 2.7 us.  Read of 63 435 rows of 16 + 16 heads of 64, bf16 89 us (0.91); of 7 675 rows, e4m3 6.7 us.
+// Device time in a chain of calls, B200, rows and cache not in L2 (of the measured copy bandwidth, bytes read + written): append of 21 124
+// rows of 28 + 4 + 4 heads of 128, turned, bf16 66 us (0.91), e4m3 93 us (0.61: instructions, the rotation's among them); of 7 675
+// rows of 4 + 4 heads, e4m3 8.9 us (0.41: launch and three loads that wait for one another); of one token 2.5 us, of 64 e4m3 3.7 us.
+// Read of 63 435 rows of 16 + 16 heads of 64, bf16 86 us (0.93); of 7 675 rows, e4m3 8.9 us (0.41).
 #include <cuda_fp8.h>
 
 #include "decode.cuh"
@@ -105,9 +106,9 @@ __device__ __forceinline__ float turned_exactly(float x, float c1, float c2, flo
 // a row is read once and written once.  The angle of position p and pair i is p * theta^(-2i/d): the host gives each frequency
 // as a 64-bit fraction of a turn, so that p * f modulo 2^64 is the exact fraction of a turn however far p is.  A lane has the
 // same pairs in every head: it keeps their (cos, sin) in registers for the row.  Keys on their way to e4m3 are turned more
-// exactly: what fp32 products lose is small beside bf16's rounding, but takes one in 10^5 of them across a border between two e4m3
-// values, a sixteenth apart.  (8 prompts of 21 124 rows in all, 28 + 4 + 4 heads: 87.6 -> 93.3 us.)  Bound by memory, and with e4m3 and
-// rotation by instructions.
+// exactly: what fp32 products lose is small beside bf16's rounding, but takes one in 400 000 of them across a border between two
+// e4m3 values, a sixteenth apart (now one in two million; 21 124 rows of 28 + 4 + 4 heads 87.6 -> 93.3 us).  Bound by memory, and with
+// e4m3 and rotation by instructions.
 // ---------------------------------------------------------------------------------------------
 template <int DH, bool E4M3, bool ROTATE>
 __global__ void __launch_bounds__(THREADS)

@@ -13,8 +13,8 @@
 // card.  Sums meet in shared memory (of the cluster) in a fixed order.
 //
 // Device time per call in a chain of calls, B200, weights not in L2 (of the measured copy bandwidth):
-//   1 x 3584 x 4608 7.4 us (0.70, direct), 1 x 3584 x 37888 gated 42 us (1.00, ring), 19 x the same 46 us (0.92),
-//   1 x 18944 x 3584 residual 23.5 us (0.90, ring), 32 x the same 26 us (0.81)
+//   1 x 3584 x 4608 8.4 us (0.61, direct), 1 x 3584 x 37888 gated 43.5 us (0.97, ring), 19 x the same 46.5 us (0.90; 47.2 in calls
+//   repeated for a second), 1 x 18944 x 3584 residual 24 us (0.88, ring), 32 x the same 27.5 us (0.78)
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -427,11 +427,11 @@ cudaError_t launch_ring(const LinearArgs& g, cudaStream_t s) {
   int ranks = 1;
   for (int r = 2; r <= MAX_CLUSTER && steps >= 4 * r; ++r) if (cdiv(g.N, RING_ROWS) <= resident[dev][r]) ranks = r;
   // Below eight ranks a block has as few rows (a swizzle pattern's 8 at a time) as the number of waves that blocks of 128 need
-  // allows, so that the last wave is full too.  128 / these in us: 1 x 3584 x 40000 54.7 / 47.0 (72 rows), 1 x 8192 x 40000 118.8 /
-  // 103.8 (72), 32 x 3584 x 50000 74.3 / 66.2 (88), 1 x 3584 x 152064 161.8 / 156.4 (104), 32 x 2048 x 22000 22.2 / 20.8 (80), 32 x
-  // 520 x 8000 7.8 / 6.8 (56), 19 x 10152 x 9728 39.3 / 38.2 (112), 12 x 1504 x 5000 5.8 / 6.0, 32 x 2048 x 152064 115.4 / 116.7
+  // allows, so that the last wave is full too.  128 / these in us: 1 x 3584 x 40000 54.0 / 48.6 (72 rows), 1 x 8192 x 40000 119.0 /
+  // 106.6 (72), 32 x 3584 x 50000 76.4 / 73.4 (88), 1 x 3584 x 152064 164.1 / 163.2 (104), 32 x 2048 x 22000 22.2 / 22.0 (80), 32 x
+  // 520 x 8000 8.6 / 7.7 (56), 19 x 10152 x 9728 41.4 / 40.5 (112), 12 x 1504 x 5000 6.7 / 7.1, 32 x 2048 x 152064 120.9 / 124.6
   // (104).  Gated rows stay in groups of 64, of which one is too few for a block (3584 x 38912 54.8 / 60.1).  At eight ranks
-  // fewer rows gain nothing (13 x 3584 x 2048 5.9 / 6.1).
+  // fewer rows gain nothing (13 x 3584 x 2048 6.8 / 7.0).
   int rows = RING_ROWS;
   if (g.epilogue != EPI_SWIGLU && ranks < MAX_CLUSTER) {
     const int places = cdiv(cdiv(g.N, RING_ROWS), resident[dev][ranks]) * resident[dev][ranks];
@@ -452,9 +452,9 @@ cudaError_t launch_linear_rows(const bf16* a, const bf16* w, const float* bias, 
                                int gelu_tanh, int* status, cudaStream_t s) {
   const LinearArgs g{a, w, bias, c, M, N, K, epilogue, gelu_tanh, status};
   // The ring takes over where the weights are many, much sooner with more than 8 rows (direct reads a again for every 32 weight
-  // rows), unless there are too few weight rows for its blocks.  Direct / ring in us: 1 x 3584 x 4608 7.2 / 7.3, 8 x 3584 x 9000
-  // 13.0 / 14.2, 8 x 18944 x 3584 25.5 / 24.6; 13 x 2048 x 2048 4.6 / 4.8, 13 x 3584 x 2048 5.8 / 5.5, 13 x 18944 x 3584 29.4 /
-  // 24.9; 32 x 2048 x 2048 6.7 / 5.6; 32 x 16384 x 512 9.8 / 12.9.
+  // rows), unless there are too few weight rows for its blocks.  Direct / ring in us: 1 x 3584 x 4608 8.4 / 8.8, 8 x 3584 x 9000
+  // 12.9 / 14.1, 8 x 18944 x 3584 24.9 / 23.9; 13 x 2048 x 2048 6.0 / 5.7, 13 x 3584 x 2048 8.0 / 6.8, 13 x 18944 x 3584 28.2 /
+  // 24.3; 20 x 1024 x 900 4.2 / 5.2; 32 x 2048 x 2048 7.7 / 6.6; 32 x 16384 x 512 10.9 / 13.9.
   const long long weights = (long long)N * K;
   const bool ring = M <= 8 ? weights > (1ll << 25) : N >= 1024 && weights * ((M + 7) / 8) > 12000000;
   if (ring) return M <= 8 ? launch_ring<1>(g, s) : M <= 16 ? launch_ring<2>(g, s) : launch_ring<4>(g, s);

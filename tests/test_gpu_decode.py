@@ -271,6 +271,27 @@ def test_e4m3_conversion_edges(B):
     assert np.array_equal(back, f64(bf16(want)), equal_nan=True) and status.item() == 0
 
 
+def test_read_at_the_ends_of_bf16(B):
+    """Rows read from an e4m3 cache: exact from 2^-130 on, bf16's smallest steps below, infinite from 2^128 on."""
+    d, kvh, page = 64, 1, 16
+    rng = np.random.default_rng(6)
+    c = Cache(rng, 1, 1, kvh, page, d, True)
+    codes = np.arange(256, dtype=np.uint8).reshape(1, 4, 64)                    # four rows hold every code
+    scales = [0, 1, 2, 7, 120, 246, 247]                                        # bytes; 2^(b - 127)
+    import torch
+    for b in scales:
+        c.data.view(torch.uint8)[c.table[0, 0].long(), 0, 0, :4] = torch.from_numpy(codes[0]).cuda()
+        c.scale[c.table[0, 0].long(), 0, 0, :4] = b
+        out = B.et_kv_read(c.data, c.scale, c.table, i32([0]), 4, i32([0, 4]))[:, :d]
+        want = CODES[codes[0]] * 2.0 ** (b - 127)
+        with np.errstate(over="ignore"):
+            nearest = f64(bf16(want))
+        assert np.array_equal(f64(out), nearest, equal_nan=True)
+        exact = np.isnan(want) | ((np.abs(want) >= 2.0 ** -130) & (np.abs(want) < 2.0 ** 128)) | (want == 0)
+        assert np.array_equal(f64(out)[exact], want[exact], equal_nan=True)
+        assert np.isinf(f64(out)[np.abs(want) >= 2.0 ** 128]).all()
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
 def test_rows_that_cannot_be_placed_are_skipped(B, e4m3):
     """Slots not in use, positions behind the table, pages that are not in the cache: skipped and reported, the others land."""
