@@ -544,6 +544,54 @@ def test_attention_long_sums(B, heads, n, rising, e4m3):
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("heads,kvh,d", [(1, 1, 128), (14, 2, 64), (23, 1, 128)])
+def test_attention_long_runs_of_uneven_sequences(B, heads, kvh, d, e4m3):
+    """Runs of more tiles than a piece has, that begin and end anywhere in sequences of very different lengths: every way in which
+    pieces go on from one another, inside a CTA and from one to the next; the workspace is full of NaN before.  Scores rise along
+    the cache, so that the pieces' maxima differ."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(heads)
+    rng = np.random.default_rng(heads + e4m3)
+    page, longest = 64, 600_000
+    lens = [int(x) for x in rng.integers(1, longest, 44 // kvh)]
+    lens[2], lens[5], lens[8], lens[9], lens[-1] = longest, 1, 0, 130, 65_536
+    pages = longest // page
+    rows = torch.randn((longest, 2, kvh, d), device="cuda", generator=gen)
+    rows[:, 0, :, 0] = (torch.linspace(-20, 20, longest, device="cuda") * math.sqrt(d) / 16).unsqueeze(1)
+    rows[:, 1] += torch.linspace(-2, 2, longest, device="cuda").view(-1, 1, 1)
+    data = torch.zeros((pages, 2, kvh, page, d), device="cuda", dtype=torch.float8_e4m3fn if e4m3 else torch.bfloat16)
+    scale = torch.zeros((pages, 2, kvh, page), device="cuda", dtype=torch.uint8) if e4m3 else None
+    table = torch.randperm(pages, device="cuda", generator=gen).to(torch.int32).view(1, -1)
+    B.et_kv_append(data, scale, rows.to(torch.bfloat16).view(longest, -1), 0, table, i32([0]), i32([0, longest]))
+    stored = B.et_kv_read(data, scale, table, i32([0]), longest, i32([0, longest])).view(longest, 2, kvh, d)
+    n_seq = len(lens)
+    q = torch.randn((n_seq, kvh, heads // kvh, d), device="cuda", generator=gen)
+    q[:, :, :, 0] = 16 * torch.rand((n_seq, kvh, heads // kvh), device="cuda", generator=gen)      # some flat, some steep
+    q = q.to(torch.bfloat16)
+    lse, status = torch.empty((n_seq, heads), device="cuda"), i32([0])
+    ws = torch.full((B.ET_PAGED_WORKSPACE,), 255, dtype=torch.uint8, device="cuda")
+    out = B.et_attention_paged(q.view(n_seq, -1), heads, data, scale, table.expand(n_seq, -1).contiguous(), i32(lens), lse=lse,
+                               workspace=ws, status=status)
+    assert status.item() == 0
+    for s, n in enumerate(lens):
+        got, got_lse = out[s].view(kvh, -1, d).double(), lse[s].view(kvh, -1).double()
+        if n == 0:
+            assert (got == 0).all() and (got_lse == -math.inf).all()
+            continue
+        for h in range(kvh):
+            k, v, qs = stored[:n, 0, h].double(), stored[:n, 1, h].double(), q[s, h].double()
+            z = qs @ k.T / math.sqrt(d)
+            drift = d * 2.0 ** -23 * (qs.abs() @ k.abs().T).amax(-1) / math.sqrt(d) + 2.0 ** -20
+            p = torch.softmax(z, -1)
+            want, mass = p @ v, p @ v.abs()
+            # 1024 instructions of the tensor core between sums in fp32, of which there are n / 512 and fewer
+            tol = BF16 * want.abs() + (2.0 ** -11 + 2 * drift + 1024 * 2.0 ** -23 + n / 512 * 2.0 ** -24).unsqueeze(-1) * mass
+            off = (got[h] - want).abs() / tol
+            assert (off <= 1).all(), f"sequence {s} of {n}: off by {off.max().item():.3g} of the tolerance"
+            assert ((got_lse[h] - torch.logsumexp(z, -1)).abs() <= drift + n / 512 * 2.0 ** -24 + 2.0 ** -19).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
 def test_attention_peaked_and_far_apart_scores(B, e4m3):
     """Scores from one key that takes all to thousands apart, growing and falling along the cache; queries of very different
     sizes; values of very different sizes, the large ones where nothing looks."""
