@@ -1,6 +1,6 @@
 /* earlytom_decode.h -- what a decode step of the language model needs beside the prefill of earlytom_llm.h: a paged
- * key / value cache (bf16, or e4m3 with one power of two per row), attention of one new token over it, and dense
- * layers for a handful of rows.  No counterpart in the paper, whose time-to-first-token ends with the prefill; the
+ * key / value cache (bf16, e4m3 with one power of two per row, or 4 bits with one scale per 32 values), attention of one
+ * new token over it, and dense layers for a handful of rows.  No counterpart in the paper, whose time-to-first-token ends with the prefill; the
  * architecture is the one of earlytom_llm.h (grouped-query attention, rotate-half rotary embedding, bf16 activations,
  * fp32 residual stream and statistics).
  *
@@ -28,13 +28,16 @@
 extern "C" {
 #endif
 
-typedef enum { ET_KV_BF16 = 0, ET_KV_E4M3 = 1 } et_kv_format;
+typedef enum { ET_KV_BF16 = 0, ET_KV_E4M3 = 1, ET_KV_INT4 = 2 } et_kv_format;
 enum { ET_PAGED_CAPACITY = 3, ET_PAGED_BAD_PAGE = 5 };
 
 /* A paged cache of one layer.  Row t of page p holds the key (plane 0) and value (plane 1) of one position:
  *   data  [n_pages][2][kv_heads][page_size][head_dim], bf16 or e4m3 (4 exponent bits, 3 mantissa bits, no infinities);
- *   scale [n_pages][2][kv_heads][page_size], ET_KV_E4M3 only (NULL otherwise): a byte b stands for 2^(b - 127), the factor
- *         of its row of head_dim values; b is never 255.
+ *         ET_KV_INT4: [n_pages][2][kv_heads][page_size][head_dim / 2] bytes, value 2i in the low four bits of byte i, value 2i + 1 in
+ *         the high ones; a code c stands for c - 8 times the scale of its 32 values;
+ *   scale ET_KV_E4M3: [n_pages][2][kv_heads][page_size], a byte b stands for 2^(b - 127), the factor of its row of head_dim
+ *         values; b is never 255.  ET_KV_INT4: bf16 [n_pages][2][kv_heads][page_size][head_dim / 32], values 32 j .. 32 j + 31 of a row
+ *         have the j-th.  ET_KV_BF16: NULL.
  * Both 16-byte aligned.  Rows never written hold whatever was there; nothing reads behind a sequence's length. */
 typedef struct {
   void* data;
@@ -68,6 +71,10 @@ typedef struct {
  * rounding.  Turned keys are converted from fp32, off by two roundings of that.  A value that is not finite is stored as NaN
  * and not counted in the maximum.
  *
+ * ET_KV_INT4: the scale s of 32 values is the smallest bf16 that is not below max|x| / 7, a code is 8 + x / s rounded to nearest, ties to
+ * even (1 .. 15): a value is off by at most s / 2.  Scales and codes are those of 64-bit arithmetic, turned keys' as well.  32
+ * values of which one is not finite (or, of a turned key, beyond fp32) have a NaN for their scale: all of them read as NaN.
+ *
  * new_len_dev (int [n_seq], may be NULL, not start_dev): positions in the cache after the call, start + rows but at most
  * max_pages * page_size (also where the start is behind that already), or the negative start. */
 ET_API et_status et_kv_append(const et_kv_cache* cache, const void* qkv_dev, long long row_stride, int rows, int heads,
@@ -77,7 +84,7 @@ ET_API et_status et_kv_append(const et_kv_cache* cache, const void* qkv_dev, lon
 
 /* Reads rows back: out bf16, row r at out + r * row_stride elements = [K (kv_heads) | V (kv_heads)] x head_dim as stored
  * (an e4m3 value times a power of two has 4 significant bits: exact from 2^-130 on, rounded to bf16's smallest steps of 2^-133
- * below, infinite from 2^128 on).  Rows are named as in et_kv_append; rows that are skipped there are left as they were here. */
+ * below, infinite from 2^128 on; a 4-bit value, a whole number times a bf16, is rounded once).  Rows are named as in et_kv_append; rows that are skipped there are left as they were here. */
 ET_API et_status et_kv_read(const et_kv_cache* cache, void* out_dev, long long row_stride, int rows,
                             const int* block_table_dev, int n_seq, int max_pages, const int* row_offsets_dev,
                             const int* start_dev, int* status_dev, void* cuda_stream);
@@ -89,9 +96,10 @@ ET_API et_status et_kv_read(const et_kv_cache* cache, void* out_dev, long long r
  * exponentials.  len_dev [n_seq]; a length of 0 or less gives zeros and -infinity.  Positions behind max_pages * page_size
  * and on pages that are not in the cache are left out (see status_dev).  Whatever stands behind a sequence's length, NaN
  * included, has no influence.  Scores, their maximum and sum and the outputs are fp32.  A probability counts with 16 bits for a
- * bf16 cache; for e4m3 with 11 or more down to 2^-21 of the largest one, below that it is off by at most 2^-32 of the largest.
+ * bf16 cache and for one of 4 bits; for e4m3 with 11 or more down to 2^-21 of the largest one, below that it is off by at most 2^-32 of the largest.
  * An infinite value is its column's result, the other columns keep theirs; below 2^-100 of the
- * largest weight it may make a NaN of its column instead (0 * infinity).
+ * largest weight it may make a NaN of its column instead (0 * infinity).  In 4 bits a scale that is NaN makes NaN of the 32 columns that
+ * it counts for (a key's: of all); infinite scales are not stored by any call and give NaN or infinities.
  * workspace_dev: ET_PAGED_WORKSPACE bytes, 16-byte aligned, contents neither needed nor kept; one call at a time may use
  * it (calls, captured or not, that can run at the same time need one each). */
 #define ET_PAGED_WORKSPACE (4u << 20)

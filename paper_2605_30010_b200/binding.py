@@ -33,7 +33,7 @@ EXPORTS = ["et_encoder_create", "et_encode_video", "et_encode_batch", "et_encode
            "et_llm_profile_read", "et_rmsnorm", "et_rope", "et_swiglu", "et_attention_causal",
            # include/earlytom_decode.h
            "et_kv_append", "et_kv_read", "et_attention_paged", "et_linear_rows"]
-ET_KV_BF16, ET_KV_E4M3 = 0, 1
+ET_KV_BF16, ET_KV_E4M3, ET_KV_INT4 = 0, 1, 2
 ET_PAGED_CAPACITY, ET_PAGED_BAD_PAGE = 3, 5        # values of a paged call's status word
 ET_PAGED_WORKSPACE = 4 << 20
 
@@ -832,8 +832,8 @@ _KV_CACHE = struct.Struct("@PPiiiii0P")       # et_kv_cache as bytes, a third of
 
 
 def _kv_cache(cache, scale):
-    """cache [n_pages, 2, kv_heads, page_size, head_dim] bf16 or e4m3 (scale uint8 [n_pages, 2, kv_heads, page_size]) as
-    (et_kv_cache, kv_heads, head_dim)."""
+    """cache [n_pages, 2, kv_heads, page_size, head_dim] bf16, e4m3 (scale uint8 [n_pages, 2, kv_heads, page_size]) or 4 bits (uint8
+    [..., head_dim / 2], scale bf16 [n_pages, 2, kv_heads, page_size, head_dim / 32]) as (et_kv_cache, kv_heads, head_dim)."""
     shape = cache.shape
     if len(shape) != 5 or shape[1] != 2 or not cache.is_contiguous():
         _refuse("cache: contiguous [n_pages, 2, kv_heads, page_size, head_dim]")
@@ -842,8 +842,14 @@ def _kv_cache(cache, scale):
         if scale is not None:
             _refuse("scale goes with an e4m3 cache only")
         return _KV_CACHE.pack(cache.data_ptr(), 0, n_pages, kv_heads, page_size, head_dim, ET_KV_BF16), kv_heads, head_dim
+    if cache.dtype is _torch.uint8:
+        if (scale is None or scale.dtype is not _torch.bfloat16 or scale.shape[:4] != shape[:4] or scale.dim() != 5
+                or 16 * scale.shape[4] != head_dim or not scale.is_contiguous()):
+            _refuse("a cache of 4 bits (uint8 [..., head_dim / 2]) needs scale: contiguous bf16 [n_pages, 2, kv_heads, page_size, head_dim / 32]")
+        return (_KV_CACHE.pack(cache.data_ptr(), scale.data_ptr(), n_pages, kv_heads, page_size, 2 * head_dim, ET_KV_INT4), kv_heads,
+                2 * head_dim)
     if cache.dtype is not _torch.float8_e4m3fn:
-        _refuse("cache: bfloat16 or float8_e4m3fn")
+        _refuse("cache: bfloat16, float8_e4m3fn or uint8 (4 bits)")
     if scale is None or scale.dtype is not _torch.uint8 or scale.shape != shape[:4] or not scale.is_contiguous():
         _refuse("an e4m3 cache needs scale: contiguous uint8 [n_pages, 2, kv_heads, page_size]")
     return (_KV_CACHE.pack(cache.data_ptr(), scale.data_ptr(), n_pages, kv_heads, page_size, head_dim, ET_KV_E4M3), kv_heads,

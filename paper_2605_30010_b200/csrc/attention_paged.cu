@@ -67,9 +67,9 @@ constexpr int PAD = 4;                         // floats between heads of the jo
 constexpr int SMEM_LIMIT = 232448 - 512;       // 227 KB, less the static part
 constexpr int CONTROL_BYTES = 1024;            // barriers and the ring's flags
 
-template <int DH, bool E4M3, int NT>
+template <int DH, int FMT, int NT>
 struct Cfg {
-  static constexpr int ROW = DH * (E4M3 ? 1 : 2);                 // bytes of a row
+  static constexpr int ROW = kv_row_bytes(FMT, DH);               // bytes of a row
   static constexpr int BOX_ROW = ROW > 128 ? 128 : ROW;           // bytes of a box row: the swizzle's width
   static constexpr int BOXES = ROW / BOX_ROW;
   static constexpr int PLANE = TILE * ROW;
@@ -77,8 +77,9 @@ struct Cfg {
   // What an item costs beside its tiles, in tiles' worth of time (measured: 2.3 us beside 0.6 us a tile for bf16 rows of 128, 2.0
   // and 0.3 for e4m3 ones, 1.4 and 0.25 for bf16 rows of 64; with 16 heads 2.8 and 0.65, 3.7 and 0.4; e4m3 rows of 64 follow the
   // same formula unmeasured); an item that a group takes alone costs a good third of it.
-  static constexpr int COST = (2 + 65536 / STAGE) * (NT + 1) / 2, COST_SHORT = NT == 1 ? 1 + 32768 / STAGE : COST;
-  static constexpr int SCALES = E4M3 ? 2 * TILE : 0;
+  static constexpr int COST_ = (2 + 65536 / STAGE) * (NT + 1) / 2, COST_SHORT_ = NT == 1 ? 1 + 32768 / STAGE : COST_;
+  static constexpr int COST = COST_ < PAGED_ITEM_COST_MAX ? COST_ : PAGED_ITEM_COST_MAX, COST_SHORT = COST_SHORT_ < COST ? COST_SHORT_ : COST;
+  static constexpr int SCALES = 2 * TILE * kv_scale_bytes(FMT, DH);
   static constexpr int HEADS = 8 * NT;
   static constexpr int JOIN = COMPUTE_WARPS * HEADS * (DH + PAD) * 4 + COMPUTE_WARPS * HEADS * 3 * 4;   // the warps' results of a piece
   static constexpr int JOINS = NT == 1 ? 2 : 1;                   // pieces whose results can wait to be joined
@@ -151,12 +152,56 @@ __device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t x) {
   const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x));
   return pack_bf16(f.x, f.y);
 }
+// Eight 4-bit codes of a word as x[i] = codes i and i + 4, less 8, in two halves: over the mantissa of 1024 a code counts as itself or,
+// four bits higher, 16 times, so that a mask and one packed multiply-add make two values of them.
+__device__ __forceinline__ uint32_t fma_f16x2(uint32_t x, uint32_t a, uint32_t b) {
+  uint32_t y;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(x), "r"(a), "r"(b));
+  return y;
+}
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t x, uint32_t a, uint32_t b) {
+  uint32_t y;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(x), "r"(a), "r"(b));
+  return y;
+}
+__device__ __forceinline__ void int4_to_f16(uint32_t w, uint32_t (&x)[4]) {
+  const uint32_t v = w >> 8;
+  x[0] = fma_f16x2((w & 0x000f000fu) | 0x64006400u, 0x3c003c00u, 0xe408e408u);         // (1024 + c) - 1032
+  x[1] = fma_f16x2((w & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, 0xd480d480u);         // (1024 + 16 c) / 16 - 72
+  x[2] = fma_f16x2((v & 0x000f000fu) | 0x64006400u, 0x3c003c00u, 0xe408e408u);
+  x[3] = fma_f16x2((v & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, 0xd480d480u);
+}
+// The same in bf16, whose mantissa has room for a code in its four low or its four high bits: over 128.
+__device__ __forceinline__ void int4_to_bf16(uint32_t w, uint32_t (&x)[4]) {
+  x[0] = fma_bf16x2((w & 0x000f000fu) | 0x43004300u, 0x3f803f80u, 0xc308c308u);        // (128 + c) - 136
+  x[1] = fma_bf16x2(((w >> 1) & 0x00780078u) | 0x43004300u, 0x3e003e00u, 0xc1c0c1c0u); // (128 + 8 c) / 8 - 24
+  x[2] = fma_bf16x2(((w >> 8) & 0x000f000fu) | 0x43004300u, 0x3f803f80u, 0xc308c308u);
+  x[3] = fma_bf16x2(((w >> 9) & 0x00780078u) | 0x43004300u, 0x3e003e00u, 0xc1c0c1c0u);
+}
+// N bf16 scales next to one another (zeros if not live)
+template <int N>
+__device__ __forceinline__ void load_scales(const uint8_t* src, float (&f)[N], bool live = true) {
+  static_assert(N == 2 || N == 4, "head sizes of 64 and 128");
+  uint32_t w[N / 2];
+  if constexpr (N == 4) {
+    const uint2 v = *reinterpret_cast<const uint2*>(src);
+    w[0] = v.x; w[N / 2 - 1] = v.y;
+  } else w[0] = *reinterpret_cast<const uint32_t*>(src);
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    if (!live) w[i] = 0;
+    f[2 * i] = __uint_as_float(w[i] << 16);
+    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
 constexpr float WEIGHT_SHIFT = 15.f;           // e4m3: the largest weight is 2^15, halves end at 65504
 constexpr float SCALE_SPAN = 8.f;              // e4m3: binades that a tile's scales may lie low for halves to hold its weights
 // A weight as the sum of two bf16: its upper half, which is cut off and not rounded, and the rest.  The rest is above zero
 // wherever the weight is (by 2^-24 of the weight too large), since an infinite value is multiplied by both, and with a zero or a
 // negative number it would become a NaN or the other infinity.
 __device__ __forceinline__ uint32_t upper_halves(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632); }
+__device__ __forceinline__ uint32_t lower_halves(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410); }
+__device__ __forceinline__ float rest_of(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u); }     // of a finite value's weight
 __device__ __forceinline__ float lower_part(float x) {
   return fmaf(__uint_as_float(__float_as_uint(x) & 0xffff0000u), -(1.f - 0x1p-24f), x);
 }
@@ -259,11 +304,12 @@ __device__ __forceinline__ bool next_piece(const Args& g, int parts_all, Walk& w
   return false;
 }
 
-template <int DH, bool E4M3, int NT>
+template <int DH, int FMT, int NT>
 __global__ void __launch_bounds__(THREADS, 1)
 attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ Args g) {
-  using C = Cfg<DH, E4M3, NT>;
-  constexpr int STAGES = C::STAGES, KS = DH / 16;
+  using C = Cfg<DH, FMT, NT>;
+  constexpr bool BF16 = FMT == ET_KV_BF16, E4M3 = FMT == ET_KV_E4M3, INT4 = FMT == ET_KV_INT4;
+  constexpr int STAGES = C::STAGES, KS = DH / 16, SCALE = kv_scale_bytes(FMT, DH);     // SCALE: bytes of a row's scales
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const gen = smem_raw + (base - raw);
@@ -340,7 +386,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     // ------------------------------------------------------------------ copies
     const int me = warp - COMPUTE_WARPS;
     const int box_shift = min(g.c.page_shift, 6), box_rows = 1 << box_shift, boxes_tile = TILE >> box_shift;
-    const uint32_t box_bytes = (uint32_t)box_rows * (2 * C::ROW + (E4M3 ? 2 : 0));
+    const uint32_t box_bytes = (uint32_t)box_rows * (2 * C::ROW + 2 * SCALE);
     const int plane_rows = kv_heads << g.c.page_shift;
     // the cache is read once (several head tiles read it soon after one another): it need not push other things out of L2
     uint64_t policy;
@@ -417,8 +463,8 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 #pragma unroll
               for (int half = 0; half < C::BOXES; ++half)
                 tma_load_elect(dst + plane * C::PLANE + half * (TILE * C::BOX_ROW) + r0 * C::BOX_ROW, &map, bar,
-                               half * (C::BOX_ROW / (E4M3 ? 1 : 2)), y, policy);
-              if (E4M3) bulk_load_elect(sdst + plane * TILE + r0, g.c.scale + (unsigned)y, (uint32_t)box_rows, bar);
+                               half * (C::BOX_ROW / (BF16 ? 2 : 1)), y, policy);
+              if (!BF16) bulk_load_elect(sdst + (plane * TILE + r0) * SCALE, g.c.scale + (size_t)(unsigned)y * SCALE, (uint32_t)(box_rows * SCALE), bar);
             }
           }
         }
@@ -441,13 +487,18 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     const int gq = lane >> 2, tq = lane & 3;                         // mma's row group and column pair
     // this lane's row of the 16 and its 16-byte chunk (K: both halves of a k-step; V, transposed: see below)
     const int krow = r0 + (lane & 7) + ((lane >> 3) & 1) * 8, kchunk = lane >> 4;
-    const int vrow = E4M3 ? krow : r0 + (lane & 7) + (lane >> 4) * 8, vchunk = E4M3 ? kchunk : (lane >> 3) & 1;
+    const int vrow = !BF16 ? krow : r0 + (lane & 7) + (lane >> 4) * 8, vchunk = !BF16 ? kchunk : (lane >> 3) & 1;
     auto swizzled = [&](int row, int chunk) -> uint32_t {            // 16-byte chunk of a row, as the copies place it
       if constexpr (C::BOX_ROW == 128)
         return (uint32_t)((chunk >> 3) * (TILE * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4));
-      else
+      else if constexpr (C::BOX_ROW == 64)
         return (uint32_t)(row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4));
+      else
+        return (uint32_t)(row * 32 + ((chunk ^ ((row >> 2) & 1)) << 4));
     };
+    // where a head's outputs of o[.][k] are: dimension, and the distance between the accumulator's two rows
+    auto out_dim = [&](int k) { return BF16 ? 16 * k + gq : E4M3 ? 16 * k + 2 * gq : 32 * (k >> 1) + 4 * gq + 2 * (k & 1); };
+    constexpr int OUT_STEP = BF16 ? 8 : 1;
     const float softmax_scale = 1.4426950408889634f * (DH == 128 ? 0.08838834764831845f : 0.125f);   // log2(e) / sqrt(DH)
 
     // Four values of a head's output (not yet divided), its maximum and sum: to the output, or to the workspace if others follow.
@@ -528,7 +579,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const uint8_t* src = query + (n * 8 + gq) * C::Q_ROW;
-          if constexpr (!E4M3) {
+          if constexpr (BF16) {
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
               q[n][k][0] = *reinterpret_cast<const uint32_t*>(src + k * 32 + 4 * tq);
@@ -538,12 +589,22 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
           } else {
             // e4m3 keys are multiplied as halves, which hold them exactly.  A query row is scaled by a power of two that
             // brings its largest value to 2^14 .. 2^15: a value below 2^-29 of that loses bits, no other.  The dimensions of
-            // a k-step are taken in the order that the keys' bytes come in: 4 tq, 4 tq + 1 | 4 tq + 2, 4 tq + 3.
+            // a k-step are taken in the order that the keys' bytes come in: 4 tq, 4 tq + 1 | 4 tq + 2, 4 tq + 3.  Codes of 4 bits are
+            // multiplied as halves, too; of the 32 dimensions of two k-steps a lane has 8 tq .. 8 tq + 7, and takes i and i + 4
+            // together, which one mask takes out of a word.
             uint2 raw_q[KS];
             float top = 0.f;
+            if constexpr (INT4) {
+#pragma unroll
+              for (int k = 0; k < KS; k += 2) {
+                const uint4 w = *reinterpret_cast<const uint4*>(src + k * 32 + 16 * tq);
+                raw_q[k] = make_uint2(__byte_perm(w.x, w.z, 0x5410), __byte_perm(w.x, w.z, 0x7632));
+                raw_q[k + 1] = make_uint2(__byte_perm(w.y, w.w, 0x5410), __byte_perm(w.y, w.w, 0x7632));
+              }
+            }
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-              raw_q[k] = *reinterpret_cast<const uint2*>(src + k * 32 + 8 * tq);
+              if constexpr (E4M3) raw_q[k] = *reinterpret_cast<const uint2*>(src + k * 32 + 8 * tq);
               const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].x));
               const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].y));
               top = fmaxf(top, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(y.x), fabsf(y.y))));
@@ -604,7 +665,37 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
           for (int j = 0; j < BLOCKS; ++j)
 #pragma unroll
             for (int n = 0; n < NT; ++n) s[j][n][0] = s[j][n][1] = s[j][n][2] = s[j][n][3] = 0.f;
-          if constexpr (!E4M3) {
+          if constexpr (INT4) {
+            // a block of 32 dimensions is two k-steps; its sum counts with the scale that the position has for it
+#pragma unroll
+            for (int j = 0; j < BLOCKS; ++j) {
+              const uint8_t* sc = gen + STAGES * C::STAGE + st * C::SCALES + (r0 + 16 * j + gq) * SCALE;
+              float ks[2][DH / INT4_BLOCK];
+              load_scales<DH / INT4_BLOCK>(sc, ks[0]);
+              load_scales<DH / INT4_BLOCK>(sc + 8 * SCALE, ks[1]);
+#pragma unroll
+              for (int k = 0; k < KS; k += 4) {
+                uint32_t a[4];                                        // positions gq / gq + 8 of a block, then of the next
+                ldmatrix4(kb + swizzled(krow + 16 * j, k / 2 + kchunk), a);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                  uint32_t x[4], y[4];
+                  int4_to_f16(a[2 * i], x);
+                  int4_to_f16(a[2 * i + 1], y);
+#pragma unroll
+                  for (int n = 0; n < NT; ++n) {
+                    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+                    mma16816<true>(acc, x[0], y[0], x[1], y[1], q[n][k + 2 * i][0], q[n][k + 2 * i][1]);
+                    mma16816<true>(acc, x[2], y[2], x[3], y[3], q[n][k + 2 * i + 1][0], q[n][k + 2 * i + 1][1]);
+                    s[j][n][0] = fmaf(acc[0], ks[0][k / 2 + i], s[j][n][0]);
+                    s[j][n][1] = fmaf(acc[1], ks[0][k / 2 + i], s[j][n][1]);
+                    s[j][n][2] = fmaf(acc[2], ks[1][k / 2 + i], s[j][n][2]);
+                    s[j][n][3] = fmaf(acc[3], ks[1][k / 2 + i], s[j][n][3]);
+                  }
+                }
+              }
+            }
+          } else if constexpr (BF16) {
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -704,14 +795,22 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
           // into two bf16 (16 bits of it count); halves hold 11 bits of it.  Whatever stands behind the length must not meet a
           // zero probability (0 * NaN is NaN): the values there are cleared.
           auto add_values = [&](auto pair) {
-            constexpr bool PAIR = decltype(pair)::value;
+            [[maybe_unused]] constexpr bool PAIR = decltype(pair)::value;
 #pragma unroll
             for (int j = 0; j < BLOCKS; ++j) {
-              uint32_t ph0[NT], ph1[NT], pl0[NT], pl1[NT];
+              [[maybe_unused]] uint32_t ph0[NT], ph1[NT], pl0[NT], pl1[NT];
+              [[maybe_unused]] float pt[NT][4];                                      // 4 bits: weights of head gq at positions 2 tq, 2 tq + 1, + 8, + 9
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
                 const float* x = s[j][n];
-                if constexpr (!PAIR) {
+                if constexpr (INT4) {
+#pragma unroll
+                  for (int i = 0; i < 4; i += 2) {
+                    const uint32_t hi = transpose8x8(upper_halves(x[i], x[i + 1])), lo = transpose8x8(lower_halves(x[i], x[i + 1]));
+                    pt[n][i] = __uint_as_float(__byte_perm(lo, hi, 0x5410));
+                    pt[n][i + 1] = __uint_as_float(__byte_perm(lo, hi, 0x7632));
+                  }
+                } else if constexpr (!PAIR) {
                   ph0[n] = transpose8x8(pack_f16(x[0], x[1]));
                   ph1[n] = transpose8x8(pack_f16(x[2], x[3]));
                 } else {
@@ -721,9 +820,42 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                   pl1[n] = transpose8x8(pack_bf16(lower_part(x[2]), lower_part(x[3])));
                 }
               }
-              const uint32_t keep0 = (2 * tq < valid[j] ? 0xffffu : 0u) | (2 * tq + 1 < valid[j] ? 0xffff0000u : 0u);
-              const uint32_t keep1 = (2 * tq + 8 < valid[j] ? 0xffffu : 0u) | (2 * tq + 9 < valid[j] ? 0xffff0000u : 0u);
-              if constexpr (!E4M3) {
+              [[maybe_unused]] const uint32_t keep0 = (2 * tq < valid[j] ? 0xffffu : 0u) | (2 * tq + 1 < valid[j] ? 0xffff0000u : 0u);
+              [[maybe_unused]] const uint32_t keep1 = (2 * tq + 8 < valid[j] ? 0xffffu : 0u) | (2 * tq + 9 < valid[j] ? 0xffff0000u : 0u);
+              if constexpr (INT4) {
+                // a value's scale goes to its weight, which has a bf16's exponents; behind the length it is cleared, whatever it was
+                const uint8_t* sc = gen + STAGES * C::STAGE + st * C::SCALES + (TILE + r0 + 16 * j + 2 * tq) * SCALE;
+                float vs[4][DH / INT4_BLOCK];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const int at = (i & 1) + 8 * (i >> 1);
+                  load_scales<DH / INT4_BLOCK>(sc + at * SCALE, vs[i], 2 * tq + at < valid[j]);
+                }
+#pragma unroll
+                for (int k = 0; k < KS; k += 4) {
+                  uint32_t a[4];                                      // positions 2 tq, + 1 / + 8, + 9 of a block, then of the next
+                  ldmatrix4_trans(vb + swizzled(vrow + 16 * j, k / 2 + vchunk), a);
+#pragma unroll
+                  for (int i = 0; i < 2; ++i) {
+                    uint32_t x[4], y[4];                              // dimensions 4 gq + 0 .. 3 of the block
+                    int4_to_bf16(a[2 * i], x);
+                    int4_to_bf16(a[2 * i + 1], y);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                      float w[4];
+#pragma unroll
+                      for (int e = 0; e < 4; ++e) w[e] = pt[n][e] * vs[e][k / 2 + i];
+                      const uint32_t h0 = upper_halves(w[0], w[1]), h1 = upper_halves(w[2], w[3]);
+                      const uint32_t l0 = pack_bf16(rest_of(w[0]), rest_of(w[1])), l1 = pack_bf16(rest_of(w[2]), rest_of(w[3]));
+#pragma unroll
+                      for (int e = 0; e < 2; ++e) {
+                        mma16816<false>(o[n][k + 2 * i + e], x[2 * e], x[2 * e + 1], y[2 * e], y[2 * e + 1], h0, h1);
+                        mma16816<false>(o[n][k + 2 * i + e], x[2 * e], x[2 * e + 1], y[2 * e], y[2 * e + 1], l0, l1);
+                      }
+                    }
+                  }
+                }
+              } else if constexpr (BF16) {
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
                   uint32_t a[4];                                      // rows d = 16 k + gq, + 8; columns = positions
@@ -774,7 +906,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                 added = true;
               }
           }
-          if (!added) add_values(std::bool_constant<!E4M3>());
+          if (!added) add_values(std::bool_constant<BF16>());
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(empty(st));
@@ -806,8 +938,9 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
             if (h >= live) continue;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-              if (E4M3) *reinterpret_cast<float2*>(dst + h * (DH + PAD) + 16 * k + 2 * gq) = make_float2(o[n][k][i], o[n][k][i + 2]);
-              else { dst[h * (DH + PAD) + 16 * k + gq] = o[n][k][i]; dst[h * (DH + PAD) + 16 * k + 8 + gq] = o[n][k][i + 2]; }
+              float* const x = dst + h * (DH + PAD) + out_dim(k);
+              if (OUT_STEP == 1) *reinterpret_cast<float2*>(x) = make_float2(o[n][k][i], o[n][k][i + 2]);
+              else { x[0] = o[n][k][i]; x[OUT_STEP] = o[n][k][i + 2]; }
             }
           }
       };
@@ -836,8 +969,8 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
             if (h < live)
 #pragma unroll
               for (int k = 0; k < KS; ++k) {
-                float* const x = dst + 16 * k + (E4M3 ? 2 * gq : gq);
-                float* const y = x + (E4M3 ? 1 : 8);
+                float* const x = dst + out_dim(k);
+                float* const y = x + OUT_STEP;
                 *x = *x * fa + o[0][k][i] * fb;
                 *y = *y * fa + o[0][k][i + 2] * fb;
               }
@@ -968,20 +1101,20 @@ attention_join_kernel(const __grid_constant__ Args g) {
 bool make_cache_map(CUtensorMap* out, const PagedCache& c) {
   EncodeTiledFn fn = tensor_map_encoder();
   if (!fn) return false;
-  const bool e4m3 = c.scale != nullptr;
-  const int row = c.head_dim * (e4m3 ? 1 : 2), box_row = row > 128 ? 128 : row;
-  const cuuint64_t dims[2] = {(cuuint64_t)c.head_dim, ((cuuint64_t)c.n_pages * 2 * c.kv_heads) << c.page_shift};
+  const bool two = c.format == ET_KV_BF16;                             // bytes an element of the map
+  const int row = kv_row_bytes(c.format, c.head_dim), box_row = row > 128 ? 128 : row;
+  const cuuint64_t dims[2] = {(cuuint64_t)(row / (two ? 2 : 1)), ((cuuint64_t)c.n_pages * 2 * c.kv_heads) << c.page_shift};
   const cuuint64_t strides[1] = {(cuuint64_t)row};
-  const cuuint32_t box[2] = {(cuuint32_t)(box_row / (e4m3 ? 1 : 2)), (cuuint32_t)(1 << (c.page_shift < 6 ? c.page_shift : 6))};
+  const cuuint32_t box[2] = {(cuuint32_t)(box_row / (two ? 2 : 1)), (cuuint32_t)(1 << (c.page_shift < 6 ? c.page_shift : 6))};
   const cuuint32_t estr[2] = {1, 1};
-  return fn(out, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.data, dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, box_row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+  return fn(out, two ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, c.data, dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, box_row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : box_row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int DH, bool E4M3, int NT>
+template <int DH, int FMT, int NT>
 cudaError_t launch(const CUtensorMap& map, const Args& g, int ctas, cudaStream_t s) {
-  using C = Cfg<DH, E4M3, NT>;
+  using C = Cfg<DH, FMT, NT>;
   static std::atomic<bool> ready[64];                                // per device
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -990,17 +1123,17 @@ cudaError_t launch(const CUtensorMap& map, const Args& g, int ctas, cudaStream_t
     if (NT == 2) {
       // setmaxnreg.inc waits for registers that only exist if the block was launched with LAUNCH_REGS of them a thread
       cudaFuncAttributes fa;
-      e = cudaFuncGetAttributes(&fa, attention_paged_kernel<DH, E4M3, NT>);
+      e = cudaFuncGetAttributes(&fa, attention_paged_kernel<DH, FMT, NT>);
       if (e != cudaSuccess) return e;
       if (fa.numRegs < LAUNCH_REGS) return cudaErrorLaunchOutOfResources;
     }
-    e = cudaFuncSetAttribute(attention_paged_kernel<DH, E4M3, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    e = cudaFuncSetAttribute(attention_paged_kernel<DH, FMT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) ready[dev] = true;
   }
   ET_COUNT_LAUNCH();
   Launch l(ctas, THREADS, C::SMEM, s);
-  e = cudaLaunchKernelEx(&l.cfg, attention_paged_kernel<DH, E4M3, NT>, map, g);
+  e = cudaLaunchKernelEx(&l.cfg, attention_paged_kernel<DH, FMT, NT>, map, g);
   if (e != cudaSuccess || g.whole) return e;
   ET_COUNT_LAUNCH();
   Launch join(dim3(ctas, g.group < C::HEADS ? g.group : C::HEADS), JOIN_THREADS, 0, s);
@@ -1025,8 +1158,9 @@ cudaError_t launch_attention_paged(const PagedCache& c, const PagedAttention& a,
   if (most >= (1ll << 31) - MAX_CTAS) return cudaErrorInvalidValue;   // refused by the entry point already
   const int ctas = (int)(most < MAX_CTAS ? most : MAX_CTAS);
 #define ET_PAGED(D, E) (nt == 1 ? launch<D, E, 1>(map, g, ctas, s) : launch<D, E, 2>(map, g, ctas, s))
-  if (c.head_dim == 64) return c.scale ? ET_PAGED(64, true) : ET_PAGED(64, false);
-  return c.scale ? ET_PAGED(128, true) : ET_PAGED(128, false);
+#define ET_PAGED_D(D) (c.format == ET_KV_INT4 ? ET_PAGED(D, ET_KV_INT4) : c.format == ET_KV_E4M3 ? ET_PAGED(D, ET_KV_E4M3) : ET_PAGED(D, ET_KV_BF16))
+  return c.head_dim == 64 ? ET_PAGED_D(64) : ET_PAGED_D(128);
+#undef ET_PAGED_D
 #undef ET_PAGED
 }
 

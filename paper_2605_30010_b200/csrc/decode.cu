@@ -5,14 +5,12 @@
 
 using namespace et;
 
-namespace {
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+namespace et {
 
 et_status check_cache(const et_kv_cache* c, PagedCache* out) {
   if (!c || !c->data) return ET_ERR_INVALID_ARG;
-  if (c->format != ET_KV_BF16 && c->format != ET_KV_E4M3) return ET_ERR_INVALID_ARG;
-  if ((c->format == ET_KV_E4M3) != (c->scale != nullptr)) return ET_ERR_INVALID_ARG;
+  if (c->format != ET_KV_BF16 && c->format != ET_KV_E4M3 && c->format != ET_KV_INT4) return ET_ERR_INVALID_ARG;
+  if ((c->format != ET_KV_BF16) != (c->scale != nullptr)) return ET_ERR_INVALID_ARG;
   if (!aligned16(c->data) || !aligned16(c->scale)) return ET_ERR_INVALID_ARG;
   if (c->n_pages < 1 || c->kv_heads < 1 || (c->head_dim != 64 && c->head_dim != 128)) return ET_ERR_SHAPE;
   int shift = 4;
@@ -20,9 +18,19 @@ et_status check_cache(const et_kv_cache* c, PagedCache* out) {
   if ((1 << shift) != c->page_size) return ET_ERR_SHAPE;
   // row numbers of the cache are 32-bit (TMA coordinates); byte offsets are 64-bit
   if ((long long)c->n_pages > ((1ll << 31) - 1) / (2ll * c->page_size) / c->kv_heads) return ET_ERR_CAPACITY;
-  *out = PagedCache{(uint8_t*)c->data, c->scale, c->n_pages, c->kv_heads, shift, c->head_dim};
+  *out = PagedCache{(uint8_t*)c->data, c->scale, c->n_pages, c->kv_heads, shift, c->head_dim, c->format};
   return ET_OK;
 }
+
+et_status launched(cudaError_t e) {
+  if (e == cudaSuccess) return ET_OK;
+  cudaGetLastError();
+  return ET_ERR_CUDA;
+}
+
+}  // namespace et
+
+namespace {
 
 et_status check_table(const int* table, int n_seq, int max_pages, int page_shift) {
   if (!table) return ET_ERR_INVALID_ARG;
@@ -58,13 +66,6 @@ const RopeTurns& rope_turns(float theta, int head_dim) {
     of_theta = theta; of_dim = head_dim;
   }
   return t;
-}
-
-// A launch's own result: an error that an earlier call left behind is not this call's, and none is left for a later one.
-et_status launched(cudaError_t e) {
-  if (e == cudaSuccess) return ET_OK;
-  cudaGetLastError();
-  return ET_ERR_CUDA;
 }
 
 }  // namespace

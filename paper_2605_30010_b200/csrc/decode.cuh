@@ -11,7 +11,22 @@ struct PagedCache {
   uint8_t* data;
   uint8_t* scale;        // NULL: bf16
   int n_pages, kv_heads, page_shift, head_dim;
+  int format;            // et_kv_format
 };
+// bytes of a row of head_dim values, and of its scales
+constexpr int INT4_BLOCK = 32;                    // values of a 4-bit row that share a scale
+__host__ __device__ constexpr int kv_row_bytes(int format, int head_dim) {
+  return format == ET_KV_BF16 ? 2 * head_dim : format == ET_KV_E4M3 ? head_dim : head_dim / 2;
+}
+__host__ __device__ constexpr int kv_scale_bytes(int format, int head_dim) {
+  return format == ET_KV_BF16 ? 0 : format == ET_KV_E4M3 ? 1 : 2 * (head_dim / INT4_BLOCK);
+}
+
+// Shared by the C entry points.
+static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+et_status check_cache(const et_kv_cache* c, PagedCache* out);
+// A launch's own result: an error that an earlier call left behind is not this call's, and none is left for a later one.
+et_status launched(cudaError_t e);
 
 // The rows of a call and the pages that they go to.
 struct PagedRows {

@@ -94,6 +94,34 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
   return v;
 }
 
+// ---- 4 bits.  A block of 32 values has one bf16 scale s, the smallest that is not below max|x| / 7, and codes n + 8 with n = x / s
+// rounded to nearest, ties to even.  Both follow what 64-bit arithmetic gives: a quotient from an approximate reciprocal is within
+// one of the right whole number, and the rest x - n s, which is exact (or off by 2^-53 of x where x has 64 bits), says which it is.
+__device__ __forceinline__ float next_bf16(float x) { return __int_as_float(__float_as_int(x) + 0x10000); }        // x >= 0
+__device__ __forceinline__ float int4_scale(double top) {
+  // the quotient cut off to bf16 is the one below, or the one that is sought, or (the product is rounded) one further below
+  float s = __int_as_float(__float_as_int((float)top * (1.f / 7)) & 0xffff0000);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) if (7.0 * s < top) s = next_bf16(s);
+  return s;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t int4_codes(const T (&x)[8], float s, float up, float inv) {      // inv = 1 / (s up), up a power of two
+  uint32_t w = 0;
+  const T h = (T)s * (T)0.5;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    float n = rintf((float)x[k] * up * inv);
+    const T r = sizeof(T) == 8 ? fma((double)-n, (double)s, (double)x[k]) : (T)fmaf(-n, s, (float)x[k]);
+    const bool odd = (int)n & 1;
+    if (r > h || (odd && r == h)) n += 1.f;
+    else if (r < -h || (odd && r == -h)) n -= 1.f;
+    w |= (uint32_t)((int)n + 8) << (4 * k);
+  }
+  return w;
+}
+constexpr uint32_t INT4_ZEROS = 0x88888888u;                 // eight codes of 0
+
 // x c - y s with two roundings (but for 2^-39 of x and y): x and y have 8 bits, c = c1 + c2 and s = s1 + s2 16 in their first parts,
 // so that the products of those are exact.
 __device__ __forceinline__ float turned_exactly(float x, float c1, float c2, float y, float s1, float s2) {
@@ -110,10 +138,11 @@ __device__ __forceinline__ float turned_exactly(float x, float c1, float c2, flo
 // e4m3 values, a sixteenth apart (now one in two million; 21 124 rows of 28 + 4 + 4 heads 87.6 -> 93.3 us).  Bound by memory, and with
 // e4m3 and rotation by instructions.
 // ---------------------------------------------------------------------------------------------
-template <int DH, bool E4M3, bool ROTATE>
+template <int DH, int FMT, bool ROTATE>
 __global__ void __launch_bounds__(THREADS)
 kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c, PagedRows r,
                  const __grid_constant__ RopeTurns turns, bf16* q_out, int* new_len, int rows_each, int parts) {
+  constexpr bool E4M3 = FMT == ET_KV_E4M3, INT4 = FMT == ET_KV_INT4;
   constexpr int HALF = DH / 2, CHUNKS = DH / 16, UNROLL = 2;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int part = warp % parts, chunk = lane % CHUNKS, head_lane = lane / CHUNKS;
@@ -159,10 +188,12 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
     if (!places.find(c, r, (int)row, page, place, pos)) continue;          // the same for all lanes
     constexpr bool EXACT = ROTATE && E4M3;
     float cs[8], sn[8], c1[8], s1[8];                        // EXACT: c1 + cs, s1 + sn
+    double cd[INT4 && ROTATE ? 8 : 1], sd[INT4 && ROTATE ? 8 : 1];
     if (ROTATE) {
       // HALF pairs, found by HALF lanes' worth of sincos and handed to the lanes that need them
       constexpr int EACH = HALF / 32 > 0 ? HALF / 32 : 1;
       float mc[EACH], ms[EACH], mc1[EACH], ms1[EACH];
+      double mcd[EACH], msd[EACH];
 #pragma unroll
       for (int j = 0; j < EACH; ++j) {
         const unsigned long long turn = (unsigned long long)pos * turns.f[(lane * EACH + j) % HALF];
@@ -173,6 +204,8 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
           ms1[j] = __int_as_float(__float_as_int((float)s) & 0xffffff00);
           mc[j] = (float)(c - mc1[j]);
           ms[j] = (float)(s - ms1[j]);
+        } else if (INT4) {
+          sincospi((double)(long long)turn * 0x1p-63, &msd[j], &mcd[j]);
         } else {
           sincospif(__ll2float_rn((long long)turn) * 0x1p-63f, &ms[j], &mc[j]);       // half turns in [-1, 1)
         }
@@ -180,6 +213,13 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const int from = (chunk * 8 + k) / EACH;
+        if constexpr (INT4 && ROTATE) {
+          cd[k] = __shfl_sync(0xffffffffu, mcd[k % EACH], from);
+          sd[k] = __shfl_sync(0xffffffffu, msd[k % EACH], from);
+          cs[k] = (float)cd[k];
+          sn[k] = (float)sd[k];
+          continue;
+        }
         cs[k] = __shfl_sync(0xffffffffu, mc[k % EACH], from);
         sn[k] = __shfl_sync(0xffffffffu, ms[k % EACH], from);
         if (EXACT) {
@@ -195,6 +235,20 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
         float a[8], b[8];
         unpack8(va[j], a);
         unpack8(vb[j], b);
+        // 4 bits: the codes of a key are those that 64-bit arithmetic gives.  With keys turned in fp32 one value in a few hundred
+        // thousand lies on the other side of a border between two codes, which is a seventh of the block's largest value.
+        double ad[INT4 && ROTATE ? 8 : 1], bd[INT4 && ROTATE ? 8 : 1];
+        const bool key = head >= heads && head < heads + c.kv_heads;
+        if constexpr (INT4 && ROTATE) {
+          if (key) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const double x = a[k], y = b[k];
+              ad[k] = x * cd[k] - y * sd[k];
+              bd[k] = y * cd[k] + x * sd[k];
+            }
+          }
+        }
         if (EXACT && head >= heads && head < heads + c.kv_heads) {
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
@@ -202,7 +256,7 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
             a[k] = turned_exactly(x, c1[k], cs[k], y, s1[k], sn[k]);
             b[k] = turned_exactly(y, c1[k], cs[k], x, -s1[k], -sn[k]);
           }
-        } else if (ROTATE && head < heads + c.kv_heads) {
+        } else if (ROTATE && head < (INT4 ? heads : heads + c.kv_heads)) {
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
             const float x = a[k], y = b[k], co = EXACT ? c1[k] + cs[k] : cs[k], si = EXACT ? s1[k] + sn[k] : sn[k];
@@ -226,11 +280,50 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
 #pragma unroll
           for (int o = CHUNKS / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         }
+        float sa = 0.f, sb = 0.f;                                // 4 bits: scales of the two blocks that this lane has values of
+        if constexpr (INT4) {
+          double ta = 0., tb = 0.;                               // infinite where the block has a value that is not finite
+          auto most = [](double& top, double x) { top = x <= 3.402823466e38 ? fmax(top, x) : (double)INFINITY; };
+          if (ROTATE && key) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) { most(ta, fabs(ad[ROTATE ? k : 0])); most(tb, fabs(bd[ROTATE ? k : 0])); }
+          } else {
+            float fa = 0.f, fb = 0.f;
+            auto most_f = [](float& top, float x) { top = x <= 3.402823466e38f ? fmaxf(top, x) : INFINITY; };
+#pragma unroll
+            for (int k = 0; k < 8; ++k) { most_f(fa, fabsf(a[k])); most_f(fb, fabsf(b[k])); }
+            ta = fa; tb = fb;
+          }
+#pragma unroll
+          for (int o = 1; o < INT4_BLOCK / 8; o <<= 1) {
+            ta = fmax(ta, __shfl_xor_sync(0xffffffffu, ta, o));
+            tb = fmax(tb, __shfl_xor_sync(0xffffffffu, tb, o));
+          }
+          sa = ta < INFINITY ? int4_scale(ta) : NAN;
+          sb = tb < INFINITY ? int4_scale(tb) : NAN;
+        }
         if (head >= heads && head < all_heads) {
           const int kvh = head - heads;
           const int plane = kvh >= c.kv_heads ? 1 : 0;
           const size_t at = cache_row(c, page, plane, kvh - plane * c.kv_heads, place);
-          if (E4M3) {
+          if constexpr (INT4) {
+            auto codes = [&](const auto& x, float s) {
+              if (!(s > 0.f)) return INT4_ZEROS;                 // a block of zeros, or of a scale that is NaN
+              const float up = s < 0x1p-100f ? 0x1p64f : 1.f;    // 1 / s would overflow
+              return int4_codes(x, s, up, 1.f / (s * up));
+            };
+            uint32_t* dst = reinterpret_cast<uint32_t*>(c.data + at * (DH / 2) + chunk * 4);
+            if (ROTATE && key) {
+              if constexpr (ROTATE) { dst[0] = codes(ad, sa); dst[HALF / 8] = codes(bd, sb); }
+            } else {
+              dst[0] = codes(a, sa); dst[HALF / 8] = codes(b, sb);
+            }
+            if (chunk % (INT4_BLOCK / 8) == 0) {
+              bf16* scale = reinterpret_cast<bf16*>(c.scale) + at * (DH / INT4_BLOCK) + chunk / (INT4_BLOCK / 8);
+              scale[0] = __float2bfloat16_rn(sa);
+              scale[HALF / INT4_BLOCK] = __float2bfloat16_rn(sb);
+            }
+          } else if (E4M3) {
             const int e = e4m3_exponent(top);
             const float inv = pow2(-e);
             uint2* dst = reinterpret_cast<uint2*>(c.data + at * DH + chunk * 8);
@@ -253,12 +346,14 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
 
 // ---------------------------------------------------------------------------------------------
 // Read: a warp (or `parts` of them) takes a row, a lane 16 bytes of the cache at a time (8 bf16 or 16 e4m3 values), four of
-// them on their way.  Bound by memory.
+// them on their way; of 4-bit values 4 bytes, eight of them on their way, so that what it writes stays 16 bytes next to its
+// neighbours'.  Bound by memory.
 // ---------------------------------------------------------------------------------------------
-template <int DH, bool E4M3>
+template <int DH, int FMT>
 __global__ void __launch_bounds__(THREADS)
 kv_read_kernel(bf16* out, long long row_stride, PagedCache c, PagedRows r, int rows_each, int parts) {
-  constexpr int VEC = E4M3 ? 16 : 8, CHUNKS = DH / VEC, UNROLL = 4;
+  constexpr bool E4M3 = FMT == ET_KV_E4M3, INT4 = FMT == ET_KV_INT4;
+  constexpr int VEC = E4M3 ? 16 : 8, CHUNKS = DH / VEC, UNROLL = INT4 ? 8 : 4;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % parts;
   const int units = 2 * c.kv_heads * CHUNKS;
   begin_after_previous();
@@ -281,7 +376,10 @@ kv_read_kernel(bf16* out, long long row_stride, PagedCache c, PagedRows r, int r
         if (u < units) {
           const int plane = head >= c.kv_heads ? 1 : 0;
           const size_t at = cache_row(c, page, plane, head - plane * c.kv_heads, place);
-          v[j] = *reinterpret_cast<const uint4*>(c.data + at * (DH * (E4M3 ? 1 : 2)) + chunk * 16);
+          if (INT4) {
+            v[j].x = *reinterpret_cast<const uint32_t*>(c.data + at * (DH / 2) + chunk * 4);
+            b[j] = (reinterpret_cast<const uint16_t*>(c.scale))[at * (DH / INT4_BLOCK) + chunk / (INT4_BLOCK / 8)];
+          } else v[j] = *reinterpret_cast<const uint4*>(c.data + at * (DH * (E4M3 ? 1 : 2)) + chunk * 16);
           if (E4M3) b[j] = c.scale[at];
         }
       }
@@ -290,7 +388,13 @@ kv_read_kernel(bf16* out, long long row_stride, PagedCache c, PagedRows r, int r
         const int u = u0 + 32 * j;
         if (u >= units) continue;
         uint4* dst = reinterpret_cast<uint4*>(dst_row + (size_t)u * VEC);
-        if (E4M3) {
+        if (INT4) {
+          const float s = __int_as_float(b[j] << 16);
+          float y[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) y[k] = (float)((int)(v[j].x >> (4 * k) & 15) - 8) * s;
+          *dst = pack8(y);
+        } else if (E4M3) {
           const float f = pow2(b[j] - 127);
           const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
           float lo[8], hi[8];
@@ -335,8 +439,9 @@ cudaError_t launch_kv_append(const PagedCache& c, const PagedRows& r, const bf16
 #define ET_APPEND(D, E, R) return cudaLaunchKernelEx(&l.cfg, kv_append_kernel<D, E, R>, qkv, row_stride, heads, c, r, turns, q_out, new_len, d.each, d.parts)
 #define ET_APPEND_D(D)                                                       \
   do {                                                                       \
-    if (c.scale) { if (rotate) ET_APPEND(D, true, true); else ET_APPEND(D, true, false); }   \
-    else { if (rotate) ET_APPEND(D, false, true); else ET_APPEND(D, false, false); }         \
+    if (c.format == ET_KV_INT4) { if (rotate) ET_APPEND(D, ET_KV_INT4, true); else ET_APPEND(D, ET_KV_INT4, false); }   \
+    else if (c.format == ET_KV_E4M3) { if (rotate) ET_APPEND(D, ET_KV_E4M3, true); else ET_APPEND(D, ET_KV_E4M3, false); }   \
+    else { if (rotate) ET_APPEND(D, ET_KV_BF16, true); else ET_APPEND(D, ET_KV_BF16, false); }                         \
   } while (0)
   if (c.head_dim == 64) ET_APPEND_D(64); else ET_APPEND_D(128);
 #undef ET_APPEND_D
@@ -345,11 +450,17 @@ cudaError_t launch_kv_append(const PagedCache& c, const PagedRows& r, const bf16
 
 cudaError_t launch_kv_read(const PagedCache& c, const PagedRows& r, bf16* out, long long row_stride, cudaStream_t s) {
   ET_COUNT_LAUNCH();
-  const Deal d = deal_rows(r.rows, cdiv(2 * c.kv_heads * c.head_dim / (c.scale ? 16 : 8), 128));
+  const Deal d = deal_rows(r.rows, cdiv(2 * c.kv_heads * c.head_dim / (c.format == ET_KV_E4M3 ? 16 : 8), c.format == ET_KV_INT4 ? 256 : 128));
   Launch l(d.blocks, THREADS, 0, s);
 #define ET_READ(D, E) return cudaLaunchKernelEx(&l.cfg, kv_read_kernel<D, E>, out, row_stride, c, r, d.each, d.parts)
-  if (c.head_dim == 64) { if (c.scale) ET_READ(64, true); else ET_READ(64, false); }
-  else { if (c.scale) ET_READ(128, true); else ET_READ(128, false); }
+#define ET_READ_D(D)                                                         \
+  do {                                                                       \
+    if (c.format == ET_KV_INT4) ET_READ(D, ET_KV_INT4);                      \
+    else if (c.format == ET_KV_E4M3) ET_READ(D, ET_KV_E4M3);                 \
+    else ET_READ(D, ET_KV_BF16);                                             \
+  } while (0)
+  if (c.head_dim == 64) ET_READ_D(64); else ET_READ_D(128);
+#undef ET_READ_D
 #undef ET_READ
 }
 
