@@ -32,10 +32,27 @@ EXPORTS = ["et_encoder_create", "et_encode_video", "et_encode_batch", "et_encode
            "et_llm_create", "et_llm_prefill", "et_llm_destroy", "et_llm_last_error", "et_llm_profile_enable",
            "et_llm_profile_read", "et_rmsnorm", "et_rope", "et_swiglu", "et_attention_causal",
            # include/earlytom_decode.h
-           "et_kv_append", "et_kv_read", "et_attention_paged", "et_linear_rows"]
+           "et_kv_append", "et_kv_read", "et_attention_paged", "et_linear_rows",
+           # include/earlytom_pages.h
+           "et_pages_update", "et_pages_fork", "et_kv_copy", "et_beam_select"]
 ET_KV_BF16, ET_KV_E4M3, ET_KV_INT4 = 0, 1, 2
 ET_PAGED_CAPACITY, ET_PAGED_BAD_PAGE = 3, 5        # values of a paged call's status word
+ET_PAGED_NO_PAGE, ET_PAGED_BAD_COUNT, ET_PAGED_BAD_ROW = 6, 7, 8
 ET_PAGED_WORKSPACE = 4 << 20
+ET_BEAM_CHUNK = 4096
+
+
+def ET_PAGES_WORKSPACE(n_pages: int, n_seq: int) -> int:
+    return 4 * n_pages + 8 * n_seq
+
+
+def ET_FORK_WORKSPACE(n_pages: int, n_new: int) -> int:
+    return 4 * n_pages + 16 * n_new
+
+
+def ET_BEAM_WORKSPACE(rows: int, vocab: int, k: int) -> int:
+    return rows * (-(-vocab // ET_BEAM_CHUNK)) * (8 * k + 16)
+
 
 
 class EarlyTomError(RuntimeError):
@@ -192,6 +209,10 @@ def load_library(path: str = _LIB_PATH) -> C.CDLL:
     lib.et_kv_read.argtypes = [vp, vp, ll, i, vp, i, i, vp, vp, vp, vp]
     lib.et_attention_paged.argtypes = [vp, vp, ll, vp, vp, i, i, vp, i, vp, vp, C.c_size_t, vp, vp]
     lib.et_linear_rows.argtypes = [vp, vp, vp, vp, i, i, i, i, i, vp, vp]
+    lib.et_pages_update.argtypes = [vp, i, i, vp, i, i, vp, vp, vp, vp, vp, vp, i, vp, C.c_size_t, vp, vp]
+    lib.et_pages_fork.argtypes = [vp, i, i, vp, i, i, vp, vp, i, vp, vp, vp, vp, C.c_size_t, vp, vp]
+    lib.et_kv_copy.argtypes = [vp, vp, i, vp, vp]
+    lib.et_beam_select.argtypes = [vp, i, ll, i, i, i, vp, vp, i, i, vp, vp, vp, vp, vp, C.c_size_t, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name.startswith("et_") and name not in ("et_destroy", "et_status_string", "et_last_error",
@@ -984,3 +1005,137 @@ def et_linear_rows(a, w, bias=None, epilogue=0, gelu_tanh=1, c=None, status=None
     if st:
         _check(st)
     return c
+
+
+# --------------------------------------------------------------------------------------------
+# Pages of the cache and beam search (include/earlytom_pages.h)
+# --------------------------------------------------------------------------------------------
+
+def _workspace(workspace, size, like, stream):
+    if workspace is None:
+        return _new(_torch.empty, size, _torch.uint8, like, stream)
+    if not workspace.is_contiguous():
+        _refuse("workspace: contiguous")
+    return workspace
+
+
+def _vector(t, what):
+    """The length of a contiguous int32 vector."""
+    if t.dtype is not _torch.int32 or t.dim() != 1 or not t.is_contiguous():
+        _refuse(f"{what}: contiguous int32 vector")
+    return t.shape[0]
+
+
+def et_pages_update(refs, page_size, block_table, lens, keep=None, add=None, new_len=None, row_offsets=None, slots=None, status=None,
+                    workspace=None, stream=None):
+    """Sequences keep the first keep of their lens positions (None: all) and get add more (None: one each).  refs int32 [n_pages] and
+    block_table follow in place; returns new_len (created if none is given; may be lens).  row_offsets int32 [n_seq + 1] and slots
+    int32 [rows] are filled if given."""
+    if _torch is None:
+        _import_torch()
+    n_seq, max_pages = _table(block_table)
+    n_pages = _vector(refs, "refs")
+    for t, what in ((lens, "lens"), (keep, "keep"), (add, "add"), (new_len, "new_len")):
+        if t is not None:
+            _ints(t, n_seq, what)
+    if row_offsets is not None:
+        _ints(row_offsets, n_seq + 1, "row_offsets")
+    rows = 0 if slots is None else _vector(slots, "slots")
+    if status is not None:
+        _ints(status, 1, "status")
+    if new_len is None:
+        new_len = _new(_torch.empty, (n_seq,), _torch.int32, lens, stream)
+    workspace = _workspace(workspace, ET_PAGES_WORKSPACE(n_pages, n_seq), refs, stream)
+    s = _launch_on(stream, refs, block_table, lens, keep, add, new_len, row_offsets, slots, workspace, status)
+    st = lib().et_pages_update(refs.data_ptr(), n_pages, page_size, block_table.data_ptr(), n_seq, max_pages, lens.data_ptr(), _at(keep),
+                               _at(add), new_len.data_ptr(), _at(row_offsets), _at(slots), rows, workspace.data_ptr(),
+                               workspace.numel() * workspace.element_size(), _at(status), s)
+    if st:
+        _check(st)
+    return new_len
+
+
+def et_pages_fork(refs, page_size, block_table, lens, parent, new_table, new_len=None, copies=None, status=None, workspace=None,
+                  stream=None):
+    """Rows of new_table continue rows parent of block_table, whose rows end; refs follows in place.  Returns (new_len, copies):
+    int32 [n_new], and int32 [n_new, 3] for et_kv_copy; created if none are given."""
+    if _torch is None:
+        _import_torch()
+    n_old, max_pages = _table(block_table)
+    n_new, columns = _table(new_table)
+    if columns != max_pages:
+        _refuse("new_table: as many columns as block_table")
+    n_pages = _vector(refs, "refs")
+    _ints(lens, n_old, "lens")
+    _ints(parent, n_new, "parent")
+    if status is not None:
+        _ints(status, 1, "status")
+    if new_len is None:
+        new_len = _new(_torch.empty, (n_new,), _torch.int32, lens, stream)
+    _ints(new_len, n_new, "new_len")
+    if copies is None:
+        copies = _new(_torch.empty, (n_new, 3), _torch.int32, lens, stream)
+    _ints(copies, 3 * n_new, "copies")
+    workspace = _workspace(workspace, ET_FORK_WORKSPACE(n_pages, n_new), refs, stream)
+    s = _launch_on(stream, refs, block_table, lens, parent, new_table, new_len, copies, workspace, status)
+    st = lib().et_pages_fork(refs.data_ptr(), n_pages, page_size, block_table.data_ptr(), n_old, max_pages, lens.data_ptr(),
+                             parent.data_ptr(), n_new, new_table.data_ptr(), new_len.data_ptr(), copies.data_ptr(), workspace.data_ptr(),
+                             workspace.numel() * workspace.element_size(), _at(status), s)
+    if st:
+        _check(st)
+    return new_len, copies
+
+
+def et_kv_copy(cache, scale, copies, status=None, stream=None):
+    """Copies positions of pages within a layer's cache: copies int32 [n, 3] = (from, to, positions) as et_pages_fork leaves it."""
+    if _torch is None:
+        _import_torch()
+    c, _, _ = _kv_cache(cache, scale)
+    if copies.dtype is not _torch.int32 or copies.dim() != 2 or copies.shape[1] != 3 or not copies.is_contiguous():
+        _refuse("copies: contiguous int32 [n, 3]")
+    if status is not None:
+        _ints(status, 1, "status")
+    s = _launch_on(stream, cache, scale, copies, status)
+    st = lib().et_kv_copy(c, copies.data_ptr(), copies.shape[0], _at(status), s)
+    if st:
+        _check(st)
+
+
+def et_beam_select(logits, beams, k, scores=None, done=None, eos=-1, parent=None, token=None, new_scores=None, new_done=None,
+                   workspace=None, stream=None):
+    """The k best continuations of each request's beams: logits [n_req * beams, vocab] fp32 or bf16, scores fp32 and done bool of its
+    rows.  Returns (parent, token, new_scores, new_done), int32, int32, fp32 and bool [n_req * k], created if none are given."""
+    if _torch is None:
+        _import_torch()
+    if logits.dim() != 2 or logits.dtype not in (_torch.float32, _torch.bfloat16) or (logits.stride(1) != 1 and logits.shape[1] > 1):
+        _refuse("logits: fp32 or bf16 [n_req * beams, vocab] with contiguous columns")
+    rows, vocab = logits.shape
+    if beams < 1 or k < 1 or rows % beams != 0:
+        _refuse("logits: a row for each of n_req * beams beams, beams >= 1, k >= 1")
+    n_req = rows // beams
+    outs = n_req * k
+    if parent is None:
+        parent = _new(_torch.empty, (outs,), _torch.int32, logits, stream)
+    if token is None:
+        token = _new(_torch.empty, (outs,), _torch.int32, logits, stream)
+    if new_scores is None:
+        new_scores = _new(_torch.empty, (outs,), _torch.float32, logits, stream)
+    if new_done is None:
+        new_done = _new(_torch.empty, (outs,), _torch.bool, logits, stream)
+    _ints(parent, outs, "parent")
+    _ints(token, outs, "token")
+    for t, n, what in ((scores, rows, "scores"), (new_scores, outs, "new_scores")):
+        if t is not None and (t.dtype is not _torch.float32 or t.numel() != n or not t.is_contiguous()):
+            _refuse(f"{what}: contiguous float32 [{n}]")
+    for t, n, what in ((done, rows, "done"), (new_done, outs, "new_done")):
+        if t is not None and (t.dtype not in (_torch.bool, _torch.uint8) or t.numel() != n or not t.is_contiguous()):
+            _refuse(f"{what}: contiguous bool [{n}]")
+    workspace = _workspace(workspace, ET_BEAM_WORKSPACE(rows, vocab, k), logits, stream)
+    s = _launch_on(stream, logits, scores, done, parent, token, new_scores, new_done, workspace)
+    stride = logits.stride(0) if rows > 1 else max(logits.stride(0), vocab)
+    st = lib().et_beam_select(logits.data_ptr(), int(logits.dtype is _torch.float32), stride, n_req, beams, vocab, _at(scores), _at(done),
+                              eos, k, parent.data_ptr(), token.data_ptr(), new_scores.data_ptr(), new_done.data_ptr(),
+                              workspace.data_ptr(), workspace.numel() * workspace.element_size(), s)
+    if st:
+        _check(st)
+    return parent, token, new_scores, new_done

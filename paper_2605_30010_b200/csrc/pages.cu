@@ -1,0 +1,444 @@
+// Pages of the cache, handed out and taken back on the device, and the beams' tables that follow a selection.
+//
+// What a step changes is little (a page for one sequence in page_size, a row of a table for each beam), so these calls are bound by
+// latency: by launches, and by loads that wait for one another.
+//
+//   * The free pages are those whose count is 0, the i-th one the one with i smaller ones: there is no list to keep, so counts can be
+//     changed by whoever likes, in any order, with the same result.  What it costs is a look at all counts (4 bytes a page).
+//   * The parts of et_pages_update that depend on everything (which pages are free, how many pages and rows the sequences before
+//     take) are done by one cluster of eight CTAs, whose barrier costs a fraction of a launch: each CTA owns an eighth of the sequences
+//     and of the counts, totals go round through distributed shared memory.
+//   * Work of uneven sequences is dealt to threads entry by entry: a prefix sum over the sequences, and a search in it.
+#include "decode.cuh"
+#include "earlytom_pages.h"
+
+namespace et {
+
+namespace {
+
+constexpr int CLUSTER = 8, THREADS = 1024, WARPS = THREADS / 32;
+constexpr int SEGMENTS = CLUSTER * WARPS;          // each warp of the cluster looks for free pages in one of them
+
+__device__ __forceinline__ int cluster_rank() {
+  int r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// *p = v in the shared memory of CTA `cta` of the cluster
+__device__ __forceinline__ void store_in(int* p, int cta, int v) {
+  const uint32_t own = (uint32_t)__cvta_generic_to_shared(p);
+  uint32_t there;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(own), "r"(cta));
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(there), "r"(v) : "memory");
+}
+__device__ __forceinline__ void report(int* status, int code) { if (status) atomicMax(status, code); }
+
+// Exclusive sum over the block's threads; `total`: all of them.  One barrier behind the last use of `sums` is the caller's.
+__device__ __forceinline__ int block_scan(int v, int* sums, int& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int inc = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int u = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += u; }
+  __syncthreads();                                 // sums is free
+  if (lane == 31) sums[warp] = inc;
+  __syncthreads();
+  int w = sums[lane];                              // WARPS is 32
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int u = __shfl_up_sync(0xffffffffu, w, o); if (lane >= o) w += u; }
+  total = __shfl_sync(0xffffffffu, w, 31);
+  const int before = __shfl_sync(0xffffffffu, w, warp ? warp - 1 : 0);
+  return inc - v + (warp ? before : 0);
+}
+
+// The last i of [0, n) with prefix[i] <= x (prefix ascending, prefix[0] <= x)
+__device__ __forceinline__ int search(const int* prefix, int n, int x) {
+  int lo = 0;
+  while (n > 1) {
+    const int half = n >> 1;
+    if (prefix[lo + half] <= x) { lo += half; n -= half; } else n = half;
+  }
+  return lo;
+}
+
+// ---- free pages -------------------------------------------------------------------------------------------------------------------
+// Each warp writes the free pages of its segment to the workspace, at the segment's own place; the segments' counts go to all CTAs.
+// pages of a segment, a multiple of 32
+__device__ __forceinline__ int segment_size(int n_pages) { return ((n_pages + SEGMENTS - 1) / SEGMENTS + 31) & ~31; }
+
+__device__ __forceinline__ void collect_free(const int* refs, int n_pages, int rank, int* list, int* counts) {
+  const int lane = threadIdx.x & 31, segment = rank * WARPS + (threadIdx.x >> 5), size = segment_size(n_pages);
+  const int begin = min((long long)segment * size, (long long)n_pages), end = min((long long)begin + size, (long long)n_pages);
+  constexpr int AHEAD = 8;
+  int found = 0;
+  for (int p0 = begin; p0 < end; p0 += 32 * AHEAD) {
+    int r[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) r[j] = p0 + 32 * j + lane < end ? __ldcg(refs + p0 + 32 * j + lane) : 1;
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const unsigned free = __ballot_sync(0xffffffffu, r[j] == 0);
+      if (r[j] == 0) list[begin + found + __popc(free & ((1u << lane) - 1))] = p0 + 32 * j + lane;
+      found += __popc(free);
+    }
+  }
+  if (lane < CLUSTER) store_in(counts + segment, lane, found);
+}
+// Behind the cluster's barrier: counts become an exclusive sum; returns how many free pages there are.
+__device__ __forceinline__ int sum_segments(int* counts, int* sums) {
+  int total;
+  const int v = threadIdx.x < SEGMENTS ? counts[threadIdx.x] : 0, before = block_scan(v, sums, total);
+  if (threadIdx.x < SEGMENTS) counts[threadIdx.x] = before;
+  __syncthreads();
+  return total;
+}
+__device__ __forceinline__ int free_page(const int* list, const int* counts, int n_pages, int i) {
+  const int segment = search(counts, SEGMENTS, i);
+  return __ldcg(list + (size_t)segment * segment_size(n_pages) + i - counts[segment]);
+}
+
+// ---- et_pages_update --------------------------------------------------------------------------------------------------------------
+struct Update {
+  int* refs;
+  int* table;
+  const int* len;
+  const int* keep;        // may be NULL
+  const int* add;         // may be NULL
+  int* new_len;
+  int* offsets;           // may be NULL
+  int* slots;             // may be NULL
+  int* list;              // workspace: [n_pages] free pages,
+  int* row0;              // [n_seq] first row,
+  int* start;             // [n_seq] position of the first row, -1: none was got
+  int n_pages, page_shift, n_seq, max_pages, rows;
+  int* status;
+};
+
+struct Turn { int kept, add, stay, drop, take; bool fits; };
+__device__ __forceinline__ int entries_of(long long n, int shift) { return (int)((n + (1 << shift) - 1) >> shift); }
+__device__ __forceinline__ Turn turn_of(const Update& u, int s) {
+  const int cap = u.max_pages << u.page_shift;     // <= 2^30
+  const int len = u.len[s], held = min(max(len, 0), cap);
+  Turn t;
+  t.kept = u.keep ? min(u.keep[s], held) : len < 0 ? -1 : held;
+  if (t.kept < 0) t.kept = -1;
+  t.add = t.kept < 0 ? 0 : u.add ? max(u.add[s], 0) : 1;
+  t.stay = entries_of(max(t.kept, 0), u.page_shift);
+  t.drop = entries_of(held, u.page_shift) - t.stay;
+  t.fits = (long long)t.kept + t.add <= cap;
+  t.take = t.fits ? entries_of(max(t.kept, 0) + t.add, u.page_shift) - t.stay : 0;
+  return t;
+}
+
+__device__ __forceinline__ int slot_of(const Update& u, int row, int total) {
+  if (row >= total) return -1;
+  const int s = search(u.row0, u.n_seq, row), start = __ldcg(u.start + s);
+  const long long pos = (long long)start + row - u.row0[s];
+  if (start < 0 || pos < 0 || pos >> u.page_shift >= u.max_pages) return -1;
+  const int page = __ldcg(u.table + (size_t)s * u.max_pages + (pos >> u.page_shift));
+  if ((unsigned)page >= (unsigned)u.n_pages) { report(u.status, ET_PAGED_BAD_PAGE); return -1; }
+  return (page << u.page_shift) + (int)(pos & ((1 << u.page_shift) - 1));
+}
+
+__global__ void __launch_bounds__(THREADS, 1)
+pages_update_kernel(const __grid_constant__ Update u, bool slots_here) {
+  __shared__ int counts[SEGMENTS], totals[2][CLUSTER], sums[WARPS], prefix[THREADS], stay_s[THREADS], got_s[THREADS];
+  const int tid = threadIdx.x, rank = cluster_rank();
+  const int per = (u.n_seq + CLUSTER - 1) / CLUSTER, s0 = min(rank * per, u.n_seq), s1 = min(s0 + per, u.n_seq);
+  begin_after_previous();
+  // ---- entries are given back; what is asked for is added up
+  int take = 0, rows = 0;
+  for (int b = s0; b < s1; b += THREADS) {
+    const int s = b + tid;
+    Turn t{};
+    if (s < s1) t = turn_of(u, s);
+    take += t.take; rows += t.add;
+    int dropped;
+    const int before = block_scan(t.drop, sums, dropped);
+    if (dropped == 0) continue;
+    prefix[tid] = before; stay_s[tid] = t.stay;
+    __syncthreads();
+    for (int i = tid; i < dropped; i += THREADS) {
+      const int k = search(prefix, min(THREADS, s1 - b), i);
+      int* const entry = u.table + (size_t)(b + k) * u.max_pages + stay_s[k] + i - prefix[k];
+      const int page = *entry;
+      *entry = -1;
+      if ((unsigned)page >= (unsigned)u.n_pages) report(u.status, ET_PAGED_BAD_PAGE);
+      else if (atomicSub(u.refs + page, 1) <= 0) {
+        atomicAdd(u.refs + page, 1);
+        report(u.status, ET_PAGED_BAD_COUNT);
+      }
+    }
+    __syncthreads();
+  }
+  int take_cta, rows_cta;
+  block_scan(take, sums, take_cta);
+  block_scan(rows, sums, rows_cta);
+  cluster_sync();                                  // all counts have come down (and all CTAs have begun)
+  if (tid < CLUSTER) { store_in(&totals[0][rank], tid, take_cta); store_in(&totals[1][rank], tid, rows_cta); }
+  collect_free(u.refs, u.n_pages, rank, u.list, counts);
+  cluster_sync();
+  const int n_free = sum_segments(counts, sums);
+  int taken = 0, row = 0, rows_all = 0;            // by the sequences before
+  for (int c = 0; c < CLUSTER; ++c) {
+    if (c < rank) { taken += totals[0][c]; row += totals[1][c]; }
+    rows_all += totals[1][c];
+  }
+  // ---- entries are taken
+  for (int b = s0; b < s1; b += THREADS) {
+    const int s = b + tid;
+    Turn t{};
+    if (s < s1) t = turn_of(u, s);
+    int take_all, rows_batch;
+    const int before = block_scan(t.take, sums, take_all), rows_before = block_scan(t.add, sums, rows_batch);
+    const bool got = t.fits && (t.take == 0 || taken + before + t.take <= n_free);
+    if (s < s1) {
+      if (!got) report(u.status, t.fits ? (int)ET_PAGED_NO_PAGE : (int)ET_PAGED_CAPACITY);
+      u.new_len[s] = t.kept < 0 ? -1 : t.kept + (got ? t.add : 0);
+      if (u.offsets) u.offsets[s] = row + rows_before;
+      if (u.slots) { u.row0[s] = row + rows_before; u.start[s] = got ? t.kept : -1; }
+    }
+    prefix[tid] = before; stay_s[tid] = t.stay; got_s[tid] = got;
+    __syncthreads();
+    for (int i = tid; i < take_all; i += THREADS) {
+      const int k = search(prefix, min(THREADS, s1 - b), i);
+      int page = -1;
+      if (got_s[k]) {
+        page = free_page(u.list, counts, u.n_pages, taken + i);
+        u.refs[page] = 1;
+      }
+      u.table[(size_t)(b + k) * u.max_pages + stay_s[k] + i - prefix[k]] = page;
+    }
+    taken += take_all; row += rows_batch;
+    __syncthreads();
+  }
+  if (rank == 0 && tid == 0) {
+    if (u.offsets) u.offsets[u.n_seq] = rows_all;
+    if (u.slots && rows_all > u.rows) report(u.status, ET_PAGED_CAPACITY);
+  }
+  cluster_sync();                                  // also: no CTA ends while another may write into its shared memory
+  if (slots_here) {
+    for (int r = rank * THREADS + tid; r < u.rows; r += CLUSTER * THREADS) u.slots[r] = slot_of(u, r, rows_all);
+  } else if (rank == 0 && tid == 0) {
+    u.list[0] = rows_all;                          // for the next kernel; the free pages have been dealt
+  }
+}
+
+// Slots of many rows: four of them a thread.
+constexpr int SLOT_THREADS = 256, SLOT_ROWS = 4, SLOTS_HERE = 2 * CLUSTER * THREADS;
+__global__ void __launch_bounds__(SLOT_THREADS)
+slots_kernel(const __grid_constant__ Update u) {
+  begin_after_previous();
+  const int all = u.list[0];
+  const int r0 = (blockIdx.x * SLOT_THREADS + threadIdx.x) * SLOT_ROWS;
+  for (int r = r0; r < min(r0 + SLOT_ROWS, u.rows); ++r) u.slots[r] = slot_of(u, r, all);
+}
+
+// ---- et_pages_fork ----------------------------------------------------------------------------------------------------------------
+struct Fork {
+  int* refs;
+  const int* table;
+  const int* len;
+  const int* parent;
+  int* new_table;
+  int* new_len;
+  int* copies;
+  int* list;              // workspace: [n_pages] free pages,
+  int* family;            // [n_new] how many rows the row's parent has, negative for the first of them
+  int n_pages, page_shift, n_old, n_new, max_pages;
+  int* status;
+};
+
+// A block takes an old row (or a slice of it) to its children; the counts of its pages go up by one less than it has children.
+constexpr int FORK_THREADS = 256;
+__global__ void __launch_bounds__(FORK_THREADS)
+fork_rows_kernel(const __grid_constant__ Fork f) {
+  extern __shared__ unsigned short children[];
+  __shared__ int n_children, first;
+  const int p = blockIdx.x, tid = threadIdx.x;
+  begin_after_previous();
+  if (tid == 0) { n_children = 0; first = f.n_new; }
+  __syncthreads();
+  for (int b = tid; b < f.n_new; b += FORK_THREADS)
+    if (f.parent[b] == p) { children[atomicAdd(&n_children, 1)] = (unsigned short)b; atomicMin(&first, b); }
+  __syncthreads();
+  const int n = n_children;
+  if (blockIdx.y == 0) for (int i = tid; i < n; i += FORK_THREADS) f.family[children[i]] = children[i] == first ? -n : n;
+  const int used = min(entries_of(max(f.len[p], 0), f.page_shift), f.max_pages);
+  for (int c = blockIdx.y * FORK_THREADS + tid; c < used; c += gridDim.y * FORK_THREADS) {
+    const int page = f.table[(size_t)p * f.max_pages + c];
+    if ((unsigned)page >= (unsigned)f.n_pages) report(f.status, ET_PAGED_BAD_PAGE);
+    else if (n > 1) atomicAdd(f.refs + page, n - 1);
+    else if (n == 0 && atomicSub(f.refs + page, 1) <= 0) {
+      atomicAdd(f.refs + page, 1);
+      report(f.status, ET_PAGED_BAD_COUNT);
+    }
+    for (int i = 0; i < n; ++i) f.new_table[(size_t)children[i] * f.max_pages + c] = page;
+  }
+}
+
+// Half-filled last pages: which rows need one of their own, and which it is.
+constexpr int FORK_EACH = 2, FORK_ROWS = 16384;
+static_assert(CLUSTER * THREADS * FORK_EACH >= FORK_ROWS, "rows of a thread");
+__global__ void __launch_bounds__(THREADS, 1)
+fork_last_pages_kernel(const __grid_constant__ Fork f) {
+  __shared__ int counts[SEGMENTS], totals[CLUSTER], sums[WARPS];
+  const int tid = threadIdx.x, rank = cluster_rank();
+  const int per = (f.n_new + CLUSTER - 1) / CLUSTER, b0 = rank * per, b1 = min(b0 + per, f.n_new);
+  cluster_sync();                                  // all CTAs have begun
+  begin_after_previous();
+  int old[FORK_EACH], length[FORK_EACH];
+  bool own[FORK_EACH];
+  int wanted = 0;
+#pragma unroll
+  for (int j = 0; j < FORK_EACH; ++j) {
+    const int b = b0 + tid * FORK_EACH + j;
+    own[j] = false; old[j] = -1; length[j] = -1;
+    if (b >= b1) continue;
+    const int p = f.parent[b];
+    if (p >= f.n_old) report(f.status, ET_PAGED_BAD_ROW);
+    if ((unsigned)p >= (unsigned)f.n_old) continue;
+    length[j] = max(f.len[p], -1);
+    const int column = length[j] >> f.page_shift;
+    if (length[j] <= 0 || (length[j] & ((1 << f.page_shift) - 1)) == 0 || column >= f.max_pages) continue;
+    old[j] = f.new_table[(size_t)b * f.max_pages + column];
+    if ((unsigned)old[j] >= (unsigned)f.n_pages) continue;
+    const int n = f.family[b];
+    own[j] = !(n < 0 && __ldcg(f.refs + old[j]) == -n);
+    wanted += own[j];
+  }
+  int all;
+  int i = block_scan(wanted, sums, all);
+  if (tid < CLUSTER) store_in(totals + rank, tid, all);
+  collect_free(f.refs, f.n_pages, rank, f.list, counts);
+  cluster_sync();                                  // counts change from here on
+  const int n_free = sum_segments(counts, sums);
+  for (int c = 0; c < rank; ++c) i += totals[c];
+#pragma unroll
+  for (int j = 0; j < FORK_EACH; ++j) {
+    const int b = b0 + tid * FORK_EACH + j;
+    if (b >= b1) continue;
+    int from = -1, to = -1, n = 0;
+    if (own[j]) {
+      const int column = length[j] >> f.page_shift;
+      atomicSub(f.refs + old[j], 1);
+      if (i < n_free) {
+        from = old[j]; to = free_page(f.list, counts, f.n_pages, i); n = length[j] & ((1 << f.page_shift) - 1);
+        f.refs[to] = 1;
+      } else {
+        report(f.status, ET_PAGED_NO_PAGE);
+      }
+      f.new_table[(size_t)b * f.max_pages + column] = to;
+      ++i;
+    }
+    f.new_len[b] = length[j];
+    f.copies[3 * b] = from; f.copies[3 * b + 1] = to; f.copies[3 * b + 2] = n;
+  }
+  cluster_sync();                                  // no CTA ends while another may write into its shared memory
+}
+
+// ---- et_kv_copy: a page's rows of one plane and head are contiguous; a block takes some of these runs ------------------------------
+constexpr int COPY_THREADS = 256;
+__global__ void __launch_bounds__(COPY_THREADS)
+kv_copy_kernel(PagedCache c, const int* copies, int* status, int runs_each) {
+  begin_after_previous();
+  const int from = copies[3 * blockIdx.x], to = copies[3 * blockIdx.x + 1];
+  const int rows = min(copies[3 * blockIdx.x + 2], 1 << c.page_shift);
+  if (from < 0 || to < 0 || rows <= 0) return;
+  if (from >= c.n_pages || to >= c.n_pages) { if (threadIdx.x == 0) report(status, ET_PAGED_BAD_PAGE); return; }
+  if (from == to) return;
+  const int runs = 2 * c.kv_heads, run0 = blockIdx.y * runs_each, run1 = min(run0 + runs_each, runs);
+  const int row_bytes = kv_row_bytes(c.format, c.head_dim), scale_bytes = kv_scale_bytes(c.format, c.head_dim);
+  const int vectors = rows * row_bytes / 16;       // of a run
+  constexpr int AHEAD = 4;
+  for (int run = run0; run < run1; ++run) {
+    const size_t a = ((size_t)from * runs + run) << c.page_shift, b = ((size_t)to * runs + run) << c.page_shift;     // rows
+    const uint4* const src = reinterpret_cast<const uint4*>(c.data + a * row_bytes);
+    uint4* const dst = reinterpret_cast<uint4*>(c.data + b * row_bytes);
+    for (int i0 = threadIdx.x; i0 < vectors; i0 += AHEAD * COPY_THREADS) {
+      uint4 v[AHEAD];
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) if (i0 + j * COPY_THREADS < vectors) v[j] = src[i0 + j * COPY_THREADS];
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) if (i0 + j * COPY_THREADS < vectors) dst[i0 + j * COPY_THREADS] = v[j];
+    }
+    for (int i = threadIdx.x; i < rows * scale_bytes; i += COPY_THREADS) c.scale[b * scale_bytes + i] = c.scale[a * scale_bytes + i];
+  }
+}
+
+int shift_of(int page_size) {
+  for (int s = 4; s <= 7; ++s) if (page_size == 1 << s) return s;
+  return -1;
+}
+
+}  // namespace
+
+}  // namespace et
+
+using namespace et;
+
+extern "C" {
+
+et_status et_pages_update(int* refs_dev, int n_pages, int page_size, int* block_table_dev, int n_seq, int max_pages, const int* len_dev,
+                          const int* keep_dev, const int* add_dev, int* new_len_dev, int* row_offsets_dev, int* slots_dev, int rows,
+                          void* workspace_dev, size_t workspace_bytes, int* status_dev, void* cuda_stream) {
+  if (!refs_dev || !block_table_dev || !len_dev || !new_len_dev || !workspace_dev || !aligned16(workspace_dev)) return ET_ERR_INVALID_ARG;
+  if (new_len_dev == keep_dev || new_len_dev == add_dev) return ET_ERR_INVALID_ARG;
+  const int shift = shift_of(page_size);
+  if (shift < 0 || n_pages < 1 || n_seq < 1 || max_pages < 1 || rows < 0 || (rows > 0 && !slots_dev)) return ET_ERR_SHAPE;
+  if ((long long)n_pages << shift >= 1ll << 31 || (long long)max_pages << shift > 1ll << 30 || n_seq > 65536 ||
+      (long long)n_seq * max_pages >= 1ll << 31 || rows > 1 << 30) return ET_ERR_CAPACITY;
+  if (workspace_bytes < ET_PAGES_WORKSPACE(n_pages, n_seq)) return ET_ERR_CAPACITY;
+  int* const ws = (int*)workspace_dev;
+  const Update u{refs_dev, block_table_dev, len_dev, keep_dev, add_dev, new_len_dev, row_offsets_dev, rows > 0 ? slots_dev : nullptr, ws,
+                 ws + n_pages, ws + n_pages + n_seq, n_pages, shift, n_seq, max_pages, rows, status_dev};
+  ET_COUNT_LAUNCH();
+  const bool here = rows <= SLOTS_HERE;
+  Launch l(CLUSTER, THREADS, 0, (cudaStream_t)cuda_stream, CLUSTER);
+  const cudaError_t e = cudaLaunchKernelEx(&l.cfg, pages_update_kernel, u, here);
+  if (here || e != cudaSuccess) return launched(e);
+  ET_COUNT_LAUNCH();
+  Launch slots(cdiv(rows, SLOT_THREADS * SLOT_ROWS), SLOT_THREADS, 0, (cudaStream_t)cuda_stream);
+  return launched(cudaLaunchKernelEx(&slots.cfg, slots_kernel, u));
+}
+
+et_status et_pages_fork(int* refs_dev, int n_pages, int page_size, const int* block_table_dev, int n_old, int max_pages,
+                        const int* len_dev, const int* parent_dev, int n_new, int* new_table_dev, int* new_len_dev, int* copies_dev,
+                        void* workspace_dev, size_t workspace_bytes, int* status_dev, void* cuda_stream) {
+  if (!refs_dev || !block_table_dev || !len_dev || !parent_dev || !new_table_dev || !new_len_dev || !copies_dev || !workspace_dev ||
+      !aligned16(workspace_dev)) return ET_ERR_INVALID_ARG;
+  if (new_table_dev == block_table_dev || new_len_dev == len_dev || new_len_dev == parent_dev) return ET_ERR_INVALID_ARG;
+  const int shift = shift_of(page_size);
+  if (shift < 0 || n_pages < 1 || n_old < 1 || n_new < 1 || max_pages < 1) return ET_ERR_SHAPE;
+  if ((long long)n_pages << shift >= 1ll << 31 || (long long)max_pages << shift > 1ll << 30 || n_old > FORK_ROWS || n_new > FORK_ROWS ||
+      (long long)(n_old > n_new ? n_old : n_new) * max_pages >= 1ll << 31) return ET_ERR_CAPACITY;
+  if (workspace_bytes < ET_FORK_WORKSPACE(n_pages, n_new)) return ET_ERR_CAPACITY;
+  int* const ws = (int*)workspace_dev;
+  const Fork f{refs_dev, block_table_dev, len_dev, parent_dev, new_table_dev, new_len_dev, copies_dev, ws, ws + n_pages, n_pages, shift,
+               n_old, n_new, max_pages, status_dev};
+  const int slices = max_pages / FORK_THREADS + 1, most = 148 * 4 / n_old + 1;
+  ET_COUNT_LAUNCH();
+  Launch rows(dim3(n_old, slices < most ? slices : most), FORK_THREADS, 2 * (size_t)n_new, (cudaStream_t)cuda_stream);
+  cudaError_t e = cudaLaunchKernelEx(&rows.cfg, fork_rows_kernel, f);
+  if (e != cudaSuccess) return launched(e);
+  ET_COUNT_LAUNCH();
+  Launch last(CLUSTER, THREADS, 0, (cudaStream_t)cuda_stream, CLUSTER);
+  return launched(cudaLaunchKernelEx(&last.cfg, fork_last_pages_kernel, f));
+}
+
+et_status et_kv_copy(const et_kv_cache* cache, const int* copies_dev, int n, int* status_dev, void* cuda_stream) {
+  PagedCache c;
+  const et_status st = check_cache(cache, &c);
+  if (st != ET_OK) return st;
+  if (!copies_dev) return ET_ERR_INVALID_ARG;
+  if (n < 1) return ET_ERR_SHAPE;
+  if (n > 1 << 24 || c.kv_heads > 1 << 15) return ET_ERR_CAPACITY;
+  const int runs = 2 * c.kv_heads, split = cdiv(148 * 8, n) < runs ? cdiv(148 * 8, n) : runs, each = cdiv(runs, split);
+  ET_COUNT_LAUNCH();
+  Launch l(dim3(n, cdiv(runs, each)), COPY_THREADS, 0, (cudaStream_t)cuda_stream);
+  return launched(cudaLaunchKernelEx(&l.cfg, kv_copy_kernel, c, copies_dev, status_dev, each));
+}
+
+}  // extern "C"
