@@ -44,9 +44,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int TILE = 64;                       // positions
-constexpr int GROUP_WARPS = 2;                 // warps of one tile, BLOCKS blocks of 16 positions each
-constexpr int BLOCKS = TILE / 16 / GROUP_WARPS;
+constexpr int GROUP_WARPS = 2;                 // warps of one tile
 constexpr int COMPUTE_WARPS = 8;
 constexpr int GROUPS = COMPUTE_WARPS / GROUP_WARPS;   // tiles are dealt to the groups in turn
 constexpr int COPY_WARPS = GROUPS;             // one for each group's tiles
@@ -55,20 +53,27 @@ constexpr int THREADS = 32 * (COMPUTE_WARPS + COPY_WARPS);
 constexpr int LAUNCH_REGS = 168, COMPUTE_REGS = 208, COPY_REGS = 88;
 static_assert(COMPUTE_WARPS % 4 == 0 && COPY_WARPS % 4 == 0, "whole warpgroups");
 static_assert(COMPUTE_WARPS * COMPUTE_REGS + COPY_WARPS * COPY_REGS <= (COMPUTE_WARPS + COPY_WARPS) * LAUNCH_REGS, "register budget");
-// A group takes an item of up to so many tiles alone, where a CTA has several: 72 sequences of 250, 16 heads of 128, e4m3:
-// 29.8 -> 18.3 us, 56 of 320 29.9 -> 21.5 us; with 32 a batch of long and short ones gets slower (55.8 -> 60.2 us).
-constexpr int ALONE_TILES = 8;
+// A group takes an item of up to so many positions alone, where a CTA has several: 72 sequences of 250, 16 heads of 128, e4m3:
+// 29.8 -> 18.3 us, 56 of 320 29.9 -> 21.5 us; with 2 048 a batch of long and short ones gets slower (55.8 -> 60.2 us).
+constexpr int ALONE_POSITIONS = 512;
 // The tensor core cuts off what does not fit an accumulator, which adds up over long sums (0.0016 of positive outputs after a
-// million positions in a CTA).  So a piece has at most this many tiles, a quarter for each group; what is longer becomes several
+// million positions in a CTA).  So a piece has at most this many positions, a quarter for each group; what is longer becomes several
 // pieces, whose outputs are added in fp32.
-constexpr int PIECE_TILES = 256 * GROUPS;
+constexpr int PIECE_POSITIONS = 64 * 256 * GROUPS;
 constexpr int MAX_CTAS = 148;
 constexpr int PAD = 4;                         // floats between heads of the joining buffer: no bank conflicts
 constexpr int SMEM_LIMIT = 232448 - 512;       // 227 KB, less the static part
 constexpr int CONTROL_BYTES = 1024;            // barriers and the ring's flags
 
+// Rows of 4 bits come in tiles of twice as many positions: what a tile costs beside its rows (a copying warp's work, waits, the search
+// for a maximum) is then half as much a row.
+constexpr int tile_positions(int format, int nt) { return format == ET_KV_INT4 && nt == 1 ? 128 : 64; }
+
 template <int DH, int FMT, int NT>
 struct Cfg {
+  // positions of a tile, which is computed in parts; of a part each of a group's warps has BLOCKS blocks of 16
+  static constexpr int TILE = tile_positions(FMT, NT), PART = 64, BLOCKS = PART / 16 / GROUP_WARPS;
+  static constexpr int ALONE_TILES = ALONE_POSITIONS / TILE, PIECE_TILES = PIECE_POSITIONS / TILE;
   static constexpr int ROW = kv_row_bytes(FMT, DH);               // bytes of a row
   static constexpr int BOX_ROW = ROW > 128 ? 128 : ROW;           // bytes of a box row: the swizzle's width
   static constexpr int BOXES = ROW / BOX_ROW;
@@ -82,7 +87,7 @@ struct Cfg {
   static constexpr int SCALES = 2 * TILE * kv_scale_bytes(FMT, DH);
   static constexpr int HEADS = 8 * NT;
   static constexpr int JOIN = COMPUTE_WARPS * HEADS * (DH + PAD) * 4 + COMPUTE_WARPS * HEADS * 3 * 4;   // the warps' results of a piece
-  static constexpr int JOINS = NT == 1 ? 2 : 1;                   // pieces whose results can wait to be joined
+  static constexpr int JOINS = NT == 1 && TILE == 64 ? 2 : 1;                   // pieces whose results can wait to be joined
   static constexpr int Q_ROW = DH * 2 + 16;                       // a head's query; 16 bytes more: no bank conflicts
   static constexpr bool ALONE = NT == 1;                          // (with 16 heads there is no room for what it takes)
   static constexpr int PAIR = ALONE ? HEADS * (DH + PAD) * 4 + 3 * HEADS * 4 : 0;   // a group's own results
@@ -152,35 +157,34 @@ __device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t x) {
   const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x));
   return pack_bf16(f.x, f.y);
 }
-// Eight 4-bit codes of a word as x[i] = codes i and i + 4, less 8, in two halves: over the mantissa of 1024 a code counts as itself or,
-// four bits higher, 16 times, so that a mask and one packed multiply-add make two values of them.
-__device__ __forceinline__ uint32_t fma_f16x2(uint32_t x, uint32_t a, uint32_t b) {
-  uint32_t y;
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(x), "r"(a), "r"(b));
-  return y;
+// Eight 4-bit codes of a word, i and i + 4 together.
+// As halves: a code's four bits alone are the subnormal half c 2^-24 or, four bits higher, 16 c 2^-24.  x[1] and x[3] are 16 times too
+// large, and the 8 that a code is above its value is still in it: the queries make up for both.
+__device__ __forceinline__ void int4_to_f16(uint32_t w, uint32_t (&x)[4]) {
+  const uint32_t v = w >> 8;
+  x[0] = w & 0x000f000fu;
+  x[1] = w & 0x00f000f0u;
+  x[2] = v & 0x000f000fu;
+  x[3] = v & 0x00f000f0u;
 }
+// As bf16, less 8, times 2^-6 (x[0], x[2]) or 2^-2 (x[1], x[3]), which the outputs make up for: a code's bits alone are the bf16 c 2^-133
+// or 16 c 2^-133 (below 256 steps there is nothing but steps of 2^-133), and a multiply-add by 2^127 takes the 8 off.
+constexpr float INT4_EVEN = 64.f, INT4_ODD = 4.f;
 __device__ __forceinline__ uint32_t fma_bf16x2(uint32_t x, uint32_t a, uint32_t b) {
   uint32_t y;
   asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(x), "r"(a), "r"(b));
   return y;
 }
-__device__ __forceinline__ void int4_to_f16(uint32_t w, uint32_t (&x)[4]) {
-  const uint32_t v = w >> 8;
-  x[0] = fma_f16x2((w & 0x000f000fu) | 0x64006400u, 0x3c003c00u, 0xe408e408u);         // (1024 + c) - 1032
-  x[1] = fma_f16x2((w & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, 0xd480d480u);         // (1024 + 16 c) / 16 - 72
-  x[2] = fma_f16x2((v & 0x000f000fu) | 0x64006400u, 0x3c003c00u, 0xe408e408u);
-  x[3] = fma_f16x2((v & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, 0xd480d480u);
-}
-// The same in bf16, whose mantissa has room for a code in its four low or its four high bits: over 128.
 __device__ __forceinline__ void int4_to_bf16(uint32_t w, uint32_t (&x)[4]) {
-  x[0] = fma_bf16x2((w & 0x000f000fu) | 0x43004300u, 0x3f803f80u, 0xc308c308u);        // (128 + c) - 136
-  x[1] = fma_bf16x2(((w >> 1) & 0x00780078u) | 0x43004300u, 0x3e003e00u, 0xc1c0c1c0u); // (128 + 8 c) / 8 - 24
-  x[2] = fma_bf16x2(((w >> 8) & 0x000f000fu) | 0x43004300u, 0x3f803f80u, 0xc308c308u);
-  x[3] = fma_bf16x2(((w >> 9) & 0x00780078u) | 0x43004300u, 0x3e003e00u, 0xc1c0c1c0u);
+  const uint32_t v = w >> 8;
+  x[0] = fma_bf16x2(w & 0x000f000fu, 0x7f007f00u, 0xbe00be00u);       // c 2^-6 - 2^-3
+  x[1] = fma_bf16x2(w & 0x00f000f0u, 0x7f007f00u, 0xc000c000u);       // c 2^-2 - 2
+  x[2] = fma_bf16x2(v & 0x000f000fu, 0x7f007f00u, 0xbe00be00u);
+  x[3] = fma_bf16x2(v & 0x00f000f0u, 0x7f007f00u, 0xc000c000u);
 }
-// N bf16 scales next to one another (zeros if not live)
+// N bf16 scales next to one another
 template <int N>
-__device__ __forceinline__ void load_scales(const uint8_t* src, float (&f)[N], bool live = true) {
+__device__ __forceinline__ void load_scales(const uint8_t* src, float (&f)[N]) {
   static_assert(N == 2 || N == 4, "head sizes of 64 and 128");
   uint32_t w[N / 2];
   if constexpr (N == 4) {
@@ -189,8 +193,7 @@ __device__ __forceinline__ void load_scales(const uint8_t* src, float (&f)[N], b
   } else w[0] = *reinterpret_cast<const uint32_t*>(src);
 #pragma unroll
   for (int i = 0; i < N / 2; ++i) {
-    if (!live) w[i] = 0;
-    f[2 * i] = __uint_as_float(w[i] << 16);
+    f[2 * i] = __uint_as_float(w[i] * 65536u);
     f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
   }
 }
@@ -201,7 +204,10 @@ constexpr float SCALE_SPAN = 8.f;              // e4m3: binades that a tile's sc
 // negative number it would become a NaN or the other infinity.
 __device__ __forceinline__ uint32_t upper_halves(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632); }
 __device__ __forceinline__ uint32_t lower_halves(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410); }
-__device__ __forceinline__ float rest_of(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u); }     // of a finite value's weight
+// what is left of a and b behind their upper halves h (for values that are finite: the rest may be zero)
+__device__ __forceinline__ uint32_t pack_rests(float a, float b, uint32_t h) {
+  return pack_bf16(a - __uint_as_float(h * 65536u), b - __uint_as_float(h & 0xffff0000u));
+}
 __device__ __forceinline__ float lower_part(float x) {
   return fmaf(__uint_as_float(__float_as_uint(x) & 0xffff0000u), -(1.f - 0x1p-24f), x);
 }
@@ -234,10 +240,10 @@ __device__ __forceinline__ int clamped_len(const Args& g, int s) {
   return (int)min((long long)max(g.a.len[s], 0), cap);
 }
 // An item's units: its tiles and, in front of them, units for what it costs beside them.  C: the kernel's Cfg
-__device__ __forceinline__ int tiles_of(int len) { return (int)((unsigned)(len + (TILE - 1)) / TILE); }
-template <class C> __device__ __forceinline__ int cost_of(int tiles) { return tiles <= ALONE_TILES ? C::COST_SHORT : C::COST; }
+template <class C> __device__ __forceinline__ int tiles_of(int len) { return (int)((unsigned)(len + (C::TILE - 1)) / C::TILE); }
+template <class C> __device__ __forceinline__ int cost_of(int tiles) { return tiles <= C::ALONE_TILES ? C::COST_SHORT : C::COST; }
 template <class C> __device__ __forceinline__ int units_of(const Args& g, int len) {
-  const int tiles = tiles_of(len);
+  const int tiles = tiles_of<C>(len);
   return len <= 0 ? 0 : g.whole ? 1 : tiles + cost_of<C>(tiles);
 }
 
@@ -262,10 +268,11 @@ struct Piece {
 // piece that the groups share costs them all its queries, its result and a wait for one another, as much as several tiles).
 // `turn` goes round the groups; copying and computing warps deal alike.
 struct Deal { int t, step; bool alone; };
-__device__ __forceinline__ Deal deal(const Piece& p, bool may, int chunk, int group, int& turn) {
+template <class C>
+__device__ __forceinline__ Deal deal(const Piece& p, int chunk, int group, int& turn) {
   Deal d;
   const int n = p.t1 - p.t0;
-  d.alone = may && n <= ALONE_TILES && p.units * GROUPS <= chunk && !p.goes_on;
+  d.alone = C::ALONE && n <= C::ALONE_TILES && p.units * GROUPS <= chunk && !p.goes_on;
   const int behind = (group - turn) & (GROUPS - 1);
   d.t = d.alone ? (behind == 0 ? p.t0 : p.t1) : p.t0 + behind;
   d.step = d.alone ? 1 : GROUPS;
@@ -280,11 +287,11 @@ __device__ __forceinline__ bool next_piece(const Args& g, int parts_all, Walk& w
     if (units > 0) {
       int end = w.unit + min(w.left, units - w.unit);
       p.s = w.s; p.part = w.part; p.len = w.len; p.units = units;
-      const int tiles = tiles_of(w.len), cost = cost_of<C>(tiles);
+      const int tiles = tiles_of<C>(w.len), cost = cost_of<C>(tiles);
       p.t0 = g.whole ? 0 : max(w.unit - cost, 0);
       p.t1 = g.whole ? tiles : max(end - cost, 0);
-      p.more = p.t1 - p.t0 > PIECE_TILES;
-      if (p.more) { p.t1 = p.t0 + PIECE_TILES; end = p.t1 + cost; }        // (an item that is not cut has no such length)
+      p.more = p.t1 - p.t0 > C::PIECE_TILES;
+      if (p.more) { p.t1 = p.t0 + C::PIECE_TILES; end = p.t1 + cost; }        // (an item that is not cut has no such length)
       p.goes_on = w.cut;
       p.first = w.cut ? w.cut_first : p.t0 == 0;
       p.last = end == units; p.units_end = end;
@@ -309,7 +316,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ Args g) {
   using C = Cfg<DH, FMT, NT>;
   constexpr bool BF16 = FMT == ET_KV_BF16, E4M3 = FMT == ET_KV_E4M3, INT4 = FMT == ET_KV_INT4;
-  constexpr int STAGES = C::STAGES, KS = DH / 16, SCALE = kv_scale_bytes(FMT, DH);     // SCALE: bytes of a row's scales
+  constexpr int TILE = C::TILE, BLOCKS = C::BLOCKS, STAGES = C::STAGES, KS = DH / 16, SCALE = kv_scale_bytes(FMT, DH);     // SCALE: bytes of a row's scales
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const gen = smem_raw + (base - raw);
@@ -385,7 +392,8 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
   if (warp >= COMPUTE_WARPS) {
     // ------------------------------------------------------------------ copies
     const int me = warp - COMPUTE_WARPS;
-    const int box_shift = min(g.c.page_shift, 6), box_rows = 1 << box_shift, boxes_tile = TILE >> box_shift;
+    constexpr int TILE_SHIFT = TILE == 128 ? 7 : 6, BOXES = TILE / 16;         // a page has 16 positions or more
+    const int box_shift = min(g.c.page_shift, TILE_SHIFT), box_rows = 1 << box_shift, boxes_tile = TILE >> box_shift;
     const uint32_t box_bytes = (uint32_t)box_rows * (2 * C::ROW + 2 * SCALE);
     const int plane_rows = kv_heads << g.c.page_shift;
     // the cache is read once (several head tiles read it soon after one another): it need not push other things out of L2
@@ -399,7 +407,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     uint32_t q_phase = 0;
     Piece p;
     while (ok && next_piece<C>(g, parts_all, walk, p)) {
-      const Deal dl = deal(p, C::ALONE, chunk, me, turn);
+      const Deal dl = deal<C>(p, chunk, me, turn);
       if (dl.t >= p.t1) continue;
       // the piece's queries: rows of the heads, zeros for heads that the group does not have
       ok = mbar_wait_warp(q_empty(me), q_phase ^ 1u, abort_flag);
@@ -437,9 +445,9 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         while ((page0 >> 5) > batch) { ++batch; rows = rows_of(ids_next); ids_next = load_ids(batch + 1); }
         const int in_page = pos & ((1 << g.c.page_shift) - 1);
         const int boxes = min(boxes_tile, (p.len - pos + box_rows - 1) >> box_shift);      // with positions
-        int row[4], missing = 0;                                      // first row of each box's keys; negative: none
+        int row[BOXES], missing = 0;                                  // first row of each box's keys; negative: none
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < BOXES; ++i) {
           row[i] = __shfl_sync(0xffffffffu, rows, (page0 + i) & 31);
           if (i >= boxes) row[i] = -1;
           else if (row[i] < 0) missing |= 1 << i;
@@ -454,7 +462,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         const uint32_t bar = full(stage), dst = base + stage * C::STAGE, sdst = scales + stage * C::SCALES;
         arrive_expect_elect(bar, (boxes - __popc(missing)) * box_bytes);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < BOXES; ++i) {
           if (row[i] >= 0) {
             const int r0 = i << box_shift;
 #pragma unroll
@@ -567,7 +575,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         const int item0 = begin + chunk - p.units_end;               // this piece ends this CTA's run (whole items are not cut)
         mine = Join{p.s, p.part, (item0 + p.units - 1) / chunk - b + 1, 2 * b + (p.opens ? 0 : 1)};
       }
-      const Deal dl = deal(p, C::ALONE, chunk, my_group, turn);
+      const Deal dl = deal<C>(p, chunk, my_group, turn);
       const bool busy = dl.t < p.t1;                                 // this group has tiles of the piece
       if (dl.alone && !busy) continue;
       if (busy && ok) ok = mbar_wait_warp(q_full(my_group), q_phase, abort_flag);
@@ -575,6 +583,9 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
       // ---- Q^T as the B operand: column gq = head, two rows (pairs of dimensions) a register
       uint32_t q[NT][KS][2];
       float qscale[NT][2];                                           // of heads 2 tq and 2 tq + 1
+      // 4 bits: -8 times the sum of a block's queries, for each of a head's blocks, as the sum of three bf16: the B operand for an A of the
+      // positions' scales, [hi | middle | low] x blocks along k
+      uint32_t eights[NT][2];
       if (busy) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -617,10 +628,41 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
             for (int k = 0; k < KS; ++k) {
               const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].x));
               const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw_q[k].y));
+              const float g = INT4 ? f * 0.0625f : f;
               q[n][k][0] = pack_f16(x.x * f, x.y * f);
-              q[n][k][1] = pack_f16(y.x * f, y.y * f);
+              q[n][k][1] = pack_f16(y.x * g, y.y * g);
             }
-            const float back = pow2(e) * softmax_scale;
+            if constexpr (INT4) {
+              float block_sum[DH / INT4_BLOCK];
+#pragma unroll
+              for (int k = 0; k < KS; k += 2) {
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&q[n][k + i][0]));
+                  const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&q[n][k + i][1]));
+                  sum += (x.x + x.y) + 16.f * (y.x + y.y);
+                }
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                block_sum[k / 2] = sum * (-8.f * 0x1p-24f);
+              }
+              constexpr int PAIRS = DH / INT4_BLOCK / 2;             // k-steps' pairs of a piece
+              const float c0 = PAIRS == 2 && (tq & 1) ? block_sum[PAIRS == 2 ? 2 : 0] : block_sum[0];
+              const float c1 = PAIRS == 2 && (tq & 1) ? block_sum[PAIRS == 2 ? 3 : 1] : block_sum[1];
+              const uint32_t hi = upper_halves(c0, c1);
+              const float r0 = c0 - __uint_as_float(hi << 16), r1 = c1 - __uint_as_float(hi & 0xffff0000u);
+              const uint32_t mid = upper_halves(r0, r1);
+              const uint32_t low = pack_bf16(r0 - __uint_as_float(mid << 16), r1 - __uint_as_float(mid & 0xffff0000u));
+              if (PAIRS == 2) {
+                eights[n][0] = tq < 2 ? hi : mid;
+                eights[n][1] = tq < 2 ? low : 0u;
+              } else {
+                eights[n][0] = tq == 0 ? hi : tq == 1 ? mid : tq == 2 ? low : 0u;
+                eights[n][1] = 0u;
+              }
+            }
+            const float back = pow2(e) * (INT4 ? softmax_scale * 0x1p24f : softmax_scale);
             qscale[n][0] = __shfl_sync(0xffffffffu, back, 8 * tq);
             qscale[n][1] = __shfl_sync(0xffffffffu, back, 8 * tq + 4);
           }
@@ -648,17 +690,19 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         if ((stage += GROUPS) >= STAGES) { stage = my_group; phase ^= 1u; }
         if (ok) ok = mbar_wait_warp(full(st), ph, abort_flag);
         if (!ok) continue;
+#pragma unroll 1
+        for (int part = 0; part < TILE / C::PART; ++part) {
         // positions of each block that count: up to the length, none on an absent page (a page has whole slices)
-        const int gone = absent[st] >> slice;
+        const int gone = absent[st] >> (slice + part * (C::PART / 16));
         int valid[BLOCKS], any = 0;
 #pragma unroll
         for (int j = 0; j < BLOCKS; ++j) {
-          const int room = p.len - t * TILE - r0 - 16 * j;
+          const int room = p.len - t * TILE - part * C::PART - r0 - 16 * j;
           valid[j] = (gone >> j & 1) ? 0 : max(0, min(16, room));
           any |= valid[j];
         }
         if (any) {
-          const uint32_t kb = base + st * C::STAGE, vb = kb + C::PLANE;
+          const uint32_t kb = base + st * C::STAGE + part * (C::PART * C::BOX_ROW), vb = kb + C::PLANE;
           // ---- S^T = K Q^T: rows = positions gq, gq + 8 of a block, columns = heads 2 tq, 2 tq + 1
           float s[BLOCKS][NT][4];
 #pragma unroll
@@ -669,10 +713,14 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
             // a block of 32 dimensions is two k-steps; its sum counts with the scale that the position has for it
 #pragma unroll
             for (int j = 0; j < BLOCKS; ++j) {
-              const uint8_t* sc = gen + STAGES * C::STAGE + st * C::SCALES + (r0 + 16 * j + gq) * SCALE;
+              const uint8_t* sc = gen + STAGES * C::STAGE + st * C::SCALES + (part * C::PART + r0 + 16 * j + gq) * SCALE;
               float ks[2][DH / INT4_BLOCK];
               load_scales<DH / INT4_BLOCK>(sc, ks[0]);
               load_scales<DH / INT4_BLOCK>(sc + 8 * SCALE, ks[1]);
+              const uint32_t w0 = *reinterpret_cast<const uint32_t*>(sc + (SCALE == 8 ? 4 * (tq & 1) : 0));
+              const uint32_t w1 = *reinterpret_cast<const uint32_t*>(sc + 8 * SCALE + (SCALE == 8 ? 4 * (tq & 1) : 0));
+#pragma unroll
+              for (int n = 0; n < NT; ++n) mma16816<false>(s[j][n], w0, w1, w0, w1, eights[n][0], eights[n][1]);
 #pragma unroll
               for (int k = 0; k < KS; k += 4) {
                 uint32_t a[4];                                        // positions gq / gq + 8 of a block, then of the next
@@ -824,12 +872,15 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
               [[maybe_unused]] const uint32_t keep1 = (2 * tq + 8 < valid[j] ? 0xffffu : 0u) | (2 * tq + 9 < valid[j] ? 0xffff0000u : 0u);
               if constexpr (INT4) {
                 // a value's scale goes to its weight, which has a bf16's exponents; behind the length it is cleared, whatever it was
-                const uint8_t* sc = gen + STAGES * C::STAGE + st * C::SCALES + (TILE + r0 + 16 * j + 2 * tq) * SCALE;
+                const uint8_t* sc = gen + STAGES * C::STAGE + st * C::SCALES + (TILE + part * C::PART + r0 + 16 * j + 2 * tq) * SCALE;
                 float vs[4][DH / INT4_BLOCK];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const int at = (i & 1) + 8 * (i >> 1);
-                  load_scales<DH / INT4_BLOCK>(sc + at * SCALE, vs[i], 2 * tq + at < valid[j]);
+                for (int i = 0; i < 4; ++i) load_scales<DH / INT4_BLOCK>(sc + ((i & 1) + 8 * (i >> 1)) * SCALE, vs[i]);
+                if (valid[j] < 16) {
+#pragma unroll
+                  for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int c = 0; c < DH / INT4_BLOCK; ++c) if (2 * tq + (i & 1) + 8 * (i >> 1) >= valid[j]) vs[i][c] = 0.f;
                 }
 #pragma unroll
                 for (int k = 0; k < KS; k += 4) {
@@ -846,7 +897,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 #pragma unroll
                       for (int e = 0; e < 4; ++e) w[e] = pt[n][e] * vs[e][k / 2 + i];
                       const uint32_t h0 = upper_halves(w[0], w[1]), h1 = upper_halves(w[2], w[3]);
-                      const uint32_t l0 = pack_bf16(rest_of(w[0]), rest_of(w[1])), l1 = pack_bf16(rest_of(w[2]), rest_of(w[3]));
+                      const uint32_t l0 = pack_rests(w[0], w[1], h0), l1 = pack_rests(w[2], w[3], h1);
 #pragma unroll
                       for (int e = 0; e < 2; ++e) {
                         mma16816<false>(o[n][k + 2 * i + e], x[2 * e], x[2 * e + 1], y[2 * e], y[2 * e + 1], h0, h1);
@@ -908,6 +959,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
           }
           if (!added) add_values(std::bool_constant<BF16>());
         }
+        }
         __syncwarp();
         if (lane == 0) mbar_arrive(empty(st));
       }
@@ -920,6 +972,14 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
           for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[n][k][i] *= 1.f / 32768.f;       // 2^-WEIGHT_SHIFT
+      }
+      if constexpr (INT4) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[n][k][i] *= i < 2 ? INT4_EVEN : INT4_ODD;
       }
       const int live = heads_of(p);
 #pragma unroll
@@ -1098,14 +1158,14 @@ attention_join_kernel(const __grid_constant__ Args g) {
   }
 }
 
-bool make_cache_map(CUtensorMap* out, const PagedCache& c) {
+bool make_cache_map(CUtensorMap* out, const PagedCache& c, int tile) {
   EncodeTiledFn fn = tensor_map_encoder();
   if (!fn) return false;
   const bool two = c.format == ET_KV_BF16;                             // bytes an element of the map
   const int row = kv_row_bytes(c.format, c.head_dim), box_row = row > 128 ? 128 : row;
   const cuuint64_t dims[2] = {(cuuint64_t)(row / (two ? 2 : 1)), ((cuuint64_t)c.n_pages * 2 * c.kv_heads) << c.page_shift};
   const cuuint64_t strides[1] = {(cuuint64_t)row};
-  const cuuint32_t box[2] = {(cuuint32_t)(box_row / (two ? 2 : 1)), (cuuint32_t)(1 << (c.page_shift < 6 ? c.page_shift : 6))};
+  const cuuint32_t box[2] = {(cuuint32_t)(box_row / (two ? 2 : 1)), (cuuint32_t)(1 << c.page_shift < tile ? 1 << c.page_shift : tile)};
   const cuuint32_t estr[2] = {1, 1};
   return fn(out, two ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, c.data, dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, box_row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : box_row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
@@ -1143,14 +1203,14 @@ cudaError_t launch(const CUtensorMap& map, const Args& g, int ctas, cudaStream_t
 }  // namespace
 
 cudaError_t launch_attention_paged(const PagedCache& c, const PagedAttention& a, cudaStream_t s) {
-  CUtensorMap map;
-  if (!make_cache_map(&map, c)) return cudaErrorUnknown;
   Args g;
   g.c = c; g.a = a;
   g.group = a.heads / c.kv_heads;
   const int nt = g.group <= 8 ? 1 : 2;
   g.parts = (g.group + 8 * nt - 1) / (8 * nt);
-  const long long tiles = (((long long)a.max_pages << c.page_shift) + TILE - 1) / TILE;      // of the longest sequence there can be
+  CUtensorMap map;
+  if (!make_cache_map(&map, c, tile_positions(c.format, nt))) return cudaErrorUnknown;
+  const long long tiles = (((long long)a.max_pages << c.page_shift) + 63) / 64;      // of the longest sequence there can be (or half as many)
   // Where no sequence can have more than four tiles, items are not cut and nothing has to be joined.  The host knows the table's width
   // only: in one for 32 768 positions the same lengths take the other way, 1 x 61 6.7 us in place of 5.5, 16 x 200 8.7 of 6.5.
   g.whole = tiles <= 4;

@@ -6,6 +6,8 @@
 // Read of 63 435 rows of 16 + 16 heads of 64, bf16 86 us (0.93); of 7 675 rows, e4m3 8.9 us (0.41).
 #include <cuda_fp8.h>
 
+#include <type_traits>
+
 #include "decode.cuh"
 
 namespace et {
@@ -81,16 +83,22 @@ __device__ __forceinline__ uint2 to_e4m3(const float (&x)[8], float inv) {
   return make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
 }
 
-__device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
+// 8 or 4 bf16
+template <int N> struct Bf16s;
+template <> struct Bf16s<8> { using type = uint4; };
+template <> struct Bf16s<4> { using type = uint2; };
+template <int N>
+__device__ __forceinline__ void unpack(const typename Bf16s<N>::type& v, float (&x)[N]) {
   const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) { const float2 f = __bfloat1622float2(p[k]); x[2 * k] = f.x; x[2 * k + 1] = f.y; }
+  for (int k = 0; k < N / 2; ++k) { const float2 f = __bfloat1622float2(p[k]); x[2 * k] = f.x; x[2 * k + 1] = f.y; }
 }
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-  uint4 v;
+template <int N>
+__device__ __forceinline__ typename Bf16s<N>::type pack(const float (&x)[N]) {
+  typename Bf16s<N>::type v;
   __nv_bfloat162* p = reinterpret_cast<__nv_bfloat162*>(&v);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) p[k] = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]);
+  for (int k = 0; k < N / 2; ++k) p[k] = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]);
   return v;
 }
 
@@ -105,12 +113,12 @@ __device__ __forceinline__ float int4_scale(double top) {
   for (int i = 0; i < 2; ++i) if (7.0 * s < top) s = next_bf16(s);
   return s;
 }
-template <typename T>
-__device__ __forceinline__ uint32_t int4_codes(const T (&x)[8], float s, float up, float inv) {      // inv = 1 / (s up), up a power of two
+template <typename T, int N>
+__device__ __forceinline__ uint32_t int4_codes(const T (&x)[N], float s, float up, float inv) {      // inv = 1 / (s up), up a power of two
   uint32_t w = 0;
   const T h = (T)s * (T)0.5;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
+  for (int k = 0; k < N; ++k) {
     float n = rintf((float)x[k] * up * inv);
     const T r = sizeof(T) == 8 ? fma((double)-n, (double)s, (double)x[k]) : (T)fmaf(-n, s, (float)x[k]);
     const bool odd = (int)n & 1;
@@ -138,12 +146,17 @@ __device__ __forceinline__ float turned_exactly(float x, float c1, float c2, flo
 // e4m3 values, a sixteenth apart (now one in two million; 21 124 rows of 28 + 4 + 4 heads 87.6 -> 93.3 us).  Bound by memory, and with
 // e4m3 and rotation by instructions.
 // ---------------------------------------------------------------------------------------------
+// Values of each half that a lane has.  With 4-bit codes and rotation it holds sines, cosines and keys in 64 bits: half as many, so that
+// more blocks fit an SM.
+__host__ __device__ constexpr int append_each(int format, bool rotate) { return format == ET_KV_INT4 && rotate ? 4 : 8; }
+
 template <int DH, int FMT, bool ROTATE>
 __global__ void __launch_bounds__(THREADS)
 kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c, PagedRows r,
                  const __grid_constant__ RopeTurns turns, bf16* q_out, int* new_len, int rows_each, int parts) {
   constexpr bool E4M3 = FMT == ET_KV_E4M3, INT4 = FMT == ET_KV_INT4;
-  constexpr int HALF = DH / 2, CHUNKS = DH / 16, UNROLL = 2;
+  constexpr int HALF = DH / 2, E = append_each(FMT, ROTATE), CHUNKS = HALF / E, UNROLL = 16 / E;
+  using Vec = typename Bf16s<E>::type;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int part = warp % parts, chunk = lane % CHUNKS, head_lane = lane / CHUNKS;
   constexpr int HEADS_ITER = 32 / CHUNKS;
@@ -167,17 +180,17 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
   const int step = WARPS / parts;
   const long long row0 = (long long)blockIdx.x * step * rows_each, row1 = min(row0 + step * rows_each, (long long)r.rows);
   for (long long row = row0 + warp / parts; row < row1; row += step) {
-    const bf16* const src_row = qkv + row * row_stride + chunk * 8;
-    uint4 va[UNROLL], vb[UNROLL];
+    const bf16* const src_row = qkv + row * row_stride + chunk * E;
+    Vec va[UNROLL], vb[UNROLL];
     auto load = [&](int h0) {
 #pragma unroll
       for (int j = 0; j < UNROLL; ++j) {
         const int head = h0 + j * HEADS_ITER + head_lane;
-        va[j] = vb[j] = make_uint4(0, 0, 0, 0);
+        va[j] = vb[j] = Vec{};
         if (head < all_heads) {
           const bf16* src = src_row + (size_t)head * DH;
-          va[j] = *reinterpret_cast<const uint4*>(src);
-          vb[j] = *reinterpret_cast<const uint4*>(src + HALF);
+          va[j] = *reinterpret_cast<const Vec*>(src);
+          vb[j] = *reinterpret_cast<const Vec*>(src + HALF);
         }
       }
     };
@@ -187,8 +200,8 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
     long long pos;
     if (!places.find(c, r, (int)row, page, place, pos)) continue;          // the same for all lanes
     constexpr bool EXACT = ROTATE && E4M3;
-    float cs[8], sn[8], c1[8], s1[8];                        // EXACT: c1 + cs, s1 + sn
-    double cd[INT4 && ROTATE ? 8 : 1], sd[INT4 && ROTATE ? 8 : 1];
+    float cs[E], sn[E], c1[E], s1[E];                        // EXACT: c1 + cs, s1 + sn
+    double cd[INT4 && ROTATE ? E : 1], sd[INT4 && ROTATE ? E : 1];
     if (ROTATE) {
       // HALF pairs, found by HALF lanes' worth of sincos and handed to the lanes that need them
       constexpr int EACH = HALF / 32 > 0 ? HALF / 32 : 1;
@@ -211,8 +224,8 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
         }
       }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int from = (chunk * 8 + k) / EACH;
+      for (int k = 0; k < E; ++k) {
+        const int from = (chunk * E + k) / EACH;
         if constexpr (INT4 && ROTATE) {
           cd[k] = __shfl_sync(0xffffffffu, mcd[k % EACH], from);
           sd[k] = __shfl_sync(0xffffffffu, msd[k % EACH], from);
@@ -232,17 +245,17 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
 #pragma unroll
       for (int j = 0; j < UNROLL; ++j) {
         const int head = h0 + j * HEADS_ITER + head_lane;
-        float a[8], b[8];
-        unpack8(va[j], a);
-        unpack8(vb[j], b);
+        float a[E], b[E];
+        unpack<E>(va[j], a);
+        unpack<E>(vb[j], b);
         // 4 bits: the codes of a key are those that 64-bit arithmetic gives.  With keys turned in fp32 one value in a few hundred
         // thousand lies on the other side of a border between two codes, which is a seventh of the block's largest value.
-        double ad[INT4 && ROTATE ? 8 : 1], bd[INT4 && ROTATE ? 8 : 1];
+        double ad[INT4 && ROTATE ? E : 1], bd[INT4 && ROTATE ? E : 1];
         const bool key = head >= heads && head < heads + c.kv_heads;
         if constexpr (INT4 && ROTATE) {
           if (key) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < E; ++k) {
               const double x = a[k], y = b[k];
               ad[k] = x * cd[k] - y * sd[k];
               bd[k] = y * cd[k] + x * sd[k];
@@ -251,28 +264,28 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
         }
         if (EXACT && head >= heads && head < heads + c.kv_heads) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
+          for (int k = 0; k < E; ++k) {
             const float x = a[k], y = b[k];
             a[k] = turned_exactly(x, c1[k], cs[k], y, s1[k], sn[k]);
             b[k] = turned_exactly(y, c1[k], cs[k], x, -s1[k], -sn[k]);
           }
         } else if (ROTATE && head < (INT4 ? heads : heads + c.kv_heads)) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
+          for (int k = 0; k < E; ++k) {
             const float x = a[k], y = b[k], co = EXACT ? c1[k] + cs[k] : cs[k], si = EXACT ? s1[k] + sn[k] : sn[k];
             a[k] = x * co - y * si;
             b[k] = y * co + x * si;
           }
         }
         if (ROTATE && head < heads) {
-          uint4* dst = reinterpret_cast<uint4*>(q_out + ((size_t)row * heads + head) * DH + chunk * 8);
-          dst[0] = pack8(a);
-          dst[HALF / 8] = pack8(b);
+          Vec* dst = reinterpret_cast<Vec*>(q_out + ((size_t)row * heads + head) * DH + chunk * E);
+          dst[0] = pack<E>(a);
+          dst[HALF / E] = pack<E>(b);
         }
         float top = 0.f;
         if (E4M3) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
+          for (int k = 0; k < E; ++k) {
             const float x = fabsf(a[k]), y = fabsf(b[k]);
             if (x <= 3.402823466e38f) top = fmaxf(top, x);
             if (y <= 3.402823466e38f) top = fmaxf(top, y);
@@ -281,21 +294,21 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
           for (int o = CHUNKS / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         }
         float sa = 0.f, sb = 0.f;                                // 4 bits: scales of the two blocks that this lane has values of
-        if constexpr (INT4) {
+        if (INT4 && __any_sync(0xffffffffu, head >= heads)) {
           double ta = 0., tb = 0.;                               // infinite where the block has a value that is not finite
           auto most = [](double& top, double x) { top = x <= 3.402823466e38 ? fmax(top, x) : (double)INFINITY; };
           if (ROTATE && key) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) { most(ta, fabs(ad[ROTATE ? k : 0])); most(tb, fabs(bd[ROTATE ? k : 0])); }
+            for (int k = 0; k < E; ++k) { most(ta, fabs(ad[ROTATE ? k : 0])); most(tb, fabs(bd[ROTATE ? k : 0])); }
           } else {
             float fa = 0.f, fb = 0.f;
             auto most_f = [](float& top, float x) { top = x <= 3.402823466e38f ? fmaxf(top, x) : INFINITY; };
 #pragma unroll
-            for (int k = 0; k < 8; ++k) { most_f(fa, fabsf(a[k])); most_f(fb, fabsf(b[k])); }
+            for (int k = 0; k < E; ++k) { most_f(fa, fabsf(a[k])); most_f(fb, fabsf(b[k])); }
             ta = fa; tb = fb;
           }
 #pragma unroll
-          for (int o = 1; o < INT4_BLOCK / 8; o <<= 1) {
+          for (int o = 1; o < INT4_BLOCK / E; o <<= 1) {
             ta = fmax(ta, __shfl_xor_sync(0xffffffffu, ta, o));
             tb = fmax(tb, __shfl_xor_sync(0xffffffffu, tb, o));
           }
@@ -312,28 +325,29 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
               const float up = s < 0x1p-100f ? 0x1p64f : 1.f;    // 1 / s would overflow
               return int4_codes(x, s, up, 1.f / (s * up));
             };
-            uint32_t* dst = reinterpret_cast<uint32_t*>(c.data + at * (DH / 2) + chunk * 4);
+            using Codes = typename std::conditional<E == 8, uint32_t, uint16_t>::type;
+            Codes* dst = reinterpret_cast<Codes*>(c.data + at * (DH / 2) + chunk * (E / 2));
             if (ROTATE && key) {
-              if constexpr (ROTATE) { dst[0] = codes(ad, sa); dst[HALF / 8] = codes(bd, sb); }
+              if constexpr (ROTATE) { dst[0] = (Codes)codes(ad, sa); dst[HALF / E] = (Codes)codes(bd, sb); }
             } else {
-              dst[0] = codes(a, sa); dst[HALF / 8] = codes(b, sb);
+              dst[0] = (Codes)codes(a, sa); dst[HALF / E] = (Codes)codes(b, sb);
             }
-            if (chunk % (INT4_BLOCK / 8) == 0) {
-              bf16* scale = reinterpret_cast<bf16*>(c.scale) + at * (DH / INT4_BLOCK) + chunk / (INT4_BLOCK / 8);
+            if (chunk % (INT4_BLOCK / E) == 0) {
+              bf16* scale = reinterpret_cast<bf16*>(c.scale) + at * (DH / INT4_BLOCK) + chunk / (INT4_BLOCK / E);
               scale[0] = __float2bfloat16_rn(sa);
               scale[HALF / INT4_BLOCK] = __float2bfloat16_rn(sb);
             }
-          } else if (E4M3) {
+          } else if constexpr (E4M3) {
             const int e = e4m3_exponent(top);
             const float inv = pow2(-e);
-            uint2* dst = reinterpret_cast<uint2*>(c.data + at * DH + chunk * 8);
+            uint2* dst = reinterpret_cast<uint2*>(c.data + at * DH + chunk * E);
             dst[0] = to_e4m3(a, inv);
             dst[HALF / 8] = to_e4m3(b, inv);
             if (chunk == 0) c.scale[at] = (uint8_t)(e + 127);
           } else {
-            uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(c.data) + at * DH + chunk * 8);
-            dst[0] = pack8(a);
-            dst[HALF / 8] = pack8(b);
+            Vec* dst = reinterpret_cast<Vec*>(reinterpret_cast<bf16*>(c.data) + at * DH + chunk * E);
+            dst[0] = pack<E>(a);
+            dst[HALF / E] = pack<E>(b);
           }
         }
       }
@@ -393,7 +407,7 @@ kv_read_kernel(bf16* out, long long row_stride, PagedCache c, PagedRows r, int r
           float y[8];
 #pragma unroll
           for (int k = 0; k < 8; ++k) y[k] = (float)((int)(v[j].x >> (4 * k) & 15) - 8) * s;
-          *dst = pack8(y);
+          *dst = pack<8>(y);
         } else if (E4M3) {
           const float f = pow2(b[j] - 127);
           const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
@@ -405,8 +419,8 @@ kv_read_kernel(bf16* out, long long row_stride, PagedCache c, PagedRows r, int r
             (k < 4 ? lo : hi)[(2 * k) % 8] = y.x * f;
             (k < 4 ? lo : hi)[(2 * k + 1) % 8] = y.y * f;
           }
-          dst[0] = pack8(lo);
-          dst[1] = pack8(hi);
+          dst[0] = pack<8>(lo);
+          dst[1] = pack<8>(hi);
         } else {
           *dst = v[j];
         }
