@@ -44,15 +44,8 @@ namespace {
 
 using namespace tc;
 
-constexpr int GROUP_WARPS = 2;                 // warps of one tile
-constexpr int COMPUTE_WARPS = 8;
-constexpr int GROUPS = COMPUTE_WARPS / GROUP_WARPS;   // tiles are dealt to the groups in turn
+constexpr int GROUPS = 4;                      // of computing warps; tiles are dealt to them in turn
 constexpr int COPY_WARPS = GROUPS;             // one for each group's tiles
-constexpr int THREADS = 32 * (COMPUTE_WARPS + COPY_WARPS);
-// With 16 heads (NT = 2) the computing warps take registers from the copying ones: of what a block is launched with, never more.
-constexpr int LAUNCH_REGS = 168, COMPUTE_REGS = 208, COPY_REGS = 88;
-static_assert(COMPUTE_WARPS % 4 == 0 && COPY_WARPS % 4 == 0, "whole warpgroups");
-static_assert(COMPUTE_WARPS * COMPUTE_REGS + COPY_WARPS * COPY_REGS <= (COMPUTE_WARPS + COPY_WARPS) * LAUNCH_REGS, "register budget");
 // A group takes an item of up to so many positions alone, where a CTA has several: 72 sequences of 250, 16 heads of 128, e4m3:
 // 29.8 -> 18.3 us, 56 of 320 29.9 -> 21.5 us; with 2 048 a batch of long and short ones gets slower (55.8 -> 60.2 us).
 constexpr int ALONE_POSITIONS = 512;
@@ -67,12 +60,19 @@ constexpr int CONTROL_BYTES = 1024;            // barriers and the ring's flags
 
 // Rows of 4 bits come in tiles of twice as many positions: what a tile costs beside its rows (a copying warp's work, waits, the search
 // for a maximum) is then half as much a row.
-constexpr int tile_positions(int format, int nt) { return format == ET_KV_INT4 && nt == 1 ? 128 : 64; }
+constexpr int tile_positions(int format, int nt) { return 64; }
 
 template <int DH, int FMT, int NT>
 struct Cfg {
-  // positions of a tile, which is computed in parts; of a part each of a group's warps has BLOCKS blocks of 16
-  static constexpr int TILE = tile_positions(FMT, NT), PART = 64, BLOCKS = PART / 16 / GROUP_WARPS;
+  static constexpr int GROUP_WARPS = 2, COMPUTE_WARPS = GROUPS * GROUP_WARPS;
+  static constexpr int THREADS = 32 * (COMPUTE_WARPS + COPY_WARPS);
+  // The computing warps take registers from the copying ones: of what a block is launched with, never more.
+  static constexpr bool SPLIT = NT == 2 || GROUP_WARPS == 4;
+  static constexpr int LAUNCH_REGS = NT == 2 ? 168 : 96, COMPUTE_REGS = NT == 2 ? 208 : 104, COPY_REGS = NT == 2 ? 88 : 64;
+  static_assert(COMPUTE_WARPS % 4 == 0 && COPY_WARPS % 4 == 0, "whole warpgroups");
+  static_assert(!SPLIT || COMPUTE_WARPS * COMPUTE_REGS + COPY_WARPS * COPY_REGS <= (COMPUTE_WARPS + COPY_WARPS) * LAUNCH_REGS, "register budget");
+  // positions of a tile; each of a group's warps has BLOCKS blocks of 16 of them
+  static constexpr int TILE = tile_positions(FMT, NT), BLOCKS = TILE / 16 / GROUP_WARPS;
   static constexpr int ALONE_TILES = ALONE_POSITIONS / TILE, PIECE_TILES = PIECE_POSITIONS / TILE;
   static constexpr int ROW = kv_row_bytes(FMT, DH);               // bytes of a row
   static constexpr int BOX_ROW = ROW > 128 ? 128 : ROW;           // bytes of a box row: the swizzle's width
@@ -87,7 +87,7 @@ struct Cfg {
   static constexpr int SCALES = 2 * TILE * kv_scale_bytes(FMT, DH);
   static constexpr int HEADS = 8 * NT;
   static constexpr int JOIN = COMPUTE_WARPS * HEADS * (DH + PAD) * 4 + COMPUTE_WARPS * HEADS * 3 * 4;   // the warps' results of a piece
-  static constexpr int JOINS = NT == 1 && TILE == 64 ? 2 : 1;                   // pieces whose results can wait to be joined
+  static constexpr int JOINS = NT == 1 && GROUP_WARPS == 2 ? 2 : 1;                   // pieces whose results can wait to be joined
   static constexpr int Q_ROW = DH * 2 + 16;                       // a head's query; 16 bytes more: no bank conflicts
   static constexpr bool ALONE = NT == 1;                          // (with 16 heads there is no room for what it takes)
   static constexpr int PAIR = ALONE ? HEADS * (DH + PAD) * 4 + 3 * HEADS * 4 : 0;   // a group's own results
@@ -175,6 +175,15 @@ __device__ __forceinline__ uint32_t fma_bf16x2(uint32_t x, uint32_t a, uint32_t 
   asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(x), "r"(a), "r"(b));
   return y;
 }
+// (hi + lo) * s of two weights each, as two bf16 again: h = hi * s rounded, l = lo * s + (hi * s - h), whose difference is exact
+__device__ __forceinline__ void scaled_weight(uint32_t hi, uint32_t lo, uint32_t s, uint32_t& h, uint32_t& l) {
+  asm("{\n\t.reg .b32 n;\n\t"
+      "mul.rn.bf16x2 %0, %2, %4;\n\t"
+      "neg.bf16x2 n, %0;\n\t"
+      "fma.rn.bf16x2 n, %2, %4, n;\n\t"
+      "fma.rn.bf16x2 %1, %3, %4, n;\n\t}"
+      : "=&r"(h), "=r"(l) : "r"(hi), "r"(lo), "r"(s));
+}
 __device__ __forceinline__ void int4_to_bf16(uint32_t w, uint32_t (&x)[4]) {
   const uint32_t v = w >> 8;
   x[0] = fma_bf16x2(w & 0x000f000fu, 0x7f007f00u, 0xbe00be00u);       // c 2^-6 - 2^-3
@@ -203,11 +212,6 @@ constexpr float SCALE_SPAN = 8.f;              // e4m3: binades that a tile's sc
 // wherever the weight is (by 2^-24 of the weight too large), since an infinite value is multiplied by both, and with a zero or a
 // negative number it would become a NaN or the other infinity.
 __device__ __forceinline__ uint32_t upper_halves(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632); }
-__device__ __forceinline__ uint32_t lower_halves(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410); }
-// what is left of a and b behind their upper halves h (for values that are finite: the rest may be zero)
-__device__ __forceinline__ uint32_t pack_rests(float a, float b, uint32_t h) {
-  return pack_bf16(a - __uint_as_float(h * 65536u), b - __uint_as_float(h & 0xffff0000u));
-}
 __device__ __forceinline__ float lower_part(float x) {
   return fmaf(__uint_as_float(__float_as_uint(x) & 0xffff0000u), -(1.f - 0x1p-24f), x);
 }
@@ -226,7 +230,7 @@ __device__ __forceinline__ void bulk_load_elect(uint32_t dst, const void* src, u
                "@q cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}"
                ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void group_sync(int group) { asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(32 * GROUP_WARPS) : "memory"); }
+template <int N> __device__ __forceinline__ void group_sync(int group) { asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(32 * N) : "memory"); }
 // 16 bytes by a lane's own asynchronous copy (zeros if not live); copies_arrive: an arrival once the lane's copies so far are there
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
@@ -312,10 +316,11 @@ __device__ __forceinline__ bool next_piece(const Args& g, int parts_all, Walk& w
 }
 
 template <int DH, int FMT, int NT>
-__global__ void __launch_bounds__(THREADS, 1)
+__global__ void __launch_bounds__(Cfg<DH, FMT, NT>::THREADS, 1)
 attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ Args g) {
   using C = Cfg<DH, FMT, NT>;
   constexpr bool BF16 = FMT == ET_KV_BF16, E4M3 = FMT == ET_KV_E4M3, INT4 = FMT == ET_KV_INT4;
+  constexpr int GROUP_WARPS = C::GROUP_WARPS, COMPUTE_WARPS = C::COMPUTE_WARPS, THREADS = C::THREADS;
   constexpr int TILE = C::TILE, BLOCKS = C::BLOCKS, STAGES = C::STAGES, KS = DH / 16, SCALE = kv_scale_bytes(FMT, DH);     // SCALE: bytes of a row's scales
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -385,9 +390,9 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
   }
 
   bool ok = true;
-  if constexpr (NT == 2) {
-    if (warp >= COMPUTE_WARPS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(COPY_REGS));
-    else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(COMPUTE_REGS));
+  if constexpr (C::SPLIT) {
+    if (warp >= COMPUTE_WARPS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::COPY_REGS));
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::COMPUTE_REGS));
   }
   if (warp >= COMPUTE_WARPS) {
     // ------------------------------------------------------------------ copies
@@ -690,19 +695,17 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         if ((stage += GROUPS) >= STAGES) { stage = my_group; phase ^= 1u; }
         if (ok) ok = mbar_wait_warp(full(st), ph, abort_flag);
         if (!ok) continue;
-#pragma unroll 1
-        for (int part = 0; part < TILE / C::PART; ++part) {
         // positions of each block that count: up to the length, none on an absent page (a page has whole slices)
-        const int gone = absent[st] >> (slice + part * (C::PART / 16));
+        const int gone = absent[st] >> slice;
         int valid[BLOCKS], any = 0;
 #pragma unroll
         for (int j = 0; j < BLOCKS; ++j) {
-          const int room = p.len - t * TILE - part * C::PART - r0 - 16 * j;
+          const int room = p.len - t * TILE - r0 - 16 * j;
           valid[j] = (gone >> j & 1) ? 0 : max(0, min(16, room));
           any |= valid[j];
         }
         if (any) {
-          const uint32_t kb = base + st * C::STAGE + part * (C::PART * C::BOX_ROW), vb = kb + C::PLANE;
+          const uint32_t kb = base + st * C::STAGE, vb = kb + C::PLANE;
           // ---- S^T = K Q^T: rows = positions gq, gq + 8 of a block, columns = heads 2 tq, 2 tq + 1
           float s[BLOCKS][NT][4];
 #pragma unroll
@@ -713,7 +716,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
             // a block of 32 dimensions is two k-steps; its sum counts with the scale that the position has for it
 #pragma unroll
             for (int j = 0; j < BLOCKS; ++j) {
-              const uint8_t* sc = gen + STAGES * C::STAGE + st * C::SCALES + (part * C::PART + r0 + 16 * j + gq) * SCALE;
+              const uint8_t* sc = gen + STAGES * C::STAGE + st * C::SCALES + (r0 + 16 * j + gq) * SCALE;
               float ks[2][DH / INT4_BLOCK];
               load_scales<DH / INT4_BLOCK>(sc, ks[0]);
               load_scales<DH / INT4_BLOCK>(sc + 8 * SCALE, ks[1]);
@@ -846,19 +849,11 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
             [[maybe_unused]] constexpr bool PAIR = decltype(pair)::value;
 #pragma unroll
             for (int j = 0; j < BLOCKS; ++j) {
-              [[maybe_unused]] uint32_t ph0[NT], ph1[NT], pl0[NT], pl1[NT];
-              [[maybe_unused]] float pt[NT][4];                                      // 4 bits: weights of head gq at positions 2 tq, 2 tq + 1, + 8, + 9
+              uint32_t ph0[NT], ph1[NT], pl0[NT], pl1[NT];
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
                 const float* x = s[j][n];
-                if constexpr (INT4) {
-#pragma unroll
-                  for (int i = 0; i < 4; i += 2) {
-                    const uint32_t hi = transpose8x8(upper_halves(x[i], x[i + 1])), lo = transpose8x8(lower_halves(x[i], x[i + 1]));
-                    pt[n][i] = __uint_as_float(__byte_perm(lo, hi, 0x5410));
-                    pt[n][i + 1] = __uint_as_float(__byte_perm(lo, hi, 0x7632));
-                  }
-                } else if constexpr (!PAIR) {
+                if constexpr (!PAIR) {
                   ph0[n] = transpose8x8(pack_f16(x[0], x[1]));
                   ph1[n] = transpose8x8(pack_f16(x[2], x[3]));
                 } else {
@@ -871,39 +866,45 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
               [[maybe_unused]] const uint32_t keep0 = (2 * tq < valid[j] ? 0xffffu : 0u) | (2 * tq + 1 < valid[j] ? 0xffff0000u : 0u);
               [[maybe_unused]] const uint32_t keep1 = (2 * tq + 8 < valid[j] ? 0xffffu : 0u) | (2 * tq + 9 < valid[j] ? 0xffff0000u : 0u);
               if constexpr (INT4) {
-                // a value's scale goes to its weight, which has a bf16's exponents; behind the length it is cleared, whatever it was
-                const uint8_t* sc = gen + STAGES * C::STAGE + st * C::SCALES + (TILE + part * C::PART + r0 + 16 * j + 2 * tq) * SCALE;
-                float vs[4][DH / INT4_BLOCK];
+                // A value's scale goes to its weight: both parts of the weight times the scale, and what the first product's rounding
+                // left goes to the second.  Behind the length scales are cleared, whatever they were.
+                constexpr int WORDS = SCALE / 4;
+                const uint8_t* sc = gen + STAGES * C::STAGE + st * C::SCALES + (TILE + r0 + 16 * j + 2 * tq) * SCALE;
+                uint32_t vs[2][2 * WORDS];                            // of positions 2 tq, + 1 / + 8, + 9, for each block
 #pragma unroll
-                for (int i = 0; i < 4; ++i) load_scales<DH / INT4_BLOCK>(sc + ((i & 1) + 8 * (i >> 1)) * SCALE, vs[i]);
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                  for (int c = 0; c < WORDS; ++c) {
+                    const uint32_t x = *reinterpret_cast<const uint32_t*>(sc + 8 * i * SCALE + 4 * c);
+                    const uint32_t y = *reinterpret_cast<const uint32_t*>(sc + (8 * i + 1) * SCALE + 4 * c);
+                    vs[i][2 * c] = __byte_perm(x, y, 0x5410);
+                    vs[i][2 * c + 1] = __byte_perm(x, y, 0x7632);
+                  }
                 if (valid[j] < 16) {
 #pragma unroll
-                  for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int c = 0; c < DH / INT4_BLOCK; ++c) if (2 * tq + (i & 1) + 8 * (i >> 1) >= valid[j]) vs[i][c] = 0.f;
+                  for (int c = 0; c < 2 * WORDS; ++c) { vs[0][c] &= keep0; vs[1][c] &= keep1; }
                 }
 #pragma unroll
                 for (int k = 0; k < KS; k += 4) {
                   uint32_t a[4];                                      // positions 2 tq, + 1 / + 8, + 9 of a block, then of the next
                   ldmatrix4_trans(vb + swizzled(vrow + 16 * j, k / 2 + vchunk), a);
+                  uint32_t x[2][4], y[2][4];                          // dimensions 4 gq + 0 .. 3 of each block
 #pragma unroll
-                  for (int i = 0; i < 2; ++i) {
-                    uint32_t x[4], y[4];                              // dimensions 4 gq + 0 .. 3 of the block
-                    int4_to_bf16(a[2 * i], x);
-                    int4_to_bf16(a[2 * i + 1], y);
+                  for (int i = 0; i < 2; ++i) { int4_to_bf16(a[2 * i], x[i]); int4_to_bf16(a[2 * i + 1], y[i]); }
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                      float w[4];
+                  for (int n = 0; n < NT; ++n) {
+                    uint32_t h0[2], h1[2], l0[2], l1[2];
 #pragma unroll
-                      for (int e = 0; e < 4; ++e) w[e] = pt[n][e] * vs[e][k / 2 + i];
-                      const uint32_t h0 = upper_halves(w[0], w[1]), h1 = upper_halves(w[2], w[3]);
-                      const uint32_t l0 = pack_rests(w[0], w[1], h0), l1 = pack_rests(w[2], w[3], h1);
-#pragma unroll
-                      for (int e = 0; e < 2; ++e) {
-                        mma16816<false>(o[n][k + 2 * i + e], x[2 * e], x[2 * e + 1], y[2 * e], y[2 * e + 1], h0, h1);
-                        mma16816<false>(o[n][k + 2 * i + e], x[2 * e], x[2 * e + 1], y[2 * e], y[2 * e + 1], l0, l1);
-                      }
+                    for (int i = 0; i < 2; ++i) {
+                      scaled_weight(ph0[n], pl0[n], vs[0][k / 2 + i], h0[i], l0[i]);
+                      scaled_weight(ph1[n], pl1[n], vs[1][k / 2 + i], h1[i], l1[i]);
                     }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                      mma16816<false>(o[n][k + i], x[i / 2][2 * (i & 1)], x[i / 2][2 * (i & 1) + 1], y[i / 2][2 * (i & 1)], y[i / 2][2 * (i & 1) + 1], h0[i / 2], h1[i / 2]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                      mma16816<false>(o[n][k + i], x[i / 2][2 * (i & 1)], x[i / 2][2 * (i & 1) + 1], y[i / 2][2 * (i & 1)], y[i / 2][2 * (i & 1) + 1], l0[i / 2], l1[i / 2]);
                   }
                 }
               } else if constexpr (BF16) {
@@ -957,8 +958,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                 added = true;
               }
           }
-          if (!added) add_values(std::bool_constant<BF16>());
-        }
+          if (!added) add_values(std::bool_constant<!E4M3>());
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(empty(st));
@@ -1005,10 +1005,10 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
           }
       };
       if (C::ALONE && dl.alone) {
-        // the group's two warps: the first leaves its result, the second adds its own, both put the sum out
+        // the group's warps: the first leaves its result, the others add their own, all put the sum out
         float* const pair = pair_of(my_group);
         float* const pair_m = pair + C::HEADS * (DH + PAD);           // [3][HEADS]: maximum, output's maximum, sum
-        group_sync(my_group);                                         // the memory is free
+        group_sync<GROUP_WARPS>(my_group);                                         // the memory is free
         if (warp % GROUP_WARPS == 0) {
           leave_output(pair);
 #pragma unroll
@@ -1017,8 +1017,10 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
             if (gq == 0) { pair_m[h] = m[0][i]; pair_m[C::HEADS + h] = E4M3 ? mo[0][i] : m[0][i]; pair_m[2 * C::HEADS + h] = l[0][i]; }
           }
         }
-        group_sync(my_group);
-        if (warp % GROUP_WARPS == 1) {
+#pragma unroll 1
+        for (int turn_of = 1; turn_of < GROUP_WARPS; ++turn_of) {
+        group_sync<GROUP_WARPS>(my_group);
+        if (warp % GROUP_WARPS == turn_of) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int h = 2 * tq + i;
@@ -1035,10 +1037,11 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                 *y = *y * fa + o[0][k][i + 2] * fb;
               }
             __syncwarp();
-            if (gq == 0) { pair_m[h] = top; pair_m[2 * C::HEADS + h] = la * exp2_fast(ma - ref) + l[0][i] * exp2_fast(m[0][i] - ref); }
+            if (gq == 0) { pair_m[h] = pair_m[C::HEADS + h] = top; pair_m[2 * C::HEADS + h] = la * exp2_fast(ma - ref) + l[0][i] * exp2_fast(m[0][i] - ref); }
           }
         }
-        group_sync(my_group);
+        }
+        group_sync<GROUP_WARPS>(my_group);
         for (int e = tid % (32 * GROUP_WARPS); ok && e < live * (DH / 4); e += 32 * GROUP_WARPS) {
           const int h = e / (DH / 4), d = (e % (DH / 4)) * 4;
           put(p, h, d, *reinterpret_cast<const float4*>(pair + h * (DH + PAD) + d), pair_m[h], pair_m[2 * C::HEADS + h], 0u);
@@ -1180,19 +1183,19 @@ cudaError_t launch(const CUtensorMap& map, const Args& g, int ctas, cudaStream_t
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64 || !ready[dev]) {
-    if (NT == 2) {
+    if (C::SPLIT) {
       // setmaxnreg.inc waits for registers that only exist if the block was launched with LAUNCH_REGS of them a thread
       cudaFuncAttributes fa;
       e = cudaFuncGetAttributes(&fa, attention_paged_kernel<DH, FMT, NT>);
       if (e != cudaSuccess) return e;
-      if (fa.numRegs < LAUNCH_REGS) return cudaErrorLaunchOutOfResources;
+      if (fa.numRegs < C::LAUNCH_REGS) return cudaErrorLaunchOutOfResources;
     }
     e = cudaFuncSetAttribute(attention_paged_kernel<DH, FMT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) ready[dev] = true;
   }
   ET_COUNT_LAUNCH();
-  Launch l(ctas, THREADS, C::SMEM, s);
+  Launch l(ctas, C::THREADS, C::SMEM, s);
   e = cudaLaunchKernelEx(&l.cfg, attention_paged_kernel<DH, FMT, NT>, map, g);
   if (e != cudaSuccess || g.whole) return e;
   ET_COUNT_LAUNCH();
