@@ -67,8 +67,8 @@ struct Cfg {
   static constexpr int GROUP_WARPS = 2, COMPUTE_WARPS = GROUPS * GROUP_WARPS;
   static constexpr int THREADS = 32 * (COMPUTE_WARPS + COPY_WARPS);
   // The computing warps take registers from the copying ones: of what a block is launched with, never more.
-  static constexpr bool SPLIT = NT == 2 || GROUP_WARPS == 4;
-  static constexpr int LAUNCH_REGS = NT == 2 ? 168 : 96, COMPUTE_REGS = NT == 2 ? 208 : 104, COPY_REGS = NT == 2 ? 88 : 64;
+  static constexpr bool SPLIT = NT == 2 || FMT == ET_KV_INT4;
+  static constexpr int LAUNCH_REGS = 168, COMPUTE_REGS = 208, COPY_REGS = 88;
   static_assert(COMPUTE_WARPS % 4 == 0 && COPY_WARPS % 4 == 0, "whole warpgroups");
   static_assert(!SPLIT || COMPUTE_WARPS * COMPUTE_REGS + COPY_WARPS * COPY_REGS <= (COMPUTE_WARPS + COPY_WARPS) * LAUNCH_REGS, "register budget");
   // positions of a tile; each of a group's warps has BLOCKS blocks of 16 of them
