@@ -83,52 +83,30 @@ __device__ __forceinline__ uint2 to_e4m3(const float (&x)[8], float inv) {
   return make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
 }
 
-// 8 or 4 bf16
-template <int N> struct Bf16s;
-template <> struct Bf16s<8> { using type = uint4; };
-template <> struct Bf16s<4> { using type = uint2; };
-template <int N>
-__device__ __forceinline__ void unpack(const typename Bf16s<N>::type& v, float (&x)[N]) {
+__device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
   const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
 #pragma unroll
-  for (int k = 0; k < N / 2; ++k) { const float2 f = __bfloat1622float2(p[k]); x[2 * k] = f.x; x[2 * k + 1] = f.y; }
+  for (int k = 0; k < 4; ++k) { const float2 f = __bfloat1622float2(p[k]); x[2 * k] = f.x; x[2 * k + 1] = f.y; }
 }
-template <int N>
-__device__ __forceinline__ typename Bf16s<N>::type pack(const float (&x)[N]) {
-  typename Bf16s<N>::type v;
+__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
+  uint4 v;
   __nv_bfloat162* p = reinterpret_cast<__nv_bfloat162*>(&v);
 #pragma unroll
-  for (int k = 0; k < N / 2; ++k) p[k] = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]);
+  for (int k = 0; k < 4; ++k) p[k] = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]);
   return v;
 }
 
-// ---- 4 bits.  A block of 32 values has one bf16 scale s, the smallest that is not below max|x| / 7, and codes n + 8 with n = x / s
-// rounded to nearest, ties to even.  Both follow what 64-bit arithmetic gives: a quotient from an approximate reciprocal is within
-// one of the right whole number, and the rest x - n s, which is exact (or off by 2^-53 of x where x has 64 bits), says which it is.
-__device__ __forceinline__ float next_bf16(float x) { return __int_as_float(__float_as_int(x) + 0x10000); }        // x >= 0
-__device__ __forceinline__ float int4_scale(double top) {
-  // the quotient cut off to bf16 is the one below, or the one that is sought, or (the product is rounded) one further below
-  float s = __int_as_float(__float_as_int((float)top * (1.f / 7)) & 0xffff0000);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) if (7.0 * s < top) s = next_bf16(s);
-  return s;
-}
-template <typename T, int N>
-__device__ __forceinline__ uint32_t int4_codes(const T (&x)[N], float s, float up, float inv) {      // inv = 1 / (s up), up a power of two
-  uint32_t w = 0;
-  const T h = (T)s * (T)0.5;
-#pragma unroll
-  for (int k = 0; k < N; ++k) {
-    float n = rintf((float)x[k] * up * inv);
-    const T r = sizeof(T) == 8 ? fma((double)-n, (double)s, (double)x[k]) : (T)fmaf(-n, s, (float)x[k]);
-    const bool odd = (int)n & 1;
-    if (r > h || (odd && r == h)) n += 1.f;
-    else if (r < -h || (odd && r == -h)) n -= 1.f;
-    w |= (uint32_t)((int)n + 8) << (4 * k);
+// Lengths after the call: of the sequences' starts and rows.
+__device__ __forceinline__ void advance_lengths(const PagedCache& c, const PagedRows& r, int* new_len) {
+  for (unsigned s = threadIdx.x; s < (unsigned)r.n_seq; s += THREADS) {
+    const int start = r.start[s];
+    // rows that the call has: an offset that is none of theirs counts as the first or as the end
+    auto row_at = [&](unsigned i) { return min(max(r.offsets[i], 0), r.rows); };
+    const int n = r.offsets ? max(0, row_at(s + 1) - row_at(s)) : 1;
+    const long long cap = (long long)r.max_pages << c.page_shift;
+    new_len[s] = start < 0 ? start : (int)min((long long)start + n, cap);
   }
-  return w;
 }
-constexpr uint32_t INT4_ZEROS = 0x88888888u;                 // eight codes of 0
 
 // x c - y s with two roundings (but for 2^-39 of x and y): x and y have 8 bits, c = c1 + c2 and s = s1 + s2 16 in their first parts,
 // so that the products of those are exact.
@@ -146,17 +124,11 @@ __device__ __forceinline__ float turned_exactly(float x, float c1, float c2, flo
 // e4m3 values, a sixteenth apart (now one in two million; 21 124 rows of 28 + 4 + 4 heads 87.6 -> 93.3 us).  Bound by memory, and with
 // e4m3 and rotation by instructions.
 // ---------------------------------------------------------------------------------------------
-// Values of each half that a lane has.  With 4-bit codes and rotation it holds sines, cosines and keys in 64 bits: half as many, so that
-// more blocks fit an SM.
-__host__ __device__ constexpr int append_each(int format, bool rotate) { return format == ET_KV_INT4 && rotate ? 4 : 8; }
-
-template <int DH, int FMT, bool ROTATE>
+template <int DH, bool E4M3, bool ROTATE>
 __global__ void __launch_bounds__(THREADS)
 kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c, PagedRows r,
                  const __grid_constant__ RopeTurns turns, bf16* q_out, int* new_len, int rows_each, int parts) {
-  constexpr bool E4M3 = FMT == ET_KV_E4M3, INT4 = FMT == ET_KV_INT4;
-  constexpr int HALF = DH / 2, E = append_each(FMT, ROTATE), CHUNKS = HALF / E, UNROLL = 16 / E;
-  using Vec = typename Bf16s<E>::type;
+  constexpr int HALF = DH / 2, CHUNKS = DH / 16, UNROLL = 2;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int part = warp % parts, chunk = lane % CHUNKS, head_lane = lane / CHUNKS;
   constexpr int HEADS_ITER = 32 / CHUNKS;
@@ -180,17 +152,17 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
   const int step = WARPS / parts;
   const long long row0 = (long long)blockIdx.x * step * rows_each, row1 = min(row0 + step * rows_each, (long long)r.rows);
   for (long long row = row0 + warp / parts; row < row1; row += step) {
-    const bf16* const src_row = qkv + row * row_stride + chunk * E;
-    Vec va[UNROLL], vb[UNROLL];
+    const bf16* const src_row = qkv + row * row_stride + chunk * 8;
+    uint4 va[UNROLL], vb[UNROLL];
     auto load = [&](int h0) {
 #pragma unroll
       for (int j = 0; j < UNROLL; ++j) {
         const int head = h0 + j * HEADS_ITER + head_lane;
-        va[j] = vb[j] = Vec{};
+        va[j] = vb[j] = make_uint4(0, 0, 0, 0);
         if (head < all_heads) {
           const bf16* src = src_row + (size_t)head * DH;
-          va[j] = *reinterpret_cast<const Vec*>(src);
-          vb[j] = *reinterpret_cast<const Vec*>(src + HALF);
+          va[j] = *reinterpret_cast<const uint4*>(src);
+          vb[j] = *reinterpret_cast<const uint4*>(src + HALF);
         }
       }
     };
@@ -200,13 +172,11 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
     long long pos;
     if (!places.find(c, r, (int)row, page, place, pos)) continue;          // the same for all lanes
     constexpr bool EXACT = ROTATE && E4M3;
-    float cs[E], sn[E], c1[E], s1[E];                        // EXACT: c1 + cs, s1 + sn
-    double cd[INT4 && ROTATE ? E : 1], sd[INT4 && ROTATE ? E : 1];
+    float cs[8], sn[8], c1[8], s1[8];                        // EXACT: c1 + cs, s1 + sn
     if (ROTATE) {
       // HALF pairs, found by HALF lanes' worth of sincos and handed to the lanes that need them
       constexpr int EACH = HALF / 32 > 0 ? HALF / 32 : 1;
       float mc[EACH], ms[EACH], mc1[EACH], ms1[EACH];
-      double mcd[EACH], msd[EACH];
 #pragma unroll
       for (int j = 0; j < EACH; ++j) {
         const unsigned long long turn = (unsigned long long)pos * turns.f[(lane * EACH + j) % HALF];
@@ -217,22 +187,13 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
           ms1[j] = __int_as_float(__float_as_int((float)s) & 0xffffff00);
           mc[j] = (float)(c - mc1[j]);
           ms[j] = (float)(s - ms1[j]);
-        } else if (INT4) {
-          sincospi((double)(long long)turn * 0x1p-63, &msd[j], &mcd[j]);
         } else {
           sincospif(__ll2float_rn((long long)turn) * 0x1p-63f, &ms[j], &mc[j]);       // half turns in [-1, 1)
         }
       }
 #pragma unroll
-      for (int k = 0; k < E; ++k) {
-        const int from = (chunk * E + k) / EACH;
-        if constexpr (INT4 && ROTATE) {
-          cd[k] = __shfl_sync(0xffffffffu, mcd[k % EACH], from);
-          sd[k] = __shfl_sync(0xffffffffu, msd[k % EACH], from);
-          cs[k] = (float)cd[k];
-          sn[k] = (float)sd[k];
-          continue;
-        }
+      for (int k = 0; k < 8; ++k) {
+        const int from = (chunk * 8 + k) / EACH;
         cs[k] = __shfl_sync(0xffffffffu, mc[k % EACH], from);
         sn[k] = __shfl_sync(0xffffffffu, ms[k % EACH], from);
         if (EXACT) {
@@ -245,47 +206,33 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
 #pragma unroll
       for (int j = 0; j < UNROLL; ++j) {
         const int head = h0 + j * HEADS_ITER + head_lane;
-        float a[E], b[E];
-        unpack<E>(va[j], a);
-        unpack<E>(vb[j], b);
-        // 4 bits: the codes of a key are those that 64-bit arithmetic gives.  With keys turned in fp32 one value in a few hundred
-        // thousand lies on the other side of a border between two codes, which is a seventh of the block's largest value.
-        double ad[INT4 && ROTATE ? E : 1], bd[INT4 && ROTATE ? E : 1];
-        const bool key = head >= heads && head < heads + c.kv_heads;
-        if constexpr (INT4 && ROTATE) {
-          if (key) {
-#pragma unroll
-            for (int k = 0; k < E; ++k) {
-              const double x = a[k], y = b[k];
-              ad[k] = x * cd[k] - y * sd[k];
-              bd[k] = y * cd[k] + x * sd[k];
-            }
-          }
-        }
+        float a[8], b[8];
+        unpack8(va[j], a);
+        unpack8(vb[j], b);
         if (EXACT && head >= heads && head < heads + c.kv_heads) {
 #pragma unroll
-          for (int k = 0; k < E; ++k) {
+          for (int k = 0; k < 8; ++k) {
             const float x = a[k], y = b[k];
             a[k] = turned_exactly(x, c1[k], cs[k], y, s1[k], sn[k]);
             b[k] = turned_exactly(y, c1[k], cs[k], x, -s1[k], -sn[k]);
           }
-        } else if (ROTATE && head < (INT4 ? heads : heads + c.kv_heads)) {
+        } else if (ROTATE && head < heads + c.kv_heads) {
 #pragma unroll
-          for (int k = 0; k < E; ++k) {
+          for (int k = 0; k < 8; ++k) {
             const float x = a[k], y = b[k], co = EXACT ? c1[k] + cs[k] : cs[k], si = EXACT ? s1[k] + sn[k] : sn[k];
             a[k] = x * co - y * si;
             b[k] = y * co + x * si;
           }
         }
         if (ROTATE && head < heads) {
-          Vec* dst = reinterpret_cast<Vec*>(q_out + ((size_t)row * heads + head) * DH + chunk * E);
-          dst[0] = pack<E>(a);
-          dst[HALF / E] = pack<E>(b);
+          uint4* dst = reinterpret_cast<uint4*>(q_out + ((size_t)row * heads + head) * DH + chunk * 8);
+          dst[0] = pack8(a);
+          dst[HALF / 8] = pack8(b);
         }
         float top = 0.f;
         if (E4M3) {
 #pragma unroll
-          for (int k = 0; k < E; ++k) {
+          for (int k = 0; k < 8; ++k) {
             const float x = fabsf(a[k]), y = fabsf(b[k]);
             if (x <= 3.402823466e38f) top = fmaxf(top, x);
             if (y <= 3.402823466e38f) top = fmaxf(top, y);
@@ -293,62 +240,270 @@ kv_append_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c,
 #pragma unroll
           for (int o = CHUNKS / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         }
-        float sa = 0.f, sb = 0.f;                                // 4 bits: scales of the two blocks that this lane has values of
-        if (INT4 && __any_sync(0xffffffffu, head >= heads)) {
-          double ta = 0., tb = 0.;                               // infinite where the block has a value that is not finite
-          auto most = [](double& top, double x) { top = x <= 3.402823466e38 ? fmax(top, x) : (double)INFINITY; };
-          if (ROTATE && key) {
-#pragma unroll
-            for (int k = 0; k < E; ++k) { most(ta, fabs(ad[ROTATE ? k : 0])); most(tb, fabs(bd[ROTATE ? k : 0])); }
-          } else {
-            float fa = 0.f, fb = 0.f;
-            auto most_f = [](float& top, float x) { top = x <= 3.402823466e38f ? fmaxf(top, x) : INFINITY; };
-#pragma unroll
-            for (int k = 0; k < E; ++k) { most_f(fa, fabsf(a[k])); most_f(fb, fabsf(b[k])); }
-            ta = fa; tb = fb;
-          }
-#pragma unroll
-          for (int o = 1; o < INT4_BLOCK / E; o <<= 1) {
-            ta = fmax(ta, __shfl_xor_sync(0xffffffffu, ta, o));
-            tb = fmax(tb, __shfl_xor_sync(0xffffffffu, tb, o));
-          }
-          sa = ta < INFINITY ? int4_scale(ta) : NAN;
-          sb = tb < INFINITY ? int4_scale(tb) : NAN;
-        }
         if (head >= heads && head < all_heads) {
           const int kvh = head - heads;
           const int plane = kvh >= c.kv_heads ? 1 : 0;
           const size_t at = cache_row(c, page, plane, kvh - plane * c.kv_heads, place);
-          if constexpr (INT4) {
-            auto codes = [&](const auto& x, float s) {
-              if (!(s > 0.f)) return INT4_ZEROS;                 // a block of zeros, or of a scale that is NaN
-              const float up = s < 0x1p-100f ? 0x1p64f : 1.f;    // 1 / s would overflow
-              return int4_codes(x, s, up, 1.f / (s * up));
-            };
-            using Codes = typename std::conditional<E == 8, uint32_t, uint16_t>::type;
-            Codes* dst = reinterpret_cast<Codes*>(c.data + at * (DH / 2) + chunk * (E / 2));
-            if (ROTATE && key) {
-              if constexpr (ROTATE) { dst[0] = (Codes)codes(ad, sa); dst[HALF / E] = (Codes)codes(bd, sb); }
-            } else {
-              dst[0] = (Codes)codes(a, sa); dst[HALF / E] = (Codes)codes(b, sb);
-            }
-            if (chunk % (INT4_BLOCK / E) == 0) {
-              bf16* scale = reinterpret_cast<bf16*>(c.scale) + at * (DH / INT4_BLOCK) + chunk / (INT4_BLOCK / E);
-              scale[0] = __float2bfloat16_rn(sa);
-              scale[HALF / INT4_BLOCK] = __float2bfloat16_rn(sb);
-            }
-          } else if constexpr (E4M3) {
+          if (E4M3) {
             const int e = e4m3_exponent(top);
             const float inv = pow2(-e);
-            uint2* dst = reinterpret_cast<uint2*>(c.data + at * DH + chunk * E);
+            uint2* dst = reinterpret_cast<uint2*>(c.data + at * DH + chunk * 8);
             dst[0] = to_e4m3(a, inv);
             dst[HALF / 8] = to_e4m3(b, inv);
             if (chunk == 0) c.scale[at] = (uint8_t)(e + 127);
           } else {
-            Vec* dst = reinterpret_cast<Vec*>(reinterpret_cast<bf16*>(c.data) + at * DH + chunk * E);
-            dst[0] = pack<E>(a);
-            dst[HALF / E] = pack<E>(b);
+            uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(c.data) + at * DH + chunk * 8);
+            dst[0] = pack8(a);
+            dst[HALF / 8] = pack8(b);
           }
+        }
+      }
+      h0 += parts * HEADS_ITER * UNROLL;
+      if (h0 >= all_heads) break;
+      load(h0);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Append to a cache of 4 bits.  A block of 32 values has one bf16 scale s, the smallest that is not below max|x| / 7, and codes n + 8
+// with n = x / s rounded to nearest, ties to even.  Both are what 64-bit arithmetic gives, turned keys' as well: with keys turned in
+// fp32 one value in a few hundred thousand lies on the other side of a border between two codes, a seventh of the block's largest
+// value away.
+//
+// A warp takes a row as above.  The queries come first, eight values of each half a lane, then keys and values, four of each half where
+// keys are turned: sines, cosines and keys in 64 bits take twice the registers.
+// ---------------------------------------------------------------------------------------------
+// N bf16, four or eight
+template <int N> struct Bf16s { uint32_t w[N / 2]; };
+template <int N>
+__device__ __forceinline__ Bf16s<N> load_bf16s(const bf16* p) {
+  Bf16s<N> v;
+  if constexpr (N == 8) {
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
+    v.w[0] = x.x; v.w[1] = x.y; v.w[N / 2 - 2] = x.z; v.w[N / 2 - 1] = x.w;
+  } else {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    v.w[0] = x.x; v.w[1] = x.y;
+  }
+  return v;
+}
+template <int N>
+__device__ __forceinline__ void unpack(const Bf16s<N>& v, float (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) { x[2 * i] = __uint_as_float(v.w[i] << 16); x[2 * i + 1] = __uint_as_float(v.w[i] & 0xffff0000u); }
+}
+// The largest magnitude, infinite if one of them is not finite.
+template <int N>
+__device__ __forceinline__ float largest(const Bf16s<N>& v) {
+  uint32_t m = v.w[0] & 0x7fff7fffu;
+#pragma unroll
+  for (int i = 1; i < N / 2; ++i) m = __vmaxu2(m, v.w[i] & 0x7fff7fffu);
+  const uint32_t top = max(m & 0xffffu, m >> 16);
+  return top < 0x7f80u ? __uint_as_float(top << 16) : INFINITY;
+}
+// A row's queries, turned; a lane has the cosines and sines of HALF / 32 pairs.
+template <int DH>
+__device__ __forceinline__ void turn_queries(const bf16* src, int heads, bf16* dst, const double (&mc)[DH / 64], const double (&ms)[DH / 64],
+                                             int part, int parts) {
+  constexpr int HALF = DH / 2, CHUNKS = HALF / 8, HEADS_ITER = 32 / CHUNKS, UNROLL = 2, EACH = HALF / 32;
+  const int lane = threadIdx.x & 31, chunk = lane % CHUNKS, head_lane = lane / CHUNKS;
+  float co[8], si[8], mcf[EACH], msf[EACH];
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) { mcf[j] = (float)mc[j]; msf[j] = (float)ms[j]; }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    co[k] = __shfl_sync(0xffffffffu, mcf[k % EACH], (chunk * 8 + k) / EACH);
+    si[k] = __shfl_sync(0xffffffffu, msf[k % EACH], (chunk * 8 + k) / EACH);
+  }
+  for (int h0 = part * HEADS_ITER * UNROLL + head_lane; h0 < heads; h0 += parts * HEADS_ITER * UNROLL) {
+    uint4 va[UNROLL], vb[UNROLL];
+#pragma unroll
+    for (int j = 0; j < UNROLL; ++j)
+      if (h0 + j * HEADS_ITER < heads) {
+        const bf16* const p = src + (size_t)(h0 + j * HEADS_ITER) * DH + chunk * 8;
+        va[j] = *reinterpret_cast<const uint4*>(p);
+        vb[j] = *reinterpret_cast<const uint4*>(p + HALF);
+      }
+#pragma unroll
+    for (int j = 0; j < UNROLL; ++j)
+      if (h0 + j * HEADS_ITER < heads) {
+        float a[8], b[8];
+        unpack8(va[j], a);
+        unpack8(vb[j], b);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float x = a[k], y = b[k];
+          a[k] = x * co[k] - y * si[k];
+          b[k] = y * co[k] + x * si[k];
+        }
+        uint4* const q = reinterpret_cast<uint4*>(dst + (size_t)(h0 + j * HEADS_ITER) * DH + chunk * 8);
+        q[0] = pack8(a);
+        q[HALF / 8] = pack8(b);
+      }
+  }
+}
+
+constexpr float MAGIC = 12582912.f;                          // 1.5 * 2^23: adding it rounds to a whole number, ties to even
+
+// The smallest bf16 s with 7 s >= top; top >= 0, finite.  7 s has eleven bits.
+template <typename T>
+__device__ __forceinline__ float int4_scale(T top) {
+  // the quotient cut off to bf16 is the one below, or the one that is sought, or (the product is rounded) one further below
+  float s = __int_as_float(__float_as_int((float)top * (1.f / 7)) & 0xffff0000);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) if ((T)7 * s < top) s = __int_as_float(__float_as_int(s) + 0x10000);
+  return s;
+}
+// The magnitude of a 64-bit number by its upper word, rounded up: enough to find the largest one and to compare it with numbers of up
+// to 21 bits; as integers such words have the numbers' order.
+__device__ __forceinline__ int upper_word(double x) { return (__double2hiint(x) & 0x7fffffff) + (__double2loint(x) != 0 ? 1 : 0); }
+constexpr int UPPER_BEYOND = 0x47f00000;                     // of 2^128
+
+// Four or eight codes.  A quotient of two bf16 that is not half way between two whole numbers is 2^-12 or more away from that; one that
+// is comes out exactly, since one step of Newton's takes its error below 2^-40: adding MAGIC then rounds it as it should be.  Of a
+// number of 64 bits fp32 loses 2^-24, so a quotient next to the half is looked at in 64 bits.
+template <typename T, int N>
+__device__ __forceinline__ uint32_t int4_codes(const T (&x)[N], float s) {
+  if (!(s > 0.f)) return 0x88888888u;                        // a block of zeros, or one whose scale is NaN
+  const bool tiny = s < 0x1p-100f;                           // 1 / s could overflow
+  const float up = tiny ? 0x1p64f : 1.f, su = s * up, inv = __fdividef(1.f, su);
+  float n[N];
+  bool near = false;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const float y = tiny ? (float)(x[k] * (T)up) : (float)x[k], q0 = y * inv, q = fmaf(fmaf(-q0, su, y), inv, q0);
+    n[k] = (q + MAGIC) - MAGIC;
+    if (sizeof(T) == 8) near |= fabsf(fabsf(q - n[k]) - 0.5f) < 0x1p-18f;
+  }
+  if (sizeof(T) == 8 && near) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const double r = fma((double)-n[k], (double)s, (double)x[k]), h = 0.5 * s;
+      const bool odd = (int)n[k] & 1;
+      if (r > h || (odd && r == h)) n[k] += 1.f;
+      else if (r < -h || (odd && r == -h)) n[k] -= 1.f;
+    }
+  }
+  uint32_t w = 0;
+#pragma unroll
+  for (int k = 0; k < N; k += 4) {
+    const float all = fmaf(n[k + 3], 4096.f, fmaf(n[k + 2], 256.f, fmaf(n[k + 1], 16.f, n[k]))) + (34952.f + 8388608.f);       // 34952 = 0x8888
+    w |= (__float_as_uint(all) & 0xffffu) << (4 * k);
+  }
+  return w;
+}
+
+template <int DH, bool ROTATE>
+__global__ void __launch_bounds__(THREADS, ROTATE ? 3 : 4)
+kv_append_int4_kernel(const bf16* qkv, long long row_stride, int heads, PagedCache c, PagedRows r,
+                      const __grid_constant__ RopeTurns turns, bf16* q_out, int* new_len, int rows_each, int parts) {
+  constexpr int HALF = DH / 2;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % parts;
+
+  begin_after_previous();
+  if (new_len && blockIdx.x == 0) advance_lengths(c, r, new_len);
+
+  Places places;
+  const int step = WARPS / parts;
+  const long long row0 = (long long)blockIdx.x * step * rows_each, row1 = min(row0 + step * rows_each, (long long)r.rows);
+  for (long long row = row0 + warp / parts; row < row1; row += step) {
+    const bf16* const src_row = qkv + row * row_stride;
+    // keys and values
+    constexpr int E = ROTATE ? 4 : 8, CHUNKS = HALF / E, HEADS_ITER = 32 / CHUNKS, UNROLL = 2;
+    using Codes = typename std::conditional<E == 8, uint32_t, uint16_t>::type;
+    const int chunk = lane % CHUNKS, head_lane = lane / CHUNKS, all_heads = 2 * c.kv_heads;
+    Bf16s<E> va[UNROLL], vb[UNROLL];
+    auto load = [&](int h0) {
+#pragma unroll
+      for (int j = 0; j < UNROLL; ++j) {
+        const int head = h0 + j * HEADS_ITER + head_lane;
+        va[j] = vb[j] = Bf16s<E>{};
+        if (head < all_heads) {
+          const bf16* src = src_row + (size_t)(heads + head) * DH + chunk * E;
+          va[j] = load_bf16s<E>(src);
+          vb[j] = load_bf16s<E>(src + HALF);
+        }
+      }
+    };
+    int h0 = part * HEADS_ITER * UNROLL;
+    load(h0);                                                // on its way while the row's place is looked up
+    int page, place;
+    long long pos;
+    if (!places.find(c, r, (int)row, page, place, pos)) continue;          // the same for all lanes
+    double cd[ROTATE ? E : 1], sd[ROTATE ? E : 1];
+    if constexpr (ROTATE) {
+      constexpr int EACH = HALF / 32;
+      double mc[EACH], ms[EACH];
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) {
+        const unsigned long long turn = (unsigned long long)pos * turns.f[lane * EACH + j];
+        sincospi((double)(long long)turn * 0x1p-63, &ms[j], &mc[j]);
+      }
+      turn_queries<DH>(src_row, heads, q_out + (size_t)row * heads * DH, mc, ms, part, parts);
+#pragma unroll
+      for (int k = 0; k < E; ++k) {
+        cd[k] = __shfl_sync(0xffffffffu, mc[k % EACH], (chunk * E + k) / EACH);
+        sd[k] = __shfl_sync(0xffffffffu, ms[k % EACH], (chunk * E + k) / EACH);
+      }
+    }
+    for (;;) {
+#pragma unroll
+      for (int j = 0; j < UNROLL; ++j) {
+        const int head = h0 + j * HEADS_ITER + head_lane;
+        if (h0 + j * HEADS_ITER >= all_heads) break;         // the same for all lanes
+        const bool key = ROTATE && head < c.kv_heads;
+        float a[E], b[E];
+        unpack(va[j], a);
+        unpack(vb[j], b);
+        float sa, sb;
+        uint32_t ca, cb;
+        // keys among the warp's heads, values among them; where both are, every lane goes both ways
+        if constexpr (ROTATE) if (__any_sync(0xffffffffu, key)) {
+          double ad[E], bd[E];
+          int ta = 0, tb = 0;
+#pragma unroll
+          for (int k = 0; k < E; ++k) {
+            const double x = a[k], y = b[k], co = cd[k], si = sd[k];
+            ad[k] = x * co - y * si;
+            bd[k] = y * co + x * si;
+            ta = max(ta, upper_word(ad[k]));
+            tb = max(tb, upper_word(bd[k]));
+          }
+#pragma unroll
+          for (int o = 1; o < INT4_BLOCK / E; o <<= 1) {
+            ta = max(ta, __shfl_xor_sync(0xffffffffu, ta, o));
+            tb = max(tb, __shfl_xor_sync(0xffffffffu, tb, o));
+          }
+          sa = ta <= UPPER_BEYOND ? int4_scale(__hiloint2double(ta, 0)) : NAN;
+          sb = tb <= UPPER_BEYOND ? int4_scale(__hiloint2double(tb, 0)) : NAN;
+          ca = int4_codes(ad, sa);
+          cb = int4_codes(bd, sb);
+        }
+        if (!ROTATE || __any_sync(0xffffffffu, !key)) {
+          float ta = largest(va[j]), tb = largest(vb[j]);
+#pragma unroll
+          for (int o = 1; o < INT4_BLOCK / E; o <<= 1) {
+            ta = fmaxf(ta, __shfl_xor_sync(0xffffffffu, ta, o));
+            tb = fmaxf(tb, __shfl_xor_sync(0xffffffffu, tb, o));
+          }
+          if (!key) {
+            sa = ta < INFINITY ? int4_scale(ta) : NAN;
+            sb = tb < INFINITY ? int4_scale(tb) : NAN;
+            ca = int4_codes(a, sa);
+            cb = int4_codes(b, sb);
+          }
+        }
+        if (head >= all_heads) continue;
+        const int plane = head >= c.kv_heads ? 1 : 0;
+        const size_t at = cache_row(c, page, plane, head - plane * c.kv_heads, place);
+        Codes* const dst = reinterpret_cast<Codes*>(c.data + at * (DH / 2) + chunk * (E / 2));
+        dst[0] = (Codes)ca;
+        dst[HALF / E] = (Codes)cb;
+        if (chunk % (INT4_BLOCK / E) == 0) {
+          bf16* const scale = reinterpret_cast<bf16*>(c.scale) + at * (DH / INT4_BLOCK) + chunk / (INT4_BLOCK / E);
+          scale[0] = __float2bfloat16_rn(sa);
+          scale[HALF / INT4_BLOCK] = __float2bfloat16_rn(sb);
         }
       }
       h0 += parts * HEADS_ITER * UNROLL;
@@ -407,7 +562,7 @@ kv_read_kernel(bf16* out, long long row_stride, PagedCache c, PagedRows r, int r
           float y[8];
 #pragma unroll
           for (int k = 0; k < 8; ++k) y[k] = (float)((int)(v[j].x >> (4 * k) & 15) - 8) * s;
-          *dst = pack<8>(y);
+          *dst = pack8(y);
         } else if (E4M3) {
           const float f = pow2(b[j] - 127);
           const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
@@ -419,8 +574,8 @@ kv_read_kernel(bf16* out, long long row_stride, PagedCache c, PagedRows r, int r
             (k < 4 ? lo : hi)[(2 * k) % 8] = y.x * f;
             (k < 4 ? lo : hi)[(2 * k + 1) % 8] = y.y * f;
           }
-          dst[0] = pack<8>(lo);
-          dst[1] = pack<8>(hi);
+          dst[0] = pack8(lo);
+          dst[1] = pack8(hi);
         } else {
           *dst = v[j];
         }
@@ -451,14 +606,16 @@ cudaError_t launch_kv_append(const PagedCache& c, const PagedRows& r, const bf16
   const Deal d = deal_rows(r.rows, cdiv(((rotate ? heads : 0) + 2 * c.kv_heads) * (c.head_dim / 16), 64));
   Launch l(d.blocks, THREADS, 0, s);
 #define ET_APPEND(D, E, R) return cudaLaunchKernelEx(&l.cfg, kv_append_kernel<D, E, R>, qkv, row_stride, heads, c, r, turns, q_out, new_len, d.each, d.parts)
+#define ET_APPEND4(D, R) return cudaLaunchKernelEx(&l.cfg, kv_append_int4_kernel<D, R>, qkv, row_stride, heads, c, r, turns, q_out, new_len, d.each, d.parts)
 #define ET_APPEND_D(D)                                                       \
   do {                                                                       \
-    if (c.format == ET_KV_INT4) { if (rotate) ET_APPEND(D, ET_KV_INT4, true); else ET_APPEND(D, ET_KV_INT4, false); }   \
-    else if (c.format == ET_KV_E4M3) { if (rotate) ET_APPEND(D, ET_KV_E4M3, true); else ET_APPEND(D, ET_KV_E4M3, false); }   \
-    else { if (rotate) ET_APPEND(D, ET_KV_BF16, true); else ET_APPEND(D, ET_KV_BF16, false); }                         \
+    if (c.format == ET_KV_INT4) { if (rotate) ET_APPEND4(D, true); else ET_APPEND4(D, false); }      \
+    else if (c.format == ET_KV_E4M3) { if (rotate) ET_APPEND(D, true, true); else ET_APPEND(D, true, false); }   \
+    else { if (rotate) ET_APPEND(D, false, true); else ET_APPEND(D, false, false); }               \
   } while (0)
   if (c.head_dim == 64) ET_APPEND_D(64); else ET_APPEND_D(128);
 #undef ET_APPEND_D
+#undef ET_APPEND4
 #undef ET_APPEND
 }
 
