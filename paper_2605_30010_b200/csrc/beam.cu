@@ -21,7 +21,8 @@ constexpr int THREADS = 256, WARPS = THREADS / 32, EACH = 16, CHUNK = THREADS * 
 static_assert(CHUNK == ET_BEAM_CHUNK, "workspace");
 constexpr int K_MAX = 64, BEAMS_MAX = 32, SEGMENTS_MAX = 64;
 constexpr int LONG = 192, LIST = CHUNK + LONG;      // the list is cut back when it has more than LONG entries; a chunk adds CHUNK at most
-constexpr int RANKED = 1024;                        // up to so many entries each one's rank is counted
+constexpr int RANKED = 1024;                        // up to so many keys each one's rank is counted
+constexpr int FEW = 8;                              // up to so many of a first chunk are bounded by groups of threads, more by warps
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct Select {
@@ -39,6 +40,19 @@ struct Select {
 
 // What a segment leaves: its best k (value, token) in order, (-infinity, -1) behind the last, and (maximum, sum).
 struct Entry { float value; int token; };
+// Floats as whole numbers of the same order, above 0.
+__device__ __forceinline__ uint32_t ordered(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+}
+// A (value, token) as one number, larger for a larger value, among equal ones for the lower token; no such number is 0.
+__device__ __forceinline__ unsigned long long key_of(float value, int token) {
+  return (unsigned long long)ordered(value + 0.f) << 32 | (0xffffffffu - (uint32_t)token);      // (the zeros are equal)
+}
+__device__ __forceinline__ Entry entry_of(unsigned long long key) {
+  const uint32_t u = (uint32_t)(key >> 32);
+  return Entry{__uint_as_float(u ^ (u >> 31 ? 0x80000000u : 0xffffffffu)), (int)(0xffffffffu - (uint32_t)key)};
+}
 __host__ __device__ constexpr size_t segment_bytes(int k) { return 8 * (size_t)k + 16; }
 __device__ __forceinline__ unsigned char* segment_of(const Select& a, int row, int segment) {
   return a.workspace + ((size_t)row * a.segments + segment) * segment_bytes(a.k);
@@ -52,52 +66,46 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
-// The list's best k entries, in order, to its front.  All threads; the list is complete.
-__device__ __forceinline__ int cut_back(Entry* list, int n, int k, Entry* best, uint2* reduce) {
-  const int tid = threadIdx.x;
-  auto before = [](const Entry& a, const Entry& b) { return a.value > b.value || (a.value == b.value && a.token < b.token); };
-  const int kept = min(n, k);
+// The list's best k keys, in order, to its front; returns how many.  All threads; the list is complete.
+__device__ __forceinline__ int cut_back(unsigned long long* list, int n, int k, unsigned long long* best) {
+  const int tid = threadIdx.x, kept = min(n, k);
   if (n <= RANKED) {
-    Entry mine[RANKED / THREADS];
+    // each key's rank is how many are larger
+    unsigned long long mine[RANKED / THREADS];
     int rank[RANKED / THREADS];
 #pragma unroll
     for (int j = 0; j < RANKED / THREADS; ++j) {
-      if (j * THREADS >= n) break;
-      rank[j] = k;
       const int e = tid + j * THREADS;
+      rank[j] = k;
       if (e >= n) continue;
       mine[j] = list[e];
       int r = 0;
-      for (int i = 0; i < n; ++i) r += before(list[i], mine[j]);
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) r += list[i] > mine[j];
       rank[j] = r;
     }
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < RANKED / THREADS; ++j) {
-      if (j * THREADS >= n) break;
-      if (rank[j] < k) list[rank[j]] = mine[j];
-    }
+    for (int j = 0; j < RANKED / THREADS; ++j) if (rank[j] < k) list[rank[j]] = mine[j];
   } else {
-    // many values that are equal or come in an unlucky order: the best one, k times
+    // many values that are equal or come in an unlucky order: the largest one, k times
     for (int r = 0; r < kept; ++r) {
-      Entry top{-INFINITY, 0x7fffffff};
-      int at = -1;
-      for (int e = tid; e < n; e += THREADS) if (before(list[e], top)) { top = list[e]; at = e; }
+      unsigned long long top = 0;
+      int at = 0;
+      for (int e = tid; e < n; e += THREADS) if (list[e] > top) { top = list[e]; at = e; }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) {
-        Entry other;
-        other.value = __shfl_xor_sync(0xffffffffu, top.value, o);
-        other.token = __shfl_xor_sync(0xffffffffu, top.token, o);
+        const unsigned long long other = __shfl_xor_sync(0xffffffffu, top, o);
         const int other_at = __shfl_xor_sync(0xffffffffu, at, o);
-        if (before(other, top)) { top = other; at = other_at; }
+        if (other > top) { top = other; at = other_at; }
       }
-      if ((tid & 31) == 0) { best[WARPS + (tid >> 5)] = top; reduce[tid >> 5].x = at; }
+      if ((tid & 31) == 0) { best[2 * (tid >> 5)] = top; best[2 * (tid >> 5) + 1] = (unsigned long long)at; }
       __syncthreads();
       if (tid == 0) {
         int w = 0;
-        for (int i = 1; i < WARPS; ++i) if (before(best[WARPS + i], best[WARPS + w])) w = i;
-        best[2 * WARPS + r] = best[WARPS + w];
-        list[reduce[w].x] = Entry{-INFINITY, 0x7fffffff};
+        for (int i = 1; i < WARPS; ++i) if (best[2 * i] > best[2 * w]) w = i;
+        best[2 * WARPS + r] = best[2 * w];
+        list[best[2 * w + 1]] = 0;
       }
       __syncthreads();
     }
@@ -107,14 +115,27 @@ __device__ __forceinline__ int cut_back(Entry* list, int n, int k, Entry* best, 
   return kept;
 }
 
+// A warp's 32 values in descending order.
+__device__ __forceinline__ float sorted(float g) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+    for (int o = size >> 1; o > 0; o >>= 1) {
+      const float other = __shfl_xor_sync(0xffffffffu, g, o);
+      g = ((lane & size) == 0) == ((lane & o) == 0) ? fmaxf(g, other) : fminf(g, other);
+    }
+  return g;
+}
+
 template <bool FP32, bool ALIGNED>
 __global__ void __launch_bounds__(THREADS)
 beam_scan_kernel(const __grid_constant__ Select a) {
   constexpr int SIZE = FP32 ? 4 : 2, VEC = 16 / SIZE, SLOTS = EACH / VEC;
-  extern __shared__ Entry list[];                   // [LIST]
-  __shared__ int listed;
-  __shared__ float group_top[64];
-  __shared__ Entry best[2 * WARPS + K_MAX];
+  extern __shared__ unsigned long long list[];      // [LIST] keys
+  __shared__ int added_s[3];                        // keys that a chunk adds, in turn
+  __shared__ float group_top[32];
+  __shared__ unsigned long long best[2 * WARPS + K_MAX];
   __shared__ uint2 reduce[WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, segment = blockIdx.x, row = blockIdx.y;
   begin_after_previous();
@@ -165,9 +186,10 @@ beam_scan_kernel(const __grid_constant__ Select a) {
   };
   uint32_t raw[SLOTS][WORDS];
   if (first < last) load(first, raw);
-  if (tid == 0) listed = 0;
+  if (tid < 3) added_s[tid] = 0;
+  __syncthreads();
   float m = -INFINITY, s = 0.f, bar = -INFINITY;    // bar: what a logit has to reach or, behind the first chunk, to pass
-  int n = 0;
+  int n = 0, turn = 0;
   bool begun = false;
   for (int at = first; at < last; at += CHUNK) {
     float x[EACH];
@@ -179,9 +201,12 @@ beam_scan_kernel(const __grid_constant__ Select a) {
         x[j * VEC + v] = __uint_as_float(FP32 ? raw[j][v & 3] : v & 1 ? raw[j][v / 2] & 0xffff0000u : raw[j][v / 2] << 16);
     }
     if (at + CHUNK < last) load(at + CHUNK, raw);   // on its way while this chunk is looked at
-    float top = x[0];
+    float top4[EACH / 4], top;
 #pragma unroll
-    for (int i = 1; i < EACH; ++i) top = fmaxf(top, x[i]);
+    for (int i = 0; i < EACH; i += 4) top4[i / 4] = fmaxf(fmaxf(x[i], x[i + 1]), fmaxf(x[i + 2], x[i + 3]));
+    top = top4[0];
+#pragma unroll
+    for (int i = 1; i < EACH / 4; ++i) top = fmaxf(top, top4[i]);
     if (top > m) { s *= exp2_fast((m - top) * LOG2E); m = top; }
     const float ref = m == -INFINITY ? 0.f : m;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
@@ -189,50 +214,49 @@ beam_scan_kernel(const __grid_constant__ Select a) {
     for (int i = 0; i < EACH; ++i) sum[i & 3] += exp2_fast((x[i] - ref) * LOG2E);
     s += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     if (!begun) {
-      float g = top;
-      const int lanes = a.k <= 32 ? 8 : 4;          // of a group
-      for (int o = 1; o < lanes; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
-      if (lane % lanes == 0) group_top[(warp * 32 + lane) / lanes] = g;
-      __syncthreads();
-      if (a.k <= 32) {
-        g = group_top[lane];
-        // the 32 maxima in descending order
+      if (a.k <= FEW) {
+        // the k-th largest of the maxima of 32 groups of eight threads
+        float g = top;
 #pragma unroll
-        for (int size = 2; size <= 32; size <<= 1)
-#pragma unroll
-          for (int o = size >> 1; o > 0; o >>= 1) {
-            const float other = __shfl_xor_sync(0xffffffffu, g, o);
-            g = ((lane & size) == 0) == ((lane & o) == 0) ? fmaxf(g, other) : fminf(g, other);
-          }
-        bar = __shfl_sync(0xffffffffu, g, a.k - 1);
+        for (int o = 1; o < 8; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
+        if (lane % 8 == 0) group_top[warp * 4 + lane / 8] = g;
+        __syncthreads();
+        bar = __shfl_sync(0xffffffffu, sorted(group_top[lane]), a.k - 1);
       } else {
-        g = fminf(group_top[lane], group_top[lane + 32]);
+        // in each warp as many threads' maxima as its share of k; the least of these
+        const float g = __shfl_sync(0xffffffffu, sorted(top), (a.k + WARPS - 1) / WARPS - 1);
+        if (lane == 0) group_top[warp] = g;
+        __syncthreads();
+        bar = group_top[0];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) g = fminf(g, __shfl_xor_sync(0xffffffffu, g, o));
-        bar = g;
+        for (int w = 1; w < WARPS; ++w) bar = fminf(bar, group_top[w]);
       }
     }
+    int* const added = added_s + turn;
     if (begun ? top > bar : top >= bar)
 #pragma unroll
-      for (int j = 0; j < SLOTS; ++j)
+      for (int i = 0; i < EACH; i += 4)
+        if (begun ? top4[i / 4] > bar : top4[i / 4] >= bar)
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          const float y = x[j * VEC + v];
-          if ((begun ? y > bar : y >= bar) && y > -INFINITY) list[atomicAdd(&listed, 1)] = Entry{y + 0.f, at + place(j) + v};
-        }
+          for (int e = i; e < i + 4; ++e)
+            if ((begun ? x[e] > bar : x[e] >= bar) && x[e] > -INFINITY)
+              list[n + atomicAdd(added, 1)] = key_of(x[e], at + place(e / VEC) + e % VEC);
+    // Counters go round three: this one is read behind the barrier, when the next chunk may be adding to the next one already, which was
+    // read before the last barrier.
+    if (tid == 0) added_s[turn == 2 ? 0 : turn + 1] = 0;
     __syncthreads();
-    n = listed;
+    n += *added;
+    turn = turn == 2 ? 0 : turn + 1;
     if (!begun || n > LONG) {
-      n = cut_back(list, n, a.k, best, reduce);
-      bar = n == a.k ? list[a.k - 1].value : -INFINITY;
+      n = cut_back(list, n, a.k, best);
+      bar = n == a.k ? entry_of(list[a.k - 1]).value : -INFINITY;
       begun = true;
-      if (tid == 0) listed = n;
+      __syncthreads();                              // the list is read before the next chunk adds to it
     }
-    __syncthreads();                                // listed is read before the next chunk adds to it
   }
-  n = cut_back(list, n, a.k, best, reduce);
+  n = cut_back(list, n, a.k, best);
   unsigned char* const out = segment_of(a, row, segment);
-  if (tid < a.k) reinterpret_cast<Entry*>(out)[tid] = tid < n ? list[tid] : Entry{-INFINITY, -1};
+  if (tid < a.k) reinterpret_cast<Entry*>(out)[tid] = tid < n ? entry_of(list[tid]) : Entry{-INFINITY, -1};
   float big = m;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
@@ -252,124 +276,181 @@ beam_scan_kernel(const __grid_constant__ Select a) {
   }
 }
 
-// Floats and doubles as whole numbers of the same order, above 0.
-__device__ __forceinline__ uint32_t ordered(float x) {
-  const uint32_t u = __float_as_uint(x);
-  return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
-}
-__device__ __forceinline__ unsigned long long ordered(double x) {
-  const unsigned long long u = (unsigned long long)__double_as_longlong(x);
-  return u ^ (u >> 63 ? ~0ull : 1ull << 63);
-}
-
-// The front of one segment's list, a few entries in registers.
-struct Front {
-  static constexpr int AHEAD = 4;
-  const Entry* from;
-  Entry e[AHEAD];
-  int have, next;
-  __device__ __forceinline__ void fill(int k) {
+// The best 32 EACH keys of a row's lists, in order, key lane + 32 j in best[j]; the first k are put out.  Returns how many there are.
+template <int EACH, class Put>
+__device__ __forceinline__ int merge_lists(const Select& a, int row, Put put) {
+  const int lane = threadIdx.x & 31;
+  auto load = [&](int segment, unsigned long long (&key)[EACH]) {
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      e[i] = Entry{-INFINITY, -1};
-      if (from && next + i < k) {
-        const float2 v = __ldcg(reinterpret_cast<const float2*>(from + next + i));
-        e[i] = Entry{v.x, __float_as_int(v.y)};
-      }
+    for (int j = 0; j < EACH; ++j) {
+      const int e = lane + 32 * j;
+      float2 v = make_float2(-INFINITY, 0.f);
+      if (e < a.k && segment < a.segments) v = __ldcg(reinterpret_cast<const float2*>(segment_of(a, row, segment)) + e);
+      key[j] = v.x > -INFINITY ? key_of(v.x, __float_as_int(v.y)) : 0;
     }
-    next += AHEAD;
-    have = AHEAD;
-  }
-  __device__ __forceinline__ uint32_t key() const { return e[0].token < 0 ? 0u : ordered(e[0].value); }
-  __device__ __forceinline__ void pop(int k) {
+  };
+  unsigned long long best[EACH], next[EACH], after[EACH];
+  load(0, best);
+  load(1, next);
+  for (int segment = 1; segment < a.segments; ++segment) {
+    load(segment + 1, after);
+    // the first of the one list with the last of the other: the larger ones are the best of both, and go up and down at most once
+    unsigned long long x[EACH];
 #pragma unroll
-    for (int i = 0; i + 1 < AHEAD; ++i) e[i] = e[i + 1];
-    e[AHEAD - 1] = Entry{-INFINITY, -1};
-    if (--have == 0) fill(k);
+    for (int j = 0; j < EACH; ++j) x[j] = __shfl_sync(0xffffffffu, next[EACH - 1 - j], 31 - lane);
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) if (x[j] > best[j]) best[j] = x[j];
+    if (EACH == 2 && best[EACH - 1] > best[0]) { const unsigned long long y = best[0]; best[0] = best[EACH - 1]; best[EACH - 1] = y; }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) {
+        const unsigned long long other = __shfl_xor_sync(0xffffffffu, best[j], o);
+        if ((lane & o) == 0 ? other > best[j] : other < best[j]) best[j] = other;
+      }
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) next[j] = after[j];
   }
-};
+  int count = 0;
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) {
+    const int e = lane + 32 * j;
+    if (e < a.k && best[j] != 0) put(e, best[j]);
+    count += __popc(__ballot_sync(0xffffffffu, e < a.k && best[j] != 0));
+  }
+  return count;
+}
 
-// A block joins a request: a warp each beam's segments, the first warp the beams.
-__global__ void beam_join_kernel(const __grid_constant__ Select a) {
-  extern __shared__ Entry beam_list[];              // [beams][k]
-  __shared__ double base_s[BEAMS_MAX];
+// A block joins a request, a warp each beam: the best k of its segments' lists, in order, then where these stand among all beams'.
+constexpr int NEAR = 64;                            // keys of a beam that may be among its best k: up to so many are ranked at once
+__host__ __device__ constexpr size_t join_bytes(int beams, int k) { return (size_t)beams * (NEAR * 8 + 12 * (size_t)k); }
+__global__ void __launch_bounds__(32 * BEAMS_MAX, 1)
+beam_join_kernel(const __grid_constant__ Select a) {
+  extern __shared__ unsigned long long join_smem[];                         // [beams][NEAR] keys, [beams][k] scores, [beams][k] tokens
   __shared__ int count_s[BEAMS_MAX];
   const int lane = threadIdx.x & 31, beam = threadIdx.x >> 5, request = blockIdx.x, row = request * a.beams + beam, k = a.k;
+  unsigned long long* const near = join_smem + beam * NEAR;
+  double* const scores = reinterpret_cast<double*>(join_smem + a.beams * NEAR);
+  int* const tokens = reinterpret_cast<int*>(scores + a.beams * k);
+  double* const mine = scores + beam * k;
   begin_after_previous();
   const float score = score_of(a, row);
-  Entry* const mine = beam_list + beam * k;
   int count = 0;
-  double base = 0.;
   if (!finite(score)) {
   } else if (done_of(a, row)) {
-    if (lane == 0) mine[0] = Entry{0.f, a.eos};
-    base = score;
+    if (lane == 0) { mine[0] = score; tokens[beam * k] = a.eos; }
     count = 1;
   } else {
-    Front front[2];
-    float2 part[2];
+    // Two lists a lane, their maxima and sums; entries: all of them where they are few (lane + 32 i of the lists one behind the other),
+    // else the first ones of the lane's lists.  All are on their way at once.
+    constexpr int AHEAD = 4;
+    const bool few = a.segments * k <= 64 * AHEAD;
+    auto list_of = [&](int segment) { return reinterpret_cast<const float2*>(segment_of(a, row, segment)); };
+    float2 part[2], e[2][AHEAD];
+    auto load = [&](int i, int first) {
+#pragma unroll
+      for (int p = 0; p < AHEAD; ++p)
+        e[i][p] = lane + 32 * i < a.segments && first + p < k ? __ldcg(list_of(lane + 32 * i) + first + p) : make_float2(-INFINITY, 0.f);
+    };
+    // what at least k entries reach: of the first 32 lists' first ones the k-th largest, of their later ones the least
+    const int lists = min(a.segments, 32), each = (k + lists - 1) / lists;
+    float bar = lane < lists ? __ldcg(list_of(lane) + each - 1).x : -INFINITY;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int segment = lane + 32 * i;
-      const unsigned char* const at = segment_of(a, row, segment);
-      front[i].from = segment < a.segments ? reinterpret_cast<const Entry*>(at) : nullptr;
-      front[i].next = 0;
-      part[i] = segment < a.segments ? __ldcg(reinterpret_cast<const float2*>(at + 8 * (size_t)k)) : make_float2(-INFINITY, 0.f);
-      front[i].fill(k);
+      part[i] = lane + 32 * i < a.segments ? __ldcg(list_of(lane + 32 * i) + k) : make_float2(-INFINITY, 0.f);
+      if (!few) { load(i, 0); continue; }
+#pragma unroll
+      for (int p = 0; p < AHEAD; ++p) {
+        const int at = lane + 32 * (i * AHEAD + p), segment = at / k;
+        e[i][p] = segment < a.segments ? __ldcg(list_of(segment) + at - segment * k) : make_float2(-INFINITY, 0.f);
+      }
     }
+    if (each == 1) {
+      bar = __shfl_sync(0xffffffffu, sorted(bar), k - 1);
+    } else {
+      if (lane >= lists) bar = INFINITY;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) bar = fminf(bar, __shfl_xor_sync(0xffffffffu, bar, o));
+    }
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      bool more = few || 32 * i < a.segments;
+      for (int first = 0; more; first += AHEAD) {
+        if (first > 0) load(i, first);
+#pragma unroll
+        for (int p = 0; p < AHEAD; ++p) {
+          const bool take = e[i][p].x >= bar && e[i][p].x > -INFINITY;
+          const unsigned who = __ballot_sync(0xffffffffu, take);
+          const int at = n + __popc(who & ((1u << lane) - 1));
+          if (take && at < NEAR) near[at] = key_of(e[i][p].x, __float_as_int(e[i][p].y));
+          n += __popc(who);
+          more = !few && who != 0 && n <= NEAR;
+        }
+      }
+    }
+    __syncwarp();
     float big = fmaxf(part[0].x, part[1].x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
     double sum = 0.;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) sum += part[i].y * (part[i].x == big ? 1. : exp((double)part[i].x - big));
+    for (int i = 0; i < 2; ++i) sum += part[i].y * (part[i].x == big ? 1.f : expf(part[i].x - big));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    base = (double)score - ((double)big + log(sum));
-    if (finite(big) && base >= -1.7e308 && base <= 1.7e308) {
-      for (; count < k; ++count) {
-        const uint32_t u0 = front[0].key(), u1 = front[1].key(), top = __reduce_max_sync(0xffffffffu, max(u0, u1));
-        if (top == 0) break;
-        const unsigned low = __ballot_sync(0xffffffffu, u0 == top), high = __ballot_sync(0xffffffffu, u1 == top);
-        // lower segments have lower tokens
-        if (low) {
-          if (lane == __ffs(low) - 1) { mine[count] = front[0].e[0]; front[0].pop(k); }
-        } else if (lane == __ffs(high) - 1) {
-          mine[count] = front[1].e[0]; front[1].pop(k);
-        }
-        __syncwarp();
+    const double base = (double)score - ((double)big + log(sum));
+    auto put = [&](int rank, unsigned long long key) {
+      const Entry e = entry_of(key);
+      mine[rank] = base + (double)e.value;
+      tokens[beam * k + rank] = e.token;
+    };
+    if (!finite(big) || !(base >= -1.7e308 && base <= 1.7e308)) {
+    } else if (n <= NEAR) {
+      for (int e = lane; e < n; e += 32) {
+        const unsigned long long key = near[e];
+        int rank = 0;
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) rank += near[i] > key;
+        if (rank < k) put(rank, key);
       }
+      count = min(n, k);
+    } else {
+      // too many: list by list, of two lists in order the best of both and these in order again
+      count = k <= 32 ? merge_lists<1>(a, row, put) : merge_lists<2>(a, row, put);
     }
   }
-  if (lane == 0) { base_s[beam] = base; count_s[beam] = count; }
+  if (lane == 0) count_s[beam] = count;
   __syncthreads();
-  if (beam != 0) return;
-  const int n = lane < a.beams ? count_s[lane] : 0;
-  base = lane < a.beams ? base_s[lane] : 0.;
-  const Entry* const of = beam_list + lane * k;
-  Entry e{};
-  int next = 0;
-  unsigned long long key = 0;
-  auto advance = [&]() {
-    key = 0;
-    if (next < n) { e = of[next]; key = ordered(base + (double)e.value); }
-    ++next;
-  };
-  advance();
-  for (int i = 0; i < k; ++i) {
-    const uint32_t hi = (uint32_t)(key >> 32), top = __reduce_max_sync(0xffffffffu, hi);
-    const uint32_t lo = hi == top ? (uint32_t)key : 0u, top_lo = __reduce_max_sync(0xffffffffu, lo);
-    const unsigned who = __ballot_sync(0xffffffffu, key != 0 && hi == top && (uint32_t)key == top_lo);
-    const int winner = who ? __ffs(who) - 1 : 0;
-    if (lane == winner) {
-      const size_t at = (size_t)request * k + i;
-      a.parent[at] = who ? request * a.beams + lane : -1;
-      a.token[at] = who ? e.token : -1;
-      a.new_scores[at] = who ? (float)(base + (double)e.value) : -INFINITY;
-      if (a.new_done) a.new_done[at] = !who || e.token == a.eos;
-      if (who) advance();
+  // a continuation's place: those of its beam before it, and those of the others that are better, or as good and of a lower beam
+  for (int e = lane; e < count; e += 32) {
+    const double x = mine[e];
+    int rank = e;
+    for (int b = 0; b < a.beams && rank < k; ++b) {
+      if (b == beam) continue;
+      const double* const of = scores + b * k;
+      int lo = 0, n = count_s[b];                   // how many of the list's are before this one: it is in descending order
+      while (n > 0) {
+        const int half = n >> 1;
+        if (of[lo + half] > x || (of[lo + half] == x && b < beam)) { lo += half + 1; n -= half + 1; } else n = half;
+      }
+      rank += lo;
     }
-    __syncwarp();
+    if (rank < k) {
+      const size_t at = (size_t)request * k + rank;
+      const int token = tokens[beam * k + e];
+      a.parent[at] = row;
+      a.token[at] = token;
+      a.new_scores[at] = (float)x;
+      if (a.new_done) a.new_done[at] = token == a.eos;
+    }
+  }
+  int all = 0;
+  for (int b = 0; b < a.beams; ++b) all += count_s[b];
+  for (int i = all + threadIdx.x; i < k; i += blockDim.x) {
+    const size_t at = (size_t)request * k + i;
+    a.parent[at] = a.token[at] = -1;
+    a.new_scores[at] = -INFINITY;
+    if (a.new_done) a.new_done[at] = 1;
   }
 }
 
@@ -391,8 +472,9 @@ extern "C" et_status et_beam_select(const void* logits_dev, int logits_fp32, lon
   if (beams > BEAMS_MAX || k > K_MAX || vocab > 1 << 20 || (long long)n_req * beams > 65535) return ET_ERR_CAPACITY;
   const int rows = n_req * beams, chunks = cdiv(vocab, CHUNK);
   if (workspace_bytes < ET_BEAM_WORKSPACE(rows, vocab, k)) return ET_ERR_CAPACITY;
-  // six blocks an SM are there at once; more segments than that are only more lists to join
-  int segments = cdiv(148 * 6, rows);
+  // as many segments as keep all blocks resident at once
+  constexpr int BLOCKS = 148 * 4;
+  int segments = rows < BLOCKS ? BLOCKS / rows : 1;
   if (segments > chunks) segments = chunks;
   if (segments > SEGMENTS_MAX) segments = SEGMENTS_MAX;
   const int each = cdiv(chunks, segments);
@@ -401,13 +483,18 @@ extern "C" et_status et_beam_select(const void* logits_dev, int logits_fp32, lon
                  parent_dev, token_dev, new_scores_dev, new_done_dev};
   cudaStream_t s = (cudaStream_t)cuda_stream;
   ET_COUNT_LAUNCH();
-  Launch scan(dim3(segments, rows), THREADS, LIST * sizeof(Entry), s);
+  Launch scan(dim3(segments, rows), THREADS, LIST * sizeof(unsigned long long), s);
   const bool aligned = aligned16(logits_dev) && (rows == 1 || row_stride % (logits_fp32 ? 4 : 8) == 0);
   auto* const kernel = logits_fp32 ? aligned ? beam_scan_kernel<true, true> : beam_scan_kernel<true, false>
                                    : aligned ? beam_scan_kernel<false, true> : beam_scan_kernel<false, false>;
   cudaError_t e = cudaLaunchKernelEx(&scan.cfg, kernel, a);
   if (e != cudaSuccess) return launched(e);
   ET_COUNT_LAUNCH();
-  Launch join(n_req, 32 * beams, (size_t)beams * k * sizeof(Entry), s);
+  const size_t bytes = join_bytes(beams, k);
+  if (bytes > 48 * 1024) {
+    e = cudaFuncSetAttribute(beam_join_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)join_bytes(BEAMS_MAX, K_MAX));
+    if (e != cudaSuccess) return launched(e);
+  }
+  Launch join(n_req, 32 * beams, bytes, s);
   return launched(cudaLaunchKernelEx(&join.cfg, beam_join_kernel, a));
 }
