@@ -20,7 +20,10 @@ namespace {
 constexpr int THREADS = 256, WARPS = THREADS / 32, EACH = 16, CHUNK = THREADS * EACH;
 static_assert(CHUNK == ET_BEAM_CHUNK, "workspace");
 constexpr int K_MAX = 64, BEAMS_MAX = 32, SEGMENTS_MAX = 64;
-constexpr int LONG = 192, LIST = CHUNK + LONG;      // the list is cut back when it has more than LONG entries; a chunk adds CHUNK at most
+// The list is cut back when it has more than so many keys; a chunk adds CHUNK at most.  With k more than the best k the bar follows the
+// segment in four or five steps, and a chunk adds few keys.
+__host__ __device__ constexpr int longest(int k) { return 2 * k + 8; }
+constexpr int LIST = CHUNK + longest(K_MAX);
 constexpr int RANKED = 1024;                        // up to so many keys each one's rank is counted
 constexpr int FEW = 8;                              // up to so many of a first chunk are bounded by groups of threads, more by warps
 constexpr float LOG2E = 1.4426950408889634f;
@@ -247,7 +250,7 @@ beam_scan_kernel(const __grid_constant__ Select a) {
     __syncthreads();
     n += *added;
     turn = turn == 2 ? 0 : turn + 1;
-    if (!begun || n > LONG) {
+    if (!begun || n > longest(a.k)) {
       n = cut_back(list, n, a.k, best);
       bar = n == a.k ? entry_of(list[a.k - 1]).value : -INFINITY;
       begun = true;
