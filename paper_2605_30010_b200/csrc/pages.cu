@@ -36,22 +36,25 @@ __device__ __forceinline__ void store_in(int* p, int cta, int v) {
 }
 __device__ __forceinline__ void report(int* status, int code) { if (status) atomicMax(status, code); }
 
-// Exclusive sum over the block's threads; `total`: all of them.  One barrier behind the last use of `sums` is the caller's.
-__device__ __forceinline__ int block_scan(int v, int* sums, int& total) {
+// Exclusive sums over the block's threads; `total`: all of them.  T: an integer, or two in one 64-bit number.
+template <typename T>
+__device__ __forceinline__ T block_scan(T v, T* sums, T& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int inc = v;
+  T inc = v;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) { const int u = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += u; }
+  for (int o = 1; o < 32; o <<= 1) { const T u = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += u; }
   __syncthreads();                                 // sums is free
   if (lane == 31) sums[warp] = inc;
   __syncthreads();
-  int w = sums[lane];                              // WARPS is 32
+  T w = sums[lane];                                // WARPS is 32
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) { const int u = __shfl_up_sync(0xffffffffu, w, o); if (lane >= o) w += u; }
+  for (int o = 1; o < 32; o <<= 1) { const T u = __shfl_up_sync(0xffffffffu, w, o); if (lane >= o) w += u; }
   total = __shfl_sync(0xffffffffu, w, 31);
-  const int before = __shfl_sync(0xffffffffu, w, warp ? warp - 1 : 0);
-  return inc - v + (warp ? before : 0);
+  const T before = __shfl_sync(0xffffffffu, w, warp ? warp - 1 : 0);
+  return inc - v + (warp ? before : (T)0);
 }
+typedef unsigned long long Two;                    // takes above, rows below; neither sum leaves 32 bits
+__device__ __forceinline__ Two two(int takes, int rows) { return (Two)(unsigned)takes << 32 | (unsigned)rows; }
 
 // The last i of [0, n) with prefix[i] <= x (prefix ascending, prefix[0] <= x)
 __device__ __forceinline__ int search(const int* prefix, int n, int x) {
@@ -110,7 +113,7 @@ struct Update {
   int* offsets;           // may be NULL
   int* slots;             // may be NULL
   int* list;              // workspace: [n_pages] free pages,
-  int* row0;              // [n_seq] first row,
+  int* ends;              // [n_seq] the row behind the last one,
   int* start;             // [n_seq] position of the first row, -1: none was got
   int n_pages, page_shift, n_seq, max_pages, rows;
   int* status;
@@ -132,108 +135,179 @@ __device__ __forceinline__ Turn turn_of(const Update& u, int s) {
   return t;
 }
 
-__device__ __forceinline__ int slot_of(const Update& u, int row, int total) {
-  if (row >= total) return -1;
-  const int s = search(u.row0, u.n_seq, row), start = __ldcg(u.start + s);
-  const long long pos = (long long)start + row - u.row0[s];
-  if (start < 0 || pos < 0 || pos >> u.page_shift >= u.max_pages) return -1;
-  const int page = __ldcg(u.table + (size_t)s * u.max_pages + (pos >> u.page_shift));
-  if ((unsigned)page >= (unsigned)u.n_pages) { report(u.status, ET_PAGED_BAD_PAGE); return -1; }
-  return (page << u.page_shift) + (int)(pos & ((1 << u.page_shift) - 1));
-}
+// The slot of position pos of sequence s, -1 if it has none; `column` and `page` are of the last one asked for
+struct Slots {
+  int column = -1, page = 0;
+  __device__ __forceinline__ int find(const Update& u, int s, long long pos) {
+    const long long c = pos >> u.page_shift;
+    if (pos < 0 || c >= u.max_pages) return -1;
+    if ((int)c != column) {
+      column = (int)c;
+      page = __ldcg(u.table + (size_t)s * u.max_pages + column);
+      if ((unsigned)page >= (unsigned)u.n_pages) report(u.status, ET_PAGED_BAD_PAGE);
+    }
+    return (unsigned)page < (unsigned)u.n_pages ? (page << u.page_shift) + (int)(pos & ((1 << u.page_shift) - 1)) : -1;
+  }
+};
 
+constexpr int AHEAD = 4;                           // entries of a thread that are on their way at once
 __global__ void __launch_bounds__(THREADS, 1)
 pages_update_kernel(const __grid_constant__ Update u, bool slots_here) {
-  __shared__ int counts[SEGMENTS], totals[2][CLUSTER], sums[WARPS], prefix[THREADS], stay_s[THREADS], got_s[THREADS];
+  __shared__ int counts[SEGMENTS], taken_s[CLUSTER], rows_s[CLUSTER], sums[WARPS], prefix[THREADS], stay_s[THREADS], got_s[THREADS], row_s[THREADS], kept_s[THREADS];
+  __shared__ Two sums2[WARPS];
   const int tid = threadIdx.x, rank = cluster_rank();
   const int per = (u.n_seq + CLUSTER - 1) / CLUSTER, s0 = min(rank * per, u.n_seq), s1 = min(s0 + per, u.n_seq);
   begin_after_previous();
   // ---- entries are given back; what is asked for is added up
-  int take = 0, rows = 0;
+  Two asked = 0;
+  Turn t{};
   for (int b = s0; b < s1; b += THREADS) {
     const int s = b + tid;
-    Turn t{};
+    t = Turn{};
     if (s < s1) t = turn_of(u, s);
-    take += t.take; rows += t.add;
+    asked += two(t.take, t.add);
     int dropped;
     const int before = block_scan(t.drop, sums, dropped);
     if (dropped == 0) continue;
     prefix[tid] = before; stay_s[tid] = t.stay;
     __syncthreads();
-    for (int i = tid; i < dropped; i += THREADS) {
-      const int k = search(prefix, min(THREADS, s1 - b), i);
-      int* const entry = u.table + (size_t)(b + k) * u.max_pages + stay_s[k] + i - prefix[k];
-      const int page = *entry;
-      *entry = -1;
-      if ((unsigned)page >= (unsigned)u.n_pages) report(u.status, ET_PAGED_BAD_PAGE);
-      else if (atomicSub(u.refs + page, 1) <= 0) {
-        atomicAdd(u.refs + page, 1);
-        report(u.status, ET_PAGED_BAD_COUNT);
+    for (int i0 = tid; i0 < dropped; i0 += AHEAD * THREADS) {
+      int page[AHEAD], old[AHEAD];
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        const int i = i0 + j * THREADS;
+        if (i >= dropped) continue;
+        const int k = search(prefix, min(THREADS, s1 - b), i);
+        int* const entry = u.table + (size_t)(b + k) * u.max_pages + stay_s[k] + i - prefix[k];
+        page[j] = *entry;
+        *entry = -1;
       }
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        old[j] = 1;
+        if (i0 + j * THREADS >= dropped) continue;
+        if ((unsigned)page[j] >= (unsigned)u.n_pages) report(u.status, ET_PAGED_BAD_PAGE);
+        else old[j] = atomicSub(u.refs + page[j], 1);
+      }
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j)
+        if (old[j] <= 0) {
+          atomicAdd(u.refs + page[j], 1);
+          report(u.status, ET_PAGED_BAD_COUNT);
+        }
     }
     __syncthreads();
   }
-  int take_cta, rows_cta;
-  block_scan(take, sums, take_cta);
-  block_scan(rows, sums, rows_cta);
+  Two cta;
+  block_scan(asked, sums2, cta);
   cluster_sync();                                  // all counts have come down (and all CTAs have begun)
-  if (tid < CLUSTER) { store_in(&totals[0][rank], tid, take_cta); store_in(&totals[1][rank], tid, rows_cta); }
+  if (tid < CLUSTER) { store_in(taken_s + rank, tid, (int)(cta >> 32)); store_in(rows_s + rank, tid, (int)cta); }
   collect_free(u.refs, u.n_pages, rank, u.list, counts);
-  cluster_sync();
+  cluster_sync();                                  // nobody writes into another's memory behind this
   const int n_free = sum_segments(counts, sums);
   int taken = 0, row = 0, rows_all = 0;            // by the sequences before
   for (int c = 0; c < CLUSTER; ++c) {
-    if (c < rank) { taken += totals[0][c]; row += totals[1][c]; }
-    rows_all += totals[1][c];
+    if (c < rank) { taken += taken_s[c]; row += rows_s[c]; }
+    rows_all += rows_s[c];
   }
   // ---- entries are taken
   for (int b = s0; b < s1; b += THREADS) {
     const int s = b + tid;
-    Turn t{};
-    if (s < s1) t = turn_of(u, s);
-    int take_all, rows_batch;
-    const int before = block_scan(t.take, sums, take_all), rows_before = block_scan(t.add, sums, rows_batch);
+    if (s1 - s0 > THREADS) { t = Turn{}; if (s < s1) t = turn_of(u, s); }          // else it is known
+    Two batch;
+    const Two ahead = block_scan(two(t.take, t.add), sums2, batch);
+    const int before = (int)(ahead >> 32), rows_before = (int)ahead, take_all = (int)(batch >> 32), rows_batch = (int)batch;
     const bool got = t.fits && (t.take == 0 || taken + before + t.take <= n_free);
     if (s < s1) {
       if (!got) report(u.status, t.fits ? (int)ET_PAGED_NO_PAGE : (int)ET_PAGED_CAPACITY);
       u.new_len[s] = t.kept < 0 ? -1 : t.kept + (got ? t.add : 0);
       if (u.offsets) u.offsets[s] = row + rows_before;
-      if (u.slots) { u.row0[s] = row + rows_before; u.start[s] = got ? t.kept : -1; }
+      if (u.slots && !slots_here) { u.ends[s] = row + rows_before + t.add; u.start[s] = got ? t.kept : -1; }
     }
-    prefix[tid] = before; stay_s[tid] = t.stay; got_s[tid] = got;
+    prefix[tid] = before; stay_s[tid] = t.stay; got_s[tid] = got; row_s[tid] = rows_before; kept_s[tid] = t.kept;
     __syncthreads();
-    for (int i = tid; i < take_all; i += THREADS) {
-      const int k = search(prefix, min(THREADS, s1 - b), i);
-      int page = -1;
-      if (got_s[k]) {
-        page = free_page(u.list, counts, u.n_pages, taken + i);
-        u.refs[page] = 1;
+    for (int i0 = tid; i0 < take_all; i0 += AHEAD * THREADS) {
+      int page[AHEAD];
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        const int i = i0 + j * THREADS;
+        page[j] = -1;
+        if (i < take_all && taken + i < n_free) page[j] = free_page(u.list, counts, u.n_pages, taken + i);
       }
-      u.table[(size_t)(b + k) * u.max_pages + stay_s[k] + i - prefix[k]] = page;
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        const int i = i0 + j * THREADS;
+        if (i >= take_all) continue;
+        const int k = search(prefix, min(THREADS, s1 - b), i);
+        if (!got_s[k]) page[j] = -1;
+        u.table[(size_t)(b + k) * u.max_pages + stay_s[k] + i - prefix[k]] = page[j];
+        if (page[j] >= 0) u.refs[page[j]] = 1;
+      }
+    }
+    if (slots_here && u.slots) {
+      __syncthreads();                             // the entries are there
+      for (int i = tid; i < min(rows_batch, u.rows - row); i += THREADS) {
+        const int k = search(row_s, min(THREADS, s1 - b), i);
+        u.slots[row + i] = got_s[k] ? Slots().find(u, b + k, (long long)kept_s[k] + i - row_s[k]) : -1;
+      }
     }
     taken += take_all; row += rows_batch;
     __syncthreads();
   }
-  if (rank == 0 && tid == 0) {
-    if (u.offsets) u.offsets[u.n_seq] = rows_all;
-    if (u.slots && rows_all > u.rows) report(u.status, ET_PAGED_CAPACITY);
-  }
-  cluster_sync();                                  // also: no CTA ends while another may write into its shared memory
-  if (slots_here) {
-    for (int r = rank * THREADS + tid; r < u.rows; r += CLUSTER * THREADS) u.slots[r] = slot_of(u, r, rows_all);
-  } else if (rank == 0 && tid == 0) {
-    u.list[0] = rows_all;                          // for the next kernel; the free pages have been dealt
+  if (rank == 0) {
+    if (tid == 0) {
+      if (u.offsets) u.offsets[u.n_seq] = rows_all;
+      if (u.slots && rows_all > u.rows) report(u.status, ET_PAGED_CAPACITY);
+    }
+    if (slots_here && u.slots) for (int r = rows_all + tid; r < u.rows; r += THREADS) u.slots[r] = -1;
   }
 }
 
-// Slots of many rows: four of them a thread.
-constexpr int SLOT_THREADS = 256, SLOT_ROWS = 4, SLOTS_HERE = 2 * CLUSTER * THREADS;
+// Slots of many rows: a block takes neighbouring rows, a thread four next to one another, whose sequence it looks for once.
+constexpr int SLOT_THREADS = 256, SLOT_ROWS = 4, SLOT_SEQS = 8192, SLOTS_HERE = 4 * THREADS;
 __global__ void __launch_bounds__(SLOT_THREADS)
-slots_kernel(const __grid_constant__ Update u) {
+slots_kernel(const __grid_constant__ Update u, int rows_each) {
+  extern __shared__ int ends_s[];                  // [n_seq], where they fit
   begin_after_previous();
-  const int all = u.list[0];
-  const int r0 = (blockIdx.x * SLOT_THREADS + threadIdx.x) * SLOT_ROWS;
-  for (int r = r0; r < min(r0 + SLOT_ROWS, u.rows); ++r) u.slots[r] = slot_of(u, r, all);
+  const int* ends = u.ends;
+  if (u.n_seq <= SLOT_SEQS) {
+    for (int s = threadIdx.x; s < u.n_seq; s += SLOT_THREADS) ends_s[s] = __ldcg(u.ends + s);
+    __syncthreads();
+    ends = ends_s;
+  }
+  const int total = ends[u.n_seq - 1];
+  const bool aligned = (reinterpret_cast<uintptr_t>(u.slots) & 15) == 0;
+  const int first = blockIdx.x * rows_each, last = min(first + rows_each, u.rows);
+  for (int r0 = first + threadIdx.x * SLOT_ROWS; r0 < last; r0 += SLOT_THREADS * SLOT_ROWS) {
+    int slot[SLOT_ROWS], s = -1, behind = r0, start = -1, from = 0;
+    Slots slots;
+#pragma unroll
+    for (int j = 0; j < SLOT_ROWS; ++j) {
+      const int r = r0 + j;
+      slot[j] = -1;
+      if (r >= total || r >= last) continue;
+      if (r >= behind) {
+        // the first sequence whose rows end behind this one
+        int n = u.n_seq - s - 1;
+        ++s;
+        while (n > 0) {
+          const int half = n >> 1;
+          if (ends[s + half] <= r) { s += half + 1; n -= half + 1; } else n = half;
+        }
+        s = min(s, u.n_seq - 1);                   // (sums beyond 2^31 are in no order)
+        from = s > 0 ? ends[s - 1] : 0; behind = ends[s];
+        start = __ldcg(u.start + s);
+        slots = Slots();
+      }
+      if (start >= 0) slot[j] = slots.find(u, s, (long long)start + r - from);
+    }
+    if (aligned && r0 + SLOT_ROWS <= last) {
+      *reinterpret_cast<int4*>(u.slots + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < SLOT_ROWS; ++j) if (r0 + j < last) u.slots[r0 + j] = slot[j];
+    }
+  }
 }
 
 // ---- et_pages_fork ----------------------------------------------------------------------------------------------------------------
@@ -246,7 +320,7 @@ struct Fork {
   int* new_len;
   int* copies;
   int* list;              // workspace: [n_pages] free pages,
-  int* family;            // [n_new] how many rows the row's parent has, negative for the first of them
+  int4* info;             // [n_new] how many rows the row's parent has, negative for the first of them; length; last page, if half-filled
   int n_pages, page_shift, n_old, n_new, max_pages;
   int* status;
 };
@@ -265,8 +339,13 @@ fork_rows_kernel(const __grid_constant__ Fork f) {
     if (f.parent[b] == p) { children[atomicAdd(&n_children, 1)] = (unsigned short)b; atomicMin(&first, b); }
   __syncthreads();
   const int n = n_children;
-  if (blockIdx.y == 0) for (int i = tid; i < n; i += FORK_THREADS) f.family[children[i]] = children[i] == first ? -n : n;
-  const int used = min(entries_of(max(f.len[p], 0), f.page_shift), f.max_pages);
+  const int length = max(f.len[p], -1), used = min(entries_of(max(length, 0), f.page_shift), f.max_pages);
+  if (blockIdx.y == 0 && n > 0) {
+    const int column = length >> f.page_shift;
+    const bool half = length > 0 && (length & ((1 << f.page_shift) - 1)) != 0 && column < f.max_pages;
+    const int page = half ? f.table[(size_t)p * f.max_pages + column] : -1;
+    for (int i = tid; i < n; i += FORK_THREADS) f.info[children[i]] = make_int4(children[i] == first ? -n : n, length, page, 0);
+  }
   for (int c = blockIdx.y * FORK_THREADS + tid; c < used; c += gridDim.y * FORK_THREADS) {
     const int page = f.table[(size_t)p * f.max_pages + c];
     if ((unsigned)page >= (unsigned)f.n_pages) report(f.status, ET_PAGED_BAD_PAGE);
@@ -298,22 +377,20 @@ fork_last_pages_kernel(const __grid_constant__ Fork f) {
     own[j] = false; old[j] = -1; length[j] = -1;
     if (b >= b1) continue;
     const int p = f.parent[b];
+    const int4 info = __ldcg(f.info + b);            // (of a row whose parent is none whatever was there)
     if (p >= f.n_old) report(f.status, ET_PAGED_BAD_ROW);
     if ((unsigned)p >= (unsigned)f.n_old) continue;
-    length[j] = max(f.len[p], -1);
-    const int column = length[j] >> f.page_shift;
-    if (length[j] <= 0 || (length[j] & ((1 << f.page_shift) - 1)) == 0 || column >= f.max_pages) continue;
-    old[j] = f.new_table[(size_t)b * f.max_pages + column];
+    length[j] = info.y;
+    old[j] = info.z;
     if ((unsigned)old[j] >= (unsigned)f.n_pages) continue;
-    const int n = f.family[b];
-    own[j] = !(n < 0 && __ldcg(f.refs + old[j]) == -n);
+    own[j] = !(info.x < 0 && __ldcg(f.refs + old[j]) == -info.x);
     wanted += own[j];
   }
   int all;
   int i = block_scan(wanted, sums, all);
   if (tid < CLUSTER) store_in(totals + rank, tid, all);
   collect_free(f.refs, f.n_pages, rank, f.list, counts);
-  cluster_sync();                                  // counts change from here on
+  cluster_sync();                                  // counts change from here on, and nobody writes into another's memory
   const int n_free = sum_segments(counts, sums);
   for (int c = 0; c < rank; ++c) i += totals[c];
 #pragma unroll
@@ -336,7 +413,6 @@ fork_last_pages_kernel(const __grid_constant__ Fork f) {
     f.new_len[b] = length[j];
     f.copies[3 * b] = from; f.copies[3 * b + 1] = to; f.copies[3 * b + 2] = n;
   }
-  cluster_sync();                                  // no CTA ends while another may write into its shared memory
 }
 
 // ---- et_kv_copy: a page's rows of one plane and head are contiguous; a block takes some of these runs ------------------------------
@@ -400,8 +476,9 @@ et_status et_pages_update(int* refs_dev, int n_pages, int page_size, int* block_
   const cudaError_t e = cudaLaunchKernelEx(&l.cfg, pages_update_kernel, u, here);
   if (here || e != cudaSuccess) return launched(e);
   ET_COUNT_LAUNCH();
-  Launch slots(cdiv(rows, SLOT_THREADS * SLOT_ROWS), SLOT_THREADS, 0, (cudaStream_t)cuda_stream);
-  return launched(cudaLaunchKernelEx(&slots.cfg, slots_kernel, u));
+  const int tile = SLOT_THREADS * SLOT_ROWS, each = cdiv(cdiv(rows, 148 * 8), tile) * tile;
+  Launch slots(cdiv(rows, each), SLOT_THREADS, n_seq <= SLOT_SEQS ? sizeof(int) * (size_t)n_seq : 0, (cudaStream_t)cuda_stream);
+  return launched(cudaLaunchKernelEx(&slots.cfg, slots_kernel, u, each));
 }
 
 et_status et_pages_fork(int* refs_dev, int n_pages, int page_size, const int* block_table_dev, int n_old, int max_pages,
@@ -416,7 +493,7 @@ et_status et_pages_fork(int* refs_dev, int n_pages, int page_size, const int* bl
       (long long)(n_old > n_new ? n_old : n_new) * max_pages >= 1ll << 31) return ET_ERR_CAPACITY;
   if (workspace_bytes < ET_FORK_WORKSPACE(n_pages, n_new)) return ET_ERR_CAPACITY;
   int* const ws = (int*)workspace_dev;
-  const Fork f{refs_dev, block_table_dev, len_dev, parent_dev, new_table_dev, new_len_dev, copies_dev, ws, ws + n_pages, n_pages, shift,
+  const Fork f{refs_dev, block_table_dev, len_dev, parent_dev, new_table_dev, new_len_dev, copies_dev, ws + 4 * n_new, (int4*)ws, n_pages, shift,
                n_old, n_new, max_pages, status_dev};
   const int slices = max_pages / FORK_THREADS + 1, most = 148 * 4 / n_old + 1;
   ET_COUNT_LAUNCH();
