@@ -151,8 +151,45 @@ struct Slots {
 };
 
 constexpr int AHEAD = 4;                           // entries of a thread that are on their way at once
+__device__ __forceinline__ void give_back(const Update& u, int* const (&entry)[AHEAD]) {
+  int page[AHEAD], old[AHEAD];
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j) if (entry[j]) { page[j] = *entry[j]; *entry[j] = -1; }
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j) {
+    old[j] = 1;
+    if (!entry[j]) continue;
+    if ((unsigned)page[j] >= (unsigned)u.n_pages) report(u.status, ET_PAGED_BAD_PAGE);
+    else old[j] = atomicSub(u.refs + page[j], 1);
+  }
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j)
+    if (old[j] <= 0) {
+      atomicAdd(u.refs + page[j], 1);
+      report(u.status, ET_PAGED_BAD_COUNT);
+    }
+}
+
+// Entries of large tables are given back by all SMs: a block takes a sequence's, or a slice of them.  (700 prompts of up to 240 pages:
+// 46 us with the entries given back by the eight SMs below, whose scattered atomics bound them, 36 with this kernel before them.)
+constexpr int GIVE_THREADS = 128;
+constexpr long long GIVE_ENTRIES = 1 << 14;        // tables of more
+__global__ void __launch_bounds__(GIVE_THREADS)
+pages_give_back_kernel(const __grid_constant__ Update u) {
+  begin_after_previous();
+  const int s = blockIdx.x;
+  const Turn t = turn_of(u, s);
+  int* const first = u.table + (size_t)s * u.max_pages + t.stay;
+  for (int i0 = blockIdx.y * AHEAD * GIVE_THREADS + threadIdx.x; i0 < t.drop; i0 += gridDim.y * AHEAD * GIVE_THREADS) {
+    int* entry[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) entry[j] = i0 + j * GIVE_THREADS < t.drop ? first + i0 + j * GIVE_THREADS : nullptr;
+    give_back(u, entry);
+  }
+}
+
 __global__ void __launch_bounds__(THREADS, 1)
-pages_update_kernel(const __grid_constant__ Update u, bool slots_here) {
+pages_update_kernel(const __grid_constant__ Update u, bool slots_here, bool given_back) {
   __shared__ int counts[SEGMENTS], taken_s[CLUSTER], rows_s[CLUSTER], sums[WARPS], prefix[THREADS], stay_s[THREADS], got_s[THREADS], row_s[THREADS], kept_s[THREADS];
   __shared__ Two sums2[WARPS];
   const int tid = threadIdx.x, rank = cluster_rank();
@@ -167,34 +204,20 @@ pages_update_kernel(const __grid_constant__ Update u, bool slots_here) {
     if (s < s1) t = turn_of(u, s);
     asked += two(t.take, t.add);
     int dropped;
-    const int before = block_scan(t.drop, sums, dropped);
+    const int before = block_scan(given_back ? 0 : t.drop, sums, dropped);
     if (dropped == 0) continue;
     prefix[tid] = before; stay_s[tid] = t.stay;
     __syncthreads();
     for (int i0 = tid; i0 < dropped; i0 += AHEAD * THREADS) {
-      int page[AHEAD], old[AHEAD];
+      int* entry[AHEAD];
 #pragma unroll
       for (int j = 0; j < AHEAD; ++j) {
         const int i = i0 + j * THREADS;
-        if (i >= dropped) continue;
+        if (i >= dropped) { entry[j] = nullptr; continue; }
         const int k = search(prefix, min(THREADS, s1 - b), i);
-        int* const entry = u.table + (size_t)(b + k) * u.max_pages + stay_s[k] + i - prefix[k];
-        page[j] = *entry;
-        *entry = -1;
+        entry[j] = u.table + (size_t)(b + k) * u.max_pages + stay_s[k] + i - prefix[k];
       }
-#pragma unroll
-      for (int j = 0; j < AHEAD; ++j) {
-        old[j] = 1;
-        if (i0 + j * THREADS >= dropped) continue;
-        if ((unsigned)page[j] >= (unsigned)u.n_pages) report(u.status, ET_PAGED_BAD_PAGE);
-        else old[j] = atomicSub(u.refs + page[j], 1);
-      }
-#pragma unroll
-      for (int j = 0; j < AHEAD; ++j)
-        if (old[j] <= 0) {
-          atomicAdd(u.refs + page[j], 1);
-          report(u.status, ET_PAGED_BAD_COUNT);
-        }
+      give_back(u, entry);
     }
     __syncthreads();
   }
@@ -263,8 +286,8 @@ pages_update_kernel(const __grid_constant__ Update u, bool slots_here) {
   }
 }
 
-// Slots of many rows: a block takes neighbouring rows, a thread four next to one another, whose sequence it looks for once.
-constexpr int SLOT_THREADS = 256, SLOT_ROWS = 4, SLOT_SEQS = 8192, SLOTS_HERE = 4 * THREADS;
+// Slots of many rows: a block takes neighbouring rows, a thread eight next to one another, whose sequence it looks for once.
+constexpr int SLOT_THREADS = 256, SLOT_ROWS = 8, SLOT_SEQS = 8192, SLOTS_HERE = 4 * THREADS;
 __global__ void __launch_bounds__(SLOT_THREADS)
 slots_kernel(const __grid_constant__ Update u, int rows_each) {
   extern __shared__ int ends_s[];                  // [n_seq], where they fit
@@ -281,28 +304,44 @@ slots_kernel(const __grid_constant__ Update u, int rows_each) {
   for (int r0 = first + threadIdx.x * SLOT_ROWS; r0 < last; r0 += SLOT_THREADS * SLOT_ROWS) {
     int slot[SLOT_ROWS], s = -1, behind = r0, start = -1, from = 0;
     Slots slots;
-#pragma unroll
-    for (int j = 0; j < SLOT_ROWS; ++j) {
-      const int r = r0 + j;
-      slot[j] = -1;
-      if (r >= total || r >= last) continue;
-      if (r >= behind) {
-        // the first sequence whose rows end behind this one
-        int n = u.n_seq - s - 1;
-        ++s;
-        while (n > 0) {
-          const int half = n >> 1;
-          if (ends[s + half] <= r) { s += half + 1; n -= half + 1; } else n = half;
-        }
-        s = min(s, u.n_seq - 1);                   // (sums beyond 2^31 are in no order)
-        from = s > 0 ? ends[s - 1] : 0; behind = ends[s];
-        start = __ldcg(u.start + s);
-        slots = Slots();
+    auto look = [&](int r) {
+      // the first sequence whose rows end behind this one
+      int n = u.n_seq - s - 1;
+      ++s;
+      while (n > 0) {
+        const int half = n >> 1;
+        if (ends[s + half] <= r) { s += half + 1; n -= half + 1; } else n = half;
       }
-      if (start >= 0) slot[j] = slots.find(u, s, (long long)start + r - from);
+      s = min(s, u.n_seq - 1);                     // (sums beyond 2^31 are in no order)
+      from = s > 0 ? ends[s - 1] : 0; behind = ends[s];
+      start = __ldcg(u.start + s);
+      slots = Slots();
+    };
+    if (r0 < total) look(r0);
+    if (start >= 0 && r0 + SLOT_ROWS <= min(min(behind, total), last)) {
+      // one sequence's, and so of one page or of two
+      const long long pos = (long long)start + r0 - from;
+      Slots other;
+      const int a = slots.find(u, s, pos), z = other.find(u, s, pos + SLOT_ROWS - 1);
+      const int left = (1 << u.page_shift) - (int)(pos & ((1 << u.page_shift) - 1));       // of the first page
+#pragma unroll
+      for (int j = 0; j < SLOT_ROWS; ++j) slot[j] = j < left ? (a < 0 ? -1 : a + j) : z < 0 ? -1 : z + 1 + j - SLOT_ROWS;
+    } else {
+#pragma unroll 1
+      for (int j = 0; j < SLOT_ROWS; ++j) {
+        const int r = r0 + j;
+        int x = -1;
+        if (r < total && r < last) {
+          if (r >= behind) look(r);
+          if (start >= 0) x = slots.find(u, s, (long long)start + r - from);
+        }
+#pragma unroll
+        for (int i = 0; i < SLOT_ROWS; ++i) if (i == j) slot[i] = x;
+      }
     }
     if (aligned && r0 + SLOT_ROWS <= last) {
-      *reinterpret_cast<int4*>(u.slots + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+#pragma unroll
+      for (int j = 0; j < SLOT_ROWS; j += 4) *reinterpret_cast<int4*>(u.slots + r0 + j) = make_int4(slot[j], slot[j + 1], slot[j + 2], slot[j + 3]);
     } else {
 #pragma unroll
       for (int j = 0; j < SLOT_ROWS; ++j) if (r0 + j < last) u.slots[r0 + j] = slot[j];
@@ -470,10 +509,17 @@ et_status et_pages_update(int* refs_dev, int n_pages, int page_size, int* block_
   int* const ws = (int*)workspace_dev;
   const Update u{refs_dev, block_table_dev, len_dev, keep_dev, add_dev, new_len_dev, row_offsets_dev, rows > 0 ? slots_dev : nullptr, ws,
                  ws + n_pages, ws + n_pages + n_seq, n_pages, shift, n_seq, max_pages, rows, status_dev};
+  const bool here = rows <= SLOTS_HERE, many = (long long)n_seq * max_pages > GIVE_ENTRIES;
+  if (many) {
+    const int slices = cdiv(max_pages, AHEAD * GIVE_THREADS), most = 148 * 8 / n_seq + 1;
+    ET_COUNT_LAUNCH();
+    Launch give(dim3(n_seq, slices < most ? slices : most), GIVE_THREADS, 0, (cudaStream_t)cuda_stream);
+    const cudaError_t e = cudaLaunchKernelEx(&give.cfg, pages_give_back_kernel, u);
+    if (e != cudaSuccess) return launched(e);
+  }
   ET_COUNT_LAUNCH();
-  const bool here = rows <= SLOTS_HERE;
   Launch l(CLUSTER, THREADS, 0, (cudaStream_t)cuda_stream, CLUSTER);
-  const cudaError_t e = cudaLaunchKernelEx(&l.cfg, pages_update_kernel, u, here);
+  const cudaError_t e = cudaLaunchKernelEx(&l.cfg, pages_update_kernel, u, here, many);
   if (here || e != cudaSuccess) return launched(e);
   ET_COUNT_LAUNCH();
   const int tile = SLOT_THREADS * SLOT_ROWS, each = cdiv(cdiv(rows, 148 * 8), tile) * tile;
