@@ -327,6 +327,7 @@ __device__ __forceinline__ int merge_lists(const Select& a, int row, Put put) {
 // A block joins a request, a warp each beam: the best k of its segments' lists, in order, then where these stand among all beams'.
 constexpr int NEAR = 64;                            // keys of a beam that may be among its best k: up to so many are ranked at once
 __host__ __device__ constexpr size_t join_bytes(int beams, int k) { return (size_t)beams * (NEAR * 8 + 12 * (size_t)k); }
+static_assert(join_bytes(BEAMS_MAX, K_MAX) <= 48 * 1024 - 256, "shared memory");
 __global__ void __launch_bounds__(32 * BEAMS_MAX, 1)
 beam_join_kernel(const __grid_constant__ Select a) {
   extern __shared__ unsigned long long join_smem[];                         // [beams][NEAR] keys, [beams][k] scores, [beams][k] tokens
@@ -493,11 +494,6 @@ extern "C" et_status et_beam_select(const void* logits_dev, int logits_fp32, lon
   cudaError_t e = cudaLaunchKernelEx(&scan.cfg, kernel, a);
   if (e != cudaSuccess) return launched(e);
   ET_COUNT_LAUNCH();
-  const size_t bytes = join_bytes(beams, k);
-  if (bytes > 48 * 1024) {
-    e = cudaFuncSetAttribute(beam_join_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)join_bytes(BEAMS_MAX, K_MAX));
-    if (e != cudaSuccess) return launched(e);
-  }
-  Launch join(n_req, 32 * beams, bytes, s);
+  Launch join(n_req, 32 * beams, join_bytes(beams, k), s);
   return launched(cudaLaunchKernelEx(&join.cfg, beam_join_kernel, a));
 }

@@ -269,9 +269,10 @@ pages_update_kernel(const __grid_constant__ Update u, bool slots_here, bool give
     }
     if (slots_here && u.slots) {
       __syncthreads();                             // the entries are there
-      for (int i = tid; i < min(rows_batch, u.rows - row); i += THREADS) {
-        const int k = search(row_s, min(THREADS, s1 - b), i);
-        u.slots[row + i] = got_s[k] ? Slots().find(u, b + k, (long long)kept_s[k] + i - row_s[k]) : -1;
+      // (sums beyond 2^31 may say any row: none outside is written)
+      for (int i = tid; i < min(rows_batch, u.rows); i += THREADS) {
+        const int k = search(row_s, min(THREADS, s1 - b), i), at = row + i;
+        if ((unsigned)at < (unsigned)u.rows) u.slots[at] = got_s[k] ? Slots().find(u, b + k, (long long)kept_s[k] + i - row_s[k]) : -1;
       }
     }
     taken += take_all; row += rows_batch;
@@ -282,7 +283,7 @@ pages_update_kernel(const __grid_constant__ Update u, bool slots_here, bool give
       if (u.offsets) u.offsets[u.n_seq] = rows_all;
       if (u.slots && rows_all > u.rows) report(u.status, ET_PAGED_CAPACITY);
     }
-    if (slots_here && u.slots) for (int r = rows_all + tid; r < u.rows; r += THREADS) u.slots[r] = -1;
+    if (slots_here && u.slots) for (int r = max(rows_all, 0) + tid; r < u.rows; r += THREADS) u.slots[r] = -1;
   }
 }
 

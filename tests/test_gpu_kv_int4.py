@@ -445,3 +445,118 @@ def test_attention_is_reproducible_and_independent_of_its_workspace(B):
         out, lse, _ = run_attention(B, q, heads, c, lens, workspace=ws)
         first = first or (out, lse)
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+
+
+def test_rows_that_cannot_be_placed_are_skipped(B):
+    """Slots not in use, positions behind the table, pages that are not in the cache, offsets that do not fit: skipped and reported, the
+    others land, nothing else is written."""
+    import torch
+    rng = np.random.default_rng(9)
+    kvh, page, d, heads = 2, 16, 64, 2
+    c = Cache4(rng, 4, 2, kvh, page, d)
+    good = c.table.clone()
+    for bad, code in ((c.n_pages, B.ET_PAGED_BAD_PAGE), (-1, B.ET_PAGED_BAD_PAGE), (None, B.ET_PAGED_CAPACITY), ("off", 0)):
+        table, start = good.clone(), [3, 17, 30, 9]
+        if bad is None:
+            start[1] = 32
+        elif bad == "off":
+            start[1] = -1
+        else:
+            table[1, 1] = bad
+        data0, scale0 = c.data.clone(), c.scale.view(torch.int16).clone()
+        qkv, status, new_len = bf16(rng.standard_normal((4, (heads + 2 * kvh) * d))), i32([0]), i32([0] * 4)
+        q = torch.full((4, heads * d), 7.0, dtype=torch.bfloat16, device="cuda")
+        B.et_kv_append(c.data, c.scale, qkv, heads, table, i32(start), theta=1e4, q_out=q, new_len=new_len, status=status)
+        assert status.item() == code and new_len.tolist() == [4, {None: 32, "off": -1}.get(bad, 18), 31, 10]
+        assert (q[1] == 7.0).all() and not (q[[0, 2, 3]] == 7.0).all(1).any()
+        where = {(good[s, start[s] // page].item(), start[s] % page) for s in (0, 2, 3)}
+        for a, b in ((data0, c.data), (scale0, c.scale.view(torch.int16))):
+            assert {tuple(i) for i in (a != b).any(-1).any(2).any(1).nonzero().tolist()} == where
+        out = torch.full((4, 2 * kvh * d), 5.0, dtype=torch.bfloat16, device="cuda")
+        status.zero_()
+        B.et_kv_read(c.data, c.scale, table, i32(start), 4, None, out, status)
+        assert status.item() == code and (out[1] == 5.0).all()
+        for s in (0, 2, 3):
+            assert torch.equal(out[s].cpu(), torch.from_numpy(c.rows(s, start[s], 1).reshape(-1)).to(torch.bfloat16))
+    c = Cache4(rng, 2, 2, kvh, page, d)
+    x, low = bf16(rng.standard_normal((6, 2 * kvh * d))), -2 ** 31
+    for offsets, start, placed, lengths, code in (
+            ([low, low + 1, 6], [0, 3], [], [0, 9], B.ET_PAGED_CAPACITY), ([low, 6, 6], [20, 0], [], [26, 0], B.ET_PAGED_CAPACITY),
+            ([0, 6, 2], [4, 26], [(0, 4 + i) for i in range(6)], [10, 26], 0), ([9, 12, 15], [1, 2], [], [1, 2], 0)):
+        before, new, status = c.data.clone(), i32([-9, -9]), i32([0])
+        B.et_kv_append(c.data, c.scale, x, 0, c.table, i32(start), i32(offsets), new_len=new, status=status)
+        changed = {tuple(i) for i in (before != c.data).any(-1).any(2).any(1).nonzero().tolist()}
+        assert changed == {(c.table[s, p // page].item(), p % page) for s, p in placed} and new.tolist() == lengths and status.item() == code
+        c.data.copy_(before)
+
+
+@pytest.mark.parametrize("rows,heads,kvh", [(1, 40, 3), (2, 3, 16), (5, 0, 1), (90, 28, 4), (1500, 7, 1), (4000, 1, 5)])
+def test_a_row_by_one_warp_or_by_several(B, rows, heads, kvh):
+    """Few rows are split over warps, many dealt several to a warp; the last row of a batch stands alone in its block."""
+    import torch
+    rng = np.random.default_rng(rows)
+    d, page = 64, 16
+    pages = (rows + 7 + page - 1) // page
+    c = Cache4(rng, 1, pages, kvh, page, d)
+    qkv = bf16(rng.standard_normal((rows, (heads + 2 * kvh) * d)))
+    q = B.et_kv_append(c.data, c.scale, qkv, heads, c.table, i32([7]), i32([0, rows]), theta=1e4)
+    x = f64(qkv).reshape(rows, heads + 2 * kvh, d)
+    pos = np.arange(7, 7 + rows)
+    n, s = quantise(np.stack([rotate(x[:, heads:heads + kvh], pos, 1e4), x[:, heads + kvh:]], 1))
+    places = c.table.cpu().numpy()[0][pos // page], pos % page
+    assert np.array_equal(c.codes()[places[0], :, :, places[1]], n) and np.array_equal(f64(c.scale)[places[0], :, :, places[1]], s)
+    if heads:
+        want = rotate(x[:, :heads], pos, 1e4)
+        slack = 2.0 ** -20 * (np.abs(x[:, :heads]) + np.abs(np.roll(x[:, :heads], d // 2, -1)))
+        assert (np.abs(f64(q).reshape(want.shape) - want) <= BF16 * np.abs(want) + slack).all()
+
+
+def test_decode_step_follows_the_prefill(B):
+    """A prompt is prefilled, its cache moved into pages of 4 bits, and the next token decoded layer by layer: against the same step
+    over pages of bf16 that hold what the 4-bit pages read back as.  The two differ by the roundings of that reading (2^-8 of a
+    value) and of the activations between; the bound is the framework's for whole bf16 models, 2e-2 of the largest logit."""
+    import torch
+    from synthetic.llm import LLM_SMALL, llm_views, make_llm_weights, make_prompt
+    sh = LLM_SMALL
+    blob = make_llm_weights(sh, 4)
+    ids, _ = make_prompt(sh, 151, 0, 4)
+    llm = B.LanguageModel(sh, blob, max_tokens=256, keep_kv_cache=True)
+    pre = llm.prefill(ids[:100], None, ids[100:150], want_kv=True)
+    total, page, kvh, d, m = pre.n_tokens, 32, sh.kv_heads, sh.head_dim, sh.mlp_dim
+    W = {k: torch.from_numpy(np.ascontiguousarray(v)).cuda() for k, v in llm_views(sh, blob).items()}
+    t16 = lambda x: x.to(torch.bfloat16).T.contiguous()                                           # noqa: E731
+    table = i32(np.random.default_rng(1).permutation(16)[:8].reshape(1, 8))
+    logits = []
+    for four in (True, False):
+        x = W["embed"].to(torch.bfloat16)[int(ids[150])].float().view(1, -1).clone()
+        lens, new, status = i32([total]), i32([0]), i32([0])
+        for i in range(sh.num_layers):
+            w = {k[len(f"l{i}."):]: v for k, v in W.items() if k.startswith(f"l{i}.")}
+            data = torch.zeros((16, 2, kvh, page, d // 2), dtype=torch.uint8, device="cuda")
+            scale = torch.zeros((16, 2, kvh, page, d // 32), dtype=torch.bfloat16, device="cuda")
+            B.et_kv_append(data, scale, pre.kv_cache[i], 0, table, i32([0]), i32([0, total]), status=status)
+            if not four:
+                rows = B.et_kv_read(data, scale, table, i32([0]), total, i32([0, total]), status=status)
+                data, scale = torch.zeros((16, 2, kvh, page, d), dtype=torch.bfloat16, device="cuda"), None
+                B.et_kv_append(data, None, rows, 0, table, i32([0]), i32([0, total]), status=status)
+            qkv = B.et_linear_rows(B.et_rmsnorm(x, w["rms1_g"], sh.rms_eps), t16(w["wqkv"]), w["bqkv"])
+            if not four:                                          # the new token's row is quantised as well
+                one, s1 = torch.zeros((1, 2, kvh, 16, d // 2), dtype=torch.uint8, device="cuda"), torch.zeros((1, 2, kvh, 16, d // 32), dtype=torch.bfloat16, device="cuda")
+                far = i32([[0] * (total // 16 + 1)])
+                q = B.et_kv_append(one, s1, qkv, sh.heads, far, lens, theta=sh.rope_theta, new_len=new, status=status)
+                B.et_kv_append(data, None, B.et_kv_read(one, s1, far, lens, 1), 0, table, lens, status=status)
+            else:
+                q = B.et_kv_append(data, scale, qkv, sh.heads, table, lens, theta=sh.rope_theta, new_len=new, status=status)
+            att = B.et_attention_paged(q, sh.heads, data, scale, table, new, status=status)
+            B.et_linear_rows(att, t16(w["wo"]), None, 2, c=x)
+            h = B.et_rmsnorm(x, w["rms2_g"], sh.rms_eps)
+            gu = torch.zeros((1, 2 * m), dtype=torch.float32, device="cuda")
+            B.et_linear_rows(h, t16(w["wgu"]), None, 2, c=gu)
+            act = (gu[:, :m] / (1 + torch.exp(-gu[:, :m])) * gu[:, m:]).to(torch.bfloat16)
+            B.et_linear_rows(act.contiguous(), t16(w["wd"]), None, 2, c=x)
+        out = torch.zeros((1, sh.vocab), dtype=torch.float32, device="cuda")
+        B.et_linear_rows(B.et_rmsnorm(x, W["final_g"], sh.rms_eps), t16(W["lm_head"]), None, 2, c=out)
+        assert status.item() == 0 and new.item() == total + 1
+        logits.append(out[0])
+    off = (logits[0] - logits[1]).abs().max().item() / logits[1].abs().max().item()
+    assert off <= 2e-2, off

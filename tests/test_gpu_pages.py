@@ -643,3 +643,30 @@ def test_calls_on_a_stream_of_their_own(B):
     ref = fork_reference(ref[0], 16, ref[1], ref[2], np.arange(30), np.zeros_like(table))      # (pages that others hold are copied)
     assert np.array_equal(r.cpu().numpy(), ref[0]) and np.array_equal(new_table.cpu().numpy(), ref[1])
     assert np.array_equal(copies.cpu().numpy(), ref[3])
+
+
+def test_update_of_sums_beyond_32_bits_writes_nothing_outside(B):
+    """More positions asked for than numbers can say: offsets are any, but slots are written within their buffer only."""
+    import torch
+    rng = np.random.default_rng(12)
+    lens, table, refs = random_state(rng, 40, 100, 16, 50)
+    for rows in (100, 30_000):
+        wide = i32([-77] * (rows + 2_000))
+        add = i32([2 ** 31 - 1 - 7 * i if i % 3 else 5 for i in range(40)])
+        status, state = i32([0]), [i32(refs), i32(table), i32(lens)]
+        B.et_pages_update(*state[:1], 16, *state[1:], add=add, row_offsets=i32([0] * 41), slots=wide[1000:1000 + rows], status=status)
+        assert status.item() == B.ET_PAGED_CAPACITY or status.item() == B.ET_PAGED_NO_PAGE
+        assert (wide[:1000] == -77).all() and (wide[1000 + rows:] == -77).all()
+
+
+@pytest.mark.parametrize("n", [1, 700])
+def test_update_of_large_tables(B, n):
+    """Tables whose entries are given back by a kernel of their own; as many slots as make a thread's rows cross pages and sequences."""
+    rng = np.random.default_rng(n)
+    longest, page = (300_000, 16) if n == 1 else (900, 16)
+    lens, table, refs = random_state(rng, n, longest, page, 25_000)
+    assert table.size > 1 << 14
+    keep = np.maximum(lens - rng.integers(0, longest, n), 0)
+    add = np.minimum(rng.integers(0, longest, n), table.shape[1] * page - np.minimum(np.maximum(lens, 0), keep))
+    check_update(B, page, lens, table, refs, keep, add)
+    check_update(B, page, lens, table, refs, np.full(n, -1), None, in_place=True)
