@@ -1,7 +1,8 @@
 // Attention of one new token of each sequence over its paged key / value cache.
 //
 // Every cached byte is read once and used for `group` query heads (7 in a Qwen2-7B layer), about 7 multiply-adds a byte:
-// the cache's bytes over the memory bandwidth bound it, and the work is arranged to keep copies in flight.
+// the cache's bytes over the memory bandwidth bound it, and the work is arranged to keep copies in flight.  (With 4 bits a value
+// the bytes are so few that the computing warps' instructions bound it: see below.)
 //
 //   * A tile is 64 positions of one key / value head.  All tiles of the call, in the order (sequence, key / value head,
 //     tile), are cut into one equal run per CTA (one CTA per SM), so a single long sequence and a ragged batch load every
@@ -23,12 +24,19 @@
 // 2^8 below those of the values that the scores favour takes two bf16 a weight instead.  So a probability has its 11 bits down
 // to 2^-21 of the largest one, whatever the scales, and is off by at most 2^-32 of that one below.
 //
+// 4 bits (c - 8) s, a scale s for 32 dimensions.  A score is  sum over blocks of s (sum of c q) - sum over blocks of s 8 (sum of q):
+// the first sum's codes go to the tensor core as they are, as subnormal halves, one mask each; the second is one more matrix
+// product, of the positions' scales by the queries' sums, exact to 24 bits as three bf16.  An output is  sum of (w s) (c - 8):  codes
+// less 8 as bf16, one mask and one multiply-add for two of them, and weights w s as two bf16, 16 bits, whatever the scales are.
+// That is about 800 instructions of a warp for 32 positions (8 heads of 128); two warps a scheduler issue one in two cycles.
+//
 // Device time in a chain of calls, B200, cache not in L2 (of the measured copy bandwidth; a pure read can pass 1); a second figure is
 // for calls repeated for a second, at the clock that the power limit leaves.  28 heads on 4 of 128, bf16, one sequence of 100 003 38.5 us
 // (0.82), of 7 675 10.5 (0.23: start and joining kernel); e4m3, 64 ragged sequences up to 16 001 55 / 59 us (0.85 / 0.79); 16 heads
 // of 128 on 16, one of 180 000, bf16 219 / 221 us (1.04), e4m3 116 / 121 us (0.99 / 0.95); 24 ragged up to 2 049, 16 heads of 64, bf16
 // 22 / 21 us (0.51 / 0.54), e4m3 the same (0.27): short items; 16 heads to a key / value head, 64 ragged, bf16 105 / 110 us (0.88 /
-// 0.85), e4m3 71 / 74 us (0.66 / 0.64: bound by conversions and exponentials).
+// 0.85), e4m3 71 / 74 us (0.66 / 0.64: bound by conversions and exponentials).  4 bits, 28 heads on 4 of 128: one sequence of 100 003
+// 24.5 us (0.36), 64 ragged up to 16 001 64 us (0.47; its copies without arithmetic take 37, its arithmetic without copies 62).
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
@@ -44,36 +52,33 @@ namespace {
 
 using namespace tc;
 
-constexpr int GROUPS = 4;                      // of computing warps; tiles are dealt to them in turn
+constexpr int TILE = 64;                       // positions
+constexpr int GROUP_WARPS = 2;                 // warps of one tile, BLOCKS blocks of 16 positions each
+constexpr int BLOCKS = TILE / 16 / GROUP_WARPS;
+constexpr int COMPUTE_WARPS = 8;
+constexpr int GROUPS = COMPUTE_WARPS / GROUP_WARPS;   // tiles are dealt to the groups in turn
 constexpr int COPY_WARPS = GROUPS;             // one for each group's tiles
-// A group takes an item of up to so many positions alone, where a CTA has several: 72 sequences of 250, 16 heads of 128, e4m3:
-// 29.8 -> 18.3 us, 56 of 320 29.9 -> 21.5 us; with 2 048 a batch of long and short ones gets slower (55.8 -> 60.2 us).
-constexpr int ALONE_POSITIONS = 512;
+constexpr int THREADS = 32 * (COMPUTE_WARPS + COPY_WARPS);
+// With 16 heads (NT = 2) or 4 bits the computing warps take registers from the copying ones: of what a block is launched with, never
+// more.  (4 bits, 8 heads: 67 -> 64 us for 64 ragged sequences.  The others fit in 168 registers.)
+constexpr int LAUNCH_REGS = 168, COMPUTE_REGS = 208, COPY_REGS = 88;
+static_assert(COMPUTE_WARPS % 4 == 0 && COPY_WARPS % 4 == 0, "whole warpgroups");
+static_assert(COMPUTE_WARPS * COMPUTE_REGS + COPY_WARPS * COPY_REGS <= (COMPUTE_WARPS + COPY_WARPS) * LAUNCH_REGS, "register budget");
+// A group takes an item of up to so many tiles alone, where a CTA has several: 72 sequences of 250, 16 heads of 128, e4m3:
+// 29.8 -> 18.3 us, 56 of 320 29.9 -> 21.5 us; with 32 a batch of long and short ones gets slower (55.8 -> 60.2 us).
+constexpr int ALONE_TILES = 8;
 // The tensor core cuts off what does not fit an accumulator, which adds up over long sums (0.0016 of positive outputs after a
-// million positions in a CTA).  So a piece has at most this many positions, a quarter for each group; what is longer becomes several
+// million positions in a CTA).  So a piece has at most this many tiles, a quarter for each group; what is longer becomes several
 // pieces, whose outputs are added in fp32.
-constexpr int PIECE_POSITIONS = 64 * 256 * GROUPS;
+constexpr int PIECE_TILES = 256 * GROUPS;
 constexpr int MAX_CTAS = 148;
 constexpr int PAD = 4;                         // floats between heads of the joining buffer: no bank conflicts
 constexpr int SMEM_LIMIT = 232448 - 512;       // 227 KB, less the static part
 constexpr int CONTROL_BYTES = 1024;            // barriers and the ring's flags
 
-// Rows of 4 bits come in tiles of twice as many positions: what a tile costs beside its rows (a copying warp's work, waits, the search
-// for a maximum) is then half as much a row.
-constexpr int tile_positions(int format, int nt) { return 64; }
-
 template <int DH, int FMT, int NT>
 struct Cfg {
-  static constexpr int GROUP_WARPS = 2, COMPUTE_WARPS = GROUPS * GROUP_WARPS;
-  static constexpr int THREADS = 32 * (COMPUTE_WARPS + COPY_WARPS);
-  // The computing warps take registers from the copying ones: of what a block is launched with, never more.
-  static constexpr bool SPLIT = NT == 2 || FMT == ET_KV_INT4;
-  static constexpr int LAUNCH_REGS = 168, COMPUTE_REGS = 208, COPY_REGS = 88;
-  static_assert(COMPUTE_WARPS % 4 == 0 && COPY_WARPS % 4 == 0, "whole warpgroups");
-  static_assert(!SPLIT || COMPUTE_WARPS * COMPUTE_REGS + COPY_WARPS * COPY_REGS <= (COMPUTE_WARPS + COPY_WARPS) * LAUNCH_REGS, "register budget");
-  // positions of a tile; each of a group's warps has BLOCKS blocks of 16 of them
-  static constexpr int TILE = tile_positions(FMT, NT), BLOCKS = TILE / 16 / GROUP_WARPS;
-  static constexpr int ALONE_TILES = ALONE_POSITIONS / TILE, PIECE_TILES = PIECE_POSITIONS / TILE;
+  static constexpr bool SPLIT = NT == 2 || FMT == ET_KV_INT4;     // of registers, see above
   static constexpr int ROW = kv_row_bytes(FMT, DH);               // bytes of a row
   static constexpr int BOX_ROW = ROW > 128 ? 128 : ROW;           // bytes of a box row: the swizzle's width
   static constexpr int BOXES = ROW / BOX_ROW;
@@ -81,13 +86,14 @@ struct Cfg {
   static constexpr int STAGE = 2 * PLANE;                         // keys, values
   // What an item costs beside its tiles, in tiles' worth of time (measured: 2.3 us beside 0.6 us a tile for bf16 rows of 128, 2.0
   // and 0.3 for e4m3 ones, 1.4 and 0.25 for bf16 rows of 64; with 16 heads 2.8 and 0.65, 3.7 and 0.4; e4m3 rows of 64 follow the
-  // same formula unmeasured); an item that a group takes alone costs a good third of it.
-  static constexpr int COST_ = (2 + 65536 / STAGE) * (NT + 1) / 2, COST_SHORT_ = NT == 1 ? 1 + 32768 / STAGE : COST_;
-  static constexpr int COST = COST_ < PAGED_ITEM_COST_MAX ? COST_ : PAGED_ITEM_COST_MAX, COST_SHORT = COST_SHORT_ < COST ? COST_SHORT_ : COST;
+  // same formula unmeasured); an item that a group takes alone costs a good third of it.  A tile of 4 bits takes as long as its
+  // arithmetic, whatever its bytes: 64 ragged sequences 65.8, 65.0, 63.8, 64.6, 67.0 us at costs of 4, 6, 8, 10 and 13 for 8 heads.
+  static constexpr int PER_TILE = FMT == ET_KV_INT4 ? 6 : 65536 / STAGE;
+  static constexpr int COST = (2 + PER_TILE) * (NT + 1) / 2, COST_SHORT = NT == 1 ? 1 + PER_TILE / 2 : COST;
   static constexpr int SCALES = 2 * TILE * kv_scale_bytes(FMT, DH);
   static constexpr int HEADS = 8 * NT;
   static constexpr int JOIN = COMPUTE_WARPS * HEADS * (DH + PAD) * 4 + COMPUTE_WARPS * HEADS * 3 * 4;   // the warps' results of a piece
-  static constexpr int JOINS = NT == 1 && GROUP_WARPS == 2 ? 2 : 1;                   // pieces whose results can wait to be joined
+  static constexpr int JOINS = NT == 1 ? 2 : 1;                   // pieces whose results can wait to be joined
   static constexpr int Q_ROW = DH * 2 + 16;                       // a head's query; 16 bytes more: no bank conflicts
   static constexpr bool ALONE = NT == 1;                          // (with 16 heads there is no room for what it takes)
   static constexpr int PAIR = ALONE ? HEADS * (DH + PAD) * 4 + 3 * HEADS * 4 : 0;   // a group's own results
@@ -230,7 +236,7 @@ __device__ __forceinline__ void bulk_load_elect(uint32_t dst, const void* src, u
                "@q cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}"
                ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-template <int N> __device__ __forceinline__ void group_sync(int group) { asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(32 * N) : "memory"); }
+__device__ __forceinline__ void group_sync(int group) { asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(32 * GROUP_WARPS) : "memory"); }
 // 16 bytes by a lane's own asynchronous copy (zeros if not live); copies_arrive: an arrival once the lane's copies so far are there
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
@@ -244,10 +250,10 @@ __device__ __forceinline__ int clamped_len(const Args& g, int s) {
   return (int)min((long long)max(g.a.len[s], 0), cap);
 }
 // An item's units: its tiles and, in front of them, units for what it costs beside them.  C: the kernel's Cfg
-template <class C> __device__ __forceinline__ int tiles_of(int len) { return (int)((unsigned)(len + (C::TILE - 1)) / C::TILE); }
-template <class C> __device__ __forceinline__ int cost_of(int tiles) { return tiles <= C::ALONE_TILES ? C::COST_SHORT : C::COST; }
+__device__ __forceinline__ int tiles_of(int len) { return (int)((unsigned)(len + (TILE - 1)) / TILE); }
+template <class C> __device__ __forceinline__ int cost_of(int tiles) { return tiles <= ALONE_TILES ? C::COST_SHORT : C::COST; }
 template <class C> __device__ __forceinline__ int units_of(const Args& g, int len) {
-  const int tiles = tiles_of<C>(len);
+  const int tiles = tiles_of(len);
   return len <= 0 ? 0 : g.whole ? 1 : tiles + cost_of<C>(tiles);
 }
 
@@ -276,7 +282,7 @@ template <class C>
 __device__ __forceinline__ Deal deal(const Piece& p, int chunk, int group, int& turn) {
   Deal d;
   const int n = p.t1 - p.t0;
-  d.alone = C::ALONE && n <= C::ALONE_TILES && p.units * GROUPS <= chunk && !p.goes_on;
+  d.alone = C::ALONE && n <= ALONE_TILES && p.units * GROUPS <= chunk && !p.goes_on;
   const int behind = (group - turn) & (GROUPS - 1);
   d.t = d.alone ? (behind == 0 ? p.t0 : p.t1) : p.t0 + behind;
   d.step = d.alone ? 1 : GROUPS;
@@ -291,11 +297,11 @@ __device__ __forceinline__ bool next_piece(const Args& g, int parts_all, Walk& w
     if (units > 0) {
       int end = w.unit + min(w.left, units - w.unit);
       p.s = w.s; p.part = w.part; p.len = w.len; p.units = units;
-      const int tiles = tiles_of<C>(w.len), cost = cost_of<C>(tiles);
+      const int tiles = tiles_of(w.len), cost = cost_of<C>(tiles);
       p.t0 = g.whole ? 0 : max(w.unit - cost, 0);
       p.t1 = g.whole ? tiles : max(end - cost, 0);
-      p.more = p.t1 - p.t0 > C::PIECE_TILES;
-      if (p.more) { p.t1 = p.t0 + C::PIECE_TILES; end = p.t1 + cost; }        // (an item that is not cut has no such length)
+      p.more = p.t1 - p.t0 > PIECE_TILES;
+      if (p.more) { p.t1 = p.t0 + PIECE_TILES; end = p.t1 + cost; }        // (an item that is not cut has no such length)
       p.goes_on = w.cut;
       p.first = w.cut ? w.cut_first : p.t0 == 0;
       p.last = end == units; p.units_end = end;
@@ -316,12 +322,11 @@ __device__ __forceinline__ bool next_piece(const Args& g, int parts_all, Walk& w
 }
 
 template <int DH, int FMT, int NT>
-__global__ void __launch_bounds__(Cfg<DH, FMT, NT>::THREADS, 1)
+__global__ void __launch_bounds__(THREADS, 1)
 attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ Args g) {
   using C = Cfg<DH, FMT, NT>;
   constexpr bool BF16 = FMT == ET_KV_BF16, E4M3 = FMT == ET_KV_E4M3, INT4 = FMT == ET_KV_INT4;
-  constexpr int GROUP_WARPS = C::GROUP_WARPS, COMPUTE_WARPS = C::COMPUTE_WARPS, THREADS = C::THREADS;
-  constexpr int TILE = C::TILE, BLOCKS = C::BLOCKS, STAGES = C::STAGES, KS = DH / 16, SCALE = kv_scale_bytes(FMT, DH);     // SCALE: bytes of a row's scales
+  constexpr int STAGES = C::STAGES, KS = DH / 16, SCALE = kv_scale_bytes(FMT, DH);     // SCALE: bytes of a row's scales
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const gen = smem_raw + (base - raw);
@@ -391,14 +396,13 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 
   bool ok = true;
   if constexpr (C::SPLIT) {
-    if (warp >= COMPUTE_WARPS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::COPY_REGS));
-    else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::COMPUTE_REGS));
+    if (warp >= COMPUTE_WARPS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(COPY_REGS));
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(COMPUTE_REGS));
   }
   if (warp >= COMPUTE_WARPS) {
     // ------------------------------------------------------------------ copies
     const int me = warp - COMPUTE_WARPS;
-    constexpr int TILE_SHIFT = TILE == 128 ? 7 : 6, BOXES = TILE / 16;         // a page has 16 positions or more
-    const int box_shift = min(g.c.page_shift, TILE_SHIFT), box_rows = 1 << box_shift, boxes_tile = TILE >> box_shift;
+    const int box_shift = min(g.c.page_shift, 6), box_rows = 1 << box_shift, boxes_tile = TILE >> box_shift;
     const uint32_t box_bytes = (uint32_t)box_rows * (2 * C::ROW + 2 * SCALE);
     const int plane_rows = kv_heads << g.c.page_shift;
     // the cache is read once (several head tiles read it soon after one another): it need not push other things out of L2
@@ -450,9 +454,9 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         while ((page0 >> 5) > batch) { ++batch; rows = rows_of(ids_next); ids_next = load_ids(batch + 1); }
         const int in_page = pos & ((1 << g.c.page_shift) - 1);
         const int boxes = min(boxes_tile, (p.len - pos + box_rows - 1) >> box_shift);      // with positions
-        int row[BOXES], missing = 0;                                  // first row of each box's keys; negative: none
+        int row[4], missing = 0;                                  // first row of each box's keys; negative: none
 #pragma unroll
-        for (int i = 0; i < BOXES; ++i) {
+        for (int i = 0; i < 4; ++i) {
           row[i] = __shfl_sync(0xffffffffu, rows, (page0 + i) & 31);
           if (i >= boxes) row[i] = -1;
           else if (row[i] < 0) missing |= 1 << i;
@@ -467,7 +471,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         const uint32_t bar = full(stage), dst = base + stage * C::STAGE, sdst = scales + stage * C::SCALES;
         arrive_expect_elect(bar, (boxes - __popc(missing)) * box_bytes);
 #pragma unroll
-        for (int i = 0; i < BOXES; ++i) {
+        for (int i = 0; i < 4; ++i) {
           if (row[i] >= 0) {
             const int r0 = i << box_shift;
 #pragma unroll
@@ -1005,10 +1009,10 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
           }
       };
       if (C::ALONE && dl.alone) {
-        // the group's warps: the first leaves its result, the others add their own, all put the sum out
+        // the group's two warps: the first leaves its result, the second adds its own, both put the sum out
         float* const pair = pair_of(my_group);
         float* const pair_m = pair + C::HEADS * (DH + PAD);           // [3][HEADS]: maximum, output's maximum, sum
-        group_sync<GROUP_WARPS>(my_group);                                         // the memory is free
+        group_sync(my_group);                                         // the memory is free
         if (warp % GROUP_WARPS == 0) {
           leave_output(pair);
 #pragma unroll
@@ -1017,10 +1021,8 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
             if (gq == 0) { pair_m[h] = m[0][i]; pair_m[C::HEADS + h] = E4M3 ? mo[0][i] : m[0][i]; pair_m[2 * C::HEADS + h] = l[0][i]; }
           }
         }
-#pragma unroll 1
-        for (int turn_of = 1; turn_of < GROUP_WARPS; ++turn_of) {
-        group_sync<GROUP_WARPS>(my_group);
-        if (warp % GROUP_WARPS == turn_of) {
+        group_sync(my_group);
+        if (warp % GROUP_WARPS == 1) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int h = 2 * tq + i;
@@ -1037,11 +1039,10 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                 *y = *y * fa + o[0][k][i + 2] * fb;
               }
             __syncwarp();
-            if (gq == 0) { pair_m[h] = pair_m[C::HEADS + h] = top; pair_m[2 * C::HEADS + h] = la * exp2_fast(ma - ref) + l[0][i] * exp2_fast(m[0][i] - ref); }
+            if (gq == 0) { pair_m[h] = top; pair_m[2 * C::HEADS + h] = la * exp2_fast(ma - ref) + l[0][i] * exp2_fast(m[0][i] - ref); }
           }
         }
-        }
-        group_sync<GROUP_WARPS>(my_group);
+        group_sync(my_group);
         for (int e = tid % (32 * GROUP_WARPS); ok && e < live * (DH / 4); e += 32 * GROUP_WARPS) {
           const int h = e / (DH / 4), d = (e % (DH / 4)) * 4;
           put(p, h, d, *reinterpret_cast<const float4*>(pair + h * (DH + PAD) + d), pair_m[h], pair_m[2 * C::HEADS + h], 0u);
@@ -1161,14 +1162,14 @@ attention_join_kernel(const __grid_constant__ Args g) {
   }
 }
 
-bool make_cache_map(CUtensorMap* out, const PagedCache& c, int tile) {
+bool make_cache_map(CUtensorMap* out, const PagedCache& c) {
   EncodeTiledFn fn = tensor_map_encoder();
   if (!fn) return false;
   const bool two = c.format == ET_KV_BF16;                             // bytes an element of the map
   const int row = kv_row_bytes(c.format, c.head_dim), box_row = row > 128 ? 128 : row;
   const cuuint64_t dims[2] = {(cuuint64_t)(row / (two ? 2 : 1)), ((cuuint64_t)c.n_pages * 2 * c.kv_heads) << c.page_shift};
   const cuuint64_t strides[1] = {(cuuint64_t)row};
-  const cuuint32_t box[2] = {(cuuint32_t)(box_row / (two ? 2 : 1)), (cuuint32_t)(1 << c.page_shift < tile ? 1 << c.page_shift : tile)};
+  const cuuint32_t box[2] = {(cuuint32_t)(box_row / (two ? 2 : 1)), (cuuint32_t)(1 << (c.page_shift < 6 ? c.page_shift : 6))};
   const cuuint32_t estr[2] = {1, 1};
   return fn(out, two ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, c.data, dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, box_row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : box_row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
@@ -1188,14 +1189,14 @@ cudaError_t launch(const CUtensorMap& map, const Args& g, int ctas, cudaStream_t
       cudaFuncAttributes fa;
       e = cudaFuncGetAttributes(&fa, attention_paged_kernel<DH, FMT, NT>);
       if (e != cudaSuccess) return e;
-      if (fa.numRegs < C::LAUNCH_REGS) return cudaErrorLaunchOutOfResources;
+      if (fa.numRegs < LAUNCH_REGS) return cudaErrorLaunchOutOfResources;
     }
     e = cudaFuncSetAttribute(attention_paged_kernel<DH, FMT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) ready[dev] = true;
   }
   ET_COUNT_LAUNCH();
-  Launch l(ctas, C::THREADS, C::SMEM, s);
+  Launch l(ctas, THREADS, C::SMEM, s);
   e = cudaLaunchKernelEx(&l.cfg, attention_paged_kernel<DH, FMT, NT>, map, g);
   if (e != cudaSuccess || g.whole) return e;
   ET_COUNT_LAUNCH();
@@ -1212,8 +1213,8 @@ cudaError_t launch_attention_paged(const PagedCache& c, const PagedAttention& a,
   const int nt = g.group <= 8 ? 1 : 2;
   g.parts = (g.group + 8 * nt - 1) / (8 * nt);
   CUtensorMap map;
-  if (!make_cache_map(&map, c, tile_positions(c.format, nt))) return cudaErrorUnknown;
-  const long long tiles = (((long long)a.max_pages << c.page_shift) + 63) / 64;      // of the longest sequence there can be (or half as many)
+  if (!make_cache_map(&map, c)) return cudaErrorUnknown;
+  const long long tiles = (((long long)a.max_pages << c.page_shift) + TILE - 1) / TILE;      // of the longest sequence there can be
   // Where no sequence can have more than four tiles, items are not cut and nothing has to be joined.  The host knows the table's width
   // only: in one for 32 768 positions the same lengths take the other way, 1 x 61 6.7 us in place of 5.5, 16 x 200 8.7 of 6.5.
   g.whole = tiles <= 4;
