@@ -1,8 +1,8 @@
 /* earlytom_decode.h -- what a decode step of the language model needs beside the prefill of earlytom_llm.h: a paged
  * key / value cache (bf16, e4m3 with one power of two per row, or 4 bits with one scale per 32 values), attention of one
- * new token over it, and dense layers for a handful of rows.  No counterpart in the paper, whose time-to-first-token ends with the prefill; the
- * architecture is the one of earlytom_llm.h (grouped-query attention, rotate-half rotary embedding, bf16 activations,
- * fp32 residual stream and statistics).
+ * new token over it, and dense layers for a handful of rows.  No counterpart in the paper, whose time-to-first-token ends
+ * with the prefill; the architecture is the one of earlytom_llm.h (grouped-query attention, rotate-half rotary embedding,
+ * bf16 activations, fp32 residual stream and statistics).
  *
  * Conventions are those of earlytom.h's single steps: caller-owned device buffers of the current device, asynchronous on
  * cuda_stream, no allocation, no synchronisation, capturable into a CUDA graph; shapes are checked on the host and refused
@@ -73,7 +73,8 @@ typedef struct {
  *
  * ET_KV_INT4: the scale s of 32 values is the smallest bf16 that is not below max|x| / 7, a code is 8 + x / s rounded to nearest, ties to
  * even (1 .. 15): a value is off by at most s / 2.  Scales and codes are those of 64-bit arithmetic, turned keys' as well.  32
- * values of which one is not finite (or, of a turned key, beyond fp32) have a NaN for their scale: all of them read as NaN.
+ * values of which one is not finite (or, of a turned key, above 2^128 (1 - 2^-21)) have a NaN for their scale: all of them read as
+ * NaN.
  *
  * new_len_dev (int [n_seq], may be NULL, not start_dev): positions in the cache after the call, start + rows but at most
  * max_pages * page_size (also where the start is behind that already), or the negative start. */

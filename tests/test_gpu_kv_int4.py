@@ -208,6 +208,27 @@ def test_conversion_edges(B, d, rotated):
     assert torch.equal(torch.nan_to_num(back.cpu(), 3.0, 4.0, 5.0), torch.nan_to_num(want, 3.0, 4.0, 5.0))
 
 
+def test_turned_keys_at_the_end_of_fp32(B):
+    """Keys whose turned values lie between 2^128 (1 - 2^-21), which fp32 still holds, and 2^128: a NaN for a scale, never an infinity."""
+    rng = np.random.default_rng(9)
+    pos = rng.integers(0, 4096, 1 << 25)
+    x, y = (np.ldexp((128 + rng.integers(0, 128, pos.size)).astype(np.float64), 120 - rng.integers(0, 2, pos.size)) for _ in range(2))
+    turned = np.abs(x * np.cos(pos) - y * np.sin(pos))
+    hit = np.flatnonzero((turned >= 2.0 ** 128 * (1 - 2.0 ** -21)) & (turned < 2.0 ** 128))
+    below = np.flatnonzero((turned < 2.0 ** 128 * (1 - 2.0 ** -20)) & (turned > 2.0 ** 128 * (1 - 2.0 ** -17)))[:len(hit)]
+    assert len(hit) >= 3
+    rows = np.concatenate([hit, below])
+    k = np.zeros((len(rows), 2, 64))
+    k[:, 0, 0], k[:, 0, 32] = x[rows], y[rows]                # the first frequency is one radian a position
+    c = Cache4(rng, len(rows), 4096 // 128, 1, 128, 64)
+    B.et_kv_append(c.data, c.scale, bf16(k.reshape(len(rows), 128)), 0, c.table, i32(pos[rows]), theta=1e4)
+    page = c.table.cpu().numpy()[np.arange(len(rows)), pos[rows] // 128]
+    got = f64(c.scale)[page, 0, 0, pos[rows] % 128]
+    _, want = quantise(rotate(k[:, :1], pos[rows], 1e4)[:, 0])
+    assert np.isnan(got[:len(hit), 0]).all() and not np.isinf(got).any()
+    assert np.array_equal(got[len(hit):], want[len(hit):], equal_nan=True)
+
+
 def check_attention(out, lse, q, lens, c, heads, alive=None):
     d, values = c.d, c.values()
     for s, n in enumerate(lens):
