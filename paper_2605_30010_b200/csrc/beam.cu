@@ -5,11 +5,19 @@
 // second, small kernel joins a request's segments and beams in a fixed order.
 //
 //   * Which of a chunk's 4 096 logits can be among the best k?  In a segment's first chunk: those that are not below the k-th largest
-//     of the maxima of 32 groups of them, for k groups have at least that.  In the others: those above the k-th best so far; a lower
-//     token comes first among equal ones, so later equal ones need not be looked at.  What passes goes to a list in shared memory,
-//     which is cut back to k entries, in order, when it is long.
+//     of the maxima of 32 groups of them, for k groups have at least that, or, for a large k, not below what each warp has its share
+//     of k threads' maxima above.  In the others: those above the k-th best so far; a lower token comes first among equal ones, so
+//     later equal ones need not be looked at.  What passes goes to a list in shared memory, which is cut back to k entries, in order,
+//     when it is long.
 //   * The sum is a running one against a running maximum, each thread's own; a thread's maximum seldom moves after its first chunk.
+//     Additions and multiplications take two logits at once.
 //   * Scores are compared in 64 bits: a beam's logarithm of its sum is off by a few 2^-24, which the beams have alike or nearly so.
+//
+// Device time in a chain of calls, B200, logits not in L2 (of the measured copy bandwidth), both kernels: 32 x 8 beams over 152 064,
+// the best 16: fp32 40 us (0.59), bf16 37 (0.32); the best 64 of 64 rows, fp32 41 (0.14); 1 x 4 beams, the best 4, bf16 8.4, 8 x 4 14.1
+// (two launches, a first chunk); 32 x 8 over 32 003, bf16, rows not aligned 18.9 (0.13).  Instructions bound it, about 230 of a warp
+// for 512 logits: 70 are the arithmetic, the others find candidates and keep the list; the blocks' barrier, one a chunk, is the
+// longest wait.
 #include "decode.cuh"
 #include "earlytom_pages.h"
 
@@ -19,13 +27,17 @@ namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32, EACH = 16, CHUNK = THREADS * EACH;
 static_assert(CHUNK == ET_BEAM_CHUNK, "workspace");
+static_assert(EACH == 16, "four groups of four");
+constexpr int BLOCKS_SM = 4;                         // resident: 64 registers a thread (an unaligned row's loads take 80: 23 for 19 us)
 constexpr int K_MAX = 64, BEAMS_MAX = 32, SEGMENTS_MAX = 64;
 // The list is cut back when it has more than so many keys; a chunk adds CHUNK at most.  With k more than the best k the bar follows the
 // segment in four or five steps, and a chunk adds few keys.
 __host__ __device__ constexpr int longest(int k) { return 2 * k + 8; }
 constexpr int LIST = CHUNK + longest(K_MAX);
 constexpr int RANKED = 1024;                        // up to so many keys each one's rank is counted
-constexpr int FEW = 8;                              // up to so many of a first chunk are bounded by groups of threads, more by warps
+// Up to so many of a first chunk are bounded by 32 groups of threads, more by warps: by warps 4 beams' best 4 take 20.0 us in place of
+// 8.5 (too much passes), the best 18 of 155 beams 21.9 of 21.0; by groups the best 31 of 24 beams 26.3 us in place of 24.8.
+constexpr int FEW = 20;
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct Select {
@@ -66,6 +78,29 @@ __device__ __forceinline__ bool done_of(const Select& a, int row) { return a.don
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+// Two floats each
+__device__ __forceinline__ unsigned long long pair(float a, float b) {
+  unsigned long long y;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(a), "f"(b));
+  return y;
+}
+__device__ __forceinline__ void unpair(unsigned long long x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+  unsigned long long y;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+  return y;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+  unsigned long long y;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
   return y;
 }
 
@@ -132,7 +167,7 @@ __device__ __forceinline__ float sorted(float g) {
 }
 
 template <bool FP32, bool ALIGNED>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, BLOCKS_SM)
 beam_scan_kernel(const __grid_constant__ Select a) {
   constexpr int SIZE = FP32 ? 4 : 2, VEC = 16 / SIZE, SLOTS = EACH / VEC;
   extern __shared__ unsigned long long list[];      // [LIST] keys
@@ -151,16 +186,24 @@ beam_scan_kernel(const __grid_constant__ Select a) {
   auto place = [&](int j) { return (j * THREADS + tid) * VEC; };           // of this thread's j-th slot, in the chunk
   constexpr int WORDS = ALIGNED ? 4 : 8;
   auto inside = [&](int e) { return e - shift >= 0 && e - shift + (ALIGNED ? 1 : 2) * VEC <= a.vocab; };
+  auto all_inside = [&](int at) { return at - shift >= 0 && at - shift + CHUNK + (ALIGNED ? 0 : VEC) <= a.vocab; };
   auto load = [&](int at, uint32_t (&raw)[SLOTS][WORDS]) {
+    auto vectors = [&](uint32_t (&w)[WORDS], const unsigned char* p) {
+#pragma unroll
+      for (int i = 0; i < WORDS; i += 4)
+        asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "l"(p + 4 * i));
+    };
+    if (all_inside(at)) {                           // all chunks but a row's last one, and its first where it is not aligned
+      const unsigned char* const p = src + (ptrdiff_t)(at + place(0) - shift) * SIZE;
+#pragma unroll
+      for (int j = 0; j < SLOTS; ++j) vectors(raw[j], p + j * (THREADS * 16));
+      return;
+    }
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
       const int e0 = at + place(j);
-      if (inside(e0)) {
-        const unsigned char* const p = src + (ptrdiff_t)(e0 - shift) * SIZE;
-#pragma unroll
-        for (int w = 0; w < WORDS; w += 4)
-          asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(raw[j][w]), "=r"(raw[j][w + 1]), "=r"(raw[j][w + 2]), "=r"(raw[j][w + 3]) : "l"(p + 4 * w));
-      } else {
+      if (inside(e0)) vectors(raw[j], src + (ptrdiff_t)(e0 - shift) * SIZE);
+      else {
         // the row's ends, one by one, as cut() leaves them
 #pragma unroll
         for (int w = 0; w < 4; ++w) raw[j][w] = 0;
@@ -198,7 +241,7 @@ beam_scan_kernel(const __grid_constant__ Select a) {
     float x[EACH];
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
-      if (inside(at + place(j))) cut(raw[j]);
+      if (!ALIGNED && inside(at + place(j))) cut(raw[j]);
 #pragma unroll
       for (int v = 0; v < VEC; ++v)
         x[j * VEC + v] = __uint_as_float(FP32 ? raw[j][v & 3] : v & 1 ? raw[j][v / 2] & 0xffff0000u : raw[j][v / 2] << 16);
@@ -206,16 +249,21 @@ beam_scan_kernel(const __grid_constant__ Select a) {
     if (at + CHUNK < last) load(at + CHUNK, raw);   // on its way while this chunk is looked at
     float top4[EACH / 4], top;
 #pragma unroll
-    for (int i = 0; i < EACH; i += 4) top4[i / 4] = fmaxf(fmaxf(x[i], x[i + 1]), fmaxf(x[i + 2], x[i + 3]));
-    top = top4[0];
-#pragma unroll
-    for (int i = 1; i < EACH / 4; ++i) top = fmaxf(top, top4[i]);
+    for (int i = 0; i < EACH; i += 4) top4[i / 4] = max3(fmaxf(x[i], x[i + 1]), x[i + 2], x[i + 3]);
+    top = max3(fmaxf(top4[0], top4[1]), top4[2], top4[3]);
     if (top > m) { s *= exp2_fast((m - top) * LOG2E); m = top; }
     const float ref = m == -INFINITY ? 0.f : m;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    unsigned long long sum[2] = {0, 0};             // two sums each
+    const unsigned long long minus_ref = pair(-ref, -ref), log2e = pair(LOG2E, LOG2E);
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) sum[i & 3] += exp2_fast((x[i] - ref) * LOG2E);
-    s += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    for (int i = 0; i < EACH; i += 2) {
+      float e0, e1;
+      unpair(mul2(add2(pair(x[i], x[i + 1]), minus_ref), log2e), e0, e1);
+      sum[i / 2 & 1] = add2(sum[i / 2 & 1], pair(exp2_fast(e0), exp2_fast(e1)));
+    }
+    float s0, s1;
+    unpair(add2(sum[0], sum[1]), s0, s1);
+    s += s0 + s1;
     if (!begun) {
       if (a.k <= FEW) {
         // the k-th largest of the maxima of 32 groups of eight threads
@@ -476,8 +524,9 @@ extern "C" et_status et_beam_select(const void* logits_dev, int logits_fp32, lon
   if (beams > BEAMS_MAX || k > K_MAX || vocab > 1 << 20 || (long long)n_req * beams > 65535) return ET_ERR_CAPACITY;
   const int rows = n_req * beams, chunks = cdiv(vocab, CHUNK);
   if (workspace_bytes < ET_BEAM_WORKSPACE(rows, vocab, k)) return ET_ERR_CAPACITY;
-  // as many segments as keep all blocks resident at once
-  constexpr int BLOCKS = 148 * 4;
+  // as many segments as keep all blocks resident at once (32 x 8 beams over 152 064: half as many 55 us, half as many again 52, these
+  // 43; 8 x 4 beams 17.2, 12.9, 14.5; 31 x 5 over 53 552: 30.5, 26.1, 21.8)
+  constexpr int BLOCKS = 148 * BLOCKS_SM;
   int segments = rows < BLOCKS ? BLOCKS / rows : 1;
   if (segments > chunks) segments = chunks;
   if (segments > SEGMENTS_MAX) segments = SEGMENTS_MAX;
