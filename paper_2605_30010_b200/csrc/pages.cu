@@ -9,6 +9,12 @@
 //     take) are done by one cluster of eight CTAs, whose barrier costs a fraction of a launch: each CTA owns an eighth of the sequences
 //     and of the counts, totals go round through distributed shared memory.
 //   * Work of uneven sequences is dealt to threads entry by entry: a prefix sum over the sequences, and a search in it.
+//
+// Device time in a chain of calls, B200: et_pages_update, a few more positions for 64 sequences, 12 400 pages 8.7 us (a cluster's
+// launch, four rounds of loads that wait for one another, three barriers); 700 prompts of up to 240 pages in place of others, 116 000
+// pages 21 us, with their 2.1 million slots 30 (entries all over the tables, whose loads and stores bound it).  et_pages_fork, 4 rows of
+// tables of 123 entries 6.6 us, 256 rows of 52 9.9.  et_kv_copy, 2 half-filled pages of 4 + 4 heads of 128 1.9 us, 98 of them, bf16,
+// 980 positions 3.0.
 #include "decode.cuh"
 #include "earlytom_pages.h"
 
@@ -135,20 +141,17 @@ __device__ __forceinline__ Turn turn_of(const Update& u, int s) {
   return t;
 }
 
-// The slot of position pos of sequence s, -1 if it has none; `column` and `page` are of the last one asked for
-struct Slots {
-  int column = -1, page = 0;
-  __device__ __forceinline__ int find(const Update& u, int s, long long pos) {
-    const long long c = pos >> u.page_shift;
-    if (pos < 0 || c >= u.max_pages) return -1;
-    if ((int)c != column) {
-      column = (int)c;
-      page = __ldcg(u.table + (size_t)s * u.max_pages + column);
-      if ((unsigned)page >= (unsigned)u.n_pages) report(u.status, ET_PAGED_BAD_PAGE);
-    }
-    return (unsigned)page < (unsigned)u.n_pages ? (page << u.page_shift) + (int)(pos & ((1 << u.page_shift) - 1)) : -1;
-  }
-};
+// The slot of a position on the page that its table entry names, -1 if it is none (-2: there is no such entry)
+__device__ __forceinline__ int slot_of(const Update& u, int page, int pos) {
+  if ((unsigned)page < (unsigned)u.n_pages) return (page << u.page_shift) + (pos & ((1 << u.page_shift) - 1));
+  if (page != -2) report(u.status, ET_PAGED_BAD_PAGE);
+  return -1;
+}
+// The entry of a position of sequence s, -2 if the table has none
+__device__ __forceinline__ int entry_at(const Update& u, int s, long long pos) {
+  const long long column = pos >> u.page_shift;
+  return pos >= 0 && column < u.max_pages ? __ldcg(u.table + (size_t)s * u.max_pages + column) : -2;
+}
 
 constexpr int AHEAD = 4;                           // entries of a thread that are on their way at once
 __device__ __forceinline__ void give_back(const Update& u, int* const (&entry)[AHEAD]) {
@@ -170,8 +173,9 @@ __device__ __forceinline__ void give_back(const Update& u, int* const (&entry)[A
     }
 }
 
-// Entries of large tables are given back by all SMs: a block takes a sequence's, or a slice of them.  (700 prompts of up to 240 pages:
-// 46 us with the entries given back by the eight SMs below, whose scattered atomics bound them, 36 with this kernel before them.)
+// Entries of large tables are given back by all SMs: a block takes a sequence's, or a slice of them.  (700 tables of 240 entries: 41 us
+// with the entries given back by the eight SMs below, whose scattered atomics bound them, 30 with this kernel before them; 64 of 501
+// 18.1 and 18.1; smaller ones up to 0.4 us more with it, and another launch of the host's.)
 constexpr int GIVE_THREADS = 128;
 constexpr long long GIVE_ENTRIES = 1 << 14;        // tables of more
 __global__ void __launch_bounds__(GIVE_THREADS)
@@ -270,9 +274,25 @@ pages_update_kernel(const __grid_constant__ Update u, bool slots_here, bool give
     if (slots_here && u.slots) {
       __syncthreads();                             // the entries are there
       // (sums beyond 2^31 may say any row: none outside is written)
-      for (int i = tid; i < min(rows_batch, u.rows); i += THREADS) {
-        const int k = search(row_s, min(THREADS, s1 - b), i), at = row + i;
-        if ((unsigned)at < (unsigned)u.rows) u.slots[at] = got_s[k] ? Slots().find(u, b + k, (long long)kept_s[k] + i - row_s[k]) : -1;
+      const int rows = min(rows_batch, u.rows);
+      for (int i0 = tid; i0 < rows; i0 += AHEAD * THREADS) {
+        int page[AHEAD];
+        long long pos[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+          const int i = i0 + j * THREADS;
+          page[j] = -2;
+          pos[j] = 0;
+          if (i >= rows) continue;
+          const int k = search(row_s, min(THREADS, s1 - b), i);
+          pos[j] = (long long)kept_s[k] + i - row_s[k];
+          if (got_s[k]) page[j] = entry_at(u, b + k, pos[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+          const int i = i0 + j * THREADS, at = row + i;
+          if (i < rows && (unsigned)at < (unsigned)u.rows) u.slots[at] = slot_of(u, page[j], (int)pos[j]);
+        }
       }
     }
     taken += take_all; row += rows_batch;
@@ -287,8 +307,11 @@ pages_update_kernel(const __grid_constant__ Update u, bool slots_here, bool give
   }
 }
 
-// Slots of many rows: a block takes neighbouring rows, a thread eight next to one another, whose sequence it looks for once.
-constexpr int SLOT_THREADS = 256, SLOT_ROWS = 8, SLOT_SEQS = 8192, SLOTS_HERE = 4 * THREADS;
+// Slots of many rows: a block takes neighbouring rows, a thread eight next to one another.  With few rows for each CTA of the cluster
+// their threads write them, which saves a launch and its wait (32 sequences of 6 911 rows 8.6 us in place of 13.8, 200 of 21 710 11.6
+// of 16.0; one of 16 000 12.6 of 9.5, 64 of 47 102 18.3 of 15.8): the host knows neither how the rows are dealt nor their number,
+// which is `rows` at most.
+constexpr int SLOT_THREADS = 256, SLOT_ROWS = 8, SLOT_SEQS = 8192, SLOTS_HERE = 4 * THREADS;      // a CTA
 __global__ void __launch_bounds__(SLOT_THREADS)
 slots_kernel(const __grid_constant__ Update u, int rows_each) {
   extern __shared__ int ends_s[];                  // [n_seq], where they fit
@@ -304,7 +327,6 @@ slots_kernel(const __grid_constant__ Update u, int rows_each) {
   const int first = blockIdx.x * rows_each, last = min(first + rows_each, u.rows);
   for (int r0 = first + threadIdx.x * SLOT_ROWS; r0 < last; r0 += SLOT_THREADS * SLOT_ROWS) {
     int slot[SLOT_ROWS], s = -1, behind = r0, start = -1, from = 0;
-    Slots slots;
     auto look = [&](int r) {
       // the first sequence whose rows end behind this one
       int n = u.n_seq - s - 1;
@@ -315,30 +337,36 @@ slots_kernel(const __grid_constant__ Update u, int rows_each) {
       }
       s = min(s, u.n_seq - 1);                     // (sums beyond 2^31 are in no order)
       from = s > 0 ? ends[s - 1] : 0; behind = ends[s];
-      start = __ldcg(u.start + s);
-      slots = Slots();
     };
-    if (r0 < total) look(r0);
+    if (r0 < total) { look(r0); start = __ldcg(u.start + s); }
     if (start >= 0 && r0 + SLOT_ROWS <= min(min(behind, total), last)) {
       // one sequence's, and so of one page or of two
       const long long pos = (long long)start + r0 - from;
-      Slots other;
-      const int a = slots.find(u, s, pos), z = other.find(u, s, pos + SLOT_ROWS - 1);
+      const int pa = entry_at(u, s, pos), pz = entry_at(u, s, pos + SLOT_ROWS - 1);
+      const int a = slot_of(u, pa, (int)pos), z = slot_of(u, pz, (int)(pos + SLOT_ROWS - 1));
       const int left = (1 << u.page_shift) - (int)(pos & ((1 << u.page_shift) - 1));       // of the first page
 #pragma unroll
       for (int j = 0; j < SLOT_ROWS; ++j) slot[j] = j < left ? (a < 0 ? -1 : a + j) : z < 0 ? -1 : z + 1 + j - SLOT_ROWS;
     } else {
-#pragma unroll 1
+      // several sequences' rows: all starts on their way at once, then all pages
+      int seq[SLOT_ROWS], pos[SLOT_ROWS];
+#pragma unroll
       for (int j = 0; j < SLOT_ROWS; ++j) {
         const int r = r0 + j;
-        int x = -1;
-        if (r < total && r < last) {
-          if (r >= behind) look(r);
-          if (start >= 0) x = slots.find(u, s, (long long)start + r - from);
-        }
-#pragma unroll
-        for (int i = 0; i < SLOT_ROWS; ++i) if (i == j) slot[i] = x;
+        const bool live = r < total && r < last;
+        if (live && r >= behind) look(r);
+        seq[j] = live ? s : -1;
+        pos[j] = r - from;
       }
+#pragma unroll
+      for (int j = 0; j < SLOT_ROWS; ++j) {
+        const int start_j = seq[j] >= 0 ? __ldcg(u.start + seq[j]) : -1;
+        pos[j] = start_j < 0 ? -1 : (int)min((long long)start_j + pos[j], (long long)u.max_pages << u.page_shift);      // (<= 2^30)
+      }
+#pragma unroll
+      for (int j = 0; j < SLOT_ROWS; ++j) slot[j] = entry_at(u, seq[j], pos[j]);
+#pragma unroll
+      for (int j = 0; j < SLOT_ROWS; ++j) slot[j] = slot_of(u, slot[j], pos[j]);
     }
     if (aligned && r0 + SLOT_ROWS <= last) {
 #pragma unroll
@@ -548,7 +576,7 @@ et_status et_pages_update(int* refs_dev, int n_pages, int page_size, int* block_
   int* const ws = (int*)workspace_dev;
   const Update u{refs_dev, block_table_dev, len_dev, keep_dev, add_dev, new_len_dev, row_offsets_dev, rows > 0 ? slots_dev : nullptr, ws,
                  ws + n_pages, ws + n_pages + n_seq, n_pages, shift, n_seq, max_pages, rows, status_dev};
-  const bool here = rows <= SLOTS_HERE, many = (long long)n_seq * max_pages > GIVE_ENTRIES;
+  const bool here = rows <= SLOTS_HERE * (n_seq < CLUSTER ? n_seq : CLUSTER), many = (long long)n_seq * max_pages > GIVE_ENTRIES;
   if (many) {
     const int slices = cdiv(max_pages, AHEAD * GIVE_THREADS), most = 148 * 8 / n_seq + 1;
     ET_COUNT_LAUNCH();
