@@ -440,8 +440,8 @@ fork_rows_kernel(const __grid_constant__ Fork f) {
 }
 
 // The same in the cluster below, a warp each old row, where rows are few and a row is one round of a warp's loads: a launch less, 2.6 us of
-// the host's time a call.  On the device it is as fast for tables of 17 pages and 1.2 us slower for 123 (4 rows: 5.7 and 5.8 us, 7.3 and
-// 6.0), much slower for longer ones (16 rows of 481: 14.9 and 7.5 us).
+// the host's time a call, for up to 2 us of the device's (4 rows of 123 entries 6.8 us in place of 6.2, 64 of 52 8.4 of 7.1, 256 9.9 of 7.9);
+// longer rows are left to the other kernel (16 of 481: 14.9 us here, 7.5 there).
 constexpr int FORK_FEW = 256, FORK_COLUMNS = 32 * AHEAD;
 __device__ __forceinline__ void fork_row(const Fork& f, int p, unsigned short* children) {
   const int lane = threadIdx.x & 31;
