@@ -4,8 +4,8 @@
 // rows of 28 + 4 + 4 heads of 128, turned, bf16 66 us (0.91), e4m3 93 us (0.61: instructions, the rotation's among them); of 7 675
 // rows of 4 + 4 heads, e4m3 8.9 us (0.41: launch and three loads that wait for one another); of one token 2.5 us, of 64 e4m3 3.7 us.
 // Read of 63 435 rows of 16 + 16 heads of 64, bf16 86 us (0.93); of 7 675 rows, e4m3 8.9 us (0.41).
-// 4 bits, heads of 128: append of 21 124 rows of 28 + 4 + 4 heads, turned, 102 us (0.56: keys turned and scaled in 64 bits), of 7 675 rows
-// of 4 + 4 heads, not turned, 9.3 us (0.33), of one token 4.8 us; read of 21 124 rows 23 us (0.63), of 7 675 10 us (0.31), of one 2.6.
+// 4 bits, heads of 128: append of 21 124 rows of 28 + 4 + 4 heads, turned, 102 us (0.62: keys turned and scaled in 64 bits), of 7 675 rows
+// of 4 + 4 heads, not turned, 9.1 us (0.34), of one token 4.7 us; read of 21 124 rows 18.8 us (0.44), of 7 675 7.4 us (0.42), of one 2.4.
 #include <cuda_fp8.h>
 
 #include <type_traits>
@@ -516,16 +516,30 @@ kv_append_int4_kernel(const bf16* qkv, long long row_stride, int heads, PagedCac
   }
 }
 
+// Eight codes as bf16 values, i and i + 4 together: a code's bits in a bf16 of 128 are 128 + c; less 136, times the scale (twice in s).
+// The product has 12 bits and is rounded once.
+__device__ __forceinline__ uint4 int4_row8(uint32_t w, uint32_t s) {
+  uint32_t x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[i] = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+    asm("sub.rn.bf16x2 %0, %0, %1;" : "+r"(x[i]) : "r"(0x43084308u));
+    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(x[i]) : "r"(s));
+  }
+  return make_uint4(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410), __byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632));
+}
+
 // ---------------------------------------------------------------------------------------------
 // Read: a warp (or `parts` of them) takes a row, a lane 16 bytes of the cache at a time (8 bf16 or 16 e4m3 values), four of
-// them on their way; of 4-bit values 4 bytes, eight of them on their way, so that what it writes stays 16 bytes next to its
-// neighbours'.  Bound by memory.
+// them on their way; of 4-bit values 4 bytes, so that what it writes stays 16 bytes next to its neighbours' (eight of them on
+// their way: 22 us in place of 19 for 21 124 rows of 4 + 4 heads of 128, which have four a lane).  Bound by memory, of 4 bits by
+// instructions.
 // ---------------------------------------------------------------------------------------------
 template <int DH, int FMT>
 __global__ void __launch_bounds__(THREADS)
 kv_read_kernel(bf16* out, long long row_stride, PagedCache c, PagedRows r, int rows_each, int parts) {
   constexpr bool E4M3 = FMT == ET_KV_E4M3, INT4 = FMT == ET_KV_INT4;
-  constexpr int VEC = E4M3 ? 16 : 8, CHUNKS = DH / VEC, UNROLL = INT4 ? 8 : 4;
+  constexpr int VEC = E4M3 ? 16 : 8, CHUNKS = DH / VEC, UNROLL = 4;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % parts;
   const int units = 2 * c.kv_heads * CHUNKS;
   begin_after_previous();
@@ -538,6 +552,7 @@ kv_read_kernel(bf16* out, long long row_stride, PagedCache c, PagedRows r, int r
     long long pos;
     if (!places.find(c, r, (int)row, page, place, pos)) continue;          // the same for all lanes
     bf16* const dst_row = out + row * row_stride;
+    const unsigned base = ((unsigned)page * 2 * c.kv_heads << c.page_shift) + place;
     for (int u0 = part * 32 * UNROLL + lane; u0 < units; u0 += parts * 32 * UNROLL) {
       uint4 v[UNROLL];
       int b[UNROLL];
@@ -546,12 +561,11 @@ kv_read_kernel(bf16* out, long long row_stride, PagedCache c, PagedRows r, int r
         const int u = u0 + 32 * j, head = u / CHUNKS, chunk = u % CHUNKS;
         b[j] = 0;
         if (u < units) {
-          const int plane = head >= c.kv_heads ? 1 : 0;
-          const size_t at = cache_row(c, page, plane, head - plane * c.kv_heads, place);
+          const unsigned at = base + ((unsigned)head << c.page_shift);      // (plane 1 follows plane 0's heads; below 2^31)
           if (INT4) {
-            v[j].x = *reinterpret_cast<const uint32_t*>(c.data + at * (DH / 2) + chunk * 4);
-            b[j] = (reinterpret_cast<const uint16_t*>(c.scale))[at * (DH / INT4_BLOCK) + chunk / (INT4_BLOCK / 8)];
-          } else v[j] = *reinterpret_cast<const uint4*>(c.data + at * (DH * (E4M3 ? 1 : 2)) + chunk * 16);
+            v[j].x = *reinterpret_cast<const uint32_t*>(c.data + (size_t)at * (DH / 2) + chunk * 4);
+            b[j] = (reinterpret_cast<const uint16_t*>(c.scale))[(size_t)at * (DH / INT4_BLOCK) + chunk / (INT4_BLOCK / 8)];
+          } else v[j] = *reinterpret_cast<const uint4*>(c.data + (size_t)at * (DH * (E4M3 ? 1 : 2)) + chunk * 16);
           if (E4M3) b[j] = c.scale[at];
         }
       }
@@ -561,11 +575,7 @@ kv_read_kernel(bf16* out, long long row_stride, PagedCache c, PagedRows r, int r
         if (u >= units) continue;
         uint4* dst = reinterpret_cast<uint4*>(dst_row + (size_t)u * VEC);
         if (INT4) {
-          const float s = __int_as_float(b[j] << 16);
-          float y[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) y[k] = (float)((int)(v[j].x >> (4 * k) & 15) - 8) * s;
-          *dst = pack8(y);
+          *dst = int4_row8(v[j].x, (uint32_t)b[j] * 0x10001u);
         } else if (E4M3) {
           const float f = pow2(b[j] - 127);
           const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
@@ -624,7 +634,7 @@ cudaError_t launch_kv_append(const PagedCache& c, const PagedRows& r, const bf16
 
 cudaError_t launch_kv_read(const PagedCache& c, const PagedRows& r, bf16* out, long long row_stride, cudaStream_t s) {
   ET_COUNT_LAUNCH();
-  const Deal d = deal_rows(r.rows, cdiv(2 * c.kv_heads * c.head_dim / (c.format == ET_KV_E4M3 ? 16 : 8), c.format == ET_KV_INT4 ? 256 : 128));
+  const Deal d = deal_rows(r.rows, cdiv(2 * c.kv_heads * c.head_dim / (c.format == ET_KV_E4M3 ? 16 : 8), 128));
   Launch l(d.blocks, THREADS, 0, s);
 #define ET_READ(D, E) return cudaLaunchKernelEx(&l.cfg, kv_read_kernel<D, E>, out, row_stride, c, r, d.each, d.parts)
 #define ET_READ_D(D)                                                         \
