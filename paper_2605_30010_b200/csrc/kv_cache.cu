@@ -4,8 +4,8 @@
 // rows of 28 + 4 + 4 heads of 128, turned, bf16 66 us (0.91), e4m3 93 us (0.61: instructions, the rotation's among them); of 7 675
 // rows of 4 + 4 heads, e4m3 8.9 us (0.41: launch and three loads that wait for one another); of one token 2.5 us, of 64 e4m3 3.7 us.
 // Read of 63 435 rows of 16 + 16 heads of 64, bf16 86 us (0.93); of 7 675 rows, e4m3 8.9 us (0.41).
-// 4 bits, heads of 128: append of 21 124 rows of 28 + 4 + 4 heads, turned, 102 us (0.62: keys turned and scaled in 64 bits), of 7 675 rows
-// of 4 + 4 heads, not turned, 9.1 us (0.34), of one token 4.7 us; read of 21 124 rows 18.8 us (0.44), of 7 675 7.4 us (0.42), of one 2.4.
+// 4 bits, heads of 128: append of 23 942 rows of 28 + 4 + 4 heads, turned, 102 us (0.61: keys turned and scaled in 64 bits), of 7 675 rows
+// of 4 + 4 heads, not turned, 9.1 us (0.34), of one token 4.7 us; read of 23 942 rows 18.8 us (0.51), of 7 675 7.4 us (0.42), of one 2.4.
 #include <cuda_fp8.h>
 
 #include <type_traits>
@@ -532,7 +532,7 @@ __device__ __forceinline__ uint4 int4_row8(uint32_t w, uint32_t s) {
 // ---------------------------------------------------------------------------------------------
 // Read: a warp (or `parts` of them) takes a row, a lane 16 bytes of the cache at a time (8 bf16 or 16 e4m3 values), four of
 // them on their way; of 4-bit values 4 bytes, so that what it writes stays 16 bytes next to its neighbours' (eight of them on
-// their way: 22 us in place of 19 for 21 124 rows of 4 + 4 heads of 128, which have four a lane).  Bound by memory, of 4 bits by
+// their way: 22 us in place of 19 for 23 942 rows of 4 + 4 heads of 128, which have four a lane).  Bound by memory, of 4 bits by
 // instructions.
 // ---------------------------------------------------------------------------------------------
 template <int DH, int FMT>

@@ -6,15 +6,17 @@
 //   * The free pages are those whose count is 0, the i-th one the one with i smaller ones: there is no list to keep, so counts can be
 //     changed by whoever likes, in any order, with the same result.  What it costs is a look at all counts (4 bytes a page).
 //   * The parts of et_pages_update that depend on everything (which pages are free, how many pages and rows the sequences before
-//     take) are done by one cluster of eight CTAs, whose barrier costs a fraction of a launch: each CTA owns an eighth of the sequences
-//     and of the counts, totals go round through distributed shared memory.
+//     take) are done by one cluster of eight CTAs, sixteen for large tables, whose barrier costs a fraction of a launch: each CTA owns
+//     its share of the sequences and of the counts, totals go round through distributed shared memory.
 //   * Work of uneven sequences is dealt to threads entry by entry: a prefix sum over the sequences, and a search in it.
 //
 // Device time in a chain of calls, B200: et_pages_update, a few more positions for 64 sequences, 12 400 pages 8.7 us (a cluster's
 // launch, four rounds of loads that wait for one another, three barriers); 700 prompts of up to 240 pages in place of others, 116 000
-// pages 21 us, with their 2.1 million slots 30 (entries all over the tables, whose loads and stores bound it).  et_pages_fork, 4 rows of
+// pages 16 us, with their 2.1 million slots 25 (searches, and entries all over the tables).  et_pages_fork, 4 rows of
 // tables of 123 entries 6.6 us, 256 rows of 52 9.9.  et_kv_copy, 2 half-filled pages of 4 + 4 heads of 128 1.9 us, 98 of them, bf16,
 // 980 positions 3.0.
+#include <atomic>
+
 #include "decode.cuh"
 #include "earlytom_pages.h"
 
@@ -22,8 +24,8 @@ namespace et {
 
 namespace {
 
-constexpr int CLUSTER = 8, THREADS = 1024, WARPS = THREADS / 32;
-constexpr int SEGMENTS = CLUSTER * WARPS;          // each warp of the cluster looks for free pages in one of them
+constexpr int THREADS = 1024, WARPS = THREADS / 32;
+constexpr int CLUSTER = 8, LARGE = 16;             // CTAs; kernels of either are written for a cluster of C
 
 __device__ __forceinline__ int cluster_rank() {
   int r;
@@ -74,11 +76,13 @@ __device__ __forceinline__ int search(const int* prefix, int n, int x) {
 
 // ---- free pages -------------------------------------------------------------------------------------------------------------------
 // Each warp writes the free pages of its segment to the workspace, at the segment's own place; the segments' counts go to all CTAs.
+template <int C> constexpr int SEGMENTS = C * WARPS;
 // pages of a segment, a multiple of 32
-__device__ __forceinline__ int segment_size(int n_pages) { return ((n_pages + SEGMENTS - 1) / SEGMENTS + 31) & ~31; }
+template <int C> __device__ __forceinline__ int segment_size(int n_pages) { return ((n_pages + SEGMENTS<C> - 1) / SEGMENTS<C> + 31) & ~31; }
 
+template <int C>
 __device__ __forceinline__ void collect_free(const int* refs, int n_pages, int rank, int* list, int* counts) {
-  const int lane = threadIdx.x & 31, segment = rank * WARPS + (threadIdx.x >> 5), size = segment_size(n_pages);
+  const int lane = threadIdx.x & 31, segment = rank * WARPS + (threadIdx.x >> 5), size = segment_size<C>(n_pages);
   const int begin = min((long long)segment * size, (long long)n_pages), end = min((long long)begin + size, (long long)n_pages);
   constexpr int AHEAD = 8;
   int found = 0;
@@ -93,19 +97,21 @@ __device__ __forceinline__ void collect_free(const int* refs, int n_pages, int r
       found += __popc(free);
     }
   }
-  if (lane < CLUSTER) store_in(counts + segment, lane, found);
+  if (lane < C) store_in(counts + segment, lane, found);
 }
 // Behind the cluster's barrier: counts become an exclusive sum; returns how many free pages there are.
+template <int C>
 __device__ __forceinline__ int sum_segments(int* counts, int* sums) {
   int total;
-  const int v = threadIdx.x < SEGMENTS ? counts[threadIdx.x] : 0, before = block_scan(v, sums, total);
-  if (threadIdx.x < SEGMENTS) counts[threadIdx.x] = before;
+  const int v = threadIdx.x < SEGMENTS<C> ? counts[threadIdx.x] : 0, before = block_scan(v, sums, total);
+  if (threadIdx.x < SEGMENTS<C>) counts[threadIdx.x] = before;
   __syncthreads();
   return total;
 }
+template <int C>
 __device__ __forceinline__ int free_page(const int* list, const int* counts, int n_pages, int i) {
-  const int segment = search(counts, SEGMENTS, i);
-  return __ldcg(list + (size_t)segment * segment_size(n_pages) + i - counts[segment]);
+  const int segment = search(counts, SEGMENTS<C>, i);
+  return __ldcg(list + (size_t)segment * segment_size<C>(n_pages) + i - counts[segment]);
 }
 
 // ---- et_pages_update --------------------------------------------------------------------------------------------------------------
@@ -178,6 +184,9 @@ __device__ __forceinline__ void give_back(const Update& u, int* const (&entry)[A
 // 18.1 and 18.1; smaller ones up to 0.4 us more with it, and another launch of the host's.)
 constexpr int GIVE_THREADS = 128;
 constexpr long long GIVE_ENTRIES = 1 << 14;        // tables of more
+// And twice as many CTAs do the rest for tables of more than this: 700 of 240 entries 25 us in place of 30, 3 000 of 63 24 of 26, 1 000 of
+// 125 18.8 of 19.6; 64 of 501 16.4 of 15.9, 500 of 47, one position each, 9.8 of 9.3.
+constexpr long long LARGE_ENTRIES = 1 << 16;
 __global__ void __launch_bounds__(GIVE_THREADS)
 pages_give_back_kernel(const __grid_constant__ Update u) {
   begin_after_previous();
@@ -192,12 +201,13 @@ pages_give_back_kernel(const __grid_constant__ Update u) {
   }
 }
 
+template <int C>
 __global__ void __launch_bounds__(THREADS, 1)
 pages_update_kernel(const __grid_constant__ Update u, bool slots_here, bool given_back) {
-  __shared__ int counts[SEGMENTS], taken_s[CLUSTER], rows_s[CLUSTER], sums[WARPS], prefix[THREADS], stay_s[THREADS], got_s[THREADS], row_s[THREADS], kept_s[THREADS];
+  __shared__ int counts[SEGMENTS<C>], taken_s[C], rows_s[C], sums[WARPS], prefix[THREADS], stay_s[THREADS], got_s[THREADS], row_s[THREADS], kept_s[THREADS];
   __shared__ Two sums2[WARPS];
   const int tid = threadIdx.x, rank = cluster_rank();
-  const int per = (u.n_seq + CLUSTER - 1) / CLUSTER, s0 = min(rank * per, u.n_seq), s1 = min(s0 + per, u.n_seq);
+  const int per = (u.n_seq + C - 1) / C, s0 = min(rank * per, u.n_seq), s1 = min(s0 + per, u.n_seq);
   begin_after_previous();
   // ---- entries are given back; what is asked for is added up
   Two asked = 0;
@@ -228,12 +238,12 @@ pages_update_kernel(const __grid_constant__ Update u, bool slots_here, bool give
   Two cta;
   block_scan(asked, sums2, cta);
   cluster_sync();                                  // all counts have come down (and all CTAs have begun)
-  if (tid < CLUSTER) { store_in(taken_s + rank, tid, (int)(cta >> 32)); store_in(rows_s + rank, tid, (int)cta); }
-  collect_free(u.refs, u.n_pages, rank, u.list, counts);
+  if (tid < C) { store_in(taken_s + rank, tid, (int)(cta >> 32)); store_in(rows_s + rank, tid, (int)cta); }
+  collect_free<C>(u.refs, u.n_pages, rank, u.list, counts);
   cluster_sync();                                  // nobody writes into another's memory behind this
-  const int n_free = sum_segments(counts, sums);
+  const int n_free = sum_segments<C>(counts, sums);
   int taken = 0, row = 0, rows_all = 0;            // by the sequences before
-  for (int c = 0; c < CLUSTER; ++c) {
+  for (int c = 0; c < C; ++c) {
     if (c < rank) { taken += taken_s[c]; row += rows_s[c]; }
     rows_all += rows_s[c];
   }
@@ -259,7 +269,7 @@ pages_update_kernel(const __grid_constant__ Update u, bool slots_here, bool give
       for (int j = 0; j < AHEAD; ++j) {
         const int i = i0 + j * THREADS;
         page[j] = -1;
-        if (i < take_all && taken + i < n_free) page[j] = free_page(u.list, counts, u.n_pages, taken + i);
+        if (i < take_all && (unsigned)(taken + i) < (unsigned)n_free) page[j] = free_page<C>(u.list, counts, u.n_pages, taken + i);
       }
 #pragma unroll
       for (int j = 0; j < AHEAD; ++j) {
@@ -463,7 +473,7 @@ static_assert(CLUSTER * THREADS * FORK_EACH >= FORK_ROWS, "rows of a thread");
 template <bool ALL>
 __global__ void __launch_bounds__(THREADS, 1)
 fork_last_pages_kernel(const __grid_constant__ Fork f) {
-  __shared__ int counts[SEGMENTS], totals[CLUSTER], sums[WARPS];
+  __shared__ int counts[SEGMENTS<CLUSTER>], totals[CLUSTER], sums[WARPS];
   __shared__ unsigned short children[ALL ? WARPS : 1][FORK_FEW];
   const int tid = threadIdx.x, rank = cluster_rank();
   const int per = (f.n_new + CLUSTER - 1) / CLUSTER, b0 = rank * per, b1 = min(b0 + per, f.n_new);
@@ -471,7 +481,7 @@ fork_last_pages_kernel(const __grid_constant__ Fork f) {
   begin_after_previous();
   if (ALL) {
     const int warp = tid >> 5;
-    for (int p = rank * WARPS + warp; p < f.n_old; p += SEGMENTS) fork_row(f, p, children[ALL ? warp : 0]);
+    for (int p = rank * WARPS + warp; p < f.n_old; p += SEGMENTS<CLUSTER>) fork_row(f, p, children[ALL ? warp : 0]);
     cluster_sync();
   }
   int old[FORK_EACH], length[FORK_EACH];
@@ -495,9 +505,9 @@ fork_last_pages_kernel(const __grid_constant__ Fork f) {
   int all;
   int i = block_scan(wanted, sums, all);
   if (tid < CLUSTER) store_in(totals + rank, tid, all);
-  collect_free(f.refs, f.n_pages, rank, f.list, counts);
+  collect_free<CLUSTER>(f.refs, f.n_pages, rank, f.list, counts);
   cluster_sync();                                  // counts change from here on, and nobody writes into another's memory
-  const int n_free = sum_segments(counts, sums);
+  const int n_free = sum_segments<CLUSTER>(counts, sums);
   for (int c = 0; c < rank; ++c) i += totals[c];
 #pragma unroll
   for (int j = 0; j < FORK_EACH; ++j) {
@@ -508,7 +518,7 @@ fork_last_pages_kernel(const __grid_constant__ Fork f) {
       const int column = length[j] >> f.page_shift;
       atomicSub(f.refs + old[j], 1);
       if (i < n_free) {
-        from = old[j]; to = free_page(f.list, counts, f.n_pages, i); n = length[j] & ((1 << f.page_shift) - 1);
+        from = old[j]; to = free_page<CLUSTER>(f.list, counts, f.n_pages, i); n = length[j] & ((1 << f.page_shift) - 1);
         f.refs[to] = 1;
       } else {
         report(f.status, ET_PAGED_NO_PAGE);
@@ -550,6 +560,22 @@ kv_copy_kernel(PagedCache c, const int* copies, int* status, int runs_each) {
   }
 }
 
+// Whether this device takes clusters of LARGE CTAs, more than every device has to.
+bool large_clusters() {
+  static std::atomic<int> known[64];               // per device; 0: not yet, 1: no, 2: yes
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+  if (known[dev] == 0) {
+    int clusters = 0;
+    Launch l(LARGE, THREADS, 0, nullptr, LARGE);
+    const bool yes = cudaFuncSetAttribute(pages_update_kernel<LARGE>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                     cudaOccupancyMaxActiveClusters(&clusters, pages_update_kernel<LARGE>, &l.cfg) == cudaSuccess && clusters > 0;
+    if (!yes) (void)cudaGetLastError();
+    known[dev] = yes ? 2 : 1;
+  }
+  return known[dev] == 2;
+}
+
 int shift_of(int page_size) {
   for (int s = 4; s <= 7; ++s) if (page_size == 1 << s) return s;
   return -1;
@@ -584,9 +610,10 @@ et_status et_pages_update(int* refs_dev, int n_pages, int page_size, int* block_
     const cudaError_t e = cudaLaunchKernelEx(&give.cfg, pages_give_back_kernel, u);
     if (e != cudaSuccess) return launched(e);
   }
+  const int cluster = (long long)n_seq * max_pages > LARGE_ENTRIES && large_clusters() ? LARGE : CLUSTER;
   ET_COUNT_LAUNCH();
-  Launch l(CLUSTER, THREADS, 0, (cudaStream_t)cuda_stream, CLUSTER);
-  const cudaError_t e = cudaLaunchKernelEx(&l.cfg, pages_update_kernel, u, here, many);
+  Launch l(cluster, THREADS, 0, (cudaStream_t)cuda_stream, cluster);
+  const cudaError_t e = cudaLaunchKernelEx(&l.cfg, cluster == LARGE ? pages_update_kernel<LARGE> : pages_update_kernel<CLUSTER>, u, here, many);
   if (here || e != cudaSuccess) return launched(e);
   ET_COUNT_LAUNCH();
   const int tile = SLOT_THREADS * SLOT_ROWS, each = cdiv(cdiv(rows, 148 * 8), tile) * tile;

@@ -670,3 +670,15 @@ def test_update_of_large_tables(B, n):
     add = np.minimum(rng.integers(0, longest, n), table.shape[1] * page - np.minimum(np.maximum(lens, 0), keep))
     check_update(B, page, lens, table, refs, keep, add)
     check_update(B, page, lens, table, refs, np.full(n, -1), None, in_place=True)
+
+
+@pytest.mark.parametrize("n,longest,page", [(1500, 900, 16), (20_000, 70, 16), (2, 640_000, 16)])
+def test_update_of_tables_for_the_larger_cluster(B, n, longest, page):
+    """Tables of more than 2^16 entries, also with more sequences than the cluster's threads and with fewer than it has CTAs."""
+    rng = np.random.default_rng(n)
+    lens, table, refs = random_state(rng, n, longest, page, 3_000)
+    assert table.size > 1 << 16
+    keep = np.maximum(lens - rng.integers(0, longest, n), 0)
+    add = np.minimum(rng.integers(0, longest, n), table.shape[1] * page - np.minimum(np.maximum(lens, 0), keep))
+    check_update(B, page, lens, table, refs, keep, add)
+    check_update(B, page, lens, table, refs, None, None, in_place=True)
