@@ -166,13 +166,37 @@ __device__ __forceinline__ float sorted(float g) {
   return g;
 }
 
+// The k-th largest of the threads' values: each warp's in order, a value's place among the other warps' by search.  All threads.
+__device__ __noinline__ float kth_top(float top, int k, float (*tops)[32], float* result) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const float g = sorted(top);
+  tops[warp][lane] = g;
+  __syncthreads();
+  int rank = lane;
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) {
+    int before = 0;                                 // how many of the 32 come before this one
+#pragma unroll
+    for (int step = 16; step > 0; step >>= 1) {
+      const float other = tops[w][before + step - 1];
+      if (other > g || (other == g && w < warp)) before += step;
+    }
+    const float other = tops[w][31];
+    if (before == 31 && (other > g || (other == g && w < warp))) ++before;
+    if (w != warp) rank += before;
+  }
+  if (rank == k - 1) *result = g;
+  __syncthreads();
+  return *result;
+}
+
 template <bool FP32, bool ALIGNED>
 __global__ void __launch_bounds__(THREADS, BLOCKS_SM)
 beam_scan_kernel(const __grid_constant__ Select a) {
   constexpr int SIZE = FP32 ? 4 : 2, VEC = 16 / SIZE, SLOTS = EACH / VEC;
   extern __shared__ unsigned long long list[];      // [LIST] keys
   __shared__ int added_s[3];                        // keys that a chunk adds, in turn
-  __shared__ float group_top[32];
+  __shared__ float group_top[32], thread_top[WARPS][32];
   __shared__ unsigned long long best[2 * WARPS + K_MAX];
   __shared__ uint2 reduce[WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, segment = blockIdx.x, row = blockIdx.y;
@@ -282,6 +306,8 @@ beam_scan_kernel(const __grid_constant__ Select a) {
 #pragma unroll
         for (int w = 1; w < WARPS; ++w) bar = fminf(bar, group_top[w]);
       }
+      // Too few groups or warps have logits, of a short vocabulary: all that there are would pass (the best 32 of 721 tokens 43 us, so 17).
+      if (bar == -INFINITY) bar = kth_top(top, a.k, thread_top, group_top);
     }
     int* const added = added_s + turn;
     if (begun ? top > bar : top >= bar)

@@ -682,3 +682,15 @@ def test_update_of_tables_for_the_larger_cluster(B, n, longest, page):
     add = np.minimum(rng.integers(0, longest, n), table.shape[1] * page - np.minimum(np.maximum(lens, 0), keep))
     check_update(B, page, lens, table, refs, keep, add)
     check_update(B, page, lens, table, refs, None, None, in_place=True)
+
+
+@pytest.mark.parametrize("k", [10, 16, 32, 64])
+@pytest.mark.parametrize("vocab,allowed", [(300, 1.0), (721, 1.0), (2500, 1.0), (9001, 0.01), (4096, 0.02)])
+def test_select_of_few_tokens(B, vocab, allowed, k):
+    """Vocabularies and grammars that leave most of a block's threads without a token."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(vocab + k)
+    x = torch.randn((6, vocab), device="cuda", generator=gen) * 4
+    x = torch.where(torch.rand((6, vocab), device="cuda", generator=gen) < allowed, x, -math.inf)
+    x[5, vocab // 3:] = -math.inf
+    check_select(B, x, 3, k, scores=[-1.0, -2.0, -3.0, -1.0, -2.0, -3.0])
