@@ -450,10 +450,11 @@ beam_join_kernel(const __grid_constant__ Select a) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) bar = fminf(bar, __shfl_xor_sync(0xffffffffu, bar, o));
     }
-    int n = 0;
+    // one list is in order as it is; and as many entries as reach the bar at least are to be merged if they are too many
+    int n = a.segments == 1 || each * lists >= NEAR ? NEAR + 1 : 0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      bool more = few || 32 * i < a.segments;
+      bool more = n <= NEAR && (few || 32 * i < a.segments);
       for (int first = 0; more; first += AHEAD) {
         if (first > 0) load(i, first);
 #pragma unroll
