@@ -14,7 +14,7 @@
 //   * Scores are compared in 64 bits: a beam's logarithm of its sum is off by a few 2^-24, which the beams have alike or nearly so.
 //
 // Device time in a chain of calls, B200, logits not in L2 (of the measured copy bandwidth), both kernels: 32 x 8 beams over 152 064,
-// the best 16: fp32 40 us (0.59), bf16 37 (0.32); the best 64 of 64 rows, fp32 41 (0.14); 1 x 4 beams, the best 4, bf16 8.4, 8 x 4 14.1
+// the best 16: fp32 41 us (0.58), bf16 37 (0.32); the best 64 of 64 rows, fp32 41 (0.15); the best 31 of 6 x 4 beams over 194 849 20; 1 x 4 beams, the best 4, bf16 8.4, 8 x 4 14.1
 // (two launches, a first chunk); 32 x 8 over 32 003, bf16, rows not aligned 18.9 (0.13).  Instructions bound it, about 230 of a warp
 // for 512 logits: 70 are the arithmetic, the others find candidates and keep the list; the blocks' barrier, one a chunk, is the
 // longest wait.
@@ -430,9 +430,16 @@ beam_join_kernel(const __grid_constant__ Select a) {
       for (int p = 0; p < AHEAD; ++p)
         e[i][p] = lane + 32 * i < a.segments && first + p < k ? __ldcg(list_of(lane + 32 * i) + first + p) : make_float2(-INFINITY, 0.f);
     };
-    // what at least k entries reach: of the first 32 lists' first ones the k-th largest, of their later ones the least
+    // What at least k entries reach: if m of the first 32 lists have a j-th one that does, m j entries do.  From the first j on for which
+    // there are enough lists, some j are tried; for the first entries alone one will do.  (Where all entries can be ranked none is needed,
+    // which saves 0.6 to 1 us.)  The best 31 of 24 beams' 24 lists each: 25.0 us with the lists' second entries alone, 20.5.
+    constexpr int TRIED = 4;
+    const bool tried = a.segments * k > NEAR;
     const int lists = min(a.segments, 32), each = (k + lists - 1) / lists;
-    float bar = lane < lists ? __ldcg(list_of(lane) + each - 1).x : -INFINITY;
+    float reach[TRIED];
+#pragma unroll
+    for (int t = 0; t < TRIED; ++t)
+      reach[t] = tried && (t == 0 || each > 1) && lane < lists && each + t <= k ? __ldcg(list_of(lane) + each + t - 1).x : -INFINITY;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       part[i] = lane + 32 * i < a.segments ? __ldcg(list_of(lane + 32 * i) + k) : make_float2(-INFINITY, 0.f);
@@ -443,15 +450,13 @@ beam_join_kernel(const __grid_constant__ Select a) {
         e[i][p] = segment < a.segments ? __ldcg(list_of(segment) + at - segment * k) : make_float2(-INFINITY, 0.f);
       }
     }
-    if (each == 1) {
-      bar = __shfl_sync(0xffffffffu, sorted(bar), k - 1);
-    } else {
-      if (lane >= lists) bar = INFINITY;
+    float bar = -INFINITY;
+    if (tried) bar = __shfl_sync(0xffffffffu, sorted(reach[0]), (k + each - 1) / each - 1);
+    if (tried && each > 1)
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) bar = fminf(bar, __shfl_xor_sync(0xffffffffu, bar, o));
-    }
-    // one list is in order as it is; and as many entries as reach the bar at least are to be merged if they are too many
-    int n = a.segments == 1 || each * lists >= NEAR ? NEAR + 1 : 0;
+      for (int t = 1; t < TRIED; ++t) bar = fmaxf(bar, __shfl_sync(0xffffffffu, sorted(reach[t]), (k + each + t - 1) / (each + t) - 1));
+    // One list is in order as it is, and k entries at least reach the bar.
+    int n = a.segments == 1 || k >= NEAR ? NEAR + 1 : 0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       bool more = n <= NEAR && (few || 32 * i < a.segments);
