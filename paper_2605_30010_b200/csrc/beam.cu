@@ -14,10 +14,10 @@
 //   * Scores are compared in 64 bits: a beam's logarithm of its sum is off by a few 2^-24, which the beams have alike or nearly so.
 //
 // Device time in a chain of calls, B200, logits not in L2 (of the measured copy bandwidth), both kernels: 32 x 8 beams over 152 064,
-// the best 16: fp32 41 us (0.58), bf16 37 (0.32); the best 64 of 64 rows, fp32 41 (0.15); the best 31 of 6 x 4 beams over 194 849 20; 1 x 4 beams, the best 4, bf16 8.4, 8 x 4 14.1
-// (two launches, a first chunk); 32 x 8 over 32 003, bf16, rows not aligned 18.9 (0.13).  Instructions bound it, about 230 of a warp
-// for 512 logits: 70 are the arithmetic, the others find candidates and keep the list; the blocks' barrier, one a chunk, is the
-// longest wait.
+// the best 16: fp32 40 us (0.59), bf16 37 (0.32); the best 64 of 64 rows, fp32 40 (0.15); the best 31 of 6 x 4 beams over 194 849 20;
+// 1 x 4 beams, the best 4, bf16 8.4, 8 x 4 14.1 (two launches, a first chunk); 32 x 8 over 32 003, bf16, rows not aligned 18.9 (0.13).
+// Instructions bound it, about 230 of a warp for 512 logits: 70 are the arithmetic, the others find candidates and keep the list;
+// the blocks' barrier, one a chunk, is the longest wait.
 #include "decode.cuh"
 #include "earlytom_pages.h"
 
@@ -167,13 +167,13 @@ __device__ __forceinline__ float sorted(float g) {
 }
 
 // The k-th largest of the threads' values: each warp's in order, a value's place among the other warps' by search.  All threads.
-__device__ __noinline__ float kth_top(float top, int k, float (*tops)[32], float* result) {
+__device__ __forceinline__ float kth_top(float top, int k, float (*tops)[32], float* result) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const float g = sorted(top);
   tops[warp][lane] = g;
   __syncthreads();
   int rank = lane;
-#pragma unroll
+#pragma unroll 2
   for (int w = 0; w < WARPS; ++w) {
     int before = 0;                                 // how many of the 32 come before this one
 #pragma unroll
