@@ -49,7 +49,8 @@ enum { ET_PAGED_NO_PAGE = 6, ET_PAGED_BAD_COUNT = 7, ET_PAGED_BAD_ROW = 8 };
  * A given-back entry that is no page is skipped (ET_PAGED_BAD_PAGE), a count that is not above 0 stays (ET_PAGED_BAD_COUNT).
  * workspace_dev: ET_PAGES_WORKSPACE(n_pages, n_seq) bytes, 16-byte aligned, contents neither needed nor kept; one call at a time.
  * Limits (ET_ERR_CAPACITY): n_pages * page_size < 2^31, max_pages * page_size <= 2^30, n_seq <= 65536, n_seq * max_pages < 2^31.  The
- * sums of what is asked for have to stay below 2^31. */
+ * sums of what is asked for have to stay below 2^31: beyond that row_offsets and slots hold any values, while tables, counts and lengths
+ * stay right. */
 #define ET_PAGES_WORKSPACE(n_pages, n_seq) (4ull * (n_pages) + 8ull * (n_seq))
 ET_API et_status et_pages_update(int* refs_dev, int n_pages, int page_size, int* block_table_dev, int n_seq, int max_pages,
                                  const int* len_dev, const int* keep_dev, const int* add_dev, int* new_len_dev, int* row_offsets_dev,

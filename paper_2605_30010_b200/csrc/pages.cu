@@ -44,25 +44,33 @@ __device__ __forceinline__ void store_in(int* p, int cta, int v) {
 }
 __device__ __forceinline__ void report(int* status, int code) { if (status) atomicMax(status, code); }
 
-// Exclusive sums over the block's threads; `total`: all of them.  T: an integer, or two in one 64-bit number.
+// Two sums side by side.  What is asked for in total may be more than a number holds (it then says any row); the takes, of entries that
+// the tables have, never are, and nothing of the one sum reaches the other.
+struct Two { int takes; unsigned rows; };
+__device__ __forceinline__ Two operator+(Two a, Two b) { return Two{a.takes + b.takes, a.rows + b.rows}; }
+__device__ __forceinline__ Two operator-(Two a, Two b) { return Two{a.takes - b.takes, a.rows - b.rows}; }
+__device__ __forceinline__ int shfl_up(int v, int o) { return __shfl_up_sync(0xffffffffu, v, o); }
+__device__ __forceinline__ int shfl(int v, int from) { return __shfl_sync(0xffffffffu, v, from); }
+__device__ __forceinline__ Two shfl_up(Two v, int o) { return Two{__shfl_up_sync(0xffffffffu, v.takes, o), __shfl_up_sync(0xffffffffu, v.rows, o)}; }
+__device__ __forceinline__ Two shfl(Two v, int from) { return Two{__shfl_sync(0xffffffffu, v.takes, from), __shfl_sync(0xffffffffu, v.rows, from)}; }
+
+// Exclusive sums over the block's threads; `total`: all of them.  T: int or Two.
 template <typename T>
 __device__ __forceinline__ T block_scan(T v, T* sums, T& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   T inc = v;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) { const T u = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += u; }
+  for (int o = 1; o < 32; o <<= 1) { const T u = shfl_up(inc, o); if (lane >= o) inc = inc + u; }
   __syncthreads();                                 // sums is free
   if (lane == 31) sums[warp] = inc;
   __syncthreads();
   T w = sums[lane];                                // WARPS is 32
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) { const T u = __shfl_up_sync(0xffffffffu, w, o); if (lane >= o) w += u; }
-  total = __shfl_sync(0xffffffffu, w, 31);
-  const T before = __shfl_sync(0xffffffffu, w, warp ? warp - 1 : 0);
-  return inc - v + (warp ? before : (T)0);
+  for (int o = 1; o < 32; o <<= 1) { const T u = shfl_up(w, o); if (lane >= o) w = w + u; }
+  total = shfl(w, 31);
+  const T before = shfl(w, warp ? warp - 1 : 0);
+  return warp ? inc - v + before : inc - v;
 }
-typedef unsigned long long Two;                    // takes above, rows below; neither sum leaves 32 bits
-__device__ __forceinline__ Two two(int takes, int rows) { return (Two)(unsigned)takes << 32 | (unsigned)rows; }
 
 // The last i of [0, n) with prefix[i] <= x (prefix ascending, prefix[0] <= x)
 __device__ __forceinline__ int search(const int* prefix, int n, int x) {
@@ -210,13 +218,13 @@ pages_update_kernel(const __grid_constant__ Update u, bool slots_here, bool give
   const int per = (u.n_seq + C - 1) / C, s0 = min(rank * per, u.n_seq), s1 = min(s0 + per, u.n_seq);
   begin_after_previous();
   // ---- entries are given back; what is asked for is added up
-  Two asked = 0;
+  Two asked{0, 0};
   Turn t{};
   for (int b = s0; b < s1; b += THREADS) {
     const int s = b + tid;
     t = Turn{};
     if (s < s1) t = turn_of(u, s);
-    asked += two(t.take, t.add);
+    asked = asked + Two{t.take, (unsigned)t.add};
     int dropped;
     const int before = block_scan(given_back ? 0 : t.drop, sums, dropped);
     if (dropped == 0) continue;
@@ -238,28 +246,31 @@ pages_update_kernel(const __grid_constant__ Update u, bool slots_here, bool give
   Two cta;
   block_scan(asked, sums2, cta);
   cluster_sync();                                  // all counts have come down (and all CTAs have begun)
-  if (tid < C) { store_in(taken_s + rank, tid, (int)(cta >> 32)); store_in(rows_s + rank, tid, (int)cta); }
+  if (tid < C) { store_in(taken_s + rank, tid, cta.takes); store_in(rows_s + rank, tid, (int)cta.rows); }
   collect_free<C>(u.refs, u.n_pages, rank, u.list, counts);
   cluster_sync();                                  // nobody writes into another's memory behind this
   const int n_free = sum_segments<C>(counts, sums);
-  int taken = 0, row = 0, rows_all = 0;            // by the sequences before
+  Two so_far{0, 0}, all{0, 0};                     // by the sequences before, by all
   for (int c = 0; c < C; ++c) {
-    if (c < rank) { taken += taken_s[c]; row += rows_s[c]; }
-    rows_all += rows_s[c];
+    const Two of{taken_s[c], (unsigned)rows_s[c]};
+    if (c < rank) so_far = so_far + of;
+    all = all + of;
   }
+  const int rows_all = (int)all.rows;
   // ---- entries are taken
   for (int b = s0; b < s1; b += THREADS) {
     const int s = b + tid;
     if (s1 - s0 > THREADS) { t = Turn{}; if (s < s1) t = turn_of(u, s); }          // else it is known
     Two batch;
-    const Two ahead = block_scan(two(t.take, t.add), sums2, batch);
-    const int before = (int)(ahead >> 32), rows_before = (int)ahead, take_all = (int)(batch >> 32), rows_batch = (int)batch;
+    const Two ahead = block_scan(Two{t.take, (unsigned)t.add}, sums2, batch);
+    const int taken = so_far.takes, row = (int)so_far.rows, before = ahead.takes, rows_before = (int)ahead.rows, take_all = batch.takes,
+              rows_batch = (int)batch.rows;
     const bool got = t.fits && (t.take == 0 || taken + before + t.take <= n_free);
     if (s < s1) {
       if (!got) report(u.status, t.fits ? (int)ET_PAGED_NO_PAGE : (int)ET_PAGED_CAPACITY);
       u.new_len[s] = t.kept < 0 ? -1 : t.kept + (got ? t.add : 0);
-      if (u.offsets) u.offsets[s] = row + rows_before;
-      if (u.slots && !slots_here) { u.ends[s] = row + rows_before + t.add; u.start[s] = got ? t.kept : -1; }
+      if (u.offsets) u.offsets[s] = (int)(so_far.rows + ahead.rows);
+      if (u.slots && !slots_here) { u.ends[s] = (int)(so_far.rows + ahead.rows + t.add); u.start[s] = got ? t.kept : -1; }
     }
     prefix[tid] = before; stay_s[tid] = t.stay; got_s[tid] = got; row_s[tid] = rows_before; kept_s[tid] = t.kept;
     __syncthreads();
@@ -305,7 +316,7 @@ pages_update_kernel(const __grid_constant__ Update u, bool slots_here, bool give
         }
       }
     }
-    taken += take_all; row += rows_batch;
+    so_far = so_far + batch;
     __syncthreads();
   }
   if (rank == 0) {
