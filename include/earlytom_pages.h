@@ -67,7 +67,8 @@ ET_API et_status et_pages_update(int* refs_dev, int n_pages, int page_size, int*
  * ascending order, after the counts have followed) and an entry of copies_dev [n_new][3]: old page, new page, positions in it; rows that
  * copy nothing have -1, -1, 0.  Where there is no free page left the entry becomes -1 (ET_PAGED_NO_PAGE); the row keeps its length, and
  * every later call over it reports the page that is missing.  new_len_dev [n_new] (may not be len_dev): the row's positions, -1 for
- * slots not in use.  Entries that are no pages of the cache are copied and not counted (ET_PAGED_BAD_PAGE).
+ * slots not in use.  Entries that are no pages of the cache are copied and not counted (ET_PAGED_BAD_PAGE).  No count falls
+ * below 0 (ET_PAGED_BAD_COUNT); a half-filled last page whose count is not above 0 stays with its rows, as it is.
  * workspace_dev: ET_FORK_WORKSPACE(n_pages, n_new) bytes, as above.  Limits (ET_ERR_CAPACITY): n_old, n_new <= 16384, and those of
  * et_pages_update. */
 #define ET_FORK_WORKSPACE(n_pages, n_new) (4ull * (n_pages) + 16ull * (n_new))

@@ -510,7 +510,10 @@ fork_last_pages_kernel(const __grid_constant__ Fork f) {
     length[j] = info.y;
     old[j] = info.z;
     if ((unsigned)old[j] >= (unsigned)f.n_pages) continue;
-    own[j] = !(info.x < 0 && __ldcg(f.refs + old[j]) == -info.x);
+    // A page that is named and has no count may be handed to another row below: nothing is copied from it, and its count stays.
+    const int count = __ldcg(f.refs + old[j]);
+    if (count <= 0) { report(f.status, ET_PAGED_BAD_COUNT); continue; }
+    own[j] = !(info.x < 0 && count == -info.x);
     wanted += own[j];
   }
   int all;
@@ -520,14 +523,16 @@ fork_last_pages_kernel(const __grid_constant__ Fork f) {
   cluster_sync();                                  // counts change from here on, and nobody writes into another's memory
   const int n_free = sum_segments<CLUSTER>(counts, sums);
   for (int c = 0; c < rank; ++c) i += totals[c];
+  int left[FORK_EACH];
 #pragma unroll
   for (int j = 0; j < FORK_EACH; ++j) {
     const int b = b0 + tid * FORK_EACH + j;
+    left[j] = 1;
     if (b >= b1) continue;
     int from = -1, to = -1, n = 0;
     if (own[j]) {
       const int column = length[j] >> f.page_shift;
-      atomicSub(f.refs + old[j], 1);
+      left[j] = atomicSub(f.refs + old[j], 1);
       if (i < n_free) {
         from = old[j]; to = free_page<CLUSTER>(f.list, counts, f.n_pages, i); n = length[j] & ((1 << f.page_shift) - 1);
         f.refs[to] = 1;
@@ -540,6 +545,12 @@ fork_last_pages_kernel(const __grid_constant__ Fork f) {
     f.new_len[b] = length[j];
     f.copies[3 * b] = from; f.copies[3 * b + 1] = to; f.copies[3 * b + 2] = n;
   }
+#pragma unroll
+  for (int j = 0; j < FORK_EACH; ++j)
+    if (left[j] <= 0) {                              // fewer counts than rows
+      atomicAdd(f.refs + old[j], 1);
+      report(f.status, ET_PAGED_BAD_COUNT);
+    }
 }
 
 // ---- et_kv_copy: a page's rows of one plane and head are contiguous; a block takes some of these runs ------------------------------

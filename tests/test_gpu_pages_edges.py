@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from tests.test_gpu_decode import i32
-from tests.test_gpu_pages import B, random_state, update_reference                                # noqa: F401
+from tests.test_gpu_pages import B, random_state, up, update_reference                            # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +50,77 @@ def test_update_of_sums_beyond_32_bits_leaves_tables_right(B, n_seq, longest, ro
     for (_, got), expected in zip(bufs, want[:3]):
         assert np.array_equal(got.cpu().numpy(), expected)
     assert status.item() >= max(want[5])                  # (rows of no order may meet entries that are no pages)
+
+
+# ---- et_pages_fork ----------------------------------------------------------------------------------------------------
+
+def fork_of_low_counts(refs, page, table, lens, parent, new_table):
+    """As fork_reference, for counts that may be lower than the entries that name their pages."""
+    refs, new_table = refs.copy(), new_table.copy()
+    codes, lengths, kids = set(), [], {}
+    for b, p in enumerate(parent):
+        if p >= 0:
+            kids.setdefault(p, []).append(b)
+        lengths.append(max(lens[p], -1) if p >= 0 else -1)
+
+    def down(g):
+        if refs[g] <= 0:
+            codes.add(7)
+        else:
+            refs[g] -= 1
+    for p in range(len(table)):
+        for j in range(up(max(lens[p], 0), page)):
+            family = kids.get(p, [])
+            if family:
+                refs[table[p, j]] += len(family) - 1
+            else:
+                down(table[p, j])
+            for b in family:
+                new_table[b, j] = table[p, j]
+    last = {}
+    for b, n in enumerate(lengths):
+        if n > 0 and n % page:
+            g, family = new_table[b, n // page], kids[parent[b]]
+            if refs[g] <= 0:
+                codes.add(7)
+            elif not (b == family[0] and refs[g] == len(family)):
+                last[b] = g
+    free = list(np.nonzero(refs == 0)[0])
+    copies = np.array([[-1, -1, 0]] * len(parent))
+    for i, (b, g) in enumerate(last.items()):
+        down(g)
+        assert i < len(free)
+        new_table[b, lengths[b] // page] = free[i]
+        copies[b] = g, free[i], lengths[b] % page
+    for i in range(len(last)):
+        refs[free[i]] = 1
+    return refs, new_table, np.array(lengths), copies, codes
+
+
+@pytest.mark.parametrize("wide", [0, 200])
+def test_fork_with_counts_that_are_too_low(B, wide):                                              # noqa: F811
+    """Half-filled last pages whose counts are 0, below it, or lower than the rows that leave them: no count becomes negative, and no page
+    that is copied is another row's new one.  In one launch and in two (wider tables)."""
+    page, rows, columns = 16, 12, 4
+    table = np.full((rows, columns + wide), -5)
+    table[:, :columns] = np.arange(rows * columns).reshape(rows, columns)[:, ::-1]
+    lens = np.full(rows, 3 * page + 7)
+    refs = np.ones(rows * columns + 30, int)
+    refs[rows * columns:] = 0
+    parent = np.array([0, 1, 2, 3, 3, 4, 4, 4, 5, 5, 6, 8, 9, 9, 9])                               # rows 7, 10 and 11 end
+    for row, count in ((0, 0), (1, -4), (3, 0), (4, -1), (5, 2), (6, 3), (7, 0), (9, -9), (10, -2)):
+        refs[table[row, 3]] = count
+    refs[table[2, 1]], refs[table[11, 0]] = 0, 0                                                  # whole pages, kept and given up
+    for counts in (refs, np.where(refs < 0, refs, np.minimum(refs, 1))):
+        new = np.full((len(parent), table.shape[1]), -5)
+        want = fork_of_low_counts(counts, page, table, lens, parent, new)
+        assert 7 in want[4]
+        bufs = [guarded(x) for x in (counts, new, np.full(len(parent), -9), np.full((len(parent), 3), -9))]
+        status = i32([0])
+        B.et_pages_fork(bufs[0][1], page, i32(table), i32(lens), i32(parent), bufs[1][1], bufs[2][1], bufs[3][1], status)
+        assert all(guards_hold(wide) for wide, _ in bufs)
+        for (_, got), expected in zip(bufs, want[:4]):
+            assert np.array_equal(got.cpu().numpy(), expected)
+        assert status.item() == 7
+        copied, fresh = want[3][want[3][:, 0] >= 0, 0], want[3][want[3][:, 0] >= 0, 1]
+        assert not set(copied) & set(fresh)
