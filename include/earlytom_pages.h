@@ -40,6 +40,11 @@ enum { ET_PAGED_NO_PAGE = 6, ET_PAGED_BAD_COUNT = 7, ET_PAGED_BAD_ROW = 8 };
  * with i smaller ones.  A sequence whose last one there is no free page for gets no position (status ET_PAGED_NO_PAGE; its entries
  * become -1), nor does one whose positions the table cannot hold (ET_PAGED_CAPACITY; it takes no pages).
  *
+ * The new positions begin in the last kept page if that one is not full, and then it has to be the sequence's own: nothing is copied and
+ * no other page taken in its place, so two sequences that hold it would get the same places in it, and no status says so.  Where others
+ * hold it too (a beginning in common that ends inside a page, positions given back into pages that are shared) et_pages_fork gives
+ * each row one of its own: et_pages_update with add = 0, et_pages_fork with each row its own parent, et_kv_copy, then the new positions.
+ *
  * new_len_dev [n_seq] (may be len_dev): keep + add, keep where it got none, -1 where the slot is not in use.
  * row_offsets_dev [n_seq + 1] (may be NULL): where the new positions' rows stand when they are packed in the order of the sequences,
  * the exclusive sum of what was asked for, whether it was got or not; et_kv_append takes it with the kept lengths as its start.

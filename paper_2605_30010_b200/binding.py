@@ -1030,7 +1030,8 @@ def et_pages_update(refs, page_size, block_table, lens, keep=None, add=None, new
                     workspace=None, stream=None):
     """Sequences keep the first keep of their lens positions (None: all) and get add more (None: one each).  refs int32 [n_pages] and
     block_table follow in place; returns new_len (created if none is given; may be lens).  row_offsets int32 [n_seq + 1] and slots
-    int32 [rows] are filled if given."""
+    int32 [rows] are filled if given.  A kept last page that is not full has to be the sequence's own where it gets more (et_pages_fork
+    makes it so)."""
     if _torch is None:
         _import_torch()
     n_seq, max_pages = _table(block_table)

@@ -52,6 +52,46 @@ def test_update_of_sums_beyond_32_bits_leaves_tables_right(B, n_seq, longest, ro
     assert status.item() >= max(want[5])                  # (rows of no order may meet entries that are no pages)
 
 
+def rows_of(B, cache, table, lens):                                                               # noqa: F811
+    """Each sequence's stored rows."""
+    return [B.et_kv_read(cache, None, table[i:i + 1].contiguous(), i32([0]), n, i32([0, n])) if n > 0 else None for i, n in enumerate(lens.tolist())]
+
+
+def test_sequences_grow_behind_a_shared_beginning(B):                                             # noqa: F811
+    """Three conversations go on from 40 positions that a fourth holder keeps, a fifth gives drafts back into a shared page: each one gets
+    its last page from et_pages_fork before it grows.  No two have a place in common, and nobody's stored rows change."""
+    import torch
+    page, n_pages, kvh, d = 16, 60, 2, 64
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    cache = torch.randn((n_pages, 2, kvh, page, d), device="cuda", generator=gen).to(torch.bfloat16)
+    table = np.full((5, 8), -1)
+    table[:4, :3] = [7, 30, 12]                                                                  # 40 positions, the last 8 in page 12
+    table[4, :4] = [7, 30, 12, 5]                                                                # 55 of which 41 stay, 9 in page 12
+    refs = np.bincount(table[table >= 0], minlength=n_pages)
+    refs[12] += 1                                                                                # kept for later ones
+    r, t, lens, status = i32(refs), i32(table), i32([40, 40, 40, 40, 55]), i32([0])
+    before = rows_of(B, cache, t, i32([40, 40, 40, 40, 41]))
+    lens = B.et_pages_update(r, page, t, lens, keep=i32([40, 40, 40, 40, 41]), add=i32([0] * 5), status=status)
+    other = i32(np.full((5, 8), -1))
+    lens, copies = B.et_pages_fork(r, page, t, lens, i32(range(5)), other, status=status)
+    B.et_kv_copy(cache, None, copies, status)
+    add, offsets, slots = i32([1, 25, 8, 0, 3]), i32([0] * 6), i32([-9] * 37)
+    new = B.et_pages_update(r, page, other, lens, add=add, row_offsets=offsets, slots=slots, status=status)
+    qkv = torch.randn((37, 2 * kvh * d), device="cuda", generator=gen).to(torch.bfloat16)
+    B.et_kv_append(cache, None, qkv, 0, other, lens, offsets, status=status)
+    assert status.item() == 0 and new.tolist() == [41, 65, 48, 40, 44]
+    places = slots.tolist()
+    assert min(places) >= 0 and len(set(places)) == 37 and not {p // page for p in places} & {7, 30, 12}
+    now, first = rows_of(B, cache, other, new), offsets.tolist()
+    for i in range(5):
+        n = len(before[i])
+        assert torch.equal(now[i][:n], before[i]) and torch.equal(now[i][n:], qkv[first[i]:first[i + 1]])
+    live = np.arange(8) < up(new.cpu().numpy(), page)[:, None]
+    held = np.bincount(other.cpu().numpy()[live], minlength=n_pages)
+    held[12] += 1
+    assert np.array_equal(r.cpu().numpy(), held)
+
+
 # ---- et_pages_fork ----------------------------------------------------------------------------------------------------
 
 def fork_of_low_counts(refs, page, table, lens, parent, new_table):
