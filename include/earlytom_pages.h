@@ -47,7 +47,8 @@ enum { ET_PAGED_NO_PAGE = 6, ET_PAGED_BAD_COUNT = 7, ET_PAGED_BAD_ROW = 8 };
  *
  * new_len_dev [n_seq] (may be len_dev): keep + add, keep where it got none, -1 where the slot is not in use.
  * row_offsets_dev [n_seq + 1] (may be NULL): where the new positions' rows stand when they are packed in the order of the sequences,
- * the exclusive sum of what was asked for, whether it was got or not; et_kv_append takes it with the kept lengths as its start.
+ * the exclusive sum of what was asked for, whether it was got or not; et_kv_append takes it with the kept lengths as its start, and with
+ * a negative start for a sequence that got none: its rows would go through the entries behind the used ones, whatever those name.
  * slots_dev [rows] (may be NULL with rows = 0): for each of these rows page * page_size + place, the place of its position in the
  * cache, or -1 for a position that was not got and for rows behind the last; rows more than that are left out (ET_PAGED_CAPACITY).
  *

@@ -92,6 +92,26 @@ def test_sequences_grow_behind_a_shared_beginning(B):                           
     assert np.array_equal(r.cpu().numpy(), held)
 
 
+def test_rows_of_a_sequence_that_got_no_place_are_not_written(B):                                # noqa: F811
+    """A sequence asks for more than its table holds; its entries behind the used ones name another one's pages, as they may after a fork.
+    Appended with a negative start, nothing of its rows is stored anywhere."""
+    import torch
+    page, n_pages, kvh, d = 16, 20, 1, 64
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    cache = torch.randn((n_pages, 2, kvh, page, d), device="cuda", generator=gen).to(torch.bfloat16)
+    table = np.array([[3, 9, 4, 11], [8, 2, 3, 9]])                                              # 50 positions; 20, and two old entries
+    refs = np.zeros(n_pages, int)
+    refs[[3, 9, 4, 11, 8, 2]] = 1
+    r, t, keep, add, offsets, status = i32(refs), i32(table), i32([50, 20]), i32([3, 60]), i32([0] * 3), i32([0])
+    new = B.et_pages_update(r, page, t, keep, add=add, row_offsets=offsets, status=status)
+    assert new.tolist() == [53, 20] and status.item() == B.ET_PAGED_CAPACITY
+    qkv = torch.randn((63, 2 * kvh * d), device="cuda", generator=gen).to(torch.bfloat16)
+    want = cache.clone()
+    want[11, :, :, 2:5] = qkv[:3].view(3, 2, kvh, d).permute(1, 2, 0, 3)
+    B.et_kv_append(cache, None, qkv, 0, t, torch.where(new - keep == add, keep, -1), offsets)
+    assert torch.equal(cache, want)
+
+
 # ---- et_pages_fork ----------------------------------------------------------------------------------------------------
 
 def fork_of_low_counts(refs, page, table, lens, parent, new_table):
