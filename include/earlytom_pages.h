@@ -96,7 +96,7 @@ ET_API et_status et_kv_copy(const et_kv_cache* cache, const int* copies_dev, int
  * Out, [n_req * k], best first: parent_dev the row that is continued, token_dev, new_scores_dev fp32, new_done_dev bytes (may be
  * NULL): 1 where the token is eos.  Where there are fewer than k: -1, -1, minus infinity, 1.  eos may be -1 if done_dev is NULL.
  * beams * vocab >= 1; k need not be beams (k = 2 * beams leaves room for those that end; beams = 1 begins a search).
- * The logarithm is off by 2^-20 at most.  Continuations of one beam are in the order of their logits.
+ * The logarithm is off by 2^-20 at most, by 2^-19 of rows whose largest logit is 2^23 or more in magnitude.  Continuations of one beam are in the order of their logits.
  * workspace_dev: ET_BEAM_WORKSPACE(n_req * beams, vocab, k) bytes, 16-byte aligned, as above.
  * Limits (ET_ERR_CAPACITY): beams <= 32, k <= 64, vocab <= 2^20, n_req * beams <= 65535. */
 #define ET_BEAM_CHUNK 4096

@@ -9,13 +9,13 @@
 //     of k threads' maxima above.  In the others: those above the k-th best so far; a lower token comes first among equal ones, so
 //     later equal ones need not be looked at.  What passes goes to a list in shared memory, which is cut back to k entries, in order,
 //     when it is long.
-//   * The sum is a running one against a running maximum, each thread's own; a thread's maximum seldom moves after its first chunk.
-//     Additions and multiplications take two logits at once.
-//   * Scores are compared in 64 bits: a beam's logarithm of its sum is off by a few 2^-24, which the beams have alike or nearly so.
+//   * The sum is a running one against a reference near the running maximum, each thread's own; it seldom moves after a thread's first
+//     chunk.  A chunk's terms are added in fp32, the chunks in 64 bits.  Additions and multiplications take two logits at once.
+//   * Scores are compared in 64 bits.
 //
 // Device time in a chain of calls, B200, logits not in L2 (of the measured copy bandwidth), both kernels: 32 x 8 beams over 152 064,
-// the best 16: fp32 40 us (0.59), bf16 37 (0.32); the best 64 of 64 rows, fp32 40 (0.15); the best 31 of 6 x 4 beams over 194 849 20;
-// 1 x 4 beams, the best 4, bf16 8.4, 8 x 4 14.1 (two launches, a first chunk); 32 x 8 over 32 003, bf16, rows not aligned 18.9 (0.13).
+// the best 16: fp32 42 us (0.57), bf16 40 (0.30); the best 64 of 64 rows, fp32 39 (0.15); the best 31 of 6 x 4 beams over 194 849 20;
+// 1 x 4 beams, the best 4, bf16 9.1, 8 x 4 14.5 (two launches, a first chunk); 32 x 8 over 32 003, bf16, rows not aligned 19.0 (0.13).
 // Instructions bound it, about 230 of a warp for 512 logits: 70 are the arithmetic, the others find candidates and keep the list;
 // the blocks' barrier, one a chunk, is the longest wait.
 #include "decode.cuh"
@@ -53,7 +53,7 @@ struct Select {
   unsigned char* new_done;        // may be NULL
 };
 
-// What a segment leaves: its best k (value, token) in order, (-infinity, -1) behind the last, and (maximum, sum).
+// What a segment leaves: its best k (value, token) in order, (-infinity, -1) behind the last, and its Sum.
 struct Entry { float value; int token; };
 // Floats as whole numbers of the same order, above 0.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -98,10 +98,52 @@ __device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigne
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
   return y;
 }
-__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
   unsigned long long y;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
   return y;
+}
+
+// A sum of powers 2^(LOG2E x), held as total * 2^(LOG2E from - lift): a term is 2^(LOG2E (x - from) + lift), of an exponent that is rounded
+// once.  lift puts the largest term between 2^6 and 2^14, so that those which count, down to 2^-20 of it, have exponents below 16
+// whose rounding is 2^-21 at most.  `from` is 0 and lift a whole number up to logits of 2^23: then x - from is exact and a new reference
+// costs no rounding.  Of larger logits `from` is the largest one when it was set.
+// In units of 2^-24 the logarithm is off by 5.5 (the exponents' rounding), 4 (ex2.approx, 2^-22), 4 (a chunk's sixteen terms; chunks are
+// added in 64 bits) and 2.2 (LOG2E's own rounding, at most 9.7 from the reference): less than 16, 2^-20.  Beyond 2^23 up to three new
+// references count, 4 each (exp2f, two units in the last place): less than 32.  (A running fp32 sum of exponents rounded twice, 40.1 us in
+// place of 42.0 for 32 x 8 beams fp32, is off by up to 2^-16 where logits are equal: its roundings do not cancel.)
+struct Sum { float from, lift; double total; };
+constexpr float LARGE_LOGIT = 8388608.f, LIFT = 7.f, LEEWAY = 4.f;          // LEEWAY: how far above the reference's logit one has to be for a new one
+__device__ __forceinline__ double place_of(const Sum& s) { return s.total == 0. ? -1e300 : (double)LOG2E * s.from - s.lift; }
+// 2^k for k <= 0, 2^-1022 at least; 1 for k > 0, where there is nothing yet that it could count for
+__device__ __forceinline__ double power(int k) { return __hiloint2double((1023 + min(max(k, -1022), 0)) << 20, 0); }
+// total * 2^d, d <= 0
+__device__ __forceinline__ double scaled(double total, double d) {
+  const double k = rint(d);
+  const float f = (float)(d - k);
+  double p = power((int)fmax(k, -1022.));
+  if (f != 0.f) p *= exp2f(f);
+  return total * p;
+}
+// The sums of the first N lanes, added up at the highest reference; the other lanes' are zero.
+template <int N>
+__device__ __forceinline__ void add_lanes(Sum& s) {
+  if (__all_sync(0xffffffffu, s.from == 0.f)) {
+    const int at = s.total == 0. ? -(1 << 30) : -(int)s.lift, top = __reduce_max_sync(0xffffffffu, at);
+    s.total *= power(at - top);
+    s.lift = (float)-top;
+  } else {
+    const double at = place_of(s);
+    double top = at;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const int who = __ffs(__ballot_sync(0xffffffffu, at == top)) - 1;
+    s.from = __shfl_sync(0xffffffffu, s.from, who);
+    s.lift = __shfl_sync(0xffffffffu, s.lift, who);
+    s.total = scaled(s.total, at - top);
+  }
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) s.total += __shfl_xor_sync(0xffffffffu, s.total, o);
 }
 
 // The list's best k keys, in order, to its front; returns how many.  All threads; the list is complete.
@@ -198,7 +240,7 @@ beam_scan_kernel(const __grid_constant__ Select a) {
   __shared__ int added_s[3];                        // keys that a chunk adds, in turn
   __shared__ float group_top[32], thread_top[WARPS][32];
   __shared__ unsigned long long best[2 * WARPS + K_MAX];
-  __shared__ uint2 reduce[WARPS];
+  __shared__ Sum reduce[WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, segment = blockIdx.x, row = blockIdx.y;
   begin_after_previous();
   if (done_of(a, row) || !finite(score_of(a, row))) return;
@@ -258,7 +300,8 @@ beam_scan_kernel(const __grid_constant__ Select a) {
   if (first < last) load(first, raw);
   if (tid < 3) added_s[tid] = 0;
   __syncthreads();
-  float m = -INFINITY, s = 0.f, bar = -INFINITY;    // bar: what a logit has to reach or, behind the first chunk, to pass
+  Sum sum{0.f, 0.f, 0.};
+  float limit = -INFINITY, bar = -INFINITY;         // bar: what a logit has to reach or, behind the first chunk, to pass
   int n = 0, turn = 0;
   bool begun = false;
   for (int at = first; at < last; at += CHUNK) {
@@ -275,19 +318,27 @@ beam_scan_kernel(const __grid_constant__ Select a) {
 #pragma unroll
     for (int i = 0; i < EACH; i += 4) top4[i / 4] = max3(fmaxf(x[i], x[i + 1]), x[i + 2], x[i + 3]);
     top = max3(fmaxf(top4[0], top4[1]), top4[2], top4[3]);
-    if (top > m) { s *= exp2_fast((m - top) * LOG2E); m = top; }
-    const float ref = m == -INFINITY ? 0.f : m;
-    unsigned long long sum[2] = {0, 0};             // two sums each
-    const unsigned long long minus_ref = pair(-ref, -ref), log2e = pair(LOG2E, LOG2E);
-#pragma unroll
-    for (int i = 0; i < EACH; i += 2) {
-      float e0, e1;
-      unpair(mul2(add2(pair(x[i], x[i + 1]), minus_ref), log2e), e0, e1);
-      sum[i / 2 & 1] = add2(sum[i / 2 & 1], pair(exp2_fast(e0), exp2_fast(e1)));
+    if (top > limit) {
+      const Sum old = sum;
+      const bool large = !(fabsf(top) < LARGE_LOGIT);
+      sum.from = large ? top : 0.f;
+      sum.lift = large ? LIFT : LIFT - rintf(top * LOG2E);
+      if (sum.from == 0.f && old.from == 0.f) sum.total *= power((int)(sum.lift - old.lift));
+      else if (old.total != 0.) sum.total = scaled(old.total, place_of(old) - place_of(sum));
+      limit = top + LEEWAY;
     }
+    const unsigned long long minus_from = pair(-sum.from, -sum.from), lift = pair(sum.lift, sum.lift), log2e = pair(LOG2E, LOG2E);
+    auto terms = [&](int i) {                       // two of them
+      float e0, e1;
+      unpair(fma2(add2(pair(x[i], x[i + 1]), minus_from), log2e, lift), e0, e1);
+      return pair(exp2_fast(e0), exp2_fast(e1));
+    };
+    unsigned long long four[EACH / 4];
+#pragma unroll
+    for (int i = 0; i < EACH; i += 4) four[i / 4] = add2(terms(i), terms(i + 2));
     float s0, s1;
-    unpair(add2(sum[0], sum[1]), s0, s1);
-    s += s0 + s1;
+    unpair(add2(add2(four[0], four[1]), add2(four[2], four[3])), s0, s1);
+    sum.total += (double)(s0 + s1);
     if (!begun) {
       if (a.k <= FEW) {
         // the k-th largest of the maxima of 32 groups of eight threads
@@ -334,22 +385,13 @@ beam_scan_kernel(const __grid_constant__ Select a) {
   n = cut_back(list, n, a.k, best);
   unsigned char* const out = segment_of(a, row, segment);
   if (tid < a.k) reinterpret_cast<Entry*>(out)[tid] = tid < n ? entry_of(list[tid]) : Entry{-INFINITY, -1};
-  float big = m;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-  s *= m == big ? 1.f : exp2_fast((m - big) * LOG2E);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if (lane == 0) reduce[warp] = make_uint2(__float_as_uint(big), __float_as_uint(s));
+  add_lanes<32>(sum);
+  if (lane == 0) reduce[warp] = sum;
   __syncthreads();
-  if (tid == 0) {
-    for (int w = 0; w < WARPS; ++w) big = fmaxf(big, __uint_as_float(reduce[w].x));
-    float all = 0.f;
-    for (int w = 0; w < WARPS; ++w) {
-      const float mw = __uint_as_float(reduce[w].x);
-      all += __uint_as_float(reduce[w].y) * (mw == big ? 1.f : exp2_fast((mw - big) * LOG2E));
-    }
-    *reinterpret_cast<float2*>(out + 8 * (size_t)a.k) = make_float2(big, all);
+  if (warp == 0) {
+    sum = lane < WARPS ? reduce[lane] : Sum{0.f, 0.f, 0.};
+    add_lanes<WARPS>(sum);
+    if (lane == 0) *reinterpret_cast<Sum*>(out + 8 * (size_t)a.k) = sum;
   }
 }
 
@@ -357,24 +399,27 @@ beam_scan_kernel(const __grid_constant__ Select a) {
 template <int EACH, class Put>
 __device__ __forceinline__ int merge_lists(const Select& a, int row, Put put) {
   const int lane = threadIdx.x & 31;
-  auto load = [&](int segment, unsigned long long (&key)[EACH]) {
+  auto load = [&](int segment, float2 (&v)[EACH]) {
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
       const int e = lane + 32 * j;
-      float2 v = make_float2(-INFINITY, 0.f);
-      if (e < a.k && segment < a.segments) v = __ldcg(reinterpret_cast<const float2*>(segment_of(a, row, segment)) + e);
-      key[j] = v.x > -INFINITY ? key_of(v.x, __float_as_int(v.y)) : 0;
+      v[j] = make_float2(-INFINITY, 0.f);
+      if (e < a.k && segment < a.segments) v[j] = __ldcg(reinterpret_cast<const float2*>(segment_of(a, row, segment)) + e);
     }
   };
-  unsigned long long best[EACH], next[EACH], after[EACH];
-  load(0, best);
+  auto key = [](const float2& v) { return v.x > -INFINITY ? key_of(v.x, __float_as_int(v.y)) : 0ull; };
+  unsigned long long best[EACH];
+  float2 first[EACH], next[EACH], after[EACH];
+  load(0, first);
   load(1, next);
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) best[j] = key(first[j]);
   for (int segment = 1; segment < a.segments; ++segment) {
-    load(segment + 1, after);
+    load(segment + 1, after);                       // (as it is: its key is formed an iteration later, when it is there)
     // the first of the one list with the last of the other: the larger ones are the best of both, and go up and down at most once
     unsigned long long x[EACH];
 #pragma unroll
-    for (int j = 0; j < EACH; ++j) x[j] = __shfl_sync(0xffffffffu, next[EACH - 1 - j], 31 - lane);
+    for (int j = 0; j < EACH; ++j) x[j] = __shfl_sync(0xffffffffu, key(next[EACH - 1 - j]), 31 - lane);
 #pragma unroll
     for (int j = 0; j < EACH; ++j) if (x[j] > best[j]) best[j] = x[j];
     if (EACH == 2 && best[EACH - 1] > best[0]) { const unsigned long long y = best[0]; best[0] = best[EACH - 1]; best[EACH - 1] = y; }
@@ -424,7 +469,8 @@ beam_join_kernel(const __grid_constant__ Select a) {
     constexpr int AHEAD = 4;
     const bool few = a.segments * k <= 64 * AHEAD;
     auto list_of = [&](int segment) { return reinterpret_cast<const float2*>(segment_of(a, row, segment)); };
-    float2 part[2], e[2][AHEAD];
+    Sum part[2];
+    float2 e[2][AHEAD];
     auto load = [&](int i, int first) {
 #pragma unroll
       for (int p = 0; p < AHEAD; ++p)
@@ -442,7 +488,11 @@ beam_join_kernel(const __grid_constant__ Select a) {
       reach[t] = tried && (t == 0 || each > 1) && lane < lists && each + t <= k ? __ldcg(list_of(lane) + each + t - 1).x : -INFINITY;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      part[i] = lane + 32 * i < a.segments ? __ldcg(list_of(lane + 32 * i) + k) : make_float2(-INFINITY, 0.f);
+      part[i] = Sum{0.f, 0.f, 0.};
+      if (lane + 32 * i < a.segments) {
+        const float2 reference = __ldcg(list_of(lane + 32 * i) + k);
+        part[i] = Sum{reference.x, reference.y, __ldcg(reinterpret_cast<const double*>(list_of(lane + 32 * i) + k + 1))};
+      }
       if (!few) { load(i, 0); continue; }
 #pragma unroll
       for (int p = 0; p < AHEAD; ++p) {
@@ -474,21 +524,20 @@ beam_join_kernel(const __grid_constant__ Select a) {
       }
     }
     __syncwarp();
-    float big = fmaxf(part[0].x, part[1].x);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-    double sum = 0.;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) sum += part[i].y * (part[i].x == big ? 1.f : expf(part[i].x - big));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    const double base = (double)score - ((double)big + log(sum));
+    add_lanes<32>(part[0]);
+    if (a.segments > 32) {
+      add_lanes<32>(part[1]);
+      const double d = place_of(part[1]) - place_of(part[0]);
+      if (d > 0.) part[0] = Sum{part[1].from, part[1].lift, part[1].total + scaled(part[0].total, -d)};
+      else part[0].total += scaled(part[1].total, d);
+    }
+    const double base = (double)score - ((double)part[0].from + (log(part[0].total) - (double)part[0].lift * (1. / LOG2E)));
     auto put = [&](int rank, unsigned long long key) {
       const Entry e = entry_of(key);
       mine[rank] = base + (double)e.value;
       tokens[beam * k + rank] = e.token;
     };
-    if (!finite(big) || !(base >= -1.7e308 && base <= 1.7e308)) {
+    if (!(base >= -1.7e308 && base <= 1.7e308)) {       // no token, NaN or an infinity
     } else if (n <= NEAR) {
       for (int e = lane; e < n; e += 32) {
         const unsigned long long key = near[e];

@@ -1,5 +1,7 @@
 """Pages of the cache and beam search (include/earlytom_pages.h) where numbers, counts and orders are unlucky: against the plain
 implementations of test_gpu_pages.py, with buffers between guards."""
+import math
+
 import numpy as np
 import pytest
 
@@ -184,3 +186,108 @@ def test_fork_with_counts_that_are_too_low(B, wide):                            
         assert status.item() == 7
         copied, fresh = want[3][want[3][:, 0] >= 0, 0], want[3][want[3][:, 0] >= 0, 1]
         assert not set(copied) & set(fresh)
+
+
+# ---- et_beam_select: rows of many chunks, a block each ------------------------------------------------------------------
+# From 592 rows on a block walks a whole row, 4 096 logits at a time.
+
+def many_rows(patterns, dtype, rows=600):
+    """`rows` rows on the GPU, patterns one after the other and over again."""
+    import torch
+    x = torch.empty((rows, len(patterns[0])), dtype=dtype, device="cuda")
+    for i, y in enumerate(patterns):
+        x[i::len(patterns)] = y.to(dtype)
+    return x
+
+
+def check_many(B, patterns, k, dtype, accurate=None):                                            # noqa: F811
+    """Each row's best k, in order, and their scores against 64 bits; equal rows have equal results, bit by bit."""
+    import torch
+    rows, n = 600, len(patterns)
+    x = many_rows(patterns, dtype, rows)
+    parent, token, score, done = (t.view(rows, k) for t in B.et_beam_select(x, 1, k))
+    assert not (done & (parent >= 0)).any()
+    for i in range(n):
+        y = x[i].double()
+        # in descending order, equal ones by their tokens: sort() is stable
+        order = torch.sort(y, descending=True, stable=True).indices[:k]
+        live = y[order] > -math.inf
+        if not math.isfinite(torch.logsumexp(y, 0).item()):
+            live[:] = False
+        want = torch.where(live, order, -1).int()
+        want = torch.cat([want, want.new_full((k - len(want),), -1)])
+        assert (token[i::n] == want).all(), i
+        assert (parent[i::n] == torch.where(want >= 0, torch.arange(i, rows, n, device="cuda").unsqueeze(1), -1)).all(), i
+        assert (score[i::n] == score[i]).all() and (done[i::n] == (want < 0)).all(), i
+        got = (want >= 0).sum().item()
+        value = y[order[:got]] - torch.logsumexp(y, 0)
+        bound = 2.0 ** -20 if y.abs().max() < 2 ** 23 or accurate is None else accurate
+        assert ((score[i, :got].double() - value).abs() <= bound + 2.0 ** -24 * value.abs()).all(), i
+        assert (score[i, got:] == -math.inf).all()
+
+
+@pytest.mark.parametrize("fp32", [True, False])
+@pytest.mark.parametrize("k", [1, 20, 33, 64])
+@pytest.mark.parametrize("vocab", [9 * 4096 + 55, 10 * 4096, 31 * 4096 + 4])
+def test_select_of_unlucky_orders_in_long_rows(B, vocab, k, fp32):                               # noqa: F811
+    """What floods the list behind the first chunk: rising logits, each chunk above the last, values that are equal across chunks' ends, a
+    bar that only the next chunks' equals reach."""
+    import torch
+    i = torch.arange(vocab, device="cuda").float()
+    gen = torch.Generator(device="cuda").manual_seed(k)
+    noise = torch.randn(vocab, device="cuda", generator=gen)
+    patterns = [i / 512, -i / 512, torch.full_like(i, 0.3), i * 7919 % 3, torch.div(i, 4096, rounding_mode="floor"), -torch.div(i, 4096, rounding_mode="floor"),
+                torch.div(i + 2048, 4096, rounding_mode="floor"), torch.where(i % 4096 < 4096 - k, -5.0, 1.0), torch.where(i % 4096 > 4090, 2.0, noise),
+                torch.where(i < 2 * 4096, i / 4096, 2.0 - 1e-4 * (i % 3)), noise + i / 20_000, torch.where(i > vocab - 20, 9.0, -9.0), noise * 1000,
+                torch.where((i % 4096 // 4 % 256) < 8, 50 + i / 1000, -i / 100)]
+    if not fp32:
+        patterns = [y * 4 for y in patterns]
+    check_many(B, patterns, k, torch.float32 if fp32 else torch.bfloat16)
+
+
+@pytest.mark.parametrize("fp32", [True, False])
+def test_select_of_long_rows_that_are_not_finite(B, fp32):                                       # noqa: F811
+    """Banned tokens in whole chunks, infinities and NaN in the first chunk, a middle one and the last one."""
+    import torch
+    vocab, inf = 12 * 4096 + 7, math.inf
+    i = torch.arange(vocab, device="cuda")
+    y = torch.randn(vocab, device="cuda")
+    patterns = [y, torch.where(i < 4096, -inf, y), torch.where(i >= 4096, -inf, y), torch.where(i // 4096 % 2 == 0, -inf, y), torch.where(i < vocab - 3, -inf, y),
+                torch.full_like(y, -inf), torch.where(i % 4096 == 4095, y, -inf)]
+    for at in (5, 6 * 4096 + 100, vocab - 1):
+        patterns += [torch.where(i == at, math.nan, y), torch.where(i == at, inf, y), torch.where(i == at, -inf, y), torch.where(i == at, 3e38, y),
+                     torch.where(i == at, -3e38, y)]
+    for k in (3, 64):
+        check_many(B, patterns, k, torch.float32 if fp32 else torch.bfloat16)
+
+
+def sums_patterns(vocab):
+    """Rows whose terms round alike: one token, or one of each thread, above equal ones that weigh as much together; rising ones; large
+    offsets."""
+    import torch
+    i = torch.arange(vocab, device="cuda").double()
+    one, first = i == vocab // 3, (i < 1024) & (i % 4 == 0)
+    got = [torch.where(one, 0, -t) for t in (3.1, 7.77, 9.7, 11.1, 11.46, 12.7, 13.6, 13.75, 13.86)]
+    got += [torch.where(first, 0, -t) for t in (3.3, 6.1, 8.3, 11.46)]
+    got += [torch.where(one, 0.3, -t) for t in (8.05, 11.2, 13.3)] + [torch.full_like(i, c) for c in (0.1234, -77.7, 1000.1, 40_000.3, -705.2, -706.0, -3543.3)]
+    got += [i * 2e-6, i * 1e-4, -i * 2e-6, 5e-8 * i + 1, torch.floor(i / 4096) * 3.9, torch.floor(i / 4096) * 0.7, torch.sin(i) * 3, torch.cos(i * i) * 9 + 700]
+    got += [torch.where(one, 0, -t) + c for t in (8.3, 11.46) for c in (17.3, -511.9, 4095.3, 70_000.0)]
+    return got
+
+
+@pytest.mark.parametrize("vocab,fp32", [(152_064, True), (152_064, False), (40_003, True), (600_000, True), (1 << 20, True)])
+def test_select_accurate_sums_of_long_rows(B, vocab, fp32):                                      # noqa: F811
+    """The logarithm within the documented 2^-20 where a thread adds up the terms of 10 to 256 chunks."""
+    import torch
+    check_many(B, sums_patterns(vocab), 2, torch.float32 if fp32 else torch.bfloat16)
+
+
+def test_select_accurate_sums_of_large_logits(B):                                                # noqa: F811
+    """Beyond 2^23 logits are whole numbers at least, and the logarithm is within 2^-19."""
+    import torch
+    vocab = 152_064
+    i = torch.arange(vocab, device="cuda").double()
+    chunk = torch.floor(i / 4096)
+    patterns = [2.0 ** 23 + i % 3, 2.0 ** 23 + chunk * 5, -2.0 ** 24 + 2 * chunk, torch.where(i == 99_000, 2.0 ** 23 + 12, 2.0 ** 23), 2.0 ** 23 - 30 + chunk,
+                -2.0 ** 23 + chunk, 1e30 + 0 * i, torch.where(chunk > 20, 2.0 ** 23, -1e30), -3e38 + i * 1e33, torch.where(chunk < 9, -2.0 ** 25, chunk)]
+    check_many(B, patterns, 5, torch.float32, accurate=2.0 ** -19)
