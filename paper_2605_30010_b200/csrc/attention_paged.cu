@@ -592,6 +592,7 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
       // ---- Q^T as the B operand: column gq = head, two rows (pairs of dimensions) a register
       uint32_t q[NT][KS][2];
       float qscale[NT][2];                                           // of heads 2 tq and 2 tq + 1
+      [[maybe_unused]] bool any_far = false;
       // 4 bits: -8 times the sum of a block's queries, for each of a head's blocks, as the sum of three bf16: the B operand for an A of the
       // positions' scales, [hi | middle | low] x blocks along k
       uint32_t eights[NT][2];
@@ -671,9 +672,13 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                 eights[n][1] = 0u;
               }
             }
-            const float back = pow2(e) * (INT4 ? softmax_scale * 0x1p24f : softmax_scale);
+            // (4 bits: 2^e times the codes' 2^24 may not be a float where queries reach 2^121.  Such a head's factor is 2^8 less, and
+            // negative, which tells the tiles to multiply its scores by that beforehand.)
+            const bool far = INT4 && e > 106;
+            const float back = pow2(e) * (far ? softmax_scale * -0x1p16f : INT4 ? softmax_scale * 0x1p24f : softmax_scale);
             qscale[n][0] = __shfl_sync(0xffffffffu, back, 8 * tq);
             qscale[n][1] = __shfl_sync(0xffffffffu, back, 8 * tq + 4);
+            if (INT4) any_far |= __any_sync(0xffffffffu, far);
           }
         }
       }
@@ -750,6 +755,13 @@ attention_paged_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                 }
               }
             }
+            if (any_far)
+#pragma unroll
+              for (int j = 0; j < BLOCKS; ++j)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) s[j][n][i] *= qscale[n][i & 1] < 0.f ? -0x1p8f : 1.f;
           } else if constexpr (BF16) {
 #pragma unroll
             for (int k = 0; k < KS; ++k)
