@@ -38,7 +38,9 @@ enum { ET_PAGED_NO_PAGE = 6, ET_PAGED_BAD_COUNT = 7, ET_PAGED_BAD_ROW = 8 };
  * by one and the entries become -1.  Then entries up to ceil((keep + add) / page_size) - 1 are taken: free pages (those that have just
  * become free among them), whose counts become 1.  The taken pages are numbered by sequence, then by entry; the i-th is the free page
  * with i smaller ones.  A sequence whose last one there is no free page for gets no position (status ET_PAGED_NO_PAGE; its entries
- * become -1), nor does one whose positions the table cannot hold (ET_PAGED_CAPACITY; it takes no pages).
+ * become -1), nor does one whose positions the table cannot hold (ET_PAGED_CAPACITY; it takes no pages).  The numbers of pages that
+ * were not to be had are not given to the sequences behind: those that need a page get none either, so one request for more than
+ * there is belongs into a call of its own, or behind the others.
  *
  * The new positions begin in the last kept page if that one is not full, and then it has to be the sequence's own: nothing is copied and
  * no other page taken in its place, so two sequences that hold it would get the same places in it, and no status says so.  Where others
@@ -94,9 +96,11 @@ ET_API et_status et_kv_copy(const et_kv_cache* cache, const int* copies_dev, int
  * comes first.  Continuations at minus infinity are none: a row whose score or whose logits' sum is not finite has none.
  *
  * Out, [n_req * k], best first: parent_dev the row that is continued, token_dev, new_scores_dev fp32, new_done_dev bytes (may be
- * NULL): 1 where the token is eos.  Where there are fewer than k: -1, -1, minus infinity, 1.  eos may be -1 if done_dev is NULL.
+ * NULL): 1 where the token is eos.  Where there are fewer than k: -1, -1, minus infinity, 1.  (A score below fp32's range is
+ * put out as minus infinity.)  eos may be -1 if done_dev is NULL.
  * beams * vocab >= 1; k need not be beams (k = 2 * beams leaves room for those that end; beams = 1 begins a search).
- * The logarithm is off by 2^-20 at most, by 2^-19 of rows whose largest logit is 2^23 or more in magnitude.  Continuations of one beam are in the order of their logits.
+ * The logarithm is off by 2^-20 at most, by 2^-19 of rows whose largest logit is 2^23 or more in magnitude.  Continuations of one beam
+ * are in the order of their logits.
  * workspace_dev: ET_BEAM_WORKSPACE(n_req * beams, vocab, k) bytes, 16-byte aligned, as above.
  * Limits (ET_ERR_CAPACITY): beams <= 32, k <= 64, vocab <= 2^20, n_req * beams <= 65535. */
 #define ET_BEAM_CHUNK 4096

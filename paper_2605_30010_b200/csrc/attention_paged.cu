@@ -36,7 +36,9 @@
 // of 128 on 16, one of 180 000, bf16 219 / 221 us (1.04), e4m3 116 / 121 us (0.99 / 0.95); 24 ragged up to 2 049, 16 heads of 64, bf16
 // 22 / 21 us (0.51 / 0.54), e4m3 the same (0.27): short items; 16 heads to a key / value head, 64 ragged, bf16 105 / 110 us (0.88 /
 // 0.85), e4m3 71 / 74 us (0.66 / 0.64: bound by conversions and exponentials).  4 bits, 28 heads on 4 of 128: one sequence of 100 003
-// 24.5 us (0.36), 64 ragged up to 16 001 64 us (0.47; its copies without arithmetic take 37, its arithmetic without copies 62).
+// 24.5 us (0.36), 64 ragged up to 16 001 64 us (0.47; its copies without arithmetic take 37, its arithmetic without copies 62); 64 heads
+// on 4 97 us (0.31; with 16 heads of 128 a thread spills 82 bytes).  The same batches as bf16 110 and 118 us, as e4m3 64 and 82: what 4
+// bits save over e4m3 is memory, not time.
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
@@ -87,7 +89,8 @@ struct Cfg {
   // What an item costs beside its tiles, in tiles' worth of time (measured: 2.3 us beside 0.6 us a tile for bf16 rows of 128, 2.0
   // and 0.3 for e4m3 ones, 1.4 and 0.25 for bf16 rows of 64; with 16 heads 2.8 and 0.65, 3.7 and 0.4; e4m3 rows of 64 follow the
   // same formula unmeasured); an item that a group takes alone costs a good third of it.  A tile of 4 bits takes as long as its
-  // arithmetic, whatever its bytes: 64 ragged sequences 65.8, 65.0, 63.8, 64.6, 67.0 us at costs of 4, 6, 8, 10 and 13 for 8 heads.
+  // arithmetic, whatever its bytes: 64 ragged sequences 65.8, 65.0, 63.8, 64.6, 67.0 us at costs of 4, 6, 8, 10 and 13 for 8 heads; with
+  // 16 heads 103, 96.4, 95.6, 97.6, 99.4 and 100 at 6, 8, 10, 12 (the formula's), 14 and 16.
   static constexpr int PER_TILE = FMT == ET_KV_INT4 ? 6 : 65536 / STAGE;
   static constexpr int COST = (2 + PER_TILE) * (NT + 1) / 2, COST_SHORT = NT == 1 ? 1 + PER_TILE / 2 : COST;
   static constexpr int SCALES = 2 * TILE * kv_scale_bytes(FMT, DH);

@@ -28,7 +28,8 @@ namespace {
 constexpr int THREADS = 256, WARPS = THREADS / 32, EACH = 16, CHUNK = THREADS * EACH;
 static_assert(CHUNK == ET_BEAM_CHUNK, "workspace");
 static_assert(EACH == 16, "four groups of four");
-constexpr int BLOCKS_SM = 4;                         // resident: 64 registers a thread (an unaligned row's loads take 80: 23 for 19 us)
+// Resident: 64 registers a thread (an unaligned row's loads take 80: 23 for 19 us; of fp32 rows they spill 168 bytes).
+constexpr int BLOCKS_SM = 4;
 constexpr int K_MAX = 64, BEAMS_MAX = 32, SEGMENTS_MAX = 64;
 // The list is cut back when it has more than so many keys; a chunk adds CHUNK at most.  With k more than the best k the bar follows the
 // segment in four or five steps, and a chunk adds few keys.

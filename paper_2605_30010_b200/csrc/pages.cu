@@ -10,11 +10,11 @@
 //     its share of the sequences and of the counts, totals go round through distributed shared memory.
 //   * Work of uneven sequences is dealt to threads entry by entry: a prefix sum over the sequences, and a search in it.
 //
-// Device time in a chain of calls, B200: et_pages_update, a few more positions for 64 sequences, 12 400 pages 8.7 us (a cluster's
+// Device time in a chain of calls, B200: et_pages_update, a few more positions for 64 sequences, 12 400 pages 8.3 us (a cluster's
 // launch, four rounds of loads that wait for one another, three barriers); 700 prompts of up to 240 pages in place of others, 116 000
-// pages 16 us, with their 2.1 million slots 25 (searches, and entries all over the tables).  et_pages_fork, 4 rows of
-// tables of 123 entries 6.6 us, 256 rows of 52 9.9.  et_kv_copy, 2 half-filled pages of 4 + 4 heads of 128 1.9 us, 98 of them, bf16,
-// 980 positions 3.0.
+// pages, with their 2.1 million slots 30.6 (searches, and entries all over the tables; 25 where tables are in L2, without slots 16).
+// The figures at the rules below are of tables in L2.  et_pages_fork, 4 rows of tables of 123 entries 6.6 us, 256 rows of 52 9.9.
+// et_kv_copy, 2 half-filled pages of 4 + 4 heads of 128 1.7 us, 98 of them, bf16, 980 positions 3.0: a launch each.
 #include <atomic>
 
 #include "decode.cuh"
@@ -462,7 +462,7 @@ fork_rows_kernel(const __grid_constant__ Fork f) {
 
 // The same in the cluster below, a warp each old row, where rows are few and a row is one round of a warp's loads: a launch less, 2.6 us of
 // the host's time a call, for up to 2 us of the device's (4 rows of 123 entries 6.8 us in place of 6.2, 64 of 52 8.4 of 7.1, 256 9.9 of 7.9);
-// longer rows are left to the other kernel (16 of 481: 14.9 us here, 7.5 there).
+// longer rows are left to the other kernel (16 of 481: 14.9 us here, 7.9 there).
 constexpr int FORK_FEW = 256, FORK_COLUMNS = 32 * AHEAD;
 __device__ __forceinline__ void fork_row(const Fork& f, int p, unsigned short* children) {
   const int lane = threadIdx.x & 31;
