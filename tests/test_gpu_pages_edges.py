@@ -114,6 +114,54 @@ def test_rows_of_a_sequence_that_got_no_place_are_not_written(B):               
     assert torch.equal(cache, want)
 
 
+@pytest.mark.parametrize("n_pages,page", [((1 << 27) - 1, 16), ((1 << 24) - 1, 128)])
+def test_update_of_the_largest_pools(B, n_pages, page):                                          # noqa: F811
+    """As many pages as slots can name, the free ones far apart and at the very end."""
+    import torch
+    refs = torch.ones(n_pages, dtype=torch.int32, device="cuda")
+    free = sorted({0, 77, n_pages // 3, n_pages - 1, n_pages - 2, n_pages - 40_000, n_pages // 2 + 1})
+    refs[free] = 0
+    table, lens, status = i32(np.full((3, 4), -1)), i32([0, 0, 0]), i32([0])
+    add, slots = i32([2 * page, page + 1, 3 * page - 2]), i32([-9] * (6 * page - 1))
+    new = B.et_pages_update(refs, page, table, lens, add=add, slots=slots, status=status)
+    assert status.item() == 0 and new.tolist() == add.tolist() and not (refs == 0).any() and not (refs != 1).any()
+    assert table.tolist() == [free[:2] + [-1, -1], free[2:4] + [-1, -1], free[4:] + [-1]]
+    want = [p * page + t for entries, n in zip((free[:2], free[2:4], free[4:]), add.tolist()) for p, t in
+            [(entries[i // page], i % page) for i in range(n)]]
+    assert slots.tolist() == want
+
+
+def test_update_of_the_longest_table(B):                                                         # noqa: F811
+    """2^30 positions are given back and as many taken, each with its slot."""
+    import torch
+    page, columns = 128, 1 << 23
+    n_pages, cap = columns + 5, 1 << 30
+    refs = torch.ones(n_pages, dtype=torch.int32, device="cuda")
+    refs[-5:] = 0
+    table = torch.arange(columns - 1, -1, -1, dtype=torch.int32, device="cuda").view(1, -1)
+    status, slots = i32([0]), torch.full((cap,), -9, dtype=torch.int32, device="cuda")
+    new = B.et_pages_update(refs, page, table, i32([cap]), keep=i32([0]), add=i32([cap]), slots=slots, status=status)
+    assert status.item() == 0 and new.tolist() == [cap]
+    assert torch.equal(table[0], torch.arange(columns, dtype=torch.int32, device="cuda"))
+    assert torch.equal(slots, torch.arange(cap, dtype=torch.int32, device="cuda"))
+    assert (refs[:columns] == 1).all() and (refs[columns:] == 0).all()
+
+
+@pytest.mark.parametrize("first", [1, 2, 3])
+@pytest.mark.parametrize("rows", [2_000, 40_001])
+def test_update_into_slots_that_begin_anywhere(B, rows, first):                                  # noqa: F811
+    import torch
+    rng = np.random.default_rng(rows + first)
+    lens, table, refs = random_state(rng, 40, 3000, 32, 2000)
+    add = np.minimum(rng.integers(0, 900, 40), table.shape[1] * 32 - np.maximum(lens, 0))
+    want = update_reference(refs, 32, table, lens, None, add, rows)
+    wide = torch.full((rows + 8,), -77, dtype=torch.int32, device="cuda")
+    B.et_pages_update(i32(refs), 32, i32(table), i32(lens), add=i32(add), slots=wide[first:first + rows])
+    got, n = wide.cpu().numpy(), len(want[4])
+    assert np.array_equal(got[first:first + n], want[4]) and (got[first + n:first + rows] == -1).all()
+    assert (got[:first] == -77).all() and (got[first + rows:] == -77).all()
+
+
 # ---- et_pages_fork ----------------------------------------------------------------------------------------------------
 
 def fork_of_low_counts(refs, page, table, lens, parent, new_table):
@@ -291,3 +339,55 @@ def test_select_accurate_sums_of_large_logits(B):                               
     patterns = [2.0 ** 23 + i % 3, 2.0 ** 23 + chunk * 5, -2.0 ** 24 + 2 * chunk, torch.where(i == 99_000, 2.0 ** 23 + 12, 2.0 ** 23), 2.0 ** 23 - 30 + chunk,
                 -2.0 ** 23 + chunk, 1e30 + 0 * i, torch.where(chunk > 20, 2.0 ** 23, -1e30), -3e38 + i * 1e33, torch.where(chunk < 9, -2.0 ** 25, chunk)]
     check_many(B, patterns, 5, torch.float32, accurate=2.0 ** -19)
+
+
+@pytest.mark.parametrize("n_req,beams,k,vocab", [(65_535, 1, 3, 37), (2_047, 32, 16, 5), (900, 2, 64, 5_001)])
+def test_select_of_the_most_rows(B, n_req, beams, k, vocab):                                     # noqa: F811
+    """Against a sort of all continuations in 64 bits, where no two are near one another."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    x = torch.randn((n_req * beams, vocab), device="cuda", generator=gen) * 3
+    scores = torch.randn(n_req * beams, device="cuda", generator=gen)
+    parent, token, score, done = (t.view(n_req, k) for t in B.et_beam_select(x, beams, k, scores=scores))
+    total = (torch.log_softmax(x.double(), 1) + scores.double().unsqueeze(1)).view(n_req, -1)
+    best, at = torch.sort(total, dim=1, descending=True, stable=True)
+    n = min(k, beams * vocab)
+    clear = torch.ones((n_req, n), dtype=torch.bool, device="cuda")
+    gaps = best[:, :-1] - best[:, 1:] > 2.0 ** -18
+    clear[:, :min(n, gaps.shape[1])] &= gaps[:, :n]
+    clear[:, 1:] &= gaps[:, :n - 1]
+    first = torch.arange(n_req, device="cuda").unsqueeze(1) * beams
+    assert clear.float().mean() > 0.98
+    assert (token[:, :n] == at[:, :n] % vocab)[clear].all() and (parent[:, :n] == first + at[:, :n] // vocab)[clear].all()
+    assert ((score[:, :n].double() - best[:, :n]).abs() <= 2.0 ** -20 + 2.0 ** -24 * best[:, :n].abs()).all()
+    assert (token[:, n:] == -1).all() and (score[:, n:] == -math.inf).all() and not done[:, :n].any()
+
+
+def test_calls_at_the_same_time(B):                                                              # noqa: F811
+    """The same calls over two states on two streams at once, with a workspace each: as one after the other."""
+    import torch
+    rng = np.random.default_rng(8)
+    states = [random_state(rng, n, 900, 16, 9000) for n in (700, 90)]
+    logits = [torch.randn((r, 20_011), device="cuda") for r in (64, 300)]
+
+    def calls(state, x, stream):
+        lens, table, refs = state
+        with torch.cuda.stream(stream):
+            r, t, n, status = i32(refs), i32(table), i32(lens), i32([0])
+            other = i32(np.full((2 * len(lens), table.shape[1]), -1))
+            parent = i32(np.arange(2 * len(lens)) // 2)
+            got = []
+            for _ in range(6):
+                n = B.et_pages_update(r, 16, t, n, status=status, stream=stream)
+                got += [n, *B.et_beam_select(x, 2, 9, stream=stream)]
+            got += [*B.et_pages_fork(r, 16, t, n, parent, other, status=status, stream=stream), r, t, other, status]
+        return got
+
+    one = torch.cuda.current_stream()
+    want = [calls(s, x, one) for s, x in zip(states, logits)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+        got = [calls(s, x, stream) for s, x, stream in zip(states, logits, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, w in zip(got, want) for a, b in zip(g, w))
